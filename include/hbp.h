@@ -134,7 +134,7 @@ typedef enum { HBP_POST_NONE = 0, HBP_POST_RELU = 1, HBP_POST_RMS = 2 } hbp_post
  * gamma around 0.5 .. 0.8. */
 
 typedef struct {
-  uint32_t struct_size;      /* = sizeof(hbp_desc) */
+  uint32_t struct_size;      /* = sizeof(hbp_desc), or sizeof(hbp_transformer_desc) where this is its base */
   int32_t kind;              /* hbp_kind   */
   int32_t dtype;             /* hbp_dtype  */
   int32_t act;               /* hbp_act    */
@@ -310,6 +310,107 @@ hbp_status hbp_optimizer_step(const hbp_desc* desc, hbp_buffers* bufs, const hbp
 hbp_status hbp_train_step(const hbp_desc* desc, int k, hbp_buffers* bufs, const void* target, float* loss_out,
                           const hbp_optim* opt, hbp_optim_state* state, void* stream);
 
+/* ---- a language model's attention sub-block: rotary positions, attention with shared key/value heads ------------
+ * Operators on tensors of the caller's own, and what HBP_TRANSFORMER takes of them (hbp_transformer_desc below).  The
+ * conventions above hold: caller-owned device memory, storage type fp32 or bf16, everything enqueued on `stream`,
+ * nothing allocated or synchronised, errors found before anything is launched, calls may be captured into graphs. */
+
+/* Rows of heads: channel c of head h of row n is element data[n row_stride + h head_stride + c] of the storage type.
+ * data is 16-byte aligned, strides are multiples of 8, not negative, rows less than 2^24 apart (the stride of a single row or
+ * head does not matter); rows or heads of a tensor that is written must not overlap, those of an input may (a stride of
+ * 0 reads one row again and again).  q, k and v may so lie side by side in the rows of one projection's output, or head after head. */
+typedef struct { void* data; int64_t row_stride, head_stride; } hbp_heads;
+
+/* Rotary positions: channel pair i < dims / 2 of every head of a row at position p turns by the angle p f_i,
+ *   (a, b) -> magnitude (a cos p f_i - b sin p f_i,  a sin p f_i + b cos p f_i).
+ * HALF: the pair is channels i and i + dims / 2; INTERLEAVED: channels 2i and 2i + 1.  Channels from dims on are copied.
+ * f_i = base^(-2 i / dims), for contexts longer than those trained on changed by `factor` s:
+ *   LINEAR    f_i / s
+ *   BASE      base replaced by base s^(dims / (dims - 2))
+ *   BY_PARTS  f_i (w + (1 - w) / s), w = (original f_i / (2 pi) - low) / (high - low) within 0 .. 1: pairs that turn at
+ *             least `high` times within `original` positions stay, those that turn at most `low` times are slowed by s.
+ * Angles are formed and reduced in 64 bits, so that far positions turn as exactly as near ones. */
+typedef enum { HBP_ROTARY_HALF = 0, HBP_ROTARY_INTERLEAVED = 1 } hbp_rotary_layout;
+typedef enum { HBP_ROTARY_PLAIN = 0, HBP_ROTARY_LINEAR = 1, HBP_ROTARY_BASE = 2, HBP_ROTARY_BY_PARTS = 3 } hbp_rotary_scaling;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_rotary_desc) */
+  int32_t layout;            /* hbp_rotary_layout */
+  int32_t scaling;           /* hbp_rotary_scaling */
+  int32_t dims;              /* channels of a head that turn: even, 2 .. dh (BASE: 4 .. dh) */
+  float magnitude;           /* finite; 1 for a plain rotation */
+  float reserved;            /* 0 */
+  double base;               /* > 0 */
+  double factor;             /* > 0; unused with PLAIN */
+  double low, high;          /* BY_PARTS: low < high */
+  double original;           /* BY_PARTS: > 0 */
+} hbp_rotary_desc;
+
+/* out := x turned (inverse = 0), or turned back by the same angles, times the same magnitude (inverse = 1): the
+ * transpose, which takes a gradient with respect to `out` to the one with respect to `x`.  x and out: `rows` rows of
+ * `heads` heads of dh channels (dh a multiple of 8, at most 256), in the storage type `dtype`; out may be x itself (same
+ * data and strides), and must not overlap it otherwise.  positions: DEVICE, one int32 per row, or NULL: row n is at
+ * first + n (period = 0) or first + n mod period.  rows = 0 does nothing. */
+hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, int heads, int dh, const hbp_heads* x,
+                      const hbp_heads* out, const int32_t* positions, int64_t first, int64_t period, int inverse, void* stream);
+
+/* Attention over packed sequences.  Query heads h = 0 .. heads - 1 read key/value head h / (heads / kv_heads).  Sequence s
+ * is rows q_offsets[s] .. q_offsets[s+1] - 1 of q, o, dout, dq and rows k_offsets[s] .. k_offsets[s+1] - 1 of k, v, dk, dv;
+ * both arrays are DEVICE, int32, seqs + 1 entries that do not decrease, and may be the same; NULL: sequences of equal
+ * length, q_rows / seqs (k_rows / seqs).  Entries outside 0 .. rows are taken as the nearest of these.  Query i of a sequence with
+ * nq queries and nk keys sees its nk keys, with causal = 1 only keys j <= i + nk - nq (the last query sees all): with
+ * scores s_j = scale q . k_j over those,
+ *   o = sum_j softmax(s)_j v_j,    lse = log2 sum_j 2^(s_j log2 e).
+ * A query that sees no key, or whose scores are all minus infinity, has o = 0 and lse = minus infinity.  Sequences may
+ * be empty on either side.  Rows behind the last sequence (and before the first) are left as they were.
+ * bf16 storage: probabilities are rounded to bf16 before they meet v (and, in the backward pass, do and k, q), sums
+ * are fp32.  Infinities and NaNs reach only the rows that see them. */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_attention_desc) */
+  int32_t dtype;             /* hbp_dtype */
+  int32_t heads;             /* query heads: a multiple of kv_heads */
+  int32_t kv_heads;
+  int32_t dh;                /* head width: a multiple of 8, at most 128 */
+  int32_t causal;            /* 0 or 1 */
+  float scale;               /* > 0, finite; usually 1 / sqrt(dh) */
+  float reserved;            /* 0 */
+  int64_t seqs;              /* >= 1 */
+  int64_t q_rows, k_rows;    /* rows of all sequences together, 0 .. 2^24 */
+} hbp_attention_desc;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_attention_buffers) */
+  hbp_heads q, k, v;         /* in */
+  hbp_heads o;               /* forward: out; backward: in */
+  hbp_heads dout;            /* backward: in, the gradient of o */
+  hbp_heads dq, dk, dv;      /* backward: out */
+  float* lse;                /* [q_rows, heads], forward: out; backward: in */
+  const int32_t* q_offsets;  /* or NULL */
+  const int32_t* k_offsets;  /* or NULL */
+  void* workspace;
+  size_t workspace_bytes;
+} hbp_attention_buffers;
+
+/* Bytes of workspace that either call below needs.  Calls that overlap must not share a workspace. */
+hbp_status hbp_attention_workspace_size(const hbp_attention_desc* desc, size_t* bytes);
+/* Reads q, k, v; writes o, lse. */
+hbp_status hbp_attention_forward(const hbp_attention_desc* desc, const hbp_attention_buffers* bufs, void* stream);
+/* Rebuilds the probabilities from q, k and lse: P = 2^(s log2 e - lse), D = sum_c dout (.) o, dS = P (.) (dout v^T - D),
+ *   dq = scale dS k,   dk = scale sum dS^T q,   dv = sum P^T dout   (dk, dv: over the query heads that share the key head).
+ * Reads q, k, v, o, lse, dout; writes dq, dk, dv (keys that nothing sees: zeros).  Sums are taken in a fixed order: results are
+ * bitwise repeatable. */
+hbp_status hbp_attention_backward(const hbp_attention_desc* desc, const hbp_attention_buffers* bufs, void* stream);
+
+/* HBP_TRANSFORMER with rotary positions and shared key/value heads: pass &this.base, whose struct_size says so, wherever
+ * a call takes an hbp_desc.  The attention sub-blocks then have kv_heads heads of keys and values: Wqkv and dWqkv are
+ * [L/2, w, d] and qkv is [L/2, N, w] with w = d + 2 kv_heads dh, a row [q heads | k heads | v heads]; q and k heads are turned by
+ * `rotary` before the attention, and qkv holds them turned.  dh <= 128 where kv_heads < heads. */
+typedef struct {
+  hbp_desc base;             /* struct_size = sizeof(hbp_transformer_desc), kind = HBP_TRANSFORMER */
+  int32_t kv_heads;          /* heads % kv_heads == 0; 0: as many as heads */
+  int32_t reserved;          /* 0 */
+  hbp_rotary_desc rotary;    /* dims = 0: no positions (struct_size 0 will do) */
+  const int32_t* positions;  /* DEVICE [N], or NULL: a token's place in its sequence */
+} hbp_transformer_desc;
+
 const char* hbp_status_string(hbp_status s);
 
 /* Optional timing of the kernels the calls above enqueue, by class, with HIP
@@ -326,7 +427,7 @@ enum {
   HBP_PROF_DW = 3,      /* parameter-gradient contractions over tokens              */
   HBP_PROF_FORWARD = 4, /* forward support kernels, chains along time among them    */
   HBP_PROF_OTHER = 5,   /* copies, split-K reductions                               */
-  HBP_PROF_ATTN = 6,    /* attention between its two matrices, forward and backward  */
+  HBP_PROF_ATTN = 6,    /* attention between its two matrices, forward and backward, and rotary positions */
   HBP_PROF_CLASSES = 7
 };
 hbp_status hbp_profile_enable(int on);

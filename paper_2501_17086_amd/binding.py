@@ -30,6 +30,7 @@ LAMBDA_ONE, LAMBDA_CHANNEL, LAMBDA_TOKEN = 0, 1, 2
 
 EXPORTS = ("hbp_workspace_size", "hbp_check", "hbp_forward", "hbp_backward", "hbp_exact_backward",
            "hbp_scan_workspace_size", "hbp_initial_estimate", "hbp_initial_estimate_static",
+           "hbp_rotary", "hbp_attention_workspace_size", "hbp_attention_forward", "hbp_attention_backward",
            "hbp_param_grads", "hbp_train_scratch_size", "hbp_loss_mse", "hbp_optimizer_step", "hbp_train_step",
            "hbp_profile_enable", "hbp_profile_read", "hbp_status_string")
 PROF_CLASSES = ("vjp1", "vjp2", "scan", "dw", "forward", "other", "attn")
@@ -41,6 +42,34 @@ class hbp_desc(C.Structure):
                 ("eps", C.c_float), ("L", C.c_int64), ("N", C.c_int64), ("d", C.c_int64), ("d_ff", C.c_int64),
                 ("d_in", C.c_int64), ("gamma", C.c_float), ("post", C.c_int32),
                 ("heads", C.c_int32), ("causal", C.c_int32), ("seq_len", C.c_int64)]
+
+
+class hbp_rotary_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layout", C.c_int32), ("scaling", C.c_int32), ("dims", C.c_int32),
+                ("magnitude", C.c_float), ("reserved", C.c_float), ("base", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("original", C.c_double)]
+
+
+class hbp_transformer_desc(hbp_desc):
+    """hbp_desc with rotary positions and shared key/value heads (the C struct's `base` is the inherited part)."""
+    _fields_ = [("kv_heads", C.c_int32), ("reserved", C.c_int32), ("rotary", hbp_rotary_desc), ("positions", C.c_void_p)]
+
+
+class hbp_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class hbp_attention_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dh", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float), ("reserved", C.c_float),
+                ("seqs", C.c_int64), ("q_rows", C.c_int64), ("k_rows", C.c_int64)]
+
+
+class hbp_attention_buffers(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("q", hbp_heads), ("k", hbp_heads), ("v", hbp_heads), ("o", hbp_heads),
+                ("dout", hbp_heads), ("dq", hbp_heads), ("dk", hbp_heads), ("dv", hbp_heads), ("lse", C.c_void_p),
+                ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 class hbp_buffers(C.Structure):
@@ -108,6 +137,11 @@ def lib() -> C.CDLL:
                                          C.POINTER(hbp_optim_state), C.c_void_p]
         L.hbp_train_step.argtypes = [C.POINTER(hbp_desc), C.c_int, C.POINTER(hbp_buffers), C.c_void_p, C.c_void_p,
                                      C.POINTER(hbp_optim), C.POINTER(hbp_optim_state), C.c_void_p]
+        L.hbp_rotary.argtypes = [C.POINTER(hbp_rotary_desc), C.c_int, C.c_int64, C.c_int, C.c_int, C.POINTER(hbp_heads),
+                                 C.POINTER(hbp_heads), C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_void_p]
+        L.hbp_attention_workspace_size.argtypes = [C.POINTER(hbp_attention_desc), C.POINTER(C.c_size_t)]
+        for n in ("hbp_attention_forward", "hbp_attention_backward"):
+            getattr(L, n).argtypes = [C.POINTER(hbp_attention_desc), C.POINTER(hbp_attention_buffers), C.c_void_p]
         L.hbp_profile_enable.argtypes = [C.c_int]
         L.hbp_profile_read.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.hbp_status_string.argtypes = [C.c_int]
@@ -125,7 +159,15 @@ def status_string(status: int) -> str:
 def make_desc(kind: str, dtype: str, act: str, norm: str, L: int, N: int, d: int, d_ff: int, d_in: int = 0,
               lambda_channel: bool = False, loss_every_state: bool = False, eps: float = 1e-6,
               gamma: float = 0.0, lambda_token: bool = False, post: str = "none", heads: int = 0,
-              causal: bool = True, seq_len: int = 0) -> hbp_desc:
+              causal: bool = True, seq_len: int = 0, kv_heads: int = 0, rotary: Optional[hbp_rotary_desc] = None,
+              positions=None) -> hbp_desc:
+    """kv_heads, rotary (make_rotary) and positions (int32 [N] on the GPU, kept alive by the caller): an hbp_transformer_desc."""
+    if kv_heads or rotary is not None:
+        base = make_desc(kind, dtype, act, norm, L, N, d, d_ff, d_in, lambda_channel, loss_every_state, eps, gamma, lambda_token,
+                         post, heads, causal, seq_len)
+        base.struct_size = C.sizeof(hbp_transformer_desc)
+        return hbp_transformer_desc(*[getattr(base, f) for f, _ in hbp_desc._fields_], kv_heads, 0,
+                                    hbp_rotary_desc() if rotary is None else rotary, _ptr(positions))
     return hbp_desc(C.sizeof(hbp_desc), KIND[kind], BF16 if dtype == "bf16" else F32,
                     ACT[act], NORM[norm],
                     LAMBDA_TOKEN if lambda_token else LAMBDA_CHANNEL if lambda_channel else LAMBDA_ONE,
@@ -220,7 +262,7 @@ def hbp_backward(p: Problem, k: int, stream=None, gamma: Optional[float] = None)
     b = p.buffers()
     desc = p.desc
     if gamma is not None:
-        desc = hbp_desc.from_buffer_copy(p.desc)
+        desc = type(p.desc).from_buffer_copy(p.desc)
         desc.gamma = float(gamma)
     _call("hbp_backward", lib().hbp_backward(C.byref(desc), int(k), C.byref(b), _stream(stream)))
 
@@ -335,6 +377,153 @@ def hbp_train_step(p: Problem, k: int, target, opt: hbp_optim, st: OptimState, s
                                                  st.loss.data_ptr(), C.byref(opt), C.byref(s), _stream(stream)))
 
 
+# ---- a language model's attention sub-block ----------------------------------------------------------------------
+ROTARY_LAYOUT = {"half": 0, "interleaved": 1}
+ROTARY_SCALING = {"none": 0, "linear": 1, "base": 2, "by_parts": 3}
+
+
+def make_rotary(dims: int, layout: str = "half", base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                low: float = 1.0, high: float = 4.0, original: float = 0.0, magnitude: float = 1.0) -> hbp_rotary_desc:
+    """Rotary positions on the first `dims` channels of a head; scaling, factor, low, high, original as in hbp_rotary_desc."""
+    return hbp_rotary_desc(C.sizeof(hbp_rotary_desc), ROTARY_LAYOUT[layout], ROTARY_SCALING[scaling], dims, magnitude, 0.0,
+                           base, factor, low, high, original)
+
+
+def _storage_type(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise ValueError(f"storage type {t.dtype}: float32 and bfloat16 are known")
+
+
+def _heads(t, name: str) -> hbp_heads:
+    """A [rows, heads, dh] tensor, channels next to each other."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name}: expected [rows, heads, dh] with the channels next to each other, got {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
+    return hbp_heads(t.data_ptr() if t.numel() else None, t.stride(0), t.stride(1))
+
+
+def _same(name: str, t, shape, dtype, device) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _int32s(name: str, t, n: int, device) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    _same(name, t, (n,), torch.int32, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+    return t.data_ptr()
+
+
+def _on(t):
+    """The tensor's device made the current one for the time of a call."""
+    import torch
+    if t.device.type != "cuda":
+        raise ValueError(f"expected tensors on the GPU, got {t.device}")
+    return torch.cuda.device(t.device)
+
+
+def hbp_rotary(rotary: hbp_rotary_desc, x, out, positions=None, first: int = 0, period: int = 0, inverse: bool = False,
+               stream=None) -> None:
+    """out := x turned by its rows' positions (inverse: turned back, the gradient's way); x, out: [rows, heads, dh], out may
+    be x.  positions: int32, one per row; without them row n is at first + n, or first + n % period."""
+    rows, heads, dh = x.shape
+    hx, ho = _heads(x, "x"), _heads(out, "out")
+    _same("out", out, x.shape, x.dtype, x.device)
+    pos = _int32s("positions", positions, rows, x.device)
+    with _on(x):
+        _call("hbp_rotary", lib().hbp_rotary(C.byref(rotary), _storage_type(x), rows, heads, dh, C.byref(hx), C.byref(ho), pos,
+                                             first, period, 1 if inverse else 0, _stream(stream)))
+
+
+@dataclass
+class Attention:
+    """Device tensors of one attention call: q, o, dq [q_rows, heads, dh]; k, v, dk, dv [k_rows, kv_heads, dh];
+    lse [q_rows, heads] fp32; offsets int32 [seqs + 1] or None."""
+    desc: hbp_attention_desc
+    q: "object"
+    k: "object"
+    v: "object"
+    o: "object"
+    lse: "object"
+    q_offsets: "object" = None
+    k_offsets: "object" = None
+    dq: "object" = None
+    dk: "object" = None
+    dv: "object" = None
+    workspace: "object" = None
+
+    def buffers(self, dout=None) -> hbp_attention_buffers:
+        import torch
+        q, k, d = self.q, self.k, self.desc
+        rows, kv = (d.q_rows, d.heads, d.dh), (d.k_rows, d.kv_heads, d.dh)
+        b = hbp_attention_buffers(C.sizeof(hbp_attention_buffers))
+        named = [("q", q, rows), ("k", k, kv), ("v", self.v, kv), ("o", self.o, rows)]
+        if dout is not None:
+            named += [("dout", dout, rows), ("dq", self.dq, rows), ("dk", self.dk, kv), ("dv", self.dv, kv)]
+        for name, t, shape in named:
+            _same(name, t, shape, q.dtype, q.device)
+            setattr(b, name, _heads(t, name))
+        _same("lse", self.lse, rows[:2], torch.float32, q.device)
+        if not self.lse.is_contiguous():
+            raise ValueError("lse: not contiguous")
+        b.lse = self.lse.data_ptr()
+        b.q_offsets = _int32s("q_offsets", self.q_offsets, d.seqs + 1, q.device)
+        b.k_offsets = _int32s("k_offsets", self.k_offsets, d.seqs + 1, q.device)
+        if self.workspace is not None:
+            b.workspace, b.workspace_bytes = self.workspace.data_ptr(), self.workspace.numel() * self.workspace.element_size()
+        return b
+
+
+def attention_workspace_size(desc: hbp_attention_desc) -> int:
+    n = C.c_size_t(0)
+    _call("hbp_attention_workspace_size", lib().hbp_attention_workspace_size(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def make_attention(q, k, v, causal: bool = True, q_offsets=None, k_offsets=None, seqs: int = 1, scale: Optional[float] = None,
+                   o=None, lse=None, grad: bool = True) -> Attention:
+    """An Attention over the given q, k, v: allocates o and lse (unless given), dq, dk, dv (grad) and the workspace.  With
+    offsets there are len - 1 sequences, without them `seqs` of equal length."""
+    import torch
+    for off in (q_offsets, k_offsets):
+        if off is not None:
+            seqs = off.numel() - 1
+    if q_offsets is not None and k_offsets is not None and q_offsets.numel() != k_offsets.numel():
+        raise ValueError("q_offsets and k_offsets: different numbers of sequences")
+    dh = q.shape[2]
+    desc = hbp_attention_desc(C.sizeof(hbp_attention_desc), _storage_type(q), q.shape[1], k.shape[1], dh, 1 if causal else 0,
+                              dh ** -0.5 if scale is None else scale, 0.0, seqs, q.shape[0], k.shape[0])
+    with _on(q):
+        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        a = Attention(desc, q, k, v, new(q) if o is None else o,
+                      torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse, q_offsets, k_offsets)
+        if grad:
+            a.dq, a.dk, a.dv = new(q), new(k), new(v)
+        a.workspace = torch.empty(attention_workspace_size(desc), dtype=torch.uint8, device=q.device)
+    return a
+
+
+def hbp_attention_forward(a: Attention, stream=None) -> None:
+    """a.o, a.lse from a.q, a.k, a.v."""
+    b = a.buffers()
+    with _on(a.q):
+        _call("hbp_attention_forward", lib().hbp_attention_forward(C.byref(a.desc), C.byref(b), _stream(stream)))
+
+
+def hbp_attention_backward(a: Attention, dout, stream=None) -> None:
+    """a.dq, a.dk, a.dv from a.q, a.k, a.v, a.o, a.lse and the gradient of a.o."""
+    b = a.buffers(dout)
+    with _on(a.q):
+        _call("hbp_attention_backward", lib().hbp_attention_backward(C.byref(a.desc), C.byref(b), _stream(stream)))
+
+
 def profile_enable(on: bool) -> None:
     _call("hbp_profile_enable", lib().hbp_profile_enable(1 if on else 0))
 
@@ -368,7 +557,8 @@ def allocate(w, inputs, device="cuda:0", N: Optional[int] = None) -> Problem:
                      lambda_channel=lam is not None and not per_token, lambda_token=per_token,
                      loss_every_state=w.loss_every_state, eps=w.eps, post=getattr(w, "post", "none"),
                      heads=getattr(w, "heads", 0), causal=getattr(w, "causal", True), seq_len=getattr(w, "seq_len", 0),
-                     gamma=getattr(w, "gamma", 0.0))
+                     gamma=getattr(w, "gamma", 0.0), kv_heads=getattr(w, "kv_heads", 0),
+                     rotary=make_rotary(**w.rotary) if getattr(w, "rotary", None) else None)
     L, d, dff = w.L, w.d, w.d_ff
     tfm = w.kind == "transformer"
     Li = L // 2 if tfm else L        # rows of the inner state: one per MLP block
@@ -392,7 +582,7 @@ def allocate(w, inputs, device="cuda:0", N: Optional[int] = None) -> Problem:
     )
     if tfm:
         p.Wqkv, p.Wo = up(inputs["Wqkv"]), up(inputs["Wo"])
-        p.qkv = torch.zeros((Li, N, 3 * d), dtype=dt, device=dev)
+        p.qkv = torch.zeros((Li, N, p.Wqkv.shape[1]), dtype=dt, device=dev)
         p.attn_o = torch.zeros((Li, N, d), dtype=dt, device=dev)
         p.lse = torch.zeros((Li, N * w.heads), dtype=torch.float32, device=dev)
         p.dWqkv = torch.zeros(inputs["Wqkv"].shape, dtype=torch.float32, device=dev)

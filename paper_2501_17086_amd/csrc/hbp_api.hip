@@ -32,9 +32,77 @@ inline bool shared_w(const hbp_desc* d) { return recurrent(d); }
 // The alternating attention / MLP stack: weight sets and inner-state rows are counted per layer (L / 2).
 inline bool tfm(const hbp_desc* d) { return d->kind == HBP_TRANSFORMER; }
 inline long head_w(const hbp_desc* d) { return d->d / d->heads; }
+// Rotary positions and shared key/value heads: the descriptor is then the first member of a larger one.
+inline const hbp_transformer_desc* extended(const hbp_desc* d) {
+  return d->struct_size == sizeof(hbp_transformer_desc) ? reinterpret_cast<const hbp_transformer_desc*>(d) : nullptr;
+}
+inline int key_heads(const hbp_desc* d) {
+  const hbp_transformer_desc* x = extended(d);
+  return x && x->kv_heads ? x->kv_heads : d->heads;
+}
+inline long qkv_w(const hbp_desc* d) { return d->d + 2 * key_heads(d) * head_w(d); }    // width of a [q | k | v] row
+inline bool turned(const hbp_desc* d) { return extended(d) && extended(d)->rotary.dims != 0; }
+
+hbp_status check_rotary(const hbp_rotary_desc* r, int dtype, int dh) {
+  if (!r) return HBP_E_NULL;
+  if (r->struct_size != sizeof(hbp_rotary_desc)) return HBP_E_INVALID_ARG;
+  if (r->layout != HBP_ROTARY_HALF && r->layout != HBP_ROTARY_INTERLEAVED) return HBP_E_INVALID_ARG;
+  if (r->scaling < HBP_ROTARY_PLAIN || r->scaling > HBP_ROTARY_BY_PARTS) return HBP_E_INVALID_ARG;
+  if (dtype != HBP_F32 && dtype != HBP_BF16) return HBP_E_INVALID_ARG;
+  if (dh <= 0 || r->dims < 2 || r->dims % 2 || r->dims > dh) return HBP_E_INVALID_ARG;
+  if (!(r->base > 0) || !std::isfinite(r->base) || !std::isfinite(r->magnitude) || r->reserved != 0.f) return HBP_E_INVALID_ARG;
+  if (r->scaling != HBP_ROTARY_PLAIN && (!(r->factor > 0) || !std::isfinite(r->factor))) return HBP_E_INVALID_ARG;
+  if (r->scaling == HBP_ROTARY_BASE && r->dims < 4) return HBP_E_INVALID_ARG;
+  if (r->scaling == HBP_ROTARY_BY_PARTS &&
+      (!(r->low < r->high) || !std::isfinite(r->high - r->low) || !(r->original > 0) || !std::isfinite(r->original)))
+    return HBP_E_INVALID_ARG;
+  if (dh % 8 || dh > 2 * ROTARY_PAIRS) return HBP_E_UNSUPPORTED;
+  return HBP_OK;
+}
+
+// frequencies in turns per position
+void rotary_turns(const hbp_rotary_desc* r, double* turns) {
+  const double two_pi = 6.283185307179586476925286766559;
+  double base = r->base;
+  if (r->scaling == HBP_ROTARY_BASE) base *= pow(r->factor, (double)r->dims / (r->dims - 2));
+  for (int i = 0; i < r->dims / 2; ++i) {
+    double f = pow(base, -2.0 * i / r->dims) / two_pi;
+    if (r->scaling == HBP_ROTARY_LINEAR) f /= r->factor;
+    if (r->scaling == HBP_ROTARY_BY_PARTS) {
+      double w = (r->original * f - r->low) / (r->high - r->low);
+      w = w < 0 ? 0 : w > 1 ? 1 : w;
+      f *= w + (1 - w) / r->factor;
+    }
+    turns[i] = f;
+  }
+}
+
+RotaryArgs rotary_args(const hbp_rotary_desc* r, long rows, int heads, int dh, const HeadRows& x, const HeadRows& y,
+                       const int32_t* positions, long first, long period, int inverse) {
+  RotaryArgs a{};
+  a.x = x.p; a.x_row = x.row; a.x_head = x.head;
+  a.y = y.p; a.y_row = y.row; a.y_head = y.head;
+  a.rows = rows; a.heads = heads; a.dh = dh; a.dims = r->dims;
+  a.positions = positions; a.first = first; a.period = period < rows ? period : 0;
+  a.inverse = inverse; a.magnitude = r->magnitude;
+  rotary_turns(r, a.turns);
+  return a;
+}
+
+// the sizes of a transformer stack's attention with shared key/value heads, over all sequences of `layers` layers
+PackedAttnArgs packed_sizes(const hbp_desc* d, long layers) {
+  PackedAttnArgs a{};
+  a.seqs = (int)(layers * (d->N / d->seq_len));
+  a.q_rows = a.k_rows = (int)(layers * d->N);
+  a.heads = d->heads; a.kv_heads = key_heads(d); a.group = d->heads / a.kv_heads;
+  a.dh = (int)head_w(d); a.causal = d->causal;
+  a.scale = 1.0f / sqrtf((float)head_w(d));
+  return a;
+}
+size_t packed_ws(const hbp_desc* d) { return packed_attn_ws_bytes(d->dtype, packed_sizes(d, d->L / 2)); }
 
 struct Workspace {
-  size_t off_v, off_da, off_part, off_scan, off_wt, off_pre, off_m, off_tmp, off_dqkv, off_dsum, off_counter, total;
+  size_t off_v, off_da, off_part, off_scan, off_wt, off_pre, off_m, off_tmp, off_dqkv, off_dsum, off_packed, off_counter, total;
 };
 
 // The partial sums of a parameter gradient take at most this much: shares are taken to fill the chip, and what does that without
@@ -104,7 +172,7 @@ Splits param_splits(const hbp_desc* d) {
   if (tfm(d)) {
     const long nb = d->L / 2;
     s.s_w2 = s.s_w1 = pick_split(d, d->d, d->d_ff, nb, d->N);
-    s.s_qkv = pick_split(d, 3 * d->d, d->d, nb, d->N);
+    s.s_qkv = pick_split(d, qkv_w(d), d->d, nb, d->N);
     s.s_o = pick_split(d, d->d, d->d, nb, d->N);
     return s;
   }
@@ -133,8 +201,8 @@ Workspace carve(const hbp_desc* d) {
   partials(sp.s_w2, nb * d->d * d->d_ff);
   partials(sp.s_w1, nb * hidden_w(d) * (gru(d) ? 2 * d->d : d->d_ff));
   partials(sp.s_cand, (size_t)d->d * d->d);
-  partials(sp.s_qkv, nb * 3 * d->d * d->d);
-  partials(sp.s_o, nb * d->d * d->d);
+  if (tfm(d)) partials(sp.s_qkv, nb * qkv_w(d) * d->d);
+  if (tfm(d)) partials(sp.s_o, nb * d->d * d->d);
   partials(sp.s_u, (size_t)d->d_ff * d->d_in);
   w.off_part = o; o = align_up(o + part, 256);
   // (also where gamma is 0 and the form with the states shared out, which needs none, takes every scan: a call may bring another gamma,
@@ -155,9 +223,12 @@ Workspace carve(const hbp_desc* d) {
   // the attention sub-blocks: the gradient of the attention's output (in tmp), of [q | k | v], and rowsum(do (.) o)
   if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * d->d * es, 256);
   w.off_dqkv = o;
-  if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * 3 * d->d * es, 256);
+  if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * qkv_w(d) * es, 256);
   w.off_dsum = o;
   if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * d->heads * 4, 256);
+  // shared key/value heads: what the attention over packed sequences needs
+  w.off_packed = o;
+  if (tfm(d) && key_heads(d) < d->heads) o = align_up(o + packed_ws(d), 256);
   // the chain kernels' counters and what their workgroups exchange (4 MB)
   w.off_counter = o;
   if (recurrent(d) && d->dtype == HBP_BF16) o += RECURRENT_COUNTER_BYTES + recurrent_ring_bytes();
@@ -174,7 +245,8 @@ inline bool step_skinny(const hbp_desc* d) {
 
 hbp_status check_desc(const hbp_desc* d) {
   if (!d) return HBP_E_NULL;
-  if (d->struct_size != sizeof(hbp_desc)) return HBP_E_INVALID_ARG;
+  if (d->struct_size != sizeof(hbp_desc) && !(d->struct_size == sizeof(hbp_transformer_desc) && d->kind == HBP_TRANSFORMER))
+    return HBP_E_INVALID_ARG;
   if (d->kind < HBP_MLP || d->kind > HBP_TRANSFORMER) return HBP_E_INVALID_ARG;
   if (d->dtype != HBP_F32 && d->dtype != HBP_BF16) return HBP_E_INVALID_ARG;
   if (d->act < HBP_ACT_GELU_ERF || d->act > HBP_ACT_IDENTITY) return HBP_E_INVALID_ARG;
@@ -192,7 +264,19 @@ hbp_status check_desc(const hbp_desc* d) {
     if (d->L % 2 || d->heads <= 0 || d->seq_len <= 0 || (d->causal != 0 && d->causal != 1)) return HBP_E_INVALID_ARG;
     if (d->N % d->seq_len || d->d % d->heads) return HBP_E_INVALID_ARG;
     if (d->post == HBP_POST_RELU || head_w(d) % 8) return HBP_E_UNSUPPORTED;
-    if (!attn_supported(d->dtype, d->seq_len, (int)head_w(d))) return HBP_E_UNSUPPORTED;
+    if (const hbp_transformer_desc* x = extended(d)) {
+      if (x->kv_heads < 0 || (x->kv_heads && d->heads % x->kv_heads) || x->reserved != 0) return HBP_E_INVALID_ARG;
+      if (turned(d)) {
+        const hbp_status st = check_rotary(&x->rotary, d->dtype, (int)head_w(d));
+        if (st != HBP_OK) return st;
+      }
+    }
+    if (key_heads(d) < d->heads) {
+      if (head_w(d) > 128 || d->heads > 4096 || d->N > (1L << 24)) return HBP_E_UNSUPPORTED;
+      if ((double)(d->L / 2) * (d->N + 32 * (d->N / d->seq_len)) * d->heads >= 2147483648.0) return HBP_E_UNSUPPORTED;
+    } else if (!attn_supported(d->dtype, d->seq_len, (int)head_w(d))) {
+      return HBP_E_UNSUPPORTED;
+    }
   }
   if (d->norm == HBP_NORM_RMS && !(d->eps >= 0.f)) return HBP_E_INVALID_ARG;
   if (d->d % 8 || d->d_ff % 8 || d->d_in % 8) return HBP_E_UNSUPPORTED;
@@ -325,7 +409,7 @@ AttnArgs attn_args(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, 
   const size_t es = esize(d);
   const long N = d->N, D = d->d;
   AttnArgs a{};
-  a.qkv = at((const void*)b->qkv, (size_t)j_lo * N * 3 * D * es);
+  a.qkv = at((const void*)b->qkv, (size_t)j_lo * N * 3 * D * es);      // (key heads as many as query heads: qkv_w is 3 D)
   a.o = at(b->attn_o, (size_t)j_lo * N * D * es);
   a.lse = b->lse + j_lo * N * d->heads;
   a.dout = at((const void*)b->workspace, w.off_tmp + (size_t)j_lo * N * D * es);
@@ -342,6 +426,36 @@ AttnArgs attn_args(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, 
 
 // first half: da_j = (g[2j+2] W2_j) (.) act' for the MLP sub-blocks; do_j = g[2j+1] Wo_j and, through the attention,
 // the gradient of [q | k | v] for the attention sub-blocks
+// Shared key/value heads: the attention of layers j_lo .. j_hi - 1, whose sequences lie behind one another
+PackedAttnArgs packed_args(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, long j_lo, long j_hi) {
+  const size_t es = esize(d);
+  const long j = j_lo;
+  const long N = d->N, D = d->d, W = qkv_w(d), dh = head_w(d), kw = key_heads(d) * dh;
+  PackedAttnArgs a = packed_sizes(d, j_hi - j_lo);
+  char* qkv = at(b->qkv, (size_t)j * N * W * es);
+  char* dqkv = at(b->workspace, w.off_dqkv + (size_t)j * N * W * es);
+  a.q = {qkv, W, dh}; a.k = {at((void*)qkv, D * es), W, dh}; a.v = {at((void*)qkv, (D + kw) * es), W, dh};
+  a.dq = {dqkv, W, dh}; a.dk = {at((void*)dqkv, D * es), W, dh}; a.dv = {at((void*)dqkv, (D + kw) * es), W, dh};
+  a.o = {at(b->attn_o, (size_t)j * N * D * es), D, dh};
+  a.dout = {at(b->workspace, w.off_tmp + (size_t)j * N * D * es), D, dh};
+  a.lse = b->lse + j * N * d->heads;
+  return a;
+}
+// q and k heads of `layers` layers' rows turned in place, as many layers at a time as 2^24 rows hold (given positions are those of one
+// layer's tokens: one at a time)
+hbp_status turn_qk(const hbp_desc* d, void* qkv, long layers, int inverse, hipStream_t s) {
+  const hbp_transformer_desc* x = extended(d);
+  const long W = qkv_w(d), dh = head_w(d);
+  const long most = x->positions || d->N > (1 << 24) ? 1 : (1 << 24) / d->N;
+  for (long j = 0; j < layers; j += most) {
+    const long n = layers - j < most ? layers - j : most;
+    const HeadRows r{at(qkv, (size_t)j * d->N * W * esize(d)), W, dh};
+    const RotaryArgs a = rotary_args(&x->rotary, n * d->N, d->heads + key_heads(d), (int)dh, r, r, x->positions, 0, d->seq_len, inverse);
+    HBP_TRY(launch_rotary(d->dtype, x->rotary.layout, a, s));
+  }
+  return HBP_OK;
+}
+
 hbp_status tfm_stage1(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, long l_lo, long l_hi, hipStream_t s) {
   const size_t es = esize(d);
   const long N = d->N, D = d->d, F = d->d_ff;
@@ -385,7 +499,14 @@ hbp_status tfm_stage1(const hbp_desc* d, const hbp_buffers* b, const Workspace& 
   if (n) HBP_RUN(run_gemms(d, list, n, s, HBP_PROF_VJP1));
   if (ja_hi > ja_lo) {
     ProfScope ps(HBP_PROF_ATTN, s);
-    HBP_TRY(launch_attn_bwd(d->dtype, attn_args(d, b, w, ja_lo, ja_hi), s));
+    if (key_heads(d) < d->heads)
+      HBP_TRY(launch_packed_attn_bwd(d->dtype, packed_args(d, b, w, ja_lo, ja_hi), at(b->workspace, w.off_packed), s));
+    else
+      HBP_TRY(launch_attn_bwd(d->dtype, attn_args(d, b, w, ja_lo, ja_hi), s));
+    if (turned(d)) {
+      const long W = qkv_w(d);
+      HBP_RUN(turn_qk(d, at(b->workspace, w.off_dqkv + (size_t)ja_lo * N * W * es), ja_hi - ja_lo, 1, s));
+    }
   }
   return HBP_OK;
 }
@@ -402,7 +523,7 @@ hbp_status tfm_stage2(const hbp_desc* d, const hbp_buffers* b, const Workspace& 
     const long j_lo = attn ? ja_lo : jm_lo, j_hi = attn ? ja_hi : jm_hi;
     if (j_hi <= j_lo) continue;
     const long l0 = attn ? 2 * j_lo : 2 * j_lo + 1;        // first block of this kind in the range
-    const long kk = attn ? 3 * D : F;
+    const long kk = attn ? qkv_w(d) : F;
     GemmArgs ga{};
     ga.A = attn ? at(b->workspace, w.off_dqkv + (size_t)j_lo * N * kk * es) : at(b->workspace, w.off_da + (size_t)j_lo * N * kk * es);
     ga.B = attn ? at(b->Wqkv, (size_t)j_lo * kk * D * es) : at(b->W1, (size_t)j_lo * kk * D * es);
@@ -825,22 +946,26 @@ hbp_status run_forward(const hbp_desc* d, hbp_buffers* b, void* stream, int wait
       yl = at((const void*)b->y, xo);
     }
     if (tfm(d) && l % 2 == 0) {     // attention sub-block: [q | k | v] = y Wqkv^T, attention, x_{l+1} = lambda (.) x_l + o Wo^T
-      const long N = d->N, D = d->d;
+      const long N = d->N, D = d->d, W = qkv_w(d);
       {
         GemmArgs ga{};
         ga.A = yl;
-        ga.B = at(b->Wqkv, (size_t)wl * 3 * D * D * es);
-        ga.C = at(b->qkv, (size_t)wl * N * 3 * D * es);
-        ga.M = N; ga.N = 3 * D; ga.K = D;
+        ga.B = at(b->Wqkv, (size_t)wl * W * D * es);
+        ga.C = at(b->qkv, (size_t)wl * N * W * es);
+        ga.M = N; ga.N = W; ga.K = D;
         ga.a_sm = D; ga.a_sk = 1;
         ga.b_sk = 1; ga.b_sn = D;
-        ga.ldc = 3 * D; ga.batch = 1; ga.split_k = 1;
+        ga.ldc = W; ga.batch = 1; ga.split_k = 1;
         ga.mode = EPI_STORE;
         HBP_RUN(run_gemm(d, ga, s, HBP_PROF_FORWARD));
       }
       {
         ProfScope ps(HBP_PROF_ATTN, s);
-        HBP_TRY(launch_attn_fwd(d->dtype, attn_args(d, b, w, wl, wl + 1), s));
+        if (turned(d)) HBP_RUN(turn_qk(d, at(b->qkv, (size_t)wl * N * W * es), 1, 0, s));
+        if (key_heads(d) < d->heads)
+          HBP_TRY(launch_packed_attn_fwd(d->dtype, packed_args(d, b, w, wl, wl + 1), at(b->workspace, w.off_packed), s));
+        else
+          HBP_TRY(launch_attn_fwd(d->dtype, attn_args(d, b, w, wl, wl + 1), s));
       }
       GemmArgs ga{};
       ga.A = at((const void*)b->attn_o, (size_t)wl * N * D * es);
@@ -1243,7 +1368,7 @@ hbp_status hbp_param_grads(const hbp_desc* d, hbp_buffers* b, void* stream) {
     list[n++] = tn_args(g2, D, 2 * N * D, bb.z, F, N * F, bb.dW2, D, F, N, Lh, sp.s_w2);
     list[n++] = tn_args(da, F, N * F, y1, D, 2 * N * D, bb.dW1, F, D, N, Lh, sp.s_w1);
     list[n++] = tn_args(g1, D, 2 * N * D, bb.attn_o, D, N * D, bb.dWo, D, D, N, Lh, sp.s_o);
-    list[n++] = tn_args(at((const void*)b->workspace, w.off_dqkv), 3 * D, 3 * N * D, bb.y, D, 2 * N * D, bb.dWqkv, 3 * D, D, N, Lh,
+    list[n++] = tn_args(at((const void*)b->workspace, w.off_dqkv), qkv_w(d), qkv_w(d) * N, bb.y, D, 2 * N * D, bb.dWqkv, qkv_w(d), D, N, Lh,
                         sp.s_qkv);
     return run_tn(d, list, n, part, s);
   }
@@ -1269,7 +1394,7 @@ struct ParamSizes { long n1, n2, nu, nq, no; };
 ParamSizes param_sizes(const hbp_desc* d) {
   const long nb = shared_w(d) ? 1 : tfm(d) ? d->L / 2 : d->L;
   ParamSizes p{};
-  p.nq = tfm(d) ? nb * 3 * d->d * d->d : 0;
+  p.nq = tfm(d) ? nb * qkv_w(d) * d->d : 0;
   p.no = tfm(d) ? nb * d->d * d->d : 0;
   p.n1 = nb * d->d_ff * hidden_w(d);
   p.n2 = cell(d) ? 0 : nb * d->d * d->d_ff;
@@ -1362,6 +1487,128 @@ hbp_status hbp_train_step(const hbp_desc* d, int k, hbp_buffers* b, const void* 
   else HBP_RUN(hbp_backward(d, k, b, stream));
   HBP_RUN(hbp_param_grads(d, b, stream));
   return hbp_optimizer_step(d, b, o, st, stream);
+}
+
+namespace {
+
+// stride and alignment rules of hbp_heads; `written`: no two elements of rows x heads x dh may share a place
+hbp_status check_heads(const hbp_heads& x, int64_t rows, int heads, int dh, bool written) {
+  if (rows == 0) return HBP_OK;
+  if (!x.data) return HBP_E_NULL;
+  const bool one_row = rows == 1, one_head = heads == 1;          // (then its stride does not matter)
+  if ((!one_row && x.row_stride < 0) || (!one_head && x.head_stride < 0)) return HBP_E_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(x.data) % 16) return HBP_E_UNSUPPORTED;
+  if (!one_row && (x.row_stride % 8 || x.row_stride >= (1 << 24))) return HBP_E_UNSUPPORTED;
+  if (!one_head && (x.head_stride % 8 || x.head_stride >= (int64_t)1 << 40)) return HBP_E_UNSUPPORTED;
+  if (written) {
+    const bool by_row = (one_head || x.head_stride >= dh) && (one_row || x.row_stride >= (one_head ? dh : heads * x.head_stride));
+    const bool by_head = (one_row || x.row_stride >= dh) && (one_head || x.head_stride >= (one_row ? dh : rows * x.row_stride));
+    // heads side by side, the last of a row followed by the next row before a whole head stride is over
+    const bool packed = !one_row && !one_head && x.head_stride >= dh && x.row_stride >= (heads - 1) * x.head_stride + dh;
+    if (!by_row && !by_head && !packed) return HBP_E_INVALID_ARG;
+  }
+  return HBP_OK;
+}
+HeadRows rows_of(const hbp_heads& x, int64_t rows, int heads) {
+  return {x.data, rows > 1 ? (long)x.row_stride : 0, heads > 1 ? (long)x.head_stride : 0};
+}
+
+hbp_status check_attention(const hbp_attention_desc* d) {
+  if (!d) return HBP_E_NULL;
+  if (d->struct_size != sizeof(hbp_attention_desc)) return HBP_E_INVALID_ARG;
+  if (d->dtype != HBP_F32 && d->dtype != HBP_BF16) return HBP_E_INVALID_ARG;
+  if (d->heads <= 0 || d->kv_heads <= 0 || d->heads % d->kv_heads || d->dh <= 0) return HBP_E_INVALID_ARG;
+  if (d->causal != 0 && d->causal != 1) return HBP_E_INVALID_ARG;
+  if (!(d->scale > 0.f) || !std::isfinite(d->scale) || d->reserved != 0.f) return HBP_E_INVALID_ARG;
+  if (d->seqs < 1 || d->q_rows < 0 || d->k_rows < 0) return HBP_E_INVALID_ARG;
+  if (d->dh % 8 || d->dh > 128) return HBP_E_UNSUPPORTED;
+  if (d->seqs > (1 << 24) || d->q_rows > (1 << 24) || d->k_rows > (1 << 24) || d->heads > 4096) return HBP_E_UNSUPPORTED;
+  if ((d->q_rows + 32 * d->seqs) * d->heads >= (int64_t)1 << 31 || (d->k_rows + 32 * d->seqs) * d->kv_heads >= (int64_t)1 << 31)
+    return HBP_E_UNSUPPORTED;
+  return HBP_OK;
+}
+PackedAttnArgs attention_sizes(const hbp_attention_desc* d) {
+  PackedAttnArgs a{};
+  a.seqs = (int)d->seqs; a.q_rows = (int)d->q_rows; a.k_rows = (int)d->k_rows;
+  a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads;
+  a.dh = d->dh; a.causal = d->causal; a.scale = d->scale;
+  return a;
+}
+hbp_status attention_call(const hbp_attention_desc* d, const hbp_attention_buffers* b, bool backward, PackedAttnArgs* out) {
+  HBP_RUN(check_attention(d));
+  if (!b) return HBP_E_NULL;
+  if (b->struct_size != sizeof(hbp_attention_buffers)) return HBP_E_INVALID_ARG;
+  if ((!b->q_offsets && d->q_rows % d->seqs) || (!b->k_offsets && d->k_rows % d->seqs)) return HBP_E_INVALID_ARG;
+  HBP_RUN(check_heads(b->q, d->q_rows, d->heads, d->dh, false));
+  HBP_RUN(check_heads(b->k, d->k_rows, d->kv_heads, d->dh, false));
+  HBP_RUN(check_heads(b->v, d->k_rows, d->kv_heads, d->dh, false));
+  HBP_RUN(check_heads(b->o, d->q_rows, d->heads, d->dh, !backward));
+  if (backward) {
+    HBP_RUN(check_heads(b->dout, d->q_rows, d->heads, d->dh, false));
+    HBP_RUN(check_heads(b->dq, d->q_rows, d->heads, d->dh, true));
+    HBP_RUN(check_heads(b->dk, d->k_rows, d->kv_heads, d->dh, true));
+    HBP_RUN(check_heads(b->dv, d->k_rows, d->kv_heads, d->dh, true));
+  }
+  if (d->q_rows && !b->lse) return HBP_E_NULL;
+  PackedAttnArgs a = attention_sizes(d);
+  const size_t need = packed_attn_ws_bytes(d->dtype, a);
+  if (need && (!b->workspace || b->workspace_bytes < need)) return HBP_E_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(b->workspace) % 16) return HBP_E_UNSUPPORTED;
+  const int64_t nq = d->q_rows, nk = d->k_rows;
+  a.q = rows_of(b->q, nq, d->heads); a.o = rows_of(b->o, nq, d->heads);
+  a.k = rows_of(b->k, nk, d->kv_heads); a.v = rows_of(b->v, nk, d->kv_heads);
+  if (backward) {
+    a.dout = rows_of(b->dout, nq, d->heads); a.dq = rows_of(b->dq, nq, d->heads);
+    a.dk = rows_of(b->dk, nk, d->kv_heads); a.dv = rows_of(b->dv, nk, d->kv_heads);
+  }
+  a.lse = b->lse; a.q_off = b->q_offsets; a.k_off = b->k_offsets;
+  *out = a;
+  return HBP_OK;
+}
+
+}  // namespace
+
+hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, int heads, int dh, const hbp_heads* x,
+                      const hbp_heads* out, const int32_t* positions, int64_t first, int64_t period, int inverse, void* stream) {
+  HBP_RUN(check_rotary(rotary, dtype, dh));
+  if (!x || !out) return HBP_E_NULL;
+  if (rows < 0 || heads <= 0 || period < 0 || (inverse != 0 && inverse != 1)) return HBP_E_INVALID_ARG;
+  if (rows > (1 << 24) || heads > 65535 || first > ((int64_t)1 << 52) || first < -((int64_t)1 << 52)) return HBP_E_UNSUPPORTED;
+  HBP_RUN(check_heads(*x, rows, heads, dh, false));
+  HBP_RUN(check_heads(*out, rows, heads, dh, true));
+  if (rows == 0) return HBP_OK;
+  if (x->data == out->data && ((rows > 1 && x->row_stride != out->row_stride) || (heads > 1 && x->head_stride != out->head_stride)))
+    return HBP_E_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_ATTN, s);
+  HBP_TRY(launch_rotary(dtype, rotary->layout, rotary_args(rotary, rows, heads, dh, rows_of(*x, rows, heads), rows_of(*out, rows, heads), positions, first,
+                                                           period, inverse), s));
+  return HBP_OK;
+}
+
+hbp_status hbp_attention_workspace_size(const hbp_attention_desc* d, size_t* bytes) {
+  if (!bytes) return HBP_E_NULL;
+  HBP_RUN(check_attention(d));
+  *bytes = packed_attn_ws_bytes(d->dtype, attention_sizes(d));
+  return HBP_OK;
+}
+
+hbp_status hbp_attention_forward(const hbp_attention_desc* d, const hbp_attention_buffers* b, void* stream) {
+  PackedAttnArgs a;
+  HBP_RUN(attention_call(d, b, false, &a));
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_ATTN, s);
+  HBP_TRY(launch_packed_attn_fwd(d->dtype, a, b->workspace, s));
+  return HBP_OK;
+}
+
+hbp_status hbp_attention_backward(const hbp_attention_desc* d, const hbp_attention_buffers* b, void* stream) {
+  PackedAttnArgs a;
+  HBP_RUN(attention_call(d, b, true, &a));
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_ATTN, s);
+  HBP_TRY(launch_packed_attn_bwd(d->dtype, a, b->workspace, s));
+  return HBP_OK;
 }
 
 }  // extern "C"

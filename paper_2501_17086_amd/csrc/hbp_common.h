@@ -220,6 +220,38 @@ bool attn_supported(int dtype, long T, int dh);
 hipError_t launch_attn_fwd(int dtype, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_bwd(int dtype, const AttnArgs& a, hipStream_t s);
 
+// Rotary positions (rotary.hip): rows of heads turned pair by pair; x == y turns in place.  Strides in elements.
+constexpr int ROTARY_PAIRS = 128;
+struct RotaryArgs {
+  const void* x; long x_row, x_head;
+  void* y; long y_row, y_head;
+  long rows;
+  int heads, dh, dims;
+  const int* positions;     // one per row, or NULL: first + n, or first + n % period (period > 0)
+  long first, period;
+  int inverse;
+  float magnitude;
+  int units, per;           // set by the launcher: units of a row, heads of a thread
+  double turns[ROTARY_PAIRS];   // turns (angle / 2 pi) per position of every pair
+};
+hipError_t launch_rotary(int dtype, int layout, const RotaryArgs& a, hipStream_t s);
+
+// Attention over packed sequences with shared key/value heads (attention_packed.hip).  Strides in elements.
+struct HeadRows { void* p; long row, head; };
+struct PackedAttnArgs {
+  HeadRows q, k, v, o, dout, dq, dk, dv;
+  float* lse;               // [q_rows, heads]
+  float* dsum;              // [q_rows, heads], workspace: rowsum(dout (.) o)
+  const int* q_off;         // [seqs + 1] or NULL: equal lengths
+  const int* k_off;
+  int seqs, q_rows, k_rows;
+  int heads, kv_heads, group, dh, causal;
+  float scale;
+};
+size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a);
+hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
+hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
+
 // Few-row bf16 product with both operands K-contiguous: C[M,N] = epilogue(A[M,K] . Bt[N,K]^T).
 // Modes EPI_STORE, EPI_ACT_TANH, EPI_MUL_AUX, EPI_MUL_1MZ2, EPI_ADD_AUX; aux is bf16 [M,N] with row stride ldaux.
 // EPI_RESID here is the residual path's backward step, C = acc (+ aux) + lambda (.) next: next and

@@ -58,11 +58,18 @@ class Workload:
     heads: int = 0       # 'transformer': attention heads, sequence length, causal mask
     seq_len: int = 0
     causal: bool = True
+    kv_heads: int = 0    # 'transformer': heads of keys and values; 0: as many as query heads
+    rotary: Optional[dict] = None   # 'transformer': arguments of binding.make_rotary
     gamma: float = 0.0   # the share of the residual connection counted with the block that the workload is run with
 
     @property
     def tokens(self) -> int:
         return self.N * self.L if self.kind in ("rnn", "gated", "lstm", "gru") else self.N
+
+    @property
+    def qkv_width(self) -> int:
+        """'transformer': width of a [q | k | v] row."""
+        return self.d + 2 * (self.kv_heads or self.heads) * (self.d // self.heads)
 
 
 WORKLOADS: Dict[str, Workload] = {
@@ -161,10 +168,10 @@ def weights_block(w: Workload, l: int):
 
 
 def attention_weights_block(w: Workload, j: int):
-    """(Wqkv_j [3d,d], Wo_j [d,d]) of layer j of a 'transformer' stack; Wo scaled like W2."""
+    """(Wqkv_j [qkv_width,d], Wo_j [d,d]) of layer j of a 'transformer' stack; Wo scaled like W2."""
     s1 = w.w1_std if w.w1_std > 0 else 1.0 / np.sqrt(w.d)
     s2 = (w.w2_std if w.w2_std > 0 else 1.0 / np.sqrt(w.d)) * w.w2_scale
-    return (storage_round(w, _normal(w, _T_WQKV, j, (3 * w.d, w.d), s1)),
+    return (storage_round(w, _normal(w, _T_WQKV, j, (w.qkv_width, w.d), s1)),
             storage_round(w, _normal(w, _T_WO, j, (w.d, w.d), s2)))
 
 
@@ -204,7 +211,7 @@ def make_inputs(w: Workload, tokens=None) -> Dict[str, Optional[np.ndarray]]:
         W1 = np.empty((nb, w.d_ff, w.d), np.float32)
         W2 = np.empty((nb, w.d, w.d_ff), np.float32)
         if w.kind == "transformer":
-            out["Wqkv"] = np.empty((nb, 3 * w.d, w.d), np.float32)
+            out["Wqkv"] = np.empty((nb, w.qkv_width, w.d), np.float32)
             out["Wo"] = np.empty((nb, w.d, w.d), np.float32)
 
         def fill(l):   # every block has its own generator key: order of evaluation is free
