@@ -4,26 +4,13 @@
 // times its group, row r = query r / group of head r % group: tiles of rows then hold several heads of a query, the
 // streamed keys serve all of them, dk and dv sum over the group by summing over rows, and a single query fills `group`
 // rows of a tile.
-#include "hbp_common.h"
+#include "attention_device.h"
 
 #include <cfloat>
 
 namespace hbp {
 
 namespace {
-
-constexpr float LOG2E = 1.4426950408889634f;
-
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
 
 // One sequence: its first row and its length on either side.
 struct Seq { int q0, nq, k0, nk; };
@@ -191,7 +178,7 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
         const float L = stat_of(a.lse[r * a.heads + h]);
         if (L != INFINITY) {
           p = exp2f(c * dot_rows(row_of<T>(a.q, r, h), k, a.dh) - L);
-          ds = p * (dot_rows(row_of<T>(a.dout, r, h), v, a.dh) - a.dsum[r * a.heads + h]);
+          ds = p * (dot_rows(row_of<T>(a.dout, r, h), v, a.dh) + a.dsum[r * a.heads + h]);
         }
       }
       dk.add(ds, n, row_of<T>(a.q, s.q0 + b, h), a.q.row, a.dh, lane);
@@ -218,7 +205,7 @@ __global__ __launch_bounds__(64) void packed_dq_rows_kernel(PackedAttnArgs a) {
   const Seq s = seq_of(a, sq);
   if (n < s.q0 || n >= s.q0 + s.nq) return;
   const float D = row_dsum<T>(a, n, h, threadIdx.x);
-  if (threadIdx.x == 0) a.dsum[(long)n * a.heads + h] = D;
+  if (threadIdx.x == 0) a.dsum[(long)n * a.heads + h] = -D;
   one_dq<T>(a, s, n - s.q0, h, D, threadIdx.x);
 }
 template <typename T>
@@ -229,6 +216,529 @@ __global__ __launch_bounds__(64) void packed_dkdv_rows_kernel(PackedAttnArgs a) 
   const Seq s = seq_of(a, sq);
   if (n < s.k0 || n >= s.k0 + s.nk) return;
   one_dkdv<T>(a, s, n - s.k0, hk, threadIdx.x);
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// matrix-core kernels: bf16
+// ------------------------------------------------------------------------------------------------------------
+// Which key head, sequence and tile of `per` rows (keys: `per` keys) a workgroup takes.  The key heads of a tile are next to each
+// other: all problems go on side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs
+// in turn, keep a problem's streamed tiles in one XCD's L2.
+struct Tile { int hk, t, n; Seq s; bool exists; };          // t of the sequence's n tiles
+__device__ __forceinline__ int tiles_in(int len, int per) { return (len + per - 1) / per; }
+template <bool KEYS>
+__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane) {
+  Tile x;
+  const unsigned id = blockIdx.x;
+  x.hk = (int)(id % (unsigned)a.kv_heads);
+  x.t = (int)(id / (unsigned)a.kv_heads);
+  const int* off = KEYS ? a.k_off : a.q_off;
+  const int mult = KEYS ? 1 : a.group, rows = KEYS ? a.k_rows : a.q_rows;
+  int sq = -1;
+  if (!off) {
+    x.n = tiles_in(rows / a.seqs * mult, per);
+    sq = x.t / x.n;
+    x.t -= sq * x.n;
+    if (sq >= a.seqs) sq = -1;
+  } else {
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time: a running sum of their tiles over the lanes
+      int first, n = 0;
+      if (s0 + lane < a.seqs) span_of(off, rows, a.seqs, s0 + lane, first, n);
+      n = tiles_in(n * mult, per);
+      int sum = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += up;
+      }
+      const unsigned long long past = __ballot(sum > x.t);
+      if (past) {
+        const int l = __ffsll(past) - 1;
+        sq = s0 + l;
+        x.n = __builtin_amdgcn_readlane(n, l);
+        x.t -= __builtin_amdgcn_readlane(sum, l) - x.n;
+        break;
+      }
+      x.t -= __builtin_amdgcn_readlane(sum, 63);
+    }
+  }
+  x.exists = sq >= 0;
+  if (x.exists) {
+    x.s = seq_of(a, sq);
+    x.t = __builtin_amdgcn_readfirstlane(x.t);
+    x.n = __builtin_amdgcn_readfirstlane(x.n);
+    x.s.q0 = __builtin_amdgcn_readfirstlane(x.s.q0);
+    x.s.nq = __builtin_amdgcn_readfirstlane(x.s.nq);
+    x.s.k0 = __builtin_amdgcn_readfirstlane(x.s.k0);
+    x.s.nk = __builtin_amdgcn_readfirstlane(x.s.nk);
+  }
+  return x;
+}
+// the other half's value (lanes l and l + 32 hold one row's two halves)
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// A fragment of the rows that a wavefront owns: 8 channels of this lane's row, zero past the head's width.
+__device__ __forceinline__ bf16x8 own_piece(const bf16_t* row, int kk, int dh8, int lane) {
+  const int ch = 2 * kk + (lane >> 5);
+  const bool in = ch < dh8;
+  const uint4 v = *reinterpret_cast<const uint4*>(row + 8 * (in ? ch : 0));
+  return __builtin_bit_cast(bf16x8, make_uint4(in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u));
+}
+
+// Streamed key and value tiles: a stage holds 64 keys, two tiles of 32 of k and two of v, which a workgroup's wavefronts copy together,
+// PW copies of 1 KB each.
+template <int DHP, int WAVES>
+struct KeyStream {
+  typedef Geo<DHP> G;
+  static constexpr int STAGE = 4 * G::TB;
+  static constexpr int PW = 4 * G::COPIES / WAVES;
+  unsigned off[PW];
+  const unsigned char *k, *v;
+  unsigned ldk, ldv, lds0;
+  int nk, dh8;
+  static __device__ __forceinline__ int tile(int w, int i) { return (w * PW + i) / G::COPIES; }     // k, k, v, v
+  static __device__ __forceinline__ int part(int w, int i) { return (w * PW + i) % G::COPIES; }
+  __device__ __forceinline__ KeyStream(const PackedAttnArgs& a, const Seq& s, int hk, unsigned lds, int dh8_, int w, int lane) {
+    k = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.k, s.k0, hk));
+    v = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.v, s.k0, hk));
+    ldk = (unsigned)(a.k.row * 2);
+    ldv = (unsigned)(a.v.row * 2);
+    lds0 = lds;
+    nk = s.nk;
+    dh8 = dh8_;
+#pragma unroll
+    for (int i = 0; i < PW; ++i) off[i] = copy_offset<DHP>(tile(w, i) < 2 ? ldk : ldv, part(w, i), 32, dh8, lane);
+  }
+  // keys 64 step .. into stage `at`; keys past the last repeat it
+  __device__ __forceinline__ void issue(int step, int at, int w, int lane) const {
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      const int t = tile(w, i), first = 64 * step + 32 * (t & 1);
+      const unsigned ld = t < 2 ? ldk : ldv;
+      const unsigned char* base = t < 2 ? k : v;
+      const unsigned dst = lds0 + (unsigned)at * STAGE + (unsigned)(w * PW + i) * 1024u;
+      if (first + 32 <= nk) {
+        copy16_to_lds(off[i], base + (long)first * ld, dst);
+      } else {
+        const int from = first < nk ? first : nk - 1;
+        copy16_to_lds(copy_offset<DHP>(ld, part(w, i), nk - from, dh8, lane), base + (long)from * ld, dst);
+      }
+    }
+  }
+};
+
+// The rows of a tile: row r of the sequence at this key head is query r / group of head hk group + r % group.
+struct RowPlace { int i, h; };
+__device__ __forceinline__ RowPlace place_of(const PackedAttnArgs& a, int hk, int r) {
+  RowPlace p;
+  p.i = (int)((unsigned)r / (unsigned)a.group);
+  p.h = hk * a.group + (r - p.i * a.group);
+  return p;
+}
+
+// A tile's results, scaled per row by f, to their rows (see store_tile in attention.hip: 64 bytes of a row per store).
+// row(j): where row j of the tile goes; rows_left of them.
+template <int MB, typename F>
+__device__ __forceinline__ void store_rows(F row, int rows_left, const float16v (&acc)[MB], float f, int dh, unsigned char* stg, int lane) {
+  const int r = lane & 31, hh = lane >> 5, rr = lane >> 2, ch = lane & 3;
+  bf16_t* out[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) out[u] = rr + 16 * u < rows_left ? row(rr + 16 * u) : nullptr;
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    if (32 * m >= dh) break;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      store4b(reinterpret_cast<bf16_t*>(stg + r * 64 + ((g ^ ((r >> 2) & 3)) << 4) + 8 * hh), acc[m][4 * g] * f,
+              acc[m][4 * g + 1] * f, acc[m][4 * g + 2] * f, acc[m][4 * g + 3] * f);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int w = rr + 16 * u;
+      const uint4 v = *reinterpret_cast<const uint4*>(stg + w * 64 + ((ch ^ ((w >> 2) & 3)) << 4));
+      if (out[u] && 32 * m + 8 * ch < dh) *reinterpret_cast<uint4*>(out[u] + 32 * m + 8 * ch) = v;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Infinities and NaNs: a product on the matrix cores meets every element of a tile, also those that the mask or the sequence's end
+// leaves out, and there 0 times an infinity is NaN.  A row of a result that did not come out finite is therefore computed
+// once more, term by term over what it sees.  Finite data never comes here.
+template <int MB>
+__device__ __forceinline__ float not_finite(const float16v (&acc)[MB], float t) {
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = fmaf(acc[m][r], 0.f, t);
+  return t;
+}
+template <typename F>
+__device__ __forceinline__ void redo_rows(float t, int rows_left, F f) {
+  const unsigned long long b = __ballot(t != t);
+  unsigned rows = (unsigned)b | (unsigned)(b >> 32);
+  if (rows_left < 32) rows &= (1u << rows_left) - 1u;
+  if (rows == 0) return;
+  copies_in_flight<0>();                                   // (the tile's own stores, which these replace)
+  for (; rows != 0; rows &= rows - 1) f(__ffs((int)rows) - 1);
+}
+
+constexpr int FWD_WAVES = 8;
+template <int DHP> constexpr int key_stages() { return DHP == 128 ? 3 : 4; }
+
+// Forward.  A workgroup of eight wavefronts owns 256 rows, a wavefront 32 of them: a lane holds one row of q and half of that row's
+// scores, so the running maximum and sum are scalars of the lane; the scores leave the first product in the places from which the
+// second takes them.  Keys and values come in steps of 64 through a ring of stages.  The maximum that the exponents are taken
+// from moves only when a row's has grown by more than a factor of 2^8 (probabilities then reach 2^8, sums 2^8 times the keys:
+// far inside fp32, and bf16 rounds relatively), so the output is rarely rescaled.
+template <int DHP>
+__global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_fwd_mfma_kernel(PackedAttnArgs a) {
+  typedef Geo<DHP> G;
+  typedef KeyStream<DHP, FWD_WAVES> KS;
+  constexpr int NST = key_stages<DHP>();
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST * KS::STAGE];
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  Tile x = find_tile<false>(a, 32 * FWD_WAVES, lane);
+  if (!x.exists) return;
+  x.t = x.n - 1 - x.t;                                     // (causal: long rows first)
+  const int R = x.s.nq * a.group, r0 = 32 * FWD_WAVES * x.t, w0 = r0 + 32 * wave;
+  const int rows_left = R - w0;                            // of this wavefront's 32; none: it only copies
+  const int dh8 = a.dh >> 3;
+  auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
+  const int last = (R < r0 + 32 * FWD_WAVES ? R : r0 + 32 * FWD_WAVES) - 1;
+  const int steps = (seen(last) + 63) >> 6;
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const KS ks(a, x.s, x.hk, lds0, dh8, wave, lane);
+  for (int i = 0; i < NST - 1 && i < steps; ++i) ks.issue(i, i, wave, lane);
+  const int r = rows_left > 0 ? w0 + ((lane & 31) < rows_left ? (lane & 31) : rows_left - 1) : R - 1;
+  const RowPlace me = place_of(a, x.hk, r);
+  const bf16_t* qrow = row_of<bf16_t>(a.q, x.s.q0 + me.i, me.h);
+  bf16x8 fq[G::KK];
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) fq[kk] = own_piece(qrow, kk, dh8, lane);
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) landed(fq[kk]);
+  const int mine = seen_by(x.s, me.i, a.causal);           // keys that this lane's row sees
+  const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
+  const float c = a.scale * LOG2E;
+  float16v o[G::MB];
+  zero_acc(o);
+  float m = -FLT_MAX, l = 0.f;                             // m: in units of the exponent; l: this half's sum
+  auto step = [&](int i, int at, bool masked) __attribute__((always_inline)) {
+    const unsigned char* tk = ring + at * KS::STAGE;
+    const unsigned char* tv = tk + 2 * G::TB;
+    float16v s[2];
+    zero_acc(s);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) s[b] = mfma(frag_cols_lds<DHP>(tk + b * G::TB, kk, lane), fq[kk], s[b]);
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (64 * i + 32 * b + tile_row_of(e, hh) >= mine) s[b][e] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
+    top = fmaxf(top, other_half(top)) * c;
+    if (__any(top > m + 8.f)) {
+      const float mn = fmaxf(m, top), alpha = fast_exp2(m - mn);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < G::MB; ++mb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[mb][e] *= alpha;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = fast_exp2(fmaf(s[b][e], c, -m));
+        l += p[e];
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 pt = pack8(p + 8 * t);                // rounded to bf16: the matrix cores' operand
+#pragma unroll
+        for (int mb = 0; mb < G::MB; ++mb) o[mb] = mfma(frag_rows_lds<DHP>(tv + b * G::TB, mb, t, lane), pt, o[mb]);
+      }
+    }
+  };
+  int at = 0;
+  for (int i = 0; i < steps; ++i) {
+    if (i + NST - 2 < steps) copies_in_flight<KS::PW * (NST - 2)>();
+    else copies_in_flight<0>();
+    workgroup_handover();
+    if (i + NST - 1 < steps) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+    if (64 * i < most) step(i, at, 64 * i + 64 > fewest);
+    at = at == NST - 1 ? 0 : at + 1;
+  }
+  __syncthreads();                                         // the ring is free: results leave through it
+  if (rows_left <= 0) return;
+  l += other_half(l);
+  const float f = l == 0.f ? 0.f : 1.f / l;
+  store_rows([&](int j) __attribute__((always_inline)) {
+    const RowPlace q = place_of(a, x.hk, w0 + j);
+    return row_out<bf16_t>(a.o, x.s.q0 + q.i, q.h);
+  }, rows_left, o, f, a.dh, ring + wave * 2048, lane);
+  if (lane < 32 && lane < rows_left) a.lse[(long)(x.s.q0 + me.i) * a.heads + me.h] = l == 0.f ? -INFINITY : m + log2f(l);
+  redo_rows(not_finite(o, f * 0.f), rows_left, [&](int j) {
+    const RowPlace q = place_of(a, x.hk, w0 + j);
+    one_forward<bf16_t>(a, x.s, q.i, q.h, lane);
+  });
+}
+
+// dq, and minus D = sum_c dout (.) o of every row for the other kernel.  As the forward pass: a lane holds a row of q and of dout,
+// dS leaves the first two products in the places from which the third takes it.
+template <int DHP>
+__global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(PackedAttnArgs a) {
+  typedef Geo<DHP> G;
+  typedef KeyStream<DHP, FWD_WAVES> KS;
+  constexpr int NST = key_stages<DHP>();
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST * KS::STAGE];
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  Tile x = find_tile<false>(a, 32 * FWD_WAVES, lane);
+  if (!x.exists) return;
+  x.t = x.n - 1 - x.t;
+  const int R = x.s.nq * a.group, r0 = 32 * FWD_WAVES * x.t, w0 = r0 + 32 * wave;
+  const int rows_left = R - w0;
+  const int dh8 = a.dh >> 3;
+  auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
+  const int last = (R < r0 + 32 * FWD_WAVES ? R : r0 + 32 * FWD_WAVES) - 1;
+  const int steps = (seen(last) + 63) >> 6;
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const KS ks(a, x.s, x.hk, lds0, dh8, wave, lane);
+  for (int i = 0; i < NST - 1 && i < steps; ++i) ks.issue(i, i, wave, lane);
+  const int r = rows_left > 0 ? w0 + ((lane & 31) < rows_left ? (lane & 31) : rows_left - 1) : R - 1;
+  const RowPlace me = place_of(a, x.hk, r);
+  const long n = x.s.q0 + me.i;
+  const bf16_t* qrow = row_of<bf16_t>(a.q, n, me.h);
+  const bf16_t* grow = row_of<bf16_t>(a.dout, n, me.h);
+  const bf16_t* orow = row_of<bf16_t>(a.o, n, me.h);
+  bf16x8 fq[G::KK], fg[G::KK];
+  float D = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) {
+    fq[kk] = own_piece(qrow, kk, dh8, lane);
+    fg[kk] = own_piece(grow, kk, dh8, lane);
+    D += dot8(fg[kk], own_piece(orow, kk, dh8, lane));
+  }
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) { landed(fq[kk]); landed(fg[kk]); }
+  D += other_half(D);
+  float L = stat_of(a.lse[n * a.heads + me.h]);
+  landed(L);
+  if (rows_left > 0 && lane < 32 && lane < rows_left) a.dsum[n * a.heads + me.h] = -D;
+  const int mine = seen_by(x.s, me.i, a.causal);
+  const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
+  const float c = a.scale * LOG2E;
+  float16v dq[G::MB];
+  zero_acc(dq);
+  auto step = [&](int i, int at, bool masked) __attribute__((always_inline)) {
+    const unsigned char* tk = ring + at * KS::STAGE;
+    const unsigned char* tv = tk + 2 * G::TB;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float16v s[1], dp[1];
+      zero_acc(s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[0][e] = -D;
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) {
+        s[0] = mfma(frag_cols_lds<DHP>(tk + b * G::TB, kk, lane), fq[kk], s[0]);
+        dp[0] = mfma(frag_cols_lds<DHP>(tv + b * G::TB, kk, lane), fg[kk], dp[0]);
+      }
+      float ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = fast_exp2(fmaf(s[0][e], c, -L));
+        ds[e] = p * dp[0][e];
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (64 * i + 32 * b + tile_row_of(e, hh) >= mine) ds[e] = 0.f;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 dst = pack8(ds + 8 * t);
+#pragma unroll
+        for (int mb = 0; mb < G::MB; ++mb) dq[mb] = mfma(frag_rows_lds<DHP>(tk + b * G::TB, mb, t, lane), dst, dq[mb]);
+      }
+    }
+  };
+  int at = 0;
+  for (int i = 0; i < steps; ++i) {
+    if (i + NST - 2 < steps) copies_in_flight<KS::PW * (NST - 2)>();
+    else copies_in_flight<0>();
+    workgroup_handover();
+    if (i + NST - 1 < steps) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+    if (64 * i < most) step(i, at, 64 * i + 64 > fewest);
+    at = at == NST - 1 ? 0 : at + 1;
+  }
+  __syncthreads();
+  if (rows_left <= 0) return;
+  store_rows([&](int j) __attribute__((always_inline)) {
+    const RowPlace q = place_of(a, x.hk, w0 + j);
+    return row_out<bf16_t>(a.dq, x.s.q0 + q.i, q.h);
+  }, rows_left, dq, a.scale, a.dh, ring + wave * 2048, lane);
+  redo_rows(not_finite(dq, 0.f), rows_left, [&](int j) {
+    const RowPlace q = place_of(a, x.hk, w0 + j);
+    one_dq<bf16_t>(a, x.s, q.i, q.h, row_dsum<bf16_t>(a, x.s.q0 + q.i, q.h, lane), lane);
+  });
+}
+
+constexpr int KV_WAVES = 4;
+template <int DHP> constexpr int row_stages() { return DHP == 128 ? 4 : 4; }
+
+// dk, dv.  A workgroup of four wavefronts owns 128 keys of a key head, a wavefront 32 of them: a lane holds one key's k and v and
+// half of that key's probabilities.  The rows that see them, q and dout in tiles of 32 with their statistics, come through a ring.
+template <int DHP>
+__global__ __launch_bounds__(64 * KV_WAVES, DHP == 128 ? 1 : 2) void packed_dkdv_mfma_kernel(PackedAttnArgs a) {
+  typedef Geo<DHP> G;
+  constexpr int NST = row_stages<DHP>();
+  constexpr int PW = 2 * G::COPIES / KV_WAVES;             // copies of a pair of tiles by one wavefront
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST][2][G::TB];     // [stage][q | dout]
+  __shared__ __attribute__((aligned(256))) float stats[NST][2][64];              // [stage][lse | -D]: 32 rows, then their copies
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const Tile x = find_tile<true>(a, 32 * KV_WAVES, lane);
+  if (!x.exists) return;
+  const int k0 = 32 * KV_WAVES * x.t, w0 = k0 + 32 * wave;
+  const int keys_left = x.s.nk - w0;
+  const int dh8 = a.dh >> 3;
+  const int R = x.s.nq * a.group, shift = x.s.nk - x.s.nq;
+  // the first row that sees a key: query max(0, key - shift)
+  auto first_row = [&](int key) __attribute__((always_inline)) {
+    if (!a.causal) return 0;
+    const int i = key - shift;
+    return i <= 0 ? 0 : i * a.group;
+  };
+  const int from = first_row(k0) >> 5;                     // first tile of 32 rows
+  const int steps = ((R + 31) >> 5) - from;
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const unsigned lds1 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(stats));
+  auto issue = [&](int i, int at) __attribute__((always_inline)) {
+    const int first = 32 * (from + i);
+#pragma unroll
+    for (int u = 0; u < PW; ++u) {
+      const int ci = wave * PW + u, t = ci / G::COPIES, part = ci % G::COPIES;
+      const int lr = G::RPC * part + lane / G::CPR;
+      int ch = (lane % G::CPR) ^ G::swz(lr);
+      ch = ch < dh8 ? ch : dh8 - 1;
+      const int r = first + lr < R ? first + lr : R - 1;
+      const RowPlace q = place_of(a, x.hk, r);
+      const bf16_t* src = row_of<bf16_t>(t ? a.dout : a.q, x.s.q0 + q.i, q.h) + 8 * ch;
+      copy16_from_to_lds(src, lds0 + (unsigned)at * (2u * G::TB) + (unsigned)ci * 1024u);
+    }
+    const int r = first + (lane & 31) < R ? first + (lane & 31) : R - 1;
+    const RowPlace q = place_of(a, x.hk, r);
+    const long e = (long)(x.s.q0 + q.i) * a.heads + q.h;
+    // (every wavefront copies a statistic: the waits count the same for all)
+    copy4_to_lds((wave & 1 ? a.dsum : a.lse) + e, lds1 + (unsigned)at * 512u + (wave & 1) * 256u);
+  };
+  for (int i = 0; i < NST - 1 && i < steps; ++i) issue(i, i);
+  const int key = keys_left > 0 ? w0 + ((lane & 31) < keys_left ? (lane & 31) : keys_left - 1) : x.s.nk - 1;
+  const bf16_t* krow = row_of<bf16_t>(a.k, x.s.k0 + key, x.hk);
+  const bf16_t* vrow = row_of<bf16_t>(a.v, x.s.k0 + key, x.hk);
+  bf16x8 fk[G::KK], fv[G::KK];
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) { fk[kk] = own_piece(krow, kk, dh8, lane); fv[kk] = own_piece(vrow, kk, dh8, lane); }
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) { landed(fk[kk]); landed(fv[kk]); }
+  const int mine = first_row(key);                         // the first row that sees this lane's key
+  const int begin = keys_left > 0 ? first_row(w0) : R, all = keys_left > 0 ? first_row(w0 + (keys_left < 32 ? keys_left : 32) - 1) : R;
+  const float c = a.scale * LOG2E;
+  float16v dk[G::MB], dv[G::MB];
+  zero_acc(dk);
+  zero_acc(dv);
+  auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
+    const unsigned char* tq = ring[at][0];
+    const unsigned char* tg = ring[at][1];
+    float16v s[1], dp;
+    zero_acc(s);
+    float L[16];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float4 u = *reinterpret_cast<const float4*>(&stats[at][0][8 * g + 4 * hh]);
+      const float4 v = *reinterpret_cast<const float4*>(&stats[at][1][8 * g + 4 * hh]);
+      L[4 * g] = u.x; L[4 * g + 1] = u.y; L[4 * g + 2] = u.z; L[4 * g + 3] = u.w;
+      dp[4 * g] = v.x; dp[4 * g + 1] = v.y; dp[4 * g + 2] = v.z; dp[4 * g + 3] = v.w;
+    }
+#pragma unroll
+    for (int kk = 0; kk < G::KK; ++kk) {
+      s[0] = mfma(frag_cols_lds<DHP>(tq, kk, lane), fk[kk], s[0]);
+      dp = mfma(frag_cols_lds<DHP>(tg, kk, lane), fv[kk], dp);
+    }
+    float p[16], ds[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = fast_exp2(fmaf(s[0][e], c, -stat_of(L[e])));
+      ds[e] = p[e] * dp[e];
+    }
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int r = first + tile_row_of(e, hh);
+        if (r < mine || r >= R) p[e] = ds[e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 pt = pack8(p + 8 * t), dst = pack8(ds + 8 * t);
+#pragma unroll
+      for (int mb = 0; mb < G::MB; ++mb) {
+        dv[mb] = mfma(frag_rows_lds<DHP>(tg, mb, t, lane), pt, dv[mb]);
+        dk[mb] = mfma(frag_rows_lds<DHP>(tq, mb, t, lane), dst, dk[mb]);
+      }
+    }
+  };
+  int at = 0;
+  for (int i = 0; i < steps; ++i) {
+    if (i + NST - 2 < steps) copies_in_flight<(PW + 1) * (NST - 2)>();
+    else copies_in_flight<0>();
+    workgroup_handover();
+    if (i + NST - 1 < steps) issue(i + NST - 1, at == 0 ? NST - 1 : at - 1);
+    const int first = 32 * (from + i);
+    if (first + 32 > begin && keys_left > 0) step(first, at, first < all || first + 32 > R);
+    at = at == NST - 1 ? 0 : at + 1;
+  }
+  __syncthreads();
+  if (keys_left <= 0) return;
+  unsigned char* stg = &ring[0][0][0] + wave * 2048;
+  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, x.s.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale,
+             a.dh, stg, lane);
+  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, x.s.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, a.dh,
+             stg, lane);
+  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, lane); });
+}
+
+// workgroups for tiles of `per` rows (keys)
+template <bool KEYS>
+unsigned tile_grid(const PackedAttnArgs& a, int per) {
+  const long rows = KEYS ? a.k_rows : (long)a.q_rows * a.group;
+  if (rows == 0) return 0;
+  const bool equal = KEYS ? !a.k_off : !a.q_off;
+  const long tiles = equal ? a.seqs * ((rows / a.seqs + per - 1) / per) : rows / per + a.seqs;
+  return (unsigned)(tiles * a.kv_heads);
+}
+template <int DHP>
+hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
+  if (const unsigned grid = tile_grid<false>(a, 32 * FWD_WAVES)) packed_fwd_mfma_kernel<DHP><<<grid, 64 * FWD_WAVES, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int DHP>
+hipError_t bwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
+  if (const unsigned grid = tile_grid<false>(a, 32 * FWD_WAVES)) packed_dq_mfma_kernel<DHP><<<grid, 64 * FWD_WAVES, 0, s>>>(a);
+  if (const unsigned grid = tile_grid<true>(a, 32 * KV_WAVES)) packed_dkdv_mfma_kernel<DHP><<<grid, 64 * KV_WAVES, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename T>
@@ -250,12 +760,12 @@ size_t packed_attn_ws_bytes(int, const PackedAttnArgs& a) {
   return ((size_t)a.q_rows * a.heads * 4 + 255) / 256 * 256;
 }
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void*, hipStream_t s) {
-  return dtype == 0 ? fwd_t<float>(a, s) : fwd_t<bf16_t>(a, s);
+  return dtype == 0 ? fwd_t<float>(a, s) : a.dh <= 64 ? fwd_mfma<64>(a, s) : fwd_mfma<128>(a, s);
 }
 hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s) {
   PackedAttnArgs b = a;
   b.dsum = reinterpret_cast<float*>(workspace);
-  return dtype == 0 ? bwd_t<float>(b, s) : bwd_t<bf16_t>(b, s);
+  return dtype == 0 ? bwd_t<float>(b, s) : a.dh <= 64 ? bwd_mfma<64>(b, s) : bwd_mfma<128>(b, s);
 }
 
 }  // namespace hbp

@@ -241,7 +241,7 @@ struct HeadRows { void* p; long row, head; };
 struct PackedAttnArgs {
   HeadRows q, k, v, o, dout, dq, dk, dv;
   float* lse;               // [q_rows, heads]
-  float* dsum;              // [q_rows, heads], workspace: rowsum(dout (.) o)
+  float* dsum;              // [q_rows, heads], workspace: minus rowsum(dout (.) o)
   const int* q_off;         // [seqs + 1] or NULL: equal lengths
   const int* k_off;
   int seqs, q_rows, k_rows;
