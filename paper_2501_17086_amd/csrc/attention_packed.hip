@@ -175,9 +175,9 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
       const int n = s.nq - b < 64 ? s.nq - b : 64;
       if (lane < n) {
         const long r = s.q0 + b + lane;
-        const float L = stat_of(a.lse[r * a.heads + h]);
-        if (L != INFINITY) {
-          p = exp2f(c * dot_rows(row_of<T>(a.q, r, h), k, a.dh) - L);
+        const float L = a.nlse[r * a.heads + h];
+        if (L != -INFINITY) {
+          p = exp2f(c * dot_rows(row_of<T>(a.q, r, h), k, a.dh) + L);
           ds = p * (dot_rows(row_of<T>(a.dout, r, h), v, a.dh) + a.dsum[r * a.heads + h]);
         }
       }
@@ -205,7 +205,10 @@ __global__ __launch_bounds__(64) void packed_dq_rows_kernel(PackedAttnArgs a) {
   const Seq s = seq_of(a, sq);
   if (n < s.q0 || n >= s.q0 + s.nq) return;
   const float D = row_dsum<T>(a, n, h, threadIdx.x);
-  if (threadIdx.x == 0) a.dsum[(long)n * a.heads + h] = -D;
+  if (threadIdx.x == 0) {
+    a.dsum[(long)n * a.heads + h] = -D;
+    a.nlse[(long)n * a.heads + h] = -stat_of(a.lse[(long)n * a.heads + h]);
+  }
   one_dq<T>(a, s, n - s.q0, h, D, threadIdx.x);
 }
 template <typename T>
@@ -276,6 +279,36 @@ __device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int 
 }
 // the other half's value (lanes l and l + 32 hold one row's two halves)
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// Fragments by LDS byte addresses.  The tiles' chunk swizzle is an XOR of address bits, so one register per direction holds all there
+// is of a lane in an address: a step adds its stage, an XOR with a constant picks the fragment, and tiles of the same stage
+// are constant offsets.  (Addresses formed from the row and the chunk each time cost an addition per read, a third of
+// the forward pass's vector instructions.)
+template <int DHP>
+struct Frags {
+  typedef Geo<DHP> G;
+  typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) const uint4v* chunk_p;
+  typedef __attribute__((address_space(3))) short4v* quad_p;
+  static __device__ __forceinline__ unsigned cols_lane(int lane) {
+    const int r = lane & 31;
+    return (unsigned)(r * G::RB + (((lane >> 5) ^ G::swz(r)) << 4));
+  }
+  static __device__ __forceinline__ unsigned rows_lane(int lane) {
+    const int q = lane & 15, e = 16 * ((lane >> 4) & 1) + 4 * (q & 3), r = 4 * (lane >> 5) + (q >> 2);
+    return (unsigned)(r * G::RB + (((e >> 3) ^ G::swz(r)) << 4) + (e & 7) * 2);
+  }
+  // frag_cols_lds and frag_rows_lds of the tile at `tile` (a constant) behind the address `at` of a stage and lane
+  static __device__ __forceinline__ bf16x8 cols(unsigned at, unsigned tile, int kk) {
+    const uint4v v = *(chunk_p)(uintptr_t)((at ^ (32u * kk)) + tile);
+    return __builtin_bit_cast(bf16x8, v);
+  }
+  static __device__ __forceinline__ bf16x8 rows(unsigned at, unsigned tile, int m, int t) {
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_p)(uintptr_t)((at ^ (64u * m)) + (tile + 16 * t * G::RB)));
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_p)(uintptr_t)((at ^ (64u * m + 32u)) + (tile + (16 * t + 8) * G::RB)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
 
 // A fragment of the rows that a wavefront owns: 8 channels of this lane's row, zero past the head's width.
 __device__ __forceinline__ bf16x8 own_piece(const bf16_t* row, int kk, int dh8, int lane) {
@@ -422,18 +455,18 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_fwd_mfma_kernel(Pack
   const int mine = seen_by(x.s, me.i, a.causal);           // keys that this lane's row sees
   const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
   const float c = a.scale * LOG2E;
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rv = lds0 + Frags<DHP>::rows_lane(lane);
   float16v o[G::MB];
   zero_acc(o);
   float m = -FLT_MAX, l = 0.f;                             // m: in units of the exponent; l: this half's sum
   auto step = [&](int i, int at, bool masked) __attribute__((always_inline)) {
-    const unsigned char* tk = ring + at * KS::STAGE;
-    const unsigned char* tv = tk + 2 * G::TB;
+    const unsigned tk = ck + (unsigned)at * KS::STAGE, tv = rv + (unsigned)at * KS::STAGE;
     float16v s[2];
     zero_acc(s);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int kk = 0; kk < G::KK; ++kk) s[b] = mfma(frag_cols_lds<DHP>(tk + b * G::TB, kk, lane), fq[kk], s[b]);
+      for (int kk = 0; kk < G::KK; ++kk) s[b] = mfma(Frags<DHP>::cols(tk, b * G::TB, kk), fq[kk], s[b]);
     if (masked) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -466,7 +499,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_fwd_mfma_kernel(Pack
       for (int t = 0; t < 2; ++t) {
         const bf16x8 pt = pack8(p + 8 * t);                // rounded to bf16: the matrix cores' operand
 #pragma unroll
-        for (int mb = 0; mb < G::MB; ++mb) o[mb] = mfma(frag_rows_lds<DHP>(tv + b * G::TB, mb, t, lane), pt, o[mb]);
+        for (int mb = 0; mb < G::MB; ++mb) o[mb] = mfma(Frags<DHP>::rows(tv, (2 + b) * G::TB, mb, t), pt, o[mb]);
       }
     }
   };
@@ -535,15 +568,18 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(Packe
   D += other_half(D);
   float L = stat_of(a.lse[n * a.heads + me.h]);
   landed(L);
-  if (rows_left > 0 && lane < 32 && lane < rows_left) a.dsum[n * a.heads + me.h] = -D;
+  if (rows_left > 0 && lane < 32 && lane < rows_left) {
+    a.dsum[n * a.heads + me.h] = -D;
+    a.nlse[n * a.heads + me.h] = -L;
+  }
   const int mine = seen_by(x.s, me.i, a.causal);
   const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
   const float c = a.scale * LOG2E;
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rk = lds0 + Frags<DHP>::rows_lane(lane);
   float16v dq[G::MB];
   zero_acc(dq);
   auto step = [&](int i, int at, bool masked) __attribute__((always_inline)) {
-    const unsigned char* tk = ring + at * KS::STAGE;
-    const unsigned char* tv = tk + 2 * G::TB;
+    const unsigned tc = ck + (unsigned)at * KS::STAGE, tr = rk + (unsigned)at * KS::STAGE;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       float16v s[1], dp[1];
@@ -552,8 +588,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(Packe
       for (int e = 0; e < 16; ++e) dp[0][e] = -D;
 #pragma unroll
       for (int kk = 0; kk < G::KK; ++kk) {
-        s[0] = mfma(frag_cols_lds<DHP>(tk + b * G::TB, kk, lane), fq[kk], s[0]);
-        dp[0] = mfma(frag_cols_lds<DHP>(tv + b * G::TB, kk, lane), fg[kk], dp[0]);
+        s[0] = mfma(Frags<DHP>::cols(tc, b * G::TB, kk), fq[kk], s[0]);
+        dp[0] = mfma(Frags<DHP>::cols(tc, (2 + b) * G::TB, kk), fg[kk], dp[0]);
       }
       float ds[16];
 #pragma unroll
@@ -562,7 +598,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(Packe
         ds[e] = p * dp[0][e];
       }
       if (masked) {
-#pragma unroll
+  #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (64 * i + 32 * b + tile_row_of(e, hh) >= mine) ds[e] = 0.f;
       }
@@ -570,7 +606,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(Packe
       for (int t = 0; t < 2; ++t) {
         const bf16x8 dst = pack8(ds + 8 * t);
 #pragma unroll
-        for (int mb = 0; mb < G::MB; ++mb) dq[mb] = mfma(frag_rows_lds<DHP>(tk + b * G::TB, mb, t, lane), dst, dq[mb]);
+        for (int mb = 0; mb < G::MB; ++mb) dq[mb] = mfma(Frags<DHP>::rows(tr, b * G::TB, mb, t), dst, dq[mb]);
       }
     }
   };
@@ -595,124 +631,183 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(Packe
   });
 }
 
-constexpr int KV_WAVES = 4;
-template <int DHP> constexpr int row_stages() { return DHP == 128 ? 4 : 4; }
-
-// dk, dv.  A workgroup of four wavefronts owns 128 keys of a key head, a wavefront 32 of them: a lane holds one key's k and v and
-// half of that key's probabilities.  The rows that see them, q and dout in tiles of 32 with their statistics, come through a ring.
+// dk, dv.  A workgroup owns 128 keys of a key head, and eight wavefronts: four times 32 keys, twice, for every other tile of 32
+// queries; the two halves' sums meet in LDS at the end.  A lane holds one key's k and v and half of that key's probabilities.
+// (128 keys with four wavefronts: half the wavefronts on a SIMD, or two workgroups on a compute unit that a causal mask leaves
+// unequally long; 256 keys: half as many workgroups to share out.)  Queries come from the last one down, all heads of the group
+// for a tile of queries before the next tile: whatever the mask leaves them, the workgroups of a key head begin with the same
+// tiles and stay in step, so that the tiles come from the XCD's L2.
+// At 128 channels k stays in LDS, which leaves registers for two wavefronts on every SIMD.
+constexpr int KV_KEYS = 128, KV_WAVES = 8;
 template <int DHP>
-__global__ __launch_bounds__(64 * KV_WAVES, DHP == 128 ? 1 : 2) void packed_dkdv_mfma_kernel(PackedAttnArgs a) {
+__global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(PackedAttnArgs a) {
   typedef Geo<DHP> G;
-  constexpr int NST = row_stages<DHP>();
-  constexpr int PW = 2 * G::COPIES / KV_WAVES;             // copies of a pair of tiles by one wavefront
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST][2][G::TB];     // [stage][q | dout]
-  __shared__ __attribute__((aligned(256))) float stats[NST][2][64];              // [stage][lse | -D]: 32 rows, then their copies
+  constexpr bool KLDS = DHP == 128;
+  constexpr int NST = 3;
+  constexpr int STAGE = 4 * G::TB;                         // two tiles of q, two of dout
+  constexpr int PW = 4 * G::COPIES / KV_WAVES;             // copies of a stage by one wavefront
+  constexpr int SUMS = 4 * G::MB * 16 * 64 * 4;            // the sums of four wavefronts, dk or dv
+  constexpr int RING = NST * STAGE + (KLDS ? 4 * G::TB : 0);
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING > SUMS ? RING : SUMS];
+  __shared__ __attribute__((aligned(256))) float stats[NST][2][2][64];           // [stage][tile][-lse | -D][32 rows, and again]
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const Tile x = find_tile<true>(a, 32 * KV_WAVES, lane);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), turn = wave >> 2;
+  const Tile x = find_tile<true>(a, KV_KEYS, lane);
   if (!x.exists) return;
-  const int k0 = 32 * KV_WAVES * x.t, w0 = k0 + 32 * wave;
+  const int k0 = KV_KEYS * x.t, w0 = k0 + 32 * (wave & 3);
   const int keys_left = x.s.nk - w0;
   const int dh8 = a.dh >> 3;
-  const int R = x.s.nq * a.group, shift = x.s.nk - x.s.nq;
-  // the first row that sees a key: query max(0, key - shift)
-  auto first_row = [&](int key) __attribute__((always_inline)) {
-    if (!a.causal) return 0;
+  const int nq = x.s.nq, shift = x.s.nk - nq;
+  // the first query that sees a key (causal; the last query sees the last key)
+  auto first_query = [&](int key) __attribute__((always_inline)) {
     const int i = key - shift;
-    return i <= 0 ? 0 : i * a.group;
+    return !a.causal || i < 0 ? 0 : i;
   };
-  const int from = first_row(k0) >> 5;                     // first tile of 32 rows
-  const int steps = ((R + 31) >> 5) - from;
+  const int top = (nq - 1) >> 5;                           // last tile of queries
+  const int tiles = nq > 0 ? (top + 1 - (first_query(k0) >> 5)) * a.group : 0;     // times heads
+  const int steps = (tiles + 1) >> 1;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const unsigned lds1 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(stats));
-  auto issue = [&](int i, int at) __attribute__((always_inline)) {
-    const int first = 32 * (from + i);
+  const unsigned ldq = (unsigned)(a.q.row * 2), ldg = (unsigned)(a.dout.row * 2);
+  // copy u of this wavefront: of tile (q, q, dout, dout) wave PW / COPIES ..., the same one for all of them
+  static_assert(G::COPIES % PW == 0, "a wavefront's copies are of one tile");
+  const int ct = wave * PW / G::COPIES, cp = wave * PW % G::COPIES;
+  const unsigned ld = ct < 2 ? ldq : ldg;
+  unsigned off[PW];
 #pragma unroll
-    for (int u = 0; u < PW; ++u) {
-      const int ci = wave * PW + u, t = ci / G::COPIES, part = ci % G::COPIES;
-      const int lr = G::RPC * part + lane / G::CPR;
-      int ch = (lane % G::CPR) ^ G::swz(lr);
-      ch = ch < dh8 ? ch : dh8 - 1;
-      const int r = first + lr < R ? first + lr : R - 1;
-      const RowPlace q = place_of(a, x.hk, r);
-      const bf16_t* src = row_of<bf16_t>(t ? a.dout : a.q, x.s.q0 + q.i, q.h) + 8 * ch;
-      copy16_from_to_lds(src, lds0 + (unsigned)at * (2u * G::TB) + (unsigned)ci * 1024u);
+  for (int u = 0; u < PW; ++u) off[u] = copy_offset<DHP>(ld, cp + u, 32, dh8, lane);
+  int ih = 0, iq = top;                                    // the next tile to ask for: its head of the group, its tile of queries
+  auto ask = [&](int at) __attribute__((always_inline)) {
+    int h[2], t[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {                          // (an odd number of tiles: one that nobody reads, the first one below or tile 0)
+      h[b] = x.hk * a.group + ih;
+      t[b] = iq < 0 ? 0 : iq;
+      if (++ih == a.group) { ih = 0; --iq; }
     }
-    const int r = first + (lane & 31) < R ? first + (lane & 31) : R - 1;
-    const RowPlace q = place_of(a, x.hk, r);
-    const long e = (long)(x.s.q0 + q.i) * a.heads + q.h;
+    {
+      const int b = ct & 1, first = 32 * (b ? t[1] : t[0]), left = nq - first;
+      const unsigned char* base = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(ct < 2 ? a.q : a.dout, x.s.q0 + first, b ? h[1] : h[0]));
+      const unsigned dst = lds0 + (unsigned)at * STAGE + (unsigned)(wave * PW) * 1024u;
+      if (left >= 32) {
+#pragma unroll
+        for (int u = 0; u < PW; ++u) copy16_to_lds(off[u], base, dst + 1024u * u);
+      } else {
+#pragma unroll
+        for (int u = 0; u < PW; ++u) copy16_to_lds(copy_offset<DHP>(ld, cp + u, left, dh8, lane), base, dst + 1024u * u);
+      }
+    }
     // (every wavefront copies a statistic: the waits count the same for all)
-    copy4_to_lds((wave & 1 ? a.dsum : a.lse) + e, lds1 + (unsigned)at * 512u + (wave & 1) * 256u);
+    const int b = (wave >> 1) & 1, first = 32 * (b ? t[1] : t[0]), r = first + (lane & 31) < nq ? first + (lane & 31) : nq - 1;
+    copy4_to_lds((wave & 1 ? a.dsum : a.nlse) + (long)(x.s.q0 + r) * a.heads + (b ? h[1] : h[0]),
+                 lds1 + (unsigned)at * 1024u + (unsigned)(wave & 3) * 256u);
   };
-  for (int i = 0; i < NST - 1 && i < steps; ++i) issue(i, i);
+  for (int i = 0; i < NST - 1 && i < steps; ++i) ask(i);
   const int key = keys_left > 0 ? w0 + ((lane & 31) < keys_left ? (lane & 31) : keys_left - 1) : x.s.nk - 1;
   const bf16_t* krow = row_of<bf16_t>(a.k, x.s.k0 + key, x.hk);
   const bf16_t* vrow = row_of<bf16_t>(a.v, x.s.k0 + key, x.hk);
+  const unsigned cl = Frags<DHP>::cols_lane(lane), cq = lds0 + cl + (unsigned)turn * G::TB;
+  const unsigned rq = lds0 + Frags<DHP>::rows_lane(lane) + (unsigned)turn * G::TB;
+  const unsigned kl = lds0 + NST * STAGE + (unsigned)(wave & 3) * G::TB + cl;
   bf16x8 fk[G::KK], fv[G::KK];
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) { fk[kk] = own_piece(krow, kk, dh8, lane); fv[kk] = own_piece(vrow, kk, dh8, lane); }
 #pragma unroll
-  for (int kk = 0; kk < G::KK; ++kk) { landed(fk[kk]); landed(fv[kk]); }
-  const int mine = first_row(key);                         // the first row that sees this lane's key
-  const int begin = keys_left > 0 ? first_row(w0) : R, all = keys_left > 0 ? first_row(w0 + (keys_left < 32 ? keys_left : 32) - 1) : R;
+  for (int kk = 0; kk < G::KK; ++kk) {
+    landed(fk[kk]);
+    landed(fv[kk]);
+    // (both wavefronts of these keys write the same)
+    if (KLDS) put_cols_lds<DHP>(ring + NST * STAGE + (wave & 3) * G::TB, kk, lane, fk[kk]);
+  }
+  const int mine = first_query(key);                       // the first query that sees this lane's key
+  const int begin = keys_left > 0 ? first_query(w0) : nq, all = keys_left > 0 ? first_query(w0 + (keys_left < 32 ? keys_left : 32) - 1) : nq;
   const float c = a.scale * LOG2E;
   float16v dk[G::MB], dv[G::MB];
   zero_acc(dk);
   zero_acc(dv);
   auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
-    const unsigned char* tq = ring[at][0];
-    const unsigned char* tg = ring[at][1];
+    const unsigned tc = cq + (unsigned)at * STAGE, tr = rq + (unsigned)at * STAGE;
     float16v s[1], dp;
+    float p[16];
     zero_acc(s);
-    float L[16];
+#pragma unroll
+    for (int kk = 0; kk < G::KK; ++kk) s[0] = mfma(Frags<DHP>::cols(tc, 0, kk), KLDS ? Frags<DHP>::cols(kl, 0, kk) : fk[kk], s[0]);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const float4 u = *reinterpret_cast<const float4*>(&stats[at][0][8 * g + 4 * hh]);
-      const float4 v = *reinterpret_cast<const float4*>(&stats[at][1][8 * g + 4 * hh]);
-      L[4 * g] = u.x; L[4 * g + 1] = u.y; L[4 * g + 2] = u.z; L[4 * g + 3] = u.w;
-      dp[4 * g] = v.x; dp[4 * g + 1] = v.y; dp[4 * g + 2] = v.z; dp[4 * g + 3] = v.w;
+      const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn][1][8 * g + 4 * hh]);
+      dp[4 * g] = u.x; dp[4 * g + 1] = u.y; dp[4 * g + 2] = u.z; dp[4 * g + 3] = u.w;
     }
 #pragma unroll
-    for (int kk = 0; kk < G::KK; ++kk) {
-      s[0] = mfma(frag_cols_lds<DHP>(tq, kk, lane), fk[kk], s[0]);
-      dp = mfma(frag_cols_lds<DHP>(tg, kk, lane), fv[kk], dp);
-    }
-    float p[16], ds[16];
+    for (int kk = 0; kk < G::KK; ++kk) dp = mfma(Frags<DHP>::cols(tc, 2 * G::TB, kk), fv[kk], dp);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = fast_exp2(fmaf(s[0][e], c, -stat_of(L[e])));
-      ds[e] = p[e] * dp[e];
+    for (int g = 0; g < 4; ++g) {
+      const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn][0][8 * g + 4 * hh]);
+      p[4 * g] = fast_exp2(fmaf(s[0][4 * g], c, u.x));
+      p[4 * g + 1] = fast_exp2(fmaf(s[0][4 * g + 1], c, u.y));
+      p[4 * g + 2] = fast_exp2(fmaf(s[0][4 * g + 2], c, u.z));
+      p[4 * g + 3] = fast_exp2(fmaf(s[0][4 * g + 3], c, u.w));
     }
     if (masked) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int r = first + tile_row_of(e, hh);
-        if (r < mine || r >= R) p[e] = ds[e] = 0.f;
+        const int i = first + tile_row_of(e, hh);
+        if (i < mine || i >= nq) p[e] = 0.f;
       }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const bf16x8 pt = pack8(p + 8 * t), dst = pack8(ds + 8 * t);
+      const bf16x8 pt = pack8(p + 8 * t);
 #pragma unroll
-      for (int mb = 0; mb < G::MB; ++mb) {
-        dv[mb] = mfma(frag_rows_lds<DHP>(tg, mb, t, lane), pt, dv[mb]);
-        dk[mb] = mfma(frag_rows_lds<DHP>(tq, mb, t, lane), dst, dk[mb]);
-      }
+      for (int mb = 0; mb < G::MB; ++mb) dv[mb] = mfma(Frags<DHP>::rows(tr, 2 * G::TB, mb, t), pt, dv[mb]);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) p[e] *= dp[e];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 dst = pack8(p + 8 * t);
+#pragma unroll
+      for (int mb = 0; mb < G::MB; ++mb) dk[mb] = mfma(Frags<DHP>::rows(tr, 0, mb, t), dst, dk[mb]);
     }
   };
-  int at = 0;
+  int at = 0, sh = turn, sq = top;                         // this wavefront's next tile
+  if (sh >= a.group) { sh -= a.group; --sq; }
   for (int i = 0; i < steps; ++i) {
     if (i + NST - 2 < steps) copies_in_flight<(PW + 1) * (NST - 2)>();
     else copies_in_flight<0>();
     workgroup_handover();
-    if (i + NST - 1 < steps) issue(i + NST - 1, at == 0 ? NST - 1 : at - 1);
-    const int first = 32 * (from + i);
-    if (first + 32 > begin && keys_left > 0) step(first, at, first < all || first + 32 > R);
+    if (i + NST - 1 < steps) ask(at == 0 ? NST - 1 : at - 1);
+    const int first = 32 * sq;
+    if (2 * i + turn < tiles && first + 32 > begin && keys_left > 0) step(first, at, first < all || first + 32 > nq);
     at = at == NST - 1 ? 0 : at + 1;
+    sh += 2;
+    if (sh >= a.group) {
+      sh -= a.group;
+      --sq;
+      if (sh >= a.group) { sh -= a.group; --sq; }          // (a group of one)
+    }
   }
+  float* const sums = reinterpret_cast<float*>(ring) + (wave & 3) * (G::MB * 16 * 64) + lane;
+  auto meet = [&](float16v (&acc)[G::MB]) __attribute__((always_inline)) {
+    __syncthreads();                                       // (the ring, or the sums before, are free)
+    if (turn == 1) {
+#pragma unroll
+      for (int m = 0; m < G::MB; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[(m * 16 + e) * 64] = acc[m][e];
+    }
+    __syncthreads();
+    if (turn == 0) {
+#pragma unroll
+      for (int m = 0; m < G::MB; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[m][e] += sums[(m * 16 + e) * 64];
+    }
+  };
+  meet(dk);
+  meet(dv);
   __syncthreads();
-  if (keys_left <= 0) return;
-  unsigned char* stg = &ring[0][0][0] + wave * 2048;
+  if (turn == 1 || keys_left <= 0) return;
+  unsigned char* stg = ring + wave * 2048;
   store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, x.s.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale,
              a.dh, stg, lane);
   store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, x.s.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, a.dh,
@@ -737,7 +832,7 @@ hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
 template <int DHP>
 hipError_t bwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
   if (const unsigned grid = tile_grid<false>(a, 32 * FWD_WAVES)) packed_dq_mfma_kernel<DHP><<<grid, 64 * FWD_WAVES, 0, s>>>(a);
-  if (const unsigned grid = tile_grid<true>(a, 32 * KV_WAVES)) packed_dkdv_mfma_kernel<DHP><<<grid, 64 * KV_WAVES, 0, s>>>(a);
+  if (const unsigned grid = tile_grid<true>(a, KV_KEYS)) packed_dkdv_mfma_kernel<DHP><<<grid, 64 * KV_WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -756,8 +851,9 @@ hipError_t bwd_t(const PackedAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t packed_attn_ws_bytes(int, const PackedAttnArgs& a) {
-  return ((size_t)a.q_rows * a.heads * 4 + 255) / 256 * 256;
+size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a) {
+  (void)dtype;
+  return 2 * (((size_t)a.q_rows * a.heads * 4 + 255) / 256 * 256);
 }
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void*, hipStream_t s) {
   return dtype == 0 ? fwd_t<float>(a, s) : a.dh <= 64 ? fwd_mfma<64>(a, s) : fwd_mfma<128>(a, s);
@@ -765,6 +861,7 @@ hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void*, hip
 hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s) {
   PackedAttnArgs b = a;
   b.dsum = reinterpret_cast<float*>(workspace);
+  b.nlse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + packed_attn_ws_bytes(dtype, a) / 2);
   return dtype == 0 ? bwd_t<float>(b, s) : a.dh <= 64 ? bwd_mfma<64>(b, s) : bwd_mfma<128>(b, s);
 }
 

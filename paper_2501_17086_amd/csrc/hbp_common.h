@@ -242,6 +242,7 @@ struct PackedAttnArgs {
   HeadRows q, k, v, o, dout, dq, dk, dv;
   float* lse;               // [q_rows, heads]
   float* dsum;              // [q_rows, heads], workspace: minus rowsum(dout (.) o)
+  float* nlse;              // [q_rows, heads], workspace: minus lse; minus infinity where a row weighs nothing
   const int* q_off;         // [seqs + 1] or NULL: equal lengths
   const int* k_off;
   int seqs, q_rows, k_rows;
