@@ -1,0 +1,293 @@
+// What the kernels of the attention over packed sequences share (attention_packed.hip, attention_packed_f32.hip): sequences, tiles of
+// rows, and the term-by-term computation of one row or key.
+//
+// A key/value head's `group` query heads see the same keys, so the rows that a sequence brings to it are its queries
+// times its group, row r = query r / group of head r % group: tiles of rows then hold several heads of a query, the
+// streamed keys serve all of them, and a single query fills `group` rows of a tile.
+#pragma once
+#include "attention_device.h"
+
+#include <cfloat>
+
+namespace hbp {
+
+namespace {
+
+// One sequence: its first row and its length on either side.
+struct Seq { int q0, nq, k0, nk; };
+__device__ __forceinline__ int clamp_row(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
+__device__ __forceinline__ void span_of(const int* off, int rows, int seqs, int s, int& first, int& n) {
+  if (!off) {
+    n = rows / seqs;
+    first = s * n;
+    return;
+  }
+  first = clamp_row(off[s], rows);
+  n = clamp_row(off[s + 1], rows) - first;
+  if (n < 0) n = 0;
+}
+__device__ __forceinline__ Seq seq_of(const PackedAttnArgs& a, int s) {
+  Seq q;
+  span_of(a.q_off, a.q_rows, a.seqs, s, q.q0, q.nq);
+  span_of(a.k_off, a.k_rows, a.seqs, s, q.k0, q.nk);
+  return q;
+}
+// the sequence that row n belongs to (offsets that do not decrease), -1: none
+__device__ __forceinline__ int seq_with(const int* off, int rows, int seqs, int n) {
+  if (!off) return n / (rows / seqs);
+  int lo = 0, hi = seqs;                                   // off[lo] <= n < off[hi], where there is such a sequence
+  if (n < off[0] || n >= off[seqs]) return -1;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid] <= n) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+template <typename T> __device__ __forceinline__ const T* row_of(const HeadRows& x, long n, int h) {
+  return reinterpret_cast<const T*>(x.p) + n * x.row + (long)h * x.head;
+}
+template <typename T> __device__ __forceinline__ T* row_out(const HeadRows& x, long n, int h) {
+  return reinterpret_cast<T*>(x.p) + n * x.row + (long)h * x.head;
+}
+template <typename T>
+__device__ __forceinline__ float dot_rows(const T* a, const T* b, int n) {
+  float s = 0.f;
+  for (int c = 0; c < n; c += 8) {
+    float x[8], y[8];
+    load8(a + c, x);
+    load8(b + c, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(x[i], y[i], s);
+  }
+  return s;
+}
+
+// out[c] += sum over n rows of w (lane j: row j) times column c of `rows`; a lane holds columns lane and lane + 64
+struct TwoColumns {
+  float v[2] = {0.f, 0.f};
+  template <typename T>
+  __device__ __forceinline__ void add(float w, int n, const T* rows, long ld, int dh, int lane) {
+    for (int j = 0; j < n; ++j) {
+      const float wj = __shfl(w, j, 64);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (lane + 64 * u < dh) v[u] = fmaf(wj, Elem<T>::load(rows + j * ld + lane + 64 * u), v[u]);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* out, float f, int dh, int lane) const {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (lane + 64 * u < dh) Elem<T>::store(out + lane + 64 * u, v[u] * f);
+  }
+};
+
+// keys that query i of a sequence sees
+__device__ __forceinline__ int seen_by(const Seq& s, int i, int causal) {
+  if (!causal) return s.nk;
+  const int n = i + 1 + s.nk - s.nq;
+  return n < 0 ? 0 : n;
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// term by term: one wavefront per (query, head), one per (key, key head)
+// ------------------------------------------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& s, int i, int h, int lane) {
+  const int hk = h / a.group, seen = seen_by(s, i, a.causal);
+  const T* q = row_of<T>(a.q, s.q0 + i, h);
+  const T* k = row_of<T>(a.k, s.k0, hk);
+  const T* v = row_of<T>(a.v, s.k0, hk);
+  const float c = a.scale * LOG2E;
+  float m = -INFINITY, sum = 0.f;
+  for (int j = lane; j < seen; j += 64) {
+    const float x = c * dot_rows(q, k + j * a.k.row, a.dh);
+    m = x > m || x != x ? x : m;                           // (a NaN stays)
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float x = __shfl_xor(m, o, 64);
+    m = x > m || x != x ? x : m;
+  }
+  const float base = m == -INFINITY ? 0.f : m;             // nothing seen, or minus infinity throughout: every weight is 0
+  TwoColumns out;
+  for (int j0 = 0; j0 < seen; j0 += 64) {
+    float p = 0.f;
+    if (j0 + lane < seen) {
+      p = exp2f(c * dot_rows(q, k + (j0 + lane) * a.k.row, a.dh) - base);
+      sum += p;
+    }
+    out.add(p, seen - j0 < 64 ? seen - j0 : 64, v + j0 * a.v.row, a.v.row, a.dh, lane);
+  }
+  sum = wave_sum(sum);
+  const bool none = m == -INFINITY;
+  if (none) out = TwoColumns();
+  out.store(row_out<T>(a.o, s.q0 + i, h), none ? 0.f : 1.f / sum, a.dh, lane);
+  if (lane == 0) a.lse[(long)(s.q0 + i) * a.heads + h] = none ? -INFINITY : m + log2f(sum);
+}
+// the statistic that the backward pass subtracts: a row that weighs nothing keeps weighing nothing
+__device__ __forceinline__ float stat_of(float lse) { return lse == -INFINITY ? INFINITY : lse; }
+
+template <typename T>
+__device__ __forceinline__ float row_dsum(const PackedAttnArgs& a, long n, int h, int lane) {
+  const T* g = row_of<T>(a.dout, n, h);
+  const T* o = row_of<T>(a.o, n, h);
+  float d = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (lane + 64 * u < a.dh) d = fmaf(Elem<T>::load(g + lane + 64 * u), Elem<T>::load(o + lane + 64 * u), d);
+  return wave_sum(d);
+}
+
+template <typename T>
+__device__ __forceinline__ void one_dq(const PackedAttnArgs& a, const Seq& s, int i, int h, float D, int lane) {
+  const int hk = h / a.group, seen = seen_by(s, i, a.causal);
+  const long n = s.q0 + i;
+  const T* q = row_of<T>(a.q, n, h);
+  const T* g = row_of<T>(a.dout, n, h);
+  const T* k = row_of<T>(a.k, s.k0, hk);
+  const T* v = row_of<T>(a.v, s.k0, hk);
+  const float c = a.scale * LOG2E, L = stat_of(a.lse[n * a.heads + h]);
+  TwoColumns out;
+  if (L != INFINITY)
+    for (int j0 = 0; j0 < seen; j0 += 64) {
+      float ds = 0.f;
+      if (j0 + lane < seen) {
+        const float p = exp2f(c * dot_rows(q, k + (j0 + lane) * a.k.row, a.dh) - L);
+        ds = p * (dot_rows(g, v + (j0 + lane) * a.v.row, a.dh) - D);
+      }
+      out.add(ds, seen - j0 < 64 ? seen - j0 : 64, k + j0 * a.k.row, a.k.row, a.dh, lane);
+    }
+  out.store(row_out<T>(a.dq, n, h), a.scale, a.dh, lane);
+}
+
+template <typename T>
+__device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, int j, int hk, int lane) {
+  const T* k = row_of<T>(a.k, s.k0 + j, hk);
+  const T* v = row_of<T>(a.v, s.k0 + j, hk);
+  const float c = a.scale * LOG2E;
+  int i0 = a.causal ? j - (s.nk - s.nq) : 0;               // the first query that sees it
+  if (i0 < 0) i0 = 0;
+  TwoColumns dk, dv;
+  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
+    for (int b = i0; b < s.nq; b += 64) {
+      float p = 0.f, ds = 0.f;
+      const int n = s.nq - b < 64 ? s.nq - b : 64;
+      if (lane < n) {
+        const long r = s.q0 + b + lane;
+        const float L = a.nlse[r * a.heads + h];
+        if (L != -INFINITY) {
+          p = exp2f(c * dot_rows(row_of<T>(a.q, r, h), k, a.dh) + L);
+          ds = p * (dot_rows(row_of<T>(a.dout, r, h), v, a.dh) + a.dsum[r * a.heads + h]);
+        }
+      }
+      dk.add(ds, n, row_of<T>(a.q, s.q0 + b, h), a.q.row, a.dh, lane);
+      dv.add(p, n, row_of<T>(a.dout, s.q0 + b, h), a.dout.row, a.dh, lane);
+    }
+  dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, a.dh, lane);
+  dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, a.dh, lane);
+}
+
+// Which key head, sequence and tile of `per` rows (keys: `per` keys) a workgroup takes.  The key heads of a tile are next to each
+// other: all problems go on side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs
+// in turn, keep a problem's streamed tiles in one XCD's L2.
+struct Tile { int hk, t, n; Seq s; bool exists; };          // t of the sequence's n tiles
+__device__ __forceinline__ int tiles_in(int len, int per) { return (len + per - 1) / per; }
+template <bool KEYS>
+__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane) {
+  Tile x;
+  const unsigned id = blockIdx.x;
+  x.hk = (int)(id % (unsigned)a.kv_heads);
+  x.t = (int)(id / (unsigned)a.kv_heads);
+  const int* off = KEYS ? a.k_off : a.q_off;
+  const int mult = KEYS ? 1 : a.group, rows = KEYS ? a.k_rows : a.q_rows;
+  int sq = -1;
+  if (!off) {
+    x.n = tiles_in(rows / a.seqs * mult, per);
+    sq = x.t / x.n;
+    x.t -= sq * x.n;
+    if (sq >= a.seqs) sq = -1;
+  } else {
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time: a running sum of their tiles over the lanes
+      int first, n = 0;
+      if (s0 + lane < a.seqs) span_of(off, rows, a.seqs, s0 + lane, first, n);
+      n = tiles_in(n * mult, per);
+      int sum = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += up;
+      }
+      const unsigned long long past = __ballot(sum > x.t);
+      if (past) {
+        const int l = __ffsll(past) - 1;
+        sq = s0 + l;
+        x.n = __builtin_amdgcn_readlane(n, l);
+        x.t -= __builtin_amdgcn_readlane(sum, l) - x.n;
+        break;
+      }
+      x.t -= __builtin_amdgcn_readlane(sum, 63);
+    }
+  }
+  x.exists = sq >= 0;
+  if (x.exists) {
+    x.s = seq_of(a, sq);
+    x.t = __builtin_amdgcn_readfirstlane(x.t);
+    x.n = __builtin_amdgcn_readfirstlane(x.n);
+    x.s.q0 = __builtin_amdgcn_readfirstlane(x.s.q0);
+    x.s.nq = __builtin_amdgcn_readfirstlane(x.s.nq);
+    x.s.k0 = __builtin_amdgcn_readfirstlane(x.s.k0);
+    x.s.nk = __builtin_amdgcn_readfirstlane(x.s.nk);
+  }
+  return x;
+}
+// the other half's value (lanes l and l + 32 hold one row's two halves)
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// The rows of a tile: row r of the sequence at this key head is query r / group of head hk group + r % group.
+struct RowPlace { int i, h; };
+__device__ __forceinline__ RowPlace place_of(const PackedAttnArgs& a, int hk, int r) {
+  RowPlace p;
+  p.i = (int)((unsigned)r / (unsigned)a.group);
+  p.h = hk * a.group + (r - p.i * a.group);
+  return p;
+}
+
+// Infinities and NaNs: a product on the matrix cores meets every element of a tile, also those that the mask or the sequence's end
+// leaves out, and there 0 times an infinity is NaN.  A row of a result that did not come out finite is therefore computed
+// once more, term by term over what it sees.  Finite data never comes here.
+template <int MB>
+__device__ __forceinline__ float not_finite(const float16v (&acc)[MB], float t) {
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = fmaf(acc[m][r], 0.f, t);
+  return t;
+}
+template <typename F>
+__device__ __forceinline__ void redo_rows(float t, int rows_left, F f) {
+  const unsigned long long b = __ballot(t != t);
+  unsigned rows = (unsigned)b | (unsigned)(b >> 32);
+  if (rows_left < 32) rows &= (1u << rows_left) - 1u;
+  if (rows == 0) return;
+  copies_in_flight<0>();                                   // (the tile's own stores, which these replace)
+  for (; rows != 0; rows &= rows - 1) f(__ffs((int)rows) - 1);
+}
+
+// workgroups for tiles of `per` rows (keys)
+template <bool KEYS>
+unsigned tile_grid(const PackedAttnArgs& a, int per) {
+  const long rows = KEYS ? a.k_rows : (long)a.q_rows * a.group;
+  if (rows == 0) return 0;
+  const bool equal = KEYS ? !a.k_off : !a.q_off;
+  const long tiles = equal ? a.seqs * ((rows / a.seqs + per - 1) / per) : rows / per + a.seqs;
+  return (unsigned)(tiles * a.kv_heads);
+}
+
+}  // namespace
+
+hipError_t launch_packed_attn_fwd_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_attn_bwd_f32(const PackedAttnArgs& a, hipStream_t s);
+
+}  // namespace hbp

@@ -1,289 +1,15 @@
-// Attention over packed sequences, forward and backward, whose key/value heads serve groups of query heads.
-//
-// A key/value head's `group` query heads see the same keys, so the rows that a sequence brings to it are its queries
-// times its group, row r = query r / group of head r % group: tiles of rows then hold several heads of a query, the
-// streamed keys serve all of them, dk and dv sum over the group by summing over rows, and a single query fills `group`
-// rows of a tile.
-#include "attention_device.h"
-
-#include <cfloat>
+// Attention over packed sequences, forward and backward, whose key/value heads serve groups of query heads: bf16 storage, on the
+// matrix cores; and the entry points of both storage types.
+#include "attention_packed.h"
 
 namespace hbp {
 
 namespace {
 
-// One sequence: its first row and its length on either side.
-struct Seq { int q0, nq, k0, nk; };
-__device__ __forceinline__ int clamp_row(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
-__device__ __forceinline__ void span_of(const int* off, int rows, int seqs, int s, int& first, int& n) {
-  if (!off) {
-    n = rows / seqs;
-    first = s * n;
-    return;
-  }
-  first = clamp_row(off[s], rows);
-  n = clamp_row(off[s + 1], rows) - first;
-  if (n < 0) n = 0;
-}
-__device__ __forceinline__ Seq seq_of(const PackedAttnArgs& a, int s) {
-  Seq q;
-  span_of(a.q_off, a.q_rows, a.seqs, s, q.q0, q.nq);
-  span_of(a.k_off, a.k_rows, a.seqs, s, q.k0, q.nk);
-  return q;
-}
-// the sequence that row n belongs to (offsets that do not decrease), -1: none
-__device__ __forceinline__ int seq_with(const int* off, int rows, int seqs, int n) {
-  if (!off) return n / (rows / seqs);
-  int lo = 0, hi = seqs;                                   // off[lo] <= n < off[hi], where there is such a sequence
-  if (n < off[0] || n >= off[seqs]) return -1;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid] <= n) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
-template <typename T> __device__ __forceinline__ const T* row_of(const HeadRows& x, long n, int h) {
-  return reinterpret_cast<const T*>(x.p) + n * x.row + (long)h * x.head;
-}
-template <typename T> __device__ __forceinline__ T* row_out(const HeadRows& x, long n, int h) {
-  return reinterpret_cast<T*>(x.p) + n * x.row + (long)h * x.head;
-}
-template <typename T>
-__device__ __forceinline__ float dot_rows(const T* a, const T* b, int n) {
-  float s = 0.f;
-  for (int c = 0; c < n; c += 8) {
-    float x[8], y[8];
-    load8(a + c, x);
-    load8(b + c, y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(x[i], y[i], s);
-  }
-  return s;
-}
-
-// out[c] += sum over n rows of w (lane j: row j) times column c of `rows`; a lane holds columns lane and lane + 64
-struct TwoColumns {
-  float v[2] = {0.f, 0.f};
-  template <typename T>
-  __device__ __forceinline__ void add(float w, int n, const T* rows, long ld, int dh, int lane) {
-    for (int j = 0; j < n; ++j) {
-      const float wj = __shfl(w, j, 64);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (lane + 64 * u < dh) v[u] = fmaf(wj, Elem<T>::load(rows + j * ld + lane + 64 * u), v[u]);
-    }
-  }
-  template <typename T>
-  __device__ __forceinline__ void store(T* out, float f, int dh, int lane) const {
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (lane + 64 * u < dh) Elem<T>::store(out + lane + 64 * u, v[u] * f);
-  }
-};
-
-// keys that query i of a sequence sees
-__device__ __forceinline__ int seen_by(const Seq& s, int i, int causal) {
-  if (!causal) return s.nk;
-  const int n = i + 1 + s.nk - s.nq;
-  return n < 0 ? 0 : n;
-}
-
-// ------------------------------------------------------------------------------------------------------------
-// term by term: one wavefront per (query, head), one per (key, key head)
-// ------------------------------------------------------------------------------------------------------------
-template <typename T>
-__device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& s, int i, int h, int lane) {
-  const int hk = h / a.group, seen = seen_by(s, i, a.causal);
-  const T* q = row_of<T>(a.q, s.q0 + i, h);
-  const T* k = row_of<T>(a.k, s.k0, hk);
-  const T* v = row_of<T>(a.v, s.k0, hk);
-  const float c = a.scale * LOG2E;
-  float m = -INFINITY, sum = 0.f;
-  for (int j = lane; j < seen; j += 64) {
-    const float x = c * dot_rows(q, k + j * a.k.row, a.dh);
-    m = x > m || x != x ? x : m;                           // (a NaN stays)
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float x = __shfl_xor(m, o, 64);
-    m = x > m || x != x ? x : m;
-  }
-  const float base = m == -INFINITY ? 0.f : m;             // nothing seen, or minus infinity throughout: every weight is 0
-  TwoColumns out;
-  for (int j0 = 0; j0 < seen; j0 += 64) {
-    float p = 0.f;
-    if (j0 + lane < seen) {
-      p = exp2f(c * dot_rows(q, k + (j0 + lane) * a.k.row, a.dh) - base);
-      sum += p;
-    }
-    out.add(p, seen - j0 < 64 ? seen - j0 : 64, v + j0 * a.v.row, a.v.row, a.dh, lane);
-  }
-  sum = wave_sum(sum);
-  const bool none = m == -INFINITY;
-  if (none) out = TwoColumns();
-  out.store(row_out<T>(a.o, s.q0 + i, h), none ? 0.f : 1.f / sum, a.dh, lane);
-  if (lane == 0) a.lse[(long)(s.q0 + i) * a.heads + h] = none ? -INFINITY : m + log2f(sum);
-}
-// the statistic that the backward pass subtracts: a row that weighs nothing keeps weighing nothing
-__device__ __forceinline__ float stat_of(float lse) { return lse == -INFINITY ? INFINITY : lse; }
-
-template <typename T>
-__device__ __forceinline__ float row_dsum(const PackedAttnArgs& a, long n, int h, int lane) {
-  const T* g = row_of<T>(a.dout, n, h);
-  const T* o = row_of<T>(a.o, n, h);
-  float d = 0.f;
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-    if (lane + 64 * u < a.dh) d = fmaf(Elem<T>::load(g + lane + 64 * u), Elem<T>::load(o + lane + 64 * u), d);
-  return wave_sum(d);
-}
-
-template <typename T>
-__device__ __forceinline__ void one_dq(const PackedAttnArgs& a, const Seq& s, int i, int h, float D, int lane) {
-  const int hk = h / a.group, seen = seen_by(s, i, a.causal);
-  const long n = s.q0 + i;
-  const T* q = row_of<T>(a.q, n, h);
-  const T* g = row_of<T>(a.dout, n, h);
-  const T* k = row_of<T>(a.k, s.k0, hk);
-  const T* v = row_of<T>(a.v, s.k0, hk);
-  const float c = a.scale * LOG2E, L = stat_of(a.lse[n * a.heads + h]);
-  TwoColumns out;
-  if (L != INFINITY)
-    for (int j0 = 0; j0 < seen; j0 += 64) {
-      float ds = 0.f;
-      if (j0 + lane < seen) {
-        const float p = exp2f(c * dot_rows(q, k + (j0 + lane) * a.k.row, a.dh) - L);
-        ds = p * (dot_rows(g, v + (j0 + lane) * a.v.row, a.dh) - D);
-      }
-      out.add(ds, seen - j0 < 64 ? seen - j0 : 64, k + j0 * a.k.row, a.k.row, a.dh, lane);
-    }
-  out.store(row_out<T>(a.dq, n, h), a.scale, a.dh, lane);
-}
-
-template <typename T>
-__device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, int j, int hk, int lane) {
-  const T* k = row_of<T>(a.k, s.k0 + j, hk);
-  const T* v = row_of<T>(a.v, s.k0 + j, hk);
-  const float c = a.scale * LOG2E;
-  int i0 = a.causal ? j - (s.nk - s.nq) : 0;               // the first query that sees it
-  if (i0 < 0) i0 = 0;
-  TwoColumns dk, dv;
-  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
-    for (int b = i0; b < s.nq; b += 64) {
-      float p = 0.f, ds = 0.f;
-      const int n = s.nq - b < 64 ? s.nq - b : 64;
-      if (lane < n) {
-        const long r = s.q0 + b + lane;
-        const float L = a.nlse[r * a.heads + h];
-        if (L != -INFINITY) {
-          p = exp2f(c * dot_rows(row_of<T>(a.q, r, h), k, a.dh) + L);
-          ds = p * (dot_rows(row_of<T>(a.dout, r, h), v, a.dh) + a.dsum[r * a.heads + h]);
-        }
-      }
-      dk.add(ds, n, row_of<T>(a.q, s.q0 + b, h), a.q.row, a.dh, lane);
-      dv.add(p, n, row_of<T>(a.dout, s.q0 + b, h), a.dout.row, a.dh, lane);
-    }
-  dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, a.dh, lane);
-  dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, a.dh, lane);
-}
-
-template <typename T>
-__global__ __launch_bounds__(64) void packed_fwd_rows_kernel(PackedAttnArgs a) {
-  const int n = (int)(blockIdx.x / (unsigned)a.heads), h = (int)(blockIdx.x % (unsigned)a.heads);
-  const int sq = seq_with(a.q_off, a.q_rows, a.seqs, n);
-  if (sq < 0) return;
-  const Seq s = seq_of(a, sq);
-  if (n < s.q0 || n >= s.q0 + s.nq) return;                // (offsets that decrease)
-  one_forward<T>(a, s, n - s.q0, h, threadIdx.x);
-}
-template <typename T>
-__global__ __launch_bounds__(64) void packed_dq_rows_kernel(PackedAttnArgs a) {
-  const int n = (int)(blockIdx.x / (unsigned)a.heads), h = (int)(blockIdx.x % (unsigned)a.heads);
-  const int sq = seq_with(a.q_off, a.q_rows, a.seqs, n);
-  if (sq < 0) return;
-  const Seq s = seq_of(a, sq);
-  if (n < s.q0 || n >= s.q0 + s.nq) return;
-  const float D = row_dsum<T>(a, n, h, threadIdx.x);
-  if (threadIdx.x == 0) {
-    a.dsum[(long)n * a.heads + h] = -D;
-    a.nlse[(long)n * a.heads + h] = -stat_of(a.lse[(long)n * a.heads + h]);
-  }
-  one_dq<T>(a, s, n - s.q0, h, D, threadIdx.x);
-}
-template <typename T>
-__global__ __launch_bounds__(64) void packed_dkdv_rows_kernel(PackedAttnArgs a) {
-  const int n = (int)(blockIdx.x / (unsigned)a.kv_heads), hk = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int sq = seq_with(a.k_off, a.k_rows, a.seqs, n);
-  if (sq < 0) return;
-  const Seq s = seq_of(a, sq);
-  if (n < s.k0 || n >= s.k0 + s.nk) return;
-  one_dkdv<T>(a, s, n - s.k0, hk, threadIdx.x);
-}
-
-// ------------------------------------------------------------------------------------------------------------
-// matrix-core kernels: bf16
-// ------------------------------------------------------------------------------------------------------------
-// Which key head, sequence and tile of `per` rows (keys: `per` keys) a workgroup takes.  The key heads of a tile are next to each
-// other: all problems go on side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs
-// in turn, keep a problem's streamed tiles in one XCD's L2.
-struct Tile { int hk, t, n; Seq s; bool exists; };          // t of the sequence's n tiles
-__device__ __forceinline__ int tiles_in(int len, int per) { return (len + per - 1) / per; }
-template <bool KEYS>
-__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane) {
-  Tile x;
-  const unsigned id = blockIdx.x;
-  x.hk = (int)(id % (unsigned)a.kv_heads);
-  x.t = (int)(id / (unsigned)a.kv_heads);
-  const int* off = KEYS ? a.k_off : a.q_off;
-  const int mult = KEYS ? 1 : a.group, rows = KEYS ? a.k_rows : a.q_rows;
-  int sq = -1;
-  if (!off) {
-    x.n = tiles_in(rows / a.seqs * mult, per);
-    sq = x.t / x.n;
-    x.t -= sq * x.n;
-    if (sq >= a.seqs) sq = -1;
-  } else {
-    for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time: a running sum of their tiles over the lanes
-      int first, n = 0;
-      if (s0 + lane < a.seqs) span_of(off, rows, a.seqs, s0 + lane, first, n);
-      n = tiles_in(n * mult, per);
-      int sum = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += up;
-      }
-      const unsigned long long past = __ballot(sum > x.t);
-      if (past) {
-        const int l = __ffsll(past) - 1;
-        sq = s0 + l;
-        x.n = __builtin_amdgcn_readlane(n, l);
-        x.t -= __builtin_amdgcn_readlane(sum, l) - x.n;
-        break;
-      }
-      x.t -= __builtin_amdgcn_readlane(sum, 63);
-    }
-  }
-  x.exists = sq >= 0;
-  if (x.exists) {
-    x.s = seq_of(a, sq);
-    x.t = __builtin_amdgcn_readfirstlane(x.t);
-    x.n = __builtin_amdgcn_readfirstlane(x.n);
-    x.s.q0 = __builtin_amdgcn_readfirstlane(x.s.q0);
-    x.s.nq = __builtin_amdgcn_readfirstlane(x.s.nq);
-    x.s.k0 = __builtin_amdgcn_readfirstlane(x.s.k0);
-    x.s.nk = __builtin_amdgcn_readfirstlane(x.s.nk);
-  }
-  return x;
-}
-// the other half's value (lanes l and l + 32 hold one row's two halves)
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
-
 // Fragments by LDS byte addresses.  The tiles' chunk swizzle is an XOR of address bits, so one register per direction holds all there
 // is of a lane in an address: a step adds its stage, an XOR with a constant picks the fragment, and tiles of the same stage
-// are constant offsets.  (Addresses formed from the row and the chunk each time cost an addition per read, a third of
-// the forward pass's vector instructions.)
+// are constant offsets.  (Registers of the forward kernel at 128 channels: 235 with addresses formed from row and chunk, 216
+// with these.)
 template <int DHP>
 struct Frags {
   typedef Geo<DHP> G;
@@ -318,18 +44,20 @@ __device__ __forceinline__ bf16x8 own_piece(const bf16_t* row, int kk, int dh8, 
   return __builtin_bit_cast(bf16x8, make_uint4(in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u));
 }
 
-// Streamed key and value tiles: a stage holds 64 keys, two tiles of 32 of k and two of v, which a workgroup's wavefronts copy together,
-// PW copies of 1 KB each.
-template <int DHP, int WAVES>
+constexpr int WAVES = 8;
+
+// Streamed key and value tiles: a stage holds 32 NT keys, NT tiles of k, then NT of v, which a workgroup's wavefronts copy together, PW
+// copies of 1 KB each, all of one tile or of whole ones.
+template <int DHP, int NT>
 struct KeyStream {
   typedef Geo<DHP> G;
-  static constexpr int STAGE = 4 * G::TB;
-  static constexpr int PW = 4 * G::COPIES / WAVES;
+  static constexpr int STAGE = 2 * NT * G::TB;
+  static constexpr int PW = 2 * NT * G::COPIES / WAVES;
   unsigned off[PW];
   const unsigned char *k, *v;
   unsigned ldk, ldv, lds0;
   int nk, dh8;
-  static __device__ __forceinline__ int tile(int w, int i) { return (w * PW + i) / G::COPIES; }     // k, k, v, v
+  static __device__ __forceinline__ int tile(int w, int i) { return (w * PW + i) / G::COPIES; }
   static __device__ __forceinline__ int part(int w, int i) { return (w * PW + i) % G::COPIES; }
   __device__ __forceinline__ KeyStream(const PackedAttnArgs& a, const Seq& s, int hk, unsigned lds, int dh8_, int w, int lane) {
     k = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.k, s.k0, hk));
@@ -340,15 +68,15 @@ struct KeyStream {
     nk = s.nk;
     dh8 = dh8_;
 #pragma unroll
-    for (int i = 0; i < PW; ++i) off[i] = copy_offset<DHP>(tile(w, i) < 2 ? ldk : ldv, part(w, i), 32, dh8, lane);
+    for (int i = 0; i < PW; ++i) off[i] = copy_offset<DHP>(tile(w, i) < NT ? ldk : ldv, part(w, i), 32, dh8, lane);
   }
-  // keys 64 step .. into stage `at`; keys past the last repeat it
+  // keys 32 NT step .. into stage `at`; keys past the last repeat it
   __device__ __forceinline__ void issue(int step, int at, int w, int lane) const {
 #pragma unroll
     for (int i = 0; i < PW; ++i) {
-      const int t = tile(w, i), first = 64 * step + 32 * (t & 1);
-      const unsigned ld = t < 2 ? ldk : ldv;
-      const unsigned char* base = t < 2 ? k : v;
+      const int t = tile(w, i), first = 32 * NT * step + 32 * (t % NT);
+      const unsigned ld = t < NT ? ldk : ldv;
+      const unsigned char* base = t < NT ? k : v;
       const unsigned dst = lds0 + (unsigned)at * STAGE + (unsigned)(w * PW + i) * 1024u;
       if (first + 32 <= nk) {
         copy16_to_lds(off[i], base + (long)first * ld, dst);
@@ -360,26 +88,99 @@ struct KeyStream {
   }
 };
 
-// The rows of a tile: row r of the sequence at this key head is query r / group of head hk group + r % group.
-struct RowPlace { int i, h; };
-__device__ __forceinline__ RowPlace place_of(const PackedAttnArgs& a, int hk, int r) {
-  RowPlace p;
-  p.i = (int)((unsigned)r / (unsigned)a.group);
-  p.h = hk * a.group + (r - p.i * a.group);
-  return p;
-}
+// How a workgroup's eight wavefronts share rows and keys.  COLS = 1: 256 rows, 32 for each wavefront, which goes over all keys in
+// steps of 64.  COLS = 4, for few rows: 64 rows, and of every step of 128 keys a wavefront takes 32; the four that share rows
+// meet in LDS at the end.
+template <int DHP, int COLS>
+struct Shape {
+  typedef Geo<DHP> G;
+  static constexpr int ROWS = 32 * WAVES / COLS;
+  static constexpr int NT = COLS == 1 ? 2 : 4, KEYS = 32 * NT, SUB = NT / COLS;
+  typedef KeyStream<DHP, NT> KS;
+  static constexpr int NST = COLS == 1 ? (DHP == 128 ? 3 : 4) : (DHP == 128 ? 2 : 3);
+  static constexpr int SUMS = COLS == 1 ? 0 : WAVES * G::MB * 16 * 64 * 4;       // everyone's output, fp32
+  static constexpr int RING = NST * KS::STAGE > SUMS ? NST * KS::STAGE : SUMS;
+};
+
+// The rows of a workgroup, and the keys that they see: steps from .. to - 1 of this workgroup's share of them.
+template <int DHP, int COLS>
+struct RowBlock {
+  typedef Shape<DHP, COLS> S;
+  Tile x;
+  int w0, rows_left, mine, fewest, most, from, to, share;
+  RowPlace me;
+  __device__ __forceinline__ bool find(const PackedAttnArgs& a, int rw, int lane) {
+    x = find_tile<false>(a, S::ROWS, lane);
+    if (!x.exists) return false;
+    x.t = x.n - 1 - x.t;                                   // (causal: long rows first)
+    const int R = x.s.nq * a.group, r0 = S::ROWS * x.t;
+    w0 = r0 + 32 * rw;
+    rows_left = R - w0;
+    auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
+    const int steps = (seen((R < r0 + S::ROWS ? R : r0 + S::ROWS) - 1) + S::KEYS - 1) / S::KEYS;
+    share = (int)blockIdx.y;
+    from = (int)((long)steps * share / a.shares);
+    to = (int)((long)steps * (share + 1) / a.shares);
+    const int r = rows_left > 0 ? w0 + ((lane & 31) < rows_left ? (lane & 31) : rows_left - 1) : R - 1;
+    me = place_of(a, x.hk, r);
+    mine = seen_by(x.s, me.i, a.causal);
+    fewest = rows_left > 0 ? seen(w0) : 0;
+    most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
+    return true;
+  }
+};
+
+// Scores into the second product's operand, rounded to bf16, or, in a sequence of few keys (queries), as two parts that hold 16 bits:
+// a few roundings do not average out, and such sequences are not bound by their products.
+constexpr int FEW = 64;
+struct Operand {
+  bf16x8 hi[2], lo[2];
+  __device__ __forceinline__ void set(const float* p, bool few) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) hi[t] = pack8(p + 8 * t);
+    if (few) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint4 h = __builtin_bit_cast(uint4, hi[t]);
+        const unsigned w[4] = {h.x, h.y, h.z, h.w};
+        float rest[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          rest[2 * i] = p[8 * t + 2 * i] - __uint_as_float(w[i] << 16);
+          rest[2 * i + 1] = p[8 * t + 2 * i + 1] - __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+        lo[t] = pack8(rest);
+      }
+    }
+  }
+  // acc += the tile's columns (behind `at`, at `tile`) times the scores
+  template <int DHP>
+  __device__ __forceinline__ void times(unsigned at, unsigned tile, float16v (&acc)[Geo<DHP>::MB], bool few) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int mb = 0; mb < Geo<DHP>::MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), hi[t], acc[mb]);
+    if (few) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int mb = 0; mb < Geo<DHP>::MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), lo[t], acc[mb]);
+    }
+  }
+};
 
 // A tile's results, scaled per row by f, to their rows (see store_tile in attention.hip: 64 bytes of a row per store).
-// row(j): where row j of the tile goes; rows_left of them.
+// row(j): where row j of the tile goes; rows_left of them.  acc: blocks of 32 channels from block m0 on.
 template <int MB, typename F>
-__device__ __forceinline__ void store_rows(F row, int rows_left, const float16v (&acc)[MB], float f, int dh, unsigned char* stg, int lane) {
+__device__ __forceinline__ void store_rows(F row, int rows_left, const float16v (&acc)[MB], float f, int m0, int dh, unsigned char* stg,
+                                           int lane) {
   const int r = lane & 31, hh = lane >> 5, rr = lane >> 2, ch = lane & 3;
   bf16_t* out[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) out[u] = rr + 16 * u < rows_left ? row(rr + 16 * u) : nullptr;
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
-    if (32 * m >= dh) break;
+    if (32 * (m0 + m) >= dh) break;
 #pragma unroll
     for (int g = 0; g < 4; ++g)
       store4b(reinterpret_cast<bf16_t*>(stg + r * 64 + ((g ^ ((r >> 2) & 3)) << 4) + 8 * hh), acc[m][4 * g] * f,
@@ -389,94 +190,97 @@ __device__ __forceinline__ void store_rows(F row, int rows_left, const float16v 
     for (int u = 0; u < 2; ++u) {
       const int w = rr + 16 * u;
       const uint4 v = *reinterpret_cast<const uint4*>(stg + w * 64 + ((ch ^ ((w >> 2) & 3)) << 4));
-      if (out[u] && 32 * m + 8 * ch < dh) *reinterpret_cast<uint4*>(out[u] + 32 * m + 8 * ch) = v;
+      const int c = 32 * (m0 + m) + 8 * ch;
+      if (out[u] && c < dh) *reinterpret_cast<uint4*>(out[u] + c) = v;
     }
     __builtin_amdgcn_wave_barrier();
   }
 }
 
-// Infinities and NaNs: a product on the matrix cores meets every element of a tile, also those that the mask or the sequence's end
-// leaves out, and there 0 times an infinity is NaN.  A row of a result that did not come out finite is therefore computed
-// once more, term by term over what it sees.  Finite data never comes here.
+// The outputs of the wavefronts that share rows (sums: [wavefront][block of 32 channels][element][lane]) into block `m` of the sum, each
+// times its f.
 template <int MB>
-__device__ __forceinline__ float not_finite(const float16v (&acc)[MB], float t) {
+__device__ __forceinline__ void put_sums(float* sums, int wave, const float16v (&acc)[MB], int lane) {
 #pragma unroll
   for (int m = 0; m < MB; ++m)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) t = fmaf(acc[m][r], 0.f, t);
-  return t;
+    for (int e = 0; e < 16; ++e) sums[((wave * MB + m) * 16 + e) * 64 + lane] = acc[m][e];
 }
-template <typename F>
-__device__ __forceinline__ void redo_rows(float t, int rows_left, F f) {
-  const unsigned long long b = __ballot(t != t);
-  unsigned rows = (unsigned)b | (unsigned)(b >> 32);
-  if (rows_left < 32) rows &= (1u << rows_left) - 1u;
-  if (rows == 0) return;
-  copies_in_flight<0>();                                   // (the tile's own stores, which these replace)
-  for (; rows != 0; rows &= rows - 1) f(__ffs((int)rows) - 1);
+template <int MB, int COLS>
+__device__ __forceinline__ void get_sums(const float* sums, int rw, int m, const float (&f)[COLS], float16v (&acc)[1], int lane) {
+  constexpr int RW = WAVES / COLS;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) t = fmaf(f[j], sums[(((j * RW + rw) * MB + m) * 16 + e) * 64 + lane], t);
+    acc[0][e] = t;
+  }
+}
+// A block of 32 channels of a tile's rows as fp32 shares: [share][(query, head)][dh].
+__device__ __forceinline__ void store_share(const PackedAttnArgs& a, float* part, int share, long row, const float16v& acc, int m, int hh) {
+  float* p = part + ((long)share * a.q_rows * a.heads + row) * a.dh;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int c = 32 * m + 8 * g + 4 * hh;
+    if (c < a.dh) *reinterpret_cast<float4*>(p + c) = make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
+  }
 }
 
-constexpr int FWD_WAVES = 8;
-template <int DHP> constexpr int key_stages() { return DHP == 128 ? 3 : 4; }
-
-// Forward.  A workgroup of eight wavefronts owns 256 rows, a wavefront 32 of them: a lane holds one row of q and half of that row's
-// scores, so the running maximum and sum are scalars of the lane; the scores leave the first product in the places from which the
-// second takes them.  Keys and values come in steps of 64 through a ring of stages.  The maximum that the exponents are taken
-// from moves only when a row's has grown by more than a factor of 2^8 (probabilities then reach 2^8, sums 2^8 times the keys:
-// far inside fp32, and bf16 rounds relatively), so the output is rarely rescaled.
-template <int DHP>
-__global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_fwd_mfma_kernel(PackedAttnArgs a) {
+// Forward.  A lane holds one row of q and half of that row's scores, so the running maximum and sum are scalars of the lane; the scores
+// leave the first product in the places from which the second takes them.  Keys and values come through a ring of stages.
+// The maximum that the exponents are taken from moves only when a row's has grown by more than a factor of 2^8 (probabilities
+// then reach 2^8, sums 2^8 times the keys: far inside fp32, and bf16 rounds relatively), so the output is rarely rescaled.
+// Few rows over long keys (a.shares > 1): a workgroup takes a share of the steps and leaves sums, maxima and outputs for
+// packed_join_fwd_kernel.
+template <int DHP, int COLS>
+__global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma_kernel(PackedAttnArgs a) {
   typedef Geo<DHP> G;
-  typedef KeyStream<DHP, FWD_WAVES> KS;
-  constexpr int NST = key_stages<DHP>();
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST * KS::STAGE];
+  typedef Shape<DHP, COLS> S;
+  typedef typename S::KS KS;
+  constexpr int NST = S::NST, RW = WAVES / COLS;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[S::RING];
+  __shared__ float stats[COLS == 1 ? 1 : WAVES][2][64];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  Tile x = find_tile<false>(a, 32 * FWD_WAVES, lane);
-  if (!x.exists) return;
-  x.t = x.n - 1 - x.t;                                     // (causal: long rows first)
-  const int R = x.s.nq * a.group, r0 = 32 * FWD_WAVES * x.t, w0 = r0 + 32 * wave;
-  const int rows_left = R - w0;                            // of this wavefront's 32; none: it only copies
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = wave % RW, col = wave / RW;
+  RowBlock<DHP, COLS> b;
+  if (!b.find(a, rw, lane)) return;
+  const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3;
-  auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
-  const int last = (R < r0 + 32 * FWD_WAVES ? R : r0 + 32 * FWD_WAVES) - 1;
-  const int steps = (seen(last) + 63) >> 6;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
-  const KS ks(a, x.s, x.hk, lds0, dh8, wave, lane);
-  for (int i = 0; i < NST - 1 && i < steps; ++i) ks.issue(i, i, wave, lane);
-  const int r = rows_left > 0 ? w0 + ((lane & 31) < rows_left ? (lane & 31) : rows_left - 1) : R - 1;
-  const RowPlace me = place_of(a, x.hk, r);
-  const bf16_t* qrow = row_of<bf16_t>(a.q, x.s.q0 + me.i, me.h);
+  const KS ks(a, sq, b.x.hk, lds0, dh8, wave, lane);
+  for (int i = 0; i < NST - 1 && b.from + i < b.to; ++i) ks.issue(b.from + i, i, wave, lane);
+  const long n = sq.q0 + b.me.i;
+  const bf16_t* qrow = row_of<bf16_t>(a.q, n, b.me.h);
   bf16x8 fq[G::KK];
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) fq[kk] = own_piece(qrow, kk, dh8, lane);
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) landed(fq[kk]);
-  const int mine = seen_by(x.s, me.i, a.causal);           // keys that this lane's row sees
-  const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
+  const bool few = sq.nk <= FEW;
   const float c = a.scale * LOG2E;
-  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rv = lds0 + Frags<DHP>::rows_lane(lane);
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane) + col * S::SUB * G::TB, rv = lds0 + Frags<DHP>::rows_lane(lane) + col * S::SUB * G::TB;
   float16v o[G::MB];
   zero_acc(o);
   float m = -FLT_MAX, l = 0.f;                             // m: in units of the exponent; l: this half's sum
-  auto step = [&](int i, int at, bool masked) __attribute__((always_inline)) {
+  auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
     const unsigned tk = ck + (unsigned)at * KS::STAGE, tv = rv + (unsigned)at * KS::STAGE;
-    float16v s[2];
+    float16v s[S::SUB];
     zero_acc(s);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int u = 0; u < S::SUB; ++u)
 #pragma unroll
-      for (int kk = 0; kk < G::KK; ++kk) s[b] = mfma(Frags<DHP>::cols(tk, b * G::TB, kk), fq[kk], s[b]);
+      for (int kk = 0; kk < G::KK; ++kk) s[u] = mfma(Frags<DHP>::cols(tk, u * G::TB, kk), fq[kk], s[u]);
     if (masked) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int u = 0; u < S::SUB; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (64 * i + 32 * b + tile_row_of(e, hh) >= mine) s[b][e] = -INFINITY;
+          if (first + 32 * u + tile_row_of(e, hh) >= b.mine) s[u][e] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
+    for (int e = 1; e < 16 * S::SUB; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
     top = fmaxf(top, other_half(top)) * c;
     if (__any(top > m + 8.f)) {
       const float mn = fmaxf(m, top), alpha = fast_exp2(m - mn);
@@ -488,73 +292,133 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_fwd_mfma_kernel(Pack
         for (int e = 0; e < 16; ++e) o[mb][e] *= alpha;
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int u = 0; u < S::SUB; ++u) {
       float p[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        p[e] = fast_exp2(fmaf(s[b][e], c, -m));
+        p[e] = fast_exp2(fmaf(s[u][e], c, -m));
         l += p[e];
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 pt = pack8(p + 8 * t);                // rounded to bf16: the matrix cores' operand
-#pragma unroll
-        for (int mb = 0; mb < G::MB; ++mb) o[mb] = mfma(Frags<DHP>::rows(tv, (2 + b) * G::TB, mb, t), pt, o[mb]);
-      }
+      Operand op;
+      op.set(p, few);
+      op.template times<DHP>(tv, (S::NT + u) * G::TB, o, few);
     }
   };
   int at = 0;
-  for (int i = 0; i < steps; ++i) {
-    if (i + NST - 2 < steps) copies_in_flight<KS::PW * (NST - 2)>();
+  for (int i = b.from; i < b.to; ++i) {
+    if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
     else copies_in_flight<0>();
     workgroup_handover();
-    if (i + NST - 1 < steps) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
-    if (64 * i < most) step(i, at, 64 * i + 64 > fewest);
+    if (i + NST - 1 < b.to) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+    const int first = S::KEYS * i + 32 * S::SUB * col;
+    if (first < b.most) step(first, at, first + 32 * S::SUB > b.fewest);
     at = at == NST - 1 ? 0 : at + 1;
   }
-  __syncthreads();                                         // the ring is free: results leave through it
-  if (rows_left <= 0) return;
   l += other_half(l);
-  const float f = l == 0.f ? 0.f : 1.f / l;
-  store_rows([&](int j) __attribute__((always_inline)) {
-    const RowPlace q = place_of(a, x.hk, w0 + j);
-    return row_out<bf16_t>(a.o, x.s.q0 + q.i, q.h);
-  }, rows_left, o, f, a.dh, ring + wave * 2048, lane);
-  if (lane < 32 && lane < rows_left) a.lse[(long)(x.s.q0 + me.i) * a.heads + me.h] = l == 0.f ? -INFINITY : m + log2f(l);
-  redo_rows(not_finite(o, f * 0.f), rows_left, [&](int j) {
-    const RowPlace q = place_of(a, x.hk, w0 + j);
-    one_forward<bf16_t>(a, x.s, q.i, q.h, lane);
-  });
+  __syncthreads();                                         // the ring is free: results meet in it, or leave through it
+  auto row = [&](int j) __attribute__((always_inline)) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    return row_out<bf16_t>(a.o, sq.q0 + q.i, q.h);
+  };
+  auto redo = [&](int j) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    one_forward<bf16_t>(a, sq, q.i, q.h, lane);
+  };
+  const bool stat = lane < 32 && lane < b.rows_left;
+  if constexpr (COLS == 1) {
+    if (b.rows_left <= 0) return;
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    store_rows(row, b.rows_left, o, f, 0, a.dh, ring + wave * 2048, lane);
+    if (stat) a.lse[n * a.heads + b.me.h] = l == 0.f ? -INFINITY : m + log2f(l);
+    redo_rows(not_finite(o, f * 0.f), b.rows_left, redo);
+  } else {
+    float* const sums = reinterpret_cast<float*>(ring);
+    put_sums<G::MB>(sums, wave, o, lane);
+    stats[wave][0][lane] = m;
+    stats[wave][1][lane] = l;
+    __syncthreads();
+    float f[COLS], top = stats[rw][0][lane], sum = 0.f;
+#pragma unroll
+    for (int j = 1; j < COLS; ++j) top = fmaxf(top, stats[j * RW + rw][0][lane]);
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) {
+      f[j] = fast_exp2(stats[j * RW + rw][0][lane] - top);
+      sum = fmaf(f[j], stats[j * RW + rw][1][lane], sum);
+    }
+    float16v acc[1];
+    if (col < G::MB) get_sums<G::MB, COLS>(sums, rw, col, f, acc, lane);
+    __syncthreads();
+    if (b.rows_left <= 0 || col >= G::MB) return;          // (a block of 32 channels each)
+    if (a.shares > 1) {
+      const long r = n * a.heads + b.me.h;
+      if ((lane & 31) < b.rows_left) store_share(a, a.part, b.share, r, acc[0], col, hh);
+      if (stat && col == 0) {
+        a.part_stats[((long)b.share * a.q_rows * a.heads + r) * 2] = top;
+        a.part_stats[((long)b.share * a.q_rows * a.heads + r) * 2 + 1] = sum;
+      }
+      return;
+    }
+    const float g = sum == 0.f ? 0.f : 1.f / sum;
+    store_rows(row, b.rows_left, acc, g, col, a.dh, ring + wave * 2048, lane);
+    if (stat && col == 0) a.lse[n * a.heads + b.me.h] = sum == 0.f ? -INFINITY : top + log2f(sum);
+    redo_rows(not_finite(acc, g * 0.f), b.rows_left, redo);
+  }
 }
 
-// dq, and minus D = sum_c dout (.) o of every row for the other kernel.  As the forward pass: a lane holds a row of q and of dout,
-// dS leaves the first two products in the places from which the third takes it.
-template <int DHP>
-__global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(PackedAttnArgs a) {
+// The shares of one (query, head): a wavefront, two channels per lane.
+__global__ __launch_bounds__(256) void packed_join_fwd_kernel(PackedAttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long)a.q_rows * a.heads;
+  if (r >= rows) return;
+  const int n = (int)(r / a.heads), h = (int)(r - (long)n * a.heads);
+  const int sq = seq_with(a.q_off, a.q_rows, a.seqs, n);
+  if (sq < 0) return;
+  const Seq s = seq_of(a, sq);
+  if (n < s.q0 || n >= s.q0 + s.nq) return;
+  float top = -FLT_MAX, sum = 0.f, v[2] = {0.f, 0.f};
+  for (int i = lane; i < a.shares; i += 64) top = fmaxf(top, a.part_stats[(i * rows + r) * 2]);
+  top = wave_max(top);
+  const int c = 2 * lane;
+  for (int i = 0; i < a.shares; ++i) {
+    const float f = fast_exp2(a.part_stats[(i * rows + r) * 2] - top);
+    sum = fmaf(f, a.part_stats[(i * rows + r) * 2 + 1], sum);
+    if (c < a.dh) {
+      const float2 x = *reinterpret_cast<const float2*>(a.part + (i * rows + r) * a.dh + c);
+      v[0] = fmaf(f, x.x, v[0]);
+      v[1] = fmaf(f, x.y, v[1]);
+    }
+  }
+  const float g = sum == 0.f ? 0.f : 1.f / sum;
+  if (__any(!(fabsf(v[0] * g) < INFINITY && fabsf(v[1] * g) < INFINITY))) {      // (see redo_rows)
+    one_forward<bf16_t>(a, s, n - s.q0, h, lane);
+    return;
+  }
+  if (c < a.dh) *reinterpret_cast<unsigned*>(row_out<bf16_t>(a.o, n, h) + c) = pack_bf16x2(v[0] * g, v[1] * g);
+  if (lane == 0) a.lse[r] = sum == 0.f ? -INFINITY : top + log2f(sum);
+}
+
+// dq, and for the other kernel minus D = sum_c dout (.) o and minus lse of every row.  As the forward pass: a lane holds a row of q and
+// of dout, dS leaves the first two products in the places from which the third takes it.
+template <int DHP, int COLS>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAttnArgs a) {
   typedef Geo<DHP> G;
-  typedef KeyStream<DHP, FWD_WAVES> KS;
-  constexpr int NST = key_stages<DHP>();
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST * KS::STAGE];
+  typedef Shape<DHP, COLS> S;
+  typedef typename S::KS KS;
+  constexpr int NST = S::NST, RW = WAVES / COLS;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[S::RING];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  Tile x = find_tile<false>(a, 32 * FWD_WAVES, lane);
-  if (!x.exists) return;
-  x.t = x.n - 1 - x.t;
-  const int R = x.s.nq * a.group, r0 = 32 * FWD_WAVES * x.t, w0 = r0 + 32 * wave;
-  const int rows_left = R - w0;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = wave % RW, col = wave / RW;
+  RowBlock<DHP, COLS> b;
+  if (!b.find(a, rw, lane)) return;
+  const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3;
-  auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
-  const int last = (R < r0 + 32 * FWD_WAVES ? R : r0 + 32 * FWD_WAVES) - 1;
-  const int steps = (seen(last) + 63) >> 6;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
-  const KS ks(a, x.s, x.hk, lds0, dh8, wave, lane);
-  for (int i = 0; i < NST - 1 && i < steps; ++i) ks.issue(i, i, wave, lane);
-  const int r = rows_left > 0 ? w0 + ((lane & 31) < rows_left ? (lane & 31) : rows_left - 1) : R - 1;
-  const RowPlace me = place_of(a, x.hk, r);
-  const long n = x.s.q0 + me.i;
-  const bf16_t* qrow = row_of<bf16_t>(a.q, n, me.h);
-  const bf16_t* grow = row_of<bf16_t>(a.dout, n, me.h);
-  const bf16_t* orow = row_of<bf16_t>(a.o, n, me.h);
+  const KS ks(a, sq, b.x.hk, lds0, dh8, wave, lane);
+  for (int i = 0; i < NST - 1 && i < b.to; ++i) ks.issue(i, i, wave, lane);
+  const long n = sq.q0 + b.me.i;
+  const bf16_t* qrow = row_of<bf16_t>(a.q, n, b.me.h);
+  const bf16_t* grow = row_of<bf16_t>(a.dout, n, b.me.h);
+  const bf16_t* orow = row_of<bf16_t>(a.o, n, b.me.h);
   bf16x8 fq[G::KK], fg[G::KK];
   float D = 0.f;
 #pragma unroll
@@ -566,95 +430,106 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 2) void packed_dq_mfma_kernel(Packe
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) { landed(fq[kk]); landed(fg[kk]); }
   D += other_half(D);
-  float L = stat_of(a.lse[n * a.heads + me.h]);
+  float L = stat_of(a.lse[n * a.heads + b.me.h]);
   landed(L);
-  if (rows_left > 0 && lane < 32 && lane < rows_left) {
-    a.dsum[n * a.heads + me.h] = -D;
-    a.nlse[n * a.heads + me.h] = -L;
+  if (col == 0 && lane < 32 && lane < b.rows_left) {
+    a.dsum[n * a.heads + b.me.h] = -D;
+    a.nlse[n * a.heads + b.me.h] = -L;
   }
-  const int mine = seen_by(x.s, me.i, a.causal);
-  const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
+  const bool few = sq.nk <= FEW;
   const float c = a.scale * LOG2E;
-  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rk = lds0 + Frags<DHP>::rows_lane(lane);
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane) + col * S::SUB * G::TB, rk = lds0 + Frags<DHP>::rows_lane(lane) + col * S::SUB * G::TB;
   float16v dq[G::MB];
   zero_acc(dq);
-  auto step = [&](int i, int at, bool masked) __attribute__((always_inline)) {
+  auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
     const unsigned tc = ck + (unsigned)at * KS::STAGE, tr = rk + (unsigned)at * KS::STAGE;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      float16v s[1], dp[1];
+    for (int u = 0; u < S::SUB; ++u) {
+      float16v s[1], dp;
       zero_acc(s);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dp[0][e] = -D;
+      for (int e = 0; e < 16; ++e) dp[e] = -D;
 #pragma unroll
       for (int kk = 0; kk < G::KK; ++kk) {
-        s[0] = mfma(Frags<DHP>::cols(tc, b * G::TB, kk), fq[kk], s[0]);
-        dp[0] = mfma(Frags<DHP>::cols(tc, (2 + b) * G::TB, kk), fg[kk], dp[0]);
+        s[0] = mfma(Frags<DHP>::cols(tc, u * G::TB, kk), fq[kk], s[0]);
+        dp = mfma(Frags<DHP>::cols(tc, (S::NT + u) * G::TB, kk), fg[kk], dp);
       }
       float ds[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = fast_exp2(fmaf(s[0][e], c, -L));
-        ds[e] = p * dp[0][e];
-      }
+      for (int e = 0; e < 16; ++e) ds[e] = fast_exp2(fmaf(s[0][e], c, -L)) * dp[e];
       if (masked) {
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (64 * i + 32 * b + tile_row_of(e, hh) >= mine) ds[e] = 0.f;
+          if (first + 32 * u + tile_row_of(e, hh) >= b.mine) ds[e] = 0.f;
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 dst = pack8(ds + 8 * t);
-#pragma unroll
-        for (int mb = 0; mb < G::MB; ++mb) dq[mb] = mfma(Frags<DHP>::rows(tr, b * G::TB, mb, t), dst, dq[mb]);
-      }
+      Operand op;
+      op.set(ds, few);
+      op.template times<DHP>(tr, u * G::TB, dq, few);
     }
   };
   int at = 0;
-  for (int i = 0; i < steps; ++i) {
-    if (i + NST - 2 < steps) copies_in_flight<KS::PW * (NST - 2)>();
+  for (int i = 0; i < b.to; ++i) {
+    if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
     else copies_in_flight<0>();
     workgroup_handover();
-    if (i + NST - 1 < steps) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
-    if (64 * i < most) step(i, at, 64 * i + 64 > fewest);
+    if (i + NST - 1 < b.to) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+    const int first = S::KEYS * i + 32 * S::SUB * col;
+    if (first < b.most) step(first, at, first + 32 * S::SUB > b.fewest);
     at = at == NST - 1 ? 0 : at + 1;
   }
   __syncthreads();
-  if (rows_left <= 0) return;
-  store_rows([&](int j) __attribute__((always_inline)) {
-    const RowPlace q = place_of(a, x.hk, w0 + j);
-    return row_out<bf16_t>(a.dq, x.s.q0 + q.i, q.h);
-  }, rows_left, dq, a.scale, a.dh, ring + wave * 2048, lane);
-  redo_rows(not_finite(dq, 0.f), rows_left, [&](int j) {
-    const RowPlace q = place_of(a, x.hk, w0 + j);
-    one_dq<bf16_t>(a, x.s, q.i, q.h, row_dsum<bf16_t>(a, x.s.q0 + q.i, q.h, lane), lane);
-  });
+  auto row = [&](int j) __attribute__((always_inline)) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    return row_out<bf16_t>(a.dq, sq.q0 + q.i, q.h);
+  };
+  auto redo = [&](int j) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    one_dq<bf16_t>(a, sq, q.i, q.h, row_dsum<bf16_t>(a, sq.q0 + q.i, q.h, lane), lane);
+  };
+  if constexpr (COLS == 1) {
+    if (b.rows_left <= 0) return;
+    store_rows(row, b.rows_left, dq, a.scale, 0, a.dh, ring + wave * 2048, lane);
+    redo_rows(not_finite(dq, 0.f), b.rows_left, redo);
+  } else {
+    float* const sums = reinterpret_cast<float*>(ring);
+    put_sums<G::MB>(sums, wave, dq, lane);
+    __syncthreads();
+    float f[COLS];
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) f[j] = 1.f;
+    float16v acc[1];
+    if (col < G::MB) get_sums<G::MB, COLS>(sums, rw, col, f, acc, lane);
+    __syncthreads();
+    if (b.rows_left <= 0 || col >= G::MB) return;
+    store_rows(row, b.rows_left, acc, a.scale, col, a.dh, ring + wave * 2048, lane);
+    redo_rows(not_finite(acc, 0.f), b.rows_left, redo);
+  }
 }
 
-// dk, dv.  A workgroup owns 128 keys of a key head, and eight wavefronts: four times 32 keys, twice, for every other tile of 32
-// queries; the two halves' sums meet in LDS at the end.  A lane holds one key's k and v and half of that key's probabilities.
-// (128 keys with four wavefronts: half the wavefronts on a SIMD, or two workgroups on a compute unit that a causal mask leaves
-// unequally long; 256 keys: half as many workgroups to share out.)  Queries come from the last one down, all heads of the group
-// for a tile of queries before the next tile: whatever the mask leaves them, the workgroups of a key head begin with the same
-// tiles and stay in step, so that the tiles come from the XCD's L2.
+// dk, dv.  A workgroup's eight wavefronts own 32 keys each, TURNS wavefronts the same ones: they take every TURNS-th tile of 32 queries
+// in turn, and their sums meet in LDS at the end.  A lane holds one key's k and v and half of that key's probabilities.
+// TURNS = 2, 128 keys; 4, 64 keys, for few of them.  (128 keys with four wavefronts: half the wavefronts on a SIMD, or two
+// workgroups on a compute unit that a causal mask leaves unequally long; 256 keys: half as many workgroups to share out.)
+// Queries come from the last one down, all heads of the group for a tile of queries before the next tile: whatever the mask
+// leaves them, the workgroups of a key head begin with the same tiles and stay in step, so that the tiles come from the XCD's L2.
 // At 128 channels k stays in LDS, which leaves registers for two wavefronts on every SIMD.
-constexpr int KV_KEYS = 128, KV_WAVES = 8;
-template <int DHP>
-__global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(PackedAttnArgs a) {
+template <int DHP, int TURNS>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedAttnArgs a) {
   typedef Geo<DHP> G;
   constexpr bool KLDS = DHP == 128;
-  constexpr int NST = 3;
-  constexpr int STAGE = 4 * G::TB;                         // two tiles of q, two of dout
-  constexpr int PW = 4 * G::COPIES / KV_WAVES;             // copies of a stage by one wavefront
-  constexpr int SUMS = 4 * G::MB * 16 * 64 * 4;            // the sums of four wavefronts, dk or dv
-  constexpr int RING = NST * STAGE + (KLDS ? 4 * G::TB : 0);
+  constexpr int NST = DHP == 128 && TURNS == 4 ? 2 : 3;
+  constexpr int KW = WAVES / TURNS, KEYS = 32 * KW;
+  constexpr int STAGE = 2 * TURNS * G::TB;                 // TURNS tiles of q, as many of dout
+  constexpr int PW = 2 * TURNS * G::COPIES / WAVES;        // copies of a stage by one wavefront
+  constexpr int SUMS = KW * (TURNS - 1) * G::MB * 16 * 64 * 4;     // the sums of all but the first, dk or dv
+  constexpr int RING = NST * STAGE + (KLDS ? KW * G::TB : 0);
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RING > SUMS ? RING : SUMS];
-  __shared__ __attribute__((aligned(256))) float stats[NST][2][2][64];           // [stage][tile][-lse | -D][32 rows, and again]
+  __shared__ __attribute__((aligned(256))) float stats[NST][TURNS][2][64];       // [stage][tile][-lse | -D][32 rows, and again]
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), turn = wave >> 2;
-  const Tile x = find_tile<true>(a, KV_KEYS, lane);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), turn = wave / KW, kw = wave % KW;
+  const Tile x = find_tile<true>(a, KEYS, lane);
   if (!x.exists) return;
-  const int k0 = KV_KEYS * x.t, w0 = k0 + 32 * (wave & 3);
+  const int k0 = KEYS * x.t, w0 = k0 + 32 * kw;
   const int keys_left = x.s.nk - w0;
   const int dh8 = a.dh >> 3;
   const int nq = x.s.nq, shift = x.s.nk - nq;
@@ -665,29 +540,31 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(Pack
   };
   const int top = (nq - 1) >> 5;                           // last tile of queries
   const int tiles = nq > 0 ? (top + 1 - (first_query(k0) >> 5)) * a.group : 0;     // times heads
-  const int steps = (tiles + 1) >> 1;
+  const int steps = (tiles + TURNS - 1) / TURNS;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const unsigned lds1 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(stats));
-  const unsigned ldq = (unsigned)(a.q.row * 2), ldg = (unsigned)(a.dout.row * 2);
-  // copy u of this wavefront: of tile (q, q, dout, dout) wave PW / COPIES ..., the same one for all of them
+  // this wavefront's copies: PW parts of one of the stage's tiles, and a statistic of another
   static_assert(G::COPIES % PW == 0, "a wavefront's copies are of one tile");
-  const int ct = wave * PW / G::COPIES, cp = wave * PW % G::COPIES;
-  const unsigned ld = ct < 2 ? ldq : ldg;
+  const int ct = wave * PW / G::COPIES, cp = wave * PW % G::COPIES, st = (wave >> 1) % TURNS;
+  const HeadRows& from = ct < TURNS ? a.q : a.dout;
+  const unsigned ld = (unsigned)(from.row * 2);
   unsigned off[PW];
 #pragma unroll
   for (int u = 0; u < PW; ++u) off[u] = copy_offset<DHP>(ld, cp + u, 32, dh8, lane);
-  int ih = 0, iq = top;                                    // the next tile to ask for: its head of the group, its tile of queries
-  auto ask = [&](int at) __attribute__((always_inline)) {
-    int h[2], t[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {                          // (an odd number of tiles: one that nobody reads, the first one below or tile 0)
-      h[b] = x.hk * a.group + ih;
-      t[b] = iq < 0 ? 0 : iq;
-      if (++ih == a.group) { ih = 0; --iq; }
+  // a place in the list of (tile of queries, head of the group)
+  struct Place {
+    int h, q;
+    __device__ __forceinline__ void on(int n, int group) {
+      for (h += n; h >= group; h -= group) --q;
     }
+  };
+  Place pc{0, top}, pt{0, top};
+  pc.on(ct % TURNS, a.group);
+  pt.on(st, a.group);
+  auto ask = [&](int at) __attribute__((always_inline)) {
     {
-      const int b = ct & 1, first = 32 * (b ? t[1] : t[0]), left = nq - first;
-      const unsigned char* base = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(ct < 2 ? a.q : a.dout, x.s.q0 + first, b ? h[1] : h[0]));
+      const int first = pc.q < 0 ? 0 : 32 * pc.q, left = nq - first;               // (past the last: a tile that nobody reads)
+      const unsigned char* base = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(from, x.s.q0 + first, x.hk * a.group + pc.h));
       const unsigned dst = lds0 + (unsigned)at * STAGE + (unsigned)(wave * PW) * 1024u;
       if (left >= 32) {
 #pragma unroll
@@ -698,9 +575,11 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(Pack
       }
     }
     // (every wavefront copies a statistic: the waits count the same for all)
-    const int b = (wave >> 1) & 1, first = 32 * (b ? t[1] : t[0]), r = first + (lane & 31) < nq ? first + (lane & 31) : nq - 1;
-    copy4_to_lds((wave & 1 ? a.dsum : a.nlse) + (long)(x.s.q0 + r) * a.heads + (b ? h[1] : h[0]),
-                 lds1 + (unsigned)at * 1024u + (unsigned)(wave & 3) * 256u);
+    const int first = pt.q < 0 ? 0 : 32 * pt.q, r = first + (lane & 31) < nq ? first + (lane & 31) : nq - 1;
+    copy4_to_lds((wave & 1 ? a.dsum : a.nlse) + (long)(x.s.q0 + r) * a.heads + x.hk * a.group + pt.h,
+                 lds1 + (unsigned)at * (TURNS * 512u) + (unsigned)(2 * st + (wave & 1)) * 256u);
+    pc.on(TURNS, a.group);
+    pt.on(TURNS, a.group);
   };
   for (int i = 0; i < NST - 1 && i < steps; ++i) ask(i);
   const int key = keys_left > 0 ? w0 + ((lane & 31) < keys_left ? (lane & 31) : keys_left - 1) : x.s.nk - 1;
@@ -708,7 +587,7 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(Pack
   const bf16_t* vrow = row_of<bf16_t>(a.v, x.s.k0 + key, x.hk);
   const unsigned cl = Frags<DHP>::cols_lane(lane), cq = lds0 + cl + (unsigned)turn * G::TB;
   const unsigned rq = lds0 + Frags<DHP>::rows_lane(lane) + (unsigned)turn * G::TB;
-  const unsigned kl = lds0 + NST * STAGE + (unsigned)(wave & 3) * G::TB + cl;
+  const unsigned kl = lds0 + NST * STAGE + (unsigned)kw * G::TB + cl;
   bf16x8 fk[G::KK], fv[G::KK];
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) { fk[kk] = own_piece(krow, kk, dh8, lane); fv[kk] = own_piece(vrow, kk, dh8, lane); }
@@ -716,11 +595,12 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(Pack
   for (int kk = 0; kk < G::KK; ++kk) {
     landed(fk[kk]);
     landed(fv[kk]);
-    // (both wavefronts of these keys write the same)
-    if (KLDS) put_cols_lds<DHP>(ring + NST * STAGE + (wave & 3) * G::TB, kk, lane, fk[kk]);
+    // (all wavefronts of these keys write the same)
+    if (KLDS) put_cols_lds<DHP>(ring + NST * STAGE + kw * G::TB, kk, lane, fk[kk]);
   }
   const int mine = first_query(key);                       // the first query that sees this lane's key
   const int begin = keys_left > 0 ? first_query(w0) : nq, all = keys_left > 0 ? first_query(w0 + (keys_left < 32 ? keys_left : 32) - 1) : nq;
+  const bool few = nq <= FEW;
   const float c = a.scale * LOG2E;
   float16v dk[G::MB], dv[G::MB];
   zero_acc(dk);
@@ -738,7 +618,7 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(Pack
       dp[4 * g] = u.x; dp[4 * g + 1] = u.y; dp[4 * g + 2] = u.z; dp[4 * g + 3] = u.w;
     }
 #pragma unroll
-    for (int kk = 0; kk < G::KK; ++kk) dp = mfma(Frags<DHP>::cols(tc, 2 * G::TB, kk), fv[kk], dp);
+    for (int kk = 0; kk < G::KK; ++kk) dp = mfma(Frags<DHP>::cols(tc, TURNS * G::TB, kk), fv[kk], dp);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn][0][8 * g + 4 * hh]);
@@ -754,115 +634,118 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void packed_dkdv_mfma_kernel(Pack
         if (i < mine || i >= nq) p[e] = 0.f;
       }
     }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const bf16x8 pt = pack8(p + 8 * t);
-#pragma unroll
-      for (int mb = 0; mb < G::MB; ++mb) dv[mb] = mfma(Frags<DHP>::rows(tr, 2 * G::TB, mb, t), pt, dv[mb]);
-    }
+    Operand op;
+    op.set(p, few);
+    op.template times<DHP>(tr, TURNS * G::TB, dv, few);
 #pragma unroll
     for (int e = 0; e < 16; ++e) p[e] *= dp[e];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const bf16x8 dst = pack8(p + 8 * t);
-#pragma unroll
-      for (int mb = 0; mb < G::MB; ++mb) dk[mb] = mfma(Frags<DHP>::rows(tr, 0, mb, t), dst, dk[mb]);
-    }
+    op.set(p, few);
+    op.template times<DHP>(tr, 0, dk, few);
   };
-  int at = 0, sh = turn, sq = top;                         // this wavefront's next tile
-  if (sh >= a.group) { sh -= a.group; --sq; }
+  int at = 0;
+  Place me{0, top};                                        // this wavefront's next tile
+  me.on(turn, a.group);
   for (int i = 0; i < steps; ++i) {
     if (i + NST - 2 < steps) copies_in_flight<(PW + 1) * (NST - 2)>();
     else copies_in_flight<0>();
     workgroup_handover();
     if (i + NST - 1 < steps) ask(at == 0 ? NST - 1 : at - 1);
-    const int first = 32 * sq;
-    if (2 * i + turn < tiles && first + 32 > begin && keys_left > 0) step(first, at, first < all || first + 32 > nq);
+    const int first = 32 * me.q;
+    if (TURNS * i + turn < tiles && first + 32 > begin && keys_left > 0) step(first, at, first < all || first + 32 > nq);
     at = at == NST - 1 ? 0 : at + 1;
-    sh += 2;
-    if (sh >= a.group) {
-      sh -= a.group;
-      --sq;
-      if (sh >= a.group) { sh -= a.group; --sq; }          // (a group of one)
-    }
+    me.on(TURNS, a.group);
   }
-  float* const sums = reinterpret_cast<float*>(ring) + (wave & 3) * (G::MB * 16 * 64) + lane;
   auto meet = [&](float16v (&acc)[G::MB]) __attribute__((always_inline)) {
+    float* const sums = reinterpret_cast<float*>(ring) + kw * (G::MB * 16 * 64) + lane;
     __syncthreads();                                       // (the ring, or the sums before, are free)
-    if (turn == 1) {
+    if (turn > 0) {
 #pragma unroll
       for (int m = 0; m < G::MB; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sums[(m * 16 + e) * 64] = acc[m][e];
+        for (int e = 0; e < 16; ++e) sums[((turn - 1) * KW * G::MB * 16 + m * 16 + e) * 64] = acc[m][e];
     }
     __syncthreads();
     if (turn == 0) {
 #pragma unroll
-      for (int m = 0; m < G::MB; ++m)
+      for (int j = 0; j < TURNS - 1; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[m][e] += sums[(m * 16 + e) * 64];
+        for (int m = 0; m < G::MB; ++m)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[m][e] += sums[(j * KW * G::MB * 16 + m * 16 + e) * 64];
     }
   };
   meet(dk);
   meet(dv);
   __syncthreads();
-  if (turn == 1 || keys_left <= 0) return;
+  if (turn > 0 || keys_left <= 0) return;
   unsigned char* stg = ring + wave * 2048;
-  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, x.s.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale,
+  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, x.s.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale, 0,
              a.dh, stg, lane);
-  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, x.s.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, a.dh,
-             stg, lane);
+  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, x.s.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, 0,
+             a.dh, stg, lane);
   redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, lane); });
 }
 
-// workgroups for tiles of `per` rows (keys)
-template <bool KEYS>
-unsigned tile_grid(const PackedAttnArgs& a, int per) {
-  const long rows = KEYS ? a.k_rows : (long)a.q_rows * a.group;
-  if (rows == 0) return 0;
-  const bool equal = KEYS ? !a.k_off : !a.q_off;
-  const long tiles = equal ? a.seqs * ((rows / a.seqs + per - 1) / per) : rows / per + a.seqs;
-  return (unsigned)(tiles * a.kv_heads);
-}
+// 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64 (64 keys).
+constexpr unsigned CUS = 256;
 template <int DHP>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  if (const unsigned grid = tile_grid<false>(a, 32 * FWD_WAVES)) packed_fwd_mfma_kernel<DHP><<<grid, 64 * FWD_WAVES, 0, s>>>(a);
+  const unsigned wide = tile_grid<false>(a, 256), narrow = tile_grid<false>(a, 64);
+  if (wide == 0) return hipSuccess;
+  if (a.shares == 1 && wide >= CUS) {
+    packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  packed_fwd_mfma_kernel<DHP, 4><<<dim3(narrow, a.shares), 64 * WAVES, 0, s>>>(a);
+  if (a.shares > 1) packed_join_fwd_kernel<<<(unsigned)(((long)a.q_rows * a.heads + 3) / 4), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int DHP>
 hipError_t bwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  if (const unsigned grid = tile_grid<false>(a, 32 * FWD_WAVES)) packed_dq_mfma_kernel<DHP><<<grid, 64 * FWD_WAVES, 0, s>>>(a);
-  if (const unsigned grid = tile_grid<true>(a, KV_KEYS)) packed_dkdv_mfma_kernel<DHP><<<grid, 64 * KV_WAVES, 0, s>>>(a);
+  const unsigned rows = tile_grid<false>(a, 256), keys = tile_grid<true>(a, 128);
+  if (rows >= CUS) packed_dq_mfma_kernel<DHP, 1><<<rows, 64 * WAVES, 0, s>>>(a);
+  else if (rows > 0) packed_dq_mfma_kernel<DHP, 4><<<tile_grid<false>(a, 64), 64 * WAVES, 0, s>>>(a);
+  if (keys >= CUS) packed_dkdv_mfma_kernel<DHP, 2><<<keys, 64 * WAVES, 0, s>>>(a);
+  else if (keys > 0) packed_dkdv_mfma_kernel<DHP, 4><<<tile_grid<true>(a, 64), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t fwd_t(const PackedAttnArgs& a, hipStream_t s) {
-  if (a.q_rows == 0) return hipSuccess;
-  packed_fwd_rows_kernel<T><<<(unsigned)((long)a.q_rows * a.heads), 64, 0, s>>>(a);
-  return hipGetLastError();
+// Shares of the keys for the forward pass, where there are few rows: enough for two workgroups on every compute unit, each with four
+// steps of 128 keys at least.
+int fwd_shares(int dtype, const PackedAttnArgs& a) {
+  if (dtype == 0 || a.q_rows == 0) return 1;
+  const long groups = tile_grid<false>(a, 64);
+  long n = 2 * CUS / groups;
+  const long most = a.k_rows / a.seqs / 512;
+  if (n > most) n = most;
+  return n < 2 ? 1 : (int)n;
 }
-template <typename T>
-hipError_t bwd_t(const PackedAttnArgs& a, hipStream_t s) {
-  if (a.q_rows > 0) packed_dq_rows_kernel<T><<<(unsigned)((long)a.q_rows * a.heads), 64, 0, s>>>(a);
-  if (a.k_rows > 0) packed_dkdv_rows_kernel<T><<<(unsigned)((long)a.k_rows * a.kv_heads), 64, 0, s>>>(a);
-  return hipGetLastError();
-}
+size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
+size_t row_floats(const PackedAttnArgs& a) { return aligned((size_t)a.q_rows * a.heads * 4); }
 
 }  // namespace
 
 size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a) {
-  (void)dtype;
-  return 2 * (((size_t)a.q_rows * a.heads * 4 + 255) / 256 * 256);
+  const size_t shares = fwd_shares(dtype, a), rows = (size_t)a.q_rows * a.heads;
+  const size_t fwd = shares > 1 ? aligned(shares * rows * a.dh * 4) + aligned(shares * rows * 8) : 0, bwd = 2 * row_floats(a);
+  return fwd > bwd ? fwd : bwd;
 }
-hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void*, hipStream_t s) {
-  return dtype == 0 ? fwd_t<float>(a, s) : a.dh <= 64 ? fwd_mfma<64>(a, s) : fwd_mfma<128>(a, s);
+hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s) {
+  if (dtype == 0) return launch_packed_attn_fwd_f32(a, s);
+  PackedAttnArgs b = a;
+  b.shares = fwd_shares(dtype, a);
+  if (b.shares > 1) {
+    b.part = reinterpret_cast<float*>(workspace);
+    b.part_stats = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + aligned((size_t)b.shares * a.q_rows * a.heads * a.dh * 4));
+  }
+  return a.dh <= 64 ? fwd_mfma<64>(b, s) : fwd_mfma<128>(b, s);
 }
 hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s) {
   PackedAttnArgs b = a;
+  b.shares = 1;
   b.dsum = reinterpret_cast<float*>(workspace);
-  b.nlse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + packed_attn_ws_bytes(dtype, a) / 2);
-  return dtype == 0 ? bwd_t<float>(b, s) : a.dh <= 64 ? bwd_mfma<64>(b, s) : bwd_mfma<128>(b, s);
+  b.nlse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + row_floats(a));
+  return dtype == 0 ? launch_packed_attn_bwd_f32(b, s) : a.dh <= 64 ? bwd_mfma<64>(b, s) : bwd_mfma<128>(b, s);
 }
 
 }  // namespace hbp

@@ -243,6 +243,10 @@ struct PackedAttnArgs {
   float* lse;               // [q_rows, heads]
   float* dsum;              // [q_rows, heads], workspace: minus rowsum(dout (.) o)
   float* nlse;              // [q_rows, heads], workspace: minus lse; minus infinity where a row weighs nothing
+  // forward, set by the launcher: shares of the keys, and what they leave in the workspace
+  int shares;
+  float* part;              // [share][q_rows heads][dh]
+  float* part_stats;        // [share][q_rows heads][maximum | sum]
   const int* q_off;         // [seqs + 1] or NULL: equal lengths
   const int* k_off;
   int seqs, q_rows, k_rows;
