@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 from dataclasses import dataclass
@@ -137,11 +138,12 @@ def lib() -> C.CDLL:
                                          C.POINTER(hbp_optim_state), C.c_void_p]
         L.hbp_train_step.argtypes = [C.POINTER(hbp_desc), C.c_int, C.POINTER(hbp_buffers), C.c_void_p, C.c_void_p,
                                      C.POINTER(hbp_optim), C.POINTER(hbp_optim_state), C.c_void_p]
-        L.hbp_rotary.argtypes = [C.POINTER(hbp_rotary_desc), C.c_int, C.c_int64, C.c_int, C.c_int, C.POINTER(hbp_heads),
-                                 C.POINTER(hbp_heads), C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_void_p]
+        # (hbp_heads and hbp_attention_buffers: packed bytes, or byref of the struct)
+        L.hbp_rotary.argtypes = [C.POINTER(hbp_rotary_desc), C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_void_p]
         L.hbp_attention_workspace_size.argtypes = [C.POINTER(hbp_attention_desc), C.POINTER(C.c_size_t)]
         for n in ("hbp_attention_forward", "hbp_attention_backward"):
-            getattr(L, n).argtypes = [C.POINTER(hbp_attention_desc), C.POINTER(hbp_attention_buffers), C.c_void_p]
+            getattr(L, n).argtypes = [C.POINTER(hbp_attention_desc), C.c_void_p, C.c_void_p]
         L.hbp_profile_enable.argtypes = [C.c_int]
         L.hbp_profile_read.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.hbp_status_string.argtypes = [C.c_int]
@@ -389,57 +391,78 @@ def make_rotary(dims: int, layout: str = "half", base: float = 10000.0, scaling:
                            base, factor, low, high, original)
 
 
-def _storage_type(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise ValueError(f"storage type {t.dtype}: float32 and bfloat16 are known")
+_TYPES = None
 
 
-def _heads(t, name: str) -> hbp_heads:
-    """A [rows, heads, dh] tensor, channels next to each other."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name}: expected [rows, heads, dh] with the channels next to each other, got {tuple(t.shape)} "
-                         f"with strides {t.stride()}")
-    return hbp_heads(t.data_ptr() if t.numel() else None, t.stride(0), t.stride(1))
+def _storage_type(dtype) -> int:
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"storage type {dtype}: float32 and bfloat16 are known")
+    return kind
 
 
-def _same(name: str, t, shape, dtype, device) -> None:
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+def _heads(name: str, t, shape, dtype, device: int) -> tuple:
+    """The fields of an hbp_heads for a [rows, heads, dh] tensor, channels next to each other.  (These checks are on the way of
+    every call: plain comparisons, the messages made only where one fails.)"""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on GPU {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    row, head, channel = t.stride()
+    if channel != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: the channels of a head must be next to each other, got strides {t.stride()}")
+    return t.data_ptr(), row, head
 
 
-def _int32s(name: str, t, n: int, device) -> Optional[int]:
-    import torch
+def _plain(name: str, t, shape, dtype, device: int) -> Optional[int]:
+    """The address of a contiguous tensor, or None."""
     if t is None:
         return None
-    _same(name, t, (n,), torch.int32, device)
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype}, contiguous, on GPU {device}, got {tuple(t.shape)} {t.dtype} on "
+                         f"{t.device} with strides {t.stride()}")
     return t.data_ptr()
 
 
-def _on(t):
-    """The tensor's device made the current one for the time of a call."""
+def _device_of(name: str, t) -> int:
+    if t.dim() != 3:
+        raise ValueError(f"{name}: expected [rows, heads, dh], got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a tensor on the GPU, got {t.device}")
+    return t.get_device()
+
+
+def _launch(name: str, device: int, call, *args, stream) -> None:
+    """call(*args, stream) with `device` the current one."""
     import torch
-    if t.device.type != "cuda":
-        raise ValueError(f"expected tensors on the GPU, got {t.device}")
-    return torch.cuda.device(t.device)
+    if torch.cuda.current_device() == device:
+        st = call(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            st = call(*args, _stream(stream))
+    if st != HBP_OK:
+        raise HbpError(st, name)
+
+
+_pack_heads = struct.Struct("Qqq").pack
 
 
 def hbp_rotary(rotary: hbp_rotary_desc, x, out, positions=None, first: int = 0, period: int = 0, inverse: bool = False,
                stream=None) -> None:
     """out := x turned by its rows' positions (inverse: turned back, the gradient's way); x, out: [rows, heads, dh], out may
     be x.  positions: int32, one per row; without them row n is at first + n, or first + n % period."""
-    rows, heads, dh = x.shape
-    hx, ho = _heads(x, "x"), _heads(out, "out")
-    _same("out", out, x.shape, x.dtype, x.device)
-    pos = _int32s("positions", positions, rows, x.device)
-    with _on(x):
-        _call("hbp_rotary", lib().hbp_rotary(C.byref(rotary), _storage_type(x), rows, heads, dh, C.byref(hx), C.byref(ho), pos,
-                                             first, period, 1 if inverse else 0, _stream(stream)))
+    device, shape, dtype = _device_of("x", x), x.shape, x.dtype
+    kind = _storage_type(dtype)
+    hx = _pack_heads(*_heads("x", x, shape, dtype, device))
+    ho = _pack_heads(*_heads("out", out, shape, dtype, device))
+    pos = None
+    if positions is not None:
+        import torch
+        pos = _plain("positions", positions, shape[:1], torch.int32, device)
+    _launch("hbp_rotary", device, lib().hbp_rotary, C.byref(rotary), kind, *shape, hx, ho, pos, first, period, 1 if inverse else 0,
+            stream=stream)
 
 
 @dataclass
@@ -459,26 +482,27 @@ class Attention:
     dv: "object" = None
     workspace: "object" = None
 
-    def buffers(self, dout=None) -> hbp_attention_buffers:
+    def buffers(self, dout=None) -> bytes:
+        """The C struct hbp_attention_buffers of these tensors, each checked against the descriptor; without dout no gradients."""
         import torch
-        q, k, d = self.q, self.k, self.desc
+        d, q, ws = self.desc, self.q, self.workspace
+        device, dtype = _device_of("q", q), q.dtype
         rows, kv = (d.q_rows, d.heads, d.dh), (d.k_rows, d.kv_heads, d.dh)
-        b = hbp_attention_buffers(C.sizeof(hbp_attention_buffers))
-        named = [("q", q, rows), ("k", k, kv), ("v", self.v, kv), ("o", self.o, rows)]
+        grads = (0,) * 12
         if dout is not None:
-            named += [("dout", dout, rows), ("dq", self.dq, rows), ("dk", self.dk, kv), ("dv", self.dv, kv)]
-        for name, t, shape in named:
-            _same(name, t, shape, q.dtype, q.device)
-            setattr(b, name, _heads(t, name))
-        _same("lse", self.lse, rows[:2], torch.float32, q.device)
-        if not self.lse.is_contiguous():
-            raise ValueError("lse: not contiguous")
-        b.lse = self.lse.data_ptr()
-        b.q_offsets = _int32s("q_offsets", self.q_offsets, d.seqs + 1, q.device)
-        b.k_offsets = _int32s("k_offsets", self.k_offsets, d.seqs + 1, q.device)
-        if self.workspace is not None:
-            b.workspace, b.workspace_bytes = self.workspace.data_ptr(), self.workspace.numel() * self.workspace.element_size()
-        return b
+            grads = (*_heads("dout", dout, rows, dtype, device), *_heads("dq", self.dq, rows, dtype, device),
+                     *_heads("dk", self.dk, kv, dtype, device), *_heads("dv", self.dv, kv, dtype, device))
+        off = (d.seqs + 1,)
+        return _pack_attention(_ATTENTION_SIZE, *_heads("q", q, rows, dtype, device), *_heads("k", self.k, kv, dtype, device),
+                               *_heads("v", self.v, kv, dtype, device), *_heads("o", self.o, rows, dtype, device), *grads,
+                               _plain("lse", self.lse, rows[:2], torch.float32, device),
+                               _plain("q_offsets", self.q_offsets, off, torch.int32, device) or 0,
+                               _plain("k_offsets", self.k_offsets, off, torch.int32, device) or 0,
+                               0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size())
+
+
+_ATTENTION_SIZE = C.sizeof(hbp_attention_buffers)
+_pack_attention = struct.Struct("Ixxxx" + "Qqq" * 8 + "QQQQQ").pack
 
 
 def attention_workspace_size(desc: hbp_attention_desc) -> int:
@@ -497,31 +521,31 @@ def make_attention(q, k, v, causal: bool = True, q_offsets=None, k_offsets=None,
             seqs = off.numel() - 1
     if q_offsets is not None and k_offsets is not None and q_offsets.numel() != k_offsets.numel():
         raise ValueError("q_offsets and k_offsets: different numbers of sequences")
-    dh = q.shape[2]
-    desc = hbp_attention_desc(C.sizeof(hbp_attention_desc), _storage_type(q), q.shape[1], k.shape[1], dh, 1 if causal else 0,
-                              dh ** -0.5 if scale is None else scale, 0.0, seqs, q.shape[0], k.shape[0])
-    with _on(q):
-        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        a = Attention(desc, q, k, v, new(q) if o is None else o,
-                      torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse, q_offsets, k_offsets)
-        if grad:
-            a.dq, a.dk, a.dv = new(q), new(k), new(v)
+    device = _device_of("q", q)
+    for name, t in (("k", k), ("v", v)):
+        _device_of(name, t)
+    rows, heads, dh = q.shape
+    desc = hbp_attention_desc(C.sizeof(hbp_attention_desc), _storage_type(q.dtype), heads, k.shape[1], dh, 1 if causal else 0,
+                              dh ** -0.5 if scale is None else scale, 0.0, seqs, rows, k.shape[0])
+    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    a = Attention(desc, q, k, v, new(q) if o is None else o,
+                  torch.empty((rows, heads), dtype=torch.float32, device=q.device) if lse is None else lse, q_offsets, k_offsets)
+    if grad:
+        a.dq, a.dk, a.dv = new(q), new(k), new(v)
+    with torch.cuda.device(device):
         a.workspace = torch.empty(attention_workspace_size(desc), dtype=torch.uint8, device=q.device)
+    a.buffers()                                            # (refuses what does not fit)
     return a
 
 
 def hbp_attention_forward(a: Attention, stream=None) -> None:
     """a.o, a.lse from a.q, a.k, a.v."""
-    b = a.buffers()
-    with _on(a.q):
-        _call("hbp_attention_forward", lib().hbp_attention_forward(C.byref(a.desc), C.byref(b), _stream(stream)))
+    _launch("hbp_attention_forward", a.q.get_device(), lib().hbp_attention_forward, C.byref(a.desc), a.buffers(), stream=stream)
 
 
 def hbp_attention_backward(a: Attention, dout, stream=None) -> None:
     """a.dq, a.dk, a.dv from a.q, a.k, a.v, a.o, a.lse and the gradient of a.o."""
-    b = a.buffers(dout)
-    with _on(a.q):
-        _call("hbp_attention_backward", lib().hbp_attention_backward(C.byref(a.desc), C.byref(b), _stream(stream)))
+    _launch("hbp_attention_backward", a.q.get_device(), lib().hbp_attention_backward, C.byref(a.desc), a.buffers(dout), stream=stream)
 
 
 def profile_enable(on: bool) -> None:

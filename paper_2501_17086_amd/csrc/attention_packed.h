@@ -285,9 +285,115 @@ unsigned tile_grid(const PackedAttnArgs& a, int per) {
   return (unsigned)(tiles * a.kv_heads);
 }
 
+// ------------------------------------------------------------------------------------------------------------
+// shares: a workgroup that took part of the other side's steps leaves its sums in fp32, [share][row][dh]; a wavefront per row joins them
+// ------------------------------------------------------------------------------------------------------------
+template <int MB>
+__device__ __forceinline__ void store_share(float* part, long row, const float16v (&acc)[MB], int m0, int dh, int hh) {
+  float* p = part + row * dh;
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = 32 * (m0 + m) + 8 * g + 4 * hh;
+      if (c < dh) *reinterpret_cast<float4*>(p + c) = make_float4(acc[m][4 * g], acc[m][4 * g + 1], acc[m][4 * g + 2], acc[m][4 * g + 3]);
+    }
+}
+__device__ __forceinline__ void store2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ __forceinline__ void store2(bf16_t* p, float a, float b) { *reinterpret_cast<unsigned*>(p) = pack_bf16x2(a, b); }
+__device__ __forceinline__ bool all_finite(float a, float b) { return !__any(!(fabsf(a) < INFINITY && fabsf(b) < INFINITY)); }
+// channels 2 lane, 2 lane + 1 of `shares` shares of a row, `stride` floats apart
+__device__ __forceinline__ float2 sum_shares(const float* p, long stride, int shares, int dh, int lane) {
+  float2 v = make_float2(0.f, 0.f);
+  if (2 * lane < dh)
+    for (int i = 0; i < shares; ++i) {
+      const float2 x = *reinterpret_cast<const float2*>(p + i * stride + 2 * lane);
+      v.x += x.x;
+      v.y += x.y;
+    }
+  return v;
+}
+// The (query, head) of a wavefront and its sequence; false: it is in none.
+__device__ __forceinline__ bool joined_row(const PackedAttnArgs& a, long r, Seq& s, int& n, int& h) {
+  if (r >= (long)a.q_rows * a.heads) return false;
+  n = (int)(r / a.heads);
+  h = (int)(r - (long)n * a.heads);
+  const int sq = seq_with(a.q_off, a.q_rows, a.seqs, n);
+  if (sq < 0) return false;
+  s = seq_of(a, sq);
+  return n >= s.q0 && n < s.q0 + s.nq;
+}
+template <typename T>
+__global__ __launch_bounds__(256) void packed_join_fwd_kernel(PackedAttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long)a.q_rows * a.heads;
+  Seq s;
+  int n, h;
+  if (!joined_row(a, r, s, n, h)) return;
+  float top = -FLT_MAX, sum = 0.f, v[2] = {0.f, 0.f};
+  for (int i = lane; i < a.shares; i += 64) top = fmaxf(top, a.part_stats[(i * rows + r) * 2]);
+  top = wave_max(top);
+  const int c = 2 * lane;
+  for (int i = 0; i < a.shares; ++i) {
+    const float f = fast_exp2(a.part_stats[(i * rows + r) * 2] - top);
+    sum = fmaf(f, a.part_stats[(i * rows + r) * 2 + 1], sum);
+    if (c < a.dh) {
+      const float2 x = *reinterpret_cast<const float2*>(a.part + (i * rows + r) * a.dh + c);
+      v[0] = fmaf(f, x.x, v[0]);
+      v[1] = fmaf(f, x.y, v[1]);
+    }
+  }
+  const float g = sum == 0.f ? 0.f : 1.f / sum;
+  if (!all_finite(v[0] * g, v[1] * g)) {                   // (see redo_rows)
+    one_forward<T>(a, s, n - s.q0, h, lane);
+    return;
+  }
+  if (c < a.dh) store2(row_out<T>(a.o, n, h) + c, v[0] * g, v[1] * g);
+  if (lane == 0) a.lse[r] = sum == 0.f ? -INFINITY : top + log2f(sum);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void packed_join_dq_kernel(PackedAttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long)a.q_rows * a.heads;
+  Seq s;
+  int n, h;
+  if (!joined_row(a, r, s, n, h)) return;
+  const float2 v = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane);
+  if (!all_finite(v.x, v.y)) {
+    one_dq<T>(a, s, n - s.q0, h, -a.dsum[r], lane);
+    return;
+  }
+  if (2 * lane < a.dh) store2(row_out<T>(a.dq, n, h) + 2 * lane, v.x * a.scale, v.y * a.scale);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void packed_join_dkdv_kernel(PackedAttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long)a.k_rows * a.kv_heads;
+  if (r >= rows) return;
+  const int n = (int)(r / a.kv_heads), hk = (int)(r - (long)n * a.kv_heads);
+  const int sq = seq_with(a.k_off, a.k_rows, a.seqs, n);
+  if (sq < 0) return;
+  const Seq s = seq_of(a, sq);
+  if (n < s.k0 || n >= s.k0 + s.nk) return;
+  const float2 k = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane);
+  const float2 v = sum_shares(a.part + (a.shares * rows + r) * a.dh, rows * a.dh, a.shares, a.dh, lane);
+  if (!all_finite(k.x + k.y, v.x + v.y)) {
+    one_dkdv<T>(a, s, n - s.k0, hk, lane);
+    return;
+  }
+  if (2 * lane < a.dh) {
+    store2(row_out<T>(a.dk, n, hk) + 2 * lane, k.x * a.scale, k.y * a.scale);
+    store2(row_out<T>(a.dv, n, hk) + 2 * lane, v.x, v.y);
+  }
+}
+
+constexpr unsigned CUS = 256;
+constexpr int F32_ROWS = 128;            // rows (keys) of a workgroup of the fp32 kernels
+
 }  // namespace
 
-hipError_t launch_packed_attn_fwd_f32(const PackedAttnArgs& a, hipStream_t s);
-hipError_t launch_packed_attn_bwd_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s);
 
 }  // namespace hbp

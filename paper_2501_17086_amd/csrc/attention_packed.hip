@@ -217,16 +217,6 @@ __device__ __forceinline__ void get_sums(const float* sums, int rw, int m, const
     acc[0][e] = t;
   }
 }
-// A block of 32 channels of a tile's rows as fp32 shares: [share][(query, head)][dh].
-__device__ __forceinline__ void store_share(const PackedAttnArgs& a, float* part, int share, long row, const float16v& acc, int m, int hh) {
-  float* p = part + ((long)share * a.q_rows * a.heads + row) * a.dh;
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int c = 32 * m + 8 * g + 4 * hh;
-    if (c < a.dh) *reinterpret_cast<float4*>(p + c) = make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
-  }
-}
-
 // Forward.  A lane holds one row of q and half of that row's scores, so the running maximum and sum are scalars of the lane; the scores
 // leave the first product in the places from which the second takes them.  Keys and values come through a ring of stages.
 // The maximum that the exponents are taken from moves only when a row's has grown by more than a factor of 2^8 (probabilities
@@ -351,10 +341,11 @@ __global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma
     if (b.rows_left <= 0 || col >= G::MB) return;          // (a block of 32 channels each)
     if (a.shares > 1) {
       const long r = n * a.heads + b.me.h;
-      if ((lane & 31) < b.rows_left) store_share(a, a.part, b.share, r, acc[0], col, hh);
+      const long p = (long)b.share * a.q_rows * a.heads + r;
+      if ((lane & 31) < b.rows_left) store_share<1>(a.part, p, acc, col, a.dh, hh);
       if (stat && col == 0) {
-        a.part_stats[((long)b.share * a.q_rows * a.heads + r) * 2] = top;
-        a.part_stats[((long)b.share * a.q_rows * a.heads + r) * 2 + 1] = sum;
+        a.part_stats[2 * p] = top;
+        a.part_stats[2 * p + 1] = sum;
       }
       return;
     }
@@ -363,38 +354,6 @@ __global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma
     if (stat && col == 0) a.lse[n * a.heads + b.me.h] = sum == 0.f ? -INFINITY : top + log2f(sum);
     redo_rows(not_finite(acc, g * 0.f), b.rows_left, redo);
   }
-}
-
-// The shares of one (query, head): a wavefront, two channels per lane.
-__global__ __launch_bounds__(256) void packed_join_fwd_kernel(PackedAttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long)a.q_rows * a.heads;
-  if (r >= rows) return;
-  const int n = (int)(r / a.heads), h = (int)(r - (long)n * a.heads);
-  const int sq = seq_with(a.q_off, a.q_rows, a.seqs, n);
-  if (sq < 0) return;
-  const Seq s = seq_of(a, sq);
-  if (n < s.q0 || n >= s.q0 + s.nq) return;
-  float top = -FLT_MAX, sum = 0.f, v[2] = {0.f, 0.f};
-  for (int i = lane; i < a.shares; i += 64) top = fmaxf(top, a.part_stats[(i * rows + r) * 2]);
-  top = wave_max(top);
-  const int c = 2 * lane;
-  for (int i = 0; i < a.shares; ++i) {
-    const float f = fast_exp2(a.part_stats[(i * rows + r) * 2] - top);
-    sum = fmaf(f, a.part_stats[(i * rows + r) * 2 + 1], sum);
-    if (c < a.dh) {
-      const float2 x = *reinterpret_cast<const float2*>(a.part + (i * rows + r) * a.dh + c);
-      v[0] = fmaf(f, x.x, v[0]);
-      v[1] = fmaf(f, x.y, v[1]);
-    }
-  }
-  const float g = sum == 0.f ? 0.f : 1.f / sum;
-  if (__any(!(fabsf(v[0] * g) < INFINITY && fabsf(v[1] * g) < INFINITY))) {      // (see redo_rows)
-    one_forward<bf16_t>(a, s, n - s.q0, h, lane);
-    return;
-  }
-  if (c < a.dh) *reinterpret_cast<unsigned*>(row_out<bf16_t>(a.o, n, h) + c) = pack_bf16x2(v[0] * g, v[1] * g);
-  if (lane == 0) a.lse[r] = sum == 0.f ? -INFINITY : top + log2f(sum);
 }
 
 // dq, and for the other kernel minus D = sum_c dout (.) o and minus lse of every row.  As the forward pass: a lane holds a row of q and
@@ -414,7 +373,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
   const int dh8 = a.dh >> 3;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const KS ks(a, sq, b.x.hk, lds0, dh8, wave, lane);
-  for (int i = 0; i < NST - 1 && i < b.to; ++i) ks.issue(i, i, wave, lane);
+  for (int i = 0; i < NST - 1 && b.from + i < b.to; ++i) ks.issue(b.from + i, i, wave, lane);
   const long n = sq.q0 + b.me.i;
   const bf16_t* qrow = row_of<bf16_t>(a.q, n, b.me.h);
   const bf16_t* grow = row_of<bf16_t>(a.dout, n, b.me.h);
@@ -432,7 +391,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
   D += other_half(D);
   float L = stat_of(a.lse[n * a.heads + b.me.h]);
   landed(L);
-  if (col == 0 && lane < 32 && lane < b.rows_left) {
+  if (col == 0 && b.share == 0 && lane < 32 && lane < b.rows_left) {
     a.dsum[n * a.heads + b.me.h] = -D;
     a.nlse[n * a.heads + b.me.h] = -L;
   }
@@ -468,7 +427,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
     }
   };
   int at = 0;
-  for (int i = 0; i < b.to; ++i) {
+  for (int i = b.from; i < b.to; ++i) {
     if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
     else copies_in_flight<0>();
     workgroup_handover();
@@ -501,6 +460,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
     if (col < G::MB) get_sums<G::MB, COLS>(sums, rw, col, f, acc, lane);
     __syncthreads();
     if (b.rows_left <= 0 || col >= G::MB) return;
+    if (a.shares > 1) {
+      if ((lane & 31) < b.rows_left)
+        store_share<1>(a.part, (long)b.share * a.q_rows * a.heads + n * a.heads + b.me.h, acc, col, a.dh, hh);
+      return;
+    }
     store_rows(row, b.rows_left, acc, a.scale, col, a.dh, ring + wave * 2048, lane);
     redo_rows(not_finite(acc, 0.f), b.rows_left, redo);
   }
@@ -519,12 +483,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   constexpr bool KLDS = DHP == 128;
   constexpr int NST = DHP == 128 && TURNS == 4 ? 2 : 3;
   constexpr int KW = WAVES / TURNS, KEYS = 32 * KW;
-  constexpr int STAGE = 2 * TURNS * G::TB;                 // TURNS tiles of q, as many of dout
-  constexpr int PW = 2 * TURNS * G::COPIES / WAVES;        // copies of a stage by one wavefront
+  constexpr int QT = DHP == 64 && TURNS == 2 ? 2 : 1;      // tiles of a wavefront in a step
+  constexpr int NT = TURNS * QT;                           // tiles of a step
+  constexpr int STAGE = 2 * NT * G::TB;                    // NT tiles of q, as many of dout
+  constexpr int PW = 2 * NT * G::COPIES / WAVES;           // copies of a stage by one wavefront
   constexpr int SUMS = KW * (TURNS - 1) * G::MB * 16 * 64 * 4;     // the sums of all but the first, dk or dv
   constexpr int RING = NST * STAGE + (KLDS ? KW * G::TB : 0);
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RING > SUMS ? RING : SUMS];
-  __shared__ __attribute__((aligned(256))) float stats[NST][TURNS][2][64];       // [stage][tile][-lse | -D][32 rows, and again]
+  __shared__ __attribute__((aligned(256))) float stats[NST][NT][2][64];          // [stage][tile][-lse | -D][32 rows, and again]
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), turn = wave / KW, kw = wave % KW;
   const Tile x = find_tile<true>(a, KEYS, lane);
@@ -540,14 +506,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   };
   const int top = (nq - 1) >> 5;                           // last tile of queries
   const int tiles = nq > 0 ? (top + 1 - (first_query(k0) >> 5)) * a.group : 0;     // times heads
-  const int steps = (tiles + TURNS - 1) / TURNS;
+  const int all_steps = (tiles + NT - 1) / NT, share = (int)blockIdx.y;
+  const int from = (int)((long)all_steps * share / a.shares), to = (int)((long)all_steps * (share + 1) / a.shares);
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const unsigned lds1 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(stats));
   // this wavefront's copies: PW parts of one of the stage's tiles, and a statistic of another
   static_assert(G::COPIES % PW == 0, "a wavefront's copies are of one tile");
-  const int ct = wave * PW / G::COPIES, cp = wave * PW % G::COPIES, st = (wave >> 1) % TURNS;
-  const HeadRows& from = ct < TURNS ? a.q : a.dout;
-  const unsigned ld = (unsigned)(from.row * 2);
+  const int ct = wave * PW / G::COPIES, cp = wave * PW % G::COPIES, st = (wave >> 1) % NT;
+  const HeadRows& src = ct < NT ? a.q : a.dout;
+  const unsigned ld = (unsigned)(src.row * 2);
   unsigned off[PW];
 #pragma unroll
   for (int u = 0; u < PW; ++u) off[u] = copy_offset<DHP>(ld, cp + u, 32, dh8, lane);
@@ -558,13 +525,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
       for (h += n; h >= group; h -= group) --q;
     }
   };
-  Place pc{0, top}, pt{0, top};
-  pc.on(ct % TURNS, a.group);
+  const Place begin_at{from * NT % a.group, top - from * NT / a.group};
+  Place pc = begin_at, pt = begin_at;
+  pc.on(ct % NT, a.group);
   pt.on(st, a.group);
   auto ask = [&](int at) __attribute__((always_inline)) {
     {
       const int first = pc.q < 0 ? 0 : 32 * pc.q, left = nq - first;               // (past the last: a tile that nobody reads)
-      const unsigned char* base = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(from, x.s.q0 + first, x.hk * a.group + pc.h));
+      const unsigned char* base = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(src, x.s.q0 + first, x.hk * a.group + pc.h));
       const unsigned dst = lds0 + (unsigned)at * STAGE + (unsigned)(wave * PW) * 1024u;
       if (left >= 32) {
 #pragma unroll
@@ -577,16 +545,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
     // (every wavefront copies a statistic: the waits count the same for all)
     const int first = pt.q < 0 ? 0 : 32 * pt.q, r = first + (lane & 31) < nq ? first + (lane & 31) : nq - 1;
     copy4_to_lds((wave & 1 ? a.dsum : a.nlse) + (long)(x.s.q0 + r) * a.heads + x.hk * a.group + pt.h,
-                 lds1 + (unsigned)at * (TURNS * 512u) + (unsigned)(2 * st + (wave & 1)) * 256u);
-    pc.on(TURNS, a.group);
-    pt.on(TURNS, a.group);
+                 lds1 + (unsigned)at * (NT * 512u) + (unsigned)(2 * st + (wave & 1)) * 256u);
+    pc.on(NT, a.group);
+    pt.on(NT, a.group);
   };
-  for (int i = 0; i < NST - 1 && i < steps; ++i) ask(i);
+  for (int i = 0; i < NST - 1 && from + i < to; ++i) ask(i);
   const int key = keys_left > 0 ? w0 + ((lane & 31) < keys_left ? (lane & 31) : keys_left - 1) : x.s.nk - 1;
   const bf16_t* krow = row_of<bf16_t>(a.k, x.s.k0 + key, x.hk);
   const bf16_t* vrow = row_of<bf16_t>(a.v, x.s.k0 + key, x.hk);
-  const unsigned cl = Frags<DHP>::cols_lane(lane), cq = lds0 + cl + (unsigned)turn * G::TB;
-  const unsigned rq = lds0 + Frags<DHP>::rows_lane(lane) + (unsigned)turn * G::TB;
+  const unsigned cl = Frags<DHP>::cols_lane(lane), cq = lds0 + cl + (unsigned)(turn * QT) * G::TB;
+  const unsigned rq = lds0 + Frags<DHP>::rows_lane(lane) + (unsigned)(turn * QT) * G::TB;
   const unsigned kl = lds0 + NST * STAGE + (unsigned)kw * G::TB + cl;
   bf16x8 fk[G::KK], fv[G::KK];
 #pragma unroll
@@ -605,55 +573,82 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   float16v dk[G::MB], dv[G::MB];
   zero_acc(dk);
   zero_acc(dv);
-  auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
+  // the wavefront's tiles of the stage: their first queries
+  auto step = [&](const int (&first)[QT], int at, bool masked) __attribute__((always_inline)) {
     const unsigned tc = cq + (unsigned)at * STAGE, tr = rq + (unsigned)at * STAGE;
-    float16v s[1], dp;
-    float p[16];
+    float16v s[QT], dp[QT];
+    float p[QT][16];
     zero_acc(s);
 #pragma unroll
-    for (int kk = 0; kk < G::KK; ++kk) s[0] = mfma(Frags<DHP>::cols(tc, 0, kk), KLDS ? Frags<DHP>::cols(kl, 0, kk) : fk[kk], s[0]);
+    for (int b = 0; b < QT; ++b)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn][1][8 * g + 4 * hh]);
-      dp[4 * g] = u.x; dp[4 * g + 1] = u.y; dp[4 * g + 2] = u.z; dp[4 * g + 3] = u.w;
+      for (int kk = 0; kk < G::KK; ++kk)
+        s[b] = mfma(Frags<DHP>::cols(tc, b * G::TB, kk), KLDS ? Frags<DHP>::cols(kl, 0, kk) : fk[kk], s[b]);
+#pragma unroll
+    for (int b = 0; b < QT; ++b) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn * QT + b][1][8 * g + 4 * hh]);
+        dp[b][4 * g] = u.x; dp[b][4 * g + 1] = u.y; dp[b][4 * g + 2] = u.z; dp[b][4 * g + 3] = u.w;
+      }
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) dp[b] = mfma(Frags<DHP>::cols(tc, (NT + b) * G::TB, kk), fv[kk], dp[b]);
     }
 #pragma unroll
-    for (int kk = 0; kk < G::KK; ++kk) dp = mfma(Frags<DHP>::cols(tc, TURNS * G::TB, kk), fv[kk], dp);
+    for (int b = 0; b < QT; ++b) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn][0][8 * g + 4 * hh]);
-      p[4 * g] = fast_exp2(fmaf(s[0][4 * g], c, u.x));
-      p[4 * g + 1] = fast_exp2(fmaf(s[0][4 * g + 1], c, u.y));
-      p[4 * g + 2] = fast_exp2(fmaf(s[0][4 * g + 2], c, u.z));
-      p[4 * g + 3] = fast_exp2(fmaf(s[0][4 * g + 3], c, u.w));
+      for (int g = 0; g < 4; ++g) {
+        const float4 u = *reinterpret_cast<const float4*>(&stats[at][turn * QT + b][0][8 * g + 4 * hh]);
+        p[b][4 * g] = fast_exp2(fmaf(s[b][4 * g], c, u.x));
+        p[b][4 * g + 1] = fast_exp2(fmaf(s[b][4 * g + 1], c, u.y));
+        p[b][4 * g + 2] = fast_exp2(fmaf(s[b][4 * g + 2], c, u.z));
+        p[b][4 * g + 3] = fast_exp2(fmaf(s[b][4 * g + 3], c, u.w));
+      }
     }
     if (masked) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int i = first + tile_row_of(e, hh);
-        if (i < mine || i >= nq) p[e] = 0.f;
-      }
-    }
-    Operand op;
-    op.set(p, few);
-    op.template times<DHP>(tr, TURNS * G::TB, dv, few);
+      for (int b = 0; b < QT; ++b)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) p[e] *= dp[e];
-    op.set(p, few);
-    op.template times<DHP>(tr, 0, dk, few);
+        for (int e = 0; e < 16; ++e) {
+          const int i = first[b] + tile_row_of(e, hh);
+          if (i < mine || i >= nq) p[b][e] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < QT; ++b) {
+      Operand op;
+      op.set(p[b], few);
+      op.template times<DHP>(tr, (NT + b) * G::TB, dv, few);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[b][e] *= dp[b][e];
+      op.set(p[b], few);
+      op.template times<DHP>(tr, b * G::TB, dk, few);
+    }
   };
   int at = 0;
-  Place me{0, top};                                        // this wavefront's next tile
-  me.on(turn, a.group);
-  for (int i = 0; i < steps; ++i) {
-    if (i + NST - 2 < steps) copies_in_flight<(PW + 1) * (NST - 2)>();
+  Place me[QT];                                            // this wavefront's next tiles
+#pragma unroll
+  for (int b = 0; b < QT; ++b) {
+    me[b] = begin_at;
+    me[b].on(turn * QT + b, a.group);
+  }
+  for (int i = from; i < to; ++i) {
+    if (i + NST - 2 < to) copies_in_flight<(PW + 1) * (NST - 2)>();
     else copies_in_flight<0>();
     workgroup_handover();
-    if (i + NST - 1 < steps) ask(at == 0 ? NST - 1 : at - 1);
-    const int first = 32 * me.q;
-    if (TURNS * i + turn < tiles && first + 32 > begin && keys_left > 0) step(first, at, first < all || first + 32 > nq);
+    if (i + NST - 1 < to) ask(at == 0 ? NST - 1 : at - 1);
+    int first[QT];
+    bool some = false, masked = false;
+#pragma unroll
+    for (int b = 0; b < QT; ++b) {
+      const bool there = NT * i + turn * QT + b < tiles;
+      first[b] = there ? 32 * me[b].q : nq;                // (a tile past the list: masked throughout)
+      some = some || (there && first[b] + 32 > begin);
+      masked = masked || first[b] < all || first[b] + 32 > nq;
+      me[b].on(NT, a.group);
+    }
+    if (some && keys_left > 0) step(first, at, masked);
     at = at == NST - 1 ? 0 : at + 1;
-    me.on(TURNS, a.group);
   }
   auto meet = [&](float16v (&acc)[G::MB]) __attribute__((always_inline)) {
     float* const sums = reinterpret_cast<float*>(ring) + kw * (G::MB * 16 * 64) + lane;
@@ -678,6 +673,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   meet(dv);
   __syncthreads();
   if (turn > 0 || keys_left <= 0) return;
+  if (a.shares > 1) {
+    const long r = (long)(x.s.k0 + key) * a.kv_heads + x.hk, rows = (long)a.k_rows * a.kv_heads;
+    if ((lane & 31) < keys_left) {
+      store_share<G::MB>(a.part, share * rows + r, dk, 0, a.dh, hh);
+      store_share<G::MB>(a.part, (a.shares + share) * rows + r, dv, 0, a.dh, hh);
+    }
+    return;
+  }
   unsigned char* stg = ring + wave * 2048;
   store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, x.s.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale, 0,
              a.dh, stg, lane);
@@ -687,65 +690,112 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
 }
 
 // 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64 (64 keys).
-constexpr unsigned CUS = 256;
 template <int DHP>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  const unsigned wide = tile_grid<false>(a, 256), narrow = tile_grid<false>(a, 64);
-  if (wide == 0) return hipSuccess;
-  if (a.shares == 1 && wide >= CUS) {
-    packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
-    return hipGetLastError();
-  }
-  packed_fwd_mfma_kernel<DHP, 4><<<dim3(narrow, a.shares), 64 * WAVES, 0, s>>>(a);
-  if (a.shares > 1) packed_join_fwd_kernel<<<(unsigned)(((long)a.q_rows * a.heads + 3) / 4), 256, 0, s>>>(a);
+  const unsigned wide = tile_grid<false>(a, 256);
+  if (a.shares == 1 && wide >= CUS) packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+  else packed_fwd_mfma_kernel<DHP, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int DHP>
-hipError_t bwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  const unsigned rows = tile_grid<false>(a, 256), keys = tile_grid<true>(a, 128);
-  if (rows >= CUS) packed_dq_mfma_kernel<DHP, 1><<<rows, 64 * WAVES, 0, s>>>(a);
-  else if (rows > 0) packed_dq_mfma_kernel<DHP, 4><<<tile_grid<false>(a, 64), 64 * WAVES, 0, s>>>(a);
-  if (keys >= CUS) packed_dkdv_mfma_kernel<DHP, 2><<<keys, 64 * WAVES, 0, s>>>(a);
-  else if (keys > 0) packed_dkdv_mfma_kernel<DHP, 4><<<tile_grid<true>(a, 64), 64 * WAVES, 0, s>>>(a);
+hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
+  const unsigned wide = tile_grid<false>(a, 256);
+  if (a.shares == 1 && wide >= CUS) packed_dq_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+  else packed_dq_mfma_kernel<DHP, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int DHP>
+hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
+  const unsigned wide = tile_grid<true>(a, 128);
+  if (a.shares == 1 && wide >= CUS) packed_dkdv_mfma_kernel<DHP, 2><<<wide, 64 * WAVES, 0, s>>>(a);
+  else packed_dkdv_mfma_kernel<DHP, 4><<<dim3(tile_grid<true>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 
-// Shares of the keys for the forward pass, where there are few rows: enough for two workgroups on every compute unit, each with four
-// steps of 128 keys at least.
-int fwd_shares(int dtype, const PackedAttnArgs& a) {
-  if (dtype == 0 || a.q_rows == 0) return 1;
-  const long groups = tile_grid<false>(a, 64);
+// Few rows (keys) leave compute units without a workgroup: the other side's steps are then shared out as well, for two workgroups on
+// every compute unit, but no fewer than four steps each.  Shares are fp32 sums that another kernel joins in a fixed order.
+int shares_of(long groups, long steps) {
   long n = 2 * CUS / groups;
-  const long most = a.k_rows / a.seqs / 512;
-  if (n > most) n = most;
+  if (n > steps / 4) n = steps / 4;
   return n < 2 ? 1 : (int)n;
 }
+struct Shares { int rows, keys; };       // of the keys for a tile of rows (forward, dq), of the queries for a tile of keys (dk, dv)
+Shares shares(int dtype, const PackedAttnArgs& a) {
+  const long nq = a.q_rows / a.seqs, nk = a.k_rows / a.seqs;           // (of a sequence, on average)
+  const long rows = dtype == 0 ? F32_ROWS : 64, keys = dtype == 0 ? F32_ROWS : 64;
+  const long key_step = dtype == 0 ? 32 : 128, query_step = dtype == 0 ? 32 : 128;
+  // (workgroups as with offsets, also without: the workspace is sized before a call says which)
+  return {shares_of(((long)a.q_rows * a.group / rows + a.seqs) * a.kv_heads, nk / key_step),
+          shares_of(((long)a.k_rows / keys + a.seqs) * a.kv_heads, nq * a.group / query_step)};
+}
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
-size_t row_floats(const PackedAttnArgs& a) { return aligned((size_t)a.q_rows * a.heads * 4); }
+
+// The workspace: minus D and minus lse of the rows (backward), the shares' maxima and sums (forward), the shares.
+struct Layout { size_t stats, shares, total; };
+Layout layout(const PackedAttnArgs& a, const Shares& n) {
+  const size_t rows = (size_t)a.q_rows * a.heads, keys = (size_t)a.k_rows * a.kv_heads;
+  Layout l{};
+  l.stats = aligned(rows * 4);
+  const size_t stats = 2 * l.stats > aligned(n.rows * rows * 8) || n.rows == 1 ? 2 * l.stats : aligned(n.rows * rows * 8);
+  l.shares = stats;
+  const size_t r = n.rows > 1 ? n.rows * rows * a.dh * 4 : 0, k = n.keys > 1 ? 2 * n.keys * keys * a.dh * 4 : 0;
+  l.total = stats + aligned(r > k ? r : k);
+  return l;
+}
 
 }  // namespace
 
-size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a) {
-  const size_t shares = fwd_shares(dtype, a), rows = (size_t)a.q_rows * a.heads;
-  const size_t fwd = shares > 1 ? aligned(shares * rows * a.dh * 4) + aligned(shares * rows * 8) : 0, bwd = 2 * row_floats(a);
-  return fwd > bwd ? fwd : bwd;
+size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared) {
+  const Shares n = shares(dtype, a);
+  if (shared) *shared = n.rows > 1 || n.keys > 1;
+  return layout(a, n).total;
 }
-hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s) {
-  if (dtype == 0) return launch_packed_attn_fwd_f32(a, s);
-  PackedAttnArgs b = a;
-  b.shares = fwd_shares(dtype, a);
-  if (b.shares > 1) {
-    b.part = reinterpret_cast<float*>(workspace);
-    b.part_stats = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + aligned((size_t)b.shares * a.q_rows * a.heads * a.dh * 4));
+
+hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* workspace, hipStream_t s) {
+  PackedAttnArgs a = args;
+  if (a.q_rows == 0) return hipSuccess;
+  const Shares n = shares(dtype, a);
+  const Layout l = layout(a, n);
+  a.shares = n.rows;
+  a.part_stats = reinterpret_cast<float*>(workspace);
+  a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.shares);
+  const hipError_t e = dtype == 0 ? launch_packed_fwd_f32(a, s) : a.dh <= 64 ? fwd_mfma<64>(a, s) : fwd_mfma<128>(a, s);
+  if (e != hipSuccess || a.shares == 1) return e;
+  const unsigned grid = (unsigned)(((long)a.q_rows * a.heads + 3) / 4);
+  if (dtype == 0) packed_join_fwd_kernel<float><<<grid, 256, 0, s>>>(a);
+  else packed_join_fwd_kernel<bf16_t><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& args, void* workspace, hipStream_t s) {
+  PackedAttnArgs a = args;
+  const Shares n = shares(dtype, a);
+  const Layout l = layout(a, n);
+  a.dsum = reinterpret_cast<float*>(workspace);
+  a.nlse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.stats);
+  a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.shares);
+  hipError_t e = hipSuccess;
+  if (a.q_rows > 0) {
+    a.shares = n.rows;
+    e = dtype == 0 ? launch_packed_dq_f32(a, s) : a.dh <= 64 ? dq_mfma<64>(a, s) : dq_mfma<128>(a, s);
+    if (e != hipSuccess) return e;
+    if (a.shares > 1) {
+      const unsigned grid = (unsigned)(((long)a.q_rows * a.heads + 3) / 4);
+      if (dtype == 0) packed_join_dq_kernel<float><<<grid, 256, 0, s>>>(a);
+      else packed_join_dq_kernel<bf16_t><<<grid, 256, 0, s>>>(a);
+    }
   }
-  return a.dh <= 64 ? fwd_mfma<64>(b, s) : fwd_mfma<128>(b, s);
-}
-hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s) {
-  PackedAttnArgs b = a;
-  b.shares = 1;
-  b.dsum = reinterpret_cast<float*>(workspace);
-  b.nlse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + row_floats(a));
-  return dtype == 0 ? launch_packed_attn_bwd_f32(b, s) : a.dh <= 64 ? bwd_mfma<64>(b, s) : bwd_mfma<128>(b, s);
+  if (a.k_rows > 0) {
+    a.shares = n.keys;
+    e = dtype == 0 ? launch_packed_dkdv_f32(a, s) : a.dh <= 64 ? dkdv_mfma<64>(a, s) : dkdv_mfma<128>(a, s);
+    if (e != hipSuccess) return e;
+    if (a.shares > 1) {
+      const unsigned grid = (unsigned)(((long)a.k_rows * a.kv_heads + 3) / 4);
+      if (dtype == 0) packed_join_dkdv_kernel<float><<<grid, 256, 0, s>>>(a);
+      else packed_join_dkdv_kernel<bf16_t><<<grid, 256, 0, s>>>(a);
+    }
+  }
+  return hipGetLastError();
 }
 
 }  // namespace hbp

@@ -11,7 +11,8 @@ namespace hbp {
 
 namespace {
 
-constexpr int WAVES = 4, ROWS = 32 * WAVES;
+constexpr int WAVES = 4, ROWS = F32_ROWS;
+static_assert(ROWS == 32 * WAVES, "a wavefront has 32 rows");
 
 __device__ __forceinline__ float16v mfma_f32(float x, float y, float16v acc) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, acc, 0, 0, 0);
@@ -118,7 +119,7 @@ __device__ __forceinline__ void store_row(float* row, const float16v (&acc)[MB],
 // The rows of a workgroup and what its wavefronts see of the keys.
 struct RowBlock {
   Tile x;
-  int w0, rows_left, mine, fewest, most, steps;
+  int w0, rows_left, mine, fewest, most, from, to, share;  // from .. to - 1: this workgroup's share of the steps
   RowPlace me;
   __device__ __forceinline__ bool find(const PackedAttnArgs& a, int wave, int lane) {
     x = find_tile<false>(a, ROWS, lane);
@@ -128,7 +129,10 @@ struct RowBlock {
     w0 = r0 + 32 * wave;
     rows_left = R - w0;
     auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
-    steps = (seen((R < r0 + ROWS ? R : r0 + ROWS) - 1) + 31) >> 5;
+    const int steps = (seen((R < r0 + ROWS ? R : r0 + ROWS) - 1) + 31) >> 5;
+    share = (int)blockIdx.y;
+    from = (int)((long)steps * share / a.shares);
+    to = (int)((long)steps * (share + 1) / a.shares);
     const int r = rows_left > 0 ? w0 + ((lane & 31) < rows_left ? (lane & 31) : rows_left - 1) : R - 1;
     me = place_of(a, x.hk, r);
     mine = seen_by(x.s, me.i, a.causal);
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAtt
   const PairStream<W> ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave, lane);
   const float* k = row_of<float>(a.k, s.k0, b.x.hk);
   const float* v = row_of<float>(a.v, s.k0, b.x.hk);
-  if (b.steps > 0) ps.issue(k, v, 0, s.nk, 0, lane);
+  if (b.from < b.to) ps.issue(k, v, 32 * b.from, s.nk, b.from & 1, lane);
   float q[4 * T::J];
   T::own(row_of<float>(a.q, s.q0 + b.me.i, b.me.h), a.dh, lane, q);
   const unsigned ck = lds0 + T::cols_lane(lane), rv = lds0 + T::rows_lane(lane);
@@ -159,10 +163,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAtt
   float16v o[T::MB];
   zero_acc(o);
   float m = -FLT_MAX, l = 0.f;
-  for (int i = 0; i < b.steps; ++i) {
+  for (int i = b.from; i < b.to; ++i) {
     copies_in_flight<0>();
     workgroup_handover();
-    if (i + 1 < b.steps) ps.issue(k, v, 32 * (i + 1), s.nk, (i + 1) & 1, lane);
+    if (i + 1 < b.to) ps.issue(k, v, 32 * (i + 1), s.nk, (i + 1) & 1, lane);
     if (32 * i >= b.most) continue;
     const unsigned at = (unsigned)(i & 1) * T::STAGE;
     float16v sc[1];
@@ -197,6 +201,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAtt
   l += other_half(l);
   const float f = l == 0.f ? 0.f : 1.f / l;
   const long n = s.q0 + b.me.i;
+  if (a.shares > 1) {
+    const long p = (long)b.share * a.q_rows * a.heads + n * a.heads + b.me.h;
+    if ((lane & 31) < b.rows_left) {
+      store_share<T::MB>(a.part, p, o, 0, a.dh, hh);
+      if (hh == 0) {
+        a.part_stats[2 * p] = m;
+        a.part_stats[2 * p + 1] = l;
+      }
+    }
+    return;
+  }
   if ((lane & 31) < b.rows_left) {
     store_row(row_out<float>(a.o, n, b.me.h), o, f, a.dh, hh);
     if (hh == 0) a.lse[n * a.heads + b.me.h] = l == 0.f ? -INFINITY : m + log2f(l);
@@ -220,7 +235,7 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dq_f32_ke
   const PairStream<W> ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave, lane);
   const float* k = row_of<float>(a.k, s.k0, b.x.hk);
   const float* v = row_of<float>(a.v, s.k0, b.x.hk);
-  if (b.steps > 0) ps.issue(k, v, 0, s.nk, 0, lane);
+  if (b.from < b.to) ps.issue(k, v, 32 * b.from, s.nk, b.from & 1, lane);
   const long n = s.q0 + b.me.i;
   float q[4 * T::J], g[4 * T::J], D = 0.f;
   {
@@ -234,7 +249,7 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dq_f32_ke
   D += other_half(D);
   float L = stat_of(a.lse[n * a.heads + b.me.h]);
   landed(L);
-  if (hh == 0 && lane < b.rows_left) {
+  if (hh == 0 && b.share == 0 && lane < b.rows_left) {
     a.dsum[n * a.heads + b.me.h] = -D;
     a.nlse[n * a.heads + b.me.h] = -L;
   }
@@ -242,10 +257,10 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dq_f32_ke
   const float c = a.scale * LOG2E;
   float16v dq[T::MB];
   zero_acc(dq);
-  for (int i = 0; i < b.steps; ++i) {
+  for (int i = b.from; i < b.to; ++i) {
     copies_in_flight<0>();
     workgroup_handover();
-    if (i + 1 < b.steps) ps.issue(k, v, 32 * (i + 1), s.nk, (i + 1) & 1, lane);
+    if (i + 1 < b.to) ps.issue(k, v, 32 * (i + 1), s.nk, (i + 1) & 1, lane);
     if (32 * i >= b.most) continue;
     const unsigned at = (unsigned)(i & 1) * T::STAGE;
     float16v sc[1], dp;
@@ -264,6 +279,11 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dq_f32_ke
     T::add(rk + at, 0, sc[0], dq);
   }
   if (b.rows_left <= 0) return;
+  if (a.shares > 1) {
+    if ((lane & 31) < b.rows_left)
+      store_share<T::MB>(a.part, (long)b.share * a.q_rows * a.heads + n * a.heads + b.me.h, dq, 0, a.dh, hh);
+    return;
+  }
   if ((lane & 31) < b.rows_left) store_row(row_out<float>(a.dq, n, b.me.h), dq, a.scale, a.dh, hh);
   redo_rows(not_finite(dq, 0.f), b.rows_left, [&](int j) {
     const RowPlace p = place_of(a, b.x.hk, b.w0 + j);
@@ -289,11 +309,12 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
     return !a.causal || i < 0 ? 0 : i;
   };
   const int top = (nq - 1) >> 5;
-  const int steps = nq > 0 ? (top + 1 - (first_query(k0) >> 5)) * a.group : 0;
+  const int steps = nq > 0 ? (top + 1 - (first_query(k0) >> 5)) * a.group : 0, share = (int)blockIdx.y;
+  const int from = (int)((long)steps * share / a.shares), to = (int)((long)steps * (share + 1) / a.shares);
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const unsigned lds1 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(stats));
   const PairStream<W> ps((unsigned)(a.q.row * 4), (unsigned)(a.dout.row * 4), a.dh, lds0, wave, lane);
-  int ih = 0, iq = top;                                    // the next tile to ask for
+  int ih = from % a.group, iq = top - from / a.group;      // the next tile to ask for
   auto ask = [&](int at) __attribute__((always_inline)) {
     const int h = x.hk * a.group + ih, first = 32 * iq;
     ps.issue(row_of<float>(a.q, s.q0, h), row_of<float>(a.dout, s.q0, h), first, nq, at, lane);
@@ -301,7 +322,6 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
     copy4_to_lds((wave & 1 ? a.dsum : a.nlse) + (long)(s.q0 + r) * a.heads + h, lds1 + (unsigned)at * 512u + (unsigned)(wave & 1) * 256u);
     if (++ih == a.group) { ih = 0; --iq; }
   };
-  if (steps > 0) ask(0);
   const int key = keys_left > 0 ? w0 + ((lane & 31) < keys_left ? (lane & 31) : keys_left - 1) : s.nk - 1;
   float k[4 * T::J], v[4 * T::J];
   T::own(row_of<float>(a.k, s.k0 + key, x.hk), a.dh, lane, k);
@@ -313,11 +333,12 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
   float16v dk[T::MB], dv[T::MB];
   zero_acc(dk);
   zero_acc(dv);
-  int sh = 0, first = 32 * top;
-  for (int i = 0; i < steps; ++i) {
+  int sh = ih, first = 32 * iq;
+  if (from < to) ask(from & 1);
+  for (int i = from; i < to; ++i) {
     copies_in_flight<0>();
     workgroup_handover();
-    if (i + 1 < steps) ask((i + 1) & 1);
+    if (i + 1 < to) ask((i + 1) & 1);
     if (first + 32 > begin && keys_left > 0) {
       const unsigned at = (unsigned)(i & 1) * T::STAGE;
       float16v sc[1], dp;
@@ -352,6 +373,14 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
     if (++sh == a.group) { sh = 0; first -= 32; }
   }
   if (keys_left <= 0) return;
+  if (a.shares > 1) {
+    const long r = (long)(s.k0 + key) * a.kv_heads + x.hk, rows = (long)a.k_rows * a.kv_heads;
+    if ((lane & 31) < keys_left) {
+      store_share<T::MB>(a.part, share * rows + r, dk, 0, a.dh, hh);
+      store_share<T::MB>(a.part, (a.shares + share) * rows + r, dv, 0, a.dh, hh);
+    }
+    return;
+  }
   if ((lane & 31) < keys_left) {
     store_row(row_out<float>(a.dk, s.k0 + key, x.hk), dk, a.scale, a.dh, hh);
     store_row(row_out<float>(a.dv, s.k0 + key, x.hk), dv, 1.f, a.dh, hh);
@@ -359,21 +388,25 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
   redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<float>(a, s, w0 + j, x.hk, lane); });
 }
 
-template <int W>
-hipError_t fwd(const PackedAttnArgs& a, hipStream_t s) {
-  if (const unsigned grid = tile_grid<false>(a, ROWS)) packed_fwd_f32_kernel<W><<<grid, 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
-}
-template <int W>
-hipError_t bwd(const PackedAttnArgs& a, hipStream_t s) {
-  if (const unsigned grid = tile_grid<false>(a, ROWS)) packed_dq_f32_kernel<W><<<grid, 64 * WAVES, 0, s>>>(a);
-  if (const unsigned grid = tile_grid<true>(a, ROWS)) packed_dkdv_f32_kernel<W><<<grid, 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
-}
-
 }  // namespace
 
-hipError_t launch_packed_attn_fwd_f32(const PackedAttnArgs& a, hipStream_t s) { return a.dh <= 64 ? fwd<64>(a, s) : fwd<128>(a, s); }
-hipError_t launch_packed_attn_bwd_f32(const PackedAttnArgs& a, hipStream_t s) { return a.dh <= 64 ? bwd<64>(a, s) : bwd<128>(a, s); }
+hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s) {
+  const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
+  if (a.dh <= 64) packed_fwd_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
+  else packed_fwd_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s) {
+  const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
+  if (a.dh <= 64) packed_dq_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
+  else packed_dq_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s) {
+  const dim3 grid(tile_grid<true>(a, ROWS), a.shares);
+  if (a.dh <= 64) packed_dkdv_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
+  else packed_dkdv_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
+  return hipGetLastError();
+}
 
 }  // namespace hbp

@@ -65,8 +65,16 @@ void rotary_turns(const hbp_rotary_desc* r, double* turns) {
   const double two_pi = 6.283185307179586476925286766559;
   double base = r->base;
   if (r->scaling == HBP_ROTARY_BASE) base *= pow(r->factor, (double)r->dims / (r->dims - 2));
-  for (int i = 0; i < r->dims / 2; ++i) {
-    double f = pow(base, -2.0 * i / r->dims) / two_pi;
+  // base^(-2 i / dims) from the powers for i = 1, 2, 4, ..: seven roundings at most, and seven calls of pow
+  const int pairs = r->dims / 2;
+  turns[0] = 1.0 / two_pi;
+  for (int p = 1; p < pairs; p *= 2) {
+    const double f = pow(base, -2.0 * p / r->dims);
+    for (int i = p; i < 2 * p && i < pairs; ++i) turns[i] = turns[i - p] * f;
+  }
+  if (r->scaling != HBP_ROTARY_LINEAR && r->scaling != HBP_ROTARY_BY_PARTS) return;
+  for (int i = 0; i < pairs; ++i) {
+    double f = turns[i];
     if (r->scaling == HBP_ROTARY_LINEAR) f /= r->factor;
     if (r->scaling == HBP_ROTARY_BY_PARTS) {
       double w = (r->original * f - r->low) / (r->high - r->low);
@@ -99,7 +107,16 @@ PackedAttnArgs packed_sizes(const hbp_desc* d, long layers) {
   a.scale = 1.0f / sqrtf((float)head_w(d));
   return a;
 }
-size_t packed_ws(const hbp_desc* d) { return packed_attn_ws_bytes(d->dtype, packed_sizes(d, d->L / 2)); }
+// What any number of layers at a time may need: few of them share work out further, which needs room that many do not.
+size_t packed_ws(const hbp_desc* d) {
+  size_t most = packed_attn_ws_bytes(d->dtype, packed_sizes(d, d->L / 2));
+  bool shared = true;
+  for (long n = 1; n < d->L / 2 && shared; ++n) {
+    const size_t need = packed_attn_ws_bytes(d->dtype, packed_sizes(d, n), &shared);
+    if (need > most) most = need;
+  }
+  return most;
+}
 
 struct Workspace {
   size_t off_v, off_da, off_part, off_scan, off_wt, off_pre, off_m, off_tmp, off_dqkv, off_dsum, off_packed, off_counter, total;

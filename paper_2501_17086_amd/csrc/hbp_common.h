@@ -243,17 +243,17 @@ struct PackedAttnArgs {
   float* lse;               // [q_rows, heads]
   float* dsum;              // [q_rows, heads], workspace: minus rowsum(dout (.) o)
   float* nlse;              // [q_rows, heads], workspace: minus lse; minus infinity where a row weighs nothing
-  // forward, set by the launcher: shares of the keys, and what they leave in the workspace
+  // set by the launcher: shares of the other side's steps (1: none), and what they leave in the workspace
   int shares;
-  float* part;              // [share][q_rows heads][dh]
-  float* part_stats;        // [share][q_rows heads][maximum | sum]
+  float* part;              // [share][q_rows heads][dh]; dk, dv: [dk | dv][share][k_rows kv_heads][dh]
+  float* part_stats;        // forward: [share][q_rows heads][maximum | sum]
   const int* q_off;         // [seqs + 1] or NULL: equal lengths
   const int* k_off;
   int seqs, q_rows, k_rows;
   int heads, kv_heads, group, dh, causal;
   float scale;
 };
-size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a);
+size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared = nullptr);     // shared: part of it are shares
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
 hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
 
