@@ -16,9 +16,9 @@ namespace {
 // One sequence: its first row and its length on either side.
 struct Seq { int q0, nq, k0, nk; };
 __device__ __forceinline__ int clamp_row(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
-__device__ __forceinline__ void span_of(const int* off, int rows, int seqs, int s, int& first, int& n) {
+__device__ __forceinline__ void span_of(const int* off, int rows, int len, int s, int& first, int& n) {
   if (!off) {
-    n = rows / seqs;
+    n = len;
     first = s * n;
     return;
   }
@@ -28,13 +28,13 @@ __device__ __forceinline__ void span_of(const int* off, int rows, int seqs, int 
 }
 __device__ __forceinline__ Seq seq_of(const PackedAttnArgs& a, int s) {
   Seq q;
-  span_of(a.q_off, a.q_rows, a.seqs, s, q.q0, q.nq);
-  span_of(a.k_off, a.k_rows, a.seqs, s, q.k0, q.nk);
+  span_of(a.q_off, a.q_rows, a.q_len, s, q.q0, q.nq);
+  span_of(a.k_off, a.k_rows, a.k_len, s, q.k0, q.nk);
   return q;
 }
 // the sequence that row n belongs to (offsets that do not decrease), -1: none
-__device__ __forceinline__ int seq_with(const int* off, int rows, int seqs, int n) {
-  if (!off) return n / (rows / seqs);
+__device__ __forceinline__ int seq_with(const int* off, int len, int seqs, int n) {
+  if (!off) return n / len;
   int lo = 0, hi = seqs;                                   // off[lo] <= n < off[hi], where there is such a sequence
   if (n < off[0] || n >= off[seqs]) return -1;
   while (hi - lo > 1) {
@@ -193,25 +193,25 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
 // other: all problems go on side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs
 // in turn, keep a problem's streamed tiles in one XCD's L2.
 struct Tile { int hk, t, n; Seq s; bool exists; };          // t of the sequence's n tiles
-__device__ __forceinline__ int tiles_in(int len, int per) { return (len + per - 1) / per; }
+__device__ __forceinline__ int tiles_in(int len, int per) { return (int)((unsigned)(len + per - 1) / (unsigned)per); }   // (per: a power of two)
 template <bool KEYS>
 __device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane) {
   Tile x;
   const unsigned id = blockIdx.x;
-  x.hk = (int)(id % (unsigned)a.kv_heads);
-  x.t = (int)(id / (unsigned)a.kv_heads);
+  x.t = (int)a.by_kv.quotient(id);
+  x.hk = (int)id - x.t * a.kv_heads;
   const int* off = KEYS ? a.k_off : a.q_off;
   const int mult = KEYS ? 1 : a.group, rows = KEYS ? a.k_rows : a.q_rows;
   int sq = -1;
   if (!off) {
-    x.n = tiles_in(rows / a.seqs * mult, per);
-    sq = x.t / x.n;
+    x.n = (int)a.by_tiles.d;
+    sq = (int)a.by_tiles.quotient((unsigned)x.t);
     x.t -= sq * x.n;
     if (sq >= a.seqs) sq = -1;
   } else {
     for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time: a running sum of their tiles over the lanes
       int first, n = 0;
-      if (s0 + lane < a.seqs) span_of(off, rows, a.seqs, s0 + lane, first, n);
+      if (s0 + lane < a.seqs) span_of(off, rows, 0, s0 + lane, first, n);
       n = tiles_in(n * mult, per);
       int sum = n;
 #pragma unroll
@@ -242,14 +242,18 @@ __device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int 
   }
   return x;
 }
-// the other half's value (lanes l and l + 32 hold one row's two halves)
+// the other half's value (lanes l and l + 32 hold one row's two halves), and the larger of the two
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+__device__ __forceinline__ float max_of_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 // The rows of a tile: row r of the sequence at this key head is query r / group of head hk group + r % group.
 struct RowPlace { int i, h; };
 __device__ __forceinline__ RowPlace place_of(const PackedAttnArgs& a, int hk, int r) {
   RowPlace p;
-  p.i = (int)((unsigned)r / (unsigned)a.group);
+  p.i = (int)a.by_group.quotient((unsigned)r);
   p.h = hk * a.group + (r - p.i * a.group);
   return p;
 }
@@ -275,19 +279,20 @@ __device__ __forceinline__ void redo_rows(float t, int rows_left, F f) {
   for (; rows != 0; rows &= rows - 1) f(__ffs((int)rows) - 1);
 }
 
-// workgroups for tiles of `per` rows (keys)
+// Workgroups for tiles of `per` rows (keys), of which there are some; their kernel is to be launched with these `a`.
 template <bool KEYS>
-unsigned tile_grid(const PackedAttnArgs& a, int per) {
+unsigned tile_grid(PackedAttnArgs& a, int per) {
   const long rows = KEYS ? a.k_rows : (long)a.q_rows * a.group;
-  if (rows == 0) return 0;
   const bool equal = KEYS ? !a.k_off : !a.q_off;
-  const long tiles = equal ? a.seqs * ((rows / a.seqs + per - 1) / per) : rows / per + a.seqs;
+  const long each = (rows / a.seqs + per - 1) / per, tiles = equal ? a.seqs * each : rows / per + a.seqs;
+  a.by_tiles = Divisor(equal ? (unsigned)each : 1u);
   return (unsigned)(tiles * a.kv_heads);
 }
 
 // ------------------------------------------------------------------------------------------------------------
 // shares: a workgroup that took part of the other side's steps leaves its sums in fp32, [share][row][dh]; a wavefront per row joins them
 // ------------------------------------------------------------------------------------------------------------
+constexpr int MOST_SHARES = 256;
 template <int MB>
 __device__ __forceinline__ void store_share(float* part, long row, const float16v (&acc)[MB], int m0, int dh, int hh) {
   float* p = part + row * dh;
@@ -302,15 +307,22 @@ __device__ __forceinline__ void store_share(float* part, long row, const float16
 __device__ __forceinline__ void store2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
 __device__ __forceinline__ void store2(bf16_t* p, float a, float b) { *reinterpret_cast<unsigned*>(p) = pack_bf16x2(a, b); }
 __device__ __forceinline__ bool all_finite(float a, float b) { return !__any(!(fabsf(a) < INFINITY && fabsf(b) < INFINITY)); }
-// channels 2 lane, 2 lane + 1 of `shares` shares of a row, `stride` floats apart
-__device__ __forceinline__ float2 sum_shares(const float* p, long stride, int shares, int dh, int lane) {
+// channels 2 lane, 2 lane + 1 of `shares` shares of a row, `stride` floats apart, each times f(share): eight at a time in flight
+template <typename F>
+__device__ __forceinline__ float2 sum_shares(const float* p, long stride, int shares, int dh, int lane, F f) {
   float2 v = make_float2(0.f, 0.f);
-  if (2 * lane < dh)
-    for (int i = 0; i < shares; ++i) {
-      const float2 x = *reinterpret_cast<const float2*>(p + i * stride + 2 * lane);
-      v.x += x.x;
-      v.y += x.y;
+  const float* q = p + (2 * lane < dh ? 2 * lane : 0);
+  for (int i = 0; i < shares; i += 8) {
+    float2 x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const float2*>(q + (i + u < shares ? i + u : shares - 1) * stride);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = i + u < shares ? f(i + u) : 0.f;
+      v.x = i + u < shares ? fmaf(w, x[u].x, v.x) : v.x;
+      v.y = i + u < shares ? fmaf(w, x[u].y, v.y) : v.y;
     }
+  }
   return v;
 }
 // The (query, head) of a wavefront and its sequence; false: it is in none.
@@ -318,7 +330,7 @@ __device__ __forceinline__ bool joined_row(const PackedAttnArgs& a, long r, Seq&
   if (r >= (long)a.q_rows * a.heads) return false;
   n = (int)(r / a.heads);
   h = (int)(r - (long)n * a.heads);
-  const int sq = seq_with(a.q_off, a.q_rows, a.seqs, n);
+  const int sq = seq_with(a.q_off, a.q_len, a.seqs, n);
   if (sq < 0) return false;
   s = seq_of(a, sq);
   return n >= s.q0 && n < s.q0 + s.nq;
@@ -330,19 +342,34 @@ __global__ __launch_bounds__(256) void packed_join_fwd_kernel(PackedAttnArgs a) 
   Seq s;
   int n, h;
   if (!joined_row(a, r, s, n, h)) return;
-  float top = -FLT_MAX, sum = 0.f, v[2] = {0.f, 0.f};
-  for (int i = lane; i < a.shares; i += 64) top = fmaxf(top, a.part_stats[(i * rows + r) * 2]);
-  top = wave_max(top);
-  const int c = 2 * lane;
-  for (int i = 0; i < a.shares; ++i) {
-    const float f = fast_exp2(a.part_stats[(i * rows + r) * 2] - top);
-    sum = fmaf(f, a.part_stats[(i * rows + r) * 2 + 1], sum);
-    if (c < a.dh) {
-      const float2 x = *reinterpret_cast<const float2*>(a.part + (i * rows + r) * a.dh + c);
-      v[0] = fmaf(f, x.x, v[0]);
-      v[1] = fmaf(f, x.y, v[1]);
-    }
+  // (a lane holds the factor of every 64th share, at most MOST_SHARES / 64 of them)
+  float top = -FLT_MAX, sum = 0.f, f[MOST_SHARES / 64];
+#pragma unroll
+  for (int u = 0; u < MOST_SHARES / 64; ++u) {
+    const int i = lane + 64 * u;
+    f[u] = i < a.shares ? a.part_stats[(i * rows + r) * 2] : -FLT_MAX;
+    top = fmaxf(top, f[u]);
   }
+  top = wave_max(top);
+#pragma unroll
+  for (int u = 0; u < MOST_SHARES / 64; ++u) {
+    const int i = lane + 64 * u;
+    f[u] = fast_exp2(f[u] - top);
+    if (i < a.shares) sum = fmaf(f[u], a.part_stats[(i * rows + r) * 2 + 1], sum);
+  }
+  sum = wave_sum(sum);
+  const int c = 2 * lane;
+  float2 w = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int u = 0; u < MOST_SHARES / 64; ++u) {
+    const int n64 = a.shares - 64 * u < 64 ? a.shares - 64 * u : 64;
+    if (n64 <= 0) break;
+    const float2 x = sum_shares(a.part + (64 * u * rows + r) * a.dh, rows * a.dh, n64, a.dh, lane,
+                                [&](int i) __attribute__((always_inline)) { return __shfl(f[u], i, 64); });
+    w.x += x.x;
+    w.y += x.y;
+  }
+  const float v[2] = {w.x, w.y};
   const float g = sum == 0.f ? 0.f : 1.f / sum;
   if (!all_finite(v[0] * g, v[1] * g)) {                   // (see redo_rows)
     one_forward<T>(a, s, n - s.q0, h, lane);
@@ -358,7 +385,8 @@ __global__ __launch_bounds__(256) void packed_join_dq_kernel(PackedAttnArgs a) {
   Seq s;
   int n, h;
   if (!joined_row(a, r, s, n, h)) return;
-  const float2 v = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane);
+  const auto one = [](int) { return 1.f; };
+  const float2 v = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   if (!all_finite(v.x, v.y)) {
     one_dq<T>(a, s, n - s.q0, h, -a.dsum[r], lane);
     return;
@@ -371,12 +399,13 @@ __global__ __launch_bounds__(256) void packed_join_dkdv_kernel(PackedAttnArgs a)
   const long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long)a.k_rows * a.kv_heads;
   if (r >= rows) return;
   const int n = (int)(r / a.kv_heads), hk = (int)(r - (long)n * a.kv_heads);
-  const int sq = seq_with(a.k_off, a.k_rows, a.seqs, n);
+  const int sq = seq_with(a.k_off, a.k_len, a.seqs, n);
   if (sq < 0) return;
   const Seq s = seq_of(a, sq);
   if (n < s.k0 || n >= s.k0 + s.nk) return;
-  const float2 k = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane);
-  const float2 v = sum_shares(a.part + (a.shares * rows + r) * a.dh, rows * a.dh, a.shares, a.dh, lane);
+  const auto one = [](int) { return 1.f; };
+  const float2 k = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
+  const float2 v = sum_shares(a.part + (a.shares * rows + r) * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   if (!all_finite(k.x + k.y, v.x + v.y)) {
     one_dkdv<T>(a, s, n - s.k0, hk, lane);
     return;
@@ -392,8 +421,8 @@ constexpr int F32_ROWS = 128;            // rows (keys) of a workgroup of the fp
 
 }  // namespace
 
-hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s);
-hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s);
-hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_fwd_f32(PackedAttnArgs a, hipStream_t s);
+hipError_t launch_packed_dq_f32(PackedAttnArgs a, hipStream_t s);
+hipError_t launch_packed_dkdv_f32(PackedAttnArgs a, hipStream_t s);
 
 }  // namespace hbp

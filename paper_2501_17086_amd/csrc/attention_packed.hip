@@ -2,6 +2,8 @@
 // matrix cores; and the entry points of both storage types.
 #include "attention_packed.h"
 
+#include <type_traits>
+
 namespace hbp {
 
 namespace {
@@ -133,12 +135,13 @@ struct RowBlock {
 // Scores into the second product's operand, rounded to bf16, or, in a sequence of few keys (queries), as two parts that hold 16 bits:
 // a few roundings do not average out, and such sequences are not bound by their products.
 constexpr int FEW = 64;
+template <bool FEW_TERMS>
 struct Operand {
   bf16x8 hi[2], lo[2];
-  __device__ __forceinline__ void set(const float* p, bool few) {
+  __device__ __forceinline__ explicit Operand(const float* p) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) hi[t] = pack8(p + 8 * t);
-    if (few) {
+    if (FEW_TERMS) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const uint4 h = __builtin_bit_cast(uint4, hi[t]);
@@ -155,12 +158,12 @@ struct Operand {
   }
   // acc += the tile's columns (behind `at`, at `tile`) times the scores
   template <int DHP>
-  __device__ __forceinline__ void times(unsigned at, unsigned tile, float16v (&acc)[Geo<DHP>::MB], bool few) const {
+  __device__ __forceinline__ void times(unsigned at, unsigned tile, float16v (&acc)[Geo<DHP>::MB]) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int mb = 0; mb < Geo<DHP>::MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), hi[t], acc[mb]);
-    if (few) {
+    if (FEW_TERMS) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -247,13 +250,12 @@ __global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma
   for (int kk = 0; kk < G::KK; ++kk) fq[kk] = own_piece(qrow, kk, dh8, lane);
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) landed(fq[kk]);
-  const bool few = sq.nk <= FEW;
   const float c = a.scale * LOG2E;
   const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane) + col * S::SUB * G::TB, rv = lds0 + Frags<DHP>::rows_lane(lane) + col * S::SUB * G::TB;
   float16v o[G::MB];
   zero_acc(o);
   float m = -FLT_MAX, l = 0.f;                             // m: in units of the exponent; l: this half's sum
-  auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
+  auto step = [&](int first, int at, bool masked, auto few) __attribute__((always_inline)) {
     const unsigned tk = ck + (unsigned)at * KS::STAGE, tv = rv + (unsigned)at * KS::STAGE;
     float16v s[S::SUB];
     zero_acc(s);
@@ -271,7 +273,7 @@ __global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma
     float top = s[0][0];
 #pragma unroll
     for (int e = 1; e < 16 * S::SUB; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
-    top = fmaxf(top, other_half(top)) * c;
+    top = max_of_halves(top) * c;
     if (__any(top > m + 8.f)) {
       const float mn = fmaxf(m, top), alpha = fast_exp2(m - mn);
       m = mn;
@@ -289,21 +291,24 @@ __global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma
         p[e] = fast_exp2(fmaf(s[u][e], c, -m));
         l += p[e];
       }
-      Operand op;
-      op.set(p, few);
-      op.template times<DHP>(tv, (S::NT + u) * G::TB, o, few);
+      const Operand<decltype(few)::value> op(p);
+      op.template times<DHP>(tv, (S::NT + u) * G::TB, o);
     }
   };
-  int at = 0;
-  for (int i = b.from; i < b.to; ++i) {
-    if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
-    else copies_in_flight<0>();
-    workgroup_handover();
-    if (i + NST - 1 < b.to) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
-    const int first = S::KEYS * i + 32 * S::SUB * col;
-    if (first < b.most) step(first, at, first + 32 * S::SUB > b.fewest);
-    at = at == NST - 1 ? 0 : at + 1;
-  }
+  auto walk = [&](auto few) __attribute__((always_inline)) {
+    int at = 0;
+    for (int i = b.from; i < b.to; ++i) {
+      if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
+      else copies_in_flight<0>();
+      workgroup_handover();
+      if (i + NST - 1 < b.to) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+      const int first = S::KEYS * i + 32 * S::SUB * col;
+      if (first < b.most) step(first, at, first + 32 * S::SUB > b.fewest, few);
+      at = at == NST - 1 ? 0 : at + 1;
+    }
+  };
+  if (sq.nk <= FEW) walk(std::true_type());
+  else walk(std::false_type());
   l += other_half(l);
   __syncthreads();                                         // the ring is free: results meet in it, or leave through it
   auto row = [&](int j) __attribute__((always_inline)) {
@@ -395,19 +400,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
     a.dsum[n * a.heads + b.me.h] = -D;
     a.nlse[n * a.heads + b.me.h] = -L;
   }
-  const bool few = sq.nk <= FEW;
   const float c = a.scale * LOG2E;
   const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane) + col * S::SUB * G::TB, rk = lds0 + Frags<DHP>::rows_lane(lane) + col * S::SUB * G::TB;
-  float16v dq[G::MB];
+  float16v dq[G::MB], minus_D;
   zero_acc(dq);
-  auto step = [&](int first, int at, bool masked) __attribute__((always_inline)) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) minus_D[e] = -D;
+  auto step = [&](int first, int at, bool masked, auto few) __attribute__((always_inline)) {
     const unsigned tc = ck + (unsigned)at * KS::STAGE, tr = rk + (unsigned)at * KS::STAGE;
 #pragma unroll
     for (int u = 0; u < S::SUB; ++u) {
-      float16v s[1], dp;
+      float16v s[1], dp = minus_D;
       zero_acc(s);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dp[e] = -D;
 #pragma unroll
       for (int kk = 0; kk < G::KK; ++kk) {
         s[0] = mfma(Frags<DHP>::cols(tc, u * G::TB, kk), fq[kk], s[0]);
@@ -421,21 +425,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
         for (int e = 0; e < 16; ++e)
           if (first + 32 * u + tile_row_of(e, hh) >= b.mine) ds[e] = 0.f;
       }
-      Operand op;
-      op.set(ds, few);
-      op.template times<DHP>(tr, u * G::TB, dq, few);
+      const Operand<decltype(few)::value> op(ds);
+      op.template times<DHP>(tr, u * G::TB, dq);
     }
   };
-  int at = 0;
-  for (int i = b.from; i < b.to; ++i) {
-    if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
-    else copies_in_flight<0>();
-    workgroup_handover();
-    if (i + NST - 1 < b.to) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
-    const int first = S::KEYS * i + 32 * S::SUB * col;
-    if (first < b.most) step(first, at, first + 32 * S::SUB > b.fewest);
-    at = at == NST - 1 ? 0 : at + 1;
-  }
+  auto walk = [&](auto few) __attribute__((always_inline)) {
+    int at = 0;
+    for (int i = b.from; i < b.to; ++i) {
+      if (i + NST - 2 < b.to) copies_in_flight<KS::PW * (NST - 2)>();
+      else copies_in_flight<0>();
+      workgroup_handover();
+      if (i + NST - 1 < b.to) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+      const int first = S::KEYS * i + 32 * S::SUB * col;
+      if (first < b.most) step(first, at, first + 32 * S::SUB > b.fewest, few);
+      at = at == NST - 1 ? 0 : at + 1;
+    }
+  };
+  if (sq.nk <= FEW) walk(std::true_type());
+  else walk(std::false_type());
   __syncthreads();
   auto row = [&](int j) __attribute__((always_inline)) {
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
@@ -525,7 +532,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
       for (h += n; h >= group; h -= group) --q;
     }
   };
-  const Place begin_at{from * NT % a.group, top - from * NT / a.group};
+  const int skipped = (int)a.by_group.quotient((unsigned)(from * NT));
+  const Place begin_at{from * NT - skipped * a.group, top - skipped};
   Place pc = begin_at, pt = begin_at;
   pc.on(ct % NT, a.group);
   pt.on(st, a.group);
@@ -568,13 +576,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   }
   const int mine = first_query(key);                       // the first query that sees this lane's key
   const int begin = keys_left > 0 ? first_query(w0) : nq, all = keys_left > 0 ? first_query(w0 + (keys_left < 32 ? keys_left : 32) - 1) : nq;
-  const bool few = nq <= FEW;
   const float c = a.scale * LOG2E;
   float16v dk[G::MB], dv[G::MB];
   zero_acc(dk);
   zero_acc(dv);
   // the wavefront's tiles of the stage: their first queries
-  auto step = [&](const int (&first)[QT], int at, bool masked) __attribute__((always_inline)) {
+  auto step = [&](const int (&first)[QT], int at, bool masked, auto few) __attribute__((always_inline)) {
     const unsigned tc = cq + (unsigned)at * STAGE, tr = rq + (unsigned)at * STAGE;
     float16v s[QT], dp[QT];
     float p[QT][16];
@@ -616,13 +623,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
     }
 #pragma unroll
     for (int b = 0; b < QT; ++b) {
-      Operand op;
-      op.set(p[b], few);
-      op.template times<DHP>(tr, (NT + b) * G::TB, dv, few);
+      const Operand<decltype(few)::value> op(p[b]);
+      op.template times<DHP>(tr, (NT + b) * G::TB, dv);
 #pragma unroll
       for (int e = 0; e < 16; ++e) p[b][e] *= dp[b][e];
-      op.set(p[b], few);
-      op.template times<DHP>(tr, b * G::TB, dk, few);
+      const Operand<decltype(few)::value> ds(p[b]);
+      ds.template times<DHP>(tr, b * G::TB, dk);
     }
   };
   int at = 0;
@@ -632,24 +638,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
     me[b] = begin_at;
     me[b].on(turn * QT + b, a.group);
   }
-  for (int i = from; i < to; ++i) {
-    if (i + NST - 2 < to) copies_in_flight<(PW + 1) * (NST - 2)>();
-    else copies_in_flight<0>();
-    workgroup_handover();
-    if (i + NST - 1 < to) ask(at == 0 ? NST - 1 : at - 1);
-    int first[QT];
-    bool some = false, masked = false;
+  auto walk = [&](auto few) __attribute__((always_inline)) {
+    for (int i = from; i < to; ++i) {
+      if (i + NST - 2 < to) copies_in_flight<(PW + 1) * (NST - 2)>();
+      else copies_in_flight<0>();
+      workgroup_handover();
+      if (i + NST - 1 < to) ask(at == 0 ? NST - 1 : at - 1);
+      int first[QT];
+      bool some = false, masked = false;
 #pragma unroll
-    for (int b = 0; b < QT; ++b) {
-      const bool there = NT * i + turn * QT + b < tiles;
-      first[b] = there ? 32 * me[b].q : nq;                // (a tile past the list: masked throughout)
-      some = some || (there && first[b] + 32 > begin);
-      masked = masked || first[b] < all || first[b] + 32 > nq;
-      me[b].on(NT, a.group);
+      for (int b = 0; b < QT; ++b) {
+        const bool there = NT * i + turn * QT + b < tiles;
+        first[b] = there ? 32 * me[b].q : nq;                // (a tile past the list: masked throughout)
+        some = some || (there && first[b] + 32 > begin);
+        masked = masked || first[b] < all || first[b] + 32 > nq;
+        me[b].on(NT, a.group);
+      }
+      if (some && keys_left > 0) step(first, at, masked, few);
+      at = at == NST - 1 ? 0 : at + 1;
     }
-    if (some && keys_left > 0) step(first, at, masked);
-    at = at == NST - 1 ? 0 : at + 1;
-  }
+  };
+  if (nq <= FEW) walk(std::true_type());
+  else walk(std::false_type());
   auto meet = [&](float16v (&acc)[G::MB]) __attribute__((always_inline)) {
     float* const sums = reinterpret_cast<float*>(ring) + kw * (G::MB * 16 * 64) + lane;
     __syncthreads();                                       // (the ring, or the sums before, are free)
@@ -691,24 +701,36 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
 
 // 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64 (64 keys).
 template <int DHP>
-hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
+hipError_t fwd_mfma(PackedAttnArgs a, hipStream_t s) {
   const unsigned wide = tile_grid<false>(a, 256);
-  if (a.shares == 1 && wide >= CUS) packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
-  else packed_fwd_mfma_kernel<DHP, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+  if (a.shares == 1 && wide >= CUS) {
+    packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+  } else {
+    const dim3 grid(tile_grid<false>(a, 64), a.shares);
+    packed_fwd_mfma_kernel<DHP, 4><<<grid, 64 * WAVES, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 template <int DHP>
-hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
+hipError_t dq_mfma(PackedAttnArgs a, hipStream_t s) {
   const unsigned wide = tile_grid<false>(a, 256);
-  if (a.shares == 1 && wide >= CUS) packed_dq_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
-  else packed_dq_mfma_kernel<DHP, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+  if (a.shares == 1 && wide >= CUS) {
+    packed_dq_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+  } else {
+    const dim3 grid(tile_grid<false>(a, 64), a.shares);
+    packed_dq_mfma_kernel<DHP, 4><<<grid, 64 * WAVES, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 template <int DHP>
-hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
+hipError_t dkdv_mfma(PackedAttnArgs a, hipStream_t s) {
   const unsigned wide = tile_grid<true>(a, 128);
-  if (a.shares == 1 && wide >= CUS) packed_dkdv_mfma_kernel<DHP, 2><<<wide, 64 * WAVES, 0, s>>>(a);
-  else packed_dkdv_mfma_kernel<DHP, 4><<<dim3(tile_grid<true>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+  if (a.shares == 1 && wide >= CUS) {
+    packed_dkdv_mfma_kernel<DHP, 2><<<wide, 64 * WAVES, 0, s>>>(a);
+  } else {
+    const dim3 grid(tile_grid<true>(a, 64), a.shares);
+    packed_dkdv_mfma_kernel<DHP, 4><<<grid, 64 * WAVES, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -717,6 +739,7 @@ hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
 int shares_of(long groups, long steps) {
   long n = 2 * CUS / groups;
   if (n > steps / 4) n = steps / 4;
+  if (n > MOST_SHARES) n = MOST_SHARES;
   return n < 2 ? 1 : (int)n;
 }
 struct Shares { int rows, keys; };       // of the keys for a tile of rows (forward, dq), of the queries for a tile of keys (dk, dv)
@@ -729,6 +752,15 @@ Shares shares(int dtype, const PackedAttnArgs& a) {
           shares_of(((long)a.k_rows / keys + a.seqs) * a.kv_heads, nq * a.group / query_step)};
 }
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
+
+PackedAttnArgs with_divisors(const PackedAttnArgs& args) {
+  PackedAttnArgs a = args;
+  a.q_len = a.q_rows / a.seqs;
+  a.k_len = a.k_rows / a.seqs;
+  a.by_group = Divisor((unsigned)a.group);
+  a.by_kv = Divisor((unsigned)a.kv_heads);
+  return a;
+}
 
 // The workspace: minus D and minus lse of the rows (backward), the shares' maxima and sums (forward), the shares.
 struct Layout { size_t stats, shares, total; };
@@ -752,7 +784,7 @@ size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared) {
 }
 
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* workspace, hipStream_t s) {
-  PackedAttnArgs a = args;
+  PackedAttnArgs a = with_divisors(args);
   if (a.q_rows == 0) return hipSuccess;
   const Shares n = shares(dtype, a);
   const Layout l = layout(a, n);
@@ -768,7 +800,7 @@ hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* w
 }
 
 hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& args, void* workspace, hipStream_t s) {
-  PackedAttnArgs a = args;
+  PackedAttnArgs a = with_divisors(args);
   const Shares n = shares(dtype, a);
   const Layout l = layout(a, n);
   a.dsum = reinterpret_cast<float*>(workspace);

@@ -180,7 +180,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAtt
     float top = sc[0][0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[0][e]);
-    top = fmaxf(top, other_half(top)) * c;
+    top = max_of_halves(top) * c;
     if (__any(top > m + 8.f)) {                            // (see the bf16 kernel)
       const float mn = fmaxf(m, top), alpha = fast_exp2(m - mn);
       m = mn;
@@ -390,19 +390,19 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
 
 }  // namespace
 
-hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s) {
+hipError_t launch_packed_fwd_f32(PackedAttnArgs a, hipStream_t s) {
   const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
   if (a.dh <= 64) packed_fwd_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
   else packed_fwd_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
-hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s) {
+hipError_t launch_packed_dq_f32(PackedAttnArgs a, hipStream_t s) {
   const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
   if (a.dh <= 64) packed_dq_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
   else packed_dq_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
-hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s) {
+hipError_t launch_packed_dkdv_f32(PackedAttnArgs a, hipStream_t s) {
   const dim3 grid(tile_grid<true>(a, ROWS), a.shares);
   if (a.dh <= 64) packed_dkdv_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
   else packed_dkdv_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);

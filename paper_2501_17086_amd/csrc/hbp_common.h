@@ -238,6 +238,16 @@ hipError_t launch_rotary(int dtype, int layout, const RotaryArgs& a, hipStream_t
 
 // Attention over packed sequences with shared key/value heads (attention_packed.hip).  Strides in elements.
 struct HeadRows { void* p; long row, head; };
+// Division by a number that the host knows, n < 2^31: a multiplication, an addition and a shift, in scalar registers where n is.
+struct Divisor {
+  unsigned d, mul, shift;
+  Divisor() = default;
+  explicit Divisor(unsigned d_) : d(d_), shift(0) {
+    while ((1ull << shift) < d) ++shift;
+    mul = (unsigned)((((1ull << shift) - d) << 32) / d + 1);
+  }
+  __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
 struct PackedAttnArgs {
   HeadRows q, k, v, o, dout, dq, dk, dv;
   float* lse;               // [q_rows, heads]
@@ -252,6 +262,10 @@ struct PackedAttnArgs {
   int seqs, q_rows, k_rows;
   int heads, kv_heads, group, dh, causal;
   float scale;
+  // set by the launcher: lengths of a sequence where there are no offsets; divisions by the group, the key heads, the tiles of such a
+  // sequence
+  int q_len, k_len;
+  Divisor by_group, by_kv, by_tiles;
 };
 size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared = nullptr);     // shared: part of it are shares
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
