@@ -189,52 +189,74 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
   dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, a.dh, lane);
 }
 
-// Which key head, sequence and tile of `per` rows (keys: `per` keys) a workgroup takes.  The key heads of a tile are next to each
-// other: all problems go on side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs
-// in turn, keep a problem's streamed tiles in one XCD's L2.
-struct Tile { int hk, t, n; Seq s; bool exists; };          // t of the sequence's n tiles
+// sum over the 64 lanes
+__device__ __forceinline__ int wave_total(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);     // row_shr:1, 2, 4, 8: every row's sum in its last lane
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  return __builtin_amdgcn_readlane(v, 15) + __builtin_amdgcn_readlane(v, 31) + __builtin_amdgcn_readlane(v, 47) +
+         __builtin_amdgcn_readlane(v, 63);
+}
+
+// Which key head, sequence and tile of `per` rows (KEYS: keys) a workgroup takes.  A causal mask leaves the tiles of a sequence unequally
+// long: the last tile of rows and the first tile of keys see the whole sequence, the others less and less.  Level u of a sequence
+// is its u-th shortest tile; ids go from the highest level down, all sequences that have one, so that compute units which are
+// done early take the shorter tiles (sequence after sequence, a compute unit of two rounds got two long or two short ones: dk, dv of 16
+// sequences of 1024 at 4 key heads left 43 % of the compute units' time unused).  Key heads are next to each other: all problems go on
+// side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs in turn, keep a problem's
+// streamed tiles in one XCD's L2.
+struct Tile { int hk, t; Seq s; bool exists; };
 __device__ __forceinline__ int tiles_in(int len, int per) { return (int)((unsigned)(len + per - 1) / (unsigned)per); }   // (per: a power of two)
 template <bool KEYS>
 __device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane) {
   Tile x;
   const unsigned id = blockIdx.x;
-  x.t = (int)a.by_kv.quotient(id);
-  x.hk = (int)id - x.t * a.kv_heads;
+  int j = (int)a.by_kv.quotient(id);
+  x.hk = (int)id - j * a.kv_heads;
   const int* off = KEYS ? a.k_off : a.q_off;
   const int mult = KEYS ? 1 : a.group, rows = KEYS ? a.k_rows : a.q_rows;
-  int sq = -1;
+  int sq = -1, n = 0, level = 0;
   if (!off) {
-    x.n = (int)a.by_tiles.d;
-    sq = (int)a.by_tiles.quotient((unsigned)x.t);
-    x.t -= sq * x.n;
-    if (sq >= a.seqs) sq = -1;
+    n = tiles_in((KEYS ? a.k_len : a.q_len) * mult, per);
+    const int down = (int)a.by_seqs.quotient((unsigned)j);
+    sq = j - down * a.seqs;
+    level = n - down;
+    if (level <= 0) sq = -1;
   } else {
-    for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time: a running sum of their tiles over the lanes
-      int first, n = 0;
-      if (s0 + lane < a.seqs) span_of(off, rows, 0, s0 + lane, first, n);
-      n = tiles_in(n * mult, per);
-      int sum = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += up;
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time, one per lane
+      int first, m = 0;
+      if (s0 + lane < a.seqs) span_of(off, rows, 0, s0 + lane, first, m);
+      m = tiles_in(m * mult, per);
+      const int all = wave_total(m);
+      if (j >= all) {
+        j -= all;
+        continue;
       }
-      const unsigned long long past = __ballot(sum > x.t);
-      if (past) {
-        const int l = __ffsll(past) - 1;
+      // tiles of level u and above: sum of max(0, m - u + 1); the level of tile j is the highest u with more than j of them
+      int lo = 1, hi = tiles_in(rows * mult, per);         // (no sequence has more)
+      while (lo < hi) {
+        const int u = lo + (hi - lo + 1) / 2;
+        if (wave_total(m >= u ? m - u + 1 : 0) > j) lo = u;
+        else hi = u - 1;
+      }
+      level = lo;
+      const int rank = j - wave_total(m >= level + 1 ? m - level : 0);
+      const unsigned long long has = __ballot(m >= level);
+      const int before = __popcll(has & ((1ull << lane) - 1ull));
+      const unsigned long long here = __ballot(m >= level && before == rank);
+      if (here) {                                          // (offsets that do not decrease: always)
+        const int l = __ffsll(here) - 1;
         sq = s0 + l;
-        x.n = __builtin_amdgcn_readlane(n, l);
-        x.t -= __builtin_amdgcn_readlane(sum, l) - x.n;
-        break;
+        n = __builtin_amdgcn_readlane(m, l);
       }
-      x.t -= __builtin_amdgcn_readlane(sum, 63);
+      break;
     }
   }
   x.exists = sq >= 0;
   if (x.exists) {
     x.s = seq_of(a, sq);
-    x.t = __builtin_amdgcn_readfirstlane(x.t);
-    x.n = __builtin_amdgcn_readfirstlane(x.n);
+    x.t = __builtin_amdgcn_readfirstlane(KEYS ? n - level : level - 1);
     x.s.q0 = __builtin_amdgcn_readfirstlane(x.s.q0);
     x.s.nq = __builtin_amdgcn_readfirstlane(x.s.nq);
     x.s.k0 = __builtin_amdgcn_readfirstlane(x.s.k0);
@@ -279,13 +301,12 @@ __device__ __forceinline__ void redo_rows(float t, int rows_left, F f) {
   for (; rows != 0; rows &= rows - 1) f(__ffs((int)rows) - 1);
 }
 
-// Workgroups for tiles of `per` rows (keys), of which there are some; their kernel is to be launched with these `a`.
+// workgroups for tiles of `per` rows (keys), of which there are some
 template <bool KEYS>
-unsigned tile_grid(PackedAttnArgs& a, int per) {
+unsigned tile_grid(const PackedAttnArgs& a, int per) {
   const long rows = KEYS ? a.k_rows : (long)a.q_rows * a.group;
   const bool equal = KEYS ? !a.k_off : !a.q_off;
   const long each = (rows / a.seqs + per - 1) / per, tiles = equal ? a.seqs * each : rows / per + a.seqs;
-  a.by_tiles = Divisor(equal ? (unsigned)each : 1u);
   return (unsigned)(tiles * a.kv_heads);
 }
 
@@ -421,8 +442,8 @@ constexpr int F32_ROWS = 128;            // rows (keys) of a workgroup of the fp
 
 }  // namespace
 
-hipError_t launch_packed_fwd_f32(PackedAttnArgs a, hipStream_t s);
-hipError_t launch_packed_dq_f32(PackedAttnArgs a, hipStream_t s);
-hipError_t launch_packed_dkdv_f32(PackedAttnArgs a, hipStream_t s);
+hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s);
+hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s);
 
 }  // namespace hbp

@@ -114,7 +114,6 @@ struct RowBlock {
   __device__ __forceinline__ bool find(const PackedAttnArgs& a, int rw, int lane) {
     x = find_tile<false>(a, S::ROWS, lane);
     if (!x.exists) return false;
-    x.t = x.n - 1 - x.t;                                   // (causal: long rows first)
     const int R = x.s.nq * a.group, r0 = S::ROWS * x.t;
     w0 = r0 + 32 * rw;
     rows_left = R - w0;
@@ -701,7 +700,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
 
 // 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64 (64 keys).
 template <int DHP>
-hipError_t fwd_mfma(PackedAttnArgs a, hipStream_t s) {
+hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
   const unsigned wide = tile_grid<false>(a, 256);
   if (a.shares == 1 && wide >= CUS) {
     packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
@@ -712,7 +711,7 @@ hipError_t fwd_mfma(PackedAttnArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 template <int DHP>
-hipError_t dq_mfma(PackedAttnArgs a, hipStream_t s) {
+hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
   const unsigned wide = tile_grid<false>(a, 256);
   if (a.shares == 1 && wide >= CUS) {
     packed_dq_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
@@ -723,7 +722,7 @@ hipError_t dq_mfma(PackedAttnArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 template <int DHP>
-hipError_t dkdv_mfma(PackedAttnArgs a, hipStream_t s) {
+hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
   const unsigned wide = tile_grid<true>(a, 128);
   if (a.shares == 1 && wide >= CUS) {
     packed_dkdv_mfma_kernel<DHP, 2><<<wide, 64 * WAVES, 0, s>>>(a);
@@ -759,6 +758,7 @@ PackedAttnArgs with_divisors(const PackedAttnArgs& args) {
   a.k_len = a.k_rows / a.seqs;
   a.by_group = Divisor((unsigned)a.group);
   a.by_kv = Divisor((unsigned)a.kv_heads);
+  a.by_seqs = Divisor((unsigned)a.seqs);
   return a;
 }
 

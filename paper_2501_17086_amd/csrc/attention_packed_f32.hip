@@ -124,7 +124,6 @@ struct RowBlock {
   __device__ __forceinline__ bool find(const PackedAttnArgs& a, int wave, int lane) {
     x = find_tile<false>(a, ROWS, lane);
     if (!x.exists) return false;
-    x.t = x.n - 1 - x.t;                                   // (causal: long rows first)
     const int R = x.s.nq * a.group, r0 = ROWS * x.t;
     w0 = r0 + 32 * wave;
     rows_left = R - w0;
@@ -390,19 +389,19 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
 
 }  // namespace
 
-hipError_t launch_packed_fwd_f32(PackedAttnArgs a, hipStream_t s) {
+hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s) {
   const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
   if (a.dh <= 64) packed_fwd_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
   else packed_fwd_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
-hipError_t launch_packed_dq_f32(PackedAttnArgs a, hipStream_t s) {
+hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s) {
   const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
   if (a.dh <= 64) packed_dq_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
   else packed_dq_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
-hipError_t launch_packed_dkdv_f32(PackedAttnArgs a, hipStream_t s) {
+hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s) {
   const dim3 grid(tile_grid<true>(a, ROWS), a.shares);
   if (a.dh <= 64) packed_dkdv_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
   else packed_dkdv_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);

@@ -262,10 +262,9 @@ struct PackedAttnArgs {
   int seqs, q_rows, k_rows;
   int heads, kv_heads, group, dh, causal;
   float scale;
-  // set by the launcher: lengths of a sequence where there are no offsets; divisions by the group, the key heads, the tiles of such a
-  // sequence
+  // set by the launcher: lengths of a sequence where there are no offsets; divisions by the group, the key heads, the sequences
   int q_len, k_len;
-  Divisor by_group, by_kv, by_tiles;
+  Divisor by_group, by_kv, by_seqs;
 };
 size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared = nullptr);     // shared: part of it are shares
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
