@@ -382,6 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
   const bf16_t* qrow = row_of<bf16_t>(a.q, n, b.me.h);
   const bf16_t* grow = row_of<bf16_t>(a.dout, n, b.me.h);
   const bf16_t* orow = row_of<bf16_t>(a.o, n, b.me.h);
+  float L = a.lse[n * a.heads + b.me.h];                   // (asked for with the rows, not after them)
   bf16x8 fq[G::KK], fg[G::KK];
   float D = 0.f;
 #pragma unroll
@@ -392,9 +393,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
   }
 #pragma unroll
   for (int kk = 0; kk < G::KK; ++kk) { landed(fq[kk]); landed(fg[kk]); }
-  D += other_half(D);
-  float L = stat_of(a.lse[n * a.heads + b.me.h]);
   landed(L);
+  D += other_half(D);
+  L = stat_of(L);
   if (col == 0 && b.share == 0 && lane < 32 && lane < b.rows_left) {
     a.dsum[n * a.heads + b.me.h] = -D;
     a.nlse[n * a.heads + b.me.h] = -L;
@@ -734,9 +735,11 @@ hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
 }
 
 // Few rows (keys) leave compute units without a workgroup: the other side's steps are then shared out as well, for two workgroups on
-// every compute unit, but no fewer than four steps each.  Shares are fp32 sums that another kernel joins in a fixed order.
-int shares_of(long groups, long steps) {
-  long n = 2 * CUS / groups;
+// every compute unit (fp32: four, where products are all that counts and a causal mask's unequal tiles want evening out: forward of
+// 1530 positions, 32 heads of 80 on 8, 261 us with two, 199 with four, 217 with eight; bf16 tokens over stored keys lose
+// 9 % with four), but no fewer than four steps each.  Shares are fp32 sums that another kernel joins in a fixed order.
+int shares_of(int dtype, long groups, long steps) {
+  long n = (dtype == 0 ? 4 : 2) * CUS / groups;
   if (n > steps / 4) n = steps / 4;
   if (n > MOST_SHARES) n = MOST_SHARES;
   return n < 2 ? 1 : (int)n;
@@ -747,8 +750,8 @@ Shares shares(int dtype, const PackedAttnArgs& a) {
   const long rows = dtype == 0 ? F32_ROWS : 64, keys = dtype == 0 ? F32_ROWS : 64;
   const long key_step = dtype == 0 ? 32 : 128, query_step = dtype == 0 ? 32 : 128;
   // (workgroups as with offsets, also without: the workspace is sized before a call says which)
-  return {shares_of(((long)a.q_rows * a.group / rows + a.seqs) * a.kv_heads, nk / key_step),
-          shares_of(((long)a.k_rows / keys + a.seqs) * a.kv_heads, nq * a.group / query_step)};
+  return {shares_of(dtype, ((long)a.q_rows * a.group / rows + a.seqs) * a.kv_heads, nk / key_step),
+          shares_of(dtype, ((long)a.k_rows / keys + a.seqs) * a.kv_heads, nq * a.group / query_step)};
 }
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 
