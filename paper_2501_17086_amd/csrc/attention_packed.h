@@ -8,6 +8,7 @@
 #include "attention_device.h"
 
 #include <cfloat>
+#include <type_traits>
 
 namespace hbp {
 
@@ -187,6 +188,21 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
     }
   dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, a.dh, lane);
   dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, a.dh, lane);
+}
+
+// Heads of up to W channels (32, 64, 96 or 128): tiles of 64 or 128 channels, of which products and results take W.
+template <int W> constexpr int padded() { return W <= 64 ? 64 : 128; }
+template <int W>
+struct Fit : Geo<padded<W>()> {
+  static constexpr int KK = W / 16, MB = W / 32;
+};
+// f(the smallest such W, as a constant)
+template <typename F>
+hipError_t with_width(int dh, F f) {
+  if (dh <= 32) return f(std::integral_constant<int, 32>());
+  if (dh <= 64) return f(std::integral_constant<int, 64>());
+  if (dh <= 96) return f(std::integral_constant<int, 96>());
+  return f(std::integral_constant<int, 128>());
 }
 
 // sum over the 64 lanes

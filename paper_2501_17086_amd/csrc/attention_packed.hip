@@ -2,8 +2,6 @@
 // matrix cores; and the entry points of both storage types.
 #include "attention_packed.h"
 
-#include <type_traits>
-
 namespace hbp {
 
 namespace {
@@ -93,9 +91,10 @@ struct KeyStream {
 // How a workgroup's eight wavefronts share rows and keys.  COLS = 1: 256 rows, 32 for each wavefront, which goes over all keys in
 // steps of 64.  COLS = 4, for few rows: 64 rows, and of every step of 128 keys a wavefront takes 32; the four that share rows
 // meet in LDS at the end.
-template <int DHP, int COLS>
+template <int W, int COLS>
 struct Shape {
-  typedef Geo<DHP> G;
+  static constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
   static constexpr int ROWS = 32 * WAVES / COLS;
   static constexpr int NT = COLS == 1 ? 2 : 4, KEYS = 32 * NT, SUB = NT / COLS;
   typedef KeyStream<DHP, NT> KS;
@@ -105,9 +104,9 @@ struct Shape {
 };
 
 // The rows of a workgroup, and the keys that they see: steps from .. to - 1 of this workgroup's share of them.
-template <int DHP, int COLS>
+template <int W, int COLS>
 struct RowBlock {
-  typedef Shape<DHP, COLS> S;
+  typedef Shape<W, COLS> S;
   Tile x;
   int w0, rows_left, mine, fewest, most, from, to, share;
   RowPlace me;
@@ -156,17 +155,17 @@ struct Operand {
     }
   }
   // acc += the tile's columns (behind `at`, at `tile`) times the scores
-  template <int DHP>
-  __device__ __forceinline__ void times(unsigned at, unsigned tile, float16v (&acc)[Geo<DHP>::MB]) const {
+  template <int DHP, int MB>
+  __device__ __forceinline__ void times(unsigned at, unsigned tile, float16v (&acc)[MB]) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int mb = 0; mb < Geo<DHP>::MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), hi[t], acc[mb]);
+      for (int mb = 0; mb < MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), hi[t], acc[mb]);
     if (FEW_TERMS) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int mb = 0; mb < Geo<DHP>::MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), lo[t], acc[mb]);
+        for (int mb = 0; mb < MB; ++mb) acc[mb] = mfma(Frags<DHP>::rows(at, tile, mb, t), lo[t], acc[mb]);
     }
   }
 };
@@ -225,17 +224,18 @@ __device__ __forceinline__ void get_sums(const float* sums, int rw, int m, const
 // then reach 2^8, sums 2^8 times the keys: far inside fp32, and bf16 rounds relatively), so the output is rarely rescaled.
 // Few rows over long keys (a.shares > 1): a workgroup takes a share of the steps and leaves sums, maxima and outputs for
 // packed_join_fwd_kernel.
-template <int DHP, int COLS>
-__global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma_kernel(PackedAttnArgs a) {
-  typedef Geo<DHP> G;
-  typedef Shape<DHP, COLS> S;
+template <int W, int COLS>
+__global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_kernel(PackedAttnArgs a) {
+  constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
+  typedef Shape<W, COLS> S;
   typedef typename S::KS KS;
   constexpr int NST = S::NST, RW = WAVES / COLS;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[S::RING];
   __shared__ float stats[COLS == 1 ? 1 : WAVES][2][64];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = wave % RW, col = wave / RW;
-  RowBlock<DHP, COLS> b;
+  RowBlock<W, COLS> b;
   if (!b.find(a, rw, lane)) return;
   const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3;
@@ -362,16 +362,17 @@ __global__ __launch_bounds__(64 * WAVES, DHP == 64 ? 4 : 2) void packed_fwd_mfma
 
 // dq, and for the other kernel minus D = sum_c dout (.) o and minus lse of every row.  As the forward pass: a lane holds a row of q and
 // of dout, dS leaves the first two products in the places from which the third takes it.
-template <int DHP, int COLS>
+template <int W, int COLS>
 __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAttnArgs a) {
-  typedef Geo<DHP> G;
-  typedef Shape<DHP, COLS> S;
+  constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
+  typedef Shape<W, COLS> S;
   typedef typename S::KS KS;
   constexpr int NST = S::NST, RW = WAVES / COLS;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[S::RING];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = wave % RW, col = wave / RW;
-  RowBlock<DHP, COLS> b;
+  RowBlock<W, COLS> b;
   if (!b.find(a, rw, lane)) return;
   const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3;
@@ -484,9 +485,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
 // Queries come from the last one down, all heads of the group for a tile of queries before the next tile: whatever the mask
 // leaves them, the workgroups of a key head begin with the same tiles and stay in step, so that the tiles come from the XCD's L2.
 // At 128 channels k stays in LDS, which leaves registers for two wavefronts on every SIMD.
-template <int DHP, int TURNS>
+template <int W, int TURNS>
 __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedAttnArgs a) {
-  typedef Geo<DHP> G;
+  constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
   constexpr bool KLDS = DHP == 128;
   constexpr int NST = DHP == 128 && TURNS == 4 ? 2 : 3;
   constexpr int KW = WAVES / TURNS, KEYS = 32 * KW;
@@ -700,36 +702,36 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
 }
 
 // 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64 (64 keys).
-template <int DHP>
+template <int W>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
   const unsigned wide = tile_grid<false>(a, 256);
   if (a.shares == 1 && wide >= CUS) {
-    packed_fwd_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+    packed_fwd_mfma_kernel<W, 1><<<wide, 64 * WAVES, 0, s>>>(a);
   } else {
     const dim3 grid(tile_grid<false>(a, 64), a.shares);
-    packed_fwd_mfma_kernel<DHP, 4><<<grid, 64 * WAVES, 0, s>>>(a);
+    packed_fwd_mfma_kernel<W, 4><<<grid, 64 * WAVES, 0, s>>>(a);
   }
   return hipGetLastError();
 }
-template <int DHP>
+template <int W>
 hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
   const unsigned wide = tile_grid<false>(a, 256);
   if (a.shares == 1 && wide >= CUS) {
-    packed_dq_mfma_kernel<DHP, 1><<<wide, 64 * WAVES, 0, s>>>(a);
+    packed_dq_mfma_kernel<W, 1><<<wide, 64 * WAVES, 0, s>>>(a);
   } else {
     const dim3 grid(tile_grid<false>(a, 64), a.shares);
-    packed_dq_mfma_kernel<DHP, 4><<<grid, 64 * WAVES, 0, s>>>(a);
+    packed_dq_mfma_kernel<W, 4><<<grid, 64 * WAVES, 0, s>>>(a);
   }
   return hipGetLastError();
 }
-template <int DHP>
+template <int W>
 hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
   const unsigned wide = tile_grid<true>(a, 128);
   if (a.shares == 1 && wide >= CUS) {
-    packed_dkdv_mfma_kernel<DHP, 2><<<wide, 64 * WAVES, 0, s>>>(a);
+    packed_dkdv_mfma_kernel<W, 2><<<wide, 64 * WAVES, 0, s>>>(a);
   } else {
     const dim3 grid(tile_grid<true>(a, 64), a.shares);
-    packed_dkdv_mfma_kernel<DHP, 4><<<grid, 64 * WAVES, 0, s>>>(a);
+    packed_dkdv_mfma_kernel<W, 4><<<grid, 64 * WAVES, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -794,7 +796,7 @@ hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* w
   a.shares = n.rows;
   a.part_stats = reinterpret_cast<float*>(workspace);
   a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.shares);
-  const hipError_t e = dtype == 0 ? launch_packed_fwd_f32(a, s) : a.dh <= 64 ? fwd_mfma<64>(a, s) : fwd_mfma<128>(a, s);
+  const hipError_t e = dtype == 0 ? launch_packed_fwd_f32(a, s) : with_width(a.dh, [&](auto w) { return fwd_mfma<decltype(w)::value>(a, s); });
   if (e != hipSuccess || a.shares == 1) return e;
   const unsigned grid = (unsigned)(((long)a.q_rows * a.heads + 3) / 4);
   if (dtype == 0) packed_join_fwd_kernel<float><<<grid, 256, 0, s>>>(a);
@@ -812,7 +814,7 @@ hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& args, void* w
   hipError_t e = hipSuccess;
   if (a.q_rows > 0) {
     a.shares = n.rows;
-    e = dtype == 0 ? launch_packed_dq_f32(a, s) : a.dh <= 64 ? dq_mfma<64>(a, s) : dq_mfma<128>(a, s);
+    e = dtype == 0 ? launch_packed_dq_f32(a, s) : with_width(a.dh, [&](auto w) { return dq_mfma<decltype(w)::value>(a, s); });
     if (e != hipSuccess) return e;
     if (a.shares > 1) {
       const unsigned grid = (unsigned)(((long)a.q_rows * a.heads + 3) / 4);
@@ -822,7 +824,7 @@ hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& args, void* w
   }
   if (a.k_rows > 0) {
     a.shares = n.keys;
-    e = dtype == 0 ? launch_packed_dkdv_f32(a, s) : a.dh <= 64 ? dkdv_mfma<64>(a, s) : dkdv_mfma<128>(a, s);
+    e = dtype == 0 ? launch_packed_dkdv_f32(a, s) : with_width(a.dh, [&](auto w) { return dkdv_mfma<decltype(w)::value>(a, s); });
     if (e != hipSuccess) return e;
     if (a.shares > 1) {
       const unsigned grid = (unsigned)(((long)a.k_rows * a.kv_heads + 3) / 4);

@@ -18,10 +18,10 @@ __device__ __forceinline__ float16v mfma_f32(float x, float y, float16v acc) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, acc, 0, 0, 0);
 }
 
-// W channels (64 or 128) of fp32 are the bytes of 2 W of bf16: the tiles' layout is that.
+// W channels of fp32 in tiles of 64 or 128 are the bytes of twice as many of bf16: the tiles' layout is that.
 template <int W>
 struct Tiles {
-  typedef Geo<2 * W> G;
+  typedef Geo<2 * padded<W>()> G;
   typedef float floatv4 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) const floatv4* chunk_p;
   typedef __attribute__((address_space(3))) const float* one_p;
@@ -79,7 +79,8 @@ struct Tiles {
 // Two tiles of 32 rows, x then y, that the workgroup copies into a stage together; rows past the last (of n) repeat it.
 template <int W>
 struct PairStream {
-  typedef Geo<2 * W> G;
+  static constexpr int DHP = 2 * padded<W>();
+  typedef Geo<DHP> G;
   static constexpr int PW = 2 * G::COPIES / WAVES;
   unsigned off[PW], ld, lds;
   int tile, part, dh4;
@@ -91,7 +92,7 @@ struct PairStream {
     ld = tile ? ldy : ldx;
     lds = lds0 + (unsigned)(w * PW) * 1024u;
 #pragma unroll
-    for (int u = 0; u < PW; ++u) off[u] = copy_offset<2 * W>(ld, part + u, 32, dh4, lane);
+    for (int u = 0; u < PW; ++u) off[u] = copy_offset<DHP>(ld, part + u, 32, dh4, lane);
   }
   // x, y: row 0; rows first .. into stage `at`
   __device__ __forceinline__ void issue(const float* x, const float* y, int first, int n, int at, int lane) const {
@@ -99,7 +100,7 @@ struct PairStream {
     const unsigned dst = lds + (unsigned)at * (2u * G::TB);
 #pragma unroll
     for (int u = 0; u < PW; ++u)
-      copy16_to_lds(first + 32 <= n ? off[u] : copy_offset<2 * W>(ld, part + u, n - first, dh4, lane), base, dst + 1024u * u);
+      copy16_to_lds(first + 32 <= n ? off[u] : copy_offset<DHP>(ld, part + u, n - first, dh4, lane), base, dst + 1024u * u);
   }
 };
 
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAtt
 }
 
 template <int W>
-__global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dq_f32_kernel(PackedAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, W > 96 ? 1 : 2) void packed_dq_f32_kernel(PackedAttnArgs a) {
   typedef Tiles<W> T;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[2 * T::STAGE];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dq_f32_ke
 
 // Queries from the last tile down, all heads of the group for one tile before the next.
 template <int W>
-__global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_kernel(PackedAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, W > 64 ? 1 : 2) void packed_dkdv_f32_kernel(PackedAttnArgs a) {
   typedef Tiles<W> T;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[2 * T::STAGE];
   __shared__ __attribute__((aligned(256))) float stats[2][2][64];                // [stage][-lse | -D][32 rows, and again]
@@ -391,21 +392,24 @@ __global__ __launch_bounds__(64 * WAVES, W == 128 ? 1 : 2) void packed_dkdv_f32_
 
 hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s) {
   const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
-  if (a.dh <= 64) packed_fwd_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
-  else packed_fwd_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
+  return with_width(a.dh, [&](auto w) {
+    packed_fwd_f32_kernel<decltype(w)::value><<<grid, 64 * WAVES, 0, s>>>(a);
+    return hipGetLastError();
+  });
 }
 hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s) {
   const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
-  if (a.dh <= 64) packed_dq_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
-  else packed_dq_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
+  return with_width(a.dh, [&](auto w) {
+    packed_dq_f32_kernel<decltype(w)::value><<<grid, 64 * WAVES, 0, s>>>(a);
+    return hipGetLastError();
+  });
 }
 hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s) {
   const dim3 grid(tile_grid<true>(a, ROWS), a.shares);
-  if (a.dh <= 64) packed_dkdv_f32_kernel<64><<<grid, 64 * WAVES, 0, s>>>(a);
-  else packed_dkdv_f32_kernel<128><<<grid, 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
+  return with_width(a.dh, [&](auto w) {
+    packed_dkdv_f32_kernel<decltype(w)::value><<<grid, 64 * WAVES, 0, s>>>(a);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace hbp
