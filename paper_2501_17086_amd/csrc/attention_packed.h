@@ -454,7 +454,15 @@ __global__ __launch_bounds__(256) void packed_join_dkdv_kernel(PackedAttnArgs a)
 }
 
 constexpr unsigned CUS = 256;
-constexpr int F32_ROWS = 128;            // rows (keys) of a workgroup of the fp32 kernels
+// Rows (keys) of a workgroup, `wide` or fewer of them with the other side's tiles shared out between its wavefronts: wide where that makes
+// `least` workgroups (counted as with offsets, of which the workspace's size knows nothing) and where sequences have more rows than
+// the narrow form takes at a time.
+template <bool KEYS>
+bool wide_blocks(const PackedAttnArgs& a, int wide, int narrow, long least) {
+  const long rows = KEYS ? (long)a.k_rows : (long)a.q_rows * a.group;
+  return (rows / wide + a.seqs) * a.kv_heads >= least && rows / a.seqs > narrow;
+}
+template <bool KEYS> bool f32_wide(const PackedAttnArgs& a) { return wide_blocks<KEYS>(a, 128, 32, CUS / 2); }
 
 }  // namespace
 

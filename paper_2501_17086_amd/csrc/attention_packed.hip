@@ -701,38 +701,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, lane); });
 }
 
-// 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64 (64 keys).
+// 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64
 template <int W>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  const unsigned wide = tile_grid<false>(a, 256);
-  if (a.shares == 1 && wide >= CUS) {
-    packed_fwd_mfma_kernel<W, 1><<<wide, 64 * WAVES, 0, s>>>(a);
-  } else {
-    const dim3 grid(tile_grid<false>(a, 64), a.shares);
-    packed_fwd_mfma_kernel<W, 4><<<grid, 64 * WAVES, 0, s>>>(a);
-  }
+  if (wide_blocks<false>(a, 256, 64, CUS))
+    packed_fwd_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
+  else
+    packed_fwd_mfma_kernel<W, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int W>
 hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  const unsigned wide = tile_grid<false>(a, 256);
-  if (a.shares == 1 && wide >= CUS) {
-    packed_dq_mfma_kernel<W, 1><<<wide, 64 * WAVES, 0, s>>>(a);
-  } else {
-    const dim3 grid(tile_grid<false>(a, 64), a.shares);
-    packed_dq_mfma_kernel<W, 4><<<grid, 64 * WAVES, 0, s>>>(a);
-  }
+  if (wide_blocks<false>(a, 256, 64, CUS))
+    packed_dq_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
+  else
+    packed_dq_mfma_kernel<W, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int W>
 hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  const unsigned wide = tile_grid<true>(a, 128);
-  if (a.shares == 1 && wide >= CUS) {
-    packed_dkdv_mfma_kernel<W, 2><<<wide, 64 * WAVES, 0, s>>>(a);
-  } else {
-    const dim3 grid(tile_grid<true>(a, 64), a.shares);
-    packed_dkdv_mfma_kernel<W, 4><<<grid, 64 * WAVES, 0, s>>>(a);
-  }
+  if (wide_blocks<true>(a, 128, 64, CUS))
+    packed_dkdv_mfma_kernel<W, 2><<<tile_grid<true>(a, 128), 64 * WAVES, 0, s>>>(a);
+  else
+    packed_dkdv_mfma_kernel<W, 4><<<dim3(tile_grid<true>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -749,12 +740,16 @@ int shares_of(int dtype, long groups, long steps) {
 struct Shares { int rows, keys; };       // of the keys for a tile of rows (forward, dq), of the queries for a tile of keys (dk, dv)
 Shares shares(int dtype, const PackedAttnArgs& a) {
   const long nq = a.q_rows / a.seqs, nk = a.k_rows / a.seqs;           // (of a sequence, on average)
-  const long rows = dtype == 0 ? F32_ROWS : 64, keys = dtype == 0 ? F32_ROWS : 64;
-  const long key_step = dtype == 0 ? 32 : 128, query_step = dtype == 0 ? 32 : 128;
-  // (workgroups as with offsets, also without: the workspace is sized before a call says which)
-  return {shares_of(dtype, ((long)a.q_rows * a.group / rows + a.seqs) * a.kv_heads, nk / key_step),
-          shares_of(dtype, ((long)a.k_rows / keys + a.seqs) * a.kv_heads, nq * a.group / query_step)};
+  // rows (keys) of a workgroup, and keys (queries) of a step
+  const bool f32 = dtype == 0, wide_r = f32 ? f32_wide<false>(a) : wide_blocks<false>(a, 256, 64, CUS);
+  const bool wide_k = f32 ? f32_wide<true>(a) : wide_blocks<true>(a, 128, 64, CUS);
+  const long rows = f32 ? (wide_r ? 128 : 32) : 64, keys = f32 ? (wide_k ? 128 : 32) : 64;
+  const long key_step = f32 && wide_r ? 32 : 128, query_step = f32 && wide_k ? 32 : 128;
+  const long row_blocks = ((long)a.q_rows * a.group / rows + a.seqs) * a.kv_heads, key_blocks = ((long)a.k_rows / keys + a.seqs) * a.kv_heads;
+  return {!f32 && wide_r ? 1 : shares_of(dtype, row_blocks, nk / key_step),
+          !f32 && wide_k ? 1 : shares_of(dtype, key_blocks, (nq + 31) / 32 * 32 * a.group / query_step)};
 }
+
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 
 PackedAttnArgs with_divisors(const PackedAttnArgs& args) {

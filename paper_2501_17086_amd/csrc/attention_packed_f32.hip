@@ -4,15 +4,14 @@
 // The shapes are those of the bf16 kernels (attention_packed.hip): a lane owns one row (dk, dv: one key) and half of its scores, which
 // enter the second product straight from the registers.  A product of contraction length 2 takes one number per lane from either
 // side; which channel that is may be chosen freely as long as both sides agree, so four of them come from one 16-byte read.
-// Four wavefronts of 32 rows (keys); the other side streams in tiles of 32 through two stages of LDS.
+// Four wavefronts; the other side streams in tiles of 32 rows through LDS.
 #include "attention_packed.h"
 
 namespace hbp {
 
 namespace {
 
-constexpr int WAVES = 4, ROWS = F32_ROWS;
-static_assert(ROWS == 32 * WAVES, "a wavefront has 32 rows");
+constexpr int WAVES = 4;
 
 __device__ __forceinline__ float16v mfma_f32(float x, float y, float16v acc) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, acc, 0, 0, 0);
@@ -25,7 +24,7 @@ struct Tiles {
   typedef float floatv4 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) const floatv4* chunk_p;
   typedef __attribute__((address_space(3))) const float* one_p;
-  static constexpr int STAGE = 2 * G::TB, J = W / 8, MB = W / 32;
+  static constexpr int J = W / 8, MB = W / 32;
   // A tile's row l % 32: this half's four channels 8 j + 4 (l / 32) .. + 3.
   static __device__ __forceinline__ unsigned cols_lane(int lane) {
     const int r = lane & 31;
@@ -76,60 +75,82 @@ struct Tiles {
   }
 };
 
-// Two tiles of 32 rows, x then y, that the workgroup copies into a stage together; rows past the last (of n) repeat it.
-template <int W>
+// Stages of 2 NT tiles of 32 rows, NT of x, then NT of y, that the workgroup copies together, a wavefront whole tiles or parts of one; rows
+// past the last (of n) repeat it.  NST stages: two, or one where two do not fit, which is then filled between two barriers.
+template <int W, int NT>
 struct PairStream {
   static constexpr int DHP = 2 * padded<W>();
   typedef Geo<DHP> G;
-  static constexpr int PW = 2 * G::COPIES / WAVES;
-  unsigned off[PW], ld, lds;
-  int tile, part, dh4;
-  __device__ __forceinline__ PairStream(unsigned ldx, unsigned ldy, int dh, unsigned lds0, int w, int lane) {
-    static_assert(G::COPIES % PW == 0, "a wavefront's copies are of one tile");
-    tile = w * PW / G::COPIES;
+  static constexpr int STAGE = 2 * NT * G::TB, NST = 2 * STAGE <= 128 * 1024 ? 2 : 1;
+  static constexpr int PW = 2 * NT * G::COPIES / WAVES, TILES = PW < G::COPIES ? 1 : PW / G::COPIES, PARTS = PW / TILES;
+  unsigned lds, ldx, ldy;
+  int first_tile, part, dh4;
+  __device__ __forceinline__ PairStream(unsigned ldx_, unsigned ldy_, int dh, unsigned lds0, int w) {
+    first_tile = w * PW / G::COPIES;
     part = w * PW % G::COPIES;
     dh4 = dh >> 2;
-    ld = tile ? ldy : ldx;
+    ldx = ldx_;
+    ldy = ldy_;
     lds = lds0 + (unsigned)(w * PW) * 1024u;
-#pragma unroll
-    for (int u = 0; u < PW; ++u) off[u] = copy_offset<DHP>(ld, part + u, 32, dh4, lane);
   }
-  // x, y: row 0; rows first .. into stage `at`
-  __device__ __forceinline__ void issue(const float* x, const float* y, int first, int n, int at, int lane) const {
-    const unsigned char* base = reinterpret_cast<const unsigned char*>(tile ? y : x) + (long)first * ld;
-    const unsigned dst = lds + (unsigned)at * (2u * G::TB);
+  // this wavefront's copies of its i-th tile (of x: tile() < NT), whose row 0 is at `base` and which has n rows from there
+  __device__ __forceinline__ int tile(int i) const { return first_tile + i; }
+  __device__ __forceinline__ void issue(int i, const float* base, int n, int at, int lane) const {
+    const unsigned ld = tile(i) < NT ? ldx : ldy, dst = lds + (unsigned)at * STAGE + (unsigned)(i * PARTS) * 1024u;
 #pragma unroll
-    for (int u = 0; u < PW; ++u)
-      copy16_to_lds(first + 32 <= n ? off[u] : copy_offset<DHP>(ld, part + u, n - first, dh4, lane), base, dst + 1024u * u);
+    for (int u = 0; u < PARTS; ++u) copy16_to_lds(copy_offset<DHP>(ld, part + u, n, dh4, lane), base, dst + 1024u * u);
   }
 };
+// Before the compute of step i of from .. to - 1: its stage is full.  ask(step, stage) issues the copies.
+template <int NST, typename F>
+__device__ __forceinline__ int next_stage(int i, int from, int to, F ask) {
+  if (NST == 1) {
+    if (i > from) {
+      workgroup_handover();                                // everyone is done with the step before
+      ask(i, 0);
+    }
+    copies_in_flight<0>();
+    workgroup_handover();
+    return 0;
+  }
+  copies_in_flight<0>();
+  workgroup_handover();
+  if (i + 1 < to) ask(i + 1, (i + 1) & 1);
+  return i & 1;
+}
 
-// a lane holds columns 32 m + 8 g + 4 (l / 32) .. + 3 of its row
+// Blocks of 32 channels from block m0 on: a lane holds columns 32 m + 8 g + 4 (l / 32) .. + 3 of its row.
 template <int MB>
-__device__ __forceinline__ void store_row(float* row, const float16v (&acc)[MB], float f, int dh, int hh) {
+__device__ __forceinline__ void store_row(float* row, const float16v (&acc)[MB], float f, int m0, int dh, int hh) {
 #pragma unroll
   for (int m = 0; m < MB; ++m)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int c = 32 * m + 8 * g + 4 * hh;
+      const int c = 32 * (m0 + m) + 8 * g + 4 * hh;
       if (c < dh)
         *reinterpret_cast<float4*>(row + c) = make_float4(acc[m][4 * g] * f, acc[m][4 * g + 1] * f, acc[m][4 * g + 2] * f, acc[m][4 * g + 3] * f);
     }
 }
 
-// The rows of a workgroup and what its wavefronts see of the keys.
+// How the four wavefronts share rows and keys.  COLS = 1: 128 rows, 32 for each wavefront, steps of 32 keys.  COLS = 4, for few rows: 32 rows,
+// steps of 128 keys of which a wavefront takes 32; they meet in LDS at the end.
+template <int COLS> constexpr int rows_of_block() { return 32 * WAVES / COLS; }
+template <int W, int COLS>
 struct RowBlock {
+  static constexpr int ROWS = rows_of_block<COLS>(), NT = COLS, KEYS = 32 * NT;
+  typedef PairStream<W, NT> PS;
   Tile x;
   int w0, rows_left, mine, fewest, most, from, to, share;  // from .. to - 1: this workgroup's share of the steps
   RowPlace me;
-  __device__ __forceinline__ bool find(const PackedAttnArgs& a, int wave, int lane) {
+  const float *k, *v;
+  __device__ __forceinline__ bool find(const PackedAttnArgs& a, int rw, int lane) {
     x = find_tile<false>(a, ROWS, lane);
     if (!x.exists) return false;
     const int R = x.s.nq * a.group, r0 = ROWS * x.t;
-    w0 = r0 + 32 * wave;
+    w0 = r0 + 32 * rw;
     rows_left = R - w0;
     auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
-    const int steps = (seen((R < r0 + ROWS ? R : r0 + ROWS) - 1) + 31) >> 5;
+    const int steps = (seen((R < r0 + ROWS ? R : r0 + ROWS) - 1) + KEYS - 1) / KEYS;
     share = (int)blockIdx.y;
     from = (int)((long)steps * share / a.shares);
     to = (int)((long)steps * (share + 1) / a.shares);
@@ -138,44 +159,78 @@ struct RowBlock {
     mine = seen_by(x.s, me.i, a.causal);
     fewest = rows_left > 0 ? seen(w0) : 0;
     most = rows_left > 0 ? seen(w0 + (rows_left < 32 ? rows_left : 32) - 1) : 0;
+    k = row_of<float>(a.k, x.s.k0, x.hk);
+    v = row_of<float>(a.v, x.s.k0, x.hk);
     return true;
   }
+  __device__ __forceinline__ void ask(const PS& ps, const PackedAttnArgs& a, int i, int at, int lane) const {
+#pragma unroll
+    for (int u = 0; u < PS::TILES; ++u) {
+      const int t = ps.tile(u);
+      int first = KEYS * i + 32 * (t % NT);
+      first = first < x.s.nk ? first : x.s.nk - 1;
+      ps.issue(u, (t < NT ? k : v) + (long)first * (t < NT ? a.k.row : a.v.row), x.s.nk - first < 32 ? x.s.nk - first : 32, at, lane);
+    }
+  }
 };
+// The wavefronts' outputs, [wavefront][block][element][lane], into block m of their sum, each times its f.
+template <int MB>
+__device__ __forceinline__ void put_sums(float* sums, int wave, const float16v (&acc)[MB], int lane) {
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sums[((wave * MB + m) * 16 + e) * 64 + lane] = acc[m][e];
+}
+template <int MB>
+__device__ __forceinline__ void get_sums(const float* sums, int m, const float (&f)[WAVES], float16v (&acc)[1], int lane) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < WAVES; ++j) t = fmaf(f[j], sums[((j * MB + m) * 16 + e) * 64 + lane], t);
+    acc[0][e] = t;
+  }
+}
+template <int W, int NT> constexpr int ring_bytes() {
+  typedef PairStream<W, NT> PS;
+  constexpr int ring = PS::NST * PS::STAGE, sums = NT == 1 ? 0 : WAVES * Tiles<W>::MB * 16 * 64 * 4;
+  return ring > sums ? ring : sums;
+}
 
-template <int W>
-__global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAttnArgs a) {
+template <int W, int COLS>
+__global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_kernel(PackedAttnArgs a) {
   typedef Tiles<W> T;
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[2 * T::STAGE];
+  typedef RowBlock<W, COLS> RB;
+  typedef typename RB::PS PS;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[ring_bytes<W, COLS>()];
+  __shared__ float stats[COLS == 1 ? 1 : WAVES][2][64];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  RowBlock b;
-  if (!b.find(a, wave, lane)) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = COLS == 1 ? wave : 0, col = COLS == 1 ? 0 : wave;
+  RB b;
+  if (!b.find(a, rw, lane)) return;
   const Seq& s = b.x.s;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
-  const PairStream<W> ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave, lane);
-  const float* k = row_of<float>(a.k, s.k0, b.x.hk);
-  const float* v = row_of<float>(a.v, s.k0, b.x.hk);
-  if (b.from < b.to) ps.issue(k, v, 32 * b.from, s.nk, b.from & 1, lane);
+  const PS ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave);
+  auto ask = [&](int i, int at) __attribute__((always_inline)) { b.ask(ps, a, i, at, lane); };
+  if (b.from < b.to) ask(b.from, PS::NST == 1 ? 0 : b.from & 1);
   float q[4 * T::J];
   T::own(row_of<float>(a.q, s.q0 + b.me.i, b.me.h), a.dh, lane, q);
-  const unsigned ck = lds0 + T::cols_lane(lane), rv = lds0 + T::rows_lane(lane);
+  const unsigned ck = lds0 + T::cols_lane(lane) + (unsigned)col * T::G::TB, rv = lds0 + T::rows_lane(lane) + (unsigned)col * T::G::TB;
   const float c = a.scale * LOG2E;
   float16v o[T::MB];
   zero_acc(o);
   float m = -FLT_MAX, l = 0.f;
   for (int i = b.from; i < b.to; ++i) {
-    copies_in_flight<0>();
-    workgroup_handover();
-    if (i + 1 < b.to) ps.issue(k, v, 32 * (i + 1), s.nk, (i + 1) & 1, lane);
-    if (32 * i >= b.most) continue;
-    const unsigned at = (unsigned)(i & 1) * T::STAGE;
+    const unsigned at = (unsigned)next_stage<PS::NST>(i, b.from, b.to, ask) * PS::STAGE;
+    const int first = RB::KEYS * i + 32 * col;
+    if (first >= b.most) continue;
     float16v sc[1];
     zero_acc(sc);
     sc[0] = T::product(ck + at, 0, q, sc[0]);
-    if (32 * i + 32 > b.fewest) {
+    if (first + 32 > b.fewest) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (32 * i + tile_row_of(e, hh) >= b.mine) sc[0][e] = -INFINITY;
+        if (first + tile_row_of(e, hh) >= b.mine) sc[0][e] = -INFINITY;
     }
     float top = sc[0][0];
 #pragma unroll
@@ -195,48 +250,76 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_f32_kernel(PackedAtt
       sc[0][e] = fast_exp2(fmaf(sc[0][e], c, -m));
       l += sc[0][e];
     }
-    T::add(rv + at, T::G::TB, sc[0], o);
+    T::add(rv + at, RB::NT * T::G::TB, sc[0], o);
   }
-  if (b.rows_left <= 0) return;
   l += other_half(l);
-  const float f = l == 0.f ? 0.f : 1.f / l;
-  const long n = s.q0 + b.me.i;
-  if (a.shares > 1) {
-    const long p = (long)b.share * a.q_rows * a.heads + n * a.heads + b.me.h;
-    if ((lane & 31) < b.rows_left) {
-      store_share<T::MB>(a.part, p, o, 0, a.dh, hh);
-      if (hh == 0) {
-        a.part_stats[2 * p] = m;
-        a.part_stats[2 * p + 1] = l;
+  const long n = s.q0 + b.me.i, r = n * a.heads + b.me.h, p = (long)b.share * a.q_rows * a.heads + r;
+  const bool there = (lane & 31) < b.rows_left;
+  auto redo = [&](int j) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    one_forward<float>(a, s, q.i, q.h, lane);
+  };
+  // blocks m0 .. of the rows' outputs, sums l relative to m
+  auto leave = [&](auto& acc, int m0, float m, float l) __attribute__((always_inline)) {
+    constexpr int N = sizeof(acc) / sizeof(acc[0]);
+    if (a.shares > 1) {
+      if (there) {
+        store_share<N>(a.part, p, acc, m0, a.dh, hh);
+        if (hh == 0 && m0 == 0) {
+          a.part_stats[2 * p] = m;
+          a.part_stats[2 * p + 1] = l;
+        }
       }
+      return;
     }
-    return;
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    if (there) {
+      store_row(row_out<float>(a.o, n, b.me.h), acc, f, m0, a.dh, hh);
+      if (hh == 0 && m0 == 0) a.lse[r] = l == 0.f ? -INFINITY : m + log2f(l);
+    }
+    redo_rows(not_finite(acc, f * 0.f), b.rows_left, redo);
+  };
+  if constexpr (COLS == 1) {
+    if (b.rows_left > 0) leave(o, 0, m, l);
+  } else {
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(ring);
+    put_sums(sums, wave, o, lane);
+    stats[wave][0][lane] = m;
+    stats[wave][1][lane] = l;
+    __syncthreads();
+    if (col >= T::MB) return;                              // (a block of 32 channels each)
+    float f[WAVES], top = stats[0][0][lane], sum = 0.f;
+#pragma unroll
+    for (int j = 1; j < WAVES; ++j) top = fmaxf(top, stats[j][0][lane]);
+#pragma unroll
+    for (int j = 0; j < WAVES; ++j) {
+      f[j] = fast_exp2(stats[j][0][lane] - top);
+      sum = fmaf(f[j], stats[j][1][lane], sum);
+    }
+    float16v acc[1];
+    get_sums<T::MB>(sums, col, f, acc, lane);
+    leave(acc, col, top, sum);
   }
-  if ((lane & 31) < b.rows_left) {
-    store_row(row_out<float>(a.o, n, b.me.h), o, f, a.dh, hh);
-    if (hh == 0) a.lse[n * a.heads + b.me.h] = l == 0.f ? -INFINITY : m + log2f(l);
-  }
-  redo_rows(not_finite(o, f * 0.f), b.rows_left, [&](int j) {
-    const RowPlace p = place_of(a, b.x.hk, b.w0 + j);
-    one_forward<float>(a, s, p.i, p.h, lane);
-  });
 }
 
-template <int W>
-__global__ __launch_bounds__(64 * WAVES, W > 96 ? 1 : 2) void packed_dq_f32_kernel(PackedAttnArgs a) {
+template <int W, int COLS>
+__global__ __launch_bounds__(64 * WAVES, COLS > 1 || W > 96 ? 1 : 2) void packed_dq_f32_kernel(PackedAttnArgs a) {
   typedef Tiles<W> T;
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[2 * T::STAGE];
+  typedef RowBlock<W, COLS> RB;
+  typedef typename RB::PS PS;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[ring_bytes<W, COLS>()];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  RowBlock b;
-  if (!b.find(a, wave, lane)) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = COLS == 1 ? wave : 0, col = COLS == 1 ? 0 : wave;
+  RB b;
+  if (!b.find(a, rw, lane)) return;
   const Seq& s = b.x.s;
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
-  const PairStream<W> ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave, lane);
-  const float* k = row_of<float>(a.k, s.k0, b.x.hk);
-  const float* v = row_of<float>(a.v, s.k0, b.x.hk);
-  if (b.from < b.to) ps.issue(k, v, 32 * b.from, s.nk, b.from & 1, lane);
-  const long n = s.q0 + b.me.i;
+  const PS ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave);
+  auto ask = [&](int i, int at) __attribute__((always_inline)) { b.ask(ps, a, i, at, lane); };
+  if (b.from < b.to) ask(b.from, PS::NST == 1 ? 0 : b.from & 1);
+  const long n = s.q0 + b.me.i, r = n * a.heads + b.me.h;
+  float L = a.lse[r];
   float q[4 * T::J], g[4 * T::J], D = 0.f;
   {
     float o[4 * T::J];
@@ -246,168 +329,218 @@ __global__ __launch_bounds__(64 * WAVES, W > 96 ? 1 : 2) void packed_dq_f32_kern
     for (int i = 0; i < 4 * T::J; ++i) D = fmaf(g[i], o[i], D);
   }
   T::own(row_of<float>(a.q, n, b.me.h), a.dh, lane, q);
-  D += other_half(D);
-  float L = stat_of(a.lse[n * a.heads + b.me.h]);
   landed(L);
-  if (hh == 0 && b.share == 0 && lane < b.rows_left) {
-    a.dsum[n * a.heads + b.me.h] = -D;
-    a.nlse[n * a.heads + b.me.h] = -L;
+  D += other_half(D);
+  L = stat_of(L);
+  if (hh == 0 && col == 0 && b.share == 0 && lane < b.rows_left) {
+    a.dsum[r] = -D;
+    a.nlse[r] = -L;
   }
-  const unsigned ck = lds0 + T::cols_lane(lane), rk = lds0 + T::rows_lane(lane);
+  const unsigned ck = lds0 + T::cols_lane(lane) + (unsigned)col * T::G::TB, rk = lds0 + T::rows_lane(lane) + (unsigned)col * T::G::TB;
   const float c = a.scale * LOG2E;
   float16v dq[T::MB];
   zero_acc(dq);
   for (int i = b.from; i < b.to; ++i) {
-    copies_in_flight<0>();
-    workgroup_handover();
-    if (i + 1 < b.to) ps.issue(k, v, 32 * (i + 1), s.nk, (i + 1) & 1, lane);
-    if (32 * i >= b.most) continue;
-    const unsigned at = (unsigned)(i & 1) * T::STAGE;
+    const unsigned at = (unsigned)next_stage<PS::NST>(i, b.from, b.to, ask) * PS::STAGE;
+    const int first = RB::KEYS * i + 32 * col;
+    if (first >= b.most) continue;
     float16v sc[1], dp;
     zero_acc(sc);
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = -D;
     sc[0] = T::product(ck + at, 0, q, sc[0]);
-    dp = T::product(ck + at, T::G::TB, g, dp);
+    dp = T::product(ck + at, RB::NT * T::G::TB, g, dp);
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[0][e] = fast_exp2(fmaf(sc[0][e], c, -L)) * dp[e];
-    if (32 * i + 32 > b.fewest) {
+    if (first + 32 > b.fewest) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (32 * i + tile_row_of(e, hh) >= b.mine) sc[0][e] = 0.f;
+        if (first + tile_row_of(e, hh) >= b.mine) sc[0][e] = 0.f;
     }
     T::add(rk + at, 0, sc[0], dq);
   }
-  if (b.rows_left <= 0) return;
-  if (a.shares > 1) {
-    if ((lane & 31) < b.rows_left)
-      store_share<T::MB>(a.part, (long)b.share * a.q_rows * a.heads + n * a.heads + b.me.h, dq, 0, a.dh, hh);
-    return;
+  const bool there = (lane & 31) < b.rows_left;
+  auto leave = [&](auto& acc, int m0) __attribute__((always_inline)) {
+    constexpr int N = sizeof(acc) / sizeof(acc[0]);
+    if (a.shares > 1) {
+      if (there) store_share<N>(a.part, (long)b.share * a.q_rows * a.heads + r, acc, m0, a.dh, hh);
+      return;
+    }
+    if (there) store_row(row_out<float>(a.dq, n, b.me.h), acc, a.scale, m0, a.dh, hh);
+    redo_rows(not_finite(acc, 0.f), b.rows_left, [&](int j) {
+      const RowPlace p = place_of(a, b.x.hk, b.w0 + j);
+      one_dq<float>(a, s, p.i, p.h, row_dsum<float>(a, s.q0 + p.i, p.h, lane), lane);
+    });
+  };
+  if constexpr (COLS == 1) {
+    if (b.rows_left > 0) leave(dq, 0);
+  } else {
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(ring);
+    put_sums(sums, wave, dq, lane);
+    __syncthreads();
+    if (col >= T::MB) return;
+    const float f[WAVES] = {1.f, 1.f, 1.f, 1.f};
+    float16v acc[1];
+    get_sums<T::MB>(sums, col, f, acc, lane);
+    leave(acc, col);
   }
-  if ((lane & 31) < b.rows_left) store_row(row_out<float>(a.dq, n, b.me.h), dq, a.scale, a.dh, hh);
-  redo_rows(not_finite(dq, 0.f), b.rows_left, [&](int j) {
-    const RowPlace p = place_of(a, b.x.hk, b.w0 + j);
-    one_dq<float>(a, s, p.i, p.h, row_dsum<float>(a, s.q0 + p.i, p.h, lane), lane);
-  });
 }
 
-// Queries from the last tile down, all heads of the group for one tile before the next.
-template <int W>
-__global__ __launch_bounds__(64 * WAVES, W > 64 ? 1 : 2) void packed_dkdv_f32_kernel(PackedAttnArgs a) {
+// Queries from the last tile down, all heads of the group for one tile before the next.  TURNS = 1: 128 keys, 32 for each wavefront; 4, for
+// few keys: 32, and the wavefronts take every fourth tile of queries in turn.
+template <int W, int TURNS>
+__global__ __launch_bounds__(64 * WAVES, TURNS > 1 || W > 64 ? 1 : 2) void packed_dkdv_f32_kernel(PackedAttnArgs a) {
   typedef Tiles<W> T;
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[2 * T::STAGE];
-  __shared__ __attribute__((aligned(256))) float stats[2][2][64];                // [stage][-lse | -D][32 rows, and again]
+  typedef PairStream<W, TURNS> PS;
+  constexpr int NT = TURNS, KEYS = 32 * WAVES / TURNS;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[ring_bytes<W, TURNS>()];
+  __shared__ __attribute__((aligned(256))) float stats[PS::NST][NT][2][64];      // [stage][tile][-lse | -D][32 rows, and again]
   const int lane = threadIdx.x & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const Tile x = find_tile<true>(a, ROWS, lane);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), turn = TURNS == 1 ? 0 : wave, kw = TURNS == 1 ? wave : 0;
+  const Tile x = find_tile<true>(a, KEYS, lane);
   if (!x.exists) return;
   const Seq& s = x.s;
-  const int k0 = ROWS * x.t, w0 = k0 + 32 * wave, keys_left = s.nk - w0;
+  const int w0 = KEYS * x.t + 32 * kw, keys_left = s.nk - w0;
   const int nq = s.nq, shift = s.nk - nq;
   auto first_query = [&](int key) __attribute__((always_inline)) {
     const int i = key - shift;
     return !a.causal || i < 0 ? 0 : i;
   };
   const int top = (nq - 1) >> 5;
-  const int steps = nq > 0 ? (top + 1 - (first_query(k0) >> 5)) * a.group : 0, share = (int)blockIdx.y;
-  const int from = (int)((long)steps * share / a.shares), to = (int)((long)steps * (share + 1) / a.shares);
+  const int tiles = nq > 0 ? (top + 1 - (first_query(KEYS * x.t) >> 5)) * a.group : 0, all_steps = (tiles + NT - 1) / NT;
+  const int share = (int)blockIdx.y;
+  const int from = (int)((long)all_steps * share / a.shares), to = (int)((long)all_steps * (share + 1) / a.shares);
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const unsigned lds1 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(stats));
-  const PairStream<W> ps((unsigned)(a.q.row * 4), (unsigned)(a.dout.row * 4), a.dh, lds0, wave, lane);
-  int ih = from % a.group, iq = top - from / a.group;      // the next tile to ask for
-  auto ask = [&](int at) __attribute__((always_inline)) {
-    const int h = x.hk * a.group + ih, first = 32 * iq;
-    ps.issue(row_of<float>(a.q, s.q0, h), row_of<float>(a.dout, s.q0, h), first, nq, at, lane);
-    const int r = first + (lane & 31) < nq ? first + (lane & 31) : nq - 1;
-    copy4_to_lds((wave & 1 ? a.dsum : a.nlse) + (long)(s.q0 + r) * a.heads + h, lds1 + (unsigned)at * 512u + (unsigned)(wave & 1) * 256u);
-    if (++ih == a.group) { ih = 0; --iq; }
+  const PS ps((unsigned)(a.q.row * 4), (unsigned)(a.dout.row * 4), a.dh, lds0, wave);
+  // tile j of the list: its head of the group and its first query (past the list's end: one that nobody reads)
+  struct Place { int h, first; };
+  auto place = [&](int j) __attribute__((always_inline)) {
+    const int down = (int)a.by_group.quotient((unsigned)j);
+    return Place{x.hk * a.group + j - down * a.group, down > top ? 0 : 32 * (top - down)};
   };
+  auto ask = [&](int i, int at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < PS::TILES; ++u) {
+      const int t = ps.tile(u);
+      const Place p = place(NT * i + t % NT);
+      ps.issue(u, row_of<float>(t < NT ? a.q : a.dout, s.q0 + p.first, p.h), nq - p.first < 32 ? nq - p.first : 32, at, lane);
+    }
+    // (NT = 1: the wavefronts copy the same two)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int t = wave % NT;
+      const Place p = place(NT * i + t);
+      const int r = p.first + (lane & 31) < nq ? p.first + (lane & 31) : nq - 1;
+      copy4_to_lds((u ? a.dsum : a.nlse) + (long)(s.q0 + r) * a.heads + p.h, lds1 + (unsigned)at * (NT * 512u) + (unsigned)(2 * t + u) * 256u);
+    }
+  };
+  if (from < to) ask(from, PS::NST == 1 ? 0 : from & 1);
   const int key = keys_left > 0 ? w0 + ((lane & 31) < keys_left ? (lane & 31) : keys_left - 1) : s.nk - 1;
   float k[4 * T::J], v[4 * T::J];
   T::own(row_of<float>(a.k, s.k0 + key, x.hk), a.dh, lane, k);
   T::own(row_of<float>(a.v, s.k0 + key, x.hk), a.dh, lane, v);
-  const unsigned cq = lds0 + T::cols_lane(lane), rq = lds0 + T::rows_lane(lane);
+  const unsigned cq = lds0 + T::cols_lane(lane) + (unsigned)turn * T::G::TB, rq = lds0 + T::rows_lane(lane) + (unsigned)turn * T::G::TB;
   const int mine = first_query(key);
   const int begin = keys_left > 0 ? first_query(w0) : nq, all = keys_left > 0 ? first_query(w0 + (keys_left < 32 ? keys_left : 32) - 1) : nq;
   const float c = a.scale * LOG2E;
   float16v dk[T::MB], dv[T::MB];
   zero_acc(dk);
   zero_acc(dv);
-  int sh = ih, first = 32 * iq;
-  if (from < to) ask(from & 1);
   for (int i = from; i < to; ++i) {
-    copies_in_flight<0>();
-    workgroup_handover();
-    if (i + 1 < to) ask((i + 1) & 1);
-    if (first + 32 > begin && keys_left > 0) {
-      const unsigned at = (unsigned)(i & 1) * T::STAGE;
-      float16v sc[1], dp;
-      zero_acc(sc);
+    const int st = next_stage<PS::NST>(i, from, to, ask);
+    const int j = NT * i + turn, first = place(j).first;
+    if (j >= tiles || first + 32 <= begin || keys_left <= 0) continue;
+    const unsigned at = (unsigned)st * PS::STAGE;
+    float16v sc[1], dp;
+    zero_acc(sc);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 u = *reinterpret_cast<const float4*>(&stats[i & 1][1][8 * g + 4 * hh]);
-        dp[4 * g] = u.x; dp[4 * g + 1] = u.y; dp[4 * g + 2] = u.z; dp[4 * g + 3] = u.w;
-      }
-      sc[0] = T::product(cq + at, 0, k, sc[0]);
-      dp = T::product(cq + at, T::G::TB, v, dp);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 u = *reinterpret_cast<const float4*>(&stats[i & 1][0][8 * g + 4 * hh]);
-        sc[0][4 * g] = fast_exp2(fmaf(sc[0][4 * g], c, u.x));
-        sc[0][4 * g + 1] = fast_exp2(fmaf(sc[0][4 * g + 1], c, u.y));
-        sc[0][4 * g + 2] = fast_exp2(fmaf(sc[0][4 * g + 2], c, u.z));
-        sc[0][4 * g + 3] = fast_exp2(fmaf(sc[0][4 * g + 3], c, u.w));
-      }
-      if (first < all || first + 32 > nq) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int r = first + tile_row_of(e, hh);
-          if (r < mine || r >= nq) sc[0][e] = 0.f;
-        }
-      }
-      T::add(rq + at, T::G::TB, sc[0], dv);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[0][e] *= dp[e];
-      T::add(rq + at, 0, sc[0], dk);
+    for (int g = 0; g < 4; ++g) {
+      const float4 u = *reinterpret_cast<const float4*>(&stats[st][turn][1][8 * g + 4 * hh]);
+      dp[4 * g] = u.x; dp[4 * g + 1] = u.y; dp[4 * g + 2] = u.z; dp[4 * g + 3] = u.w;
     }
-    if (++sh == a.group) { sh = 0; first -= 32; }
-  }
-  if (keys_left <= 0) return;
-  if (a.shares > 1) {
-    const long r = (long)(s.k0 + key) * a.kv_heads + x.hk, rows = (long)a.k_rows * a.kv_heads;
-    if ((lane & 31) < keys_left) {
-      store_share<T::MB>(a.part, share * rows + r, dk, 0, a.dh, hh);
-      store_share<T::MB>(a.part, (a.shares + share) * rows + r, dv, 0, a.dh, hh);
+    sc[0] = T::product(cq + at, 0, k, sc[0]);
+    dp = T::product(cq + at, NT * T::G::TB, v, dp);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float4 u = *reinterpret_cast<const float4*>(&stats[st][turn][0][8 * g + 4 * hh]);
+      sc[0][4 * g] = fast_exp2(fmaf(sc[0][4 * g], c, u.x));
+      sc[0][4 * g + 1] = fast_exp2(fmaf(sc[0][4 * g + 1], c, u.y));
+      sc[0][4 * g + 2] = fast_exp2(fmaf(sc[0][4 * g + 2], c, u.z));
+      sc[0][4 * g + 3] = fast_exp2(fmaf(sc[0][4 * g + 3], c, u.w));
     }
-    return;
+    if (first < all || first + 32 > nq) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int r = first + tile_row_of(e, hh);
+        if (r < mine || r >= nq) sc[0][e] = 0.f;
+      }
+    }
+    T::add(rq + at, NT * T::G::TB, sc[0], dv);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[0][e] *= dp[e];
+    T::add(rq + at, 0, sc[0], dk);
   }
-  if ((lane & 31) < keys_left) {
-    store_row(row_out<float>(a.dk, s.k0 + key, x.hk), dk, a.scale, a.dh, hh);
-    store_row(row_out<float>(a.dv, s.k0 + key, x.hk), dv, 1.f, a.dh, hh);
+  const bool there = (lane & 31) < keys_left;
+  const long r = (long)(s.k0 + key) * a.kv_heads + x.hk, rows = (long)a.k_rows * a.kv_heads;
+  auto leave = [&](auto& k_sum, auto& v_sum, int m0) __attribute__((always_inline)) {
+    constexpr int N = sizeof(k_sum) / sizeof(k_sum[0]);
+    if (a.shares > 1) {
+      if (there) {
+        store_share<N>(a.part, share * rows + r, k_sum, m0, a.dh, hh);
+        store_share<N>(a.part, (a.shares + share) * rows + r, v_sum, m0, a.dh, hh);
+      }
+      return;
+    }
+    if (there) {
+      store_row(row_out<float>(a.dk, s.k0 + key, x.hk), k_sum, a.scale, m0, a.dh, hh);
+      store_row(row_out<float>(a.dv, s.k0 + key, x.hk), v_sum, 1.f, m0, a.dh, hh);
+    }
+    redo_rows(not_finite(v_sum, not_finite(k_sum, 0.f)), keys_left, [&](int j) { one_dkdv<float>(a, s, w0 + j, x.hk, lane); });
+  };
+  if constexpr (TURNS == 1) {
+    if (keys_left > 0) leave(dk, dv, 0);
+  } else {
+    float* const sums = reinterpret_cast<float*>(ring);
+    const float f[WAVES] = {1.f, 1.f, 1.f, 1.f};
+    float16v k_sum[1], v_sum[1];
+    __syncthreads();
+    put_sums(sums, wave, dk, lane);
+    __syncthreads();
+    if (wave < T::MB) get_sums<T::MB>(sums, wave, f, k_sum, lane);
+    __syncthreads();
+    put_sums(sums, wave, dv, lane);
+    __syncthreads();
+    if (wave >= T::MB) return;
+    get_sums<T::MB>(sums, wave, f, v_sum, lane);
+    leave(k_sum, v_sum, wave);
   }
-  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<float>(a, s, w0 + j, x.hk, lane); });
 }
 
 }  // namespace
 
 hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s) {
-  const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
   return with_width(a.dh, [&](auto w) {
-    packed_fwd_f32_kernel<decltype(w)::value><<<grid, 64 * WAVES, 0, s>>>(a);
+    constexpr int W = decltype(w)::value;
+    if (f32_wide<false>(a)) packed_fwd_f32_kernel<W, 1><<<dim3(tile_grid<false>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
+    else packed_fwd_f32_kernel<W, 4><<<dim3(tile_grid<false>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s) {
-  const dim3 grid(tile_grid<false>(a, ROWS), a.shares);
   return with_width(a.dh, [&](auto w) {
-    packed_dq_f32_kernel<decltype(w)::value><<<grid, 64 * WAVES, 0, s>>>(a);
+    constexpr int W = decltype(w)::value;
+    if (f32_wide<false>(a)) packed_dq_f32_kernel<W, 1><<<dim3(tile_grid<false>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
+    else packed_dq_f32_kernel<W, 4><<<dim3(tile_grid<false>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s) {
-  const dim3 grid(tile_grid<true>(a, ROWS), a.shares);
   return with_width(a.dh, [&](auto w) {
-    packed_dkdv_f32_kernel<decltype(w)::value><<<grid, 64 * WAVES, 0, s>>>(a);
+    constexpr int W = decltype(w)::value;
+    if (f32_wide<true>(a)) packed_dkdv_f32_kernel<W, 1><<<dim3(tile_grid<true>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
+    else packed_dkdv_f32_kernel<W, 4><<<dim3(tile_grid<true>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
     return hipGetLastError();
   });
 }
