@@ -225,9 +225,8 @@ __device__ __forceinline__ int wave_total(int v) {
 struct Tile { int hk, t; Seq s; bool exists; };
 __device__ __forceinline__ int tiles_in(int len, int per) { return (int)((unsigned)(len + per - 1) / (unsigned)per); }   // (per: a power of two)
 template <bool KEYS>
-__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane) {
+__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane, unsigned id = blockIdx.x) {
   Tile x;
-  const unsigned id = blockIdx.x;
   int j = (int)a.by_kv.quotient(id);
   x.hk = (int)id - j * a.kv_heads;
   const int* off = KEYS ? a.k_off : a.q_off;

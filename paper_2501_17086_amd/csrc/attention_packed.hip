@@ -701,10 +701,368 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, lane); });
 }
 
+// ------------------------------------------------------------------------------------------------------------
+// many short sequences: every wavefront by itself
+// ------------------------------------------------------------------------------------------------------------
+// With a few tiles on the other side, a workgroup spends its time starting, meeting and leaving, and most sequences do not fill it.
+// Here each of its eight wavefronts has 32 rows (keys) of any sequence, a ring of its own and no barrier at all.  The other
+// side's tiles then come to LDS once for every 32 rows instead of every 256: a short sequence's are in the L2.
+template <int W>
+struct Alone {
+  static constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
+  static constexpr int NST = DHP == 64 ? 2 : 1, STAGE = 2 * G::TB, COPIES = 2 * G::COPIES;
+  unsigned ldx, ldy, off[DHP == 64 ? COPIES : 1];          // (64 channels: offsets of whole tiles, kept)
+  int dh8;
+  __device__ __forceinline__ Alone(unsigned ldx_, unsigned ldy_, int dh8_, int lane) : ldx(ldx_), ldy(ldy_), dh8(dh8_) {
+    if (DHP == 64) {
+#pragma unroll
+      for (int u = 0; u < COPIES; ++u) off[u] = copy_offset<DHP>(u < G::COPIES ? ldx : ldy, u % G::COPIES, 32, dh8, lane);
+    }
+  }
+  // tiles x and y, rows `first` .. of n, into the stage at `lds`
+  __device__ __forceinline__ void issue(const unsigned char* x, const unsigned char* y, int first, int n, unsigned lds, int lane) const {
+    x += (long)first * ldx;
+    y += (long)first * ldy;
+    if (DHP == 64 && first + 32 <= n) {
+#pragma unroll
+      for (int u = 0; u < COPIES; ++u) copy16_to_lds(off[u], u < G::COPIES ? x : y, lds + 1024u * u);
+    } else {
+      copy_tile<DHP>(x, ldx, n - first, dh8, lds, lane);
+      copy_tile<DHP>(y, ldy, n - first, dh8, lds + G::TB, lane);
+    }
+  }
+};
+// The stage of step i, full; ask(step, stage) issues copies.
+template <int W, typename F>
+__device__ __forceinline__ int stage_alone(int i, int steps, F ask) {
+  typedef Alone<W> A;
+  if (A::NST == 1) {
+    if (i > 0) {
+      copies_in_flight_read<0>();                          // (what was read of the step before has arrived)
+      ask(i, 0);
+    }
+    copies_in_flight_read<0>();
+    return 0;
+  }
+  copies_in_flight_read<0>();                              // (step i has arrived, what was read of the step before as well)
+  if (i + 1 < steps) ask(i + 1, (i + 1) & 1);
+  return i & 1;
+}
+
+// this wavefront's rows and the keys that they see
+struct OwnRows {
+  Tile x;
+  int w0, rows_left, mine, fewest, most;
+  RowPlace me;
+  __device__ __forceinline__ bool find(const PackedAttnArgs& a, unsigned id, int lane) {
+    x = find_tile<false>(a, 32, lane, id);
+    if (!x.exists) return false;
+    const int R = x.s.nq * a.group;
+    w0 = 32 * x.t;
+    rows_left = R - w0;
+    auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(x.s, place_of(a, x.hk, r).i, a.causal); };
+    me = place_of(a, x.hk, (lane & 31) < rows_left ? w0 + (lane & 31) : R - 1);
+    mine = seen_by(x.s, me.i, a.causal);
+    fewest = seen(w0);
+    most = seen(w0 + (rows_left < 32 ? rows_left : 32) - 1);
+    return true;
+  }
+};
+
+template <int W>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_short_kernel(PackedAttnArgs a) {
+  constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
+  typedef Alone<W> A;
+  __shared__ __attribute__((aligned(1024))) unsigned char rings[WAVES * A::NST * A::STAGE];
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  OwnRows b;
+  if (!b.find(a, blockIdx.x * WAVES + wave, lane)) return;
+  const Seq& sq = b.x.s;
+  const int dh8 = a.dh >> 3, steps = (b.most + 31) >> 5;
+  unsigned char* const ring = rings + wave * (A::NST * A::STAGE);
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const unsigned char* k = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.k, sq.k0, b.x.hk));
+  const unsigned char* v = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.v, sq.k0, b.x.hk));
+  const A ring_of((unsigned)(a.k.row * 2), (unsigned)(a.v.row * 2), dh8, lane);
+  auto ask = [&](int i, int at) __attribute__((always_inline)) {
+    ring_of.issue(k, v, 32 * i, sq.nk, lds0 + (unsigned)at * A::STAGE, lane);
+  };
+  if (steps > 0) ask(0, 0);
+  const long n = sq.q0 + b.me.i;
+  const bf16_t* qrow = row_of<bf16_t>(a.q, n, b.me.h);
+  bf16x8 fq[G::KK];
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) fq[kk] = own_piece(qrow, kk, dh8, lane);
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) landed(fq[kk]);
+  const float c = a.scale * LOG2E;
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rv = lds0 + Frags<DHP>::rows_lane(lane);
+  float16v o[G::MB];
+  zero_acc(o);
+  float m = -FLT_MAX, l = 0.f;
+  auto walk = [&](auto few) __attribute__((always_inline)) {
+    for (int i = 0; i < steps; ++i) {
+      const unsigned at = (unsigned)stage_alone<W>(i, steps, ask) * A::STAGE;
+      float16v s[1];
+      zero_acc(s);
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) s[0] = mfma(Frags<DHP>::cols(ck + at, 0, kk), fq[kk], s[0]);
+      if (32 * i + 32 > b.fewest) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (32 * i + tile_row_of(e, hh) >= b.mine) s[0][e] = -INFINITY;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[0][e]);
+      top = max_of_halves(top) * c;
+      if (__any(top > m + 8.f)) {
+        const float mn = fmaxf(m, top), alpha = fast_exp2(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < G::MB; ++mb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[mb][e] *= alpha;
+      }
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = fast_exp2(fmaf(s[0][e], c, -m));
+        l += p[e];
+      }
+      const Operand<decltype(few)::value> op(p);
+      op.template times<DHP>(rv + at, G::TB, o);
+    }
+  };
+  if (sq.nk <= FEW) walk(std::true_type());
+  else walk(std::false_type());
+  l += other_half(l);
+  copies_in_flight_read<0>();                              // (the ring is free: results leave through it)
+  const float f = l == 0.f ? 0.f : 1.f / l;
+  store_rows([&](int j) __attribute__((always_inline)) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    return row_out<bf16_t>(a.o, sq.q0 + q.i, q.h);
+  }, b.rows_left, o, f, 0, a.dh, ring, lane);
+  if (lane < 32 && lane < b.rows_left) a.lse[n * a.heads + b.me.h] = l == 0.f ? -INFINITY : m + log2f(l);
+  redo_rows(not_finite(o, f * 0.f), b.rows_left, [&](int j) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    one_forward<bf16_t>(a, sq, q.i, q.h, lane);
+  });
+}
+
+template <int W>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_short_kernel(PackedAttnArgs a) {
+  constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
+  typedef Alone<W> A;
+  __shared__ __attribute__((aligned(1024))) unsigned char rings[WAVES * A::NST * A::STAGE];
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  OwnRows b;
+  if (!b.find(a, blockIdx.x * WAVES + wave, lane)) return;
+  const Seq& sq = b.x.s;
+  const int dh8 = a.dh >> 3, steps = (b.most + 31) >> 5;
+  unsigned char* const ring = rings + wave * (A::NST * A::STAGE);
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const unsigned char* k = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.k, sq.k0, b.x.hk));
+  const unsigned char* v = reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.v, sq.k0, b.x.hk));
+  const A ring_of((unsigned)(a.k.row * 2), (unsigned)(a.v.row * 2), dh8, lane);
+  auto ask = [&](int i, int at) __attribute__((always_inline)) {
+    ring_of.issue(k, v, 32 * i, sq.nk, lds0 + (unsigned)at * A::STAGE, lane);
+  };
+  if (steps > 0) ask(0, 0);
+  const long n = sq.q0 + b.me.i, r = n * a.heads + b.me.h;
+  const bf16_t* qrow = row_of<bf16_t>(a.q, n, b.me.h);
+  const bf16_t* grow = row_of<bf16_t>(a.dout, n, b.me.h);
+  const bf16_t* orow = row_of<bf16_t>(a.o, n, b.me.h);
+  float L = a.lse[r], D = 0.f;
+  bf16x8 fq[G::KK], fg[G::KK];
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) {
+    fq[kk] = own_piece(qrow, kk, dh8, lane);
+    fg[kk] = own_piece(grow, kk, dh8, lane);
+    D += dot8(fg[kk], own_piece(orow, kk, dh8, lane));
+  }
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) { landed(fq[kk]); landed(fg[kk]); }
+  landed(L);
+  D += other_half(D);
+  L = stat_of(L);
+  if (lane < 32 && lane < b.rows_left) {
+    a.dsum[r] = -D;
+    a.nlse[r] = -L;
+  }
+  const float c = a.scale * LOG2E;
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rk = lds0 + Frags<DHP>::rows_lane(lane);
+  float16v dq[G::MB];
+  zero_acc(dq);
+  auto walk = [&](auto few) __attribute__((always_inline)) {
+    for (int i = 0; i < steps; ++i) {
+      const unsigned at = (unsigned)stage_alone<W>(i, steps, ask) * A::STAGE;
+      float16v s[1], dp;
+      zero_acc(s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[e] = -D;
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) {
+        s[0] = mfma(Frags<DHP>::cols(ck + at, 0, kk), fq[kk], s[0]);
+        dp = mfma(Frags<DHP>::cols(ck + at, G::TB, kk), fg[kk], dp);
+      }
+      float ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ds[e] = fast_exp2(fmaf(s[0][e], c, -L)) * dp[e];
+      if (32 * i + 32 > b.fewest) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (32 * i + tile_row_of(e, hh) >= b.mine) ds[e] = 0.f;
+      }
+      const Operand<decltype(few)::value> op(ds);
+      op.template times<DHP>(rk + at, 0, dq);
+    }
+  };
+  if (sq.nk <= FEW) walk(std::true_type());
+  else walk(std::false_type());
+  copies_in_flight_read<0>();
+  store_rows([&](int j) __attribute__((always_inline)) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    return row_out<bf16_t>(a.dq, sq.q0 + q.i, q.h);
+  }, b.rows_left, dq, a.scale, 0, a.dh, ring, lane);
+  redo_rows(not_finite(dq, 0.f), b.rows_left, [&](int j) {
+    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+    one_dq<bf16_t>(a, sq, q.i, q.h, row_dsum<bf16_t>(a, sq.q0 + q.i, q.h, lane), lane);
+  });
+}
+
+template <int W>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_short_kernel(PackedAttnArgs a) {
+  constexpr int DHP = padded<W>();
+  constexpr bool KLDS = DHP == 128;                        // (see packed_dkdv_mfma_kernel)
+  typedef Fit<W> G;
+  typedef Alone<W> A;
+  constexpr int STATS = A::NST * A::STAGE, KEEP = STATS + A::NST * 512, OWN = KEEP + (KLDS ? G::TB : 0);
+  constexpr int NW = DHP == 128 ? 4 : WAVES;               // wavefronts: what fits the LDS
+  __shared__ __attribute__((aligned(1024))) unsigned char rings[NW * OWN];
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const Tile x = find_tile<true>(a, 32, lane, blockIdx.x * NW + wave);
+  if (!x.exists) return;
+  const Seq& sq = x.s;
+  const int w0 = 32 * x.t, keys_left = sq.nk - w0, nq = sq.nq, shift = sq.nk - nq, dh8 = a.dh >> 3;
+  auto first_query = [&](int key) __attribute__((always_inline)) {
+    const int i = key - shift;
+    return !a.causal || i < 0 ? 0 : i;
+  };
+  unsigned char* const ring = rings + wave * OWN;
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const int begin = first_query(w0) & ~31, each = (nq - begin + 31) >> 5, steps = nq > 0 ? each * a.group : 0;
+  const A ring_of((unsigned)(a.q.row * 2), (unsigned)(a.dout.row * 2), dh8, lane);
+  int ih = x.hk * a.group, iq = begin;                     // the next step to ask for
+  auto ask = [&](int, int at) __attribute__((always_inline)) {
+    ring_of.issue(reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.q, sq.q0, ih)),
+                  reinterpret_cast<const unsigned char*>(row_of<bf16_t>(a.dout, sq.q0, ih)), iq, nq, lds0 + (unsigned)at * A::STAGE, lane);
+    const long r = (long)(sq.q0 + (iq + (lane & 31) < nq ? iq + (lane & 31) : nq - 1)) * a.heads + ih;
+    copy4_to_lds(a.nlse + r, lds0 + STATS + (unsigned)at * 512u);
+    copy4_to_lds(a.dsum + r, lds0 + STATS + (unsigned)at * 512u + 256u);
+    iq += 32;
+    if (iq >= nq) { iq = begin; ++ih; }
+  };
+  if (steps > 0) ask(0, 0);
+  const int key = (lane & 31) < keys_left ? w0 + (lane & 31) : sq.nk - 1;
+  const bf16_t* krow = row_of<bf16_t>(a.k, sq.k0 + key, x.hk);
+  const bf16_t* vrow = row_of<bf16_t>(a.v, sq.k0 + key, x.hk);
+  bf16x8 fk[G::KK], fv[G::KK];
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) { fk[kk] = own_piece(krow, kk, dh8, lane); fv[kk] = own_piece(vrow, kk, dh8, lane); }
+#pragma unroll
+  for (int kk = 0; kk < G::KK; ++kk) {
+    landed(fk[kk]);
+    landed(fv[kk]);
+    if (KLDS) put_cols_lds<DHP>(ring + KEEP, kk, lane, fk[kk]);
+  }
+  const int mine = first_query(key), all = first_query(w0 + (keys_left < 32 ? keys_left : 32) - 1);
+  const float c = a.scale * LOG2E;
+  const unsigned cl = Frags<DHP>::cols_lane(lane), cq = lds0 + cl, rq = lds0 + Frags<DHP>::rows_lane(lane), kl = lds0 + KEEP + cl;
+  float16v dk[G::MB], dv[G::MB];
+  zero_acc(dk);
+  zero_acc(dv);
+  auto walk = [&](auto few) __attribute__((always_inline)) {
+    int first = begin;
+    for (int i = 0; i < steps; ++i) {
+      const int st = stage_alone<W>(i, steps, ask);
+      const unsigned at = (unsigned)st * A::STAGE;
+      const float* stat = reinterpret_cast<const float*>(ring + STATS + st * 512);
+      float16v s[1], dp;
+      float p[16];
+      zero_acc(s);
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) s[0] = mfma(Frags<DHP>::cols(cq + at, 0, kk), KLDS ? Frags<DHP>::cols(kl, 0, kk) : fk[kk], s[0]);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 u = *reinterpret_cast<const float4*>(stat + 64 + 8 * g + 4 * hh);
+        dp[4 * g] = u.x; dp[4 * g + 1] = u.y; dp[4 * g + 2] = u.z; dp[4 * g + 3] = u.w;
+      }
+#pragma unroll
+      for (int kk = 0; kk < G::KK; ++kk) dp = mfma(Frags<DHP>::cols(cq + at, G::TB, kk), fv[kk], dp);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 u = *reinterpret_cast<const float4*>(stat + 8 * g + 4 * hh);
+        p[4 * g] = fast_exp2(fmaf(s[0][4 * g], c, u.x));
+        p[4 * g + 1] = fast_exp2(fmaf(s[0][4 * g + 1], c, u.y));
+        p[4 * g + 2] = fast_exp2(fmaf(s[0][4 * g + 2], c, u.z));
+        p[4 * g + 3] = fast_exp2(fmaf(s[0][4 * g + 3], c, u.w));
+      }
+      if (first < all || first + 32 > nq) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int q = first + tile_row_of(e, hh);
+          if (q < mine || q >= nq) p[e] = 0.f;
+        }
+      }
+      const Operand<decltype(few)::value> op(p);
+      op.template times<DHP>(rq + at, G::TB, dv);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[e] *= dp[e];
+      const Operand<decltype(few)::value> ds(p);
+      ds.template times<DHP>(rq + at, 0, dk);
+      first += 32;
+      if (first >= nq) first = begin;
+    }
+  };
+  if (nq <= FEW) walk(std::true_type());
+  else walk(std::false_type());
+  copies_in_flight_read<0>();
+  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, sq.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale, 0,
+             a.dh, ring, lane);
+  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, sq.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, 0,
+             a.dh, ring, lane);
+  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, sq, w0 + j, x.hk, lane); });
+}
+
+// Wavefronts by themselves: many, and with little to stream each.  Per sequence 256 of the other side's rows; 1024 where there are enough
+// wavefronts for all places (dk, dv), or where a sequence has one tile of rows, of which a workgroup's other wavefronts would have
+// nothing.  Shared / alone, us: forward and backward of 256 sequences of 64, 12 heads of 64, 62 / 26 and 188 / 72; backward of 32 of
+// 128 38 / 25, of 128 of 256, 4 heads, 86 / 55; 32 of 256, 32 heads of 128 on 8, 253 / 218; one token over 512 keys, 256
+// sequences, 32 heads of 128 on 8, 118 / 94.  The other way round: dk, dv of 128 sequences of 256, 4 heads on 1 (1024 wavefronts, 32
+// steps each), the whole backward pass 56 / 63; of 32 of 512, 16 heads of 64 on 4, 131 / 141.
+template <bool KEYS>
+bool alone(const PackedAttnArgs& a) {
+  const long rows = KEYS ? (long)a.k_rows : (long)a.q_rows * a.group;
+  const long other = KEYS ? (long)a.q_rows * a.group / a.seqs : a.k_rows / a.seqs;
+  const long waves = (rows / 32 + a.seqs) * a.kv_heads;
+  if (waves < 4 * (long)CUS) return false;
+  return other <= 256 || (other <= 1024 && (KEYS ? waves >= 8 * (long)CUS : rows / a.seqs <= 32));
+}
+
 // 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64
 template <int W>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  if (wide_blocks<false>(a, 256, 64, CUS))
+  if (alone<false>(a))
+    packed_fwd_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
+  else if (wide_blocks<false>(a, 256, 64, CUS))
     packed_fwd_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
   else
     packed_fwd_mfma_kernel<W, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
@@ -712,7 +1070,9 @@ hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
 }
 template <int W>
 hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  if (wide_blocks<false>(a, 256, 64, CUS))
+  if (alone<false>(a))
+    packed_dq_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
+  else if (wide_blocks<false>(a, 256, 64, CUS))
     packed_dq_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
   else
     packed_dq_mfma_kernel<W, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
@@ -720,7 +1080,9 @@ hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
 }
 template <int W>
 hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
-  if (wide_blocks<true>(a, 128, 64, CUS))
+  if (alone<true>(a))
+    packed_dkdv_short_kernel<W><<<(tile_grid<true>(a, 32) + (W > 64 ? 4 : WAVES) - 1) / (W > 64 ? 4 : WAVES), 64 * (W > 64 ? 4 : WAVES), 0, s>>>(a);
+  else if (wide_blocks<true>(a, 128, 64, CUS))
     packed_dkdv_mfma_kernel<W, 2><<<tile_grid<true>(a, 128), 64 * WAVES, 0, s>>>(a);
   else
     packed_dkdv_mfma_kernel<W, 4><<<dim3(tile_grid<true>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
@@ -746,8 +1108,8 @@ Shares shares(int dtype, const PackedAttnArgs& a) {
   const long rows = f32 ? (wide_r ? 128 : 32) : 64, keys = f32 ? (wide_k ? 128 : 32) : 64;
   const long key_step = f32 && wide_r ? 32 : 128, query_step = f32 && wide_k ? 32 : 128;
   const long row_blocks = ((long)a.q_rows * a.group / rows + a.seqs) * a.kv_heads, key_blocks = ((long)a.k_rows / keys + a.seqs) * a.kv_heads;
-  return {!f32 && wide_r ? 1 : shares_of(dtype, row_blocks, nk / key_step),
-          !f32 && wide_k ? 1 : shares_of(dtype, key_blocks, (nq + 31) / 32 * 32 * a.group / query_step)};
+  return {!f32 && (wide_r || alone<false>(a)) ? 1 : shares_of(dtype, row_blocks, nk / key_step),
+          !f32 && (wide_k || alone<true>(a)) ? 1 : shares_of(dtype, key_blocks, (nq + 31) / 32 * 32 * a.group / query_step)};
 }
 
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }

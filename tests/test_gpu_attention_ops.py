@@ -412,3 +412,49 @@ def test_a_stream_given_by_its_handle():
     s.synchronize()
     B.hbp_rotary(B.make_rotary(64), x, z)
     assert torch.equal(y, z)
+
+
+# Every form of the kernels by its sizes: wavefronts by themselves, workgroups of many rows, of few, shares (both sides), ragged or not.
+FORMS = [([60 + i % 9 for i in range(60)], None, 8, 8), ([3, 0, 64, 65, 1, 100, 33] * 20, None, 8, 4), ([256] * 20, None, 16, 8),
+         ([1] * 150, [200 + i % 100 for i in range(150)], 8, 8), ([1] * 40, [1000] * 40, 32, 32), ([1500, 900], None, 16, 2),
+         ([700] * 12, None, 12, 6), ([2000], None, 4, 1), ([5], [6000], 8, 8), ([900], [40], 8, 8), ([40, 2], [3000, 100], 4, 4),
+         ([64] * 70, None, 8, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("lq,lk,H,K", FORMS, ids=[f"{len(f[0])}x{f[0][0]}" for f in FORMS])
+def test_attention_forms(lq, lk, H, K, dh, dtype):
+    lk = lq if lk is None else lk
+    if len(lq) * max(lq) * max(lk) * H * dh > 3e10:        # (the reference's time)
+        H, K = H // K, 1
+    q, k, v, do = problem(lq, lk, H, K, dh, dtype, 73)
+    for causal in (True, False):
+        check_attention(q, k, v, lq, lk, causal, do)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H,K", [([64] * 70, 8, 8), ([600] * 2, 4, 4), ([1030], 4, 2)])
+def test_infinities_in_every_form(lens, H, K, dtype):
+    """A bad value at the last key of the first sequence: its earlier queries, and every other sequence, are as without it."""
+    q, k, v, do = problem(lens, lens, H, K, 64, dtype, 79)
+    clean = check_attention(q, k, v, lens, lens, True, do)
+    n = lens[0]
+    bad = v.clone()
+    bad[n - 1, :, 5] = math.nan
+    a = B.make_attention(q, k, bad, q_offsets=clean.q_offsets, k_offsets=clean.k_offsets)
+    B.hbp_attention_forward(a)
+    B.hbp_attention_backward(a, do)
+    seen = torch.zeros(sum(lens), dtype=torch.bool, device="cuda")
+    seen[n - 1] = True
+    for name in ("o", "dq"):
+        assert torch.isfinite(getattr(a, name)[~seen]).all(), name
+        assert not torch.isfinite(getattr(a, name)[seen]).all(), name
+    ref = R.Packed(q, k, v, lens, lens, True)
+    o, lse, eo, el = ref.forward()
+    R.assert_within(a.lse, lse, el, "lse")
+    R.assert_within(a.o[~seen], o[~seen], eo[~seen], "o")
+    dq, dk, dv, eq, ek, ev = ref.backward(clean.o, clean.lse, do)
+    R.assert_within(a.dq[~seen], dq[~seen], 2 * eq[~seen], "dq")
+    R.assert_within(a.dv, dv, ev, "dv")                    # (a value does not enter dv)
+    R.assert_within(a.dk[n:], dk[n:], 2 * ek[n:], "dk")
