@@ -363,7 +363,7 @@ hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, in
  * A query that sees no key, or whose scores are all minus infinity, has o = 0 and lse = minus infinity.  Sequences may
  * be empty on either side.  Rows behind the last sequence (and before the first) are left as they were.
  * bf16 storage: probabilities are rounded to bf16 before they meet v (and, in the backward pass, do and k, q), sums
- * are fp32.  Infinities and NaNs reach only the rows that see them. */
+ * are fp32.  Infinities and NaNs reach only the rows that see them.  Outputs overlap neither each other nor an input. */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(hbp_attention_desc) */
   int32_t dtype;             /* hbp_dtype */
@@ -395,6 +395,7 @@ hbp_status hbp_attention_workspace_size(const hbp_attention_desc* desc, size_t* 
 hbp_status hbp_attention_forward(const hbp_attention_desc* desc, const hbp_attention_buffers* bufs, void* stream);
 /* Rebuilds the probabilities from q, k and lse: P = 2^(s log2 e - lse), D = sum_c dout (.) o, dS = P (.) (dout v^T - D),
  *   dq = scale dS k,   dk = scale sum dS^T q,   dv = sum P^T dout   (dk, dv: over the query heads that share the key head).
+ * (P is as exact as lse, an fp32 number: where scores pass 2^20 its steps show in the gradients.)
  * Reads q, k, v, o, lse, dout; writes dq, dk, dv (keys that nothing sees: zeros).  Sums are taken in a fixed order: results are
  * bitwise repeatable. */
 hbp_status hbp_attention_backward(const hbp_attention_desc* desc, const hbp_attention_buffers* bufs, void* stream);

@@ -76,11 +76,19 @@ struct TwoColumns {
         if (lane + 64 * u < dh) v[u] = fmaf(wj, Elem<T>::load(rows + j * ld + lane + 64 * u), v[u]);
     }
   }
+  // channels c0 .. c1 - 1 of the row at `out`
   template <typename T>
-  __device__ __forceinline__ void store(T* out, float f, int dh, int lane) const {
+  __device__ __forceinline__ void store(T* out, float f, int c0, int c1, int lane) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      if (lane + 64 * u < dh) Elem<T>::store(out + lane + 64 * u, v[u] * f);
+      if (lane + 64 * u >= c0 && lane + 64 * u < c1) Elem<T>::store(out + lane + 64 * u, v[u] * f);
+  }
+  // NaN throughout: nothing that is added changes that
+  __device__ __forceinline__ bool settled(int dh, int lane) const {
+    bool nan = true;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) nan = nan && (lane + 64 * u >= dh || v[u] != v[u]);
+    return __all(nan);
   }
 };
 
@@ -92,10 +100,13 @@ __device__ __forceinline__ int seen_by(const Seq& s, int i, int causal) {
 }
 
 // ------------------------------------------------------------------------------------------------------------
-// term by term: one wavefront per (query, head), one per (key, key head)
+// term by term: one wavefront per (query, head), one per (key, key head), which leaves channels c0 .. c1 - 1 (and the statistic with c0 = 0)
 // ------------------------------------------------------------------------------------------------------------
+// Scores past 2^31 come here as well: there the rounding of the running maximum, which the kernels' fused multiply-add does not share,
+// may take every weight of a row to 0 (or infinity).  So no contraction here: the largest score less itself is 0.
 template <typename T>
-__device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& s, int i, int h, int lane) {
+__device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& s, int i, int h, int c0, int c1, int lane) {
+#pragma clang fp contract(off)
   const int hk = h / a.group, seen = seen_by(s, i, a.causal);
   const T* q = row_of<T>(a.q, s.q0 + i, h);
   const T* k = row_of<T>(a.k, s.k0, hk);
@@ -105,6 +116,7 @@ __device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& 
   for (int j = lane; j < seen; j += 64) {
     const float x = c * dot_rows(q, k + j * a.k.row, a.dh);
     m = x > m || x != x ? x : m;                           // (a NaN stays)
+    if (m != m) break;
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -120,12 +132,13 @@ __device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& 
       sum += p;
     }
     out.add(p, seen - j0 < 64 ? seen - j0 : 64, v + j0 * a.v.row, a.v.row, a.dh, lane);
+    if (m != m && out.settled(a.dh, lane)) break;
   }
   sum = wave_sum(sum);
   const bool none = m == -INFINITY;
   if (none) out = TwoColumns();
-  out.store(row_out<T>(a.o, s.q0 + i, h), none ? 0.f : 1.f / sum, a.dh, lane);
-  if (lane == 0) a.lse[(long)(s.q0 + i) * a.heads + h] = none ? -INFINITY : m + log2f(sum);
+  out.store(row_out<T>(a.o, s.q0 + i, h), none ? 0.f : 1.f / sum, c0, c1, lane);
+  if (lane == 0 && c0 == 0) a.lse[(long)(s.q0 + i) * a.heads + h] = none ? -INFINITY : m + log2f(sum);
 }
 // the statistic that the backward pass subtracts: a row that weighs nothing keeps weighing nothing
 __device__ __forceinline__ float stat_of(float lse) { return lse == -INFINITY ? INFINITY : lse; }
@@ -142,7 +155,7 @@ __device__ __forceinline__ float row_dsum(const PackedAttnArgs& a, long n, int h
 }
 
 template <typename T>
-__device__ __forceinline__ void one_dq(const PackedAttnArgs& a, const Seq& s, int i, int h, float D, int lane) {
+__device__ __forceinline__ void one_dq(const PackedAttnArgs& a, const Seq& s, int i, int h, float D, int c0, int c1, int lane) {
   const int hk = h / a.group, seen = seen_by(s, i, a.causal);
   const long n = s.q0 + i;
   const T* q = row_of<T>(a.q, n, h);
@@ -159,20 +172,22 @@ __device__ __forceinline__ void one_dq(const PackedAttnArgs& a, const Seq& s, in
         ds = p * (dot_rows(g, v + (j0 + lane) * a.v.row, a.dh) - D);
       }
       out.add(ds, seen - j0 < 64 ? seen - j0 : 64, k + j0 * a.k.row, a.k.row, a.dh, lane);
+      if (out.settled(a.dh, lane)) break;
     }
-  out.store(row_out<T>(a.dq, n, h), a.scale, a.dh, lane);
+  out.store(row_out<T>(a.dq, n, h), a.scale, c0, c1, lane);
 }
 
 template <typename T>
-__device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, int j, int hk, int lane) {
+__device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, int j, int hk, int c0, int c1, int lane) {
   const T* k = row_of<T>(a.k, s.k0 + j, hk);
   const T* v = row_of<T>(a.v, s.k0 + j, hk);
   const float c = a.scale * LOG2E;
   int i0 = a.causal ? j - (s.nk - s.nq) : 0;               // the first query that sees it
   if (i0 < 0) i0 = 0;
   TwoColumns dk, dv;
-  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
+  for (int h = hk * a.group; h < (hk + 1) * a.group && !(dk.settled(a.dh, lane) && dv.settled(a.dh, lane)); ++h)
     for (int b = i0; b < s.nq; b += 64) {
+      if (dk.settled(a.dh, lane) && dv.settled(a.dh, lane)) break;
       float p = 0.f, ds = 0.f;
       const int n = s.nq - b < 64 ? s.nq - b : 64;
       if (lane < n) {
@@ -186,8 +201,8 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
       dk.add(ds, n, row_of<T>(a.q, s.q0 + b, h), a.q.row, a.dh, lane);
       dv.add(p, n, row_of<T>(a.dout, s.q0 + b, h), a.dout.row, a.dh, lane);
     }
-  dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, a.dh, lane);
-  dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, a.dh, lane);
+  dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, c0, c1, lane);
+  dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, c0, c1, lane);
 }
 
 // Heads of up to W channels (32, 64, 96 or 128): tiles of 64 or 128 channels, of which products and results take W.
@@ -297,7 +312,8 @@ __device__ __forceinline__ RowPlace place_of(const PackedAttnArgs& a, int hk, in
 
 // Infinities and NaNs: a product on the matrix cores meets every element of a tile, also those that the mask or the sequence's end
 // leaves out, and there 0 times an infinity is NaN.  A row of a result that did not come out finite is therefore computed
-// once more, term by term over what it sees.  Finite data never comes here.
+// once more, term by term over what it sees
+// (wavefronts that hold blocks of 32 channels of a row each store, and compute once more, their own).
 template <int MB>
 __device__ __forceinline__ float not_finite(const float16v (&acc)[MB], float t) {
 #pragma unroll
@@ -306,6 +322,8 @@ __device__ __forceinline__ float not_finite(const float16v (&acc)[MB], float t) 
     for (int r = 0; r < 16; ++r) t = fmaf(acc[m][r], 0.f, t);
   return t;
 }
+// 1 / a row's sum of weights relative to its maximum m; 0 where it sees nothing.  (A sum of 0 with a maximum: infinity, which not_finite finds.)
+__device__ __forceinline__ float inverse_sum(float m, float sum) { return sum == 0.f && m == -FLT_MAX ? 0.f : 1.f / sum; }
 template <typename F>
 __device__ __forceinline__ void redo_rows(float t, int rows_left, F f) {
   const unsigned long long b = __ballot(t != t);
@@ -406,9 +424,9 @@ __global__ __launch_bounds__(256) void packed_join_fwd_kernel(PackedAttnArgs a) 
     w.y += x.y;
   }
   const float v[2] = {w.x, w.y};
-  const float g = sum == 0.f ? 0.f : 1.f / sum;
+  const float g = inverse_sum(top, sum);
   if (!all_finite(v[0] * g, v[1] * g)) {                   // (see redo_rows)
-    one_forward<T>(a, s, n - s.q0, h, lane);
+    one_forward<T>(a, s, n - s.q0, h, 0, a.dh, lane);
     return;
   }
   if (c < a.dh) store2(row_out<T>(a.o, n, h) + c, v[0] * g, v[1] * g);
@@ -424,7 +442,7 @@ __global__ __launch_bounds__(256) void packed_join_dq_kernel(PackedAttnArgs a) {
   const auto one = [](int) { return 1.f; };
   const float2 v = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   if (!all_finite(v.x, v.y)) {
-    one_dq<T>(a, s, n - s.q0, h, -a.dsum[r], lane);
+    one_dq<T>(a, s, n - s.q0, h, -a.dsum[r], 0, a.dh, lane);
     return;
   }
   if (2 * lane < a.dh) store2(row_out<T>(a.dq, n, h) + 2 * lane, v.x * a.scale, v.y * a.scale);
@@ -443,7 +461,7 @@ __global__ __launch_bounds__(256) void packed_join_dkdv_kernel(PackedAttnArgs a)
   const float2 k = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   const float2 v = sum_shares(a.part + (a.shares * rows + r) * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   if (!all_finite(k.x + k.y, v.x + v.y)) {
-    one_dkdv<T>(a, s, n - s.k0, hk, lane);
+    one_dkdv<T>(a, s, n - s.k0, hk, 0, a.dh, lane);
     return;
   }
   if (2 * lane < a.dh) {

@@ -314,14 +314,15 @@ __global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_k
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
     return row_out<bf16_t>(a.o, sq.q0 + q.i, q.h);
   };
+  const int c0 = COLS == 1 ? 0 : 32 * col, c1 = COLS == 1 || c0 + 32 > a.dh ? a.dh : c0 + 32;      // the channels that this wavefront leaves
   auto redo = [&](int j) {
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
-    one_forward<bf16_t>(a, sq, q.i, q.h, lane);
+    one_forward<bf16_t>(a, sq, q.i, q.h, c0, c1, lane);
   };
   const bool stat = lane < 32 && lane < b.rows_left;
   if constexpr (COLS == 1) {
     if (b.rows_left <= 0) return;
-    const float f = l == 0.f ? 0.f : 1.f / l;
+    const float f = inverse_sum(m, l);
     store_rows(row, b.rows_left, o, f, 0, a.dh, ring + wave * 2048, lane);
     if (stat) a.lse[n * a.heads + b.me.h] = l == 0.f ? -INFINITY : m + log2f(l);
     redo_rows(not_finite(o, f * 0.f), b.rows_left, redo);
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_k
       }
       return;
     }
-    const float g = sum == 0.f ? 0.f : 1.f / sum;
+    const float g = inverse_sum(top, sum);
     store_rows(row, b.rows_left, acc, g, col, a.dh, ring + wave * 2048, lane);
     if (stat && col == 0) a.lse[n * a.heads + b.me.h] = sum == 0.f ? -INFINITY : top + log2f(sum);
     redo_rows(not_finite(acc, g * 0.f), b.rows_left, redo);
@@ -449,9 +450,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
     return row_out<bf16_t>(a.dq, sq.q0 + q.i, q.h);
   };
+  const int c0 = COLS == 1 ? 0 : 32 * col, c1 = COLS == 1 || c0 + 32 > a.dh ? a.dh : c0 + 32;
   auto redo = [&](int j) {
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
-    one_dq<bf16_t>(a, sq, q.i, q.h, row_dsum<bf16_t>(a, sq.q0 + q.i, q.h, lane), lane);
+    one_dq<bf16_t>(a, sq, q.i, q.h, row_dsum<bf16_t>(a, sq.q0 + q.i, q.h, lane), c0, c1, lane);
   };
   if constexpr (COLS == 1) {
     if (b.rows_left <= 0) return;
@@ -698,7 +700,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
              a.dh, stg, lane);
   store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, x.s.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, 0,
              a.dh, stg, lane);
-  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, lane); });
+  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, 0, a.dh, lane); });
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -842,7 +844,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_short_kernel(PackedA
   else walk(std::false_type());
   l += other_half(l);
   copies_in_flight_read<0>();                              // (the ring is free: results leave through it)
-  const float f = l == 0.f ? 0.f : 1.f / l;
+  const float f = inverse_sum(m, l);
   store_rows([&](int j) __attribute__((always_inline)) {
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
     return row_out<bf16_t>(a.o, sq.q0 + q.i, q.h);
@@ -850,7 +852,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_short_kernel(PackedA
   if (lane < 32 && lane < b.rows_left) a.lse[n * a.heads + b.me.h] = l == 0.f ? -INFINITY : m + log2f(l);
   redo_rows(not_finite(o, f * 0.f), b.rows_left, [&](int j) {
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
-    one_forward<bf16_t>(a, sq, q.i, q.h, lane);
+    one_forward<bf16_t>(a, sq, q.i, q.h, 0, a.dh, lane);
   });
 }
 
@@ -933,7 +935,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_short_kernel(PackedAt
   }, b.rows_left, dq, a.scale, 0, a.dh, ring, lane);
   redo_rows(not_finite(dq, 0.f), b.rows_left, [&](int j) {
     const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
-    one_dq<bf16_t>(a, sq, q.i, q.h, row_dsum<bf16_t>(a, sq.q0 + q.i, q.h, lane), lane);
+    one_dq<bf16_t>(a, sq, q.i, q.h, row_dsum<bf16_t>(a, sq.q0 + q.i, q.h, lane), 0, a.dh, lane);
   });
 }
 
@@ -1039,7 +1041,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_short_kernel(Packed
              a.dh, ring, lane);
   store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, sq.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, 0,
              a.dh, ring, lane);
-  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, sq, w0 + j, x.hk, lane); });
+  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, sq, w0 + j, x.hk, 0, a.dh, lane); });
 }
 
 // Wavefronts by themselves: many, and with little to stream each.  Per sequence 256 of the other side's rows; 1024 where there are enough

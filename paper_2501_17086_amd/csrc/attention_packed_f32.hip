@@ -132,6 +132,9 @@ __device__ __forceinline__ void store_row(float* row, const float16v (&acc)[MB],
     }
 }
 
+// the end of N blocks' channels
+template <int N> __device__ __forceinline__ int past_block(int m0, int dh) { return 32 * (m0 + N) < dh ? 32 * (m0 + N) : dh; }
+
 // How the four wavefronts share rows and keys.  COLS = 1: 128 rows, 32 for each wavefront, steps of 32 keys.  COLS = 4, for few rows: 32 rows,
 // steps of 128 keys of which a wavefront takes 32; they meet in LDS at the end.
 template <int COLS> constexpr int rows_of_block() { return 32 * WAVES / COLS; }
@@ -255,10 +258,6 @@ __global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_
   l += other_half(l);
   const long n = s.q0 + b.me.i, r = n * a.heads + b.me.h, p = (long)b.share * a.q_rows * a.heads + r;
   const bool there = (lane & 31) < b.rows_left;
-  auto redo = [&](int j) {
-    const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
-    one_forward<float>(a, s, q.i, q.h, lane);
-  };
   // blocks m0 .. of the rows' outputs, sums l relative to m
   auto leave = [&](auto& acc, int m0, float m, float l) __attribute__((always_inline)) {
     constexpr int N = sizeof(acc) / sizeof(acc[0]);
@@ -272,12 +271,15 @@ __global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_
       }
       return;
     }
-    const float f = l == 0.f ? 0.f : 1.f / l;
+    const float f = inverse_sum(m, l);
     if (there) {
       store_row(row_out<float>(a.o, n, b.me.h), acc, f, m0, a.dh, hh);
       if (hh == 0 && m0 == 0) a.lse[r] = l == 0.f ? -INFINITY : m + log2f(l);
     }
-    redo_rows(not_finite(acc, f * 0.f), b.rows_left, redo);
+    redo_rows(not_finite(acc, f * 0.f), b.rows_left, [&](int j) {
+      const RowPlace q = place_of(a, b.x.hk, b.w0 + j);
+      one_forward<float>(a, s, q.i, q.h, 32 * m0, past_block<N>(m0, a.dh), lane);
+    });
   };
   if constexpr (COLS == 1) {
     if (b.rows_left > 0) leave(o, 0, m, l);
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(64 * WAVES, COLS > 1 || W > 96 ? 1 : 2) void packed
     if (there) store_row(row_out<float>(a.dq, n, b.me.h), acc, a.scale, m0, a.dh, hh);
     redo_rows(not_finite(acc, 0.f), b.rows_left, [&](int j) {
       const RowPlace p = place_of(a, b.x.hk, b.w0 + j);
-      one_dq<float>(a, s, p.i, p.h, row_dsum<float>(a, s.q0 + p.i, p.h, lane), lane);
+      one_dq<float>(a, s, p.i, p.h, row_dsum<float>(a, s.q0 + p.i, p.h, lane), 32 * m0, past_block<N>(m0, a.dh), lane);
     });
   };
   if constexpr (COLS == 1) {
@@ -497,7 +499,9 @@ __global__ __launch_bounds__(64 * WAVES, TURNS > 1 || W > 64 ? 1 : 2) void packe
       store_row(row_out<float>(a.dk, s.k0 + key, x.hk), k_sum, a.scale, m0, a.dh, hh);
       store_row(row_out<float>(a.dv, s.k0 + key, x.hk), v_sum, 1.f, m0, a.dh, hh);
     }
-    redo_rows(not_finite(v_sum, not_finite(k_sum, 0.f)), keys_left, [&](int j) { one_dkdv<float>(a, s, w0 + j, x.hk, lane); });
+    redo_rows(not_finite(v_sum, not_finite(k_sum, 0.f)), keys_left, [&](int j) {
+      one_dkdv<float>(a, s, w0 + j, x.hk, 32 * m0, past_block<N>(m0, a.dh), lane);
+    });
   };
   if constexpr (TURNS == 1) {
     if (keys_left > 0) leave(dk, dv, 0);

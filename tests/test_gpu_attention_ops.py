@@ -458,3 +458,70 @@ def test_infinities_in_every_form(lens, H, K, dtype):
     R.assert_within(a.dq[~seen], dq[~seen], 2 * eq[~seen], "dq")
     R.assert_within(a.dv, dv, ev, "dv")                    # (a value does not enter dv)
     R.assert_within(a.dk[n:], dk[n:], 2 * ek[n:], "dk")
+
+
+BIG = [([70] * 2, [250] * 2, 2, 2), ([64] * 70, None, 8, 8), ([600] * 5, None, 48, 24), ([1030], None, 4, 2), ([3], [6000], 8, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lq,lk,H,K", BIG, ids=[f"{len(f[0])}x{f[0][0]}" for f in BIG])
+def test_scores_beyond_the_exponents_steps(lq, lk, H, K, causal, dtype):
+    """Scores of up to 2^46, of which fp32 keeps steps of 2^23: no two of a head's are closer than 2^33, so that every row is the
+    value of the key with its largest score.  q holds 2^20, k the score's two parts (exact in either type), and so are the
+    products.  Roundings: lse that of log2 e, of its product and of the difference from 0, 4 f; o where the weight 2^r of the one
+    key is rounded to bf16 and divided by its sum: u each for weight and result, and 8 f for fp32's exponential, sum,
+    reciprocal and products."""
+    lk = lq if lk is None else lk
+    g = torch.Generator(device="cuda").manual_seed(83)
+    N, M = sum(lq), sum(lk)
+    q = torch.zeros((N, H, 64), dtype=TYPES[dtype], device="cuda")
+    q[:, :, 0] = q[:, :, 1] = 2.0 ** 20
+    place = torch.stack([torch.cat([torch.randperm(n, generator=g, device="cuda") for n in lk]) for _ in range(K)], 1)     # [M, K]
+    k = torch.zeros((M, K, 64), dtype=TYPES[dtype], device="cuda")
+    k[:, :, 0], k[:, :, 1] = (place // 128) * 2.0 ** 20, (place % 128) * 2.0 ** 13
+    v = normal((M, K, 64), TYPES[dtype], 84)
+    a = B.make_attention(q, k, v, causal=causal, scale=1.0, q_offsets=offsets(lq), k_offsets=offsets(lk))
+    B.hbp_attention_forward(a)
+    u = 0.0 if dtype == "f32" else R.half_step(TYPES[dtype])
+    r0 = k0 = 0
+    for n, m in zip(lq, lk):
+        s = place[k0:k0 + m].T[:, None].expand(K, n, m).clone()
+        if causal:
+            s[:, torch.arange(m, device="cuda")[None] > torch.arange(n, device="cuda")[:, None] + (m - n)] = -1
+        top, key = s.max(2)                                # [K, n]
+        want = v[k0 + key, torch.arange(K, device="cuda")[:, None]].transpose(0, 1).repeat_interleave(H // K, 1).double()
+        lse = (top.double() * 2.0 ** 33 * R.LOG2E).T.repeat_interleave(H // K, 1)
+        R.assert_within(a.o[r0:r0 + n], want, want.abs() * (2 * u + 8 * R.F) + 1e-38, "o")
+        R.assert_within(a.lse[r0:r0 + n], lse, lse.abs() * 4 * R.F + 1e-38, "lse")
+        r0, k0 = r0 + n, k0 + m
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lq,lk,H,K", BIG, ids=[f"{len(f[0])}x{f[0][0]}" for f in BIG])
+def test_nan_throughout(lq, lk, H, K, dtype):
+    """What diverged stays so, in every element that sees something."""
+    lk = lq if lk is None else lk
+    q, k, v, do = (torch.full_like(t, math.nan) for t in problem(lq, lk, H, K, 96, dtype, 89))
+    a = B.make_attention(q, k, v, causal=False, q_offsets=offsets(lq), k_offsets=offsets(lk))
+    B.hbp_attention_forward(a)
+    B.hbp_attention_backward(a, do)
+    for name in ("o", "lse", "dq", "dk", "dv"):
+        assert torch.isnan(getattr(a, name)).all(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H,K", [([300] * 2, 3, 1), ([64] * 70, 8, 8)])
+def test_rows_computed_once_more_are_repeatable(lens, H, K, dtype):
+    """An infinity in one channel of the last key's value: causal rows that do not see it meet it in a tile all the same."""
+    q, k, v, do = problem(lens, lens, H, K, 128, dtype, 97)
+    v[lens[0] - 1, :, 70] = math.inf
+    a = B.make_attention(q, k, v, q_offsets=offsets(lens), k_offsets=offsets(lens))
+    bits = torch.int32 if dtype == "f32" else torch.int16
+    first = None
+    for _ in range(6):
+        B.hbp_attention_forward(a)
+        B.hbp_attention_backward(a, do)
+        now = [getattr(a, name).clone().view(bits) for name in ("o", "dq", "dk", "dv")] + [a.lse.clone().view(torch.int32)]
+        assert first is None or all(torch.equal(x, y) for x, y in zip(first, now))
+        first = now
