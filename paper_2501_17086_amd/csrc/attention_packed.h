@@ -237,7 +237,13 @@ __device__ __forceinline__ int wave_total(int v) {
 // sequences of 1024 at 4 key heads left 43 % of the compute units' time unused).  Key heads are next to each other: all problems go on
 // side by side, and with eight of them, or a multiple, consecutive ids, which go to the eight XCDs in turn, keep a problem's
 // streamed tiles in one XCD's L2.
+// Past LEVELLED sequences the search for a level costs more than it gives (a memory latency for 64 of them), and there are workgroups
+// enough: tile t of sequence s then has the id first row / per + s + t, whose first two terms grow with s by at least the
+// sequence's tiles, and s is found 64 candidates at a time.  Levels / this, us, ragged: forward of 16384 sequences of 9, 4 heads of
+// 64, 1945 / 193; backward of 4096 of 64, 12 heads, 2870 / 1375; forward of 200 of 1000, 8 heads, 487 / 454; the other way round
+// backward of 100 of 1000, 8 heads, 1062 / 1107; forward of 24 of 700, 16 heads on 4, 55 / 66.
 struct Tile { int hk, t; Seq s; bool exists; };
+constexpr int LEVELLED = 128;
 __device__ __forceinline__ int tiles_in(int len, int per) { return (int)((unsigned)(len + per - 1) / (unsigned)per); }   // (per: a power of two)
 template <bool KEYS>
 __device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane, unsigned id = blockIdx.x) {
@@ -253,6 +259,30 @@ __device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int 
     sq = j - down * a.seqs;
     level = n - down;
     if (level <= 0) sq = -1;
+  } else if (a.seqs > LEVELLED) {
+    int lo = 0, hi = a.seqs, base = 0;                     // base of lo <= j < base of hi, where there is such a sequence
+    bool found = true;
+    do {
+      const int by = (hi - lo + 63) >> 6, at = lo + lane * by;
+      const int b = at < hi ? (int)((unsigned)(clamp_row(off[at], rows) * mult) / (unsigned)per) + at : j + 1;
+      const unsigned long long le = __ballot(b <= j);
+      found = le != 0;
+      if (!found) break;
+      const int l = 63 - __clzll(le);
+      base = __builtin_amdgcn_readlane(b, l);
+      lo += l * by;
+      hi = hi < lo + by ? hi : lo + by;
+    } while (hi - lo > 1);
+    if (found) {
+      int first;
+      span_of(off, rows, 0, lo, first, n);
+      n = __builtin_amdgcn_readfirstlane(tiles_in(n * mult, per));
+      const int t = j - base;
+      if (t < n) {
+        sq = lo;
+        level = KEYS ? n - t : t + 1;
+      }
+    }
   } else {
     for (int s0 = 0; s0 < a.seqs; s0 += 64) {              // 64 sequences at a time, one per lane
       int first, m = 0;

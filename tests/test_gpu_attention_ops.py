@@ -525,3 +525,33 @@ def test_rows_computed_once_more_are_repeatable(lens, H, K, dtype):
         now = [getattr(a, name).clone().view(bits) for name in ("o", "dq", "dk", "dv")] + [a.lse.clone().view(torch.int32)]
         assert first is None or all(torch.equal(x, y) for x, y in zip(first, now))
         first = now
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[i % 4 for i in range(3000)], [(7 * i) % 40 for i in range(300)], [0] * 200 + [300, 1] + [0] * 100,
+                                  [(i * i) % 90 for i in range(129)], [0] * 140], ids=lambda n: f"{len(n)}of{max(n)}")
+def test_attention_hundreds_and_thousands_of_sequences(lens, dtype):
+    """Some of them against the definitions, and that every row was written; empty ones between."""
+    q, k, v, do = problem(lens, lens, 4, 2, 64, dtype, 101)
+    a = B.make_attention(q, k, v, q_offsets=offsets(lens), k_offsets=offsets(lens))
+    for t in (a.o, a.dq, a.dk, a.dv, a.lse):
+        t.fill_(SENTINEL)
+    B.hbp_attention_forward(a)
+    B.hbp_attention_backward(a, do)
+    at, first = 0, []
+    for n in lens:
+        first.append(at)
+        at += n
+    some = [i for i, n in enumerate(lens) if n][:: max(1, len(lens) // 80)]
+    for i in some:
+        n, r = lens[i], slice(first[i], first[i] + lens[i])
+        ref = R.Packed(q[r], k[r], v[r], [n], [n], True)
+        o, lse, eo, el = ref.forward()
+        R.assert_within(a.lse[r], lse, el, "lse")
+        R.assert_within(a.o[r], o, eo, "o")
+        dq, dk, dv, eq, ek, ev = ref.backward(a.o[r], a.lse[r], do[r])
+        R.assert_within(a.dv[r], dv, ev, "dv")
+        R.assert_within(a.dk[r], dk, ek, "dk")
+        R.assert_within(a.dq[r], dq, eq, "dq")
+    for t in (a.o, a.dq, a.dk, a.dv, a.lse):
+        assert not (t == SENTINEL).any()                   # every row belongs to a sequence
