@@ -177,8 +177,9 @@ __device__ __forceinline__ void one_dq(const PackedAttnArgs& a, const Seq& s, in
   out.store(row_out<T>(a.dq, n, h), a.scale, c0, c1, lane);
 }
 
+constexpr int DK = 1, DV = 2;
 template <typename T>
-__device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, int j, int hk, int c0, int c1, int lane) {
+__device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, int j, int hk, int which, int c0, int c1, int lane) {
   const T* k = row_of<T>(a.k, s.k0 + j, hk);
   const T* v = row_of<T>(a.v, s.k0 + j, hk);
   const float c = a.scale * LOG2E;
@@ -201,8 +202,8 @@ __device__ __forceinline__ void one_dkdv(const PackedAttnArgs& a, const Seq& s, 
       dk.add(ds, n, row_of<T>(a.q, s.q0 + b, h), a.q.row, a.dh, lane);
       dv.add(p, n, row_of<T>(a.dout, s.q0 + b, h), a.dout.row, a.dh, lane);
     }
-  dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, c0, c1, lane);
-  dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, c0, c1, lane);
+  if (which & DK) dk.store(row_out<T>(a.dk, s.k0 + j, hk), a.scale, c0, c1, lane);
+  if (which & DV) dv.store(row_out<T>(a.dv, s.k0 + j, hk), 1.f, c0, c1, lane);
 }
 
 // Heads of up to W channels (32, 64, 96 or 128): tiles of 64 or 128 channels, of which products and results take W.
@@ -491,7 +492,7 @@ __global__ __launch_bounds__(256) void packed_join_dkdv_kernel(PackedAttnArgs a)
   const float2 k = sum_shares(a.part + r * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   const float2 v = sum_shares(a.part + (a.shares * rows + r) * a.dh, rows * a.dh, a.shares, a.dh, lane, one);
   if (!all_finite(k.x + k.y, v.x + v.y)) {
-    one_dkdv<T>(a, s, n - s.k0, hk, 0, a.dh, lane);
+    one_dkdv<T>(a, s, n - s.k0, hk, DK | DV, 0, a.dh, lane);
     return;
   }
   if (2 * lane < a.dh) {

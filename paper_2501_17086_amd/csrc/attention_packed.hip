@@ -48,11 +48,11 @@ constexpr int WAVES = 8;
 
 // Streamed key and value tiles: a stage holds 32 NT keys, NT tiles of k, then NT of v, which a workgroup's wavefronts copy together, PW
 // copies of 1 KB each, all of one tile or of whole ones.
-template <int DHP, int NT>
+template <int DHP, int NT, int NW>
 struct KeyStream {
   typedef Geo<DHP> G;
   static constexpr int STAGE = 2 * NT * G::TB;
-  static constexpr int PW = 2 * NT * G::COPIES / WAVES;
+  static constexpr int PW = 2 * NT * G::COPIES / NW;
   unsigned off[PW];
   const unsigned char *k, *v;
   unsigned ldk, ldv, lds0;
@@ -88,25 +88,25 @@ struct KeyStream {
   }
 };
 
-// How a workgroup's eight wavefronts share rows and keys.  COLS = 1: 256 rows, 32 for each wavefront, which goes over all keys in
-// steps of 64.  COLS = 4, for few rows: 64 rows, and of every step of 128 keys a wavefront takes 32; the four that share rows
+// How a workgroup's NW wavefronts (eight, or four) share rows and keys.  COLS = 1: 32 rows for each wavefront, which goes over all keys
+// in steps of 64.  COLS = 4, for few rows: 64 rows, and of every step of 128 keys a wavefront takes 32; the four that share rows
 // meet in LDS at the end.
-template <int W, int COLS>
+template <int W, int COLS, int NW>
 struct Shape {
   static constexpr int DHP = padded<W>();
   typedef Fit<W> G;
-  static constexpr int ROWS = 32 * WAVES / COLS;
+  static constexpr int ROWS = 32 * NW / COLS;
   static constexpr int NT = COLS == 1 ? 2 : 4, KEYS = 32 * NT, SUB = NT / COLS;
-  typedef KeyStream<DHP, NT> KS;
-  static constexpr int NST = COLS == 1 ? (DHP == 128 ? 3 : 4) : (DHP == 128 ? 2 : 3);
-  static constexpr int SUMS = COLS == 1 ? 0 : WAVES * G::MB * 16 * 64 * 4;       // everyone's output, fp32
+  typedef KeyStream<DHP, NT, NW> KS;
+  static constexpr int NST = COLS == 1 ? (DHP == 128 || NW == 4 ? 3 : 4) : (DHP == 128 ? 2 : 3);
+  static constexpr int SUMS = COLS == 1 ? 0 : NW * G::MB * 16 * 64 * 4;       // everyone's output, fp32
   static constexpr int RING = NST * KS::STAGE > SUMS ? NST * KS::STAGE : SUMS;
 };
 
 // The rows of a workgroup, and the keys that they see: steps from .. to - 1 of this workgroup's share of them.
-template <int W, int COLS>
+template <int W, int COLS, int NW>
 struct RowBlock {
-  typedef Shape<W, COLS> S;
+  typedef Shape<W, COLS, NW> S;
   Tile x;
   int w0, rows_left, mine, fewest, most, from, to, share;
   RowPlace me;
@@ -226,16 +226,17 @@ __device__ __forceinline__ void get_sums(const float* sums, int rw, int m, const
 // packed_join_fwd_kernel.
 template <int W, int COLS>
 __global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_kernel(PackedAttnArgs a) {
+  constexpr int NW = WAVES;
   constexpr int DHP = padded<W>();
   typedef Fit<W> G;
-  typedef Shape<W, COLS> S;
+  typedef Shape<W, COLS, NW> S;
   typedef typename S::KS KS;
-  constexpr int NST = S::NST, RW = WAVES / COLS;
+  constexpr int NST = S::NST, RW = NW / COLS;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[S::RING];
   __shared__ float stats[COLS == 1 ? 1 : WAVES][2][64];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = wave % RW, col = wave / RW;
-  RowBlock<W, COLS> b;
+  RowBlock<W, COLS, NW> b;
   if (!b.find(a, rw, lane)) return;
   const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3;
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_k
       for (int u = 0; u < S::SUB; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (first + 32 * u + tile_row_of(e, hh) >= b.mine) s[u][e] = -INFINITY;
+          if (32 * u + tile_row_of(e, 0) >= b.mine - 4 * hh - first) s[u][e] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
@@ -361,19 +362,163 @@ __global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_k
   }
 }
 
-// dq, and for the other kernel minus D = sum_c dout (.) o and minus lse of every row.  As the forward pass: a lane holds a row of q and
-// of dout, dS leaves the first two products in the places from which the third takes it.
-template <int W, int COLS>
-__global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAttnArgs a) {
+// More than 64 channels, many rows: 64 of them for a wavefront, so that a tile read from LDS meets two tiles of rows.  (32 rows each: the
+// reads of LDS take as long as the products; 16384 positions, 32 heads of 128 on 8: 2115 us, with 64 1971, of which a long
+// library product's rate would leave 1671.)  The steps are those of packed_fwd_mfma_kernel, 32 keys at a time.
+constexpr int TALL = 2 * 32 * WAVES;
+template <int W>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_tall_kernel(PackedAttnArgs a) {
   constexpr int DHP = padded<W>();
   typedef Fit<W> G;
-  typedef Shape<W, COLS> S;
+  constexpr int RT = 2, NT = 2, KEYS = 32 * NT, ROWS = TALL, NST = 3;
+  typedef KeyStream<DHP, NT, WAVES> KS;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[NST * KS::STAGE];
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const Tile x = find_tile<false>(a, ROWS, lane);
+  if (!x.exists) return;
+  const Seq& sq = x.s;
+  const int R = sq.nq * a.group, r0 = ROWS * x.t, w0 = r0 + 32 * RT * wave, rows_left = R - w0;
+  auto seen = [&](int r) __attribute__((always_inline)) { return seen_by(sq, place_of(a, x.hk, r).i, a.causal); };
+  const int steps = (seen((R < r0 + ROWS ? R : r0 + ROWS) - 1) + KEYS - 1) / KEYS;
+  const int fewest = rows_left > 0 ? seen(w0) : 0, most = rows_left > 0 ? seen(w0 + (rows_left < 32 * RT ? rows_left : 32 * RT) - 1) : 0;
+  const int dh8 = a.dh >> 3;
+  const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
+  const KS ks(a, sq, x.hk, lds0, dh8, wave, lane);
+  for (int i = 0; i < NST - 1 && i < steps; ++i) ks.issue(i, i, wave, lane);
+  bf16x8 fq[RT][G::KK];
+  int mine[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = w0 + 32 * t + (lane & 31);
+    const RowPlace me = place_of(a, x.hk, r < R ? r : R - 1);
+    mine[t] = seen_by(sq, me.i, a.causal) - 4 * hh;
+    const bf16_t* qrow = row_of<bf16_t>(a.q, sq.q0 + me.i, me.h);
+#pragma unroll
+    for (int kk = 0; kk < G::KK; ++kk) fq[t][kk] = own_piece(qrow, kk, dh8, lane);
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int kk = 0; kk < G::KK; ++kk) landed(fq[t][kk]);
+  const float c = a.scale * LOG2E;
+  const unsigned ck = lds0 + Frags<DHP>::cols_lane(lane), rv = lds0 + Frags<DHP>::rows_lane(lane);
+  float16v o[RT][G::MB];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) { zero_acc(o[t]); m[t] = -FLT_MAX; l[t] = 0.f; }
+  int at = 0;
+  for (int i = 0; i < steps; ++i) {
+    if (i + NST - 2 < steps) copies_in_flight<KS::PW * (NST - 2)>();
+    else copies_in_flight<0>();
+    workgroup_handover();
+    if (i + NST - 1 < steps) ks.issue(i + NST - 1, at == 0 ? NST - 1 : at - 1, wave, lane);
+    const unsigned tk = ck + (unsigned)at * KS::STAGE, tv = rv + (unsigned)at * KS::STAGE;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      const int first = KEYS * i + 32 * u;
+      if (first < most) {
+        float16v s[RT];
+        zero_acc(s);
+#pragma unroll
+        for (int kk = 0; kk < G::KK; ++kk) {
+          const bf16x8 f = Frags<DHP>::cols(tk, u * G::TB, kk);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) s[t] = mfma(f, fq[t][kk], s[t]);
+        }
+        if (first + 32 > fewest) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const int n = mine[t] - first;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (tile_row_of(e, 0) >= n) s[t][e] = -INFINITY;
+          }
+        }
+        float top[RT];
+        bool more = false;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          top[t] = s[t][0];
+#pragma unroll
+          for (int e = 1; e < 16; ++e) top[t] = fmaxf(top[t], s[t][e]);
+          top[t] = max_of_halves(top[t]) * c;
+          more = more || top[t] > m[t] + 8.f;
+        }
+        if (__any(more)) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const float mn = fmaxf(m[t], top[t]), alpha = fast_exp2(m[t] - mn);
+            m[t] = mn;
+            l[t] *= alpha;
+#pragma unroll
+            for (int mb = 0; mb < G::MB; ++mb)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[t][mb][e] *= alpha;
+          }
+        }
+        bf16x8 p[RT][2];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          float w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            w[e] = fast_exp2(fmaf(s[t][e], c, -m[t]));
+            l[t] += w[e];
+          }
+          p[t][0] = pack8(w);
+          p[t][1] = pack8(w + 8);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int mb = 0; mb < G::MB; ++mb) {
+            const bf16x8 f = Frags<DHP>::rows(tv, (NT + u) * G::TB, mb, g);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) o[t][mb] = mfma(f, p[t][g], o[t][mb]);
+          }
+      }
+    }
+    at = at == NST - 1 ? 0 : at + 1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int left = rows_left - 32 * t, wt = w0 + 32 * t;
+    if (left <= 0) return;
+    l[t] += other_half(l[t]);
+    const float f = inverse_sum(m[t], l[t]);
+    store_rows([&](int j) __attribute__((always_inline)) {
+      const RowPlace q = place_of(a, x.hk, wt + j);
+      return row_out<bf16_t>(a.o, sq.q0 + q.i, q.h);
+    }, left, o[t], f, 0, a.dh, ring + wave * 2048, lane);
+    if (lane < 32 && lane < left) {
+      const RowPlace me = place_of(a, x.hk, wt + lane);
+      a.lse[(long)(sq.q0 + me.i) * a.heads + me.h] = l[t] == 0.f ? -INFINITY : m[t] + log2f(l[t]);
+    }
+    redo_rows(not_finite(o[t], f * 0.f), left, [&](int j) {
+      const RowPlace q = place_of(a, x.hk, wt + j);
+      one_forward<bf16_t>(a, sq, q.i, q.h, 0, a.dh, lane);
+    });
+  }
+}
+
+// dq, and for the other kernel minus D = sum_c dout (.) o and minus lse of every row.  As the forward pass: a lane holds a row of q and
+// of dout, dS leaves the first two products in the places from which the third takes it.
+// At up to 64 channels a workgroup of many rows has four wavefronts, and a compute unit three workgroups: rows are loaded, and results
+// stored, while others compute (16 sequences of 1024, 16 heads on 4: 90 us with one workgroup of eight, of whose 22 us
+// 7.4 are not spent on products; 77 with three of four).
+template <int W, int COLS, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void packed_dq_mfma_kernel(PackedAttnArgs a) {
+  constexpr int DHP = padded<W>();
+  typedef Fit<W> G;
+  typedef Shape<W, COLS, NW> S;
   typedef typename S::KS KS;
-  constexpr int NST = S::NST, RW = WAVES / COLS;
+  constexpr int NST = S::NST, RW = NW / COLS;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[S::RING];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rw = wave % RW, col = wave / RW;
-  RowBlock<W, COLS> b;
+  RowBlock<W, COLS, NW> b;
   if (!b.find(a, rw, lane)) return;
   const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3;
@@ -425,7 +570,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_mfma_kernel(PackedAtt
       if (masked) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (first + 32 * u + tile_row_of(e, hh) >= b.mine) ds[e] = 0.f;
+          if (32 * u + tile_row_of(e, 0) >= b.mine - 4 * hh - first) ds[e] = 0.f;
       }
       const Operand<decltype(few)::value> op(ds);
       op.template times<DHP>(tr, u * G::TB, dq);
@@ -498,7 +643,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   constexpr int NT = TURNS * QT;                           // tiles of a step
   constexpr int STAGE = 2 * NT * G::TB;                    // NT tiles of q, as many of dout
   constexpr int PW = 2 * NT * G::COPIES / WAVES;           // copies of a stage by one wavefront
-  constexpr int SUMS = KW * (TURNS - 1) * G::MB * 16 * 64 * 4;     // the sums of all but the first, dk or dv
+  constexpr int SUMS = KW * (TURNS == 2 ? 2 : TURNS - 1) * G::MB * 16 * 64 * 4;    // of two turns dk and dv, of four one of them at a time
   constexpr int RING = NST * STAGE + (KLDS ? KW * G::TB : 0);
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RING > SUMS ? RING : SUMS];
   __shared__ __attribute__((aligned(256))) float stats[NST][NT][2][64];          // [stage][tile][-lse | -D][32 rows, and again]
@@ -621,8 +766,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
       for (int b = 0; b < QT; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int i = first[b] + tile_row_of(e, hh);
-          if (i < mine || i >= nq) p[b][e] = 0.f;
+          const int i = tile_row_of(e, 0);
+          if (i < mine - 4 * hh - first[b] || i >= nq - 4 * hh - first[b]) p[b][e] = 0.f;
         }
     }
 #pragma unroll
@@ -664,43 +809,51 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_mfma_kernel(PackedA
   };
   if (nq <= FEW) walk(std::true_type());
   else walk(std::false_type());
-  auto meet = [&](float16v (&acc)[G::MB]) __attribute__((always_inline)) {
-    float* const sums = reinterpret_cast<float*>(ring) + kw * (G::MB * 16 * 64) + lane;
-    __syncthreads();                                       // (the ring, or the sums before, are free)
-    if (turn > 0) {
+  // The turns' sums of dk meet in the first one, those of dv in the second, through LDS: two turns exchange them at once.
+  constexpr bool AT_ONCE = TURNS == 2;
+  float* const sums = reinterpret_cast<float*>(ring) + kw * (G::MB * 16 * 64) + lane;
+  constexpr int SLOT = KW * G::MB * 16 * 64;
+  auto put = [&](const float16v (&acc)[G::MB], int owner, int slot) __attribute__((always_inline)) {
+    if (turn == owner) return;
+    float* p = sums + (slot + (turn < owner ? turn : turn - 1)) * SLOT;
+#pragma unroll
+    for (int m = 0; m < G::MB; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[(m * 16 + e) * 64] = acc[m][e];
+  };
+  auto get = [&](float16v (&acc)[G::MB], int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < TURNS - 1; ++j)
 #pragma unroll
       for (int m = 0; m < G::MB; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sums[((turn - 1) * KW * G::MB * 16 + m * 16 + e) * 64] = acc[m][e];
-    }
-    __syncthreads();
-    if (turn == 0) {
-#pragma unroll
-      for (int j = 0; j < TURNS - 1; ++j)
-#pragma unroll
-        for (int m = 0; m < G::MB; ++m)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[m][e] += sums[(j * KW * G::MB * 16 + m * 16 + e) * 64];
-    }
+        for (int e = 0; e < 16; ++e) acc[m][e] += sums[(slot + j) * SLOT + (m * 16 + e) * 64];
   };
-  meet(dk);
-  meet(dv);
-  __syncthreads();
-  if (turn > 0 || keys_left <= 0) return;
-  if (a.shares > 1) {
-    const long r = (long)(x.s.k0 + key) * a.kv_heads + x.hk, rows = (long)a.k_rows * a.kv_heads;
-    if ((lane & 31) < keys_left) {
-      store_share<G::MB>(a.part, share * rows + r, dk, 0, a.dh, hh);
-      store_share<G::MB>(a.part, (a.shares + share) * rows + r, dv, 0, a.dh, hh);
+  auto leave = [&](const float16v (&acc)[G::MB], const HeadRows& out, float f, int which) __attribute__((always_inline)) {
+    if (a.shares > 1) {
+      const long r = (long)(x.s.k0 + key) * a.kv_heads + x.hk, rows = (long)a.k_rows * a.kv_heads;
+      if ((lane & 31) < keys_left) store_share<G::MB>(a.part, ((which == DV ? a.shares : 0) + share) * rows + r, acc, 0, a.dh, hh);
+      return;
     }
-    return;
+    store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(out, x.s.k0 + w0 + j, x.hk); }, keys_left, acc, f, 0, a.dh,
+               ring + wave * 2048, lane);
+    redo_rows(not_finite(acc, 0.f), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, which, 0, a.dh, lane); });
+  };
+  __syncthreads();
+  put(dk, 0, 0);
+  if (AT_ONCE) put(dv, 1, 1);
+  __syncthreads();
+  if (turn == 0) get(dk, 0);
+  if (!AT_ONCE) {
+    __syncthreads();
+    put(dv, 1, 0);
+    __syncthreads();
   }
-  unsigned char* stg = ring + wave * 2048;
-  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dk, x.s.k0 + w0 + j, x.hk); }, keys_left, dk, a.scale, 0,
-             a.dh, stg, lane);
-  store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, x.s.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, 0,
-             a.dh, stg, lane);
-  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, x.s, w0 + j, x.hk, 0, a.dh, lane); });
+  if (turn == 1) get(dv, AT_ONCE ? 1 : 0);
+  __syncthreads();
+  if (turn > 1 || keys_left <= 0) return;
+  if (turn == 0) leave(dk, a.dk, a.scale, DK);
+  else leave(dv, a.dv, 1.f, DV);
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -1041,7 +1194,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_short_kernel(Packed
              a.dh, ring, lane);
   store_rows([&](int j) __attribute__((always_inline)) { return row_out<bf16_t>(a.dv, sq.k0 + w0 + j, x.hk); }, keys_left, dv, 1.f, 0,
              a.dh, ring, lane);
-  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, sq, w0 + j, x.hk, 0, a.dh, lane); });
+  redo_rows(not_finite(dv, not_finite(dk, 0.f)), keys_left, [&](int j) { one_dkdv<bf16_t>(a, sq, w0 + j, x.hk, DK | DV, 0, a.dh, lane); });
 }
 
 // Wavefronts by themselves: many, and with little to stream each.  Per sequence 256 of the other side's rows; 1024 where there are enough
@@ -1059,11 +1212,16 @@ bool alone(const PackedAttnArgs& a) {
   return other <= 256 || (other <= 1024 && (KEYS ? waves >= 8 * (long)CUS : rows / a.seqs <= 32));
 }
 
-// 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64
+// 256 rows (128 keys) for a workgroup where that makes at least as many workgroups as there are compute units, otherwise 64; 512 of more
+// than 64 channels where that makes two for every compute unit and sequences have twice as many rows (256 / 512, us, heads of 128:
+// 8 sequences of 1024, 32 heads on 8, 93 / 85; 40 ragged ones of 400 159 / 148; the other way round one of 4096, 264 workgroups
+// of which a causal mask makes the longest last, 142 / 206; 24 of 700, 16 heads of 96, 121 / 127)
 template <int W>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
   if (alone<false>(a))
     packed_fwd_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
+  else if (W > 64 && wide_blocks<false>(a, TALL, 1024, 2 * CUS))
+    packed_fwd_tall_kernel<(W > 64 ? W : 128)><<<tile_grid<false>(a, TALL), 64 * WAVES, 0, s>>>(a);
   else if (wide_blocks<false>(a, 256, 64, CUS))
     packed_fwd_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
   else
@@ -1072,12 +1230,13 @@ hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
 }
 template <int W>
 hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
+  constexpr int NW = W <= 64 ? 4 : 8;
   if (alone<false>(a))
     packed_dq_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
   else if (wide_blocks<false>(a, 256, 64, CUS))
-    packed_dq_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
+    packed_dq_mfma_kernel<W, 1, NW><<<tile_grid<false>(a, 32 * NW), 64 * NW, 0, s>>>(a);
   else
-    packed_dq_mfma_kernel<W, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+    packed_dq_mfma_kernel<W, 4, WAVES><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int W>

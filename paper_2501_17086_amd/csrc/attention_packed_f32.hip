@@ -500,7 +500,7 @@ __global__ __launch_bounds__(64 * WAVES, TURNS > 1 || W > 64 ? 1 : 2) void packe
       store_row(row_out<float>(a.dv, s.k0 + key, x.hk), v_sum, 1.f, m0, a.dh, hh);
     }
     redo_rows(not_finite(v_sum, not_finite(k_sum, 0.f)), keys_left, [&](int j) {
-      one_dkdv<float>(a, s, w0 + j, x.hk, 32 * m0, past_block<N>(m0, a.dh), lane);
+      one_dkdv<float>(a, s, w0 + j, x.hk, DK | DV, 32 * m0, past_block<N>(m0, a.dh), lane);
     });
   };
   if constexpr (TURNS == 1) {

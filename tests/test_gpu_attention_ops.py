@@ -555,3 +555,44 @@ def test_attention_hundreds_and_thousands_of_sequences(lens, dtype):
         R.assert_within(a.dq[r], dq, eq, "dq")
     for t in (a.o, a.dq, a.dk, a.dv, a.lse):
         assert not (t == SENTINEL).any()                   # every row belongs to a sequence
+
+
+# many rows of wide heads: 64 for a wavefront
+TALL = [([1030] * 12, None, 16, 16), ([290 + i % 21 for i in range(20)], None, 32, 8), ([300] * 20, [340] * 20, 32, 8),
+        ([513] * 22, [9] * 22, 16, 8)]
+
+
+@pytest.mark.parametrize("dh", [72, 96, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lq,lk,H,K", TALL, ids=[f"{len(f[0])}x{f[0][0]}" for f in TALL])
+def test_attention_many_rows_of_wide_heads(lq, lk, H, K, causal, dh):
+    lk = lq if lk is None else lk
+    q, k, v, do = problem(lq, lk, H, K, dh, "bf16", 103)
+    check_attention(q, k, v, lq, lk, causal, do)
+
+
+def test_many_rows_of_wide_heads_with_infinities_and_large_scores():
+    """A NaN in the last key's value reaches the queries that see it alone; scores beyond 2^31 (see above) take their key's value."""
+    lens = [300] * 20
+    q, k, v, _ = problem(lens, lens, 32, 8, 128, "bf16", 107)
+    v[299, :, 100] = math.nan
+    a = B.make_attention(q, k, v, q_offsets=offsets(lens), k_offsets=offsets(lens))
+    B.hbp_attention_forward(a)
+    clean = v.clone()
+    clean[299] = 0
+    o, lse, eo, el = R.Packed(q, k, clean, lens, lens, True).forward()
+    seen = torch.zeros(sum(lens), dtype=torch.bool, device="cuda")
+    seen[299] = True
+    R.assert_within(a.o[~seen], o[~seen], eo[~seen], "o")
+    R.assert_within(a.lse, lse, el, "lse")
+    assert torch.isnan(a.o[299, :, 100]).all()
+    q.zero_(), k.zero_()
+    q[:, :, 0] = 2.0 ** 20
+    place = torch.randperm(256, device="cuda", generator=torch.Generator(device="cuda").manual_seed(109))
+    k[:, :, 0] = torch.cat([place, place[:44] * 0])[:300].repeat(20)[:, None] * 2.0 ** 20
+    B.hbp_attention_forward(a)
+    key = torch.cummax(torch.cat([place, place[:44] * 0]), 0).indices.repeat(20) + 300 * torch.arange(20, device="cuda").repeat_interleave(300)
+    want = v[key].repeat_interleave(4, 1)
+    ok = ~torch.isnan(want)
+    ok[299] = False
+    assert torch.equal(a.o[ok], want[ok])
