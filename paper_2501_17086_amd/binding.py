@@ -408,8 +408,9 @@ def _storage_type(dtype) -> int:
 def _heads(name: str, t, shape, dtype, device: int) -> tuple:
     """The fields of an hbp_heads for a [rows, heads, dh] tensor, channels next to each other.  (These checks are on the way of
     every call: plain comparisons, the messages made only where one fails.)"""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != device:
-        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on GPU {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t is None or t.shape != shape or t.dtype != dtype or t.get_device() != device:
+        got = "none" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}"
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on GPU {device}, got {got}")
     row, head, channel = t.stride()
     if channel != 1 and shape[2] > 1:
         raise ValueError(f"{name}: the channels of a head must be next to each other, got strides {t.stride()}")

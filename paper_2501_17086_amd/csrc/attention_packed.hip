@@ -364,7 +364,8 @@ __global__ __launch_bounds__(64 * WAVES, W <= 64 ? 4 : 2) void packed_fwd_mfma_k
 
 // More than 64 channels, many rows: 64 of them for a wavefront, so that a tile read from LDS meets two tiles of rows.  (32 rows each: the
 // reads of LDS take as long as the products; 16384 positions, 32 heads of 128 on 8: 2115 us, with 64 1971, of which a long
-// library product's rate would leave 1671.)  The steps are those of packed_fwd_mfma_kernel, 32 keys at a time.
+// library product's rate would leave 1671.)  The steps are those of packed_fwd_mfma_kernel, 32 keys at a time; weights are rounded
+// once even in a sequence of few keys among longer ones (see Operand; two parts have no registers here).
 constexpr int TALL = 2 * 32 * WAVES;
 template <int W>
 __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_tall_kernel(PackedAttnArgs a) {
@@ -1220,7 +1221,7 @@ template <int W>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
   if (alone<false>(a))
     packed_fwd_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
-  else if (W > 64 && wide_blocks<false>(a, TALL, 1024, 2 * CUS))
+  else if (W > 64 && wide_blocks<false>(a, TALL, 1024, 2 * CUS) && a.k_rows / a.seqs > FEW)
     packed_fwd_tall_kernel<(W > 64 ? W : 128)><<<tile_grid<false>(a, TALL), 64 * WAVES, 0, s>>>(a);
   else if (wide_blocks<false>(a, 256, 64, CUS))
     packed_fwd_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);

@@ -224,3 +224,9 @@ def test_reference_notices_a_wrong_element():
     wrong[0, 0, 0] = math.nan
     with pytest.raises(AssertionError):
         R.assert_within(wrong, o, eo, "planted")
+
+
+def test_a_tensor_that_is_not_there_is_refused():
+    """An Attention made without room for gradients has no dq, dk, dv."""
+    with pytest.raises(ValueError, match="dq: .* got none"):
+        B._heads("dq", None, (4, 2, 8), torch.float32, 0)

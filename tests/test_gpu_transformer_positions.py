@@ -183,3 +183,44 @@ def test_training_step_is_its_parts_and_a_graph_replays_them(case):
         torch.cuda.synchronize()
         assert torch.equal(p.g, want[0]) and torch.equal(p.dWqkv, want[1])
         B.hbp_backward(p, 0)
+
+
+class PostNorm(Stack):
+    """Layers without a norm before a sub-block, and one after every residual sum."""
+
+    def block(self, l, x):
+        w, j = self.w, l // 2
+        if l % 2:
+            return torch.nn.functional.gelu(x @ self.W["W1"][j].T) @ self.W["W2"][j].T
+        H, K, D = w.heads, w.kv_heads, w.d // w.heads
+        qkv = (x @ self.W["Wqkv"][j].T).view(-1, H + 2 * K, D)
+        qkv = torch.cat((self.turn(qkv[:, :H + K], w.rotary["dims"], "half", 1.0, {}), qkv[:, H + K:]), 1)
+        qkv = qkv.view(-1, w.seq_len, H + 2 * K, D).transpose(1, 2)
+        q, k, v = qkv[:, :H], qkv[:, H:H + K].repeat_interleave(H // K, 1), qkv[:, H + K:].repeat_interleave(H // K, 1)
+        o = torch.softmax(q @ k.transpose(2, 3) / math.sqrt(D), -1) @ v
+        return o.transpose(1, 2).reshape(x.shape) @ self.W["Wo"][j].T
+
+    def run(self):
+        self.x = [self.x0.clone()]
+        for l in range(self.w.L):
+            s = self.lam[l] * self.x[-1] + self.block(l, self.x[-1])
+            self.x.append(s / torch.sqrt((s * s).mean(-1, keepdim=True) + self.w.eps))
+        return self.x
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_post_norm_stack(dtype):
+    """As the other stacks, where the norm follows the residual sum: states, and the exact gradients of all parameters."""
+    w = synth.scaled(synth.WORKLOADS["roberta_like"], name="positions_post", dtype=dtype, L=4, N=120, seq_len=40, d=128, heads=4, d_ff=256,
+                     w1_std=0.0, w2_std=0.0, w2_scale=0.6, kv_heads=2, rotary=dict(dims=32))
+    inp = synth.make_inputs(w)
+    p = B.allocate(w, inp)
+    st = PostNorm(w, inp, torch.arange(w.N) % w.seq_len)
+    x = st.run()
+    want = dict(zip(st.W, torch.autograd.grad((x[-1] * st.e).sum(), list(st.W.values()))))
+    B.hbp_forward(p)
+    assert_close(to_np(p.x), torch.stack(x).detach().numpy(), TOL[dtype], "x")
+    B.hbp_exact_backward(p)
+    B.hbp_param_grads(p)
+    for n, t in want.items():
+        assert_close(to_np(getattr(p, "d" + n)), t.detach().numpy(), TOL[dtype], "d" + n)
