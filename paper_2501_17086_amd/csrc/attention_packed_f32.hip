@@ -200,6 +200,35 @@ template <int W, int NT> constexpr int ring_bytes() {
   return ring > sums ? ring : sums;
 }
 
+// what was read of LDS before has arrived, and all but N copies
+template <int N>
+__device__ __forceinline__ void read_and_in_flight() {
+  asm volatile("" ::: "memory");
+  copies_in_flight_read<N>();
+}
+// COLS = 4: a wavefront copies the tiles that it reads, its k and its v of every step, and waits for nobody.  (x: tile 0, y: tile 1 of its
+// stage, each of Geo::COPIES copies.)  Two stages, or one where two do not fit: then k of the next step comes while v of this one is used.
+// (One token for each of 44 sequences over 1910 keys, 8 heads of 128: 188 us, 3.7 TB/s; with stages that the workgroup fills together 238.  8
+// heads of 64 on 2, 60 over 2000: 43 and 45; 2 over 10229, one head of 96, four steps a workgroup: 31 and 30.)
+template <int W>
+struct OwnStream {
+  static constexpr int DHP = 2 * padded<W>();
+  typedef Geo<DHP> G;
+  static constexpr int NST = PairStream<W, 4>::NST, STAGE = PairStream<W, 4>::STAGE, N = G::COPIES;
+  unsigned lds, ldk, ldv;
+  const float *k, *v;
+  int nk, dh4;
+  // keys 32 t .. of the sequence, at most 32 of them, rows past the last repeat it
+  __device__ __forceinline__ void tile(const float* x, unsigned ld, int first, unsigned dst, int lane) const {
+    const int n = nk - first < 32 ? nk - first : 32;
+    const float* base = x + (long)first * (ld >> 2);
+#pragma unroll
+    for (int u = 0; u < N; ++u) copy16_to_lds(copy_offset<DHP>(ld, u, n, dh4, lane), base, dst + 1024u * u);
+  }
+  __device__ __forceinline__ void ask_k(int first, int at, int lane) const { tile(k, ldk, first, lds + (unsigned)at * STAGE, lane); }
+  __device__ __forceinline__ void ask_v(int first, int at, int lane) const { tile(v, ldv, first, lds + (unsigned)at * STAGE + 4 * G::TB, lane); }
+};
+
 template <int W, int COLS>
 __global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_kernel(PackedAttnArgs a) {
   typedef Tiles<W> T;
@@ -215,7 +244,17 @@ __global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(ring));
   const PS ps((unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), a.dh, lds0, wave);
   auto ask = [&](int i, int at) __attribute__((always_inline)) { b.ask(ps, a, i, at, lane); };
-  if (b.from < b.to) ask(b.from, PS::NST == 1 ? 0 : b.from & 1);
+  typedef OwnStream<W> OS;
+  const OS os{lds0 + (unsigned)wave * T::G::TB, (unsigned)(a.k.row * 4), (unsigned)(a.v.row * 4), b.k, b.v, s.nk, a.dh >> 2};
+  // the last step in which this wavefront's keys are seen, and one
+  int own_to = b.most > 32 * col ? (b.most - 32 * col + RB::KEYS - 1) / RB::KEYS : 0;
+  own_to = own_to < b.to ? own_to : b.to;
+  if constexpr (COLS == 1) {
+    if (b.from < b.to) ask(b.from, PS::NST == 1 ? 0 : b.from & 1);
+  } else if (b.from < own_to) {
+    os.ask_k(RB::KEYS * b.from + 32 * col, 0, lane);
+    os.ask_v(RB::KEYS * b.from + 32 * col, 0, lane);
+  }
   float q[4 * T::J];
   T::own(row_of<float>(a.q, s.q0 + b.me.i, b.me.h), a.dh, lane, q);
   const unsigned ck = lds0 + T::cols_lane(lane) + (unsigned)col * T::G::TB, rv = lds0 + T::rows_lane(lane) + (unsigned)col * T::G::TB;
@@ -223,13 +262,8 @@ __global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_
   float16v o[T::MB];
   zero_acc(o);
   float m = -FLT_MAX, l = 0.f;
-  for (int i = b.from; i < b.to; ++i) {
-    const unsigned at = (unsigned)next_stage<PS::NST>(i, b.from, b.to, ask) * PS::STAGE;
-    const int first = RB::KEYS * i + 32 * col;
-    if (first >= b.most) continue;
-    float16v sc[1];
-    zero_acc(sc);
-    sc[0] = T::product(ck + at, 0, q, sc[0]);
+  // keys first .. + 31: their scores, which become weights, relative to the row's maximum
+  auto weigh = [&](float16v (&sc)[1], int first) __attribute__((always_inline)) {
     if (first + 32 > b.fewest) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -253,7 +287,46 @@ __global__ __launch_bounds__(64 * WAVES, COLS == 1 ? 2 : 1) void packed_fwd_f32_
       sc[0][e] = fast_exp2(fmaf(sc[0][e], c, -m));
       l += sc[0][e];
     }
-    T::add(rv + at, RB::NT * T::G::TB, sc[0], o);
+  };
+  if constexpr (COLS == 1) {
+    for (int i = b.from; i < b.to; ++i) {
+      const unsigned at = (unsigned)next_stage<PS::NST>(i, b.from, b.to, ask) * PS::STAGE;
+      const int first = RB::KEYS * i;
+      if (first >= b.most) continue;
+      float16v sc[1];
+      zero_acc(sc);
+      sc[0] = T::product(ck + at, 0, q, sc[0]);
+      weigh(sc, first);
+      T::add(rv + at, RB::NT * T::G::TB, sc[0], o);
+    }
+  } else {
+    for (int i = b.from; i < own_to; ++i) {
+      const int first = RB::KEYS * i + 32 * col, next = first + RB::KEYS, st = OS::NST == 1 ? 0 : (i - b.from) & 1;
+      const bool more = i + 1 < own_to;
+      const unsigned at = (unsigned)st * OS::STAGE;
+      read_and_in_flight<OS::NST == 1 ? OS::N : 0>();   // (k is here; the other stage's reads as well)
+      if (OS::NST == 2 && more) {
+        os.ask_k(next, st ^ 1, lane);
+        os.ask_v(next, st ^ 1, lane);
+      }
+      float16v sc[1];
+      zero_acc(sc);
+      sc[0] = T::product(ck + at, 0, q, sc[0]);
+      if (OS::NST == 1) {
+        read_and_in_flight<OS::N>();                    // (k has been read)
+        if (more) os.ask_k(next, 0, lane);
+      }
+      weigh(sc, first);
+      if (OS::NST == 1) {
+        if (more) read_and_in_flight<OS::N>();
+        else read_and_in_flight<0>();                   // (v is here)
+      }
+      T::add(rv + at, RB::NT * T::G::TB, sc[0], o);
+      if (OS::NST == 1 && more) {
+        read_and_in_flight<OS::N>();                    // (v has been read)
+        os.ask_v(next, 0, lane);
+      }
+    }
   }
   l += other_half(l);
   const long n = s.q0 + b.me.i, r = n * a.heads + b.me.h, p = (long)b.share * a.q_rows * a.heads + r;
