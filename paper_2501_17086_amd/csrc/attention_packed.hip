@@ -1301,17 +1301,14 @@ Layout layout(const PackedAttnArgs& a, const Shares& n) {
 
 }  // namespace
 
-size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared) {
-  const Shares n = shares(dtype, a);
-  if (shared) *shared = n.rows > 1 || n.keys > 1;
-  return layout(a, n).total;
-}
+size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a) { return layout(a, shares(dtype, a)).total; }
 
-hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* workspace, hipStream_t s) {
+hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* workspace, size_t bytes, hipStream_t s) {
   PackedAttnArgs a = with_divisors(args);
   if (a.q_rows == 0) return hipSuccess;
   const Shares n = shares(dtype, a);
   const Layout l = layout(a, n);
+  if (bytes < l.total) return hipErrorInvalidValue;
   a.shares = n.rows;
   a.part_stats = reinterpret_cast<float*>(workspace);
   a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.shares);
@@ -1323,10 +1320,11 @@ hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& args, void* w
   return hipGetLastError();
 }
 
-hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& args, void* workspace, hipStream_t s) {
+hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& args, void* workspace, size_t bytes, hipStream_t s) {
   PackedAttnArgs a = with_divisors(args);
   const Shares n = shares(dtype, a);
   const Layout l = layout(a, n);
+  if (bytes < l.total) return hipErrorInvalidValue;
   a.dsum = reinterpret_cast<float*>(workspace);
   a.nlse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.stats);
   a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + l.shares);

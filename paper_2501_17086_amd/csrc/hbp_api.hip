@@ -107,19 +107,20 @@ PackedAttnArgs packed_sizes(const hbp_desc* d, long layers) {
   a.scale = 1.0f / sqrtf((float)head_w(d));
   return a;
 }
-// What any number of layers at a time may need: few of them share work out further, which needs room that many do not.
+// What any number of layers at a time may need.  The need does not grow with their number: few share work out, which takes room, many do
+// not, and in fp32 wider blocks, whose steps are shorter, make shares out again of what narrow ones had not (fp32, sequences of 128, 8
+// heads of 64 on 4: none for 1 to 3 layers of 512 tokens, shares for 4 to 16, none from 17 on).
 size_t packed_ws(const hbp_desc* d) {
-  size_t most = packed_attn_ws_bytes(d->dtype, packed_sizes(d, d->L / 2));
-  bool shared = true;
-  for (long n = 1; n < d->L / 2 && shared; ++n) {
-    const size_t need = packed_attn_ws_bytes(d->dtype, packed_sizes(d, n), &shared);
+  size_t most = 0;
+  for (long n = 1; n <= d->L / 2; ++n) {
+    const size_t need = packed_attn_ws_bytes(d->dtype, packed_sizes(d, n));
     if (need > most) most = need;
   }
   return most;
 }
 
 struct Workspace {
-  size_t off_v, off_da, off_part, off_scan, off_wt, off_pre, off_m, off_tmp, off_dqkv, off_dsum, off_packed, off_counter, total;
+  size_t off_v, off_da, off_part, off_scan, off_wt, off_pre, off_m, off_tmp, off_dqkv, off_dsum, off_packed, packed, off_counter, total;
 };
 
 // The partial sums of a parameter gradient take at most this much: shares are taken to fill the chip, and what does that without
@@ -245,7 +246,8 @@ Workspace carve(const hbp_desc* d) {
   if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * d->heads * 4, 256);
   // shared key/value heads: what the attention over packed sequences needs
   w.off_packed = o;
-  if (tfm(d) && key_heads(d) < d->heads) o = align_up(o + packed_ws(d), 256);
+  if (tfm(d) && key_heads(d) < d->heads) w.packed = packed_ws(d);
+  o = align_up(o + w.packed, 256);
   // the chain kernels' counters and what their workgroups exchange (4 MB)
   w.off_counter = o;
   if (recurrent(d) && d->dtype == HBP_BF16) o += RECURRENT_COUNTER_BYTES + recurrent_ring_bytes();
@@ -517,7 +519,7 @@ hbp_status tfm_stage1(const hbp_desc* d, const hbp_buffers* b, const Workspace& 
   if (ja_hi > ja_lo) {
     ProfScope ps(HBP_PROF_ATTN, s);
     if (key_heads(d) < d->heads)
-      HBP_TRY(launch_packed_attn_bwd(d->dtype, packed_args(d, b, w, ja_lo, ja_hi), at(b->workspace, w.off_packed), s));
+      HBP_TRY(launch_packed_attn_bwd(d->dtype, packed_args(d, b, w, ja_lo, ja_hi), at(b->workspace, w.off_packed), w.packed, s));
     else
       HBP_TRY(launch_attn_bwd(d->dtype, attn_args(d, b, w, ja_lo, ja_hi), s));
     if (turned(d)) {
@@ -980,7 +982,7 @@ hbp_status run_forward(const hbp_desc* d, hbp_buffers* b, void* stream, int wait
         ProfScope ps(HBP_PROF_ATTN, s);
         if (turned(d)) HBP_RUN(turn_qk(d, at(b->qkv, (size_t)wl * N * W * es), 1, 0, s));
         if (key_heads(d) < d->heads)
-          HBP_TRY(launch_packed_attn_fwd(d->dtype, packed_args(d, b, w, wl, wl + 1), at(b->workspace, w.off_packed), s));
+          HBP_TRY(launch_packed_attn_fwd(d->dtype, packed_args(d, b, w, wl, wl + 1), at(b->workspace, w.off_packed), w.packed, s));
         else
           HBP_TRY(launch_attn_fwd(d->dtype, attn_args(d, b, w, wl, wl + 1), s));
       }
@@ -1615,7 +1617,7 @@ hbp_status hbp_attention_forward(const hbp_attention_desc* d, const hbp_attentio
   HBP_RUN(attention_call(d, b, false, &a));
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps(HBP_PROF_ATTN, s);
-  HBP_TRY(launch_packed_attn_fwd(d->dtype, a, b->workspace, s));
+  HBP_TRY(launch_packed_attn_fwd(d->dtype, a, b->workspace, b->workspace_bytes, s));
   return HBP_OK;
 }
 
@@ -1624,7 +1626,7 @@ hbp_status hbp_attention_backward(const hbp_attention_desc* d, const hbp_attenti
   HBP_RUN(attention_call(d, b, true, &a));
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps(HBP_PROF_ATTN, s);
-  HBP_TRY(launch_packed_attn_bwd(d->dtype, a, b->workspace, s));
+  HBP_TRY(launch_packed_attn_bwd(d->dtype, a, b->workspace, b->workspace_bytes, s));
   return HBP_OK;
 }
 

@@ -266,9 +266,10 @@ struct PackedAttnArgs {
   int q_len, k_len;
   Divisor by_group, by_kv, by_seqs;
 };
-size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a, bool* shared = nullptr);     // shared: part of it are shares
-hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
-hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, hipStream_t s);
+// The launchers refuse (hipErrorInvalidValue, nothing launched) a workspace of fewer bytes than packed_attn_ws_bytes.
+size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a);
+hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, size_t bytes, hipStream_t s);
+hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, size_t bytes, hipStream_t s);
 
 // Few-row bf16 product with both operands K-contiguous: C[M,N] = epilogue(A[M,K] . Bt[N,K]^T).
 // Modes EPI_STORE, EPI_ACT_TANH, EPI_MUL_AUX, EPI_MUL_1MZ2, EPI_ADD_AUX; aux is bf16 [M,N] with row stride ldaux.
