@@ -243,11 +243,19 @@ __device__ __forceinline__ int wave_total(int v) {
 // sequence's tiles, and s is found 64 candidates at a time.  Levels / this, us, ragged: forward of 16384 sequences of 9, 4 heads of
 // 64, 1945 / 193; backward of 4096 of 64, 12 heads, 2870 / 1375; forward of 200 of 1000, 8 heads, 487 / 454; the other way round
 // backward of 100 of 1000, 8 heads, 1062 / 1107; forward of 24 of 700, 16 heads on 4, 55 / 66.
+// A dimension of a grid holds fewer than 2^32 threads, and what is launched beyond is cut off without an error: x has at most 2^22 workgroups
+// (of 512 threads or fewer), more of them go on in z.  The last ones there may have no tile.
+constexpr int GRID_X_LOG = 22;
+__device__ __forceinline__ unsigned workgroup_id() { return (blockIdx.z << GRID_X_LOG) + blockIdx.x; }
+inline dim3 grid_of(unsigned workgroups, int shares = 1) {
+  const unsigned most = 1u << GRID_X_LOG, x = workgroups < most ? workgroups : most;
+  return dim3(x, (unsigned)shares, (workgroups + most - 1) / most);
+}
 struct Tile { int hk, t; Seq s; bool exists; };
 constexpr int LEVELLED = 128;
 __device__ __forceinline__ int tiles_in(int len, int per) { return (int)((unsigned)(len + per - 1) / (unsigned)per); }   // (per: a power of two)
 template <bool KEYS>
-__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane, unsigned id = blockIdx.x) {
+__device__ __forceinline__ Tile find_tile(const PackedAttnArgs& a, int per, int lane, unsigned id = workgroup_id()) {
   Tile x;
   int j = (int)a.by_kv.quotient(id);
   x.hk = (int)id - j * a.kv_heads;

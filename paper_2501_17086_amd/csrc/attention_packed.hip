@@ -935,7 +935,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_fwd_short_kernel(PackedA
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   OwnRows b;
-  if (!b.find(a, blockIdx.x * WAVES + wave, lane)) return;
+  if (!b.find(a, workgroup_id() * WAVES + wave, lane)) return;
   const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3, steps = (b.most + 31) >> 5;
   unsigned char* const ring = rings + wave * (A::NST * A::STAGE);
@@ -1019,7 +1019,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dq_short_kernel(PackedAt
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   OwnRows b;
-  if (!b.find(a, blockIdx.x * WAVES + wave, lane)) return;
+  if (!b.find(a, workgroup_id() * WAVES + wave, lane)) return;
   const Seq& sq = b.x.s;
   const int dh8 = a.dh >> 3, steps = (b.most + 31) >> 5;
   unsigned char* const ring = rings + wave * (A::NST * A::STAGE);
@@ -1104,7 +1104,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_dkdv_short_kernel(Packed
   __shared__ __attribute__((aligned(1024))) unsigned char rings[NW * OWN];
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const Tile x = find_tile<true>(a, 32, lane, blockIdx.x * NW + wave);
+  const Tile x = find_tile<true>(a, 32, lane, workgroup_id() * NW + wave);
   if (!x.exists) return;
   const Seq& sq = x.s;
   const int w0 = 32 * x.t, keys_left = sq.nk - w0, nq = sq.nq, shift = sq.nk - nq, dh8 = a.dh >> 3;
@@ -1220,34 +1220,34 @@ bool alone(const PackedAttnArgs& a) {
 template <int W>
 hipError_t fwd_mfma(const PackedAttnArgs& a, hipStream_t s) {
   if (alone<false>(a))
-    packed_fwd_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
+    packed_fwd_short_kernel<W><<<grid_of((tile_grid<false>(a, 32) + WAVES - 1) / WAVES), 64 * WAVES, 0, s>>>(a);
   else if (W > 64 && wide_blocks<false>(a, TALL, 1024, 2 * CUS) && a.k_rows / a.seqs > FEW)
-    packed_fwd_tall_kernel<(W > 64 ? W : 128)><<<tile_grid<false>(a, TALL), 64 * WAVES, 0, s>>>(a);
+    packed_fwd_tall_kernel<(W > 64 ? W : 128)><<<grid_of(tile_grid<false>(a, TALL)), 64 * WAVES, 0, s>>>(a);
   else if (wide_blocks<false>(a, 256, 64, CUS))
-    packed_fwd_mfma_kernel<W, 1><<<tile_grid<false>(a, 256), 64 * WAVES, 0, s>>>(a);
+    packed_fwd_mfma_kernel<W, 1><<<grid_of(tile_grid<false>(a, 256)), 64 * WAVES, 0, s>>>(a);
   else
-    packed_fwd_mfma_kernel<W, 4><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+    packed_fwd_mfma_kernel<W, 4><<<grid_of(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int W>
 hipError_t dq_mfma(const PackedAttnArgs& a, hipStream_t s) {
   constexpr int NW = W <= 64 ? 4 : 8;
   if (alone<false>(a))
-    packed_dq_short_kernel<W><<<(tile_grid<false>(a, 32) + WAVES - 1) / WAVES, 64 * WAVES, 0, s>>>(a);
+    packed_dq_short_kernel<W><<<grid_of((tile_grid<false>(a, 32) + WAVES - 1) / WAVES), 64 * WAVES, 0, s>>>(a);
   else if (wide_blocks<false>(a, 256, 64, CUS))
-    packed_dq_mfma_kernel<W, 1, NW><<<tile_grid<false>(a, 32 * NW), 64 * NW, 0, s>>>(a);
+    packed_dq_mfma_kernel<W, 1, NW><<<grid_of(tile_grid<false>(a, 32 * NW)), 64 * NW, 0, s>>>(a);
   else
-    packed_dq_mfma_kernel<W, 4, WAVES><<<dim3(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+    packed_dq_mfma_kernel<W, 4, WAVES><<<grid_of(tile_grid<false>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int W>
 hipError_t dkdv_mfma(const PackedAttnArgs& a, hipStream_t s) {
   if (alone<true>(a))
-    packed_dkdv_short_kernel<W><<<(tile_grid<true>(a, 32) + (W > 64 ? 4 : WAVES) - 1) / (W > 64 ? 4 : WAVES), 64 * (W > 64 ? 4 : WAVES), 0, s>>>(a);
+    packed_dkdv_short_kernel<W><<<grid_of((tile_grid<true>(a, 32) + (W > 64 ? 4 : WAVES) - 1) / (W > 64 ? 4 : WAVES)), 64 * (W > 64 ? 4 : WAVES), 0, s>>>(a);
   else if (wide_blocks<true>(a, 128, 64, CUS))
-    packed_dkdv_mfma_kernel<W, 2><<<tile_grid<true>(a, 128), 64 * WAVES, 0, s>>>(a);
+    packed_dkdv_mfma_kernel<W, 2><<<grid_of(tile_grid<true>(a, 128)), 64 * WAVES, 0, s>>>(a);
   else
-    packed_dkdv_mfma_kernel<W, 4><<<dim3(tile_grid<true>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
+    packed_dkdv_mfma_kernel<W, 4><<<grid_of(tile_grid<true>(a, 64), a.shares), 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 

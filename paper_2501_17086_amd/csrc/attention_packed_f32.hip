@@ -600,24 +600,24 @@ __global__ __launch_bounds__(64 * WAVES, TURNS > 1 || W > 64 ? 1 : 2) void packe
 hipError_t launch_packed_fwd_f32(const PackedAttnArgs& a, hipStream_t s) {
   return with_width(a.dh, [&](auto w) {
     constexpr int W = decltype(w)::value;
-    if (f32_wide<false>(a)) packed_fwd_f32_kernel<W, 1><<<dim3(tile_grid<false>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
-    else packed_fwd_f32_kernel<W, 4><<<dim3(tile_grid<false>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
+    if (f32_wide<false>(a)) packed_fwd_f32_kernel<W, 1><<<grid_of(tile_grid<false>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
+    else packed_fwd_f32_kernel<W, 4><<<grid_of(tile_grid<false>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 hipError_t launch_packed_dq_f32(const PackedAttnArgs& a, hipStream_t s) {
   return with_width(a.dh, [&](auto w) {
     constexpr int W = decltype(w)::value;
-    if (f32_wide<false>(a)) packed_dq_f32_kernel<W, 1><<<dim3(tile_grid<false>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
-    else packed_dq_f32_kernel<W, 4><<<dim3(tile_grid<false>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
+    if (f32_wide<false>(a)) packed_dq_f32_kernel<W, 1><<<grid_of(tile_grid<false>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
+    else packed_dq_f32_kernel<W, 4><<<grid_of(tile_grid<false>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 hipError_t launch_packed_dkdv_f32(const PackedAttnArgs& a, hipStream_t s) {
   return with_width(a.dh, [&](auto w) {
     constexpr int W = decltype(w)::value;
-    if (f32_wide<true>(a)) packed_dkdv_f32_kernel<W, 1><<<dim3(tile_grid<true>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
-    else packed_dkdv_f32_kernel<W, 4><<<dim3(tile_grid<true>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
+    if (f32_wide<true>(a)) packed_dkdv_f32_kernel<W, 1><<<grid_of(tile_grid<true>(a, 128), a.shares), 64 * WAVES, 0, s>>>(a);
+    else packed_dkdv_f32_kernel<W, 4><<<grid_of(tile_grid<true>(a, 32), a.shares), 64 * WAVES, 0, s>>>(a);
     return hipGetLastError();
   });
 }
