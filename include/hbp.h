@@ -409,7 +409,7 @@ typedef struct {
   int32_t kv_heads;          /* heads % kv_heads == 0; 0: as many as heads */
   int32_t reserved;          /* 0 */
   hbp_rotary_desc rotary;    /* dims = 0: no positions (struct_size 0 will do) */
-  const int32_t* positions;  /* DEVICE [N], or NULL: a token's place in its sequence */
+  const int32_t* positions;  /* DEVICE [N], or NULL: a token's place in its sequence.  NULL where dims = 0 */
 } hbp_transformer_desc;
 
 const char* hbp_status_string(hbp_status s);

@@ -163,13 +163,22 @@ def make_desc(kind: str, dtype: str, act: str, norm: str, L: int, N: int, d: int
               gamma: float = 0.0, lambda_token: bool = False, post: str = "none", heads: int = 0,
               causal: bool = True, seq_len: int = 0, kv_heads: int = 0, rotary: Optional[hbp_rotary_desc] = None,
               positions=None) -> hbp_desc:
-    """kv_heads, rotary (make_rotary) and positions (int32 [N] on the GPU, kept alive by the caller): an hbp_transformer_desc."""
+    """kv_heads, rotary (make_rotary) and positions (int32 [N] on the GPU, kept alive by the caller; with rotary only): an
+    hbp_transformer_desc."""
+    at = None
+    if positions is not None:
+        import torch
+        if rotary is None:
+            raise ValueError("positions: given without rotary, which turns by them")
+        if not positions.is_cuda:
+            raise ValueError(f"positions: expected a tensor on the GPU, got {positions.device}")
+        at = _plain("positions", positions, (N,), torch.int32, positions.get_device())
     if kv_heads or rotary is not None:
         base = make_desc(kind, dtype, act, norm, L, N, d, d_ff, d_in, lambda_channel, loss_every_state, eps, gamma, lambda_token,
                          post, heads, causal, seq_len)
         base.struct_size = C.sizeof(hbp_transformer_desc)
         return hbp_transformer_desc(*[getattr(base, f) for f, _ in hbp_desc._fields_], kv_heads, 0,
-                                    hbp_rotary_desc() if rotary is None else rotary, _ptr(positions))
+                                    hbp_rotary_desc() if rotary is None else rotary, at)
     return hbp_desc(C.sizeof(hbp_desc), KIND[kind], BF16 if dtype == "bf16" else F32,
                     ACT[act], NORM[norm],
                     LAMBDA_TOKEN if lambda_token else LAMBDA_CHANNEL if lambda_channel else LAMBDA_ONE,

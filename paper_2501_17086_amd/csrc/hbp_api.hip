@@ -285,6 +285,7 @@ hbp_status check_desc(const hbp_desc* d) {
     if (d->post == HBP_POST_RELU || head_w(d) % 8) return HBP_E_UNSUPPORTED;
     if (const hbp_transformer_desc* x = extended(d)) {
       if (x->kv_heads < 0 || (x->kv_heads && d->heads % x->kv_heads) || x->reserved != 0) return HBP_E_INVALID_ARG;
+      if (x->positions && !turned(d)) return HBP_E_INVALID_ARG;
       if (turned(d)) {
         const hbp_status st = check_rotary(&x->rotary, d->dtype, (int)head_w(d));
         if (st != HBP_OK) return st;
