@@ -226,6 +226,7 @@ class Problem:
     lse: "object" = None
     dWqkv: "object" = None
     dWo: "object" = None
+    positions: "object" = None       # what desc.positions points to, if anything
 
     def buffers(self) -> hbp_buffers:
         ws = self.workspace
@@ -571,10 +572,10 @@ def profile_read() -> dict:
     return {PROF_CLASSES[i]: (ms[i], cnt[i]) for i in range(n)}
 
 
-def allocate(w, inputs, device="cuda:0", N: Optional[int] = None) -> Problem:
+def allocate(w, inputs, device="cuda:0", N: Optional[int] = None, positions=None) -> Problem:
     """Device tensors for workload `w` (a synth.Workload) from make_inputs()'s
     arrays: uploads parameters, x[0], xin and e; allocates the saved state,
-    outputs and workspace."""
+    outputs and workspace.  positions: int32 [N] on that device, for a stack with rotary."""
     import torch
     dt = torch.bfloat16 if w.dtype == "bf16" else torch.float32
     N = inputs["x0"].shape[0] if N is None else N
@@ -592,7 +593,7 @@ def allocate(w, inputs, device="cuda:0", N: Optional[int] = None) -> Problem:
                      loss_every_state=w.loss_every_state, eps=w.eps, post=getattr(w, "post", "none"),
                      heads=getattr(w, "heads", 0), causal=getattr(w, "causal", True), seq_len=getattr(w, "seq_len", 0),
                      gamma=getattr(w, "gamma", 0.0), kv_heads=getattr(w, "kv_heads", 0),
-                     rotary=make_rotary(**w.rotary) if getattr(w, "rotary", None) else None)
+                     rotary=make_rotary(**w.rotary) if getattr(w, "rotary", None) else None, positions=positions)
     L, d, dff = w.L, w.d, w.d_ff
     tfm = w.kind == "transformer"
     Li = L // 2 if tfm else L        # rows of the inner state: one per MLP block
@@ -613,6 +614,7 @@ def allocate(w, inputs, device="cuda:0", N: Optional[int] = None) -> Problem:
         dW1=torch.zeros(inputs["W1"].shape, dtype=torch.float32, device=dev),
         dW2=None if inputs["W2"] is None else torch.zeros(inputs["W2"].shape, dtype=torch.float32, device=dev),
         dU=None if inputs["U"] is None else torch.zeros(inputs["U"].shape, dtype=torch.float32, device=dev),
+        positions=positions,
     )
     if tfm:
         p.Wqkv, p.Wo = up(inputs["Wqkv"]), up(inputs["Wo"])
