@@ -1,0 +1,58 @@
+"""CPU-only: what the binding refuses of an attention call's workspace, with stand-ins for tensors on the GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2501_17086_amd import binding as B
+
+
+class OnGpu:
+    """Looks like a tensor; nothing reads it."""
+
+    def __init__(self, shape, dtype=torch.float32, device=0, contiguous=True):
+        self.shape, self.dtype, self.place, self.contiguous = torch.Size(shape), dtype, device, contiguous
+        self.device, self.is_cuda = "cpu" if device < 0 else f"cuda:{device}", device >= 0
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def get_device(self):
+        return self.place
+
+    def stride(self):
+        return tuple(self.shape[i + 1:].numel() for i in range(len(self.shape)))
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+def attention(**kw):
+    n, m, H, K, D = 6, 9, 4, 2, 16
+    desc = B.hbp_attention_desc(C.sizeof(B.hbp_attention_desc), B.F32, H, K, D, 1, 0.25, 0.0, 1, n, m)
+    t = dict(q=OnGpu((n, H, D)), k=OnGpu((m, K, D)), v=OnGpu((m, K, D)), o=OnGpu((n, H, D)), lse=OnGpu((n, H)),
+             workspace=OnGpu((B.attention_workspace_size(desc),), torch.uint8))
+    t.update(kw)
+    return B.Attention(desc, **t)
+
+
+def test_the_stand_ins_pass_as_they_are():
+    b = B.hbp_attention_buffers.from_buffer_copy(attention().buffers())
+    assert b.q.data == b.lse == b.workspace == 1 << 20 and b.workspace_bytes == B.attention_workspace_size(attention().desc)
+    assert B.hbp_attention_buffers.from_buffer_copy(attention(workspace=None).buffers()).workspace_bytes == 0
+
+
+@pytest.mark.parametrize("ws", [OnGpu((1 << 16,), torch.uint8, device=-1), OnGpu((1 << 16,), torch.uint8, device=1),
+                                OnGpu((1 << 16,), torch.uint8, contiguous=False)], ids=["host", "other_gpu", "strided"])
+def test_a_workspace_elsewhere_is_refused(ws):
+    with pytest.raises(ValueError, match="workspace"):
+        attention(workspace=ws).buffers()
