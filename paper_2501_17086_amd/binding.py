@@ -504,6 +504,8 @@ class Attention:
             grads = (*_heads("dout", dout, rows, dtype, device), *_heads("dq", self.dq, rows, dtype, device),
                      *_heads("dk", self.dk, kv, dtype, device), *_heads("dv", self.dv, kv, dtype, device))
         off = (d.seqs + 1,)
+        if self.lse is None:
+            raise ValueError(f"lse: expected {rows[:2]} torch.float32 on GPU {device}, got none")
         if ws is not None and (ws.get_device() != device or not ws.is_contiguous()):
             raise ValueError(f"workspace: expected a contiguous tensor on GPU {device}, got one on {ws.device} with strides {ws.stride()}")
         return _pack_attention(_ATTENTION_SIZE, *_heads("q", q, rows, dtype, device), *_heads("k", self.k, kv, dtype, device),

@@ -1,4 +1,4 @@
-"""CPU-only: what the binding refuses of an attention call's workspace, with stand-ins for tensors on the GPU."""
+"""CPU-only: what the binding refuses of an attention call's workspace and statistics, with stand-ins for tensors on the GPU."""
 import ctypes as C
 
 import pytest
@@ -56,3 +56,8 @@ def test_the_stand_ins_pass_as_they_are():
 def test_a_workspace_elsewhere_is_refused(ws):
     with pytest.raises(ValueError, match="workspace"):
         attention(workspace=ws).buffers()
+
+
+def test_missing_statistics_are_refused():
+    with pytest.raises(ValueError, match="lse: .* got none"):
+        attention(lse=None).buffers()
