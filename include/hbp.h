@@ -329,6 +329,7 @@ typedef struct { void* data; int64_t row_stride, head_stride; } hbp_heads;
  *   BASE      base replaced by base s^(dims / (dims - 2))
  *   BY_PARTS  f_i (w + (1 - w) / s), w = (original f_i / (2 pi) - low) / (high - low) within 0 .. 1: pairs that turn at
  *             least `high` times within `original` positions stay, those that turn at most `low` times are slowed by s.
+ * Frequencies of 2^969 and more (a base or a factor next to 0) are refused.
  * Angles are formed and reduced in 64 bits, so that far positions turn as exactly as near ones. */
 typedef enum { HBP_ROTARY_HALF = 0, HBP_ROTARY_INTERLEAVED = 1 } hbp_rotary_layout;
 typedef enum { HBP_ROTARY_PLAIN = 0, HBP_ROTARY_LINEAR = 1, HBP_ROTARY_BASE = 2, HBP_ROTARY_BY_PARTS = 3 } hbp_rotary_scaling;

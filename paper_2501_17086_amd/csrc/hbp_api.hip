@@ -43,6 +43,9 @@ inline int key_heads(const hbp_desc* d) {
 inline long qkv_w(const hbp_desc* d) { return d->d + 2 * key_heads(d) * head_w(d); }    // width of a [q | k | v] row
 inline bool turned(const hbp_desc* d) { return extended(d) && extended(d)->rotary.dims != 0; }
 
+double rotary_base(const hbp_rotary_desc* r) {
+  return r->scaling == HBP_ROTARY_BASE ? r->base * pow(r->factor, (double)r->dims / (r->dims - 2)) : r->base;
+}
 hbp_status check_rotary(const hbp_rotary_desc* r, int dtype, int dh) {
   if (!r) return HBP_E_NULL;
   if (r->struct_size != sizeof(hbp_rotary_desc)) return HBP_E_INVALID_ARG;
@@ -56,6 +59,11 @@ hbp_status check_rotary(const hbp_rotary_desc* r, int dtype, int dh) {
   if (r->scaling == HBP_ROTARY_BY_PARTS &&
       (!(r->low < r->high) || !std::isfinite(r->high - r->low) || !(r->original > 0) || !std::isfinite(r->original)))
     return HBP_E_INVALID_ARG;
+  // the largest frequency: any position (2^53 of them) times it has to be finite
+  const double base = rotary_base(r);
+  double most = r->dims > 2 && base < 1 ? pow(base, -(double)(r->dims - 2) / r->dims) : 1;
+  if (r->scaling == HBP_ROTARY_LINEAR || (r->scaling == HBP_ROTARY_BY_PARTS && r->factor < 1)) most /= r->factor;
+  if (!(most < ldexp(1.0, 969))) return HBP_E_INVALID_ARG;
   if (dh % 8 || dh > 2 * ROTARY_PAIRS) return HBP_E_UNSUPPORTED;
   return HBP_OK;
 }
@@ -63,8 +71,7 @@ hbp_status check_rotary(const hbp_rotary_desc* r, int dtype, int dh) {
 // frequencies in turns per position
 void rotary_turns(const hbp_rotary_desc* r, double* turns) {
   const double two_pi = 6.283185307179586476925286766559;
-  double base = r->base;
-  if (r->scaling == HBP_ROTARY_BASE) base *= pow(r->factor, (double)r->dims / (r->dims - 2));
+  const double base = rotary_base(r);
   // base^(-2 i / dims) from the powers for i = 1, 2, 4, ..: seven roundings at most, and seven calls of pow
   const int pairs = r->dims / 2;
   turns[0] = 1.0 / two_pi;

@@ -52,3 +52,28 @@ def test_positions_of_a_stack_are_refused_where_nothing_turns():
 def test_positions_of_a_stack_are_one_int32_for_every_token(bad):
     with pytest.raises(ValueError, match="positions"):
         B.make_desc(**STACK, rotary=B.make_rotary(32), positions=bad)
+
+
+def rotary_status(**kw):
+    """Of a call on no rows."""
+    r = B.make_rotary(**kw)
+    x, y = B.hbp_heads(1 << 20, 1024, 64), B.hbp_heads(1 << 24, 1024, 64)
+    return B.lib().hbp_rotary(C.byref(r), B.F32, 0, 4, 64, C.byref(x), C.byref(y), None, 0, 0, 0, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(dims=64, base=5e-324), INVALID),                                     # base^(-62/64) passes 2^1023
+    (dict(dims=64, base=1e-290), OK),
+    (dict(dims=2, base=5e-324), OK),                                           # one pair, which turns by 1 whatever the base
+    (dict(dims=64, scaling="linear", factor=1e-300), INVALID), (dict(dims=64, scaling="linear", factor=1e-280), OK),
+    (dict(dims=64, scaling="base", factor=1e-300), INVALID),                   # the changed base is 1e-306
+    (dict(dims=4, scaling="base", factor=1e-200), INVALID),                    # and here 0
+    (dict(dims=64, scaling="by_parts", factor=1e-300, original=64.0), INVALID), (dict(dims=64, scaling="base", factor=1e300), OK),
+])
+def test_frequencies_that_no_number_holds_are_refused(kw, want):
+    """They turned rows into NaN."""
+    assert rotary_status(**kw) == want
+    n = C.c_size_t(0)
+    if kw["dims"] == 64:
+        d = B.make_desc(**dict(STACK, d=256), rotary=B.make_rotary(**kw))
+        assert status(d) == want
