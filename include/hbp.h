@@ -372,7 +372,7 @@ typedef struct {
   int32_t kv_heads;
   int32_t dh;                /* head width: a multiple of 8, at most 128 */
   int32_t causal;            /* 0 or 1 */
-  float scale;               /* > 0, finite; usually 1 / sqrt(dh) */
+  float scale;               /* > 0, at most 2^127; usually 1 / sqrt(dh) */
   float reserved;            /* 0 */
   int64_t seqs;              /* >= 1 */
   int64_t q_rows, k_rows;    /* rows of all sequences together, 0 .. 2^24 */

@@ -1546,7 +1546,7 @@ hbp_status check_attention(const hbp_attention_desc* d) {
   if (d->dtype != HBP_F32 && d->dtype != HBP_BF16) return HBP_E_INVALID_ARG;
   if (d->heads <= 0 || d->kv_heads <= 0 || d->heads % d->kv_heads || d->dh <= 0) return HBP_E_INVALID_ARG;
   if (d->causal != 0 && d->causal != 1) return HBP_E_INVALID_ARG;
-  if (!(d->scale > 0.f) || !std::isfinite(d->scale) || d->reserved != 0.f) return HBP_E_INVALID_ARG;
+  if (!(d->scale > 0.f && d->scale <= 0x1p127f) || d->reserved != 0.f) return HBP_E_INVALID_ARG;       // (times log2 e: finite)
   if (d->seqs < 1 || d->q_rows < 0 || d->k_rows < 0) return HBP_E_INVALID_ARG;
   if (d->dh % 8 || d->dh > 128) return HBP_E_UNSUPPORTED;
   if (d->seqs > (1 << 24) || d->q_rows > (1 << 24) || d->k_rows > (1 << 24) || d->heads > 4096) return HBP_E_UNSUPPORTED;

@@ -61,3 +61,11 @@ def test_a_workspace_elsewhere_is_refused(ws):
 def test_missing_statistics_are_refused():
     with pytest.raises(ValueError, match="lse: .* got none"):
         attention(lse=None).buffers()
+
+
+@pytest.mark.parametrize("scale,status", [(2.0 ** 127, 0), (2.0 ** 127 * 1.001, 1), (3.0e38, 1)])
+def test_a_scale_that_does_not_take_the_exponents_base_is_refused(scale, status):
+    """scale log2 e was infinite in fp32, and a score of 0 not a number."""
+    n = C.c_size_t(0)
+    desc = B.hbp_attention_desc(C.sizeof(B.hbp_attention_desc), B.BF16, 4, 2, 64, 1, scale, 0.0, 1, 8, 8)
+    assert B.lib().hbp_attention_workspace_size(C.byref(desc), C.byref(n)) == status
