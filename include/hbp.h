@@ -317,8 +317,9 @@ hbp_status hbp_train_step(const hbp_desc* desc, int k, hbp_buffers* bufs, const 
 
 /* Rows of heads: channel c of head h of row n is element data[n row_stride + h head_stride + c] of the storage type.
  * data is 16-byte aligned, strides are multiples of 8, not negative, rows less than 2^24 apart (the stride of a single row or
- * head does not matter); rows or heads of a tensor that is written must not overlap, those of an input may (a stride of
- * 0 reads one row again and again).  q, k and v may so lie side by side in the rows of one projection's output, or head after head. */
+ * head does not matter).  Rows and heads of a tensor that is written must not overlap: all heads of a row lie before the next row,
+ * or all rows of a head before the next head.  Those of an input may (a stride of 0 reads one row again and again).  q, k and v
+ * may so lie side by side in the rows of one projection's output, or head after head. */
 typedef struct { void* data; int64_t row_stride, head_stride; } hbp_heads;
 
 /* Rotary positions: channel pair i < dims / 2 of every head of a row at position p turns by the angle p f_i,

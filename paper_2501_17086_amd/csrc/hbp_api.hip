@@ -1528,11 +1528,11 @@ hbp_status check_heads(const hbp_heads& x, int64_t rows, int heads, int dh, bool
   if (!one_row && (x.row_stride % 8 || x.row_stride >= (1 << 24))) return HBP_E_UNSUPPORTED;
   if (!one_head && (x.head_stride % 8 || x.head_stride >= (int64_t)1 << 40)) return HBP_E_UNSUPPORTED;
   if (written) {
-    const bool by_row = (one_head || x.head_stride >= dh) && (one_row || x.row_stride >= (one_head ? dh : heads * x.head_stride));
-    const bool by_head = (one_row || x.row_stride >= dh) && (one_head || x.head_stride >= (one_row ? dh : rows * x.row_stride));
-    // heads side by side, the last of a row followed by the next row before a whole head stride is over
-    const bool packed = !one_row && !one_head && x.head_stride >= dh && x.row_stride >= (heads - 1) * x.head_stride + dh;
-    if (!by_row && !by_head && !packed) return HBP_E_INVALID_ARG;
+    // heads side by side in a row and rows apart by all of them, or a head's rows behind one another and heads apart by all of those
+    const int64_t heads_end = one_head ? dh : (heads - 1) * x.head_stride + dh, rows_end = one_row ? dh : (rows - 1) * x.row_stride + dh;
+    const bool by_row = (one_head || x.head_stride >= dh) && (one_row || x.row_stride >= heads_end);
+    const bool by_head = (one_row || x.row_stride >= dh) && (one_head || x.head_stride >= rows_end);
+    if (!by_row && !by_head) return HBP_E_INVALID_ARG;
   }
   return HBP_OK;
 }

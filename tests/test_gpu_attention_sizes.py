@@ -36,3 +36,37 @@ def test_more_workgroups_than_one_dimension_of_a_grid_holds():
         ds = (2 * (D + 4) + 10) * R.F * (gd * vd).abs().sum(-1, keepdim=True) * 1.01 * scale
         R.assert_within(a.dq[r], torch.zeros_like(qd), ds * kd.abs() + 1e-37, "dq")
         R.assert_within(a.dk[r], torch.zeros_like(kd), ds * qd.abs() + 1e-37, "dk")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_heads_close_behind_one_another_are_no_overlap(dtype):
+    """Head after head, with room between rows and none behind a head's last row: written as any other layout."""
+    n, H, D = 37, 3, 64
+    row, head = D + 8, (n - 1) * (D + 8) + D
+    place = lambda: torch.full(((H - 1) * head + (n - 1) * row + D,), 12345.0, dtype=dtype, device="cuda")
+    x = normal((n, H, D), dtype, 5)
+    want, memory = torch.empty_like(x), place()
+    out = memory.as_strided((n, H, D), (row, head, 1))
+    rot = B.make_rotary(D)
+    B.hbp_rotary(rot, x, want)
+    B.hbp_rotary(rot, x, out)
+    assert torch.equal(out, want)
+    out.fill_(12345.0)
+    assert bool((memory == 12345.0).all())
+    q, k, v, do = (normal((n, H, D), dtype, s) for s in (6, 7, 8, 9))
+    a, b = B.make_attention(q, k, v), B.make_attention(q, k, v)
+    for name in ("o", "dq", "dk", "dv"):
+        setattr(b, name, place().as_strided((n, H, D), (row, head, 1)))
+    for t in (a, b):
+        B.hbp_attention_forward(t)
+        B.hbp_attention_backward(t, do)
+    for name in ("o", "lse", "dq", "dk", "dv"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+
+
+def test_heads_that_do_overlap_are_refused():
+    memory = torch.zeros(4096, device="cuda")
+    x = normal((5, 3, 64), torch.float32, 5)
+    for strides in ((72, 72 * 4 + 56, 1), (56, 512, 1), (64, 64, 1), (200, 72, 1), (0, 64, 1)):
+        with pytest.raises(B.HbpError):
+            B.hbp_rotary(B.make_rotary(64), x, memory.as_strided((5, 3, 64), strides))
