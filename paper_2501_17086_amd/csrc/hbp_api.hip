@@ -296,6 +296,7 @@ hbp_status check_desc(const hbp_desc* d) {
       if (turned(d)) {
         const hbp_status st = check_rotary(&x->rotary, d->dtype, (int)head_w(d));
         if (st != HBP_OK) return st;
+        if (d->heads + key_heads(d) > ROTARY_HEADS) return HBP_E_UNSUPPORTED;
       }
     }
     if (key_heads(d) < d->heads) {
@@ -1600,7 +1601,7 @@ hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, in
   HBP_RUN(check_rotary(rotary, dtype, dh));
   if (!x || !out) return HBP_E_NULL;
   if (rows < 0 || heads <= 0 || period < 0 || (inverse != 0 && inverse != 1)) return HBP_E_INVALID_ARG;
-  if (rows > (1 << 24) || heads > 65535 || first > ((int64_t)1 << 52) || first < -((int64_t)1 << 52)) return HBP_E_UNSUPPORTED;
+  if (rows > (1 << 24) || heads > ROTARY_HEADS || first > ((int64_t)1 << 52) || first < -((int64_t)1 << 52)) return HBP_E_UNSUPPORTED;
   HBP_RUN(check_heads(*x, rows, heads, dh, false));
   HBP_RUN(check_heads(*out, rows, heads, dh, true));
   if (rows == 0) return HBP_OK;

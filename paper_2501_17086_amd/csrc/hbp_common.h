@@ -221,7 +221,7 @@ hipError_t launch_attn_fwd(int dtype, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_bwd(int dtype, const AttnArgs& a, hipStream_t s);
 
 // Rotary positions (rotary.hip): rows of heads turned pair by pair; x == y turns in place.  Strides in elements.
-constexpr int ROTARY_PAIRS = 128;
+constexpr int ROTARY_PAIRS = 128, ROTARY_HEADS = 65535;       // (heads may each be a row of the grid)
 struct RotaryArgs {
   const void* x; long x_row, x_head;
   void* y; long y_row, y_head;

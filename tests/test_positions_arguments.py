@@ -77,3 +77,12 @@ def test_frequencies_that_no_number_holds_are_refused(kw, want):
     if kw["dims"] == 64:
         d = B.make_desc(**dict(STACK, d=256), rotary=B.make_rotary(**kw))
         assert status(d) == want
+
+
+def test_a_stack_has_no_more_turned_heads_than_a_call():
+    """Query and key heads are turned together, 65535 at most."""
+    wide = dict(STACK, act="gelu", norm="none", L=2, N=32, d=8 * 65535, d_ff=8)
+    for heads, want in ((65535, UNSUPPORTED), (32767, OK)):
+        sizes = dict(wide, heads=heads, d=8 * heads)
+        assert status(B.make_desc(**sizes, rotary=B.make_rotary(8))) == want
+        assert status(B.make_desc(**sizes)) == OK
