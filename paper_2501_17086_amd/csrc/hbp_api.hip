@@ -250,8 +250,8 @@ Workspace carve(const hbp_desc* d) {
   w.off_dqkv = o;
   if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * qkv_w(d) * es, 256);
   w.off_dsum = o;
-  if (tfm(d)) o = align_up(o + (size_t)(d->L / 2) * d->N * d->heads * 4, 256);
-  // shared key/value heads: what the attention over packed sequences needs
+  if (tfm(d) && key_heads(d) == d->heads) o = align_up(o + (size_t)(d->L / 2) * d->N * d->heads * 4, 256);
+  // shared key/value heads: what the attention over packed sequences needs, rowsum(do (.) o) included
   w.off_packed = o;
   if (tfm(d) && key_heads(d) < d->heads) w.packed = packed_ws(d);
   o = align_up(o + w.packed, 256);

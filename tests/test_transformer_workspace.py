@@ -46,3 +46,11 @@ def test_a_stack_reserves_what_any_number_of_its_layers_needs(sizes, dtype):
         reserved = stack_bytes(dtype, L, N, T, heads, kv, dh) - before_attention(dtype, L, N, heads, kv, dh)
         needs = [attention_bytes(dtype, n, N, T, heads, kv, dh) for n in range(1, L // 2 + 1)]
         assert reserved == aligned(max(needs)), (L, N, T, heads, kv, dh, reserved, max(needs), needs.index(max(needs)) + 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_shared_heads_reserve_nothing_for_the_attention_of_equal_heads(dtype):
+    """Before the attention's own room a stack's workspace depends on the width of q, k, v alone, not on the number of heads."""
+    for L, N in ((2, 64), (8, 4096)):
+        a, b = before_attention(dtype, L, N, 8, 4, 32), before_attention(dtype, L, N, 4, 2, 64)
+        assert a == b, (L, N)
