@@ -331,7 +331,8 @@ typedef struct { void* data; int64_t row_stride, head_stride; } hbp_heads;
  *   BY_PARTS  f_i (w + (1 - w) / s), w = (original f_i / (2 pi) - low) / (high - low) within 0 .. 1: pairs that turn at
  *             least `high` times within `original` positions stay, those that turn at most `low` times are slowed by s.
  * Frequencies of 2^969 and more (a base or a factor next to 0) are refused.
- * Angles are formed and reduced in 64 bits, so that far positions turn as exactly as near ones. */
+ * Angles are formed and reduced in 64 bits: where f_i <= 1 they are off by 2^-51 |p|, up to p = 2^27 less than their rounding to 32
+ * bits afterwards takes. */
 typedef enum { HBP_ROTARY_HALF = 0, HBP_ROTARY_INTERLEAVED = 1 } hbp_rotary_layout;
 typedef enum { HBP_ROTARY_PLAIN = 0, HBP_ROTARY_LINEAR = 1, HBP_ROTARY_BASE = 2, HBP_ROTARY_BY_PARTS = 3 } hbp_rotary_scaling;
 typedef struct {
@@ -351,7 +352,7 @@ typedef struct {
  * transpose, which takes a gradient with respect to `out` to the one with respect to `x`.  x and out: `rows` rows of
  * `heads` heads of dh channels (dh a multiple of 8, at most 256), in the storage type `dtype`; out may be x itself (same
  * data and strides), and must not overlap it otherwise.  positions: DEVICE, one int32 per row, or NULL: row n is at
- * first + n (period = 0) or first + n mod period.  rows = 0 does nothing. */
+ * first + n (period = 0) or first + n mod period.  rows = 0 does nothing.  At most 2^24 rows, 65535 heads, first +-2^52. */
 hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, int heads, int dh, const hbp_heads* x,
                       const hbp_heads* out, const int32_t* positions, int64_t first, int64_t period, int inverse, void* stream);
 
@@ -365,18 +366,20 @@ hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, in
  * A query that sees no key, or whose scores are all minus infinity, has o = 0 and lse = minus infinity.  Sequences may
  * be empty on either side.  Rows behind the last sequence (and before the first) are left as they were.
  * bf16 storage: probabilities are rounded to bf16 before they meet v (and, in the backward pass, do and k, q), sums
- * are fp32.  Infinities and NaNs reach only the rows that see them.  Outputs overlap neither each other nor an input. */
+ * are fp32.  Infinities and NaNs reach only the rows that see them; a row (dk, dv: a key) that does not come out finite is computed
+ * once more, term by term, which takes some hundred times as long as the others.  Outputs overlap neither each other nor an input. */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(hbp_attention_desc) */
   int32_t dtype;             /* hbp_dtype */
-  int32_t heads;             /* query heads: a multiple of kv_heads */
+  int32_t heads;             /* query heads: a multiple of kv_heads, at most 4096 */
   int32_t kv_heads;
   int32_t dh;                /* head width: a multiple of 8, at most 128 */
   int32_t causal;            /* 0 or 1 */
   float scale;               /* > 0, at most 2^127; usually 1 / sqrt(dh) */
   float reserved;            /* 0 */
-  int64_t seqs;              /* >= 1 */
-  int64_t q_rows, k_rows;    /* rows of all sequences together, 0 .. 2^24 */
+  int64_t seqs;              /* 1 .. 2^24 */
+  int64_t q_rows, k_rows;    /* rows of all sequences together, 0 .. 2^24; (q_rows + 32 seqs) heads and (k_rows + 32 seqs) kv_heads
+                              * are below 2^31 */
 } hbp_attention_desc;
 typedef struct {
   uint32_t struct_size;      /* = sizeof(hbp_attention_buffers) */
@@ -405,7 +408,8 @@ hbp_status hbp_attention_backward(const hbp_attention_desc* desc, const hbp_atte
 /* HBP_TRANSFORMER with rotary positions and shared key/value heads: pass &this.base, whose struct_size says so, wherever
  * a call takes an hbp_desc.  The attention sub-blocks then have kv_heads heads of keys and values: Wqkv and dWqkv are
  * [L/2, w, d] and qkv is [L/2, N, w] with w = d + 2 kv_heads dh, a row [q heads | k heads | v heads]; q and k heads are turned by
- * `rotary` before the attention, and qkv holds them turned.  dh <= 128 where kv_heads < heads. */
+ * `rotary` before the attention, and qkv holds them turned.  Where kv_heads < heads, lse is [L/2, N, heads] (per (position, head)),
+ * dh <= 128, heads <= 4096 and L/2 (N + 32 N / seq_len) heads < 2^31; with `rotary` query and key heads are at most 65535. */
 typedef struct {
   hbp_desc base;             /* struct_size = sizeof(hbp_transformer_desc), kind = HBP_TRANSFORMER */
   int32_t kv_heads;          /* heads % kv_heads == 0; 0: as many as heads */

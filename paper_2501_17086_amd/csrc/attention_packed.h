@@ -102,8 +102,9 @@ __device__ __forceinline__ int seen_by(const Seq& s, int i, int causal) {
 // ------------------------------------------------------------------------------------------------------------
 // term by term: one wavefront per (query, head), one per (key, key head), which leaves channels c0 .. c1 - 1 (and the statistic with c0 = 0)
 // ------------------------------------------------------------------------------------------------------------
-// Scores past 2^31 come here as well: there the rounding of the running maximum, which the kernels' fused multiply-add does not share,
-// may take every weight of a row to 0 (or infinity).  So no contraction here: the largest score less itself is 0.
+// Rows with scores past 2^31 may come here as well: there the rounding of the running maximum, which the kernels' fused multiply-add does
+// not share, may take every weight of a row to 0 (or infinity), and the row does not come out finite; where it does, its
+// weights keep their ratios.  So no contraction here: the largest score less itself is 0.
 template <typename T>
 __device__ __forceinline__ void one_forward(const PackedAttnArgs& a, const Seq& s, int i, int h, int c0, int c1, int lane) {
 #pragma clang fp contract(off)
