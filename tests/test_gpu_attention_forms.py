@@ -93,3 +93,24 @@ def test_rows_of_nothing_in_every_form(form, dtype):
     assert not got["dv"][:m].any()
     for name, first in (("o", n), ("lse", n), ("dq", n), ("dk", m), ("dv", m)):
         assert torch.equal(want[name][first:], got[name][first:]), name
+
+
+# ragged on one side, of equal lengths on the other: few sequences, and more than are searched one by one
+MIXED = [([3, 0, 17, 90], 64), ([300, 1, 520], 700), ([i % 5 for i in range(200)], 33), ([40 + i % 9 for i in range(140)], 8), ([1900], 1200)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,each", MIXED, ids=[f"{len(m[0])}of{max(m[0])}x{m[1]}" for m in MIXED])
+def test_offsets_on_one_side_alone(lens, each, causal, dtype):
+    """As with the equal lengths spelt out on the other side."""
+    for lq, lk in ((lens, [each] * len(lens)), ([each] * len(lens), lens)):
+        q, k, v, do = problem(lq, lk, 4, 2, 64, dtype, 233)
+        off = dict(q_offsets=offsets(lq), k_offsets=offsets(lk), causal=causal)
+        want = run(q, k, v, do, off)
+        off["k_offsets" if lq is lens else "q_offsets"] = None
+        got = run(q, k, v, do, off)
+        for name in NAMES:
+            assert torch.equal(want[name], got[name]), name
+        if len(lens) < 10:
+            check_attention(q, k, v, lq, lk, causal, do)
