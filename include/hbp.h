@@ -367,7 +367,7 @@ hbp_status hbp_rotary(const hbp_rotary_desc* rotary, int dtype, int64_t rows, in
  * be empty on either side.  Rows behind the last sequence (and before the first) are left as they were.
  * bf16 storage: probabilities are rounded to bf16 before they meet v (and, in the backward pass, do and k, q), sums
  * are fp32.  Infinities and NaNs reach only the rows that see them; a row (dk, dv: a key) that does not come out finite is computed
- * once more, term by term, which takes some hundred times as long as the others.  Outputs overlap neither each other nor an input. */
+ * once more, term by term, which takes several hundred times as long.  Outputs overlap neither each other nor an input. */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(hbp_attention_desc) */
   int32_t dtype;             /* hbp_dtype */

@@ -452,8 +452,6 @@ AttnArgs attn_args(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, 
   return a;
 }
 
-// first half: da_j = (g[2j+2] W2_j) (.) act' for the MLP sub-blocks; do_j = g[2j+1] Wo_j and, through the attention,
-// the gradient of [q | k | v] for the attention sub-blocks
 // Shared key/value heads: the attention of layers j_lo .. j_hi - 1, whose sequences lie behind one another
 PackedAttnArgs packed_args(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, long j_lo, long j_hi) {
   const size_t es = esize(d);
@@ -484,6 +482,8 @@ hbp_status turn_qk(const hbp_desc* d, void* qkv, long layers, int inverse, hipSt
   return HBP_OK;
 }
 
+// first half: da_j = (g[2j+2] W2_j) (.) act' for the MLP sub-blocks; do_j = g[2j+1] Wo_j and, through the attention,
+// the gradient of [q | k | v] for the attention sub-blocks
 hbp_status tfm_stage1(const hbp_desc* d, const hbp_buffers* b, const Workspace& w, long l_lo, long l_hi, hipStream_t s) {
   const size_t es = esize(d);
   const long N = d->N, D = d->d, F = d->d_ff;
