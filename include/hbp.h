@@ -418,6 +418,104 @@ typedef struct {
   const int32_t* positions;  /* DEVICE [N], or NULL: a token's place in its sequence.  NULL where dims = 0 */
 } hbp_transformer_desc;
 
+/* ---- a language model's two ends: embedding, dropout, cross entropy over a vocabulary ------------------------------
+ * Operators on tensors of the caller's own, around a stack: an embedding's `out` is a stack's x_0, the loss reads its last
+ * state and writes its e, hbp_backward's g_0 is the embedding's `dout`.  The conventions above hold. */
+
+/* Rows: channel c of row n is element data[n row_stride + c] of the storage type.  data is 16-byte aligned; strides are multiples of
+ * 8, not negative, at most 2^22 (that of a single row does not matter).  Rows of a tensor that is written must not overlap; those of an
+ * input may (a stride of 0 reads one row again and again).  Widths are multiples of 8, at most 65536. */
+typedef struct { void* data; int64_t row_stride; } hbp_rows;
+
+/* Dropout by a counter-based generator; no mask is stored: a call with the same descriptor makes the same mask again.  Of
+ * [rows, width] elements, numbered i = n width + c, element i is left out where its 16 bits are below T = round(65536 rate), else multiplied
+ * by 65536 / (65536 - T).  The bits: word j / 2 (j = i mod 8), low half first, of Philox4x32-10 with the key (seed's low word, high
+ * word) and the counter (low and high word of i / 8, low and high word of offset + *counter). */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_dropout_desc) */
+  float rate;                /* 0 <= rate < 1; rates that round to 1 (T = 65536) are refused */
+  uint64_t seed;
+  uint64_t offset;           /* another one for every mask: a step's number and a layer's, say */
+  const uint64_t* counter;   /* DEVICE, added to offset when the kernel runs, or NULL: a captured graph that is replayed makes new masks
+                              * once the caller has counted it up */
+} hbp_dropout_desc;
+
+/* out := dropout(x), or residual + dropout(x) (residual NULL: none), rounded once.  Of x only elements that stay are seen: an infinity or a
+ * NaN in another place leaves a zero.  The gradient with respect to x is the same call on the gradient of `out`, without a
+ * residual.  out may be x or the residual themselves (same data and stride) and must not overlap them otherwise.  rows = 0 does
+ * nothing.  At most 2^24 rows and 2^36 elements. */
+hbp_status hbp_dropout(const hbp_dropout_desc* dropout, int dtype, int64_t rows, int64_t width, const hbp_rows* x,
+                       const hbp_rows* residual, const hbp_rows* out, void* stream);
+
+/* Embedding: out[n] = scale table[tokens[n]], with dropout on the way (the mask of [rows, width]), rounded once.  A token outside
+ * 0 .. vocab - 1 gives a row of zeros and has no gradient. */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_embedding_desc) */
+  int32_t dtype;             /* hbp_dtype of table, out, dout */
+  int32_t grad_dtype;        /* hbp_dtype of dtable: HBP_F32, or dtype */
+  float scale;               /* finite, as is its product with dropout's factor */
+  int64_t rows;              /* 0 .. 2^24 tokens, rows x width at most 2^36 */
+  int64_t vocab;             /* 1 .. 2^24 */
+  int64_t width;
+  hbp_dropout_desc dropout;  /* rate = 0: none (struct_size 0 will do) */
+} hbp_embedding_desc;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_embedding_buffers) */
+  const int32_t* tokens;     /* [rows] */
+  hbp_rows table;            /* forward: in, [vocab, width] */
+  hbp_rows out;              /* forward: out, [rows, width] */
+  hbp_rows dout;             /* backward: in, the gradient of out */
+  hbp_rows dtable;           /* backward: out, [vocab, width], in grad_dtype */
+  void* workspace;           /* backward */
+  size_t workspace_bytes;
+} hbp_embedding_buffers;
+
+/* Bytes of workspace that hbp_embedding_backward needs (the other call needs none).  Calls that overlap must not share one. */
+hbp_status hbp_embedding_workspace_size(const hbp_embedding_desc* desc, size_t* bytes);
+/* Reads tokens, table; writes out. */
+hbp_status hbp_embedding_forward(const hbp_embedding_desc* desc, const hbp_embedding_buffers* bufs, void* stream);
+/* dtable[v] = scale sum over the n with tokens[n] = v of dropout(dout[n]), zeros where there are none; accumulate = 1: added to what
+ * dtable holds (a table that is also the vocabulary's weights: on top of the loss's dweight).  Reads tokens, dout.  Sums are fp32 in a
+ * fixed order: results are bitwise repeatable. */
+hbp_status hbp_embedding_backward(const hbp_embedding_desc* desc, const hbp_embedding_buffers* bufs, int accumulate, void* stream);
+
+/* Softmax cross entropy of rows against a vocabulary.  With s_nv = scale x_n . weight_v, a row whose target t is in 0 .. vocab - 1
+ * counts and has
+ *   row_loss_n = log sum_v exp(s_nv) - s_nt,    loss = factor sum_n row_loss_n, with mean = 1 divided by the number of rows that count,
+ *   dx = scale dS weight,    dweight = scale dS^T x,    dS_nv = factor (/ that number) (softmax(s_n)_v - [v = t]).
+ * Other rows (padding) have row_loss 0 and a dx of zeros, and nothing in their x reaches any result; where no row counts
+ * the loss is 0 and dweight zeros.  The vocabulary is taken in pieces and the logits are not kept.
+ * bf16 storage: dS is rounded to bf16 before it meets weight and x; logits, their sums and all products' sums are fp32. */
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_cross_entropy_desc) */
+  int32_t dtype;             /* hbp_dtype of x, weight, dx */
+  int32_t grad_dtype;        /* hbp_dtype of dweight: HBP_F32, or dtype */
+  int32_t mean;              /* 0 or 1 */
+  float scale;               /* > 0, at most 2^127; usually 1 */
+  float factor;              /* finite; usually 1 (a loss scale, or one over the number of batches whose gradients are added) */
+  int64_t rows;              /* 0 .. 2^20 */
+  int64_t vocab;             /* 1 .. 2^24 */
+  int64_t width;
+} hbp_cross_entropy_desc;
+typedef struct {
+  uint32_t struct_size;      /* = sizeof(hbp_cross_entropy_buffers) */
+  hbp_rows x;                /* in, [rows, width] */
+  hbp_rows weight;           /* in, [vocab, width] */
+  const int32_t* targets;    /* in, [rows] */
+  float* loss;               /* out, one number */
+  float* row_loss;           /* out, [rows], or NULL */
+  hbp_rows dx;               /* out, [rows, width]; data = NULL: not wanted */
+  hbp_rows dweight;          /* out, [vocab, width], in grad_dtype; data = NULL: not wanted */
+  void* workspace;
+  size_t workspace_bytes;
+} hbp_cross_entropy_buffers;
+
+/* Bytes of workspace for the loss alone (gradients = 0), or with either gradient (1).  Calls that overlap must not share one. */
+hbp_status hbp_cross_entropy_workspace_size(const hbp_cross_entropy_desc* desc, int gradients, size_t* bytes);
+/* Reads x, weight, targets; writes loss, row_loss, dx, dweight, none of which overlaps another or an input.  Sums are taken in a fixed
+ * order: results are bitwise repeatable. */
+hbp_status hbp_loss_cross_entropy(const hbp_cross_entropy_desc* desc, const hbp_cross_entropy_buffers* bufs, void* stream);
+
 const char* hbp_status_string(hbp_status s);
 
 /* Optional timing of the kernels the calls above enqueue, by class, with HIP
@@ -433,7 +531,7 @@ enum {
   HBP_PROF_SCAN = 2,    /* residual-path scan        (step (ii), and w^0)           */
   HBP_PROF_DW = 3,      /* parameter-gradient contractions over tokens              */
   HBP_PROF_FORWARD = 4, /* forward support kernels, chains along time among them    */
-  HBP_PROF_OTHER = 5,   /* copies, split-K reductions                               */
+  HBP_PROF_OTHER = 5,   /* copies, split-K reductions; dropout, embedding, cross entropy (a call of these counts once) */
   HBP_PROF_ATTN = 6,    /* attention between its two matrices, forward and backward, and rotary positions */
   HBP_PROF_CLASSES = 7
 };

@@ -32,6 +32,8 @@ LAMBDA_ONE, LAMBDA_CHANNEL, LAMBDA_TOKEN = 0, 1, 2
 EXPORTS = ("hbp_workspace_size", "hbp_check", "hbp_forward", "hbp_backward", "hbp_exact_backward",
            "hbp_scan_workspace_size", "hbp_initial_estimate", "hbp_initial_estimate_static",
            "hbp_rotary", "hbp_attention_workspace_size", "hbp_attention_forward", "hbp_attention_backward",
+           "hbp_dropout", "hbp_embedding_workspace_size", "hbp_embedding_forward", "hbp_embedding_backward",
+           "hbp_cross_entropy_workspace_size", "hbp_loss_cross_entropy",
            "hbp_param_grads", "hbp_train_scratch_size", "hbp_loss_mse", "hbp_optimizer_step", "hbp_train_step",
            "hbp_profile_enable", "hbp_profile_read", "hbp_status_string")
 PROF_CLASSES = ("vjp1", "vjp2", "scan", "dw", "forward", "other", "attn")
@@ -70,6 +72,36 @@ class hbp_attention_buffers(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("q", hbp_heads), ("k", hbp_heads), ("v", hbp_heads), ("o", hbp_heads),
                 ("dout", hbp_heads), ("dq", hbp_heads), ("dk", hbp_heads), ("dv", hbp_heads), ("lse", C.c_void_p),
                 ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class hbp_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64)]
+
+
+class hbp_dropout_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rate", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("counter", C.c_void_p)]
+
+
+class hbp_embedding_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("scale", C.c_float),
+                ("rows", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64), ("dropout", hbp_dropout_desc)]
+
+
+class hbp_embedding_buffers(C.Structure):
+    _fields_ = ([("struct_size", C.c_uint32), ("tokens", C.c_void_p)] + [(n, hbp_rows) for n in ("table", "out", "dout", "dtable")] +
+                [("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)])
+
+
+class hbp_cross_entropy_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("mean", C.c_int32),
+                ("scale", C.c_float), ("factor", C.c_float), ("rows", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64)]
+
+
+class hbp_cross_entropy_buffers(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("x", hbp_rows), ("weight", hbp_rows), ("targets", C.c_void_p), ("loss", C.c_void_p),
+                ("row_loss", C.c_void_p), ("dx", hbp_rows), ("dweight", hbp_rows), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t)]
 
 
@@ -144,6 +176,12 @@ def lib() -> C.CDLL:
         L.hbp_attention_workspace_size.argtypes = [C.POINTER(hbp_attention_desc), C.POINTER(C.c_size_t)]
         for n in ("hbp_attention_forward", "hbp_attention_backward"):
             getattr(L, n).argtypes = [C.POINTER(hbp_attention_desc), C.c_void_p, C.c_void_p]
+        L.hbp_dropout.argtypes = [C.POINTER(hbp_dropout_desc), C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.hbp_embedding_workspace_size.argtypes = [C.POINTER(hbp_embedding_desc), C.POINTER(C.c_size_t)]
+        L.hbp_embedding_forward.argtypes = [C.POINTER(hbp_embedding_desc), C.c_void_p, C.c_void_p]
+        L.hbp_embedding_backward.argtypes = [C.POINTER(hbp_embedding_desc), C.c_void_p, C.c_int, C.c_void_p]
+        L.hbp_cross_entropy_workspace_size.argtypes = [C.POINTER(hbp_cross_entropy_desc), C.c_int, C.POINTER(C.c_size_t)]
+        L.hbp_loss_cross_entropy.argtypes = [C.POINTER(hbp_cross_entropy_desc), C.c_void_p, C.c_void_p]
         L.hbp_profile_enable.argtypes = [C.c_int]
         L.hbp_profile_read.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.hbp_status_string.argtypes = [C.c_int]
@@ -561,6 +599,209 @@ def hbp_attention_forward(a: Attention, stream=None) -> None:
 def hbp_attention_backward(a: Attention, dout, stream=None) -> None:
     """a.dq, a.dk, a.dv from a.q, a.k, a.v, a.o, a.lse and the gradient of a.o."""
     _launch("hbp_attention_backward", a.q.get_device(), lib().hbp_attention_backward, C.byref(a.desc), a.buffers(dout), stream=stream)
+
+
+# ---- a language model's two ends ---------------------------------------------------------------------------------
+def _rows(name: str, t, shape, dtype, device: int) -> tuple:
+    """The fields of an hbp_rows for a [rows, width] tensor, channels next to each other."""
+    if t is None or t.shape != shape or t.dtype != dtype or t.get_device() != device:
+        got = "none" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}"
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on GPU {device}, got {got}")
+    row, channel = t.stride()
+    if channel != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: the channels of a row must be next to each other, got strides {t.stride()}")
+    return t.data_ptr(), row
+
+
+def _matrix(name: str, t) -> int:
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected [rows, width], got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a tensor on the GPU, got {t.device}")
+    return t.get_device()
+
+
+def _workspace(ws, device: int) -> tuple:
+    if ws is None:
+        return 0, 0
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on GPU {device}, got one on {ws.device} with strides {ws.stride()}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _gradient_type(name: str, t, dtype) -> int:
+    """HBP_F32 or the storage type, by the tensor that takes the gradient (none: fp32)."""
+    import torch
+    if t is None or t.dtype == torch.float32:
+        return F32
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {torch.float32} or {dtype}, got {t.dtype}")
+    return _storage_type(dtype)
+
+
+@dataclass
+class Dropout:
+    """One mask: rate, seed and offset; counter: int64 tensor of one number on the GPU that is added to the offset, or None."""
+    desc: hbp_dropout_desc
+    counter: "object" = None
+
+    def checked(self, device: int) -> hbp_dropout_desc:
+        import torch
+        self.desc.counter = _plain("counter", self.counter, (1,), torch.int64, device)
+        return self.desc
+
+
+def make_dropout(rate: float, seed: int, offset: int = 0, counter=None) -> Dropout:
+    """A mask of hbp_dropout_desc; seed and offset below 2^64."""
+    for name, v in (("seed", seed), ("offset", offset)):
+        if not 0 <= v < 1 << 64:
+            raise ValueError(f"{name}: expected 0 .. 2^64 - 1, got {v}")
+    return Dropout(hbp_dropout_desc(C.sizeof(hbp_dropout_desc), rate, seed, offset, None), counter)
+
+
+_pack_rows = struct.Struct("Qq").pack
+
+
+def hbp_dropout(dropout: Dropout, x, out, residual=None, stream=None) -> None:
+    """out := dropout(x), plus the residual if there is one; all [rows, width], out may be x or the residual."""
+    device, shape, dtype = _matrix("x", x), x.shape, x.dtype
+    kind = _storage_type(dtype)
+    hx = _pack_rows(*_rows("x", x, shape, dtype, device))
+    ho = _pack_rows(*_rows("out", out, shape, dtype, device))
+    hr = None if residual is None else _pack_rows(*_rows("residual", residual, shape, dtype, device))
+    _launch("hbp_dropout", device, lib().hbp_dropout, C.byref(dropout.checked(device)), kind, *shape, hx, hr, ho, stream=stream)
+
+
+@dataclass
+class Embedding:
+    """Device tensors of one embedding: tokens int32 [rows], table [vocab, width], out [rows, width], dtable [vocab, width] (fp32 or
+    the table's type)."""
+    desc: hbp_embedding_desc
+    tokens: "object"
+    table: "object"
+    out: "object"
+    dtable: "object" = None
+    workspace: "object" = None
+    dropout: Optional[Dropout] = None
+
+    def buffers(self, dout=None) -> bytes:
+        """The C struct hbp_embedding_buffers, each tensor checked against the descriptor; with dout the backward pass's."""
+        import torch
+        d, device, dtype = self.desc, _matrix("table", self.table), self.table.dtype
+        rows, table = (d.rows, d.width), (d.vocab, d.width)
+        d.dropout = self.dropout.checked(device) if self.dropout is not None else hbp_dropout_desc()
+        if dout is None:
+            fwd = (*_rows("table", self.table, table, dtype, device), *_rows("out", self.out, rows, dtype, device))
+            bwd = (0,) * 4
+        else:
+            fwd = (0,) * 4
+            grad = torch.float32 if d.grad_dtype == F32 else dtype
+            bwd = (*_rows("dout", dout, rows, dtype, device), *_rows("dtable", self.dtable, table, grad, device))
+        return _pack_embedding(_EMBEDDING_SIZE, _plain("tokens", self.tokens, rows[:1], torch.int32, device) or 0, *fwd, *bwd,
+                               *_workspace(self.workspace, device))
+
+
+_EMBEDDING_SIZE = C.sizeof(hbp_embedding_buffers)
+_pack_embedding = struct.Struct("IxxxxQ" + "Qq" * 4 + "QQ").pack
+
+
+def make_embedding(tokens, table, scale: float = 1.0, dropout: Optional[Dropout] = None, out=None, grad: bool = True,
+                   dtable=None) -> Embedding:
+    """An Embedding of the given tokens and table: allocates out and, with grad, dtable (fp32) unless given, and the workspace."""
+    import torch
+    device = _matrix("table", table)
+    vocab, width = table.shape
+    desc = hbp_embedding_desc(C.sizeof(hbp_embedding_desc), _storage_type(table.dtype), _gradient_type("dtable", dtable, table.dtype),
+                              scale, tokens.numel(), vocab, width, hbp_dropout_desc())
+    e = Embedding(desc, tokens, table, torch.empty((tokens.numel(), width), dtype=table.dtype, device=table.device) if out is None else out,
+                  dropout=dropout)
+    if grad:
+        e.dtable = torch.empty((vocab, width), dtype=torch.float32, device=table.device) if dtable is None else dtable
+        n = C.c_size_t(0)
+        _call("hbp_embedding_workspace_size", lib().hbp_embedding_workspace_size(C.byref(desc), C.byref(n)))
+        e.workspace = torch.empty(n.value, dtype=torch.uint8, device=table.device)
+    e.buffers()                                            # (refuses what does not fit)
+    return e
+
+
+def hbp_embedding_forward(e: Embedding, stream=None) -> None:
+    """e.out from e.tokens and e.table."""
+    b = e.buffers()
+    _launch("hbp_embedding_forward", e.table.get_device(), lib().hbp_embedding_forward, C.byref(e.desc), b, stream=stream)
+
+
+def hbp_embedding_backward(e: Embedding, dout, accumulate: bool = False, stream=None) -> None:
+    """e.dtable from e.tokens and the gradient of e.out; accumulate: added to what it holds."""
+    b = e.buffers(dout)
+    _launch("hbp_embedding_backward", e.table.get_device(), lib().hbp_embedding_backward, C.byref(e.desc), b, 1 if accumulate else 0,
+            stream=stream)
+
+
+@dataclass
+class CrossEntropy:
+    """Device tensors of one loss: x, dx [rows, width]; weight, dweight [vocab, width] (dweight fp32 or the weights' type); targets
+    int32 [rows]; loss fp32 [1]; row_loss fp32 [rows].  row_loss, dx and dweight may be None: not wanted."""
+    desc: hbp_cross_entropy_desc
+    x: "object"
+    weight: "object"
+    targets: "object"
+    loss: "object"
+    row_loss: "object" = None
+    dx: "object" = None
+    dweight: "object" = None
+    workspace: "object" = None
+
+    def buffers(self) -> bytes:
+        """The C struct hbp_cross_entropy_buffers, each tensor checked against the descriptor."""
+        import torch
+        d, device, dtype = self.desc, _matrix("x", self.x), self.x.dtype
+        rows, weight = (d.rows, d.width), (d.vocab, d.width)
+        if self.loss is None:
+            raise ValueError(f"loss: expected (1,) torch.float32 on GPU {device}, got none")
+        grad = torch.float32 if d.grad_dtype == F32 else dtype
+        dx = (0, 0) if self.dx is None else _rows("dx", self.dx, rows, dtype, device)
+        dw = (0, 0) if self.dweight is None else _rows("dweight", self.dweight, weight, grad, device)
+        return _pack_loss(_LOSS_SIZE, *_rows("x", self.x, rows, dtype, device), *_rows("weight", self.weight, weight, dtype, device),
+                          _plain("targets", self.targets, rows[:1], torch.int32, device) or 0,
+                          _plain("loss", self.loss, (1,), torch.float32, device),
+                          _plain("row_loss", self.row_loss, rows[:1], torch.float32, device) or 0, *dx, *dw,
+                          *_workspace(self.workspace, device))
+
+
+_LOSS_SIZE = C.sizeof(hbp_cross_entropy_buffers)
+_pack_loss = struct.Struct("Ixxxx" + "Qq" * 2 + "QQQ" + "Qq" * 2 + "QQ").pack
+
+
+def cross_entropy_workspace_size(desc: hbp_cross_entropy_desc, gradients: bool) -> int:
+    n = C.c_size_t(0)
+    _call("hbp_cross_entropy_workspace_size",
+          lib().hbp_cross_entropy_workspace_size(C.byref(desc), 1 if gradients else 0, C.byref(n)))
+    return n.value
+
+
+def make_cross_entropy(x, weight, targets, scale: float = 1.0, mean: bool = True, factor: float = 1.0, grad: bool = True, dx=None,
+                       dweight=None) -> CrossEntropy:
+    """A CrossEntropy of the given rows, weights and targets: allocates loss, row_loss, the workspace and, with grad, dx and dweight
+    (fp32) unless given.  A Problem's: x = p.x[-1], dx = p.e."""
+    import torch
+    device = _matrix("x", x)
+    _matrix("weight", weight)
+    (rows, width), vocab = x.shape, weight.shape[0]
+    desc = hbp_cross_entropy_desc(C.sizeof(hbp_cross_entropy_desc), _storage_type(x.dtype), _gradient_type("dweight", dweight, x.dtype),
+                                  1 if mean else 0, scale, factor, rows, vocab, width)
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=x.device)
+    c = CrossEntropy(desc, x, weight, targets, new(1), new(rows))
+    if grad:
+        c.dx = new(rows, width, dtype=x.dtype) if dx is None else dx
+        c.dweight = new(vocab, width) if dweight is None else dweight
+    c.workspace = new(cross_entropy_workspace_size(desc, grad), dtype=torch.uint8)
+    c.buffers()                                            # (refuses what does not fit)
+    return c
+
+
+def hbp_loss_cross_entropy(c: CrossEntropy, stream=None) -> None:
+    """c.loss, c.row_loss and, where they are there, c.dx and c.dweight from c.x, c.weight and c.targets."""
+    _launch("hbp_loss_cross_entropy", c.x.get_device(), lib().hbp_loss_cross_entropy, C.byref(c.desc), c.buffers(), stream=stream)
 
 
 def profile_enable(on: bool) -> None:

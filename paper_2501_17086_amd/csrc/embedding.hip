@@ -1,0 +1,495 @@
+// The embedding of a language model's tokens, its gradient, and dropout.
+//
+// All of it is bound by memory: a unit of 8 channels is read once and written once, one product an element, and with dropout ten
+// rounds of two wide integer products a unit.
+//
+// The gradient adds up rows of the same token, in 32 bits and in an order that does not change from run to run, so without atomics on
+// its sums.  Tokens are sorted (least significant digit first, up to 9 bits a pass, stable, so that a token's rows stay in order);
+// then every wavefront owns some rows of the table, finds their stretch of the sorted list by a search of 64 probes a step, and adds.
+// Text repeats few tokens very often: 64 sorted places that begin at a multiple of 64 and hold one token are added up beforehand by a
+// workgroup of their own, and the table's row adds that sum.  A table's row is written once, rows without tokens as zeros: that is most
+// of the bytes.
+#include "philox.h"
+
+namespace hbp {
+
+namespace {
+
+constexpr int NTHR = 256;
+
+// ---- dropout and lookup: a unit of 8 channels a thread and step ----------------------------------------------------------
+// Units are counted along the rows, which is also the generator's count.  A workgroup's first unit is divided once in 64 bits, a
+// thread's place behind it by a multiplication.
+struct Units {
+  long total;
+  Divisor by_row;
+  unsigned per_row;
+};
+struct Place { long row; unsigned unit; };
+__device__ __forceinline__ Place place_of(const Units& u, long row0, unsigned rem0, unsigned local) {
+  const unsigned r = rem0 + local, q = u.by_row.quotient(r);
+  return {row0 + q, r - q * u.per_row};
+}
+__device__ __forceinline__ void keep8(unsigned mask, float factor, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (mask >> j) & 1u ? v[j] * factor : 0.f;
+}
+
+// K units a thread, 256 apart: their loads go out together
+template <typename T, int K, bool RES>
+__global__ __launch_bounds__(NTHR) void dropout_kernel(DropoutArgs a, DropoutKey key, Units u) {
+  const long base = (long)blockIdx.x * (NTHR * K);
+  const long row0 = base / u.per_row;
+  const unsigned rem0 = (unsigned)(base - row0 * u.per_row);
+  const unsigned long stream = dropout_stream(key);
+  const T* x = reinterpret_cast<const T*>(a.x.p);
+  const T* r = reinterpret_cast<const T*>(a.residual.p);
+  T* y = reinterpret_cast<T*>(a.out.p);
+  Raw8<T> vx[K], vr[K];
+  Place p[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const unsigned local = threadIdx.x + NTHR * k;
+    if (base + local >= u.total) continue;
+    p[k] = place_of(u, row0, rem0, local);
+    vx[k].load(x + p[k].row * a.x.row + 8 * p[k].unit);
+    if (RES) vr[k].load(r + p[k].row * a.residual.row + 8 * p[k].unit);
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const unsigned local = threadIdx.x + NTHR * k;
+    if (base + local >= u.total) continue;
+    const unsigned mask = key.threshold ? dropout_mask8(key, stream, base + local) : 255u;
+    float v[8];
+    vx[k].unpack(v);
+    keep8(mask, key.factor, v);
+    if (RES) {
+      float w[8];
+      vr[k].unpack(w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += w[j];
+    }
+    store8(y + p[k].row * a.out.row + 8 * p[k].unit, v);
+  }
+}
+
+template <typename T, int K>
+__global__ __launch_bounds__(NTHR) void lookup_kernel(EmbeddingArgs a, DropoutKey key, Units u) {
+  const long base = (long)blockIdx.x * (NTHR * K);
+  const long row0 = base / u.per_row;
+  const unsigned rem0 = (unsigned)(base - row0 * u.per_row);
+  const unsigned long stream = key.threshold ? dropout_stream(key) : 0;
+  const T* table = reinterpret_cast<const T*>(a.table.p);
+  T* y = reinterpret_cast<T*>(a.out.p);
+  Place p[K];
+  int token[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const unsigned local = threadIdx.x + NTHR * k;
+    token[k] = -1;
+    if (base + local >= u.total) continue;
+    p[k] = place_of(u, row0, rem0, local);
+    token[k] = a.tokens[p[k].row];
+  }
+  Raw8<T> v[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (token[k] >= 0 && token[k] < a.vocab) v[k].load(table + (long)token[k] * a.table.row + 8 * p[k].unit);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const unsigned local = threadIdx.x + NTHR * k;
+    if (base + local >= u.total) continue;
+    float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (token[k] >= 0 && token[k] < a.vocab) {
+      v[k].unpack(w);
+      keep8(key.threshold ? dropout_mask8(key, stream, base + local) : 255u, key.factor, w);
+    }
+    store8(y + p[k].row * a.out.row + 8 * p[k].unit, w);
+  }
+}
+
+Units units_of(long rows, int width) {
+  const unsigned per = (unsigned)(width / 8);
+  return {rows * per, Divisor(per), per};
+}
+// Four units a thread once that leaves four workgroups for every compute unit
+bool four_units(const Units& u) { return u.total >= 4L * NTHR * 1024; }
+unsigned blocks_of(const Units& u, int k) { return (unsigned)((u.total + NTHR * k - 1) / (NTHR * k)); }
+
+template <typename T, bool RES>
+hipError_t launch_dropout_t(const DropoutArgs& a, const DropoutKey& key, hipStream_t s) {
+  const Units u = units_of(a.rows, a.width);
+  if (four_units(u)) dropout_kernel<T, 4, RES><<<blocks_of(u, 4), NTHR, 0, s>>>(a, key, u);
+  else dropout_kernel<T, 1, RES><<<blocks_of(u, 1), NTHR, 0, s>>>(a, key, u);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_lookup_t(const EmbeddingArgs& a, const DropoutKey& key, hipStream_t s) {
+  const Units u = units_of(a.rows, a.width);
+  if (four_units(u)) lookup_kernel<T, 4><<<blocks_of(u, 4), NTHR, 0, s>>>(a, key, u);
+  else lookup_kernel<T, 1><<<blocks_of(u, 1), NTHR, 0, s>>>(a, key, u);
+  return hipGetLastError();
+}
+
+// ---- the gradient: tokens sorted -----------------------------------------------------------------------------------------
+constexpr int SORT_PER = 8, SORT_E = NTHR * SORT_PER;      // places of a workgroup
+constexpr int SORT_BITS = 9, SORT_D = 1 << SORT_BITS;
+constexpr int CHUNK = 64;                                  // sorted places added up beforehand where they hold one token
+
+// What a place sorts by: its token, or `vocab` for a token that is none (behind all others).
+__device__ __forceinline__ unsigned key_of(int token, unsigned vocab) { return (unsigned)token < vocab ? (unsigned)token : vocab; }
+
+struct SortArgs {
+  const int* tokens;          // first pass: keys are made from these, places are their own numbers
+  const unsigned *keys_in, *places_in;
+  unsigned *keys_out, *places_out;
+  unsigned* counts;           // [blocks][SORT_D]: keys with each digit, after scan_kernel those in earlier blocks
+  unsigned* totals;           // [SORT_D], after scan_kernel
+  long n;
+  unsigned vocab;
+  int shift, mask, blocks, scanned;
+};
+__device__ __forceinline__ unsigned load_key(const SortArgs& a, long i) {
+  return a.tokens ? key_of(a.tokens[i], a.vocab) : a.keys_in[i];
+}
+
+__global__ __launch_bounds__(NTHR) void count_kernel(SortArgs a) {
+  __shared__ unsigned cnt[SORT_D];
+  for (int d = threadIdx.x; d < SORT_D; d += NTHR) cnt[d] = 0;
+  __syncthreads();
+  const long base = (long)blockIdx.x * SORT_E;
+#pragma unroll
+  for (int k = 0; k < SORT_PER; ++k) {
+    const long i = base + threadIdx.x + NTHR * k;
+    if (i < a.n) atomicAdd(&cnt[(load_key(a, i) >> a.shift) & a.mask], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < SORT_D; d += NTHR) a.counts[(long)blockIdx.x * SORT_D + d] = cnt[d];
+}
+
+// many blocks: their counts of a digit become the number of such keys in earlier blocks; a thread a digit
+__global__ __launch_bounds__(64) void scan_kernel(SortArgs a) {
+  const int d = blockIdx.x * 64 + threadIdx.x;
+  unsigned sum = 0;
+  int b = 0;
+  for (; b + 8 <= a.blocks; b += 8) {
+    unsigned c[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = a.counts[(long)(b + j) * SORT_D + d];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { a.counts[(long)(b + j) * SORT_D + d] = sum; sum += c[j]; }
+  }
+  for (; b < a.blocks; ++b) {
+    const unsigned c = a.counts[(long)b * SORT_D + d];
+    a.counts[(long)b * SORT_D + d] = sum;
+    sum += c;
+  }
+  a.totals[d] = sum;
+}
+
+// Every wavefront owns 512 consecutive places in 8 steps of 64; within a step lanes of one digit find each other by a ballot a bit.
+__global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
+  __shared__ unsigned cnt[4][SORT_D];                      // a wavefront's keys with each digit, then where they go
+  __shared__ unsigned sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int d = tid; d < 4 * SORT_D; d += NTHR) (&cnt[0][0])[d] = 0;
+  __syncthreads();
+  const long base = (long)blockIdx.x * SORT_E + wave * (64 * SORT_PER) + lane;
+  unsigned key[SORT_PER], rank[SORT_PER];
+  const int bits = 32 - __clz(a.mask);
+#pragma unroll
+  for (int k = 0; k < SORT_PER; ++k) {
+    const long i = base + 64 * k;
+    const bool in = i < a.n;
+    key[k] = in ? load_key(a, i) : 0u;
+    const unsigned d = (key[k] >> a.shift) & a.mask;
+    unsigned long peers = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+      const unsigned long has = __ballot((d >> b) & 1u);
+      peers &= (d >> b) & 1u ? has : ~has;
+    }
+    const unsigned before = __popcll(peers & ((1ul << lane) - 1ul));
+    rank[k] = in ? cnt[wave][d] + before : 0u;
+    __builtin_amdgcn_wave_barrier();                       // (a wavefront's LDS operations execute in order)
+    if (in && before == 0) cnt[wave][d] += __popcll(peers);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  // where the first key of each digit and wavefront goes: two digits a thread
+  const unsigned d0 = 2 * tid;
+  unsigned total[2], before[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    total[j] = before[j] = 0;
+    if (a.scanned) {
+      total[j] = a.totals[d0 + j];
+      before[j] = a.counts[(long)blockIdx.x * SORT_D + d0 + j];
+    }
+  }
+  if (!a.scanned) {
+    for (int b = 0; b < a.blocks; ++b) {
+      const uint2 c = *reinterpret_cast<const uint2*>(a.counts + (long)b * SORT_D + d0);
+      total[0] += c.x; total[1] += c.y;
+      if (b < (int)blockIdx.x) { before[0] += c.x; before[1] += c.y; }
+    }
+  }
+  unsigned pair = total[0] + total[1], scan = pair;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned t = __shfl_up(scan, o);
+    if (lane >= o) scan += t;
+  }
+  if (lane == 63) sums[wave] = scan;
+  __syncthreads();
+  unsigned start = scan - pair;
+  for (int w = 0; w < wave; ++w) start += sums[w];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    unsigned at = start + before[j];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const unsigned c = cnt[w][d0 + j];
+      cnt[w][d0 + j] = at;
+      at += c;
+    }
+    start += total[j];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < SORT_PER; ++k) {
+    const long i = base + 64 * k;
+    if (i >= a.n) continue;
+    const unsigned at = cnt[wave][(key[k] >> a.shift) & a.mask] + rank[k];
+    a.keys_out[at] = key[k];
+    a.places_out[at] = a.tokens ? (unsigned)i : a.places_in[i];
+  }
+}
+
+// ---- the gradient: sums --------------------------------------------------------------------------------------------------
+struct SumArgs {
+  EmbeddingArgs e;
+  DropoutKey key;
+  const unsigned *keys, *places;   // sorted
+  float* chunk_sums;               // [chunks][width]
+  unsigned n, units;               // places; width / 8
+  unsigned vrows;                  // rows of the table a wavefront owns
+};
+
+// G lanes hold a row's channels, 8 each, so a wavefront works on 64 / G rows at a time; slice: blockIdx.y
+template <typename T> struct Adder {
+  const T* dout;
+  const SumArgs& a;
+  unsigned long stream;
+  unsigned unit;                   // this lane's 8 channels
+  bool in;
+  __device__ __forceinline__ Adder(const SumArgs& a_, unsigned unit_)
+      : dout(reinterpret_cast<const T*>(a_.e.dout.p)), a(a_), stream(a_.key.threshold ? dropout_stream(a_.key) : 0), unit(unit_),
+        in(unit_ < a_.units) {}
+  __device__ __forceinline__ void load(Raw8<T>& r, unsigned place) const {
+    if (in) r.load(dout + (long)place * a.e.dout.row + 8 * unit);
+  }
+  __device__ __forceinline__ void add(float (&acc)[8], const Raw8<T>& r, unsigned place) const {
+    if (!in) return;
+    const unsigned mask = a.key.threshold ? dropout_mask8(a.key, stream, (unsigned long)place * a.units + unit) : 255u;
+    float v[8];
+    r.unpack(v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] += (mask >> j) & 1u ? v[j] : 0.f;
+  }
+};
+
+// 64 places of one token: each wavefront adds 16, and the four sums meet in LDS
+template <typename T, int G>
+__global__ __launch_bounds__(NTHR) void chunk_kernel(SumArgs a) {
+  __shared__ float part[4][64 / G][8 * G];
+  const unsigned first = blockIdx.x * CHUNK;
+  const unsigned v = a.keys[first];
+  if (v >= a.e.vocab || a.keys[first + CHUNK - 1] != v) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / G;
+  constexpr int R = 64 / G, STEPS = 16 / R > 0 ? 16 / R : 1;
+  const Adder<T> add(a, blockIdx.y * G + lane % G);
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  constexpr int B = STEPS < 4 ? STEPS : 4;
+#pragma unroll 1
+  for (int s = 0; s < STEPS; s += B) {
+    Raw8<T> r[B];
+    unsigned p[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) p[b] = a.places[first + 16 * wave + (s + b) * R + sub];
+#pragma unroll
+    for (int b = 0; b < B; ++b) add.load(r[b], p[b]);
+#pragma unroll
+    for (int b = 0; b < B; ++b) add.add(acc, r[b], p[b]);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) part[wave][sub][8 * (lane % G) + j] = acc[j];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 8 * G; c += NTHR) {
+    float t = 0.f;
+    for (int w = 0; w < 4; ++w)
+      for (int s = 0; s < R; ++s) t += part[w][s][c];
+    const unsigned at = blockIdx.y * (8 * G) + c;
+    if (at < 8 * a.units) a.chunk_sums[(long)blockIdx.x * (8 * a.units) + at] = t;
+  }
+}
+
+// the first place in lo .. hi whose key is at least v; the wavefront probes 64 places a step
+__device__ __forceinline__ unsigned first_at_least(const unsigned* keys, unsigned lo, unsigned hi, unsigned v, int lane) {
+  while (hi > lo) {
+    const unsigned step = (hi - lo + 63) / 64, at = lo + step * lane;
+    const bool below = at < hi && keys[at] < v;
+    const int n = __popcll(__ballot(below));               // (keys are sorted: the first n probes)
+    if (n == 0) return lo;
+    const unsigned last = lo + step * (n - 1);             // its key is below v
+    hi = last + step < hi ? last + step : hi;
+    lo = last + 1;
+  }
+  return lo;
+}
+
+template <typename O> __device__ __forceinline__ void put8(O* p, const float (&v)[8], bool accumulate) {
+  if (accumulate) {
+    float w[8];
+    load8(p, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] += v[j];
+    store8(p, w);
+  } else store8(p, v);
+}
+
+template <typename T, typename O, int G>
+__global__ __launch_bounds__(NTHR) void table_kernel(SumArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / G;
+  constexpr int R = 64 / G;
+  const long v0 = ((long)blockIdx.x * 4 + wave) * a.vrows;
+  if (v0 >= a.e.vocab) return;
+  const unsigned v1 = (unsigned)(v0 + a.vrows < a.e.vocab ? v0 + a.vrows : a.e.vocab);
+  const unsigned lo = first_at_least(a.keys, 0, a.n, (unsigned)v0, lane);
+  const unsigned hi = first_at_least(a.keys, lo, a.n, v1, lane);
+  const Adder<T> add(a, blockIdx.y * G + lane % G);
+  O* out = reinterpret_cast<O*>(a.e.dtable.p);
+  unsigned start = lo;                                     // lane l: where the places of row v0 + l begin (vrows < 64)
+  for (unsigned h = hi; start < h;) {
+    const unsigned m = (start + h) / 2;
+    if (a.keys[m] < (unsigned)v0 + lane) start = m + 1; else h = m;
+  }
+  for (unsigned r = 0; r < a.vrows; r += R) {              // R rows of the table a step, each by its own lanes
+    const unsigned mine = (unsigned)v0 + r + sub;
+    const unsigned b = (unsigned)__shfl((int)start, r + sub), e = (unsigned)__shfl((int)start, r + sub + 1);
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    unsigned i = b;
+    while (i < e) {
+      if (i % CHUNK == 0 && i + CHUNK <= e) {
+        if (add.in) {
+          float t[8];
+          load8(a.chunk_sums + (long)(i / CHUNK) * (8 * a.units) + 8 * add.unit, t);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] += t[j];
+        }
+        i += CHUNK;
+        continue;
+      }
+      const unsigned stop = (i / CHUNK + 1) * CHUNK < e ? (i / CHUNK + 1) * CHUNK : e;
+      for (; i + 4 <= stop; i += 4) {
+        Raw8<T> r[4];
+        unsigned p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = a.places[i + k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add.load(r[k], p[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add.add(acc, r[k], p[k]);
+      }
+      for (; i < stop; ++i) {
+        Raw8<T> r;
+        const unsigned p = a.places[i];
+        add.load(r, p);
+        add.add(acc, r, p);
+      }
+    }
+    if (!add.in || mine >= v1 || (a.e.accumulate && e == b)) continue;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] *= a.key.factor;
+    put8(out + (long)mine * a.e.dtable.row + 8 * add.unit, acc, a.e.accumulate);
+  }
+}
+
+struct Sorted { unsigned *keys[2], *places[2], *counts, *totals; float* sums; size_t bytes; int blocks; };
+Sorted carve(char* p, long rows, int width) {
+  Sorted w;
+  size_t off = 0;
+  auto take = [&](size_t n) { char* q = p ? p + off : nullptr; off += (n + 255) / 256 * 256; return q; };
+  w.blocks = (int)((rows + SORT_E - 1) / SORT_E);
+  for (int i = 0; i < 2; ++i) {
+    w.keys[i] = reinterpret_cast<unsigned*>(take(4 * (size_t)rows));
+    w.places[i] = reinterpret_cast<unsigned*>(take(4 * (size_t)rows));
+  }
+  w.counts = reinterpret_cast<unsigned*>(take((size_t)w.blocks * SORT_D * 4));
+  w.totals = reinterpret_cast<unsigned*>(take(SORT_D * 4));
+  w.sums = reinterpret_cast<float*>(take((size_t)(rows / CHUNK) * width * 4));
+  w.bytes = off;
+  return w;
+}
+
+template <typename T, typename O, int G>
+hipError_t launch_sums(const SumArgs& a, hipStream_t s) {
+  const unsigned slices = (a.units + G - 1) / G, chunks = a.n / CHUNK;
+  if (chunks) chunk_kernel<T, G><<<dim3(chunks, slices), NTHR, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const unsigned per = 4 * a.vrows;
+  table_kernel<T, O, G><<<dim3((unsigned)((a.e.vocab + per - 1) / per), slices), NTHR, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <typename T, typename O>
+hipError_t launch_sums_t(const SumArgs& a, hipStream_t s) {
+  if (a.units <= 8) return launch_sums<T, O, 8>(a, s);
+  if (a.units <= 16) return launch_sums<T, O, 16>(a, s);
+  if (a.units <= 32) return launch_sums<T, O, 32>(a, s);
+  return launch_sums<T, O, 64>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_dropout(int dtype, const DropoutArgs& a, const DropoutKey& key, hipStream_t s) {
+  if (dtype == 0) return a.residual.p ? launch_dropout_t<float, true>(a, key, s) : launch_dropout_t<float, false>(a, key, s);
+  return a.residual.p ? launch_dropout_t<bf16_t, true>(a, key, s) : launch_dropout_t<bf16_t, false>(a, key, s);
+}
+
+hipError_t launch_embedding_fwd(int dtype, const EmbeddingArgs& a, const DropoutKey& key, hipStream_t s) {
+  return dtype == 0 ? launch_lookup_t<float>(a, key, s) : launch_lookup_t<bf16_t>(a, key, s);
+}
+
+size_t embedding_ws_bytes(long rows, long, int width) { return carve(nullptr, rows, width).bytes; }
+
+hipError_t launch_embedding_bwd(int dtype, const EmbeddingArgs& a, const DropoutKey& key, void* workspace, size_t bytes, hipStream_t s) {
+  const Sorted w = carve(reinterpret_cast<char*>(workspace), a.rows, a.width);
+  if (bytes < w.bytes) return hipErrorInvalidValue;
+  int bits = 1;
+  while ((a.vocab >> bits) > 0) ++bits;                    // keys are 0 .. vocab
+  const int passes = (bits + SORT_BITS - 1) / SORT_BITS, per = (bits + passes - 1) / passes;
+  SortArgs q{};
+  q.n = a.rows; q.vocab = (unsigned)a.vocab; q.blocks = w.blocks; q.counts = w.counts; q.totals = w.totals;
+  q.mask = (1 << per) - 1; q.scanned = w.blocks > 64;
+  for (int i = 0; i < passes && a.rows; ++i) {
+    q.tokens = i == 0 ? a.tokens : nullptr;
+    q.keys_in = w.keys[(i + 1) & 1]; q.places_in = w.places[(i + 1) & 1];
+    q.keys_out = w.keys[i & 1]; q.places_out = w.places[i & 1];
+    q.shift = i * per;
+    count_kernel<<<w.blocks, NTHR, 0, s>>>(q);
+    if (q.scanned) scan_kernel<<<SORT_D / 64, 64, 0, s>>>(q);
+    place_kernel<<<w.blocks, NTHR, 0, s>>>(q);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  SumArgs m{};
+  m.e = a; m.key = key;
+  m.keys = w.keys[(passes - 1) & 1]; m.places = w.places[(passes - 1) & 1];
+  m.chunk_sums = w.sums;
+  m.n = (unsigned)a.rows; m.units = (unsigned)(a.width / 8);
+  m.vrows = 16;
+  if (dtype == 0) return launch_sums_t<float, float>(m, s);
+  return a.grad_dtype == 0 ? launch_sums_t<bf16_t, float>(m, s) : launch_sums_t<bf16_t, bf16_t>(m, s);
+}
+
+}  // namespace hbp

@@ -4,6 +4,7 @@
 // allocates or synchronises.
 #include "../../include/hbp.h"
 #include "hbp_common.h"
+#include "philox.h"
 
 #include <cmath>
 #include <mutex>
@@ -1636,6 +1637,184 @@ hbp_status hbp_attention_backward(const hbp_attention_desc* d, const hbp_attenti
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps(HBP_PROF_ATTN, s);
   HBP_TRY(launch_packed_attn_bwd(d->dtype, a, b->workspace, b->workspace_bytes, s));
+  return HBP_OK;
+}
+
+namespace {
+
+// stride and alignment rules of hbp_rows; `written`: rows must not overlap
+hbp_status check_rows(const hbp_rows& x, int64_t rows, int64_t width, bool written) {
+  if (rows == 0) return HBP_OK;
+  if (!x.data) return HBP_E_NULL;
+  if (rows > 1 && x.row_stride < 0) return HBP_E_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(x.data) % 16) return HBP_E_UNSUPPORTED;
+  if (rows > 1 && (x.row_stride % 8 || x.row_stride > (1 << 22))) return HBP_E_UNSUPPORTED;
+  if (written && rows > 1 && x.row_stride < width) return HBP_E_INVALID_ARG;
+  return HBP_OK;
+}
+Rows rows_at(const hbp_rows& x, int64_t rows) { return {x.data, rows > 1 ? (long)x.row_stride : 0}; }
+hbp_status check_width(int64_t width) {
+  if (width <= 0) return HBP_E_INVALID_ARG;
+  return width % 8 || width > 65536 ? HBP_E_UNSUPPORTED : HBP_OK;
+}
+// `optional`: rate = 0 stands for none, whatever else is in it.  scale: what elements are multiplied by besides
+hbp_status check_dropout(const hbp_dropout_desc* d, bool optional, float scale, DropoutKey* key) {
+  *key = {};
+  key->factor = scale;
+  if (optional && d->rate == 0.f) return HBP_OK;
+  if (d->struct_size != sizeof(hbp_dropout_desc)) return HBP_E_INVALID_ARG;
+  if (!(d->rate >= 0.f && d->rate < 1.f)) return HBP_E_INVALID_ARG;
+  const double t = std::rint((double)d->rate * 65536.0);
+  if (t >= 65536.0) return HBP_E_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(d->counter) % 8) return HBP_E_UNSUPPORTED;
+  key->k0 = (unsigned)d->seed;
+  key->k1 = (unsigned)(d->seed >> 32);
+  key->offset = d->offset;
+  key->counter = reinterpret_cast<const unsigned long*>(d->counter);
+  key->threshold = (unsigned)t;
+  key->factor = (float)((double)scale * (65536.0 / (65536.0 - t)));
+  return HBP_OK;
+}
+
+hbp_status check_embedding(const hbp_embedding_desc* d, DropoutKey* key) {
+  if (!d) return HBP_E_NULL;
+  if (d->struct_size != sizeof(hbp_embedding_desc)) return HBP_E_INVALID_ARG;
+  if (d->dtype != HBP_F32 && d->dtype != HBP_BF16) return HBP_E_INVALID_ARG;
+  if (d->grad_dtype != HBP_F32 && d->grad_dtype != d->dtype) return HBP_E_INVALID_ARG;
+  if (!std::isfinite(d->scale) || d->rows < 0 || d->vocab < 1) return HBP_E_INVALID_ARG;
+  HBP_RUN(check_width(d->width));
+  if (d->rows > (1 << 24) || d->vocab > (1 << 24) || d->rows * d->width > (int64_t)1 << 36) return HBP_E_UNSUPPORTED;
+  HBP_RUN(check_dropout(&d->dropout, true, d->scale, key));
+  return std::isfinite(key->factor) ? HBP_OK : HBP_E_INVALID_ARG;
+}
+hbp_status embedding_call(const hbp_embedding_desc* d, const hbp_embedding_buffers* b, bool backward, EmbeddingArgs* a, DropoutKey* key) {
+  HBP_RUN(check_embedding(d, key));
+  if (!b) return HBP_E_NULL;
+  if (b->struct_size != sizeof(hbp_embedding_buffers)) return HBP_E_INVALID_ARG;
+  if (d->rows && !b->tokens) return HBP_E_NULL;
+  if (reinterpret_cast<uintptr_t>(b->tokens) % 4) return HBP_E_UNSUPPORTED;
+  *a = {};
+  a->tokens = b->tokens;
+  a->rows = d->rows; a->vocab = d->vocab; a->width = (int)d->width; a->grad_dtype = d->grad_dtype;
+  if (backward) {
+    HBP_RUN(check_rows(b->dout, d->rows, d->width, false));
+    HBP_RUN(check_rows(b->dtable, d->vocab, d->width, true));
+    const size_t need = embedding_ws_bytes(d->rows, d->vocab, (int)d->width);
+    if (need && (!b->workspace || b->workspace_bytes < need)) return HBP_E_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(b->workspace) % 16) return HBP_E_UNSUPPORTED;
+    a->dout = rows_at(b->dout, d->rows);
+    a->dtable = rows_at(b->dtable, d->vocab);
+  } else {
+    HBP_RUN(check_rows(b->table, d->rows ? d->vocab : 0, d->width, false));
+    HBP_RUN(check_rows(b->out, d->rows, d->width, true));
+    a->table = rows_at(b->table, d->vocab);
+    a->out = rows_at(b->out, d->rows);
+  }
+  return HBP_OK;
+}
+
+hbp_status check_cross_entropy(const hbp_cross_entropy_desc* d) {
+  if (!d) return HBP_E_NULL;
+  if (d->struct_size != sizeof(hbp_cross_entropy_desc)) return HBP_E_INVALID_ARG;
+  if (d->dtype != HBP_F32 && d->dtype != HBP_BF16) return HBP_E_INVALID_ARG;
+  if (d->grad_dtype != HBP_F32 && d->grad_dtype != d->dtype) return HBP_E_INVALID_ARG;
+  if (d->mean != 0 && d->mean != 1) return HBP_E_INVALID_ARG;
+  if (!(d->scale > 0.f && d->scale <= 0x1p127f) || !std::isfinite(d->factor)) return HBP_E_INVALID_ARG;   // (times log2 e: finite)
+  if (d->rows < 0 || d->vocab < 1) return HBP_E_INVALID_ARG;
+  HBP_RUN(check_width(d->width));
+  return d->rows > (1 << 20) || d->vocab > (1 << 24) ? HBP_E_UNSUPPORTED : HBP_OK;
+}
+
+}  // namespace
+
+hbp_status hbp_dropout(const hbp_dropout_desc* dropout, int dtype, int64_t rows, int64_t width, const hbp_rows* x,
+                       const hbp_rows* residual, const hbp_rows* out, void* stream) {
+  if (!dropout || !x || !out) return HBP_E_NULL;
+  if (dtype != HBP_F32 && dtype != HBP_BF16) return HBP_E_INVALID_ARG;
+  DropoutKey key;
+  HBP_RUN(check_dropout(dropout, false, 1.f, &key));
+  if (rows < 0) return HBP_E_INVALID_ARG;
+  HBP_RUN(check_width(width));
+  if (rows > (1 << 24) || rows * width > (int64_t)1 << 36) return HBP_E_UNSUPPORTED;
+  HBP_RUN(check_rows(*x, rows, width, false));
+  if (residual) HBP_RUN(check_rows(*residual, rows, width, false));
+  HBP_RUN(check_rows(*out, rows, width, true));
+  if (rows == 0) return HBP_OK;
+  for (const hbp_rows* in : {x, residual})
+    if (in && in->data == out->data && rows > 1 && in->row_stride != out->row_stride) return HBP_E_INVALID_ARG;
+  DropoutArgs a{};
+  a.x = rows_at(*x, rows); a.out = rows_at(*out, rows);
+  if (residual) a.residual = rows_at(*residual, rows);
+  a.rows = rows; a.width = (int)width;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_OTHER, s);
+  HBP_TRY(launch_dropout(dtype, a, key, s));
+  return HBP_OK;
+}
+
+hbp_status hbp_embedding_workspace_size(const hbp_embedding_desc* d, size_t* bytes) {
+  if (!bytes) return HBP_E_NULL;
+  DropoutKey key;
+  HBP_RUN(check_embedding(d, &key));
+  *bytes = embedding_ws_bytes(d->rows, d->vocab, (int)d->width);
+  return HBP_OK;
+}
+
+hbp_status hbp_embedding_forward(const hbp_embedding_desc* d, const hbp_embedding_buffers* b, void* stream) {
+  EmbeddingArgs a;
+  DropoutKey key;
+  HBP_RUN(embedding_call(d, b, false, &a, &key));
+  if (d->rows == 0) return HBP_OK;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_OTHER, s);
+  HBP_TRY(launch_embedding_fwd(d->dtype, a, key, s));
+  return HBP_OK;
+}
+
+hbp_status hbp_embedding_backward(const hbp_embedding_desc* d, const hbp_embedding_buffers* b, int accumulate, void* stream) {
+  EmbeddingArgs a;
+  DropoutKey key;
+  if (accumulate != 0 && accumulate != 1) return HBP_E_INVALID_ARG;
+  HBP_RUN(embedding_call(d, b, true, &a, &key));
+  if (d->rows == 0 && accumulate) return HBP_OK;
+  a.accumulate = accumulate;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_OTHER, s);
+  HBP_TRY(launch_embedding_bwd(d->dtype, a, key, b->workspace, b->workspace_bytes, s));
+  return HBP_OK;
+}
+
+hbp_status hbp_cross_entropy_workspace_size(const hbp_cross_entropy_desc* d, int gradients, size_t* bytes) {
+  if (!bytes) return HBP_E_NULL;
+  HBP_RUN(check_cross_entropy(d));
+  *bytes = cross_entropy_ws_bytes(d->dtype, d->rows, d->vocab, (int)d->width, gradients != 0);
+  return HBP_OK;
+}
+
+hbp_status hbp_loss_cross_entropy(const hbp_cross_entropy_desc* d, const hbp_cross_entropy_buffers* b, void* stream) {
+  HBP_RUN(check_cross_entropy(d));
+  if (!b) return HBP_E_NULL;
+  if (b->struct_size != sizeof(hbp_cross_entropy_buffers)) return HBP_E_INVALID_ARG;
+  if (!b->loss || (d->rows && !b->targets)) return HBP_E_NULL;
+  for (const void* p : {(const void*)b->loss, (const void*)b->row_loss, (const void*)b->targets})
+    if (reinterpret_cast<uintptr_t>(p) % 4) return HBP_E_UNSUPPORTED;
+  HBP_RUN(check_rows(b->x, d->rows, d->width, false));
+  HBP_RUN(check_rows(b->weight, d->rows ? d->vocab : 0, d->width, false));
+  if (b->dx.data) HBP_RUN(check_rows(b->dx, d->rows, d->width, true));
+  if (b->dweight.data) HBP_RUN(check_rows(b->dweight, d->vocab, d->width, true));
+  CrossEntropyArgs a{};
+  a.x = rows_at(b->x, d->rows); a.weight = rows_at(b->weight, d->vocab);
+  a.targets = b->targets; a.loss = b->loss; a.row_loss = b->row_loss;
+  a.dx = rows_at(b->dx, d->rows); a.dweight = rows_at(b->dweight, d->vocab);
+  a.grad_dtype = d->grad_dtype; a.mean = d->mean;
+  a.scale = d->scale; a.factor = d->factor;
+  a.rows = d->rows; a.vocab = d->vocab; a.width = (int)d->width;
+  const size_t need = cross_entropy_ws_bytes(d->dtype, d->rows, d->vocab, (int)d->width, b->dx.data || b->dweight.data);
+  if (need && (!b->workspace || b->workspace_bytes < need)) return HBP_E_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(b->workspace) % 16) return HBP_E_UNSUPPORTED;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(HBP_PROF_OTHER, s);
+  HBP_TRY(launch_cross_entropy(d->dtype, a, b->workspace, b->workspace_bytes, s));
   return HBP_OK;
 }
 

@@ -271,6 +271,44 @@ size_t packed_attn_ws_bytes(int dtype, const PackedAttnArgs& a);
 hipError_t launch_packed_attn_fwd(int dtype, const PackedAttnArgs& a, void* workspace, size_t bytes, hipStream_t s);
 hipError_t launch_packed_attn_bwd(int dtype, const PackedAttnArgs& a, void* workspace, size_t bytes, hipStream_t s);
 
+// ---------------------------------------------------------------------------
+// the two ends of a language model (embedding.hip, cross_entropy.hip); row strides in elements
+// ---------------------------------------------------------------------------
+struct DropoutKey;            // philox.h
+struct Rows { void* p; long row; };
+struct DropoutArgs {
+  Rows x, residual, out;      // residual.p NULL: none
+  long rows;
+  int width;
+};
+hipError_t launch_dropout(int dtype, const DropoutArgs& a, const DropoutKey& key, hipStream_t s);
+struct EmbeddingArgs {
+  const int* tokens;
+  Rows table, out;            // forward
+  Rows dout, dtable;          // backward; dtable in grad_dtype
+  int grad_dtype, accumulate;
+  long rows, vocab;
+  int width;
+};
+// (key.factor: what a table's row is multiplied by; key.threshold 0: without dropout)
+hipError_t launch_embedding_fwd(int dtype, const EmbeddingArgs& a, const DropoutKey& key, hipStream_t s);
+size_t embedding_ws_bytes(long rows, long vocab, int width);
+hipError_t launch_embedding_bwd(int dtype, const EmbeddingArgs& a, const DropoutKey& key, void* workspace, size_t bytes, hipStream_t s);
+struct CrossEntropyArgs {
+  Rows x, weight;
+  const int* targets;
+  float* loss;
+  float* row_loss;            // or NULL
+  Rows dx, dweight;           // p NULL: not wanted; dweight in grad_dtype
+  int grad_dtype, mean;
+  float scale, factor;
+  long rows, vocab;
+  int width;
+};
+// The launchers refuse (hipErrorInvalidValue, nothing launched) a workspace of fewer bytes than these.
+size_t cross_entropy_ws_bytes(int dtype, long rows, long vocab, int width, bool gradients);
+hipError_t launch_cross_entropy(int dtype, const CrossEntropyArgs& a, void* workspace, size_t bytes, hipStream_t s);
+
 // Few-row bf16 product with both operands K-contiguous: C[M,N] = epilogue(A[M,K] . Bt[N,K]^T).
 // Modes EPI_STORE, EPI_ACT_TANH, EPI_MUL_AUX, EPI_MUL_1MZ2, EPI_ADD_AUX; aux is bf16 [M,N] with row stride ldaux.
 // EPI_RESID here is the residual path's backward step, C = acc (+ aux) + lambda (.) next: next and
