@@ -23,13 +23,15 @@ struct Parts {
   float* lse;             // [np], base 2; infinity where a row does not count: its probabilities are zeros
   int* target;            // [np], -1 where a row does not count
   float* rows;            // [np] row losses
+  float* at_target;       // [np] the target's softmax less 1
   float* scalars;         // [4]: the factor on dS
   float* sums;            // [blocks][np]: base 2 logarithms of a block's sums
   float* logits;          // [piece][np]
   void* grad;             // [piece][np], storage type (fp32: the logits' place)
   float* dx;              // [shares][np, width]
   long np, piece;
-  int blocks, pieces, shares;   // shares: products whose results lie side by side until they are added up
+  long fused;             // rows of the vocabulary whose logits meet no memory
+  int blocks, pieces, split, shares;   // shares: products whose results lie side by side until they are added up
   size_t bytes;
 };
 
@@ -37,7 +39,9 @@ struct CeArgs {
   CrossEntropyArgs c;
   Parts p;
   float to_log2;          // scale log2 e
-  long v0, nv;            // the piece at hand
+  long v0, nv;            // the rows of the vocabulary at hand
+  long block0;            // their first block of sums
+  long grad0;             // where their dS begins in its piece
 };
 
 // x's copy, the target's logit: a wavefront a row
@@ -122,7 +126,7 @@ __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
     r.add(top, nan ? NAN : sum);
   }
   const Running t = meet<TB>(r, part, row, sm, sl);
-  if (part == 0 && n < a.p.np) a.p.sums[(a.v0 / BLOCK_V + blockIdx.y) * a.p.np + n] = log2_sum(t);
+  if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = log2_sum(t);
 }
 // all blocks of a row, its loss
 template <int TB>
@@ -142,6 +146,7 @@ __global__ __launch_bounds__(NTHR) void row_loss_kernel(CeArgs a) {
   const float lse = log2_sum(t);
   const float loss = counts ? (lse - a.p.target_logit[n]) * LN2 : 0.f;
   a.p.lse[n] = counts ? lse : INFINITY;
+  a.p.at_target[n] = counts ? exp2f(a.p.target_logit[n] - lse) - 1.f : 0.f;
   a.p.rows[n] = loss;
   if (a.c.row_loss && n < a.c.rows) a.c.row_loss[n] = loss;
 }
@@ -182,11 +187,10 @@ __global__ __launch_bounds__(NTHR) void grad_kernel(CeArgs a) {
   const float g = a.p.scalars[0];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float p = lse[j] == INFINITY ? 0.f : exp2f(fmaf(s[j], a.to_log2, -lse[j]));
-    if (a.p.target[n + j] == a.v0 + v) p -= 1.f;
-    s[j] = p * g;
+    const float p = lse[j] == INFINITY ? 0.f : exp2f(fmaf(s[j], a.to_log2, -lse[j]));
+    s[j] = (a.p.target[n + j] == a.v0 + v ? a.p.at_target[n + j] : p) * g;
   }
-  store8(reinterpret_cast<T*>(a.p.grad) + v * a.p.np + n, s);
+  store8(reinterpret_cast<T*>(a.p.grad) + (a.grad0 + v) * a.p.np + n, s);
 }
 
 // the first share of dx += the others; elements of 8
@@ -233,32 +237,61 @@ __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, 
 }
 
 // ---- sizes -----------------------------------------------------------------------------------------------------------
-// A piece's logits take 1 GB at most (256 rows of the vocabulary: more, from 2^20 rows on), and four pieces' dx lie side by side.
-constexpr long PIECE_LOGITS = 1l << 28, PIECE_ROWS = 1l << 20;
-constexpr int SHARES = 4;
+// A piece of the vocabulary takes 1 GB of logits, or of dS where the logits are not written (256 rows of the vocabulary: more, from 2^20 rows
+// of x on).
+constexpr size_t PIECE_BYTES = 1ul << 30;
+constexpr long PIECE_ROWS = 1l << 20;
+constexpr int MAX_SPLIT = 16;
+
+// Rows of x are filled up to whole tiles of 256 where that is an eighth more at most, else to 8.
+long padded(long rows) {
+  const long whole = (rows + 255) / 256 * 256;
+  return whole <= rows + rows / 8 ? whole : (rows + 7) / 8 * 8;
+}
+// Rows of the vocabulary that the 256 x 256 kernel's own epilogues take: all whole tiles, where those fill the chip.
+long fused_rows(int dtype, long np, long vocab, int width) {
+  if (dtype != 1 || np % 256 || np == 0 || width % 32 || width < 128) return 0;
+  const long tiles = vocab / 256 * (np / 256);
+  return gemm_fills_chip(tiles) && tiles < (1l << 28) ? vocab / 256 * 256 : 0;
+}
+// dx has few tiles and a long contraction, the vocabulary: it is shared out until there is a tile for every compute unit.
+int dx_split(int dtype, long np, int width, long nv) {
+  const long t = dtype == 0 ? 64 : np % 256 == 0 && width % 256 == 0 ? 256 : 128;
+  const long tiles = (np + t - 1) / t * ((width + t - 1) / t);
+  long split = (256 + tiles / 2) / tiles;
+  if (split > nv / 512) split = nv / 512;
+  return (int)(split < 1 ? 1 : split > MAX_SPLIT ? MAX_SPLIT : split);
+}
+
 Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradients) {
   Parts p{};
   size_t off = 0;
   auto take = [&](size_t n) { char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
   const size_t es = dtype == 0 ? 4 : 2;
-  p.np = (rows + 7) / 8 * 8;
-  const long fit = PIECE_LOGITS / (p.np ? p.np : 1) / BLOCK_V * BLOCK_V;
-  p.piece = fit < BLOCK_V ? BLOCK_V : fit < PIECE_ROWS ? fit : PIECE_ROWS;
-  if (p.piece > vocab) p.piece = vocab;
+  p.np = padded(rows);
+  p.fused = fused_rows(dtype, p.np, vocab, width);
+  const size_t row = (p.fused ? 2 : 4) * (p.np ? p.np : 1);
+  const long fit = (long)(PIECE_BYTES / row) / BLOCK_V * BLOCK_V;
+  const long most = fit < BLOCK_V ? BLOCK_V : fit < PIECE_ROWS ? fit : PIECE_ROWS;
+  p.pieces = (int)((vocab + most - 1) / most);             // of one size, as near as whole blocks allow
+  p.piece = ((vocab + p.pieces - 1) / p.pieces + BLOCK_V - 1) / BLOCK_V * BLOCK_V;
   p.pieces = (int)((vocab + p.piece - 1) / p.piece);
-  p.blocks = (int)((vocab + BLOCK_V - 1) / BLOCK_V);
+  if (p.piece > vocab) p.piece = vocab;
+  p.blocks = p.fused ? (int)(p.fused / 128 + (p.fused < vocab)) : (int)((vocab + BLOCK_V - 1) / BLOCK_V);
   p.x = take(p.np * width * es);
   p.target_logit = reinterpret_cast<float*>(take(4 * p.np));
   p.lse = reinterpret_cast<float*>(take(4 * p.np));
   p.target = reinterpret_cast<int*>(take(4 * p.np));
   p.rows = reinterpret_cast<float*>(take(4 * p.np));
+  p.at_target = reinterpret_cast<float*>(take(4 * p.np));
   p.scalars = reinterpret_cast<float*>(take(16));
   p.sums = reinterpret_cast<float*>(take((size_t)p.blocks * p.np * 4));
-  p.logits = reinterpret_cast<float*>(take((size_t)p.piece * p.np * 4));
+  p.logits = reinterpret_cast<float*>(take((size_t)(p.fused ? vocab - p.fused : p.piece) * p.np * 4));
   p.grad = p.logits;
   if (gradients) {
     if (dtype == 1) p.grad = take((size_t)p.piece * p.np * 2);
-    p.shares = p.pieces < SHARES ? p.pieces : SHARES;
+    p.split = dx_split(dtype, p.np ? p.np : 8, width, p.piece);
+    p.shares = p.split + 2 < 4 ? 4 : p.split + 2;
     p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * width * 4));
   }
   p.bytes = off;
@@ -274,6 +307,11 @@ hipError_t product(int dtype, const GemmArgs& g, hipStream_t s) {
   }
   return launch_gemm_generic(dtype, g, s);
 }
+GemmArgs plain() {
+  GemmArgs g{};
+  g.batch = 1; g.split_k = 1; g.mode = EPI_STORE;
+  return g;
+}
 
 #define CE_TRY(call)                      \
   do {                                    \
@@ -282,91 +320,159 @@ hipError_t product(int dtype, const GemmArgs& g, hipStream_t s) {
   } while (0)
 
 template <typename T>
-hipError_t run(int dtype, const CrossEntropyArgs& c, const Parts& p, hipStream_t s) {
-  CeArgs a{};
-  a.c = c; a.p = p; a.to_log2 = c.scale * LOG2E;
-  const bool grads = c.dx.p || c.dweight.p;
-  const T* weight = reinterpret_cast<const T*>(c.weight.p);
-  if (c.rows == 0) {                                       // nothing counts
+struct Run {
+  static constexpr int DTYPE = sizeof(T) == 4 ? 0 : 1;
+  const CrossEntropyArgs& c;
+  const Parts& p;
+  hipStream_t s;
+  CeArgs a;
+  int shares = 0;
+  Run(const CrossEntropyArgs& c_, const Parts& p_, hipStream_t s_) : c(c_), p(p_), s(s_), a{} { a.c = c; a.p = p; a.to_log2 = c.scale * LOG2E; }
+
+  GemmArgs logits_args(long v0, long nv) const {
+    GemmArgs g = plain();
+    g.A = reinterpret_cast<const T*>(c.weight.p) + v0 * c.weight.row; g.a_sm = c.weight.row; g.a_sk = 1;
+    g.B = p.x; g.b_sn = c.width; g.b_sk = 1;
+    g.ldc = p.np;
+    g.M = nv; g.N = p.np; g.K = c.width;
+    return g;
+  }
+  void at(long v0, long nv) { a.v0 = v0; a.nv = nv; a.grad0 = 0; }
+  hipError_t logits() {
+    GemmArgs g = logits_args(a.v0, a.nv);
+    g.C = p.logits; g.c_is_f32 = 1;
+    return product(DTYPE, g, s);
+  }
+  hipError_t block_sums(long block0) {
+    a.block0 = block0;
+    const unsigned nb = (unsigned)((a.nv + BLOCK_V - 1) / BLOCK_V);
+    if (p.np >= 64) block_sums_kernel<64><<<dim3((unsigned)((p.np + 63) / 64), nb), NTHR, 0, s>>>(a);
+    else block_sums_kernel<8><<<dim3((unsigned)(p.np / 8), nb), NTHR, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  hipError_t softmax_grad() {
+    grad_kernel<T><<<(unsigned)((a.nv * (p.np / 8) + NTHR - 1) / NTHR), NTHR, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  hipError_t fold() {
+    const long n8 = p.np * c.width / 8;
+    fold_kernel<<<(unsigned)((n8 + NTHR - 1) / NTHR), NTHR, 0, s>>>(p.dx, n8, shares);
+    shares = 1;
+    return hipGetLastError();
+  }
+
+  hipError_t sums() {
+    if (p.fused) {
+      GemmArgs g = logits_args(0, p.fused);
+      g.C = p.sums; g.mode = EPI_VOCAB_SUMS; g.vocab.alpha = a.to_log2;
+      CE_TRY(launch_gemm_vocab(g, s));
+      if (p.fused == c.vocab) return hipSuccess;
+      at(p.fused, c.vocab - p.fused);
+      CE_TRY(logits());
+      return block_sums(p.fused / 128);
+    }
+    for (int i = 0; i < p.pieces; ++i) {
+      at(i * p.piece, c.vocab - i * p.piece < p.piece ? c.vocab - i * p.piece : p.piece);
+      CE_TRY(logits());
+      CE_TRY(block_sums(a.v0 / BLOCK_V));
+    }
+    return hipSuccess;
+  }
+  // dS of rows v0 .. v0 + nv of the vocabulary; the last ones, and with one piece all of them, have their logits in memory
+  hipError_t piece_grad(long v0, long nv) {
+    at(v0, nv);
+    if (!p.fused) {
+      if (p.pieces > 1) CE_TRY(logits());
+      return softmax_grad();
+    }
+    const long nf = v0 + nv < p.fused ? nv : p.fused > v0 ? p.fused - v0 : 0;
+    if (nf > 0) {
+      GemmArgs g = logits_args(v0, nf);
+      g.C = p.grad; g.mode = EPI_VOCAB_GRAD;
+      g.vocab = {a.to_log2, p.lse, p.target, p.at_target, p.scalars, v0};
+      CE_TRY(launch_gemm_vocab(g, s));
+    }
+    if (nf == nv) return hipSuccess;
+    at(v0 + nf, nv - nf);
+    a.grad0 = nf;
+    return softmax_grad();
+  }
+  hipError_t dweight_rows(long v0, long r0, long nr) {
+    GemmArgs g = plain();
+    g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = p.np; g.a_sk = 1;
+    g.B = p.x; g.b_sk = c.width; g.b_sn = 1;
+    g.c_is_f32 = c.grad_dtype == 0;
+    const long o = (v0 + r0) * c.dweight.row;
+    if (g.c_is_f32) g.C = reinterpret_cast<float*>(c.dweight.p) + o;
+    else g.C = reinterpret_cast<bf16_t*>(c.dweight.p) + o;
+    g.ldc = c.dweight.row;
+    g.M = nr; g.N = c.width; g.K = p.np;
+    return product(DTYPE, g, s);
+  }
+  // (whole tiles of 256 rows by themselves where those fill the chip: the last ones would take all others to smaller tiles)
+  hipError_t dweight(long v0, long nv) {
+    const long whole = nv / 256 * 256;
+    if (DTYPE == 1 && whole < nv && c.width % 256 == 0 && p.np % 32 == 0 && gemm_fills_chip(whole / 256 * (c.width / 256))) {
+      CE_TRY(dweight_rows(v0, 0, whole));
+      return dweight_rows(v0, whole, nv - whole);
+    }
+    return dweight_rows(v0, 0, nv);
+  }
+  hipError_t dx_rows(long v0, long r0, long nr, int split) {
+    GemmArgs g = plain();
+    g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = 1; g.a_sk = p.np;
+    g.B = reinterpret_cast<const T*>(c.weight.p) + (v0 + r0) * c.weight.row; g.b_sk = c.weight.row; g.b_sn = 1;
+    if (shares + split > p.shares) CE_TRY(fold());
+    g.C = p.dx + (long)shares * p.np * c.width; g.ldc = c.width; g.c_is_f32 = 1;
+    g.c_sb = p.np * c.width;
+    g.split_k = split;
+    shares += split;
+    g.M = p.np; g.N = c.width; g.K = nr;
+    return product(DTYPE, g, s);
+  }
+  // (a contraction that is no multiple of 32 keeps the 256 x 256 kernel from all of it)
+  hipError_t dx(long v0, long nv) {
+    const long whole = nv / 32 * 32;
+    if (DTYPE == 1 && whole < nv && whole > 0 && p.np % 256 == 0) {
+      CE_TRY(dx_rows(v0, 0, whole, dx_split(DTYPE, p.np, c.width, whole)));
+      return dx_rows(v0, whole, nv - whole, 1);
+    }
+    return dx_rows(v0, 0, nv, dx_split(DTYPE, p.np, c.width, nv));
+  }
+
+  hipError_t without_rows() {
     loss_kernel<<<1, 1024, 0, s>>>(a);
-    CE_TRY(hipGetLastError());
-  } else {
+    if (c.dweight.p) {
+      const unsigned blocks = (unsigned)((c.vocab * (c.width / 8) + NTHR - 1) / NTHR);
+      if (c.grad_dtype == 0) clear_kernel<float><<<blocks, NTHR, 0, s>>>(reinterpret_cast<float*>(c.dweight.p), c.dweight.row, c.vocab, c.width);
+      else clear_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(reinterpret_cast<bf16_t*>(c.dweight.p), c.dweight.row, c.vocab, c.width);
+    }
+    return hipGetLastError();
+  }
+  hipError_t all() {
+    if (c.rows == 0) return without_rows();
     rows_kernel<T><<<(unsigned)((p.np + 3) / 4), NTHR, 0, s>>>(a);
     CE_TRY(hipGetLastError());
-  }
-  auto logits = [&](long v0, long nv) {
-    GemmArgs g{};
-    g.A = weight + v0 * c.weight.row; g.a_sm = c.weight.row; g.a_sk = 1;
-    g.B = p.x; g.b_sn = c.width; g.b_sk = 1;
-    g.C = p.logits; g.ldc = p.np; g.c_is_f32 = 1;
-    g.M = nv; g.N = p.np; g.K = c.width;
-    g.batch = 1; g.split_k = 1; g.mode = EPI_STORE;
-    return product(dtype, g, s);
-  };
-  auto piece_at = [&](int i) { a.v0 = i * p.piece; a.nv = c.vocab - a.v0 < p.piece ? c.vocab - a.v0 : p.piece; };
-  if (c.rows) {
-    for (int i = 0; i < p.pieces; ++i) {
-      piece_at(i);
-      CE_TRY(logits(a.v0, a.nv));
-      const unsigned nb = (unsigned)((a.nv + BLOCK_V - 1) / BLOCK_V);
-      if (p.np >= 64) block_sums_kernel<64><<<dim3((unsigned)((p.np + 63) / 64), nb), NTHR, 0, s>>>(a);
-      else block_sums_kernel<8><<<dim3((unsigned)(p.np / 8), nb), NTHR, 0, s>>>(a);
-      CE_TRY(hipGetLastError());
-    }
+    CE_TRY(sums());
     if (p.np >= 4096) row_loss_kernel<64><<<(unsigned)((p.np + 63) / 64), NTHR, 0, s>>>(a);
     else row_loss_kernel<8><<<(unsigned)(p.np / 8), NTHR, 0, s>>>(a);
     loss_kernel<<<1, 1024, 0, s>>>(a);
     CE_TRY(hipGetLastError());
-  }
-  if (!grads) return hipSuccess;
-  if (c.rows == 0) {
-    if (!c.dweight.p) return hipSuccess;
-    const unsigned blocks = (unsigned)((c.vocab * (c.width / 8) + NTHR - 1) / NTHR);
-    if (c.grad_dtype == 0) clear_kernel<float><<<blocks, NTHR, 0, s>>>(reinterpret_cast<float*>(c.dweight.p), c.dweight.row, c.vocab, c.width);
-    else clear_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(reinterpret_cast<bf16_t*>(c.dweight.p), c.dweight.row, c.vocab, c.width);
-    return hipGetLastError();
-  }
-  int shares = 0;
-  for (int i = 0; i < p.pieces; ++i) {
-    piece_at(i);
-    if (p.pieces > 1) CE_TRY(logits(a.v0, a.nv));
-    grad_kernel<T><<<(unsigned)((a.nv * (p.np / 8) + NTHR - 1) / NTHR), NTHR, 0, s>>>(a);
-    CE_TRY(hipGetLastError());
-    if (c.dweight.p) {
-      GemmArgs g{};
-      g.A = p.grad; g.a_sm = p.np; g.a_sk = 1;
-      g.B = p.x; g.b_sk = c.width; g.b_sn = 1;
-      g.c_is_f32 = c.grad_dtype == 0;
-      if (g.c_is_f32) g.C = reinterpret_cast<float*>(c.dweight.p) + a.v0 * c.dweight.row;
-      else g.C = reinterpret_cast<bf16_t*>(c.dweight.p) + a.v0 * c.dweight.row;
-      g.ldc = c.dweight.row;
-      g.M = a.nv; g.N = c.width; g.K = p.np;
-      g.batch = 1; g.split_k = 1; g.mode = EPI_STORE;
-      CE_TRY(product(dtype, g, s));
+    if (!c.dx.p && !c.dweight.p) return hipSuccess;
+    for (int i = 0; i < p.pieces; ++i) {
+      const long v0 = i * p.piece, nv = c.vocab - v0 < p.piece ? c.vocab - v0 : p.piece;
+      CE_TRY(piece_grad(v0, nv));
+      if (c.dweight.p) CE_TRY(dweight(v0, nv));
+      if (c.dx.p) CE_TRY(dx(v0, nv));
     }
     if (c.dx.p) {
-      if (shares == p.shares) {
-        const long n8 = p.np * c.width / 8;
-        fold_kernel<<<(unsigned)((n8 + NTHR - 1) / NTHR), NTHR, 0, s>>>(p.dx, n8, shares);
-        CE_TRY(hipGetLastError());
-        shares = 1;
-      }
-      GemmArgs g{};
-      g.A = p.grad; g.a_sm = 1; g.a_sk = p.np;
-      g.B = weight + a.v0 * c.weight.row; g.b_sk = c.weight.row; g.b_sn = 1;
-      g.C = p.dx + (long)shares++ * p.np * c.width; g.ldc = c.width; g.c_is_f32 = 1;
-      g.M = p.np; g.N = c.width; g.K = a.nv;
-      g.batch = 1; g.split_k = 1; g.mode = EPI_STORE;
-      CE_TRY(product(dtype, g, s));
+      const unsigned per = (unsigned)(c.width / 8);
+      dx_kernel<T><<<(unsigned)((c.rows * per + NTHR - 1) / NTHR), NTHR, 0, s>>>(a, Divisor(per), shares);
+      CE_TRY(hipGetLastError());
     }
+    return hipSuccess;
   }
-  if (c.dx.p) {
-    const unsigned per = (unsigned)(c.width / 8);
-    dx_kernel<T><<<(unsigned)((c.rows * per + NTHR - 1) / NTHR), NTHR, 0, s>>>(a, Divisor(per), shares);
-    CE_TRY(hipGetLastError());
-  }
-  return hipSuccess;
-}
+};
 
 }  // namespace
 
@@ -377,7 +483,7 @@ size_t cross_entropy_ws_bytes(int dtype, long rows, long vocab, int width, bool 
 hipError_t launch_cross_entropy(int dtype, const CrossEntropyArgs& c, void* workspace, size_t bytes, hipStream_t s) {
   const Parts p = carve(reinterpret_cast<char*>(workspace), dtype, c.rows, c.vocab, c.width, c.dx.p || c.dweight.p);
   if (bytes < p.bytes) return hipErrorInvalidValue;
-  return dtype == 0 ? run<float>(dtype, c, p, s) : run<bf16_t>(dtype, c, p, s);
+  return dtype == 0 ? Run<float>(c, p, s).all() : Run<bf16_t>(c, p, s).all();
 }
 
 }  // namespace hbp

@@ -192,8 +192,36 @@ enum FastEpi {
   FAST_MUL_1MZ2 = 4,   // C(bf16) = acc * (1 - aux^2)
   FAST_ADD_AUX = 5,    // C(bf16) = acc + aux
   FAST_RESID = 6,      // C(bf16) = acc + lambda[n] * aux   (forward: x_{l+1}; lambda NULL = 1)
-  FAST_ACT_GELU = 7    // C(bf16) = gelu(acc), out2(bf16) = gelu'(acc)   (forward: z and act')
+  FAST_ACT_GELU = 7,   // C(bf16) = gelu(acc), out2(bf16) = gelu'(acc)   (forward: z and act')
+  FAST_VOCAB_SUMS = 8, // sums over 128 rows (EPI_VOCAB_SUMS)
+  FAST_VOCAB_GRAD = 9  // C(bf16) = gain (2^(alpha acc - lse[n]) - onehot)
 };
+
+// Sums of 2^(alpha acc) over a wavefront's 128 rows, for each of its 64 columns.  The products of this form are issued with the
+// operands the other way round, so that a lane holds 64 rows of one column in each acc[.][j] and its neighbour 32 lanes on the other 64.
+__device__ __forceinline__ void epilogue_sums(const GemmArgs& g, const TileCoord& tc, const float16v (&acc)[4][2], int wm0, int wn0,
+                                              int lane) {
+  const float alpha = g.vocab.alpha;
+  float* c = reinterpret_cast<float*>(g.C) + (tc.m0 + wm0) / 128 * g.ldc + tc.n0 + wn0 + (lane & 31);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    float top = acc[0][j][0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float shift = top == -INFINITY ? 0.f : top * alpha;      // (alpha > 0)
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[i] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], alpha, -shift));
+    float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    l += __shfl_xor(l, 32);
+    if (lane < 32) c[32 * j] = shift + __builtin_amdgcn_logf(l);
+  }
+}
 
 // Straight-line epilogue from the registers for a tile fully inside the matrix (fp32 output).
 __device__ __forceinline__ void epilogue_f32(const GemmArgs& g, const TileCoord& tc, const float16v (&acc)[4][2], int wm0, int wn0,
@@ -275,6 +303,23 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
       }
     }
   }
+  // FAST_VOCAB_GRAD: the columns' logarithms, in the MFMA layout as well, and lane c's column's target
+  constexpr bool VOCAB = FAST == FAST_VOCAB_GRAD;
+  float lse[8][4];
+  float gain = 0.f, at_target = 0.f;
+  int target = 0;
+  if (VOCAB) {
+    gain = *g.vocab.gain;
+    const float* lp = g.vocab.lse + tc.n0 + wn0 + 4 * mh;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float4 t = *reinterpret_cast<const float4*>(lp + 8 * k);
+      lse[k][0] = t.x; lse[k][1] = t.y; lse[k][2] = t.z; lse[k][3] = t.w;
+    }
+    const long n = tc.n0 + wn0 + lane, t = (long)g.vocab.target[n] - (g.vocab.row0 + tc.m0 + wm0);
+    target = t < 0 || t >= 128 ? -1 : (int)t;
+    at_target = g.vocab.at_target[n] * gain;
+  }
   // staging addresses, row layout: rows rr, rr + 8, rr + 16, rr + 24
   auto row_at = [&](int r) { return stg + r * 128 + ((rk ^ ((r >> 1) & 7)) << 4); };
   unsigned char* const p0 = row_at(rr);
@@ -327,6 +372,10 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
             else v[x] *= (1.f - t[x] * t[x]);
           }
         }
+        if (VOCAB) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_exp2f(fmaf(v[x], g.vocab.alpha, -lse[4 * j + qd][x])) * gain;
+        }
         if (TWO_OUT) {
           float dz[4];
 #pragma unroll
@@ -335,6 +384,12 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
         }
         *reinterpret_cast<uint2*>(m_base + (((4 * j + qd) ^ m_sw) << 4)) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
       }
+    if (VOCAB && (target >> 5) == i) {     // the target's row of this column is among these 32
+      __builtin_amdgcn_wave_barrier();
+      const int r = target & 31;
+      *reinterpret_cast<bf16_t*>(stg + r * 128 + (((lane >> 3) ^ ((r >> 1) & 7)) << 4) + 2 * (lane & 7)) =
+          (bf16_t)pack2(at_target, 0.f);
+    }
     flush(cp + (long)(32 * i) * g.ldc);
     if (TWO_OUT) {
 #pragma unroll
@@ -354,7 +409,8 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
   round(std::integral_constant<int, 3>(), qd);
 }
 template <int FAST> struct StagedOps {   // vector-memory operations per wave of one epilogue (a lower bound: the
-  static constexpr int value = FAST == FAST_STORE_F32 ? 32 : FAST == FAST_STORE ? 16 : 32;   // waits stay safe with more)
+  static constexpr int value = FAST == FAST_VOCAB_SUMS ? 2 : FAST == FAST_STORE || FAST == FAST_VOCAB_GRAD ? 16 : 32;   // waits stay safe
+                                                                                              // with more)
 };
 
 constexpr int PAIR_AREA = 2 * A_BYTES;                   // 256 rows x 128 bytes: two slices of a K-contiguous operand
@@ -469,6 +525,7 @@ __global__ __launch_bounds__(NTHR, 1) void gemm_mfma_lean_kernel(GemmArgs g, Wal
     }
   };
 
+  constexpr bool SUMS = FAST == FAST_VOCAB_SUMS;
   float16v acc[4][2];
   bf16x8 fa[4][2], fb[2][2];
   Quad16 aux0 = {}, aux1 = {};   // the first half of a tile's fused operand
@@ -504,7 +561,8 @@ __global__ __launch_bounds__(NTHR, 1) void gemm_mfma_lean_kernel(GemmArgs g, Wal
   // meets it after its epilogue instead: the two groups' epilogues, chains of LDS and memory latencies, then run in
   // the same tick, not one after the other.  Measured: 16384 x 4096 x 1024 with GELU 183 -> 174 us, 32768 x 1024 x 256 47 -> 41,
   // 12 x 32768 x 1024 x 256 with act' 329 -> 325; plain stores 1 % slower, so not there.
-  constexpr bool TOGETHER = EARLY || FAST == FAST_ACT_GELU;
+  constexpr bool VOCAB = FAST == FAST_VOCAB_SUMS || FAST == FAST_VOCAB_GRAD;
+  constexpr bool TOGETHER = EARLY || FAST == FAST_ACT_GELU || VOCAB;
   auto step = [&](auto first_c, auto odd_c, auto aux_c, bool last) {
     constexpr bool FIRST = decltype(first_c)::value;
     constexpr int AUX = decltype(aux_c)::value, X = AUX ? 8 : 0;
@@ -556,12 +614,13 @@ __global__ __launch_bounds__(NTHR, 1) void gemm_mfma_lean_kernel(GemmArgs g, Wal
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][0], fa[i][0], FIRST ? zero : acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(SUMS ? fa[i][0] : fb[j][0], SUMS ? fb[j][0] : fa[i][0],
+                                                            FIRST ? zero : acc[i][j], 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][1], fa[i][1], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(SUMS ? fa[i][1] : fb[j][1], SUMS ? fb[j][1] : fa[i][1], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     if (!TOGETHER || !last || grp == 0) __builtin_amdgcn_s_barrier();
@@ -608,6 +667,7 @@ __global__ __launch_bounds__(NTHR, 1) void gemm_mfma_lean_kernel(GemmArgs g, Wal
     }
     if (has_aux<FAST>() && !EARLY) { fetch_aux(aux0, g, cc, wm0, wn0, lane, 0); fetch_aux(aux1, g, cc, wm0, wn0, lane, 1); }
     if (FAST == FAST_STORE_F32) epilogue_f32(g, cc, acc, wm0, wn0, lane);
+    else if (SUMS) epilogue_sums(g, cc, acc, wm0, wn0, lane);
     else epilogue_staged_fn<FAST>(g, cc, acc, wm0, wn0, lane, smem + LEAN_NST * STAGE_BYTES + wave * 4096, aux0, aux1);
     if (TOGETHER && grp == 1) {
       __builtin_amdgcn_sched_barrier(0);
@@ -672,13 +732,16 @@ inline hipError_t launch_tile_for(const GemmArgs& g, hipStream_t s) {
 inline bool has_lean(const GemmArgs& g, bool a_kc, bool b_kc) {
   if (!a_kc) return g.mode == EPI_STORE && !g.addf && (g.c_is_f32 || g.split_k > 1);     // parameter gradients
   if (g.addf || g.split_k > 1) return false;
-  if (g.c_is_f32) return b_kc && g.mode == EPI_STORE;                                    // the recurrent kinds' U xin
+  if (g.c_is_f32) return g.mode == EPI_STORE && (b_kc || g.batch == 1);   // the recurrent kinds' U xin; a vocabulary's gradient
   if (g.mode == EPI_STORE) return true;
   if (!b_kc) return g.mode == EPI_MUL_AUX || g.mode == EPI_MUL_1MZ2 || g.mode == EPI_ADD_AUX;   // block VJPs
   if (g.mode == EPI_ACT_GELU) return g.out2;                                             // forward
   return g.mode == EPI_RESID && g.aux && !g.lambda_mn;
 }
 hipError_t launch_lean_nn(const GemmArgs& g, hipStream_t s) {
+  if (g.c_is_f32)
+    return g.K % (2 * BK) == 0 ? launch_lean_walk<true, false, FAST_STORE_F32, false, true>(g, s)
+                               : launch_lean_walk<true, false, FAST_STORE_F32, false, false>(g, s);
   switch (g.mode) {
     case EPI_STORE: return launch_lean<true, false, FAST_STORE>(g, s);
     case EPI_MUL_AUX: return launch_lean<true, false, FAST_MUL_AUX>(g, s);
@@ -773,6 +836,17 @@ bool launch_gemm_mfma(const GemmArgs& g, hipStream_t s, hipError_t* err) {
     *err = launch_tile_for(g, s);
   }
   return true;
+}
+
+bool gemm_vocab_ok(const GemmArgs& g) {
+  return g.M % BM == 0 && g.N % BN == 0 && g.K % BK == 0 && g.K >= 4 * BK && g.a_sm % 8 == 0 && g.b_sn % 8 == 0 &&
+         g.a_sm <= (1L << 22) && g.b_sn <= (1L << 22) && g.M / BM * (g.N / BN) < (1L << 28);
+}
+hipError_t launch_gemm_vocab(const GemmArgs& g, hipStream_t s) {
+  const bool pair = g.K % (2 * BK) == 0;
+  if (g.mode == EPI_VOCAB_SUMS)
+    return pair ? launch_lean_walk<true, true, FAST_VOCAB_SUMS, false, true>(g, s) : launch_lean_walk<true, true, FAST_VOCAB_SUMS, false, false>(g, s);
+  return pair ? launch_lean_walk<true, true, FAST_VOCAB_GRAD, false, true>(g, s) : launch_lean_walk<true, true, FAST_VOCAB_GRAD, false, false>(g, s);
 }
 
 namespace {

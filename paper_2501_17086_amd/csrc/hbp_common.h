@@ -127,7 +127,18 @@ enum EpiMode {
   EPI_ACT_GELU = 3,    // C = gelu(acc); out2 = gelu'(acc)
   EPI_ACT_TANH = 4,    // C = tanh(acc)
   EPI_RESID = 5,       // C = lambda[n] * aux[m,n] + acc        (x_{l+1})
-  EPI_ADD_AUX = 6      // C = acc + aux[m,n]
+  EPI_ADD_AUX = 6,     // C = acc + aux[m,n]
+  // products of a vocabulary's weights (rows m) with rows n (launch_gemm_vocab only; cross_entropy.hip)
+  EPI_VOCAB_SUMS = 7,  // C(fp32)[m / 128][n] = log2 of the sum over those 128 m of 2^(alpha acc)
+  EPI_VOCAB_GRAD = 8   // C(bf16) = gain (2^(alpha acc - lse[n]) - [row0 + m = target[n]])
+};
+struct VocabEpilogue {
+  float alpha;
+  const float* lse;         // [N]
+  const int* target;        // [N]
+  const float* at_target;   // [N] 2^(alpha acc - lse[n]) - 1 at the target
+  const float* gain;        // one number
+  long row0;
 };
 
 struct GemmArgs {
@@ -146,6 +157,7 @@ struct GemmArgs {
   const float* lambda; long lambda_sb;  // fp32 [N]
   const void* lambda_mn;              // storage type [M,N] (row stride ldc, batch stride aux_sb): EPI_RESID per element
   int c_is_f32;         // C stored as fp32 regardless of the storage type
+  VocabEpilogue vocab;  // EPI_VOCAB_...
 };
 
 // storage type: 0 = fp32, 1 = bf16
@@ -198,6 +210,9 @@ hipError_t launch_gemm_f32_group(const GemmArgs* g, int n, hipStream_t s);
 hipError_t launch_gemm_tile_group(const GemmArgs* g, int n, int tm, int tn, hipStream_t s);
 // fast bf16 MFMA path; returns false when the shape/layout is not covered
 bool launch_gemm_mfma(const GemmArgs& g, hipStream_t s, hipError_t* err);
+// Both operands K-contiguous, whole tiles of the 256 x 256 kernel, a mode EPI_VOCAB_...: does it take them?
+bool gemm_vocab_ok(const GemmArgs& g);
+hipError_t launch_gemm_vocab(const GemmArgs& g, hipStream_t s);
 // the same contractions on tiles of 128 x 128, 64 x 64, 64 x 32 or 32 x 32, any size (called through launch_gemm_mfma, which
 // checks the layout)
 hipError_t launch_gemm_tile(const GemmArgs& g, int tm, int tn, hipStream_t s);

@@ -206,6 +206,43 @@ def test_cross_entropy(n, vocab, width, dtype, grad):
     check_loss(x, w, t, scale=0.3, mean=False, factor=-1.5, grad=TYPES[grad])
 
 
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,width", [(1000, 9300, 128), (1000, 9300, 160), (4101, 2381, 256), (2048, 9216, 264), (900, 20001, 512),
+                                           (8190, 5003, 1024)])
+def test_cross_entropy_of_many_tiles(n, vocab, width, grad):
+    """Sizes whose logits meet no memory: whole tiles, tiles and a rest, contractions that are no multiple of 64, rows filled up."""
+    x, w = normal((n, width), torch.bfloat16, n), normal((vocab, width), torch.bfloat16, 2, 2.0 / math.sqrt(width))
+    t = some_tokens(n, vocab, 3)
+    t[5], t[6], t[7] = vocab - 1, vocab // 256 * 256, vocab // 256 * 256 - 1
+    check_loss(x, w, t, grad=TYPES[grad])
+    check_loss(x, w, t, scale=0.5, mean=False, factor=-0.25, grad=TYPES[grad], again=False)
+
+
+def test_cross_entropy_of_many_tiles_in_pieces():
+    n, vocab, width = 16384, 33100, 128
+    x, w = normal((n, width), torch.bfloat16, n), normal((vocab, width), torch.bfloat16, 2, 2.0 / math.sqrt(width))
+    check_loss(x, w, some_tokens(n, vocab, 3))
+
+
+def test_cross_entropy_of_many_tiles_infinities():
+    n, vocab, width = 1000, 9300, 128
+    x, w = normal((n, width), torch.bfloat16, 1), normal((vocab, width), torch.bfloat16, 2)
+    t = some_tokens(n, vocab, 3, padding=0.5)
+    out = (t < 0) | (t >= vocab)
+    clean = check_loss(x, w, t)
+    x[out] = math.nan
+    c = B.make_cross_entropy(x, w, t)
+    B.hbp_loss_cross_entropy(c)
+    for name in ("loss", "row_loss", "dx", "dweight"):
+        assert torch.equal(getattr(c, name), getattr(clean, name)), name
+    bad = (~out).nonzero()[:2, 0]
+    x[bad[0], 5], x[bad[1], 6] = math.nan, math.inf
+    B.hbp_loss_cross_entropy(c)
+    fine = torch.ones(n, dtype=torch.bool, device="cuda")
+    fine[bad] = False
+    assert torch.equal(torch.isfinite(c.row_loss), fine) and torch.equal(torch.isfinite(c.dx.float()).all(1), fine)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_cross_entropy_of_a_vocabulary_in_pieces(dtype):
     """Few rows, more weights than a piece takes."""
