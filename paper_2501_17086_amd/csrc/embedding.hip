@@ -5,8 +5,8 @@
 //
 // The gradient adds up rows of the same token, in 32 bits and in an order that does not change from run to run, so without atomics on
 // its sums.  Tokens are sorted (least significant digit first, up to 9 bits a pass, stable, so that a token's rows stay in order);
-// then every wavefront owns some rows of the table, finds their stretch of the sorted list by a search of 64 probes a step, and adds.
-// Text repeats few tokens very often: 64 sorted places that begin at a multiple of 64 and hold one token are added up beforehand by a
+// then a table's row has its stretch of the sorted list, found by bisection, and one group of lanes adds it up.
+// Text repeats few tokens very often: 32 sorted places that begin at a multiple of 32 and hold one token are added up beforehand by a
 // workgroup of their own, and the table's row adds that sum.  A table's row is written once, rows without tokens as zeros: that is most
 // of the bytes.
 #include "philox.h"
@@ -132,9 +132,9 @@ hipError_t launch_lookup_t(const EmbeddingArgs& a, const DropoutKey& key, hipStr
 }
 
 // ---- the gradient: tokens sorted -----------------------------------------------------------------------------------------
-constexpr int SORT_PER = 8, SORT_E = NTHR * SORT_PER;      // places of a workgroup
+constexpr int SORT_PER = 4, SORT_E = NTHR * SORT_PER;      // places of a workgroup
 constexpr int SORT_BITS = 9, SORT_D = 1 << SORT_BITS;
-constexpr int CHUNK = 64;                                  // sorted places added up beforehand where they hold one token
+constexpr int CHUNK = 32;                                  // sorted places added up beforehand where they hold one token
 
 // What a place sorts by: its token, or `vocab` for a token that is none (behind all others).
 __device__ __forceinline__ unsigned key_of(int token, unsigned vocab) { return (unsigned)token < vocab ? (unsigned)token : vocab; }
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64) void scan_kernel(SortArgs a) {
   a.totals[d] = sum;
 }
 
-// Every wavefront owns 512 consecutive places in 8 steps of 64; within a step lanes of one digit find each other by a ballot a bit.
+// Every wavefront owns 256 consecutive places in 4 steps of 64; within a step lanes of one digit find each other by a ballot a bit.
 __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
   __shared__ unsigned cnt[4][SORT_D];                      // a wavefront's keys with each digit, then where they go
   __shared__ unsigned sums[4];
@@ -227,10 +227,16 @@ __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
     }
   }
   if (!a.scanned) {
-    for (int b = 0; b < a.blocks; ++b) {
-      const uint2 c = *reinterpret_cast<const uint2*>(a.counts + (long)b * SORT_D + d0);
-      total[0] += c.x; total[1] += c.y;
-      if (b < (int)blockIdx.x) { before[0] += c.x; before[1] += c.y; }
+    for (int b = 0; b < a.blocks; b += 16) {               // (the loads of 16 blocks go out together)
+      uint2 c[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        c[j] = b + j < a.blocks ? *reinterpret_cast<const uint2*>(a.counts + (long)(b + j) * SORT_D + d0) : make_uint2(0, 0);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        total[0] += c[j].x; total[1] += c[j].y;
+        if (b + j < (int)blockIdx.x) { before[0] += c[j].x; before[1] += c[j].y; }
+      }
     }
   }
   unsigned pair = total[0] + total[1], scan = pair;
@@ -271,8 +277,9 @@ struct SumArgs {
   DropoutKey key;
   const unsigned *keys, *places;   // sorted
   float* chunk_sums;               // [chunks][width]
+  unsigned* starts;                // [vocab + 1]: the first place of each token
   unsigned n, units;               // places; width / 8
-  unsigned vrows;                  // rows of the table a wavefront owns
+  unsigned chunks, stride;         // stride: a wavefront's rows of the table are this many apart
 };
 
 // G lanes hold a row's channels, 8 each, so a wavefront works on 64 / G rows at a time; slice: blockIdx.y
@@ -298,53 +305,49 @@ template <typename T> struct Adder {
   }
 };
 
-// 64 places of one token: each wavefront adds 16, and the four sums meet in LDS
+// Places of one token, CHUNK of them: each wavefront adds a quarter, and the four sums meet in LDS.  Workgroups behind those (and first
+// slice): a thread a row of the table, where its places begin, by bisection.
 template <typename T, int G>
 __global__ __launch_bounds__(NTHR) void chunk_kernel(SumArgs a) {
   __shared__ float part[4][64 / G][8 * G];
+  if (blockIdx.x >= a.chunks) {
+    const unsigned v = (blockIdx.x - a.chunks) * NTHR + threadIdx.x;
+    if (v > a.e.vocab || blockIdx.y) return;
+    unsigned lo = 0, hi = a.n;
+    while (lo < hi) {
+      const unsigned m = (lo + hi) / 2;
+      if (a.keys[m] < v) lo = m + 1; else hi = m;
+    }
+    a.starts[v] = lo;
+    return;
+  }
   const unsigned first = blockIdx.x * CHUNK;
   const unsigned v = a.keys[first];
   if (v >= a.e.vocab || a.keys[first + CHUNK - 1] != v) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / G;
-  constexpr int R = 64 / G, STEPS = 16 / R > 0 ? 16 / R : 1;
+  constexpr int R = 64 / G, Q = CHUNK / 4, STEPS = Q / R;
   const Adder<T> add(a, blockIdx.y * G + lane % G);
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  constexpr int B = STEPS < 4 ? STEPS : 4;
-#pragma unroll 1
-  for (int s = 0; s < STEPS; s += B) {
-    Raw8<T> r[B];
-    unsigned p[B];
+  Raw8<T> r[STEPS];
+  unsigned p[STEPS];
 #pragma unroll
-    for (int b = 0; b < B; ++b) p[b] = a.places[first + 16 * wave + (s + b) * R + sub];
+  for (int b = 0; b < STEPS; ++b) p[b] = a.places[first + Q * wave + b * R + sub];
 #pragma unroll
-    for (int b = 0; b < B; ++b) add.load(r[b], p[b]);
+  for (int b = 0; b < STEPS; ++b) add.load(r[b], p[b]);
 #pragma unroll
-    for (int b = 0; b < B; ++b) add.add(acc, r[b], p[b]);
-  }
+  for (int b = 0; b < STEPS; ++b) add.add(acc, r[b], p[b]);
 #pragma unroll
   for (int j = 0; j < 8; ++j) part[wave][sub][8 * (lane % G) + j] = acc[j];
   __syncthreads();
   for (int c = threadIdx.x; c < 8 * G; c += NTHR) {
     float t = 0.f;
+#pragma unroll
     for (int w = 0; w < 4; ++w)
-      for (int s = 0; s < R; ++s) t += part[w][s][c];
+#pragma unroll
+      for (int k = 0; k < R; ++k) t += part[w][k][c];
     const unsigned at = blockIdx.y * (8 * G) + c;
     if (at < 8 * a.units) a.chunk_sums[(long)blockIdx.x * (8 * a.units) + at] = t;
   }
-}
-
-// the first place in lo .. hi whose key is at least v; the wavefront probes 64 places a step
-__device__ __forceinline__ unsigned first_at_least(const unsigned* keys, unsigned lo, unsigned hi, unsigned v, int lane) {
-  while (hi > lo) {
-    const unsigned step = (hi - lo + 63) / 64, at = lo + step * lane;
-    const bool below = at < hi && keys[at] < v;
-    const int n = __popcll(__ballot(below));               // (keys are sorted: the first n probes)
-    if (n == 0) return lo;
-    const unsigned last = lo + step * (n - 1);             // its key is below v
-    hi = last + step < hi ? last + step : hi;
-    lo = last + 1;
-  }
-  return lo;
 }
 
 template <typename O> __device__ __forceinline__ void put8(O* p, const float (&v)[8], bool accumulate) {
@@ -357,65 +360,71 @@ template <typename O> __device__ __forceinline__ void put8(O* p, const float (&v
   } else store8(p, v);
 }
 
-template <typename T, typename O, int G>
+// A wavefront's 64 / G groups of lanes own a row of the table each, and STEPS such rows `stride` apart: frequent tokens are often
+// numbered next to each other, and would else be one wavefront's.
+template <typename T, typename O, int G, int STEPS>
 __global__ __launch_bounds__(NTHR) void table_kernel(SumArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / G;
-  constexpr int R = 64 / G;
-  const long v0 = ((long)blockIdx.x * 4 + wave) * a.vrows;
-  if (v0 >= a.e.vocab) return;
-  const unsigned v1 = (unsigned)(v0 + a.vrows < a.e.vocab ? v0 + a.vrows : a.e.vocab);
-  const unsigned lo = first_at_least(a.keys, 0, a.n, (unsigned)v0, lane);
-  const unsigned hi = first_at_least(a.keys, lo, a.n, v1, lane);
+  const int lane = threadIdx.x & 63, sub = lane / G;
+  constexpr int R = 64 / G, B = 8;
+  const unsigned v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * R + sub;
   const Adder<T> add(a, blockIdx.y * G + lane % G);
   O* out = reinterpret_cast<O*>(a.e.dtable.p);
-  unsigned start = lo;                                     // lane l: where the places of row v0 + l begin (vrows < 64)
-  for (unsigned h = hi; start < h;) {
-    const unsigned m = (start + h) / 2;
-    if (a.keys[m] < (unsigned)v0 + lane) start = m + 1; else h = m;
-  }
-  for (unsigned r = 0; r < a.vrows; r += R) {              // R rows of the table a step, each by its own lanes
-    const unsigned mine = (unsigned)v0 + r + sub;
-    const unsigned b = (unsigned)__shfl((int)start, r + sub), e = (unsigned)__shfl((int)start, r + sub + 1);
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    unsigned i = b;
-    while (i < e) {
-      if (i % CHUNK == 0 && i + CHUNK <= e) {
-        if (add.in) {
-          float t[8];
-          load8(a.chunk_sums + (long)(i / CHUNK) * (8 * a.units) + 8 * add.unit, t);
+  unsigned from[STEPS], to[STEPS];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] += t[j];
+  for (int t = 0; t < STEPS; ++t) {
+    const unsigned v = v0 + t * a.stride;
+    const bool mine = v0 < a.stride && v < a.e.vocab;
+    from[t] = mine ? a.starts[v] : 0;
+    to[t] = mine ? a.starts[v + 1] : 0;
+  }
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    const unsigned v = v0 + t * a.stride;
+    if (!add.in || v0 >= a.stride || v >= a.e.vocab || (a.e.accumulate && to[t] == from[t])) continue;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    unsigned i = from[t];
+    const unsigned e = to[t];
+    while (i < e) {
+      if (i % CHUNK == 0 && i + CHUNK <= e) {              // whole chunks: their sums, eight on their way at once
+        const unsigned c0 = i / CHUNK, left = e / CHUNK - c0;
+        const float* p = a.chunk_sums + (long)c0 * (8 * a.units) + 8 * add.unit;
+        Raw8<float> r[B];
+#pragma unroll
+        for (int k = 0; k < B; ++k)
+          if (k < (int)left) r[k].load(p + (long)k * (8 * a.units));
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+          if (k >= (int)left) continue;
+          float w[8];
+          r[k].unpack(w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] += w[j];
         }
-        i += CHUNK;
+        i += (left < B ? left : B) * CHUNK;
         continue;
       }
-      const unsigned stop = (i / CHUNK + 1) * CHUNK < e ? (i / CHUNK + 1) * CHUNK : e;
-      for (; i + 4 <= stop; i += 4) {
-        Raw8<T> r[4];
-        unsigned p[4];
+      const unsigned stop = (i / CHUNK + 1) * CHUNK < e ? (i / CHUNK + 1) * CHUNK : e, n = stop - i < B ? stop - i : B;
+      Raw8<T> r[B];
+      unsigned p[B];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = a.places[i + k];
+      for (int k = 0; k < B; ++k)
+        if (k < (int)n) p[k] = a.places[i + k];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) add.load(r[k], p[k]);
+      for (int k = 0; k < B; ++k)
+        if (k < (int)n) add.load(r[k], p[k]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) add.add(acc, r[k], p[k]);
-      }
-      for (; i < stop; ++i) {
-        Raw8<T> r;
-        const unsigned p = a.places[i];
-        add.load(r, p);
-        add.add(acc, r, p);
-      }
+      for (int k = 0; k < B; ++k)
+        if (k < (int)n) add.add(acc, r[k], p[k]);
+      i += n;
     }
-    if (!add.in || mine >= v1 || (a.e.accumulate && e == b)) continue;
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] *= a.key.factor;
-    put8(out + (long)mine * a.e.dtable.row + 8 * add.unit, acc, a.e.accumulate);
+    put8(out + (long)v * a.e.dtable.row + 8 * add.unit, acc, a.e.accumulate);
   }
 }
 
-struct Sorted { unsigned *keys[2], *places[2], *counts, *totals; float* sums; size_t bytes; int blocks; };
-Sorted carve(char* p, long rows, int width) {
+struct Sorted { unsigned *keys[2], *places[2], *counts, *totals, *starts; float* sums; size_t bytes; int blocks; };
+Sorted carve(char* p, long rows, long vocab, int width) {
   Sorted w;
   size_t off = 0;
   auto take = [&](size_t n) { char* q = p ? p + off : nullptr; off += (n + 255) / 256 * 256; return q; };
@@ -426,19 +435,25 @@ Sorted carve(char* p, long rows, int width) {
   }
   w.counts = reinterpret_cast<unsigned*>(take((size_t)w.blocks * SORT_D * 4));
   w.totals = reinterpret_cast<unsigned*>(take(SORT_D * 4));
+  w.starts = reinterpret_cast<unsigned*>(take(4 * (size_t)(vocab + 1)));
   w.sums = reinterpret_cast<float*>(take((size_t)(rows / CHUNK) * width * 4));
   w.bytes = off;
   return w;
 }
 
 template <typename T, typename O, int G>
-hipError_t launch_sums(const SumArgs& a, hipStream_t s) {
-  const unsigned slices = (a.units + G - 1) / G, chunks = a.n / CHUNK;
-  if (chunks) chunk_kernel<T, G><<<dim3(chunks, slices), NTHR, 0, s>>>(a);
-  hipError_t e = hipGetLastError();
+hipError_t launch_sums(SumArgs a, hipStream_t s) {
+  const unsigned slices = (a.units + G - 1) / G, searches = (unsigned)((a.e.vocab + NTHR) / NTHR);
+  a.chunks = a.n / CHUNK;
+  chunk_kernel<T, G><<<dim3(a.chunks + searches, slices), NTHR, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned per = 4 * a.vrows;
-  table_kernel<T, O, G><<<dim3((unsigned)((a.e.vocab + per - 1) / per), slices), NTHR, 0, s>>>(a);
+  constexpr unsigned PER = 4 * (64 / G);
+  const bool four = a.e.vocab * slices >= 16384l * (64 / G);   // (a wavefront for every SIMD's 16 places that way, too)
+  a.stride = (unsigned)(four ? (a.e.vocab + 3) / 4 : a.e.vocab);
+  const dim3 grid((a.stride + PER - 1) / PER, slices);
+  if (four) table_kernel<T, O, G, 4><<<grid, NTHR, 0, s>>>(a);
+  else table_kernel<T, O, G, 1><<<grid, NTHR, 0, s>>>(a);
   return hipGetLastError();
 }
 template <typename T, typename O>
@@ -460,10 +475,10 @@ hipError_t launch_embedding_fwd(int dtype, const EmbeddingArgs& a, const Dropout
   return dtype == 0 ? launch_lookup_t<float>(a, key, s) : launch_lookup_t<bf16_t>(a, key, s);
 }
 
-size_t embedding_ws_bytes(long rows, long, int width) { return carve(nullptr, rows, width).bytes; }
+size_t embedding_ws_bytes(long rows, long vocab, int width) { return carve(nullptr, rows, vocab, width).bytes; }
 
 hipError_t launch_embedding_bwd(int dtype, const EmbeddingArgs& a, const DropoutKey& key, void* workspace, size_t bytes, hipStream_t s) {
-  const Sorted w = carve(reinterpret_cast<char*>(workspace), a.rows, a.width);
+  const Sorted w = carve(reinterpret_cast<char*>(workspace), a.rows, a.vocab, a.width);
   if (bytes < w.bytes) return hipErrorInvalidValue;
   int bits = 1;
   while ((a.vocab >> bits) > 0) ++bits;                    // keys are 0 .. vocab
@@ -485,9 +500,8 @@ hipError_t launch_embedding_bwd(int dtype, const EmbeddingArgs& a, const Dropout
   SumArgs m{};
   m.e = a; m.key = key;
   m.keys = w.keys[(passes - 1) & 1]; m.places = w.places[(passes - 1) & 1];
-  m.chunk_sums = w.sums;
+  m.chunk_sums = w.sums; m.starts = w.starts;
   m.n = (unsigned)a.rows; m.units = (unsigned)(a.width / 8);
-  m.vrows = 16;
   if (dtype == 0) return launch_sums_t<float, float>(m, s);
   return a.grad_dtype == 0 ? launch_sums_t<bf16_t, float>(m, s) : launch_sums_t<bf16_t, bf16_t>(m, s);
 }
