@@ -6,7 +6,7 @@
 // The gradient adds up rows of the same token, in 32 bits and in an order that does not change from run to run, so without atomics on
 // its sums.  Tokens are sorted (least significant digit first, up to 9 bits a pass, stable, so that a token's rows stay in order);
 // then a table's row has its stretch of the sorted list, found by bisection, and one group of lanes adds it up.
-// Text repeats few tokens very often: 32 sorted places that begin at a multiple of 32 and hold one token are added up beforehand by a
+// Text repeats few tokens very often: 16 sorted places that begin at a multiple of 16 and hold one token are added up beforehand by a
 // workgroup of their own, and the table's row adds that sum.  A table's row is written once, rows without tokens as zeros: that is most
 // of the bytes.
 #include "philox.h"
@@ -134,7 +134,7 @@ hipError_t launch_lookup_t(const EmbeddingArgs& a, const DropoutKey& key, hipStr
 // ---- the gradient: tokens sorted -----------------------------------------------------------------------------------------
 constexpr int SORT_PER = 4, SORT_E = NTHR * SORT_PER;      // places of a workgroup
 constexpr int SORT_BITS = 9, SORT_D = 1 << SORT_BITS;
-constexpr int CHUNK = 32;                                  // sorted places added up beforehand where they hold one token
+constexpr int CHUNK = 16;                                  // sorted places added up beforehand where they hold one token
 
 // What a place sorts by: its token, or `vocab` for a token that is none (behind all others).
 __device__ __forceinline__ unsigned key_of(int token, unsigned vocab) { return (unsigned)token < vocab ? (unsigned)token : vocab; }
@@ -295,9 +295,21 @@ template <typename T> struct Adder {
   __device__ __forceinline__ void load(Raw8<T>& r, unsigned place) const {
     if (in) r.load(dout + (long)place * a.e.dout.row + 8 * unit);
   }
-  __device__ __forceinline__ void add(float (&acc)[8], const Raw8<T>& r, unsigned place) const {
+  // The masks of n <= 8 places (even n: one more), 8 bits each.  A loop of two: eight copies of the generator wherever rows are added are 16 KB
+  // of instructions that a short launch has to fetch first, and a single one at a time waits for itself.
+  template <typename F> __device__ __forceinline__ unsigned long masks(unsigned n, F place) const {
+    if (!a.key.threshold) return ~0ul;
+    unsigned long m = 0;
+#pragma unroll 1
+    for (unsigned k = 0; k < n; k += 2) {
+      const unsigned long p = place(k), q = place(k + 1);
+      const unsigned x = dropout_mask8(a.key, stream, p * a.units + unit), y = dropout_mask8(a.key, stream, q * a.units + unit);
+      m |= (unsigned long)(x | y << 8) << (8 * k);
+    }
+    return m;
+  }
+  __device__ __forceinline__ void add(float (&acc)[8], const Raw8<T>& r, unsigned mask) const {
     if (!in) return;
-    const unsigned mask = a.key.threshold ? dropout_mask8(a.key, stream, (unsigned long)place * a.units + unit) : 255u;
     float v[8];
     r.unpack(v);
 #pragma unroll
@@ -325,17 +337,21 @@ __global__ __launch_bounds__(NTHR) void chunk_kernel(SumArgs a) {
   const unsigned v = a.keys[first];
   if (v >= a.e.vocab || a.keys[first + CHUNK - 1] != v) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / G;
-  constexpr int R = 64 / G, Q = CHUNK / 4, STEPS = Q / R;
+  constexpr int R = 64 / G, Q = CHUNK / 4, STEPS = Q / R > 0 ? Q / R : 1;     // (more lanes than a quarter's places: the others add none)
   const Adder<T> add(a, blockIdx.y * G + lane % G);
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  Raw8<T> r[STEPS];
-  unsigned p[STEPS];
+  if (R <= Q || sub < Q) {
+    const unsigned* places = a.places + first + Q * wave + sub;
+    Raw8<T> r[STEPS];
+    unsigned p[STEPS];
 #pragma unroll
-  for (int b = 0; b < STEPS; ++b) p[b] = a.places[first + Q * wave + b * R + sub];
+    for (int b = 0; b < STEPS; ++b) p[b] = places[b * R];
 #pragma unroll
-  for (int b = 0; b < STEPS; ++b) add.load(r[b], p[b]);
+    for (int b = 0; b < STEPS; ++b) add.load(r[b], p[b]);
+    const unsigned long masks = add.masks(STEPS, [&](unsigned k) { return p[k < STEPS ? k : 0]; });
 #pragma unroll
-  for (int b = 0; b < STEPS; ++b) add.add(acc, r[b], p[b]);
+    for (int b = 0; b < STEPS; ++b) add.add(acc, r[b], (unsigned)(masks >> (8 * b)));
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) part[wave][sub][8 * (lane % G) + j] = acc[j];
   __syncthreads();
@@ -360,13 +376,113 @@ template <typename O> __device__ __forceinline__ void put8(O* p, const float (&v
   } else store8(p, v);
 }
 
-// A wavefront's 64 / G groups of lanes own a row of the table each, and STEPS such rows `stride` apart: frequent tokens are often
-// numbered next to each other, and would else be one wavefront's.
+// What every step-th of `n` places adds, eight on their way at once: the first `head` of them from b on, the rest from t on.  Eight lanes
+// of the group read the places, one each.
+template <typename T, int G>
+__device__ __forceinline__ void add_places(const Adder<T>& add, float (&acc)[8], unsigned b, unsigned head, unsigned t, unsigned n,
+                                           unsigned i, unsigned step) {
+  constexpr unsigned B = 8;
+  const unsigned lane = threadIdx.x & 63, first = lane / G * G;
+  for (; i < n; i += B * step) {
+    const unsigned at = i + lane % B * step;
+    const unsigned mine = at < n ? add.a.places[at < head ? b + at : t + (at - head)] : 0;
+    Raw8<T> r[B];
+#pragma unroll
+    for (unsigned k = 0; k < B; ++k)
+      if (i + k * step < n) add.load(r[k], (unsigned)__shfl((int)mine, first + k));
+    const unsigned left = (n - i + step - 1) / step;
+    const unsigned long masks = add.masks(left < B ? left : B, [&](unsigned k) { return (unsigned)__shfl((int)mine, first + k); });
+#pragma unroll
+    for (unsigned k = 0; k < B; ++k)
+      if (i + k * step < n) add.add(acc, r[k], (unsigned)(masks >> (8 * k)));
+  }
+}
+// the same of chunks' sums
+template <typename T>
+__device__ __forceinline__ void add_chunks(const Adder<T>& add, float (&acc)[8], unsigned c, unsigned e, unsigned step) {
+  constexpr unsigned B = 8;
+  if (!add.in) return;
+  while (c < e) {
+    Raw8<float> r[B];
+#pragma unroll
+    for (unsigned k = 0; k < B; ++k)
+      if (c + k * step < e) r[k].load(add.a.chunk_sums + (long)(c + k * step) * (8 * add.a.units) + 8 * add.unit);
+#pragma unroll
+    for (unsigned k = 0; k < B; ++k) {
+      if (c + k * step >= e) continue;
+      float w[8];
+      r[k].unpack(w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += w[j];
+    }
+    c += B * step;
+  }
+}
+// the stretch b .. e of one token, this group of lanes every step-th of its places and chunks from the which-th on
+template <typename T, int G>
+__device__ __forceinline__ void add_stretch(const Adder<T>& add, float (&acc)[8], unsigned b, unsigned e, unsigned which, unsigned step) {
+  const unsigned c0 = (b + CHUNK - 1) / CHUNK, c1 = e / CHUNK;
+  unsigned head = e - b, t = 0, n = head;
+  if (c0 < c1) {
+    add_chunks(add, acc, c0 + which, c1, step);
+    head = c0 * CHUNK - b;
+    t = c1 * CHUNK;
+    n = head + e - t;
+  }
+  add_places<T, G>(add, acc, b, head, t, n, which, step);
+}
+// A token is frequent if its stretch holds a whole chunk: a workgroup for every chunk looks whether it is the first of its token, and
+// then adds the token's whole stretch, all lanes at it.  (One group of lanes takes 2 us for eight rows, half of it the generator.)
+__device__ __forceinline__ bool frequent(unsigned b, unsigned e) { return (b + CHUNK - 1) / CHUNK < e / CHUNK; }
+
+template <typename T, typename O, int G>
+__device__ void frequent_row(const SumArgs& a) {
+  __shared__ float part[4 * (64 / G)][8 * G];
+  const unsigned c = blockIdx.x, v = a.keys[c * CHUNK];
+  if (v >= a.e.vocab || a.keys[c * CHUNK + CHUNK - 1] != v) return;
+  const unsigned b = a.starts[v], e = a.starts[v + 1];
+  if ((b + CHUNK - 1) / CHUNK != c) return;
+  constexpr int R = 64 / G;
+  const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) * R + lane / G;
+  const Adder<T> add(a, blockIdx.y * G + lane % G);
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  add_stretch<T, G>(add, acc, b, e, group, 4 * R);
+  store8(&part[group][8 * (lane % G)], acc);
+  __syncthreads();
+  O* out = reinterpret_cast<O*>(a.e.dtable.p) + (long)v * a.e.dtable.row;
+  for (int c = threadIdx.x; c < 8 * G; c += NTHR) {
+    const unsigned at = blockIdx.y * (8 * G) + c;
+    if (at >= 8 * a.units) continue;
+    float t = 0.f;
+    for (int k = 0; k < 4 * R; ++k) t += part[k][c];
+    t *= a.key.factor;
+    if (a.e.accumulate) t += Elem<O>::load(out + at);
+    if constexpr (sizeof(O) == 2) out[at] = (O)pack_bf16x2(t, 0.f);
+    else out[at] = t;
+  }
+}
+
+// zeros, every store of a wavefront over consecutive places
+template <int G> __device__ __forceinline__ void clear8(float* row, unsigned slice, unsigned l, unsigned units) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const unsigned c = slice * (8 * G) + k * (4 * G) + 4 * l;
+    if (c < 8 * units) *reinterpret_cast<float4*>(row + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+template <int G> __device__ __forceinline__ void clear8(bf16_t* row, unsigned slice, unsigned l, unsigned units) {
+  const unsigned c = slice * (8 * G) + 8 * l;
+  if (c < 8 * units) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+}
+
+// A wavefront's 64 / G groups of lanes own a row of the table each, and STEPS such rows `stride` apart: tokens of like frequency are
+// often numbered next to each other.
 template <typename T, typename O, int G, int STEPS>
 __global__ __launch_bounds__(NTHR) void table_kernel(SumArgs a) {
+  if (blockIdx.x < a.chunks) { frequent_row<T, O, G>(a); return; }
   const int lane = threadIdx.x & 63, sub = lane / G;
-  constexpr int R = 64 / G, B = 8;
-  const unsigned v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * R + sub;
+  constexpr int R = 64 / G;
+  const unsigned v0 = ((blockIdx.x - a.chunks) * 4 + (threadIdx.x >> 6)) * R + sub;
   const Adder<T> add(a, blockIdx.y * G + lane % G);
   O* out = reinterpret_cast<O*>(a.e.dtable.p);
   unsigned from[STEPS], to[STEPS];
@@ -380,46 +496,18 @@ __global__ __launch_bounds__(NTHR) void table_kernel(SumArgs a) {
 #pragma unroll
   for (int t = 0; t < STEPS; ++t) {
     const unsigned v = v0 + t * a.stride;
-    if (!add.in || v0 >= a.stride || v >= a.e.vocab || (a.e.accumulate && to[t] == from[t])) continue;
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    unsigned i = from[t];
-    const unsigned e = to[t];
-    while (i < e) {
-      if (i % CHUNK == 0 && i + CHUNK <= e) {              // whole chunks: their sums, eight on their way at once
-        const unsigned c0 = i / CHUNK, left = e / CHUNK - c0;
-        const float* p = a.chunk_sums + (long)c0 * (8 * a.units) + 8 * add.unit;
-        Raw8<float> r[B];
-#pragma unroll
-        for (int k = 0; k < B; ++k)
-          if (k < (int)left) r[k].load(p + (long)k * (8 * a.units));
-#pragma unroll
-        for (int k = 0; k < B; ++k) {
-          if (k >= (int)left) continue;
-          float w[8];
-          r[k].unpack(w);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] += w[j];
-        }
-        i += (left < B ? left : B) * CHUNK;
-        continue;
-      }
-      const unsigned stop = (i / CHUNK + 1) * CHUNK < e ? (i / CHUNK + 1) * CHUNK : e, n = stop - i < B ? stop - i : B;
-      Raw8<T> r[B];
-      unsigned p[B];
-#pragma unroll
-      for (int k = 0; k < B; ++k)
-        if (k < (int)n) p[k] = a.places[i + k];
-#pragma unroll
-      for (int k = 0; k < B; ++k)
-        if (k < (int)n) add.load(r[k], p[k]);
-#pragma unroll
-      for (int k = 0; k < B; ++k)
-        if (k < (int)n) add.add(acc, r[k], p[k]);
-      i += n;
+    if (v0 >= a.stride || v >= a.e.vocab || frequent(from[t], to[t])) continue;
+    O* row = out + (long)v * a.e.dtable.row;
+    if (to[t] == from[t]) {
+      if (!a.e.accumulate) clear8<G>(row, blockIdx.y, lane % G, a.units);
+      continue;
     }
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    add_stretch<T, G>(add, acc, from[t], to[t], 0, 1);
+    if (!add.in) continue;
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] *= a.key.factor;
-    put8(out + (long)v * a.e.dtable.row + 8 * add.unit, acc, a.e.accumulate);
+    put8(row + 8 * add.unit, acc, a.e.accumulate);
   }
 }
 
@@ -451,7 +539,7 @@ hipError_t launch_sums(SumArgs a, hipStream_t s) {
   constexpr unsigned PER = 4 * (64 / G);
   const bool four = a.e.vocab * slices >= 16384l * (64 / G);   // (a wavefront for every SIMD's 16 places that way, too)
   a.stride = (unsigned)(four ? (a.e.vocab + 3) / 4 : a.e.vocab);
-  const dim3 grid((a.stride + PER - 1) / PER, slices);
+  const dim3 grid(a.chunks + (a.stride + PER - 1) / PER, slices);
   if (four) table_kernel<T, O, G, 4><<<grid, NTHR, 0, s>>>(a);
   else table_kernel<T, O, G, 1><<<grid, NTHR, 0, s>>>(a);
   return hipGetLastError();
