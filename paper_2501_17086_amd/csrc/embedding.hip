@@ -187,7 +187,17 @@ __global__ __launch_bounds__(64) void scan_kernel(SortArgs a) {
   a.totals[d] = sum;
 }
 
-// Every wavefront owns 256 consecutive places in 4 steps of 64; within a step lanes of one digit find each other by a ballot a bit.
+// Lanes whose digits agree find each other by a ballot a bit.
+__device__ __forceinline__ unsigned long same_digit(unsigned d, int bits, bool in) {
+  unsigned long peers = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long has = __ballot((d >> b) & 1u);
+    peers &= (d >> b) & 1u ? has : ~has;
+  }
+  return peers;
+}
+
+// Every wavefront owns 256 consecutive places in 4 steps of 64.
 __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
   __shared__ unsigned cnt[4][SORT_D];                      // a wavefront's keys with each digit, then where they go
   __shared__ unsigned sums[4];
@@ -203,11 +213,7 @@ __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
     const bool in = i < a.n;
     key[k] = in ? load_key(a, i) : 0u;
     const unsigned d = (key[k] >> a.shift) & a.mask;
-    unsigned long peers = __ballot(in);
-    for (int b = 0; b < bits; ++b) {
-      const unsigned long has = __ballot((d >> b) & 1u);
-      peers &= (d >> b) & 1u ? has : ~has;
-    }
+    const unsigned long peers = same_digit(d, bits, in);
     const unsigned before = __popcll(peers & ((1ul << lane) - 1ul));
     rank[k] = in ? cnt[wave][d] + before : 0u;
     __builtin_amdgcn_wave_barrier();                       // (a wavefront's LDS operations execute in order)
@@ -268,6 +274,79 @@ __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
     const unsigned at = cnt[wave][(key[k] >> a.shift) & a.mask] + rank[k];
     a.keys_out[at] = key[k];
     a.places_out[at] = a.tokens ? (unsigned)i : a.places_in[i];
+  }
+}
+
+// Up to FEW places in one workgroup, all passes in one launch: each wavefront owns a consecutive sixteenth of the list, which goes round
+// through LDS.  (The whole gradient of 4096 tokens into 16384 x 256: 24 us, with the launches of count and place 32.)
+constexpr int FEW_PER = 4, FEW_THREADS = 1024, FEW = FEW_THREADS * FEW_PER, FEW_BITS = 8, FEW_D = 1 << FEW_BITS;
+__global__ __launch_bounds__(FEW_THREADS) void sort_few_kernel(SortArgs a, int passes, int bits) {
+  constexpr int NW = FEW_THREADS / 64;
+  __shared__ unsigned cnt[NW][FEW_D], keys[FEW], places[FEW], sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = (int)a.n, steps = (n + FEW_THREADS - 1) / FEW_THREADS, base = wave * 64 * steps + lane;
+  for (int i = tid; i < n; i += FEW_THREADS) {
+    keys[i] = key_of(a.tokens[i], a.vocab);
+    places[i] = i;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * bits;
+    const unsigned mask = (1u << bits) - 1u;
+    for (int i = tid; i < NW * FEW_D; i += FEW_THREADS) (&cnt[0][0])[i] = 0;
+    __syncthreads();
+    unsigned key[FEW_PER], place[FEW_PER], rank[FEW_PER];
+#pragma unroll
+    for (int k = 0; k < FEW_PER; ++k) {
+      const int i = base + 64 * k;
+      const bool in = k < steps && i < n;
+      key[k] = in ? keys[i] : 0u;
+      place[k] = in ? places[i] : 0u;
+      if (k >= steps) continue;                            // (of the whole workgroup)
+      const unsigned d = key[k] >> shift & mask;
+      const unsigned long peers = same_digit(d, bits, in);
+      const unsigned before = __popcll(peers & ((1ul << lane) - 1ul));
+      rank[k] = in ? cnt[wave][d] + before : 0u;
+      __builtin_amdgcn_wave_barrier();
+      if (in && before == 0) cnt[wave][d] += __popcll(peers);
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    unsigned total = 0, scan = 0;
+    if (tid < FEW_D) {                                     // a thread a digit
+#pragma unroll
+      for (int w = 0; w < NW; ++w) total += cnt[w][tid];
+      scan = total;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const unsigned t = __shfl_up(scan, o);
+        if (lane >= o) scan += t;
+      }
+      if (lane == 63) sums[wave] = scan;
+    }
+    __syncthreads();
+    if (tid < FEW_D) {
+      unsigned at = scan - total;
+      for (int w = 0; w < wave; ++w) at += sums[w];
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const unsigned c = cnt[w][tid];
+        cnt[w][tid] = at;
+        at += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < FEW_PER; ++k) {
+      if (k >= steps || base + 64 * k >= n) continue;
+      const unsigned at = cnt[wave][key[k] >> shift & mask] + rank[k];
+      keys[at] = key[k];
+      places[at] = place[k];
+    }
+    __syncthreads();
+  }
+  for (int i = tid; i < n; i += FEW_THREADS) {
+    a.keys_out[i] = keys[i];
+    a.places_out[i] = places[i];
   }
 }
 
@@ -570,24 +649,32 @@ hipError_t launch_embedding_bwd(int dtype, const EmbeddingArgs& a, const Dropout
   if (bytes < w.bytes) return hipErrorInvalidValue;
   int bits = 1;
   while ((a.vocab >> bits) > 0) ++bits;                    // keys are 0 .. vocab
-  const int passes = (bits + SORT_BITS - 1) / SORT_BITS, per = (bits + passes - 1) / passes;
+  const int most = a.rows <= FEW ? FEW_BITS : SORT_BITS, passes = (bits + most - 1) / most, per = (bits + passes - 1) / passes;
   SortArgs q{};
   q.n = a.rows; q.vocab = (unsigned)a.vocab; q.blocks = w.blocks; q.counts = w.counts; q.totals = w.totals;
   q.mask = (1 << per) - 1; q.scanned = w.blocks > 64;
-  for (int i = 0; i < passes && a.rows; ++i) {
-    q.tokens = i == 0 ? a.tokens : nullptr;
-    q.keys_in = w.keys[(i + 1) & 1]; q.places_in = w.places[(i + 1) & 1];
-    q.keys_out = w.keys[i & 1]; q.places_out = w.places[i & 1];
-    q.shift = i * per;
-    count_kernel<<<w.blocks, NTHR, 0, s>>>(q);
-    if (q.scanned) scan_kernel<<<SORT_D / 64, 64, 0, s>>>(q);
-    place_kernel<<<w.blocks, NTHR, 0, s>>>(q);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  int last = 0;
+  if (a.rows <= FEW) {
+    q.tokens = a.tokens;
+    q.keys_out = w.keys[0]; q.places_out = w.places[0];
+    if (a.rows) sort_few_kernel<<<1, FEW_THREADS, 0, s>>>(q, passes, per);
+  } else {
+    for (int i = 0; i < passes; ++i) {
+      q.tokens = i == 0 ? a.tokens : nullptr;
+      q.keys_in = w.keys[(i + 1) & 1]; q.places_in = w.places[(i + 1) & 1];
+      q.keys_out = w.keys[i & 1]; q.places_out = w.places[i & 1];
+      q.shift = i * per;
+      count_kernel<<<w.blocks, NTHR, 0, s>>>(q);
+      if (q.scanned) scan_kernel<<<SORT_D / 64, 64, 0, s>>>(q);
+      place_kernel<<<w.blocks, NTHR, 0, s>>>(q);
+      last = i & 1;
+    }
   }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   SumArgs m{};
   m.e = a; m.key = key;
-  m.keys = w.keys[(passes - 1) & 1]; m.places = w.places[(passes - 1) & 1];
+  m.keys = w.keys[last]; m.places = w.places[last];
   m.chunk_sums = w.sums; m.starts = w.starts;
   m.n = (unsigned)a.rows; m.units = (unsigned)(a.width / 8);
   if (dtype == 0) return launch_sums_t<float, float>(m, s);
