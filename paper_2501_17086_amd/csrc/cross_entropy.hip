@@ -15,7 +15,7 @@ namespace {
 
 constexpr int NTHR = 256;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int BLOCK_V = 256;                               // rows of the vocabulary whose sum is one number per row of x
+constexpr int BLOCK_V = 64;                                // rows of the vocabulary whose sum is one number per row of x
 
 struct Parts {
   void* x;                // [np, width], storage type: x, zeros where a row does not count
@@ -29,10 +29,11 @@ struct Parts {
   float* logits;          // [piece][np]
   void* grad;             // [piece][np], storage type (fp32: the logits' place)
   float* dx;              // [shares][np, width]
+  float* dweight;         // [shares of the contraction][rows at hand, width], where there are several
   long np, piece;
   long fused;             // rows of the vocabulary whose logits meet no memory
   int blocks, pieces, split, shares;   // shares: products whose results lie side by side until they are added up
-  size_t bytes;
+  size_t dweight_bytes, bytes;
 };
 
 struct CeArgs {
@@ -79,71 +80,76 @@ struct Running {
   __device__ __forceinline__ void add(float om, float ol) {
     const float n = fmaxf(m, om);
     if (n == -INFINITY) { l += ol; return; }               // (nothing yet: zeros, or a NaN, which stays)
-    l = l * exp2f(m - n) + ol * exp2f(om - n);
+    l = l * __builtin_amdgcn_exp2f(m - n) + ol * __builtin_amdgcn_exp2f(om - n);
     m = n;
   }
-};
-__device__ __forceinline__ float log2_sum(const Running& r) { return r.l == 0.f ? -INFINITY : r.m + log2f(r.l); }
-
-// TB rows of x by 256 / TB parts of a block of the vocabulary a workgroup
-template <int TB>
-__device__ __forceinline__ Running meet(Running r, int part, int row, float (&sm)[NTHR / TB][TB], float (&sl)[NTHR / TB][TB]) {
-  sm[part][row] = r.m;
-  sl[part][row] = r.l;
-  __syncthreads();
-  Running t = {-INFINITY, 0.f};
-  if (part == 0) {
-    t = {sm[0][row], sl[0][row]};
-    for (int i = 1; i < NTHR / TB; ++i) t.add(sm[i][row], sl[i][row]);
+  // K numbers at once
+  template <int K> __device__ __forceinline__ void add(const float (&v)[K]) {
+    float top = v[0], sum = 0.f;
+#pragma unroll
+    for (int j = 1; j < K; ++j) top = fmaxf(top, v[j]);
+    const float shift = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int j = 0; j < K; ++j) sum += __builtin_amdgcn_exp2f(v[j] - shift);
+    add(top, sum);
   }
-  return t;
+};
+__device__ __forceinline__ float log2_sum(const Running& r) { return r.l == 0.f ? -INFINITY : r.m + __builtin_amdgcn_logf(r.l); }
+
+// the parts' sums of TB rows meet in a fixed tree; thread = part TB + row, the result is part 0's
+template <int TB, int NT>
+__device__ __forceinline__ Running meet(Running r, float (&sm)[NT], float (&sl)[NT]) {
+  const int t = threadIdx.x;
+  sm[t] = r.m;
+  sl[t] = r.l;
+  __syncthreads();
+#pragma unroll
+  for (int o = NT / 2; o >= TB; o /= 2) {
+    if (t < o) {
+      r.add(sm[t + o], sl[t + o]);
+      sm[t] = r.m;
+      sl[t] = r.l;
+    }
+    __syncthreads();
+  }
+  return r;
 }
+// a block's sums from its logits: TB rows of x a workgroup
 template <int TB>
 __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
   constexpr int PARTS = NTHR / TB, PER = BLOCK_V / PARTS;
-  __shared__ float sm[PARTS][TB], sl[PARTS][TB];
+  __shared__ float sm[NTHR], sl[NTHR];
   const int row = threadIdx.x % TB, part = threadIdx.x / TB;
   const long n = (long)blockIdx.x * TB + row, nc = n < a.p.np ? n : a.p.np - 1;
   const long v0 = (long)blockIdx.y * BLOCK_V + part;
-  Running r = {-INFINITY, 0.f};
-  for (int i = 0; i < PER; i += 8) {
-    float v[8];
-    float top = -INFINITY;
+  float v[PER];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const long at = v0 + (long)(i + j) * PARTS;
-      v[j] = at < a.nv ? a.p.logits[at * a.p.np + nc] * a.to_log2 : -INFINITY;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, v[j]);
-    float sum = 0.f;
-    bool nan = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sum += top == -INFINITY ? 0.f : exp2f(v[j] - top);
-      nan = nan || v[j] != v[j];
-    }
-    r.add(top, nan ? NAN : sum);
+  for (int j = 0; j < PER; ++j) {
+    const long at = v0 + j * PARTS;
+    v[j] = at < a.nv ? a.p.logits[at * a.p.np + nc] * a.to_log2 : -INFINITY;
   }
-  const Running t = meet<TB>(r, part, row, sm, sl);
-  if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = log2_sum(t);
+  Running r = {-INFINITY, 0.f};
+  r.add(v);
+  r = meet<TB>(r, sm, sl);
+  if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = log2_sum(r);
 }
-// all blocks of a row, its loss
-template <int TB>
-__global__ __launch_bounds__(NTHR) void row_loss_kernel(CeArgs a) {
-  constexpr int PARTS = NTHR / TB;
-  __shared__ float sm[PARTS][TB], sl[PARTS][TB];
+// all blocks of TB rows from n0 on by NT threads, and their losses
+template <int TB, int NT>
+__device__ __forceinline__ void row_losses(const CeArgs& a, long n0, float (&sm)[NT], float (&sl)[NT]) {
+  constexpr int PARTS = NT / TB, K = 8;
   const int row = threadIdx.x % TB, part = threadIdx.x / TB;
-  const long n = (long)blockIdx.x * TB + row, nc = n < a.p.np ? n : a.p.np - 1;
+  const long n = n0 + row, nc = n < a.p.np ? n : a.p.np - 1;
   Running r = {-INFINITY, 0.f};
-  for (int b = part; b < a.p.blocks; b += PARTS) {
-    const float v = a.p.sums[(long)b * a.p.np + nc];
-    r.add(v, v == -INFINITY ? 0.f : v != v ? NAN : 1.f);
+  for (int b = part; b < a.p.blocks; b += K * PARTS) {
+    float v[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) v[j] = b + j * PARTS < a.p.blocks ? a.p.sums[(long)(b + j * PARTS) * a.p.np + nc] : -INFINITY;
+    r.add(v);
   }
-  const Running t = meet<TB>(r, part, row, sm, sl);
+  r = meet<TB>(r, sm, sl);
   if (part != 0 || n >= a.p.np) return;
   const bool counts = a.p.target[n] >= 0;
-  const float lse = log2_sum(t);
+  const float lse = log2_sum(r);
   const float loss = counts ? (lse - a.p.target_logit[n]) * LN2 : 0.f;
   a.p.lse[n] = counts ? lse : INFINITY;
   a.p.at_target[n] = counts ? exp2f(a.p.target_logit[n] - lse) - 1.f : 0.f;
@@ -151,9 +157,7 @@ __global__ __launch_bounds__(NTHR) void row_loss_kernel(CeArgs a) {
   if (a.c.row_loss && n < a.c.rows) a.c.row_loss[n] = loss;
 }
 // the loss, and what dS is multiplied by: one workgroup, sums in 64 bits in a fixed order
-__global__ __launch_bounds__(1024) void loss_kernel(CeArgs a) {
-  __shared__ double sum[1024];
-  __shared__ int cnt[1024];
+__device__ __forceinline__ void whole_loss(const CeArgs& a, double (&sum)[1024], int (&cnt)[1024]) {
   const int tid = threadIdx.x;
   double s = 0.0;
   int c = 0;
@@ -173,6 +177,24 @@ __global__ __launch_bounds__(1024) void loss_kernel(CeArgs a) {
     a.c.loss[0] = (float)(sum[0] * f);
     a.p.scalars[0] = (float)(f * a.c.scale);
   }
+}
+__global__ __launch_bounds__(NTHR) void row_loss_kernel(CeArgs a) {
+  __shared__ float sm[NTHR], sl[NTHR];
+  row_losses<32>(a, 32l * blockIdx.x, sm, sl);
+}
+__global__ __launch_bounds__(1024) void loss_kernel(CeArgs a) {
+  __shared__ double sum[1024];
+  __shared__ int cnt[1024];
+  whole_loss(a, sum, cnt);
+}
+// few rows: both in one workgroup
+__global__ __launch_bounds__(1024) void few_loss_kernel(CeArgs a) {
+  __shared__ float sm[1024], sl[1024];
+  __shared__ double sum[1024];
+  __shared__ int cnt[1024];
+  for (long n0 = 0; n0 < a.p.np; n0 += 8) row_losses<8>(a, n0, sm, sl);
+  __syncthreads();                                         // (the rows' losses, written above, are read below by other threads)
+  whole_loss(a, sum, cnt);
 }
 
 // dS of a piece: 8 rows of x a thread
@@ -228,6 +250,21 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
   }
   store8(reinterpret_cast<T*>(a.c.dx.p) + n * a.c.dx.row + c, s);
 }
+// rows of dweight from their shares, n8 elements of 8
+template <typename O>
+__global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out, long row, long n8, int shares, unsigned per) {
+  const long i = (long)blockIdx.x * NTHR + threadIdx.x;
+  if (i >= n8) return;
+  float s[8];
+  load8(part + 8 * i, s);
+  for (int k = 1; k < shares; ++k) {
+    float v[8];
+    load8(part + 8 * (k * n8 + i), v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] += v[j];
+  }
+  store8(out + i / per * row + 8 * (i % per), s);
+}
 template <typename T>
 __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, int width) {
   const long i = (long)blockIdx.x * NTHR + threadIdx.x, per = width / 8;
@@ -237,6 +274,7 @@ __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, 
 }
 
 // ---- sizes -----------------------------------------------------------------------------------------------------------
+constexpr long FEW_ROWS = 32;                              // rows whose losses and sum are one workgroup's
 // A piece of the vocabulary takes 1 GB of logits, or of dS where the logits are not written (256 rows of the vocabulary: more, from 2^20 rows
 // of x on).
 constexpr size_t PIECE_BYTES = 1ul << 30;
@@ -254,13 +292,32 @@ long fused_rows(int dtype, long np, long vocab, int width) {
   const long tiles = vocab / 256 * (np / 256);
   return gemm_fills_chip(tiles) && tiles < (1l << 28) ? vocab / 256 * 256 : 0;
 }
-// dx has few tiles and a long contraction, the vocabulary: it is shared out until there is a tile for every compute unit.
-int dx_split(int dtype, long np, int width, long nv) {
-  const long t = dtype == 0 ? 64 : np % 256 == 0 && width % 256 == 0 ? 256 : 128;
-  const long tiles = (np + t - 1) / t * ((width + t - 1) / t);
-  long split = (256 + tiles / 2) / tiles;
-  if (split > nv / 512) split = nv / 512;
-  return (int)(split < 1 ? 1 : split > MAX_SPLIT ? MAX_SPLIT : split);
+// A product of few tiles and a long contraction (dx: over the vocabulary, dweight: over the rows of x) is shared out until there is a tile for
+// every compute unit.  rows, cols: of its result; wide: the 256 x 256 kernel would take it.
+int shares_of(int dtype, long rows, long cols, long k, bool wide) {
+  const long t = dtype == 0 ? 64 : wide ? 256 : 128;
+  const long tiles = (rows + t - 1) / t * ((cols + t - 1) / t);
+  if (gemm_fills_chip(tiles)) return 1;
+  long n = 256 / tiles;
+  if (n > k / 512) n = k / 512;
+  return (int)(n < 1 ? 1 : n > MAX_SPLIT ? MAX_SPLIT : n);
+}
+int dx_split(int dtype, long np, int width, long nv) { return shares_of(dtype, np, width, nv, np % 256 == 0 && width % 256 == 0); }
+int dweight_split(int dtype, long np, int width, long nv) {
+  return shares_of(dtype, nv, width, np, nv % 256 == 0 && width % 256 == 0 && np % 32 == 0);
+}
+// Rows of the vocabulary whose dweight is a product of its own: whole tiles of 256 (the last ones would take all others to smaller tiles).
+long dweight_whole(int dtype, long np, int width, long nv) {
+  return dtype == 1 && width % 256 == 0 && np % 32 == 0 && nv >= 512 ? nv / 256 * 256 : nv;
+}
+size_t dweight_part(int dtype, long np, int width, long nv) {      // bytes of the shares of nv rows in one product
+  const int n = dweight_split(dtype, np, width, nv);
+  return n > 1 ? (size_t)n * nv * width * 4 : 0;
+}
+size_t dweight_room(int dtype, long np, int width, long nv) {      // ... and of those of a piece, the last rows apart
+  const long whole = dweight_whole(dtype, np, width, nv);
+  const size_t a = dweight_part(dtype, np, width, whole), b = whole < nv ? dweight_part(dtype, np, width, nv - whole) : 0;
+  return a > b ? a : b;
 }
 
 Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradients) {
@@ -271,13 +328,14 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.np = padded(rows);
   p.fused = fused_rows(dtype, p.np, vocab, width);
   const size_t row = (p.fused ? 2 : 4) * (p.np ? p.np : 1);
-  const long fit = (long)(PIECE_BYTES / row) / BLOCK_V * BLOCK_V;
-  const long most = fit < BLOCK_V ? BLOCK_V : fit < PIECE_ROWS ? fit : PIECE_ROWS;
-  p.pieces = (int)((vocab + most - 1) / most);             // of one size, as near as whole blocks allow
-  p.piece = ((vocab + p.pieces - 1) / p.pieces + BLOCK_V - 1) / BLOCK_V * BLOCK_V;
+  constexpr long TILE = 256;
+  const long fit = (long)(PIECE_BYTES / row) / TILE * TILE;
+  const long most = fit < TILE ? TILE : fit < PIECE_ROWS ? fit : PIECE_ROWS;
+  p.pieces = (int)((vocab + most - 1) / most);             // of one size, as near as whole tiles allow
+  p.piece = ((vocab + p.pieces - 1) / p.pieces + TILE - 1) / TILE * TILE;
   p.pieces = (int)((vocab + p.piece - 1) / p.piece);
   if (p.piece > vocab) p.piece = vocab;
-  p.blocks = p.fused ? (int)(p.fused / 128 + (p.fused < vocab)) : (int)((vocab + BLOCK_V - 1) / BLOCK_V);
+  p.blocks = p.fused ? (int)(p.fused / 128 + (vocab - p.fused + BLOCK_V - 1) / BLOCK_V) : (int)((vocab + BLOCK_V - 1) / BLOCK_V);
   p.x = take(p.np * width * es);
   p.target_logit = reinterpret_cast<float*>(take(4 * p.np));
   p.lse = reinterpret_cast<float*>(take(4 * p.np));
@@ -293,6 +351,9 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
     p.split = dx_split(dtype, p.np ? p.np : 8, width, p.piece);
     p.shares = p.split + 2 < 4 ? 4 : p.split + 2;
     p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * width * 4));
+    const size_t most = dweight_room(dtype, p.np, width, p.piece), last = dweight_room(dtype, p.np, width, vocab - (p.pieces - 1) * p.piece);
+    p.dweight_bytes = most > last ? most : last;
+    p.dweight = reinterpret_cast<float*>(take(p.dweight_bytes));
   }
   p.bytes = off;
   return p;
@@ -346,7 +407,7 @@ struct Run {
   hipError_t block_sums(long block0) {
     a.block0 = block0;
     const unsigned nb = (unsigned)((a.nv + BLOCK_V - 1) / BLOCK_V);
-    if (p.np >= 64) block_sums_kernel<64><<<dim3((unsigned)((p.np + 63) / 64), nb), NTHR, 0, s>>>(a);
+    if (p.np >= 32) block_sums_kernel<32><<<dim3((unsigned)((p.np + 31) / 32), nb), NTHR, 0, s>>>(a);
     else block_sums_kernel<8><<<dim3((unsigned)(p.np / 8), nb), NTHR, 0, s>>>(a);
     return hipGetLastError();
   }
@@ -398,31 +459,40 @@ struct Run {
     return softmax_grad();
   }
   hipError_t dweight_rows(long v0, long r0, long nr) {
+    const int n = dweight_split(DTYPE, p.np, c.width, nr);
     GemmArgs g = plain();
     g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = p.np; g.a_sk = 1;
     g.B = p.x; g.b_sk = c.width; g.b_sn = 1;
-    g.c_is_f32 = c.grad_dtype == 0;
-    const long o = (v0 + r0) * c.dweight.row;
-    if (g.c_is_f32) g.C = reinterpret_cast<float*>(c.dweight.p) + o;
-    else g.C = reinterpret_cast<bf16_t*>(c.dweight.p) + o;
-    g.ldc = c.dweight.row;
     g.M = nr; g.N = c.width; g.K = p.np;
-    return product(DTYPE, g, s);
-  }
-  // (whole tiles of 256 rows by themselves where those fill the chip: the last ones would take all others to smaller tiles)
-  hipError_t dweight(long v0, long nv) {
-    const long whole = nv / 256 * 256;
-    if (DTYPE == 1 && whole < nv && c.width % 256 == 0 && p.np % 32 == 0 && gemm_fills_chip(whole / 256 * (c.width / 256))) {
-      CE_TRY(dweight_rows(v0, 0, whole));
-      return dweight_rows(v0, whole, nv - whole);
+    const long o = (v0 + r0) * c.dweight.row;
+    float* f = reinterpret_cast<float*>(c.dweight.p) + o;
+    bf16_t* b = reinterpret_cast<bf16_t*>(c.dweight.p) + o;
+    if (n == 1) {
+      g.c_is_f32 = c.grad_dtype == 0;
+      if (g.c_is_f32) g.C = f; else g.C = b;
+      g.ldc = c.dweight.row;
+      return product(DTYPE, g, s);
     }
-    return dweight_rows(v0, 0, nv);
+    if (dweight_part(DTYPE, p.np, c.width, nr) > p.dweight_bytes) return hipErrorInvalidValue;
+    g.c_is_f32 = 1; g.C = p.dweight; g.ldc = c.width; g.c_sb = nr * c.width; g.split_k = n;
+    CE_TRY(product(DTYPE, g, s));
+    const long n8 = nr * c.width / 8;
+    const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR), per = (unsigned)(c.width / 8);
+    if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per);
+    else dweight_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(p.dweight, b, c.dweight.row, n8, n, per);
+    return hipGetLastError();
+  }
+  hipError_t dweight(long v0, long nv) {
+    const long whole = dweight_whole(DTYPE, p.np, c.width, nv);
+    CE_TRY(dweight_rows(v0, 0, whole));
+    return whole < nv ? dweight_rows(v0, whole, nv - whole) : hipSuccess;
   }
   hipError_t dx_rows(long v0, long r0, long nr, int split) {
     GemmArgs g = plain();
     g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = 1; g.a_sk = p.np;
     g.B = reinterpret_cast<const T*>(c.weight.p) + (v0 + r0) * c.weight.row; g.b_sk = c.weight.row; g.b_sn = 1;
     if (shares + split > p.shares) CE_TRY(fold());
+    if (shares + split > p.shares) return hipErrorInvalidValue;
     g.C = p.dx + (long)shares * p.np * c.width; g.ldc = c.width; g.c_is_f32 = 1;
     g.c_sb = p.np * c.width;
     g.split_k = split;
@@ -454,9 +524,12 @@ struct Run {
     rows_kernel<T><<<(unsigned)((p.np + 3) / 4), NTHR, 0, s>>>(a);
     CE_TRY(hipGetLastError());
     CE_TRY(sums());
-    if (p.np >= 4096) row_loss_kernel<64><<<(unsigned)((p.np + 63) / 64), NTHR, 0, s>>>(a);
-    else row_loss_kernel<8><<<(unsigned)(p.np / 8), NTHR, 0, s>>>(a);
-    loss_kernel<<<1, 1024, 0, s>>>(a);
+    if (p.np <= FEW_ROWS) {
+      few_loss_kernel<<<1, 1024, 0, s>>>(a);
+    } else {
+      row_loss_kernel<<<(unsigned)((p.np + 31) / 32), NTHR, 0, s>>>(a);
+      loss_kernel<<<1, 1024, 0, s>>>(a);
+    }
     CE_TRY(hipGetLastError());
     if (!c.dx.p && !c.dweight.p) return hipSuccess;
     for (int i = 0; i < p.pieces; ++i) {

@@ -460,9 +460,9 @@ __global__ __launch_bounds__(NTHR, 1) void gemm_mfma_lean_kernel(GemmArgs g, Wal
   int t = (ONE_AT_A_TIME ? xcd * wpx : xcd * walk.per_xcd) + (int)(blockIdx.x >> 3);
   const int t_end = !ONE_AT_A_TIME && (xcd + 1) * walk.per_xcd < walk.total ? (xcd + 1) * walk.per_xcd : walk.total;
   if (t >= t_end) return;
-  // Shares of unequal length are met by the parameter gradients alone (the only split launches); elsewhere a launch's one
-  // length stays in a scalar register.
-  constexpr bool SHARES = !A_KC;
+  // Shares of unequal length are met by the parameter gradients and a vocabulary's alone (the only split launches); elsewhere a
+  // launch's one length stays in a scalar register.
+  constexpr bool SHARES = !A_KC || (!B_KC && FAST == FAST_STORE_F32);
   auto slices_of = [&](const TileCoord& c) { return SHARES ? c.kt : walk.KT; };
 
   const long lda = A_KC ? g.a_sm : g.a_sk;
@@ -731,7 +731,8 @@ inline hipError_t launch_tile_for(const GemmArgs& g, hipStream_t s) {
 // does the lean kernel have this pairing's epilogue?
 inline bool has_lean(const GemmArgs& g, bool a_kc, bool b_kc) {
   if (!a_kc) return g.mode == EPI_STORE && !g.addf && (g.c_is_f32 || g.split_k > 1);     // parameter gradients
-  if (g.addf || g.split_k > 1) return false;
+  if (g.addf || (g.split_k > 1 && b_kc)) return false;
+  if (g.split_k > 1) return g.mode == EPI_STORE && g.batch == 1;                         // a vocabulary's gradient in shares
   if (g.c_is_f32) return g.mode == EPI_STORE && (b_kc || g.batch == 1);   // the recurrent kinds' U xin; a vocabulary's gradient
   if (g.mode == EPI_STORE) return true;
   if (!b_kc) return g.mode == EPI_MUL_AUX || g.mode == EPI_MUL_1MZ2 || g.mode == EPI_ADD_AUX;   // block VJPs
@@ -739,8 +740,8 @@ inline bool has_lean(const GemmArgs& g, bool a_kc, bool b_kc) {
   return g.mode == EPI_RESID && g.aux && !g.lambda_mn;
 }
 hipError_t launch_lean_nn(const GemmArgs& g, hipStream_t s) {
-  if (g.c_is_f32)
-    return g.K % (2 * BK) == 0 ? launch_lean_walk<true, false, FAST_STORE_F32, false, true>(g, s)
+  if (g.c_is_f32 || g.split_k > 1)
+    return g.K % ((long)g.split_k * 2 * BK) == 0 ? launch_lean_walk<true, false, FAST_STORE_F32, false, true>(g, s)
                                : launch_lean_walk<true, false, FAST_STORE_F32, false, false>(g, s);
   switch (g.mode) {
     case EPI_STORE: return launch_lean<true, false, FAST_STORE>(g, s);

@@ -194,7 +194,7 @@ def check_loss(x, w, t, scale=1.0, mean=True, factor=1.0, grad=torch.float32, ag
 
 
 SIZES = [(1, 1, 8), (1, 50, 16), (2, 9, 8), (8, 2000, 256), (3, 257, 72), (70, 4096, 64), (333, 1009, 72), (130, 70, 264), (257, 1000, 128),
-         (64, 513, 1032), (1000, 300, 512)]
+         (64, 513, 1032), (1000, 300, 512), (2000, 70, 128), (40, 3000, 8)]
 
 
 @pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
@@ -207,7 +207,7 @@ def test_cross_entropy(n, vocab, width, dtype, grad):
 
 
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
-@pytest.mark.parametrize("n,vocab,width", [(1000, 9300, 128), (1000, 9300, 160), (4101, 2381, 256), (2048, 9216, 264), (900, 20001, 512),
+@pytest.mark.parametrize("n,vocab,width", [(1000, 9300, 128), (1000, 9300, 160), (4101, 2381, 256), (4090, 9300, 1024), (8192, 1100, 256), (2048, 9216, 264), (900, 20001, 512),
                                            (8190, 5003, 1024)])
 def test_cross_entropy_of_many_tiles(n, vocab, width, grad):
     """Sizes whose logits meet no memory: whole tiles, tiles and a rest, contractions that are no multiple of 64, rows filled up."""
