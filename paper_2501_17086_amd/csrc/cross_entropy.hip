@@ -247,6 +247,13 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += v[j];
     }
+    if constexpr (sizeof(T) == 2) {      // a confident row's dx is next to its target's coefficient times a row of the weights: what
+      const float g = a.p.at_target[n] * a.p.scalars[0], rest = g - __uint_as_float(pack_bf16x2(0.f, g) & 0xFFFF0000u);   // its rounding
+      float w[8];                                                                                                // left out
+      load8(reinterpret_cast<const T*>(a.c.weight.p) + (long)a.p.target[n] * a.c.weight.row + c, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = fmaf(rest, w[j], s[j]);
+    }
   }
   store8(reinterpret_cast<T*>(a.c.dx.p) + n * a.c.dx.row + c, s);
 }
