@@ -18,7 +18,8 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int BLOCK_V = 64;                                // rows of the vocabulary whose sum is one number per row of x
 
 struct Parts {
-  void* x;                // [np, width], storage type: x, zeros where a row does not count
+  void* x;                // [np, wp], storage type: x, zeros where a row does not count and behind its channels
+  void* weight;           // [vocab, wp]: the weights with zeros behind their channels, where wp is not the width; else NULL
   float* target_logit;    // [np], times log2 e
   float* lse;             // [np], base 2; infinity where a row does not count: its probabilities are zeros
   int* target;            // [np], -1 where a row does not count
@@ -28,9 +29,10 @@ struct Parts {
   float* sums;            // [blocks][np]: base 2 logarithms of a block's sums
   float* logits;          // [piece][np]
   void* grad;             // [piece][np], storage type (fp32: the logits' place)
-  float* dx;              // [shares][np, width]
+  float* dx;              // [shares][np, wp]
   float* dweight;         // [shares of the contraction][rows at hand, width], where there are several
   long np, piece;
+  int wp;                 // channels with those that fill up
   long fused;             // rows of the vocabulary whose logits meet no memory
   int blocks, pieces, split, shares;   // shares: products whose results lie side by side until they are added up
   size_t dweight_bytes, bytes;
@@ -53,11 +55,11 @@ __global__ __launch_bounds__(NTHR) void rows_kernel(CeArgs a) {
   if (n >= a.p.np) return;
   const int t = n < a.c.rows ? a.c.targets[n] : -1;
   const bool counts = t >= 0 && t < a.c.vocab;
-  T* copy = reinterpret_cast<T*>(a.p.x) + n * a.c.width;
+  T* copy = reinterpret_cast<T*>(a.p.x) + n * a.p.wp;
   float dot = 0.f;
-  for (int c = 8 * lane; c < a.c.width; c += 512) {
+  for (int c = 8 * lane; c < a.p.wp; c += 512) {
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (counts) {
+    if (counts && c < a.c.width) {
       float w[8];
       load8(reinterpret_cast<const T*>(a.c.x.p) + n * a.c.x.row + c, v);
       load8(reinterpret_cast<const T*>(a.c.weight.p) + t * a.c.weight.row + c, w);
@@ -71,6 +73,17 @@ __global__ __launch_bounds__(NTHR) void rows_kernel(CeArgs a) {
   if (lane == 0) {
     a.p.target_logit[n] = dot * a.to_log2;
     a.p.target[n] = counts ? t : -1;
+  }
+}
+
+// the weights with their channels filled up
+__global__ __launch_bounds__(NTHR) void weight_kernel(CeArgs a) {
+  const long per = a.p.wp / 8, total = a.c.vocab * per;
+  for (long i = (long)blockIdx.x * NTHR + threadIdx.x; i < total; i += (long)gridDim.x * NTHR) {
+    const long v = i / per, c = 8 * (i - v * per);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (c < a.c.width) w = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.c.weight.p) + v * a.c.weight.row + c);
+    *reinterpret_cast<uint4*>(reinterpret_cast<bf16_t*>(a.p.weight) + v * a.p.wp + c) = w;
   }
 }
 
@@ -243,7 +256,7 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
   if (a.p.target[n] >= 0) {
     for (int k = 0; k < shares; ++k) {
       float v[8];
-      load8(a.p.dx + ((long)k * a.p.np + n) * a.c.width + c, v);
+      load8(a.p.dx + ((long)k * a.p.np + n) * a.p.wp + c, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += v[j];
     }
@@ -274,10 +287,9 @@ __global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out
 }
 template <typename T>
 __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, int width) {
-  const long i = (long)blockIdx.x * NTHR + threadIdx.x, per = width / 8;
-  if (i >= rows * per) return;
+  const long per = width / 8;
   const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  store8(p + i / per * row + 8 * (i % per), z);
+  for (long i = (long)blockIdx.x * NTHR + threadIdx.x; i < rows * per; i += (long)gridDim.x * NTHR) store8(p + i / per * row + 8 * (i % per), z);
 }
 
 // ---- sizes -----------------------------------------------------------------------------------------------------------
@@ -293,9 +305,16 @@ long padded(long rows) {
   const long whole = (rows + 255) / 256 * 256;
   return whole <= rows + rows / 8 ? whole : (rows + 7) / 8 * 8;
 }
+// Channels are filled up with zeros to a multiple of 32, and to one of 256 where that is an eighth more at most, for the sake of the
+// 256 x 256 kernel; the weights are copied for it, which takes as long as one of the four products with 500 rows of x.
+int padded_width(int width) {
+  const int whole = (width + 255) / 256 * 256;
+  if (whole <= width + width / 8) return whole;
+  return width < 128 ? 128 : (width + 31) / 32 * 32;
+}
 // Rows of the vocabulary that the 256 x 256 kernel's own epilogues take: all whole tiles, where those fill the chip.
-long fused_rows(int dtype, long np, long vocab, int width) {
-  if (dtype != 1 || np % 256 || np == 0 || width % 32 || width < 128) return 0;
+long fused_rows(int dtype, long np, long vocab) {
+  if (dtype != 1 || np % 256 || np == 0) return 0;
   const long tiles = vocab / 256 * (np / 256);
   return gemm_fills_chip(tiles) && tiles < (1l << 28) ? vocab / 256 * 256 : 0;
 }
@@ -309,13 +328,17 @@ int shares_of(int dtype, long rows, long cols, long k, bool wide) {
   if (n > k / 512) n = k / 512;
   return (int)(n < 1 ? 1 : n > MAX_SPLIT ? MAX_SPLIT : n);
 }
-int dx_split(int dtype, long np, int width, long nv) { return shares_of(dtype, np, width, nv, np % 256 == 0 && width % 256 == 0); }
+int dx_split(int dtype, long np, int wp, long nv) {
+  const bool wide = np % 256 == 0 && wp >= 256;
+  return shares_of(dtype, np, wide ? wp / 256 * 256 : wp, nv, wide);
+}
 int dweight_split(int dtype, long np, int width, long nv) {
-  return shares_of(dtype, nv, width, np, nv % 256 == 0 && width % 256 == 0 && np % 32 == 0);
+  const bool wide = nv % 256 == 0 && width >= 256 && np % 32 == 0;
+  return shares_of(dtype, nv, wide ? width / 256 * 256 : width, np, wide);
 }
 // Rows of the vocabulary whose dweight is a product of its own: whole tiles of 256 (the last ones would take all others to smaller tiles).
 long dweight_whole(int dtype, long np, int width, long nv) {
-  return dtype == 1 && width % 256 == 0 && np % 32 == 0 && nv >= 512 ? nv / 256 * 256 : nv;
+  return dtype == 1 && width >= 256 && np % 32 == 0 && nv >= 512 ? nv / 256 * 256 : nv;
 }
 size_t dweight_part(int dtype, long np, int width, long nv) {      // bytes of the shares of nv rows in one product
   const int n = dweight_split(dtype, np, width, nv);
@@ -333,7 +356,8 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   auto take = [&](size_t n) { char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
   const size_t es = dtype == 0 ? 4 : 2;
   p.np = padded(rows);
-  p.fused = fused_rows(dtype, p.np, vocab, width);
+  p.fused = fused_rows(dtype, p.np, vocab);
+  p.wp = p.fused ? padded_width(width) : width;
   const size_t row = (p.fused ? 2 : 4) * (p.np ? p.np : 1);
   constexpr long TILE = 256;
   const long fit = (long)(PIECE_BYTES / row) / TILE * TILE;
@@ -343,7 +367,8 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.pieces = (int)((vocab + p.piece - 1) / p.piece);
   if (p.piece > vocab) p.piece = vocab;
   p.blocks = p.fused ? (int)(p.fused / 128 + (vocab - p.fused + BLOCK_V - 1) / BLOCK_V) : (int)((vocab + BLOCK_V - 1) / BLOCK_V);
-  p.x = take(p.np * width * es);
+  p.x = take(p.np * p.wp * es);
+  if (p.wp != width) p.weight = take((size_t)vocab * p.wp * es);
   p.target_logit = reinterpret_cast<float*>(take(4 * p.np));
   p.lse = reinterpret_cast<float*>(take(4 * p.np));
   p.target = reinterpret_cast<int*>(take(4 * p.np));
@@ -355,9 +380,9 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.grad = p.logits;
   if (gradients) {
     if (dtype == 1) p.grad = take((size_t)p.piece * p.np * 2);
-    p.split = dx_split(dtype, p.np ? p.np : 8, width, p.piece);
+    p.split = dx_split(dtype, p.np ? p.np : 8, p.wp, p.piece);
     p.shares = p.split + 2 < 4 ? 4 : p.split + 2;
-    p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * width * 4));
+    p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * p.wp * 4));
     const size_t most = dweight_room(dtype, p.np, width, p.piece), last = dweight_room(dtype, p.np, width, vocab - (p.pieces - 1) * p.piece);
     p.dweight_bytes = most > last ? most : last;
     p.dweight = reinterpret_cast<float*>(take(p.dweight_bytes));
@@ -397,13 +422,28 @@ struct Run {
   int shares = 0;
   Run(const CrossEntropyArgs& c_, const Parts& p_, hipStream_t s_) : c(c_), p(p_), s(s_), a{} { a.c = c; a.p = p; a.to_log2 = c.scale * LOG2E; }
 
+  // the weights' rows from v0 on as the products read them
+  long weight_row() const { return p.weight ? p.wp : c.weight.row; }
+  const T* weight_at(long v0) const { return reinterpret_cast<const T*>(p.weight ? p.weight : c.weight.p) + v0 * weight_row(); }
   GemmArgs logits_args(long v0, long nv) const {
     GemmArgs g = plain();
-    g.A = reinterpret_cast<const T*>(c.weight.p) + v0 * c.weight.row; g.a_sm = c.weight.row; g.a_sk = 1;
-    g.B = p.x; g.b_sn = c.width; g.b_sk = 1;
+    g.A = weight_at(v0); g.a_sm = weight_row(); g.a_sk = 1;
+    g.B = p.x; g.b_sn = p.wp; g.b_sk = 1;
     g.ldc = p.np;
-    g.M = nv; g.N = p.np; g.K = c.width;
+    g.M = nv; g.N = p.np; g.K = p.wp;
     return g;
+  }
+  // a product whose columns are the channels: whole tiles of 256 of them apart from the rest, on the 256 x 256 kernel
+  hipError_t by_columns(GemmArgs g, bool wide) const {
+    const long whole = DTYPE == 1 && wide ? g.N / 256 * 256 : 0, rest = g.N - whole;
+    if (whole == 0 || rest == 0) return product(DTYPE, g, s);
+    g.N = whole;
+    CE_TRY(product(DTYPE, g, s));
+    g.N = rest;
+    g.B = reinterpret_cast<const T*>(g.B) + whole;
+    if (g.c_is_f32) g.C = reinterpret_cast<float*>(g.C) + whole;
+    else g.C = reinterpret_cast<T*>(g.C) + whole;
+    return product(DTYPE, g, s);
   }
   void at(long v0, long nv) { a.v0 = v0; a.nv = nv; a.grad0 = 0; }
   hipError_t logits() {
@@ -423,7 +463,7 @@ struct Run {
     return hipGetLastError();
   }
   hipError_t fold() {
-    const long n8 = p.np * c.width / 8;
+    const long n8 = p.np * p.wp / 8;
     fold_kernel<<<(unsigned)((n8 + NTHR - 1) / NTHR), NTHR, 0, s>>>(p.dx, n8, shares);
     shares = 1;
     return hipGetLastError();
@@ -469,7 +509,7 @@ struct Run {
     const int n = dweight_split(DTYPE, p.np, c.width, nr);
     GemmArgs g = plain();
     g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = p.np; g.a_sk = 1;
-    g.B = p.x; g.b_sk = c.width; g.b_sn = 1;
+    g.B = p.x; g.b_sk = p.wp; g.b_sn = 1;
     g.M = nr; g.N = c.width; g.K = p.np;
     const long o = (v0 + r0) * c.dweight.row;
     float* f = reinterpret_cast<float*>(c.dweight.p) + o;
@@ -478,11 +518,11 @@ struct Run {
       g.c_is_f32 = c.grad_dtype == 0;
       if (g.c_is_f32) g.C = f; else g.C = b;
       g.ldc = c.dweight.row;
-      return product(DTYPE, g, s);
+      return by_columns(g, nr % 256 == 0);
     }
     if (dweight_part(DTYPE, p.np, c.width, nr) > p.dweight_bytes) return hipErrorInvalidValue;
     g.c_is_f32 = 1; g.C = p.dweight; g.ldc = c.width; g.c_sb = nr * c.width; g.split_k = n;
-    CE_TRY(product(DTYPE, g, s));
+    CE_TRY(by_columns(g, nr % 256 == 0));
     const long n8 = nr * c.width / 8;
     const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR), per = (unsigned)(c.width / 8);
     if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per);
@@ -497,30 +537,31 @@ struct Run {
   hipError_t dx_rows(long v0, long r0, long nr, int split) {
     GemmArgs g = plain();
     g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = 1; g.a_sk = p.np;
-    g.B = reinterpret_cast<const T*>(c.weight.p) + (v0 + r0) * c.weight.row; g.b_sk = c.weight.row; g.b_sn = 1;
+    g.B = weight_at(v0 + r0); g.b_sk = weight_row(); g.b_sn = 1;
     if (shares + split > p.shares) CE_TRY(fold());
     if (shares + split > p.shares) return hipErrorInvalidValue;
-    g.C = p.dx + (long)shares * p.np * c.width; g.ldc = c.width; g.c_is_f32 = 1;
-    g.c_sb = p.np * c.width;
+    g.C = p.dx + (long)shares * p.np * p.wp; g.ldc = p.wp; g.c_is_f32 = 1;
+    g.c_sb = p.np * p.wp;
     g.split_k = split;
     shares += split;
-    g.M = p.np; g.N = c.width; g.K = nr;
-    return product(DTYPE, g, s);
+    g.M = p.np; g.N = p.wp; g.K = nr;
+    return by_columns(g, p.np % 256 == 0);
   }
   // (a contraction that is no multiple of 32 keeps the 256 x 256 kernel from all of it)
   hipError_t dx(long v0, long nv) {
     const long whole = nv / 32 * 32;
     if (DTYPE == 1 && whole < nv && whole > 0 && p.np % 256 == 0) {
-      CE_TRY(dx_rows(v0, 0, whole, dx_split(DTYPE, p.np, c.width, whole)));
+      CE_TRY(dx_rows(v0, 0, whole, dx_split(DTYPE, p.np, p.wp, whole)));
       return dx_rows(v0, whole, nv - whole, 1);
     }
-    return dx_rows(v0, 0, nv, dx_split(DTYPE, p.np, c.width, nv));
+    return dx_rows(v0, 0, nv, dx_split(DTYPE, p.np, p.wp, nv));
   }
 
   hipError_t without_rows() {
     loss_kernel<<<1, 1024, 0, s>>>(a);
     if (c.dweight.p) {
-      const unsigned blocks = (unsigned)((c.vocab * (c.width / 8) + NTHR - 1) / NTHR);
+      const long all = (c.vocab * (c.width / 8) + NTHR - 1) / NTHR;
+      const unsigned blocks = all < 65536 ? (unsigned)all : 65536u;
       if (c.grad_dtype == 0) clear_kernel<float><<<blocks, NTHR, 0, s>>>(reinterpret_cast<float*>(c.dweight.p), c.dweight.row, c.vocab, c.width);
       else clear_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(reinterpret_cast<bf16_t*>(c.dweight.p), c.dweight.row, c.vocab, c.width);
     }
@@ -529,6 +570,10 @@ struct Run {
   hipError_t all() {
     if (c.rows == 0) return without_rows();
     rows_kernel<T><<<(unsigned)((p.np + 3) / 4), NTHR, 0, s>>>(a);
+    if (p.weight) {
+      const long all = (c.vocab * (p.wp / 8) + NTHR - 1) / NTHR;
+      weight_kernel<<<all < 65536 ? (unsigned)all : 65536u, NTHR, 0, s>>>(a);
+    }
     CE_TRY(hipGetLastError());
     CE_TRY(sums());
     if (p.np <= FEW_ROWS) {
