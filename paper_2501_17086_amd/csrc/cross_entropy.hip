@@ -13,6 +13,7 @@ namespace hbp {
 
 namespace {
 
+typedef float float16v __attribute__((ext_vector_type(16)));
 constexpr int NTHR = 256;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int BLOCK_V = 64;                                // rows of the vocabulary whose sum is one number per row of x
@@ -45,34 +46,45 @@ struct CeArgs {
   long v0, nv;            // the rows of the vocabulary at hand
   long block0;            // their first block of sums
   long grad0;             // where their dS begins in its piece
+  unsigned grad_blocks;   // grad_kernel's workgroups; those behind them copy x
 };
 
-// x's copy, the target's logit: a wavefront a row
+// x's copy, a wavefront a row; the product with a row of the weights
 template <typename T>
-__global__ __launch_bounds__(NTHR) void rows_kernel(CeArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long n = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (n >= a.p.np) return;
-  const int t = n < a.c.rows ? a.c.targets[n] : -1;
-  const bool counts = t >= 0 && t < a.c.vocab;
+__device__ __forceinline__ float copy_row(const CeArgs& a, long n, int lane, bool counts, const T* w) {
   T* copy = reinterpret_cast<T*>(a.p.x) + n * a.p.wp;
   float dot = 0.f;
   for (int c = 8 * lane; c < a.p.wp; c += 512) {
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (counts && c < a.c.width) {
-      float w[8];
       load8(reinterpret_cast<const T*>(a.c.x.p) + n * a.c.x.row + c, v);
-      load8(reinterpret_cast<const T*>(a.c.weight.p) + t * a.c.weight.row + c, w);
+      if (w) {
+        float u[8];
+        load8(w + c, u);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) dot = fmaf(v[j], w[j], dot);
+        for (int j = 0; j < 8; ++j) dot = fmaf(v[j], u[j], dot);
+      }
     }
     store8(copy + c, v);
   }
+  return dot;
+}
+__device__ __forceinline__ int target_of(const CeArgs& a, long n) {
+  const int t = n < a.c.rows ? a.c.targets[n] : -1;
+  return t >= 0 && t < a.c.vocab ? t : -1;
+}
+template <typename T>
+__global__ __launch_bounds__(NTHR) void rows_kernel(CeArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long n = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (n >= a.p.np) return;
+  const int t = target_of(a, n);
+  float dot = copy_row(a, n, lane, t >= 0, t >= 0 ? reinterpret_cast<const T*>(a.c.weight.p) + t * a.c.weight.row : nullptr);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
   if (lane == 0) {
     a.p.target_logit[n] = dot * a.to_log2;
-    a.p.target[n] = counts ? t : -1;
+    a.p.target[n] = t;
   }
 }
 
@@ -146,6 +158,96 @@ __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
   r = meet<TB>(r, sm, sl);
   if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = log2_sum(r);
 }
+// Small problems: logits, a block's sums and the targets' logits in one launch, without x's copy.  A workgroup takes 64 rows of the vocabulary and
+// 32 of x, its wavefronts a quarter of the channels each, straight from memory into the layout of the matrix instructions, and
+// the quarters meet in LDS.  (8 rows against 16384 x 256: 16.0 -> 10.7 us.)
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> {                          // 16 channels a step, 8 of them in each half of the wavefront
+  typedef __bf16 vec __attribute__((ext_vector_type(8)));
+  static constexpr int STEP = 16;
+  uint4 v;
+  __device__ __forceinline__ void load(const bf16_t* row, int k, int h, int end, bool in) {
+    v = make_uint4(0, 0, 0, 0);
+    if (in && k + 8 * h < end) v = *reinterpret_cast<const uint4*>(row + k + 8 * h);
+  }
+  static __device__ __forceinline__ void multiply(float16v& acc, const Frag& a, const Frag& b) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(vec, a.v), __builtin_bit_cast(vec, b.v), acc, 0, 0, 0);
+  }
+};
+template <> struct Frag<float> {                           // 8 a step, 4 and 4
+  static constexpr int STEP = 8;
+  float4 v;
+  __device__ __forceinline__ void load(const float* row, int k, int h, int end, bool in) {
+    v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (in && k < end) v = *reinterpret_cast<const float4*>(row + k + 4 * h);
+  }
+  static __device__ __forceinline__ void multiply(float16v& acc, const Frag& a, const Frag& b) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v.x, b.v.x, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v.y, b.v.y, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v.z, b.v.z, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v.w, b.v.w, acc, 0, 0, 0);
+  }
+};
+template <typename T>
+__global__ __launch_bounds__(NTHR) void small_logits_kernel(CeArgs a, int keep) {
+  constexpr int STEP = Frag<T>::STEP, U = 4;
+  __shared__ float part[4][BLOCK_V][33];
+  __shared__ float sm[NTHR], sl[NTHR];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+  const long v0 = (long)blockIdx.x * BLOCK_V, n0 = (long)blockIdx.y * 32;
+  const long va = v0 + r < a.c.vocab ? v0 + r : a.c.vocab - 1, vb = v0 + 32 + r < a.c.vocab ? v0 + 32 + r : a.c.vocab - 1;
+  const T* wa = reinterpret_cast<const T*>(a.c.weight.p) + va * a.c.weight.row;
+  const T* wb = reinterpret_cast<const T*>(a.c.weight.p) + vb * a.c.weight.row;
+  const int t = target_of(a, n0 + r);
+  const T* x = reinterpret_cast<const T*>(a.c.x.p) + (t >= 0 ? n0 + r : 0) * a.c.x.row;
+  const int quarter = (a.c.width + 4 * STEP - 1) / (4 * STEP) * STEP;
+  const int k0 = wave * quarter, end = k0 + quarter < a.c.width ? k0 + quarter : a.c.width;
+  float16v acc0, acc1;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc0[i] = acc1[i] = 0.f;
+  for (int k = k0; k < end; k += U * STEP) {
+    Frag<T> fa[U], fb[U], fx[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      fa[u].load(wa, k + u * STEP, h, end, true);
+      fb[u].load(wb, k + u * STEP, h, end, true);
+      fx[u].load(x, k + u * STEP, h, end, t >= 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      Frag<T>::multiply(acc0, fa[u], fx[u]);
+      Frag<T>::multiply(acc1, fb[u], fx[u]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {                           // (the layout of a 32 x 32 result)
+    const int row = 8 * (i / 4) + 4 * h + i % 4;
+    part[wave][row][r] = acc0[i];
+    part[wave][32 + row][r] = acc1[i];
+  }
+  __syncthreads();
+  const int col = tid & 31, p8 = tid >> 5;
+  const long n = n0 + col;
+  const int tc = target_of(a, n);
+  if (blockIdx.x == 0 && p8 == 0 && n < a.p.np) a.p.target[n] = tc;
+  float v[BLOCK_V / 8];
+#pragma unroll
+  for (int j = 0; j < BLOCK_V / 8; ++j) {
+    const int row = p8 + 8 * j;
+    const float s = (part[0][row][col] + part[1][row][col]) + (part[2][row][col] + part[3][row][col]);
+    const bool in = v0 + row < a.c.vocab;
+    v[j] = in ? s * a.to_log2 : -INFINITY;
+    if (in && n < a.p.np) {
+      if (keep) a.p.logits[(v0 + row) * a.p.np + n] = s;
+      if (tc == v0 + row) a.p.target_logit[n] = v[j];
+    }
+  }
+  Running run = {-INFINITY, 0.f};
+  run.add(v);
+  run = meet<32>(run, sm, sl);
+  if (p8 == 0 && n < a.p.np) a.p.sums[(long)blockIdx.x * a.p.np + n] = log2_sum(run);
+}
+
 // all blocks of TB rows from n0 on by NT threads, and their losses
 template <int TB, int NT>
 __device__ __forceinline__ void row_losses(const CeArgs& a, long n0, float (&sm)[NT], float (&sl)[NT]) {
@@ -205,7 +307,10 @@ __global__ __launch_bounds__(1024) void few_loss_kernel(CeArgs a) {
   __shared__ float sm[1024], sl[1024];
   __shared__ double sum[1024];
   __shared__ int cnt[1024];
-  for (long n0 = 0; n0 < a.p.np; n0 += 8) row_losses<8>(a, n0, sm, sl);
+  if (a.p.np <= 32)
+    for (long n0 = 0; n0 < a.p.np; n0 += 8) row_losses<8>(a, n0, sm, sl);
+  else
+    for (long n0 = 0; n0 < a.p.np; n0 += 32) row_losses<32>(a, n0, sm, sl);
   __syncthreads();                                         // (the rows' losses, written above, are read below by other threads)
   whole_loss(a, sum, cnt);
 }
@@ -213,6 +318,11 @@ __global__ __launch_bounds__(1024) void few_loss_kernel(CeArgs a) {
 // dS of a piece: 8 rows of x a thread
 template <typename T>
 __global__ __launch_bounds__(NTHR) void grad_kernel(CeArgs a) {
+  if (blockIdx.x >= a.grad_blocks) {
+    const long n = (long)(blockIdx.x - a.grad_blocks) * 4 + (threadIdx.x >> 6);
+    if (n < a.p.np) copy_row<T>(a, n, threadIdx.x & 63, a.p.target[n] >= 0, nullptr);
+    return;
+  }
   const long per = a.p.np / 8, i = (long)blockIdx.x * NTHR + threadIdx.x;
   if (i >= per * a.nv) return;
   const long v = i / per, n = 8 * (i - v * per);
@@ -293,18 +403,19 @@ __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, 
 }
 
 // ---- sizes -----------------------------------------------------------------------------------------------------------
-constexpr long FEW_ROWS = 32;                              // rows whose losses and sum are one workgroup's
+constexpr long FEW_ROWS = 128;                             // rows whose losses and sum are one workgroup's
+// small_logits_kernel's share: a product of its own and a launch for the sums cost more than its plain loads do up to a million logits of
+// 512 channels.  Measured, us, the loss alone, this kernel / without: 64 rows against 16384 x 256 14.1 / 21.9, 1000 against 1000 x 256 13.4 /
+// 20.4, 8 against 50000 x 1024 32.6 / 34.3, 32 (fp32) 88 / 119; beyond the lines: 100 against 10000 x 1024 34.8 / 31.3.
+bool small_problem(const Parts& p, long vocab, int width) {
+  return !p.fused && p.pieces == 1 && (p.np <= 32 || (p.np * vocab <= (1l << 20) && width <= 512));
+}
 // A piece of the vocabulary takes 1 GB of logits, or of dS where the logits are not written (256 rows of the vocabulary: more, from 2^20 rows
 // of x on).
 constexpr size_t PIECE_BYTES = 1ul << 30;
 constexpr long PIECE_ROWS = 1l << 20;
 constexpr int MAX_SPLIT = 16;
 
-// Rows of x are filled up to whole tiles of 256 where that is an eighth more at most, else to 8.
-long padded(long rows) {
-  const long whole = (rows + 255) / 256 * 256;
-  return whole <= rows + rows / 8 ? whole : (rows + 7) / 8 * 8;
-}
 // Channels are filled up with zeros to a multiple of 32, and to one of 256 where that is an eighth more at most, for the sake of the
 // 256 x 256 kernel; the weights are copied for it, which takes as long as one of the four products with 500 rows of x.
 int padded_width(int width) {
@@ -318,6 +429,15 @@ long fused_rows(int dtype, long np, long vocab) {
   const long tiles = vocab / 256 * (np / 256);
   return gemm_fills_chip(tiles) && tiles < (1l << 28) ? vocab / 256 * 256 : 0;
 }
+// Rows of x are filled up with zeros to whole tiles of 256 where that is an eighth more at most, or three eighths and those epilogues then
+// take the logits, else to 8.  Measured, us, with gradients, tiles / 8: 600 rows (768) against 40000 x 256 134 / 191, 100000 x 1024 617 / 830; 200
+// (256) 84 / 101 and 298 / 346, against 40000 x 1024 161 / 154; beyond the line, 300 (512) against 40000 x 1024 229 / 192, 100 against 40000 x 1024
+// 153 / 123.
+long padded(int dtype, long rows, long vocab) {
+  const long whole = (rows + 255) / 256 * 256;
+  if (whole <= rows + rows / 8 || (whole <= rows + rows * 3 / 8 && fused_rows(dtype, whole, vocab))) return whole;
+  return (rows + 7) / 8 * 8;
+}
 // A product of few tiles and a long contraction (dx: over the vocabulary, dweight: over the rows of x) is shared out until there is a tile for
 // every compute unit.  rows, cols: of its result; wide: the 256 x 256 kernel would take it.
 int shares_of(int dtype, long rows, long cols, long k, bool wide) {
@@ -325,7 +445,7 @@ int shares_of(int dtype, long rows, long cols, long k, bool wide) {
   const long tiles = (rows + t - 1) / t * ((cols + t - 1) / t);
   if (gemm_fills_chip(tiles)) return 1;
   long n = 256 / tiles;
-  if (n > k / 512) n = k / 512;
+  if (n > k / 512) n = k / 512;                            // (256: 512 rows of x against 2000 x 1024 72 us, 59 with 512; 2048: 4096 against 8000 x 512 218, 210)
   return (int)(n < 1 ? 1 : n > MAX_SPLIT ? MAX_SPLIT : n);
 }
 int dx_split(int dtype, long np, int wp, long nv) {
@@ -355,7 +475,7 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   size_t off = 0;
   auto take = [&](size_t n) { char* q = base ? base + off : nullptr; off += (n + 255) / 256 * 256; return q; };
   const size_t es = dtype == 0 ? 4 : 2;
-  p.np = padded(rows);
+  p.np = padded(dtype, rows, vocab);
   p.fused = fused_rows(dtype, p.np, vocab);
   p.wp = p.fused ? padded_width(width) : width;
   const size_t row = (p.fused ? 2 : 4) * (p.np ? p.np : 1);
@@ -420,7 +540,8 @@ struct Run {
   hipStream_t s;
   CeArgs a;
   int shares = 0;
-  Run(const CrossEntropyArgs& c_, const Parts& p_, hipStream_t s_) : c(c_), p(p_), s(s_), a{} { a.c = c; a.p = p; a.to_log2 = c.scale * LOG2E; }
+  bool small;
+  Run(const CrossEntropyArgs& c_, const Parts& p_, hipStream_t s_) : c(c_), p(p_), s(s_), a{} { a.c = c; a.p = p; a.to_log2 = c.scale * LOG2E; small = small_problem(p, c.vocab, c.width); }
 
   // the weights' rows from v0 on as the products read them
   long weight_row() const { return p.weight ? p.wp : c.weight.row; }
@@ -459,7 +580,8 @@ struct Run {
     return hipGetLastError();
   }
   hipError_t softmax_grad() {
-    grad_kernel<T><<<(unsigned)((a.nv * (p.np / 8) + NTHR - 1) / NTHR), NTHR, 0, s>>>(a);
+    a.grad_blocks = (unsigned)((a.nv * (p.np / 8) + NTHR - 1) / NTHR);
+    grad_kernel<T><<<a.grad_blocks + (small ? (unsigned)((p.np + 3) / 4) : 0), NTHR, 0, s>>>(a);
     return hipGetLastError();
   }
   hipError_t fold() {
@@ -569,13 +691,18 @@ struct Run {
   }
   hipError_t all() {
     if (c.rows == 0) return without_rows();
-    rows_kernel<T><<<(unsigned)((p.np + 3) / 4), NTHR, 0, s>>>(a);
+    if (small) {
+      const dim3 grid((unsigned)((c.vocab + BLOCK_V - 1) / BLOCK_V), (unsigned)((p.np + 31) / 32));
+      small_logits_kernel<T><<<grid, NTHR, 0, s>>>(a, c.dx.p || c.dweight.p);
+    } else {
+      rows_kernel<T><<<(unsigned)((p.np + 3) / 4), NTHR, 0, s>>>(a);
+    }
     if (p.weight) {
       const long all = (c.vocab * (p.wp / 8) + NTHR - 1) / NTHR;
       weight_kernel<<<all < 65536 ? (unsigned)all : 65536u, NTHR, 0, s>>>(a);
     }
     CE_TRY(hipGetLastError());
-    CE_TRY(sums());
+    if (!small) CE_TRY(sums());
     if (p.np <= FEW_ROWS) {
       few_loss_kernel<<<1, 1024, 0, s>>>(a);
     } else {
