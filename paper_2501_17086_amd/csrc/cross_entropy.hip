@@ -456,18 +456,28 @@ int dweight_split(int dtype, long np, int width, long nv) {
   const bool wide = nv % 256 == 0 && width >= 256 && np % 32 == 0;
   return shares_of(dtype, nv, wide ? width / 256 * 256 : width, np, wide);
 }
-// Rows of the vocabulary whose dweight is a product of its own: whole tiles of 256 (the last ones would take all others to smaller tiles).
-long dweight_whole(int dtype, long np, int width, long nv) {
-  return dtype == 1 && width >= 256 && np % 32 == 0 && nv >= 512 ? nv / 256 * 256 : nv;
+// How many of the next nv rows of the vocabulary have their dweight in one product: whole tiles of 256 (rows behind them would take all others to
+// smaller tiles), and of those whole rounds of the compute units where little of another would be filled and a round is long.  Measured,
+// with all else, us, so / all tiles together: 8190 rows of x against 50021 x 1024 (780 tiles) 2754 / 2858, 8192 against 20000 x 1024 1159 / 1234, 4096
+// against 50000 x 1024 1445 / 1488; below the line 1024 against 70000 x 512 376 / 352.
+long dweight_rows_of(int dtype, long np, int width, long nv) {
+  if (dtype != 1 || width < 256 || np % 32 || nv < 256) return nv;
+  const long per = width / 256, tiles = nv / 256 * per, over = tiles % 256;
+  const long take = np >= 4096 && tiles > 256 && over > 0 && over * 100 < 256 * 35 ? (tiles - over) / per : nv / 256;
+  return take * 256;
 }
 size_t dweight_part(int dtype, long np, int width, long nv) {      // bytes of the shares of nv rows in one product
   const int n = dweight_split(dtype, np, width, nv);
   return n > 1 ? (size_t)n * nv * width * 4 : 0;
 }
-size_t dweight_room(int dtype, long np, int width, long nv) {      // ... and of those of a piece, the last rows apart
-  const long whole = dweight_whole(dtype, np, width, nv);
-  const size_t a = dweight_part(dtype, np, width, whole), b = whole < nv ? dweight_part(dtype, np, width, nv - whole) : 0;
-  return a > b ? a : b;
+size_t dweight_room(int dtype, long np, int width, long nv) {      // ... and of a piece's products, one after the other
+  size_t most = 0;
+  for (long n; nv > 0; nv -= n) {
+    n = dweight_rows_of(dtype, np, width, nv);
+    const size_t b = dweight_part(dtype, np, width, n);
+    most = b > most ? b : most;
+  }
+  return most;
 }
 
 Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradients) {
@@ -652,9 +662,11 @@ struct Run {
     return hipGetLastError();
   }
   hipError_t dweight(long v0, long nv) {
-    const long whole = dweight_whole(DTYPE, p.np, c.width, nv);
-    CE_TRY(dweight_rows(v0, 0, whole));
-    return whole < nv ? dweight_rows(v0, whole, nv - whole) : hipSuccess;
+    for (long r = 0, n; r < nv; r += n) {
+      n = dweight_rows_of(DTYPE, p.np, c.width, nv - r);
+      CE_TRY(dweight_rows(v0, r, n));
+    }
+    return hipSuccess;
   }
   hipError_t dx_rows(long v0, long r0, long nr, int split) {
     GemmArgs g = plain();
