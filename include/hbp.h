@@ -443,7 +443,7 @@ typedef struct {
 /* out := dropout(x), or residual + dropout(x) (residual NULL: none), rounded once.  Of x only elements that stay are seen: an infinity or a
  * NaN in another place leaves a zero.  The gradient with respect to x is the same call on the gradient of `out`, without a
  * residual.  out may be x or the residual themselves (same data and stride) and must not overlap them otherwise.  rows = 0 does
- * nothing.  At most 2^24 rows and 2^36 elements. */
+ * nothing.  At most 2^24 rows and 2^34 elements. */
 hbp_status hbp_dropout(const hbp_dropout_desc* dropout, int dtype, int64_t rows, int64_t width, const hbp_rows* x,
                        const hbp_rows* residual, const hbp_rows* out, void* stream);
 
@@ -454,7 +454,7 @@ typedef struct {
   int32_t dtype;             /* hbp_dtype of table, out, dout */
   int32_t grad_dtype;        /* hbp_dtype of dtable: HBP_F32, or dtype */
   float scale;               /* finite, as is its product with dropout's factor */
-  int64_t rows;              /* 0 .. 2^24 tokens, rows x width at most 2^36 */
+  int64_t rows;              /* 0 .. 2^24 tokens, rows x width at most 2^34 */
   int64_t vocab;             /* 1 .. 2^24 */
   int64_t width;
   hbp_dropout_desc dropout;  /* rate = 0: none (struct_size 0 will do) */

@@ -1,12 +1,20 @@
 // Softmax cross entropy of rows x against a vocabulary's weights W, and its gradients, in pieces of the vocabulary:
 //   s = scale x W^T,  loss_n = log sum_v exp s_nv - s_n,t,   dS = g (softmax(s) - onehot(t)),  dx = scale dS W,  dW = scale dS^T x.
 // A piece's logits are formed, their row sums taken and, for the gradients, turned into dS, which meets W and x; nothing of the size
-// rows x vocabulary is kept.  Where the vocabulary takes several pieces the logits are formed twice, once for the sums.
+// rows x vocabulary is kept.  Three forms, by sizes alone:
+//   many tiles  (bf16) the logits meet no memory: the 256 x 256 kernel's epilogues take sums of 128 rows of the vocabulary from its
+//               accumulators, and once more, when a row's sum is known, dS.  Four products of 2 rows x vocabulary x width where keeping the
+//               logits would leave three; what bounds it are the matrix cores: 16384 rows against 131072 x 2048 6.65 ms for the sums,
+//               7.2 dS, 6.2 dW, 6.6 dx, 26.9 in all, 1310 TFLOP/s over the four (a large product of the library: 1316).  With 256 channels
+//               a tile's exponentials and stores take as long as its products: 32768 rows against 16384 x 256 280, 360, 250, 230 us.
+//   pieces      logits in memory in fp32, at most 1 GB at a time; with one piece they are formed once.  fp32, and few rows.
+//   small       the same with logits and sums in one launch (small_logits_kernel): launches bound it, 3 to 6 us each.
 //
 // Logits lie [vocabulary][rows]: the vocabulary may have any size (it is the product's rows), the number of rows is filled up
-// with zeros to a multiple of 8, and both gradients' products find their contraction where the kernels want it.
+// with zeros to a multiple of 8 or 256, and both gradients' products find their contraction where the kernels want it.
 // Rows whose target is no token take no part: they are zeros in the copy of x that the products read, so that not even
-// an infinity or a NaN in them reaches the others.
+// an infinity or a NaN in them reaches the others.  Logits, sums, dx and dweight are held in fp32; dS is rounded to the storage type once, as the
+// matrix instructions want it, and dx gets back what that leaves out of the target's coefficient, the one that a confident row is made of.
 #include "hbp_common.h"
 
 namespace hbp {
@@ -158,6 +166,7 @@ __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
   r = meet<TB>(r, sm, sl);
   if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = log2_sum(r);
 }
+
 // Small problems: logits, a block's sums and the targets' logits in one launch, without x's copy.  A workgroup takes 64 rows of the vocabulary and
 // 32 of x, its wavefronts a quarter of the channels each, straight from memory into the layout of the matrix instructions, and
 // the quarters meet in LDS.  (8 rows against 16384 x 256: 16.0 -> 10.7 us.)
@@ -410,8 +419,9 @@ constexpr long FEW_ROWS = 128;                             // rows whose losses 
 bool small_problem(const Parts& p, long vocab, int width) {
   return !p.fused && p.pieces == 1 && (p.np <= 32 || (p.np * vocab <= (1l << 20) && width <= 512));
 }
-// A piece of the vocabulary takes 1 GB of logits, or of dS where the logits are not written (256 rows of the vocabulary: more, from 2^20 rows
-// of x on).
+// A piece of the vocabulary takes 1 GB of logits, or of dS where the logits are not written.  Measured, us, with gradients, 1 GB / 512 / 256 / 128
+// MB: 32768 rows against 16384 x 256 1220 / 1450 / 1655 / 1889 (with its embedding), 8190 against 50021 x 1024 2818 / 2894 / 2985 / 3231, 16384 against
+// 131072 x 2048 26830 / 27266 / 27659 / 29512: smaller pieces stay in the caches, but dx meets memory once a piece and launches end more often.
 constexpr size_t PIECE_BYTES = 1ul << 30;
 constexpr long PIECE_ROWS = 1l << 20;
 constexpr int MAX_SPLIT = 16;
@@ -445,7 +455,8 @@ int shares_of(int dtype, long rows, long cols, long k, bool wide) {
   const long tiles = (rows + t - 1) / t * ((cols + t - 1) / t);
   if (gemm_fills_chip(tiles)) return 1;
   long n = 256 / tiles;
-  if (n > k / 512) n = k / 512;                            // (256: 512 rows of x against 2000 x 1024 72 us, 59 with 512; 2048: 4096 against 8000 x 512 218, 210)
+  // (at least 512 of the contraction: 512 rows of x against 2000 x 1024 59 us, with 256 72; 4096 against 8000 x 512 210, with 2048 218)
+  if (n > k / 512) n = k / 512;
   return (int)(n < 1 ? 1 : n > MAX_SPLIT ? MAX_SPLIT : n);
 }
 int dx_split(int dtype, long np, int wp, long nv) {
@@ -551,7 +562,11 @@ struct Run {
   CeArgs a;
   int shares = 0;
   bool small;
-  Run(const CrossEntropyArgs& c_, const Parts& p_, hipStream_t s_) : c(c_), p(p_), s(s_), a{} { a.c = c; a.p = p; a.to_log2 = c.scale * LOG2E; small = small_problem(p, c.vocab, c.width); }
+  Run(const CrossEntropyArgs& c_, const Parts& p_, hipStream_t s_) : c(c_), p(p_), s(s_), a{}, small(small_problem(p_, c_.vocab, c_.width)) {
+    a.c = c;
+    a.p = p;
+    a.to_log2 = c.scale * LOG2E;
+  }
 
   // the weights' rows from v0 on as the products read them
   long weight_row() const { return p.weight ? p.wp : c.weight.row; }

@@ -839,11 +839,14 @@ bool launch_gemm_mfma(const GemmArgs& g, hipStream_t s, hipError_t* err) {
   return true;
 }
 
-bool gemm_vocab_ok(const GemmArgs& g) {
+namespace {
+bool vocab_ok(const GemmArgs& g) {
   return g.M % BM == 0 && g.N % BN == 0 && g.K % BK == 0 && g.K >= 4 * BK && g.a_sm % 8 == 0 && g.b_sn % 8 == 0 &&
          g.a_sm <= (1L << 22) && g.b_sn <= (1L << 22) && g.M / BM * (g.N / BN) < (1L << 28);
 }
+}  // namespace
 hipError_t launch_gemm_vocab(const GemmArgs& g, hipStream_t s) {
+  if (!vocab_ok(g)) return hipErrorInvalidValue;
   const bool pair = g.K % (2 * BK) == 0;
   if (g.mode == EPI_VOCAB_SUMS)
     return pair ? launch_lean_walk<true, true, FAST_VOCAB_SUMS, false, true>(g, s) : launch_lean_walk<true, true, FAST_VOCAB_SUMS, false, false>(g, s);

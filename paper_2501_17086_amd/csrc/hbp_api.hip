@@ -1683,7 +1683,7 @@ hbp_status check_embedding(const hbp_embedding_desc* d, DropoutKey* key) {
   if (d->grad_dtype != HBP_F32 && d->grad_dtype != d->dtype) return HBP_E_INVALID_ARG;
   if (!std::isfinite(d->scale) || d->rows < 0 || d->vocab < 1) return HBP_E_INVALID_ARG;
   HBP_RUN(check_width(d->width));
-  if (d->rows > (1 << 24) || d->vocab > (1 << 24) || d->rows * d->width > (int64_t)1 << 36) return HBP_E_UNSUPPORTED;
+  if (d->rows > (1 << 24) || d->vocab > (1 << 24) || d->rows * d->width > (int64_t)1 << 34) return HBP_E_UNSUPPORTED;
   HBP_RUN(check_dropout(&d->dropout, true, d->scale, key));
   return std::isfinite(key->factor) ? HBP_OK : HBP_E_INVALID_ARG;
 }
@@ -1735,7 +1735,7 @@ hbp_status hbp_dropout(const hbp_dropout_desc* dropout, int dtype, int64_t rows,
   HBP_RUN(check_dropout(dropout, false, 1.f, &key));
   if (rows < 0) return HBP_E_INVALID_ARG;
   HBP_RUN(check_width(width));
-  if (rows > (1 << 24) || rows * width > (int64_t)1 << 36) return HBP_E_UNSUPPORTED;
+  if (rows > (1 << 24) || rows * width > (int64_t)1 << 34) return HBP_E_UNSUPPORTED;
   HBP_RUN(check_rows(*x, rows, width, false));
   if (residual) HBP_RUN(check_rows(*residual, rows, width, false));
   HBP_RUN(check_rows(*out, rows, width, true));

@@ -210,8 +210,7 @@ hipError_t launch_gemm_f32_group(const GemmArgs* g, int n, hipStream_t s);
 hipError_t launch_gemm_tile_group(const GemmArgs* g, int n, int tm, int tn, hipStream_t s);
 // fast bf16 MFMA path; returns false when the shape/layout is not covered
 bool launch_gemm_mfma(const GemmArgs& g, hipStream_t s, hipError_t* err);
-// Both operands K-contiguous, whole tiles of the 256 x 256 kernel, a mode EPI_VOCAB_...: does it take them?
-bool gemm_vocab_ok(const GemmArgs& g);
+// A mode EPI_VOCAB_..., both operands K-contiguous, M and N multiples of 256, K one of 32 and at least 128 (hipErrorInvalidValue: not so)
 hipError_t launch_gemm_vocab(const GemmArgs& g, hipStream_t s);
 // the same contractions on tiles of 128 x 128, 64 x 64, 64 x 32 or 32 x 32, any size (called through launch_gemm_mfma, which
 // checks the layout)

@@ -34,7 +34,7 @@ def call_dropout(n=0, width=64, dtype=B.BF16, x=None, residual=None, out=None, *
     (dict(), OK), (dict(struct_size=8), INVALID), (dict(rate=1.0), INVALID), (dict(rate=-0.1), INVALID), (dict(rate=math.nan), INVALID),
     (dict(rate=0.999999), INVALID), (dict(rate=0.99999), OK), (dict(rate=0.0), OK), (dict(counter=A + 4), UNSUPPORTED), (dict(dtype=2), INVALID),
     (dict(n=-1), INVALID), (dict(width=0), INVALID), (dict(width=-8), INVALID), (dict(width=60), UNSUPPORTED), (dict(width=65544), UNSUPPORTED),
-    (dict(n=(1 << 24) + 1), UNSUPPORTED), (dict(n=1 << 24, width=8192), UNSUPPORTED), (dict(n=1, x=rows(0)), NULL), (dict(n=1, out=rows(0)), NULL),
+    (dict(n=(1 << 24) + 1), UNSUPPORTED), (dict(n=1 << 24, width=1032), UNSUPPORTED), (dict(n=1, x=rows(0)), NULL), (dict(n=1, out=rows(0)), NULL),
     (dict(n=1, x=rows(A + 2)), UNSUPPORTED), (dict(n=2, x=rows(stride=-8)), INVALID), (dict(n=2, x=rows(stride=65)), UNSUPPORTED),
     (dict(n=2, x=rows(stride=(1 << 22) + 8)), UNSUPPORTED), (dict(n=2, out=rows(stride=56)), INVALID), (dict(n=2, out=rows(stride=0)), INVALID),
     (dict(n=2, x=rows(A, 128), out=rows(A, 64)), INVALID), (dict(n=2, residual=rows(A, 128), out=rows(A, 64)), INVALID),
@@ -67,7 +67,7 @@ def emb_desc(**kw):
     (dict(), OK), (dict(struct_size=8), INVALID), (dict(dtype=2), INVALID), (dict(grad_dtype=2), INVALID), (dict(grad_dtype=B.BF16), OK),
     (dict(dtype=B.F32, grad_dtype=B.BF16), INVALID), (dict(scale=math.inf), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=-2.0), OK),
     (dict(scale=0.0), OK), (dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(width=0), INVALID), (dict(width=12), UNSUPPORTED),
-    (dict(rows=(1 << 24) + 1), UNSUPPORTED), (dict(vocab=(1 << 24) + 1), UNSUPPORTED), (dict(rows=1 << 24, width=8192), UNSUPPORTED),
+    (dict(rows=(1 << 24) + 1), UNSUPPORTED), (dict(vocab=(1 << 24) + 1), UNSUPPORTED), (dict(rows=1 << 24, width=1024), OK), (dict(rows=1 << 24, width=1032), UNSUPPORTED),
     (dict(dropout=drop_desc()), OK), (dict(dropout=drop_desc(rate=1.5)), INVALID), (dict(dropout=drop_desc(struct_size=0)), INVALID),
     (dict(dropout=drop_desc(struct_size=0, rate=0.0)), OK), (dict(scale=3e38, dropout=drop_desc(rate=0.9)), INVALID),
 ])
