@@ -190,26 +190,11 @@ __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
   __shared__ unsigned cnt[4][SORT_D];                      // a wavefront's keys with each digit, then where they go
   __shared__ unsigned sums[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int d = tid; d < 4 * SORT_D; d += NTHR) (&cnt[0][0])[d] = 0;
-  __syncthreads();
   const long base = (long)blockIdx.x * SORT_E + wave * (64 * SORT_PER) + lane;
   unsigned key[SORT_PER], rank[SORT_PER];
-  const int bits = 32 - __clz(a.mask);
 #pragma unroll
-  for (int k = 0; k < SORT_PER; ++k) {
-    const long i = base + 64 * k;
-    const bool in = i < a.n;
-    key[k] = in ? load_key(a, i) : 0u;
-    const unsigned d = (key[k] >> a.shift) & a.mask;
-    const unsigned long peers = same_digit(d, bits, in);
-    const unsigned before = __popcll(peers & ((1ul << lane) - 1ul));
-    rank[k] = in ? cnt[wave][d] + before : 0u;
-    __builtin_amdgcn_wave_barrier();                       // (a wavefront's LDS operations execute in order)
-    if (in && before == 0) cnt[wave][d] += __popcll(peers);
-    __builtin_amdgcn_wave_barrier();
-  }
-  __syncthreads();
-  // where the first key of each digit and wavefront goes: two digits a thread
+  for (int k = 0; k < SORT_PER; ++k) key[k] = base + 64 * k < a.n ? load_key(a, base + 64 * k) : 0u;
+  // where the first key of each digit goes, two digits a thread (asked for before the keys are looked at)
   const unsigned d0 = 2 * tid;
   unsigned total[2], before[2];
 #pragma unroll
@@ -233,6 +218,21 @@ __global__ __launch_bounds__(NTHR) void place_kernel(SortArgs a) {
       }
     }
   }
+  for (int d = tid; d < 4 * SORT_D; d += NTHR) (&cnt[0][0])[d] = 0;
+  __syncthreads();
+  const int bits = 32 - __clz(a.mask);
+#pragma unroll
+  for (int k = 0; k < SORT_PER; ++k) {
+    const bool in = base + 64 * k < a.n;
+    const unsigned d = (key[k] >> a.shift) & a.mask;
+    const unsigned long peers = same_digit(d, bits, in);
+    const unsigned before = __popcll(peers & ((1ul << lane) - 1ul));
+    rank[k] = in ? cnt[wave][d] + before : 0u;
+    __builtin_amdgcn_wave_barrier();                       // (a wavefront's LDS operations execute in order)
+    if (in && before == 0) cnt[wave][d] += __popcll(peers);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
   unsigned pair = total[0] + total[1], scan = pair;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {

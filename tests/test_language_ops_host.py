@@ -14,6 +14,13 @@ OK, INVALID, UNSUPPORTED, WORKSPACE, NULL = 0, 1, 2, 3, 4
 A = 1 << 20            # a place for tensors that nothing reads
 
 
+def test_struct_layout_matches_header():
+    # field order and sizes as in the header (LP64)
+    assert C.sizeof(B.hbp_rows) == 16 and C.sizeof(B.hbp_dropout_desc) == 8 + 8 * 3
+    assert C.sizeof(B.hbp_embedding_desc) == 4 * 4 + 8 * 3 + 32 and C.sizeof(B.hbp_embedding_buffers) == 8 + 8 + 16 * 4 + 8 * 2
+    assert C.sizeof(B.hbp_cross_entropy_desc) == 4 * 6 + 8 * 3 and C.sizeof(B.hbp_cross_entropy_buffers) == 8 + 16 * 2 + 8 * 3 + 16 * 2 + 8 * 2
+
+
 def rows(data=A, stride=1024):
     return B.hbp_rows(data, stride)
 
