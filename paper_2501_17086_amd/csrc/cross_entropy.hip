@@ -302,9 +302,10 @@ __device__ __forceinline__ void whole_loss(const CeArgs& a, double (&sum)[1024],
     a.p.scalars[0] = (float)(f * a.c.scale);
   }
 }
+template <int TB>
 __global__ __launch_bounds__(NTHR) void row_loss_kernel(CeArgs a) {
   __shared__ float sm[NTHR], sl[NTHR];
-  row_losses<32>(a, 32l * blockIdx.x, sm, sl);
+  row_losses<TB>(a, (long)TB * blockIdx.x, sm, sl);
 }
 __global__ __launch_bounds__(1024) void loss_kernel(CeArgs a) {
   __shared__ double sum[1024];
@@ -326,15 +327,17 @@ __global__ __launch_bounds__(1024) void few_loss_kernel(CeArgs a) {
 
 // dS of a piece: 8 rows of x a thread
 template <typename T>
-__global__ __launch_bounds__(NTHR) void grad_kernel(CeArgs a) {
+__global__ __launch_bounds__(NTHR) void grad_kernel(CeArgs a, Divisor by_row) {
   if (blockIdx.x >= a.grad_blocks) {
     const long n = (long)(blockIdx.x - a.grad_blocks) * 4 + (threadIdx.x >> 6);
     if (n < a.p.np) copy_row<T>(a, n, threadIdx.x & 63, a.p.target[n] >= 0, nullptr);
     return;
   }
-  const long per = a.p.np / 8, i = (long)blockIdx.x * NTHR + threadIdx.x;
-  if (i >= per * a.nv) return;
-  const long v = i / per, n = 8 * (i - v * per);
+  const unsigned per = (unsigned)(a.p.np / 8);
+  const long base = (long)blockIdx.x * NTHR, row0 = base / per;
+  const unsigned r = (unsigned)(base - row0 * per) + threadIdx.x, q = by_row.quotient(r);
+  const long v = row0 + q, n = 8l * (r - q * per);
+  if (v >= a.nv) return;
   float s[8], lse[8];
   load8(a.p.logits + v * a.p.np + n, s);
   load8(a.p.lse + n, lse);
@@ -373,6 +376,7 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
   const long c = 8l * (r - q * per);
   float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (a.p.target[n] >= 0) {
+#pragma unroll 4
     for (int k = 0; k < shares; ++k) {
       float v[8];
       load8(a.p.dx + ((long)k * a.p.np + n) * a.p.wp + c, v);
@@ -391,18 +395,21 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
 }
 // rows of dweight from their shares, n8 elements of 8
 template <typename O>
-__global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out, long row, long n8, int shares, unsigned per) {
-  const long i = (long)blockIdx.x * NTHR + threadIdx.x;
+__global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out, long row, long n8, int shares, Divisor by_row) {
+  const unsigned per = by_row.d;
+  const long base = (long)blockIdx.x * NTHR, i = base + threadIdx.x, row0 = base / per;
   if (i >= n8) return;
+  const unsigned r = (unsigned)(base - row0 * per) + threadIdx.x, q = by_row.quotient(r);
   float s[8];
   load8(part + 8 * i, s);
+#pragma unroll 4
   for (int k = 1; k < shares; ++k) {
     float v[8];
     load8(part + 8 * (k * n8 + i), v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] += v[j];
   }
-  store8(out + i / per * row + 8 * (i % per), s);
+  store8(out + (row0 + q) * row + 8l * (r - q * per), s);
 }
 template <typename T>
 __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, int width) {
@@ -412,7 +419,9 @@ __global__ __launch_bounds__(NTHR) void clear_kernel(T* p, long row, long rows, 
 }
 
 // ---- sizes -----------------------------------------------------------------------------------------------------------
-constexpr long FEW_ROWS = 128;                             // rows whose losses and sum are one workgroup's
+// Rows and blocks whose losses and their sum are one workgroup's (8 rows of 782 blocks 5.7 us; 104 of 625 took it 16.6, with a workgroup for 8 rows
+// and another for the sum 8).
+constexpr long FEW_ROWS = 128, FEW_SUMS = 8192;
 // small_logits_kernel's share: a product of its own and a launch for the sums cost more than its plain loads do up to a million logits of
 // 512 channels.  Measured, us, the loss alone, this kernel / without: 64 rows against 16384 x 256 14.1 / 21.9, 1000 against 1000 x 256 13.4 /
 // 20.4, 8 against 50000 x 1024 32.6 / 34.3, 32 (fp32) 88 / 119; beyond the lines: 100 against 10000 x 1024 34.8 / 31.3.
@@ -459,20 +468,28 @@ int shares_of(int dtype, long rows, long cols, long k, bool wide) {
   if (n > k / 512) n = k / 512;
   return (int)(n < 1 ? 1 : n > MAX_SPLIT ? MAX_SPLIT : n);
 }
-int dx_split(int dtype, long np, int wp, long nv) {
-  const bool wide = np % 256 == 0 && wp >= 256;
-  return shares_of(dtype, np, wide ? wp / 256 * 256 : wp, nv, wide);
+// Does the 256 x 256 kernel take whole tiles of such a product, in shares where it needs them?  (Else nothing is gained by keeping its
+// rows, columns or contraction apart from the rest.)
+bool wide(long rows, long cols, long k) {
+  const long tiles = rows / 256 * (cols / 256);
+  return tiles > 0 && gemm_fills_chip(tiles * shares_of(1, rows, cols / 256 * 256, k, true));
 }
+bool dx_wide(int dtype, long np, int wp, long nv) { return dtype == 1 && np % 256 == 0 && wide(np, wp, nv); }
+int dx_split(int dtype, long np, int wp, long nv) {
+  const bool w = dx_wide(dtype, np, wp, nv);
+  return shares_of(dtype, np, w ? wp / 256 * 256 : wp, nv, w);
+}
+bool dweight_wide(int dtype, long np, int width, long nv) { return dtype == 1 && np % 32 == 0 && nv % 256 == 0 && wide(nv, width, np); }
 int dweight_split(int dtype, long np, int width, long nv) {
-  const bool wide = nv % 256 == 0 && width >= 256 && np % 32 == 0;
-  return shares_of(dtype, nv, wide ? width / 256 * 256 : width, np, wide);
+  const bool w = dweight_wide(dtype, np, width, nv);
+  return shares_of(dtype, nv, w ? width / 256 * 256 : width, np, w);
 }
 // How many of the next nv rows of the vocabulary have their dweight in one product: whole tiles of 256 (rows behind them would take all others to
 // smaller tiles), and of those whole rounds of the compute units where little of another would be filled and a round is long.  Measured,
 // with all else, us, so / all tiles together: 8190 rows of x against 50021 x 1024 (780 tiles) 2754 / 2858, 8192 against 20000 x 1024 1159 / 1234, 4096
 // against 50000 x 1024 1445 / 1488; below the line 1024 against 70000 x 512 376 / 352.
 long dweight_rows_of(int dtype, long np, int width, long nv) {
-  if (dtype != 1 || width < 256 || np % 32 || nv < 256) return nv;
+  if (!dweight_wide(dtype, np, width, nv / 256 * 256)) return nv;
   const long per = width / 256, tiles = nv / 256 * per, over = tiles % 256;
   const long take = np >= 4096 && tiles > 256 && over > 0 && over * 100 < 256 * 35 ? (tiles - over) / per : nv / 256;
   return take * 256;
@@ -521,10 +538,14 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.grad = p.logits;
   if (gradients) {
     if (dtype == 1) p.grad = take((size_t)p.piece * p.np * 2);
-    p.split = dx_split(dtype, p.np ? p.np : 8, p.wp, p.piece);
+    const long last_piece = vocab - (p.pieces - 1) * p.piece;
+    for (const long nv : {p.piece, p.piece / 32 * 32, last_piece, last_piece / 32 * 32}) {
+      const int n = nv ? dx_split(dtype, p.np ? p.np : 8, p.wp, nv) : 1;
+      p.split = n > p.split ? n : p.split;
+    }
     p.shares = p.split + 2 < 4 ? 4 : p.split + 2;
     p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * p.wp * 4));
-    const size_t most = dweight_room(dtype, p.np, width, p.piece), last = dweight_room(dtype, p.np, width, vocab - (p.pieces - 1) * p.piece);
+    const size_t most = dweight_room(dtype, p.np, width, p.piece), last = dweight_room(dtype, p.np, width, last_piece);
     p.dweight_bytes = most > last ? most : last;
     p.dweight = reinterpret_cast<float*>(take(p.dweight_bytes));
   }
@@ -580,8 +601,8 @@ struct Run {
     return g;
   }
   // a product whose columns are the channels: whole tiles of 256 of them apart from the rest, on the 256 x 256 kernel
-  hipError_t by_columns(GemmArgs g, bool wide) const {
-    const long whole = DTYPE == 1 && wide ? g.N / 256 * 256 : 0, rest = g.N - whole;
+  hipError_t by_columns(GemmArgs g, bool apart) const {
+    const long whole = apart ? g.N / 256 * 256 : 0, rest = g.N - whole;
     if (whole == 0 || rest == 0) return product(DTYPE, g, s);
     g.N = whole;
     CE_TRY(product(DTYPE, g, s));
@@ -606,7 +627,7 @@ struct Run {
   }
   hipError_t softmax_grad() {
     a.grad_blocks = (unsigned)((a.nv * (p.np / 8) + NTHR - 1) / NTHR);
-    grad_kernel<T><<<a.grad_blocks + (small ? (unsigned)((p.np + 3) / 4) : 0), NTHR, 0, s>>>(a);
+    grad_kernel<T><<<a.grad_blocks + (small ? (unsigned)((p.np + 3) / 4) : 0), NTHR, 0, s>>>(a, Divisor((unsigned)(p.np / 8)));
     return hipGetLastError();
   }
   hipError_t fold() {
@@ -665,13 +686,14 @@ struct Run {
       g.c_is_f32 = c.grad_dtype == 0;
       if (g.c_is_f32) g.C = f; else g.C = b;
       g.ldc = c.dweight.row;
-      return by_columns(g, nr % 256 == 0);
+      return by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr));
     }
     if (dweight_part(DTYPE, p.np, c.width, nr) > p.dweight_bytes) return hipErrorInvalidValue;
     g.c_is_f32 = 1; g.C = p.dweight; g.ldc = c.width; g.c_sb = nr * c.width; g.split_k = n;
-    CE_TRY(by_columns(g, nr % 256 == 0));
+    CE_TRY(by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr)));
     const long n8 = nr * c.width / 8;
-    const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR), per = (unsigned)(c.width / 8);
+    const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR);
+    const Divisor per((unsigned)(c.width / 8));
     if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per);
     else dweight_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(p.dweight, b, c.dweight.row, n8, n, per);
     return hipGetLastError();
@@ -694,12 +716,12 @@ struct Run {
     g.split_k = split;
     shares += split;
     g.M = p.np; g.N = p.wp; g.K = nr;
-    return by_columns(g, p.np % 256 == 0);
+    return by_columns(g, dx_wide(DTYPE, p.np, p.wp, nr));
   }
   // (a contraction that is no multiple of 32 keeps the 256 x 256 kernel from all of it)
   hipError_t dx(long v0, long nv) {
     const long whole = nv / 32 * 32;
-    if (DTYPE == 1 && whole < nv && whole > 0 && p.np % 256 == 0) {
+    if (whole < nv && dx_wide(DTYPE, p.np, p.wp, whole)) {
       CE_TRY(dx_rows(v0, 0, whole, dx_split(DTYPE, p.np, p.wp, whole)));
       return dx_rows(v0, whole, nv - whole, 1);
     }
@@ -730,10 +752,11 @@ struct Run {
     }
     CE_TRY(hipGetLastError());
     if (!small) CE_TRY(sums());
-    if (p.np <= FEW_ROWS) {
+    if (p.np <= FEW_ROWS && p.np * p.blocks <= FEW_SUMS) {
       few_loss_kernel<<<1, 1024, 0, s>>>(a);
     } else {
-      row_loss_kernel<<<(unsigned)((p.np + 31) / 32), NTHR, 0, s>>>(a);
+      if (p.np <= 2048) row_loss_kernel<8><<<(unsigned)(p.np / 8), NTHR, 0, s>>>(a);
+      else row_loss_kernel<32><<<(unsigned)((p.np + 31) / 32), NTHR, 0, s>>>(a);
       loss_kernel<<<1, 1024, 0, s>>>(a);
     }
     CE_TRY(hipGetLastError());
