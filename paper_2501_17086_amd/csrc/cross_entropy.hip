@@ -14,7 +14,8 @@
 // with zeros to a multiple of 8 or 256, and both gradients' products find their contraction where the kernels want it.
 // Rows whose target is no token take no part: they are zeros in the copy of x that the products read, so that not even
 // an infinity or a NaN in them reaches the others.  Logits, sums, dx and dweight are held in fp32; dS is rounded to the storage type once, as the
-// matrix instructions want it, and dx gets back what that leaves out of the target's coefficient, the one that a confident row is made of.
+// matrix instructions want it, with a power of two as its factor (the rest of the factor comes after the products), and dx gets back what
+// that leaves out of the target's coefficient, the one that a confident row is made of.
 #include "hbp_common.h"
 
 namespace hbp {
@@ -34,7 +35,7 @@ struct Parts {
   int* target;            // [np], -1 where a row does not count
   float* rows;            // [np] row losses
   float* at_target;       // [np] the target's softmax less 1
-  float* scalars;         // [4]: the factor on dS
+  float* scalars;         // [2]: the factor on dS, and what dx and dweight are multiplied by afterwards
   float* sums;            // [blocks][np]: base 2 logarithms of a block's sums
   float* logits;          // [piece][np]
   void* grad;             // [piece][np], storage type (fp32: the logits' place)
@@ -51,6 +52,7 @@ struct CeArgs {
   CrossEntropyArgs c;
   Parts p;
   float to_log2;          // scale log2 e
+  int power;              // bf16: dS has a power of two as its factor, the rest of it comes after the products
   long v0, nv;            // the rows of the vocabulary at hand
   long block0;            // their first block of sums
   long grad0;             // where their dS begins in its piece
@@ -299,7 +301,13 @@ __device__ __forceinline__ void whole_loss(const CeArgs& a, double (&sum)[1024],
   if (tid == 0) {
     const double f = (double)a.c.factor / (a.c.mean && cnt[0] > 1 ? cnt[0] : 1);
     a.c.loss[0] = (float)(sum[0] * f);
-    a.p.scalars[0] = (float)(f * a.c.scale);
+    // Most targets' coefficients are next to minus the factor, so that its own rounding would be all of theirs: up to 2^-8 of dweight.
+    const double g = f * a.c.scale;
+    int e = 0;
+    const double m = frexp(g, &e);
+    const bool apart = a.power && g != 0.0 && e > -100 && e < 100;
+    a.p.scalars[0] = (float)(apart ? ldexp(1.0, e - 1) : g);
+    a.p.scalars[1] = apart ? (float)(2.0 * m) : 1.f;
   }
 }
 template <int TB>
@@ -407,13 +415,16 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
       load8(reinterpret_cast<const T*>(a.c.weight.p) + (long)a.p.target[n] * a.c.weight.row + c, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = fmaf(rest, w[j], s[j]);
+      const float f = a.p.scalars[1];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] *= f;
     }
   }
   store8(reinterpret_cast<T*>(a.c.dx.p) + n * a.c.dx.row + c, s);
 }
 // rows of dweight from their shares, n8 elements of 8
 template <typename O>
-__global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out, long row, long n8, int shares, Divisor by_row) {
+__global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out, long row, long n8, int shares, Divisor by_row, const float* scale) {
   const unsigned per = by_row.d;
   const long base = (long)blockIdx.x * NTHR, i = base + threadIdx.x, row0 = base / per;
   if (i >= n8) return;
@@ -427,6 +438,9 @@ __global__ __launch_bounds__(NTHR) void dweight_kernel(const float* part, O* out
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] += v[j];
   }
+  const float f = *scale;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s[j] *= f;
   store8(out + (row0 + q) * row + 8l * (r - q * per), s);
 }
 template <typename T>
@@ -575,6 +589,7 @@ hipError_t product(int dtype, const GemmArgs& g, hipStream_t s) {
   if (dtype == 1) {
     hipError_t e;
     if (launch_gemm_mfma(g, s, &e)) return e;
+    if (g.scale) return hipErrorInvalidValue;
   } else if (gemm_f32_ok(g)) {
     return launch_gemm_f32(g, s);
   }
@@ -605,6 +620,7 @@ struct Run {
     a.c = c;
     a.p = p;
     a.to_log2 = c.scale * LOG2E;
+    a.power = DTYPE == 1;
   }
 
   // the weights' rows from v0 on as the products read them
@@ -707,6 +723,7 @@ struct Run {
       g.c_is_f32 = c.grad_dtype == 0;
       if (g.c_is_f32) g.C = f; else g.C = b;
       g.ldc = c.dweight.row;
+      g.scale = DTYPE == 1 ? p.scalars + 1 : nullptr;
       return by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr));
     }
     if (dweight_part(DTYPE, p.np, c.width, nr) > p.dweight_bytes) return hipErrorInvalidValue;
@@ -715,8 +732,8 @@ struct Run {
     const long n8 = nr * c.width / 8;
     const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR);
     const Divisor per((unsigned)(c.width / 8));
-    if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per);
-    else dweight_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(p.dweight, b, c.dweight.row, n8, n, per);
+    if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per, p.scalars + 1);
+    else dweight_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(p.dweight, b, c.dweight.row, n8, n, per, p.scalars + 1);
     return hipGetLastError();
   }
   hipError_t dweight(long v0, long nv) {

@@ -194,7 +194,9 @@ enum FastEpi {
   FAST_RESID = 6,      // C(bf16) = acc + lambda[n] * aux   (forward: x_{l+1}; lambda NULL = 1)
   FAST_ACT_GELU = 7,   // C(bf16) = gelu(acc), out2(bf16) = gelu'(acc)   (forward: z and act')
   FAST_VOCAB_SUMS = 8, // sums over 128 rows (EPI_VOCAB_SUMS)
-  FAST_VOCAB_GRAD = 9  // C(bf16) = gain (2^(alpha acc - lse[n]) - onehot)
+  FAST_VOCAB_GRAD = 9, // C(bf16) = gain (2^(alpha acc - lse[n]) - onehot)
+  FAST_SCALED = 10,    // C(bf16) = *scale acc
+  FAST_SCALED_F32 = 11 // C(fp32) = *scale acc
 };
 
 // What a vocabulary's logits are formed for (cross_entropy.hip); rows are the vocabulary's, columns those of x.  Measured, M x N x K: sums
@@ -229,10 +231,12 @@ __device__ __forceinline__ void epilogue_sums(const GemmArgs& g, const TileCoord
 }
 
 // Straight-line epilogue from the registers for a tile fully inside the matrix (fp32 output).
+template <bool SCALED>
 __device__ __forceinline__ void epilogue_f32(const GemmArgs& g, const TileCoord& tc, const float16v (&acc)[4][2], int wm0, int wn0,
                                              int lane) {
   const long cb = g.split_k > 1 ? ((long)tc.split * g.batch + tc.batch) * g.c_sb : tc.batch * g.c_sb;
   float* c = reinterpret_cast<float*>(g.C) + cb + (tc.m0 + wm0 + (lane & 31)) * g.ldc + tc.n0 + wn0 + 4 * (lane >> 5);
+  const float f = SCALED ? *g.scale : 1.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -240,7 +244,8 @@ __device__ __forceinline__ void epilogue_f32(const GemmArgs& g, const TileCoord&
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<float4*>(c + (long)(32 * i) * g.ldc + 32 * j + 8 * q) =
-            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            SCALED ? make_float4(acc[i][j][4 * q] * f, acc[i][j][4 * q + 1] * f, acc[i][j][4 * q + 2] * f, acc[i][j][4 * q + 3] * f)
+                   : make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
 }
 
 // The lean form of the kernel, for launches in which every tile lies inside the
@@ -311,6 +316,7 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
   // FAST_VOCAB_GRAD: the columns' logarithms, in the MFMA layout as well, and lane c's column's target
   constexpr bool VOCAB = FAST == FAST_VOCAB_GRAD;
   float lse[8][4];
+  const float scale = FAST == FAST_SCALED ? *g.scale : 1.f;
   float gain = 0.f, at_target = 0.f;
   int target = 0;
   if (VOCAB) {
@@ -381,6 +387,10 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
 #pragma unroll
           for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_exp2f(fmaf(v[x], g.vocab.alpha, -lse[4 * j + qd][x])) * gain;
         }
+        if (FAST == FAST_SCALED) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] *= scale;
+        }
         if (TWO_OUT) {
           float dz[4];
 #pragma unroll
@@ -414,9 +424,8 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
   round(std::integral_constant<int, 3>(), qd);
 }
 template <int FAST> struct StagedOps {   // vector-memory operations per wave of one epilogue (a lower bound: the
-  static constexpr int value = FAST == FAST_VOCAB_SUMS ? 2 : FAST == FAST_STORE || FAST == FAST_VOCAB_GRAD ? 16 : 32;   // waits stay safe
-                                                                                              // with more)
-};
+  static constexpr int value = FAST == FAST_VOCAB_SUMS ? 2 : FAST == FAST_STORE || FAST == FAST_SCALED || FAST == FAST_VOCAB_GRAD ? 16 : 32;
+};                                       // (waits stay safe with more)
 
 constexpr int PAIR_AREA = 2 * A_BYTES;                   // 256 rows x 128 bytes: two slices of a K-contiguous operand
 // Byte offset of this lane's 16 bytes of the first of a wave's four copies of a pair (rows 8 wave .. + 7 of the
@@ -672,7 +681,7 @@ __global__ __launch_bounds__(NTHR, 1) void gemm_mfma_lean_kernel(GemmArgs g, Wal
       if (PAIR) step(no, yes, a2, true); else step(no, no, a2, true);
     }
     if (has_aux<FAST>() && !EARLY) { fetch_aux(aux0, g, cc, wm0, wn0, lane, 0); fetch_aux(aux1, g, cc, wm0, wn0, lane, 1); }
-    if (FAST == FAST_STORE_F32) epilogue_f32(g, cc, acc, wm0, wn0, lane);
+    if (FAST == FAST_STORE_F32 || FAST == FAST_SCALED_F32) epilogue_f32<FAST == FAST_SCALED_F32>(g, cc, acc, wm0, wn0, lane);
     else if (SUMS) epilogue_sums(g, cc, acc, wm0, wn0, lane);
     else epilogue_staged_fn<FAST>(g, cc, acc, wm0, wn0, lane, smem + LEAN_NST * STAGE_BYTES + wave * 4096, aux0, aux1);
     if (TOGETHER && grp == 1) {
@@ -746,6 +755,12 @@ inline bool has_lean(const GemmArgs& g, bool a_kc, bool b_kc) {
   return g.mode == EPI_RESID && g.aux && !g.lambda_mn;
 }
 hipError_t launch_lean_nn(const GemmArgs& g, hipStream_t s) {
+  if (g.scale) {
+    const bool pair = g.K % (2 * BK) == 0;
+    if (g.c_is_f32)
+      return pair ? launch_lean_walk<true, false, FAST_SCALED_F32, false, true>(g, s) : launch_lean_walk<true, false, FAST_SCALED_F32, false, false>(g, s);
+    return pair ? launch_lean_walk<true, false, FAST_SCALED, false, true>(g, s) : launch_lean_walk<true, false, FAST_SCALED, false, false>(g, s);
+  }
   if (g.c_is_f32 || g.split_k > 1)
     return g.K % ((long)g.split_k * 2 * BK) == 0 ? launch_lean_walk<true, false, FAST_STORE_F32, false, true>(g, s)
                                : launch_lean_walk<true, false, FAST_STORE_F32, false, false>(g, s);
@@ -809,6 +824,7 @@ bool covered(const GemmArgs& g) {
     return false;
   if (lda > (1L << 22) || ldb > (1L << 22)) return false;   // per-lane source offsets are 32-bit
   if (g.split_k > 1 && g.mode != EPI_STORE) return false;
+  if (g.scale && (g.split_k > 1 || g.batch > 1 || g.mode != EPI_STORE || g.addf || !a_kc || b_kc)) return false;
   if (g.M <= 0 || g.N <= 0 || g.K <= 0 || g.batch <= 0 || g.split_k <= 0) return false;
   const bool act = g.mode == EPI_ACT_GELU || g.mode == EPI_ACT_TANH;
   return (a_kc && (b_kc || (b_rc && !act))) || (a_rc && b_rc && !act);

@@ -113,6 +113,11 @@ __device__ __forceinline__ void finish8(const GemmArgs& g, long batch, int split
       for (int x = 0; x < 8; ++x) v[x] = fmaf(g.lambda_mn ? l8[x] : lm[x], f[x], v[x]);
     }
   }
+  if (!ACT && g.scale) {
+    const float f = *g.scale;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] *= f;
+  }
   if (g.c_is_f32) store8(reinterpret_cast<float*>(g.C) + batch * g.c_sb + off, v);
   else store8(reinterpret_cast<bf16_t*>(g.C) + batch * g.c_sb + off, v);
 }

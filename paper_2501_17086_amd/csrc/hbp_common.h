@@ -158,6 +158,7 @@ struct GemmArgs {
   const void* lambda_mn;              // storage type [M,N] (row stride ldc, batch stride aux_sb): EPI_RESID per element
   int c_is_f32;         // C stored as fp32 regardless of the storage type
   VocabEpilogue vocab;  // EPI_VOCAB_...
+  const float* scale;   // bf16 kernels, EPI_STORE in one share, A K-contiguous and B not: C = *scale acc; or NULL
 };
 
 // storage type: 0 = fp32, 1 = bf16
