@@ -484,7 +484,8 @@ hbp_status hbp_embedding_backward(const hbp_embedding_desc* desc, const hbp_embe
  *   row_loss_n = log sum_v exp(s_nv) - s_nt,    loss = factor sum_n row_loss_n, with mean = 1 divided by the number of rows that count,
  *   dx = scale dS weight,    dweight = scale dS^T x,    dS_nv = factor (/ that number) (softmax(s_n)_v - [v = t]).
  * Other rows (padding) have row_loss 0 and a dx of zeros, and nothing in their x reaches any result; where no row counts
- * the loss is 0 and dweight zeros.  The vocabulary is taken in pieces and the logits are not kept.
+ * the loss is 0 and dweight zeros, whatever weight holds.  The vocabulary is taken in pieces and the logits are not kept.
+ * A logit of minus infinity (a weight that masks an entry) has a probability and a dweight of zero; in dx, zero times an infinite weight is NaN.
  * bf16 storage: dS is rounded to bf16 before it meets weight and x; logits, their sums and all products' sums are fp32. */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(hbp_cross_entropy_desc) */

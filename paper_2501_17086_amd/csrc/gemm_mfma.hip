@@ -313,9 +313,13 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
       }
     }
   }
-  // FAST_VOCAB_GRAD: the columns' logarithms, in the MFMA layout as well, and lane c's column's target
+  // FAST_VOCAB_GRAD: the columns' logarithms, in the MFMA layout as well, and lane c's column's target.  Columns that do not count (target -1)
+  // are zeros of x: against an infinity or a NaN in the weights their products are NaNs, so they are cleared on their way out, where a wavefront
+  // has any (on: its columns that count; keep: this lane's eight in the row layout).
   constexpr bool VOCAB = FAST == FAST_VOCAB_GRAD;
   float lse[8][4];
+  unsigned long on = ~0ul;
+  uint4v keep = {~0u, ~0u, ~0u, ~0u};
   const float scale = FAST == FAST_SCALED ? *g.scale : 1.f;
   float gain = 0.f, at_target = 0.f;
   int target = 0;
@@ -327,9 +331,15 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
       const float4 t = *reinterpret_cast<const float4*>(lp + 8 * k);
       lse[k][0] = t.x; lse[k][1] = t.y; lse[k][2] = t.z; lse[k][3] = t.w;
     }
-    const long n = tc.n0 + wn0 + lane, t = (long)g.vocab.target[n] - (g.vocab.row0 + tc.m0 + wm0);
+    const long n = tc.n0 + wn0 + lane;
+    const int token = g.vocab.target[n];
+    const long t = token - (g.vocab.row0 + tc.m0 + wm0);
     target = t < 0 || t >= 128 ? -1 : (int)t;
     at_target = g.vocab.at_target[n] * gain;
+    on = __ballot(token >= 0);
+    const unsigned mine = (unsigned)(on >> (8 * rk));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) keep[k] = (mine >> (2 * k) & 1u ? 0xFFFFu : 0u) | (mine >> (2 * k) & 2u ? 0xFFFF0000u : 0u);
   }
   // staging addresses, row layout: rows rr, rr + 8, rr + 16, rr + 24
   auto row_at = [&](int r) { return stg + r * 128 + ((rk ^ ((r >> 1) & 7)) << 4); };
@@ -342,11 +352,12 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
   // 32 rows x 64 columns now in the staging tile (MFMA layout written): read as rows, store whole lines
   auto flush = [&](bf16_t* c) {
     __builtin_amdgcn_wave_barrier();
-    const uint4v o0 = *reinterpret_cast<const uint4v*>(p0);
-    const uint4v o1 = *reinterpret_cast<const uint4v*>(p1);
-    const uint4v o2 = *reinterpret_cast<const uint4v*>(p2);
-    const uint4v o3 = *reinterpret_cast<const uint4v*>(p3);
+    uint4v o0 = *reinterpret_cast<const uint4v*>(p0);
+    uint4v o1 = *reinterpret_cast<const uint4v*>(p1);
+    uint4v o2 = *reinterpret_cast<const uint4v*>(p2);
+    uint4v o3 = *reinterpret_cast<const uint4v*>(p3);
     __builtin_amdgcn_wave_barrier();      // the next round's writes stay behind these reads
+    if (VOCAB && on != ~0ul) { o0 &= keep; o1 &= keep; o2 &= keep; o3 &= keep; }
     __builtin_nontemporal_store(o0, reinterpret_cast<uint4v*>(c));
     __builtin_nontemporal_store(o1, reinterpret_cast<uint4v*>(c + ld8));
     __builtin_nontemporal_store(o2, reinterpret_cast<uint4v*>(c + 2 * ld8));
