@@ -30,13 +30,13 @@ constexpr int BLOCK_V = 64;                                // rows of the vocabu
 struct Parts {
   void* x;                // [np, wp], storage type: x, zeros where a row does not count and behind its channels
   void* weight;           // [vocab, wp]: the weights with zeros behind their channels, where wp is not the width; else NULL
-  float* target_logit;    // [np], times log2 e
+  float* target_logit;    // [np]
   float* lse;             // [np], base 2; infinity where a row does not count: its probabilities are zeros
   int* target;            // [np], -1 where a row does not count
   float* rows;            // [np] row losses
   float* at_target;       // [np] the target's softmax less 1
   float* scalars;         // [2]: the factor on dS, and what dx and dweight are multiplied by afterwards
-  float* sums;            // [blocks][np]: base 2 logarithms of a block's sums
+  float2* sums;           // [blocks][np]: a block's largest logit, and its sum of exponentials relative to that
   float* logits;          // [piece][np]
   void* grad;             // [piece][np], storage type (fp32: the logits' place)
   float* dx;              // [shares][np, wp]
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(NTHR) void rows_kernel(CeArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
   if (lane == 0) {
-    a.p.target_logit[n] = dot * a.to_log2;
+    a.p.target_logit[n] = dot;
     a.p.target[n] = t;
   }
 }
@@ -109,31 +109,38 @@ __global__ __launch_bounds__(NTHR) void weight_kernel(CeArgs a) {
   }
 }
 
-// running maximum and sum of 2^v
+// Running maximum of logits and sum of 2^(alpha (logit - maximum)).  The pair is kept as it is until a row's loss is made of it: one logarithm
+// a block in its place is rounded at the logits' size, in every block (a vocabulary of 2000 equal logits of 105: 4e-6 of a loss of 7.6).
 struct Running {
   float m, l;
-  __device__ __forceinline__ void add(float om, float ol) {
+  __device__ __forceinline__ void add(float om, float ol, float alpha) {
     const float n = fmaxf(m, om);
     if (n == -INFINITY) { l += ol; return; }               // (nothing yet: zeros, or a NaN, which stays)
-    l = l * __builtin_amdgcn_exp2f(m - n) + ol * __builtin_amdgcn_exp2f(om - n);
+    l = l * __builtin_amdgcn_exp2f((m - n) * alpha) + ol * __builtin_amdgcn_exp2f((om - n) * alpha);
     m = n;
   }
-  // K numbers at once
-  template <int K> __device__ __forceinline__ void add(const float (&v)[K]) {
+  // K pairs at once
+  template <int K> __device__ __forceinline__ void add(const float (&v)[K], const float (&w)[K], float alpha) {
     float top = v[0], sum = 0.f;
 #pragma unroll
     for (int j = 1; j < K; ++j) top = fmaxf(top, v[j]);
     const float shift = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int j = 0; j < K; ++j) sum += __builtin_amdgcn_exp2f(v[j] - shift);
-    add(top, sum);
+    for (int j = 0; j < K; ++j) sum += w[j] * __builtin_amdgcn_exp2f((v[j] - shift) * alpha);
+    add(top, sum, alpha);
+  }
+  // K logits
+  template <int K> __device__ __forceinline__ void add(const float (&v)[K], float alpha) {
+    float one[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) one[j] = 1.f;
+    add(v, one, alpha);
   }
 };
-__device__ __forceinline__ float log2_sum(const Running& r) { return r.l == 0.f ? -INFINITY : r.m + __builtin_amdgcn_logf(r.l); }
 
 // the parts' sums of TB rows meet in a fixed tree; thread = part TB + row, the result is part 0's
 template <int TB, int NT>
-__device__ __forceinline__ Running meet(Running r, float (&sm)[NT], float (&sl)[NT]) {
+__device__ __forceinline__ Running meet(Running r, float alpha, float (&sm)[NT], float (&sl)[NT]) {
   const int t = threadIdx.x;
   sm[t] = r.m;
   sl[t] = r.l;
@@ -141,7 +148,7 @@ __device__ __forceinline__ Running meet(Running r, float (&sm)[NT], float (&sl)[
 #pragma unroll
   for (int o = NT / 2; o >= TB; o /= 2) {
     if (t < o) {
-      r.add(sm[t + o], sl[t + o]);
+      r.add(sm[t + o], sl[t + o], alpha);
       sm[t] = r.m;
       sl[t] = r.l;
     }
@@ -161,12 +168,12 @@ __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const long at = v0 + j * PARTS;
-    v[j] = at < a.nv ? a.p.logits[at * a.p.np + nc] * a.to_log2 : -INFINITY;
+    v[j] = at < a.nv ? a.p.logits[at * a.p.np + nc] : -INFINITY;
   }
   Running r = {-INFINITY, 0.f};
-  r.add(v);
-  r = meet<TB>(r, sm, sl);
-  if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = log2_sum(r);
+  r.add(v, a.to_log2);
+  r = meet<TB>(r, a.to_log2, sm, sl);
+  if (part == 0 && n < a.p.np) a.p.sums[(a.block0 + blockIdx.y) * a.p.np + n] = make_float2(r.m, r.l);
 }
 
 // Small problems: logits, a block's sums and the targets' logits in one launch, without x's copy.  A workgroup takes 64 rows of the vocabulary and
@@ -247,16 +254,16 @@ __global__ __launch_bounds__(NTHR) void small_logits_kernel(CeArgs a, int keep) 
     const int row = p8 + 8 * j;
     const float s = (part[0][row][col] + part[1][row][col]) + (part[2][row][col] + part[3][row][col]);
     const bool in = v0 + row < a.c.vocab;
-    v[j] = in ? s * a.to_log2 : -INFINITY;
+    v[j] = in ? s : -INFINITY;
     if (in && n < a.p.np) {
       if (keep) a.p.logits[(v0 + row) * a.p.np + n] = s;
       if (tc == v0 + row) a.p.target_logit[n] = v[j];
     }
   }
   Running run = {-INFINITY, 0.f};
-  run.add(v);
-  run = meet<32>(run, sm, sl);
-  if (p8 == 0 && n < a.p.np) a.p.sums[(long)blockIdx.x * a.p.np + n] = log2_sum(run);
+  run.add(v, a.to_log2);
+  run = meet<32>(run, a.to_log2, sm, sl);
+  if (p8 == 0 && n < a.p.np) a.p.sums[(long)blockIdx.x * a.p.np + n] = make_float2(run.m, run.l);
 }
 
 // all blocks of TB rows from n0 on by NT threads, and their losses
@@ -267,18 +274,22 @@ __device__ __forceinline__ void row_losses(const CeArgs& a, long n0, float (&sm)
   const long n = n0 + row, nc = n < a.p.np ? n : a.p.np - 1;
   Running r = {-INFINITY, 0.f};
   for (int b = part; b < a.p.blocks; b += K * PARTS) {
-    float v[K];
+    float2 f[K];
+    float v[K], w[K];
 #pragma unroll
-    for (int j = 0; j < K; ++j) v[j] = b + j * PARTS < a.p.blocks ? a.p.sums[(long)(b + j * PARTS) * a.p.np + nc] : -INFINITY;
-    r.add(v);
+    for (int j = 0; j < K; ++j)
+      f[j] = b + j * PARTS < a.p.blocks ? a.p.sums[(long)(b + j * PARTS) * a.p.np + nc] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int j = 0; j < K; ++j) { v[j] = f[j].x; w[j] = f[j].y; }
+    r.add(v, w, a.to_log2);
   }
-  r = meet<TB>(r, sm, sl);
+  r = meet<TB>(r, a.to_log2, sm, sl);
   if (part != 0 || n >= a.p.np) return;
   const bool counts = a.p.target[n] >= 0;
-  const float lse = log2_sum(r);
-  const float loss = counts ? (lse - a.p.target_logit[n]) * LN2 : 0.f;
-  a.p.lse[n] = counts ? lse : INFINITY;
-  a.p.at_target[n] = counts ? exp2f(a.p.target_logit[n] - lse) - 1.f : 0.f;
+  const float log2_l = __builtin_amdgcn_logf(r.l);
+  const float loss = counts ? fmaf(a.c.scale, r.m - a.p.target_logit[n], log2_l * LN2) : 0.f;
+  a.p.lse[n] = counts ? fmaf(r.m, a.to_log2, log2_l) : INFINITY;
+  a.p.at_target[n] = counts ? expm1f(-loss) : 0.f;
   a.p.rows[n] = loss;
   if (a.c.row_loss && n < a.c.rows) a.c.row_loss[n] = loss;
 }
@@ -568,7 +579,7 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.rows = reinterpret_cast<float*>(take(4 * p.np));
   p.at_target = reinterpret_cast<float*>(take(4 * p.np));
   p.scalars = reinterpret_cast<float*>(take(16));
-  p.sums = reinterpret_cast<float*>(take((size_t)p.blocks * p.np * 4));
+  p.sums = reinterpret_cast<float2*>(take((size_t)p.blocks * p.np * 8));
   p.logits = reinterpret_cast<float*>(take((size_t)(p.fused ? vocab - p.fused : p.piece) * p.np * 4));
   p.grad = p.logits;
   if (gradients) {

@@ -204,12 +204,13 @@ enum FastEpi {
 // 256 channels the epilogue's 128 exponentials a lane take as long as the products; with plain stores in place of non-temporal ones
 // the gradient's 1 GB costs a tenth more.
 //
-// Sums of 2^(alpha acc) over a wavefront's 128 rows, for each of its 64 columns.  The products of this form are issued with the
-// operands the other way round, so that a lane holds 64 rows of one column in each acc[.][j] and its neighbour 32 lanes on the other 64.
+// The largest of a wavefront's 128 rows and the sum of 2^(alpha (acc - it)), for each of its 64 columns.  The products of this form are issued with
+// the operands the other way round, so that a lane holds 64 rows of one column in each acc[.][j] and its neighbour 32 lanes on the other 64.
+// (One rounded product is taken off in the exponent of every term; what its rounding left out comes back as one factor of their sum.)
 __device__ __forceinline__ void epilogue_sums(const GemmArgs& g, const TileCoord& tc, const float16v (&acc)[4][2], int wm0, int wn0,
                                               int lane) {
   const float alpha = g.vocab.alpha;
-  float* c = reinterpret_cast<float*>(g.C) + (tc.m0 + wm0) / 128 * g.ldc + tc.n0 + wn0 + (lane & 31);
+  float* c = reinterpret_cast<float*>(g.C) + 2 * ((tc.m0 + wm0) / 128 * g.ldc + tc.n0 + wn0 + (lane & 31)) + (lane >> 5);
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     float top = acc[0][j][0];
@@ -219,6 +220,7 @@ __device__ __forceinline__ void epilogue_sums(const GemmArgs& g, const TileCoord
       for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
     top = fmaxf(top, __shfl_xor(top, 32));
     const float shift = top == -INFINITY ? 0.f : top * alpha;      // (alpha > 0)
+    const float left_out = top == -INFINITY ? 0.f : fmaf(top, alpha, -shift);
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -226,7 +228,8 @@ __device__ __forceinline__ void epilogue_sums(const GemmArgs& g, const TileCoord
       for (int r = 0; r < 16; ++r) sum[i] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], alpha, -shift));
     float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     l += __shfl_xor(l, 32);
-    if (lane < 32) c[32 * j] = shift + __builtin_amdgcn_logf(l);
+    l *= __builtin_amdgcn_exp2f(-left_out);
+    c[64 * j] = lane < 32 ? top : l;
   }
 }
 

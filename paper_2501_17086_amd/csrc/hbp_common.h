@@ -129,7 +129,7 @@ enum EpiMode {
   EPI_RESID = 5,       // C = lambda[n] * aux[m,n] + acc        (x_{l+1})
   EPI_ADD_AUX = 6,     // C = acc + aux[m,n]
   // products of a vocabulary's weights (rows m) with rows n (launch_gemm_vocab only; cross_entropy.hip)
-  EPI_VOCAB_SUMS = 7,  // C(fp32)[m / 128][n] = log2 of the sum over those 128 m of 2^(alpha acc)
+  EPI_VOCAB_SUMS = 7,  // C(2 x fp32)[m / 128][n] = the largest acc of those 128 m, the sum of 2^(alpha (acc - it))
   EPI_VOCAB_GRAD = 8   // C(bf16) = gain (2^(alpha acc - lse[n]) - [row0 + m = target[n]])
 };
 struct VocabEpilogue {

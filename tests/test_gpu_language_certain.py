@@ -1,0 +1,28 @@
+"""Cross entropy of logits that are exact: what a row's loss is then, in every form (logits and sums in one launch, logits in memory, logits that meet no memory)."""
+import math
+
+import pytest
+import torch
+
+from paper_2501_17086_amd import binding as B
+from tests import language_reference as R
+from tests.test_gpu_language_ops import TYPES, normal
+
+pytestmark = pytest.mark.gpu
+SIZES = [(8, 2000, 256), (100, 30000, 264), (1000, 9300, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+@pytest.mark.parametrize("n,vocab,width", SIZES + [(1024, 9216, 128)])
+def test_losses_of_equal_exact_logits(n, vocab, width, scale, dtype):
+    """Every logit is 21 * 5 = 105, exact in every order of its sum (one channel): exponentials of differences are ones, their sum the vocabulary's
+    size, exact, and a row's loss its logarithm whatever the logits' size: the logarithm's rounding, 2 f at most, that of ln 2 and the product's, and
+    another 2 f for the sums that a loss passes through."""
+    x, w = torch.zeros((n, width), dtype=TYPES[dtype], device="cuda"), torch.zeros((vocab, width), dtype=TYPES[dtype], device="cuda")
+    x[:, 5], w[:, 5] = 21.0, 5.0
+    c = B.make_cross_entropy(x, w, torch.arange(n, dtype=torch.int32, device="cuda") % vocab, scale=scale, grad=False)
+    B.hbp_loss_cross_entropy(c)
+    want = torch.full((n,), math.log(vocab), dtype=torch.float64, device="cuda")
+    R.assert_within(c.row_loss, want, 6 * R.F * want, "row_loss")
+    R.assert_within(c.loss, want[:1], 7 * R.F * want[:1], "loss")
