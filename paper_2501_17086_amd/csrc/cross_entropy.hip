@@ -287,7 +287,10 @@ __device__ __forceinline__ void row_losses(const CeArgs& a, long n0, float (&sm)
   if (part != 0 || n >= a.p.np) return;
   const bool counts = a.p.target[n] >= 0;
   const float log2_l = __builtin_amdgcn_logf(r.l);
-  const float loss = counts ? fmaf(a.c.scale, r.m - a.p.target_logit[n], log2_l * LN2) : 0.f;
+  float loss = counts ? fmaf(a.c.scale, r.m - a.p.target_logit[n], log2_l * LN2) : 0.f;
+  // The target's logit is a sum of its own (rows_kernel), whose order is not the products': where it is the largest it may come out above its
+  // other self by their roundings, and a probability above 1 would push the gradient the wrong way.  (NaNs stay.)
+  if (loss < 0.f) loss = 0.f;
   a.p.lse[n] = counts ? fmaf(r.m, a.to_log2, log2_l) : INFINITY;
   a.p.at_target[n] = counts ? expm1f(-loss) : 0.f;
   a.p.rows[n] = loss;

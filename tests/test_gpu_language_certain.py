@@ -1,4 +1,5 @@
-"""Cross entropy of logits that are exact: what a row's loss is then, in every form (logits and sums in one launch, logits in memory, logits that meet no memory)."""
+"""Cross entropy of rows that are certain of their target, and of logits that are exact: what a row's loss and its target's coefficient
+are then, in every form (logits and sums in one launch, logits in memory, logits that meet no memory)."""
 import math
 
 import pytest
@@ -10,6 +11,26 @@ from tests.test_gpu_language_ops import TYPES, normal
 
 pytestmark = pytest.mark.gpu
 SIZES = [(8, 2000, 256), (100, 30000, 264), (1000, 9300, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,width", SIZES)
+def test_certain_rows_have_no_negative_loss(n, vocab, width, dtype):
+    """Rows that are their target's weights: its logit is 4 width, the others' next to 4 sqrt(width), their probabilities below e^-400 and so
+    zero in 32 bits.  A loss is then never below zero, and a target's coefficient, all that its row of dweight holds, never above."""
+    w = normal((vocab, width), TYPES[dtype], 1, 2.0)
+    t = torch.randperm(vocab, generator=torch.Generator().manual_seed(2))[:n].int().cuda()
+    x = w[t.long()].clone()
+    c = B.make_cross_entropy(x, w, t, mean=False)
+    B.hbp_loss_cross_entropy(c)
+    s = x.double() @ w.double().T
+    own = s.gather(1, t.long()[:, None])
+    assert bool((own - s.scatter(1, t.long()[:, None], -math.inf).amax(1, keepdim=True) > 110).all())     # e^-110 is below fp32
+    assert bool((c.row_loss >= 0).all()) and c.loss.item() >= 0
+    R.assert_within(c.row_loss, torch.zeros(n, dtype=torch.float64, device="cuda"),
+                    R.cross_entropy(x, w, t, mean=False)["row_loss"][1], "row_loss")
+    along = (c.dweight[t.long()].double() * x.double()).sum(1) / x.double().square().sum(1)              # the coefficient
+    assert bool((along <= 0).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
