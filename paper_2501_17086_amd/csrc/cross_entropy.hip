@@ -44,7 +44,7 @@ struct Parts {
   long np, piece;
   int wp;                 // channels with those that fill up
   long fused;             // rows of the vocabulary whose logits meet no memory
-  int blocks, pieces, split, shares;   // shares: products whose results lie side by side until they are added up
+  int blocks, pieces, shares;   // shares: products whose results lie side by side until they are added up
   size_t dweight_bytes, bytes;
 };
 
@@ -528,6 +528,14 @@ int dx_split(int dtype, long np, int wp, long nv) {
   const bool w = dx_wide(dtype, np, wp, nv);
   return shares_of(dtype, np, w ? wp / 256 * 256 : wp, nv, w);
 }
+// dx of nv rows of the vocabulary: one product, or whole slices of 32 and the rest in one share (a contraction that is no multiple of 32 keeps the
+// 256 x 256 kernel from all of it)
+struct DxParts { long whole; int split, rest; };
+DxParts dx_parts(int dtype, long np, int wp, long nv) {
+  const long whole = nv / 32 * 32;
+  if (whole < nv && dx_wide(dtype, np, wp, whole)) return {whole, dx_split(dtype, np, wp, whole), 1};
+  return {nv, dx_split(dtype, np, wp, nv), 0};
+}
 bool dweight_wide(int dtype, long np, int width, long nv) { return dtype == 1 && np % 32 == 0 && nv % 256 == 0 && wide(nv, width, np); }
 int dweight_split(int dtype, long np, int width, long nv) {
   const bool w = dweight_wide(dtype, np, width, nv);
@@ -587,12 +595,12 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.grad = p.logits;
   if (gradients) {
     if (dtype == 1) p.grad = take((size_t)p.piece * p.np * 2);
+    // as many as there are, and of many pieces the largest product's, what was added up before it, and a rest, four at least
     const long last_piece = vocab - (p.pieces - 1) * p.piece;
-    for (const long nv : {p.piece, p.piece / 32 * 32, last_piece, last_piece / 32 * 32}) {
-      const int n = nv ? dx_split(dtype, p.np ? p.np : 8, p.wp, nv) : 1;
-      p.split = n > p.split ? n : p.split;
-    }
-    p.shares = p.split + 2 < 4 ? 4 : p.split + 2;
+    const DxParts each = dx_parts(dtype, p.np ? p.np : 8, p.wp, p.piece), end = dx_parts(dtype, p.np ? p.np : 8, p.wp, last_piece);
+    const long all = (p.pieces - 1l) * (each.split + each.rest) + end.split + end.rest, split = each.split > end.split ? each.split : end.split;
+    const long room = split + 2 < 4 ? 4 : split + 2;
+    p.shares = (int)(all < room ? all : room);
     p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * p.wp * 4));
     const size_t most = dweight_room(dtype, p.np, width, p.piece), last = dweight_room(dtype, p.np, width, last_piece);
     p.dweight_bytes = most > last ? most : last;
@@ -773,14 +781,10 @@ struct Run {
     g.M = p.np; g.N = p.wp; g.K = nr;
     return by_columns(g, dx_wide(DTYPE, p.np, p.wp, nr));
   }
-  // (a contraction that is no multiple of 32 keeps the 256 x 256 kernel from all of it)
   hipError_t dx(long v0, long nv) {
-    const long whole = nv / 32 * 32;
-    if (whole < nv && dx_wide(DTYPE, p.np, p.wp, whole)) {
-      CE_TRY(dx_rows(v0, 0, whole, dx_split(DTYPE, p.np, p.wp, whole)));
-      return dx_rows(v0, whole, nv - whole, 1);
-    }
-    return dx_rows(v0, 0, nv, dx_split(DTYPE, p.np, p.wp, nv));
+    const DxParts d = dx_parts(DTYPE, p.np, p.wp, nv);
+    CE_TRY(dx_rows(v0, 0, d.whole, d.split));
+    return d.rest ? dx_rows(v0, d.whole, nv - d.whole, d.rest) : hipSuccess;
   }
 
   hipError_t without_rows() {
