@@ -533,7 +533,7 @@ int dx_split(int dtype, long np, int wp, long nv) {
 struct DxParts { long whole; int split, rest; };
 DxParts dx_parts(int dtype, long np, int wp, long nv) {
   const long whole = nv / 32 * 32;
-  if (whole < nv && dx_wide(dtype, np, wp, whole)) return {whole, dx_split(dtype, np, wp, whole), 1};
+  if (whole > 0 && whole < nv && dx_wide(dtype, np, wp, whole)) return {whole, dx_split(dtype, np, wp, whole), 1};
   return {nv, dx_split(dtype, np, wp, nv), 0};
 }
 bool dweight_wide(int dtype, long np, int width, long nv) { return dtype == 1 && np % 32 == 0 && nv % 256 == 0 && wide(nv, width, np); }

@@ -19,3 +19,10 @@ def test_one_piece_keeps_dx_once_or_twice(rows, vocab, width):
     whole slice; beside them dS and at most 16 shares of dweight."""
     more = workspace(rows, vocab, width, B.BF16, 1) - workspace(rows, vocab, width, B.BF16, 0)
     assert more <= 2 * rows * width * 4 + rows * vocab * 2 + 16 * vocab * width * 4 + 4096
+
+
+@pytest.mark.parametrize("vocab", [1, 16, 31])
+def test_a_vocabulary_below_a_slice_is_one_product(vocab):
+    rows, width = 16384, 1024
+    more = workspace(rows, vocab, width, B.BF16, 1) - workspace(rows, vocab, width, B.BF16, 0)
+    assert more <= rows * width * 4 + rows * vocab * 2 + 16 * vocab * width * 4 + 4096
