@@ -494,13 +494,13 @@ long fused_rows(int dtype, long np, long vocab) {
   const long tiles = vocab / 256 * (np / 256);
   return gemm_fills_chip(tiles) && tiles < (1l << 28) ? vocab / 256 * 256 : 0;
 }
-// Rows of x are filled up with zeros to whole tiles of 256 where that is an eighth more at most, or three eighths and those epilogues then
+// Rows of x are filled up with zeros, fp32 to a multiple of 8, bf16 to whole tiles of 256 where that is an eighth more at most, or three eighths and those epilogues then
 // take the logits, else to 8.  Measured, us, with gradients, tiles / 8: 600 rows (768) against 40000 x 256 134 / 191, 100000 x 1024 617 / 830; 200
 // (256) 84 / 101 and 298 / 346, against 40000 x 1024 161 / 154; beyond the line, 300 (512) against 40000 x 1024 229 / 192, 100 against 40000 x 1024
 // 153 / 123.
 long padded(int dtype, long rows, long vocab) {
   const long whole = (rows + 255) / 256 * 256;
-  if (whole <= rows + rows / 8 || (whole <= rows + rows * 3 / 8 && fused_rows(dtype, whole, vocab))) return whole;
+  if (dtype == 1 && (whole <= rows + rows / 8 || (whole <= rows + rows * 3 / 8 && fused_rows(dtype, whole, vocab)))) return whole;
   return (rows + 7) / 8 * 8;
 }
 // A product of few tiles and a long contraction (dx: over the vocabulary, dweight: over the rows of x) is shared out until there is a tile for

@@ -26,3 +26,10 @@ def test_a_vocabulary_below_a_slice_is_one_product(vocab):
     rows, width = 16384, 1024
     more = workspace(rows, vocab, width, B.BF16, 1) - workspace(rows, vocab, width, B.BF16, 0)
     assert more <= rows * width * 4 + rows * vocab * 2 + 16 * vocab * width * 4 + 4096
+
+
+@pytest.mark.parametrize("rows,vocab,width", [(1825, 6000, 512), (3900, 8000, 512), (1, 50, 8), (8191, 100, 64)])
+def test_fp32_rows_are_filled_up_to_eight(rows, vocab, width):
+    """x's copy, five numbers a row, two for 64 of its logits, the logits; 256 bytes for each place to begin at."""
+    n = (rows + 7) // 8 * 8
+    assert workspace(rows, vocab, width, B.F32, 0) <= 4 * n * (width + 5 + 2 * ((vocab + 63) // 64) + vocab) + 10 * 256
