@@ -610,6 +610,25 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   return p;
 }
 
+// Have all products of the gradients their room?  Goes through them as the launches do (Run::dweight, Run::dx), and is asked before the first.
+bool fits(const Parts& p, int dtype, long vocab, int width) {
+  int shares = 0;
+  for (int i = 0; i < p.pieces; ++i) {
+    const long v0 = i * p.piece, nv = vocab - v0 < p.piece ? vocab - v0 : p.piece;
+    for (long r = 0, n; r < nv; r += n) {
+      n = dweight_rows_of(dtype, p.np, width, nv - r);
+      if (dweight_part(dtype, p.np, width, n) > p.dweight_bytes) return false;
+    }
+    const DxParts d = dx_parts(dtype, p.np, p.wp, nv);
+    for (const int k : {d.split, d.rest}) {
+      if (shares + k > p.shares) shares = 1;               // (Run::fold)
+      if (shares + k > p.shares) return false;
+      shares += k;
+    }
+  }
+  return true;
+}
+
 hipError_t product(int dtype, const GemmArgs& g, hipStream_t s) {
   if (dtype == 1) {
     hipError_t e;
@@ -751,7 +770,6 @@ struct Run {
       g.scale = DTYPE == 1 ? p.scalars + 1 : nullptr;
       return by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr));
     }
-    if (dweight_part(DTYPE, p.np, c.width, nr) > p.dweight_bytes) return hipErrorInvalidValue;
     g.c_is_f32 = 1; g.C = p.dweight; g.ldc = c.width; g.c_sb = nr * c.width; g.split_k = n;
     CE_TRY(by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr)));
     const long n8 = nr * c.width / 8;
@@ -773,7 +791,6 @@ struct Run {
     g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = 1; g.a_sk = p.np;
     g.B = weight_at(v0 + r0); g.b_sk = weight_row(); g.b_sn = 1;
     if (shares + split > p.shares) CE_TRY(fold());
-    if (shares + split > p.shares) return hipErrorInvalidValue;
     g.C = p.dx + (long)shares * p.np * p.wp; g.ldc = p.wp; g.c_is_f32 = 1;
     g.c_sb = p.np * p.wp;
     g.split_k = split;
@@ -838,12 +855,13 @@ struct Run {
 }  // namespace
 
 size_t cross_entropy_ws_bytes(int dtype, long rows, long vocab, int width, bool gradients) {
-  return carve(nullptr, dtype, rows, vocab, width, gradients).bytes;
+  const Parts p = carve(nullptr, dtype, rows, vocab, width, gradients);
+  return rows && gradients && !fits(p, dtype, vocab, width) ? 0 : p.bytes;
 }
 
 hipError_t launch_cross_entropy(int dtype, const CrossEntropyArgs& c, void* workspace, size_t bytes, hipStream_t s) {
   const Parts p = carve(reinterpret_cast<char*>(workspace), dtype, c.rows, c.vocab, c.width, c.dx.p || c.dweight.p);
-  if (bytes < p.bytes) return hipErrorInvalidValue;
+  if (bytes < p.bytes || (c.rows && (c.dx.p || c.dweight.p) && !fits(p, dtype, c.vocab, c.width))) return hipErrorInvalidValue;
   return dtype == 0 ? Run<float>(c, p, s).all() : Run<bf16_t>(c, p, s).all();
 }
 

@@ -1787,7 +1787,9 @@ hbp_status hbp_embedding_backward(const hbp_embedding_desc* d, const hbp_embeddi
 hbp_status hbp_cross_entropy_workspace_size(const hbp_cross_entropy_desc* d, int gradients, size_t* bytes) {
   if (!bytes) return HBP_E_NULL;
   HBP_RUN(check_cross_entropy(d));
-  *bytes = cross_entropy_ws_bytes(d->dtype, d->rows, d->vocab, (int)d->width, gradients != 0);
+  const size_t need = cross_entropy_ws_bytes(d->dtype, d->rows, d->vocab, (int)d->width, gradients != 0);
+  if (!need) return HBP_E_UNSUPPORTED;
+  *bytes = need;
   return HBP_OK;
 }
 
@@ -1810,7 +1812,8 @@ hbp_status hbp_loss_cross_entropy(const hbp_cross_entropy_desc* d, const hbp_cro
   a.scale = d->scale; a.factor = d->factor;
   a.rows = d->rows; a.vocab = d->vocab; a.width = (int)d->width;
   const size_t need = cross_entropy_ws_bytes(d->dtype, d->rows, d->vocab, (int)d->width, b->dx.data || b->dweight.data);
-  if (need && (!b->workspace || b->workspace_bytes < need)) return HBP_E_WORKSPACE;
+  if (!need) return HBP_E_UNSUPPORTED;
+  if (!b->workspace || b->workspace_bytes < need) return HBP_E_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(b->workspace) % 16) return HBP_E_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps(HBP_PROF_OTHER, s);

@@ -321,6 +321,7 @@ struct CrossEntropyArgs {
   int width;
 };
 // The launchers refuse (hipErrorInvalidValue, nothing launched) a workspace of fewer bytes than these.
+// (cross entropy: 0 where a product would not have its room in them, before anything is launched; no size is known for which that is so)
 size_t cross_entropy_ws_bytes(int dtype, long rows, long vocab, int width, bool gradients);
 hipError_t launch_cross_entropy(int dtype, const CrossEntropyArgs& a, void* workspace, size_t bytes, hipStream_t s);
 

@@ -1,5 +1,7 @@
 """CPU-only: what the cross entropy asks for as its workspace."""
 import ctypes as C
+import math
+import random
 
 import pytest
 
@@ -33,3 +35,39 @@ def test_fp32_rows_are_filled_up_to_eight(rows, vocab, width):
     """x's copy, five numbers a row, two for 64 of its logits, the logits; 256 bytes for each place to begin at."""
     n = (rows + 7) // 8 * 8
     assert workspace(rows, vocab, width, B.F32, 0) <= 4 * n * (width + 5 + 2 * ((vocab + 63) // 64) + vocab) + 10 * 256
+
+
+def sizes(seed, count):
+    """Sizes over the whole range, many of them at a tile's, a slice's or a piece's border."""
+    rng = random.Random(seed)
+
+    def near(lo, hi):
+        v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+        if rng.random() < 0.5:
+            unit = rng.choice((32, 64, 256))
+            v = round(v / unit) * unit + rng.choice((-32, -8, -1, 0, 0, 0, 1, 8, 31, 32))
+        return max(1, min(hi, int(v)))
+    for _ in range(count):
+        rows, vocab = near(1, rng.choice((4096, 1 << 20))), near(1, rng.choice((1 << 17, 1 << 17, 1 << 24)))
+        width = near(8, rng.choice((2048, 65536))) // 8 * 8
+        if rng.random() < 0.3:
+            width = (width + 255) // 256 * 256
+        yield rows, vocab, min(65536, max(8, width)), rng.choice((B.F32, B.BF16, B.BF16))
+
+
+def test_every_product_has_its_room():
+    """The library goes through a call's products as its launches do and refuses sizes of which one lacks room in what `carve` reserves: there are
+    none such."""
+    for size in sizes(1, 60000):
+        assert workspace(*size, 1) > workspace(*size, 0) > 0, size
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_sizes_around_a_tile(dtype):
+    for rows in (1, 8, 255, 256, 257, 4095, 4096, 8192, 16384, 1 << 20):
+        for tiles in (0, 1, 85, 86, 87, 141, 142, 255, 256, 257, 512):
+            for rest in (0, 1, 31, 32, 33, 255):
+                for width in (8, 128, 256, 264, 512, 1000, 1024, 2048):
+                    vocab = 256 * tiles + rest
+                    if vocab:
+                        assert workspace(rows, vocab, width, dtype, 1) > workspace(rows, vocab, width, dtype, 0) > 0
