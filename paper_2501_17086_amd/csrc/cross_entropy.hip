@@ -504,18 +504,20 @@ long padded(int dtype, long rows, long vocab) {
   return (rows + 7) / 8 * 8;
 }
 // A product of few tiles and a long contraction (dx: over the vocabulary, dweight: over the rows of x) is shared out until there is a tile for
-// every compute unit.  rows, cols: of its result; wide: the 256 x 256 kernel would take it.
+// every compute unit, in MAX_SPLIT shares at most.  rows, cols: of its result; wide: the 256 x 256 kernel would take it.
 int shares_of(int dtype, long rows, long cols, long k, bool wide) {
   const long t = dtype == 0 ? 64 : wide ? 256 : 128;
   const long tiles = (rows + t - 1) / t * ((cols + t - 1) / t);
   if (dtype != 0 && gemm_fills_chip(tiles)) return 1;
-  // (fp32: 512 tiles, from where on they are the 64-wide ones, and shares of 8192 at most, which halves the error of sums over 30000: 1000 x 1000 over
-  // 30000 756 us, in one share 881)
+  // (fp32: 512 tiles, from where on they are the 64-wide ones)
   long n = dtype == 0 ? (511 + tiles) / tiles : 256 / tiles;
-  if (dtype == 0 && n < (k + 8191) / 8192) n = (k + 8191) / 8192;
+  if (n > MAX_SPLIT) n = MAX_SPLIT;
   // (at least 512 of the contraction: 512 rows of x against 2000 x 1024 59 us, with 256 72; 4096 against 8000 x 512 210, with 2048 218)
   if (n > k / 512) n = k / 512;
-  return (int)(n < 1 ? 1 : n > MAX_SPLIT ? MAX_SPLIT : n);
+  // fp32 takes shares of 8192 at most, as many as that makes (up to 128; a piece's rows and columns are fewer then): it halves the error of sums over
+  // 30000 (1000 x 1000 over 30000 756 us, in one share 881)
+  if (dtype == 0 && n < (k + 8191) / 8192) n = (k + 8191) / 8192;
+  return (int)(n < 1 ? 1 : n);
 }
 // Does the 256 x 256 kernel take whole tiles of such a product, in shares where it needs them?  (Else nothing is gained by keeping its
 // rows, columns or contraction apart from the rest.)

@@ -71,3 +71,10 @@ def test_sizes_around_a_tile(dtype):
                     vocab = 256 * tiles + rest
                     if vocab:
                         assert workspace(rows, vocab, width, dtype, 1) > workspace(rows, vocab, width, dtype, 0) > 0
+
+
+def test_fp32_contractions_are_shared_out_by_8192():
+    """Room for a share of each 8192 of a product's contraction: the vocabulary for dx, the rows for dweight."""
+    vocab, rows, width = 1 << 20, 1 << 20, 64
+    assert workspace(8, vocab, width, B.F32, 1) - workspace(8, vocab, width, B.F32, 0) >= vocab // 8192 * 8 * width * 4
+    assert workspace(rows, 2, width, B.F32, 1) - workspace(rows, 2, width, B.F32, 0) >= rows // 8192 * 2 * width * 4 + rows * width * 4
