@@ -59,25 +59,15 @@ struct CeArgs {
   unsigned grad_blocks;   // grad_kernel's workgroups; those behind them copy x
 };
 
-// x's copy, a wavefront a row; the product with a row of the weights
+// x's copy, a wavefront a row
 template <typename T>
-__device__ __forceinline__ float copy_row(const CeArgs& a, long n, int lane, bool counts, const T* w) {
+__device__ __forceinline__ void copy_row(const CeArgs& a, long n, int lane, bool counts) {
   T* copy = reinterpret_cast<T*>(a.p.x) + n * a.p.wp;
-  float dot = 0.f;
   for (int c = 8 * lane; c < a.p.wp; c += 512) {
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (counts && c < a.c.width) {
-      load8(reinterpret_cast<const T*>(a.c.x.p) + n * a.c.x.row + c, v);
-      if (w) {
-        float u[8];
-        load8(w + c, u);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dot = fmaf(v[j], u[j], dot);
-      }
-    }
+    if (counts && c < a.c.width) load8(reinterpret_cast<const T*>(a.c.x.p) + n * a.c.x.row + c, v);
     store8(copy + c, v);
   }
-  return dot;
 }
 __device__ __forceinline__ int target_of(const CeArgs& a, long n) {
   const int t = n < a.c.rows ? a.c.targets[n] : -1;
@@ -89,13 +79,8 @@ __global__ __launch_bounds__(NTHR) void rows_kernel(CeArgs a) {
   const long n = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= a.p.np) return;
   const int t = target_of(a, n);
-  float dot = copy_row(a, n, lane, t >= 0, t >= 0 ? reinterpret_cast<const T*>(a.c.weight.p) + t * a.c.weight.row : nullptr);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
-  if (lane == 0) {
-    a.p.target_logit[n] = dot;
-    a.p.target[n] = t;
-  }
+  copy_row<T>(a, n, lane, t >= 0);
+  if (lane == 0) a.p.target[n] = t;
 }
 
 // the weights with their channels filled up
@@ -156,7 +141,7 @@ __device__ __forceinline__ Running meet(Running r, float alpha, float (&sm)[NT],
   }
   return r;
 }
-// a block's sums from its logits: TB rows of x a workgroup
+// a block's sums from its logits, and the targets' among them: TB rows of x a workgroup
 template <int TB>
 __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
   constexpr int PARTS = NTHR / TB, PER = BLOCK_V / PARTS;
@@ -170,6 +155,10 @@ __global__ __launch_bounds__(NTHR) void block_sums_kernel(CeArgs a) {
     const long at = v0 + j * PARTS;
     v[j] = at < a.nv ? a.p.logits[at * a.p.np + nc] : -INFINITY;
   }
+  const long target = n < a.p.np ? a.p.target[n] - a.v0 : -1;
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (target == v0 + j * PARTS && target < a.nv) a.p.target_logit[n] = v[j];
   Running r = {-INFINITY, 0.f};
   r.add(v, a.to_log2);
   r = meet<TB>(r, a.to_log2, sm, sl);
@@ -266,6 +255,39 @@ __global__ __launch_bounds__(NTHR) void small_logits_kernel(CeArgs a, int keep) 
   if (p8 == 0 && n < a.p.np) a.p.sums[(long)blockIdx.x * a.p.np + n] = make_float2(run.m, run.l);
 }
 
+// The targets' logits where the others meet no memory: a wavefront takes 32 rows of x and their targets' rows of the weights, and of its 32 x 32 products
+// keeps the diagonal.  Same instruction, same order along the channels: bit by bit the logits that the 256 x 256 kernel's epilogues see, so that where a
+// target holds next to all of a row's mass its logit cancels against the sum's.  (A sum in another order, as a plain dot product is, leaves a
+// rounding of the logit's size in the loss and in the target's coefficient, however small these are.)
+__global__ __launch_bounds__(NTHR) void target_kernel(CeArgs a) {
+  constexpr int STEP = Frag<bf16_t>::STEP, U = 4;
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const long n = ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) * 32 + r;
+  if (n - r >= a.p.np) return;                             // (np: whole tiles of 256)
+  const int t = a.p.target[n];
+  const bool in = t >= 0 && t < a.p.fused;
+  const bf16_t* w = a.p.weight ? reinterpret_cast<const bf16_t*>(a.p.weight) + (in ? t : 0l) * a.p.wp
+                               : reinterpret_cast<const bf16_t*>(a.c.weight.p) + (in ? t : 0l) * a.c.weight.row;
+  const bf16_t* x = reinterpret_cast<const bf16_t*>(a.p.x) + n * a.p.wp;
+  float16v acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+  for (int k = 0; k < a.p.wp; k += U * STEP) {             // (zeros behind the last channel change no sum)
+    Frag<bf16_t> fw[U], fx[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      fw[u].load(w, k + u * STEP, h, a.p.wp, in);
+      fx[u].load(x, k + u * STEP, h, a.p.wp, in);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) Frag<bf16_t>::multiply(acc, fw[u], fx[u]);
+  }
+  float own = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) own = 8 * (i / 4) + 4 * h + i % 4 == r ? acc[i] : own;
+  if (in && ((r >> 2) & 1) == h) a.p.target_logit[n] = own;
+}
+
 // all blocks of TB rows from n0 on by NT threads, and their losses
 template <int TB, int NT>
 __device__ __forceinline__ void row_losses(const CeArgs& a, long n0, float (&sm)[NT], float (&sl)[NT]) {
@@ -288,9 +310,7 @@ __device__ __forceinline__ void row_losses(const CeArgs& a, long n0, float (&sm)
   const bool counts = a.p.target[n] >= 0;
   const float log2_l = __builtin_amdgcn_logf(r.l);
   float loss = counts ? fmaf(a.c.scale, r.m - a.p.target_logit[n], log2_l * LN2) : 0.f;
-  // The target's logit is a sum of its own (rows_kernel), whose order is not the products': where it is the largest it may come out above its
-  // other self by their roundings, and a probability above 1 would push the gradient the wrong way.  (NaNs stay.)
-  if (loss < 0.f) loss = 0.f;
+  if (loss < 0.f) loss = 0.f;                              // (a sum that is 1 may come out as 1 less a rounding; NaNs stay)
   a.p.lse[n] = counts ? fmaf(r.m, a.to_log2, log2_l) : INFINITY;
   a.p.at_target[n] = counts ? expm1f(-loss) : 0.f;
   a.p.rows[n] = loss;
@@ -353,7 +373,7 @@ template <typename T, int GRAD_V>
 __global__ __launch_bounds__(NTHR) void grad_kernel(CeArgs a, Divisor by_row) {
   if (blockIdx.x >= a.grad_blocks) {
     const long n = (long)(blockIdx.x - a.grad_blocks) * 4 + (threadIdx.x >> 6);
-    if (n < a.p.np) copy_row<T>(a, n, threadIdx.x & 63, a.p.target[n] >= 0, nullptr);
+    if (n < a.p.np) copy_row<T>(a, n, threadIdx.x & 63, a.p.target[n] >= 0);
     return;
   }
   const unsigned per = by_row.d;
@@ -725,6 +745,8 @@ struct Run {
       GemmArgs g = logits_args(0, p.fused);
       g.C = p.sums; g.mode = EPI_VOCAB_SUMS; g.vocab.alpha = a.to_log2;
       CE_TRY(launch_gemm_vocab(g, s));
+      target_kernel<<<(unsigned)((p.np + 127) / 128), NTHR, 0, s>>>(a);
+      CE_TRY(hipGetLastError());
       if (p.fused == c.vocab) return hipSuccess;
       at(p.fused, c.vocab - p.fused);
       CE_TRY(logits());

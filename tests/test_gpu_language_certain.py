@@ -34,6 +34,31 @@ def test_certain_rows_have_no_negative_loss(n, vocab, width, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,width", SIZES + [(100, 1 << 20, 64), (600, 20001, 1000)])
+def test_certain_rows_have_no_loss(n, vocab, width, dtype):
+    """The same rows: a target's logit of 4 width cancels against the largest, bit by bit itself, and what is left is the logarithm of a sum of one
+    term: three exponentials of a step each, two products and the logarithm, 12 f.  (A logit's own rounding is 2 width f and more.)  At 64 channels
+    another of a million entries comes near: its term is known but for both logits' errors, (width + 3) f of the absolute terms' sum each."""
+    w = normal((vocab, width), TYPES[dtype], 1, 2.0)
+    t = torch.randperm(vocab, generator=torch.Generator().manual_seed(2))[:n].int().cuda()
+    t[0] = vocab - 1
+    t[1:][t[1:] == vocab - 1] = 0
+    x = w[t.long()].clone()
+    c = B.make_cross_entropy(x, w, t, mean=False)
+    B.hbp_loss_cross_entropy(c)
+    s = x.double() @ w.double().T
+    s -= s.gather(1, t.long()[:, None])
+    s.scatter_(1, t.long()[:, None], -math.inf)
+    want = torch.log1p(s.exp().sum(1))
+    bound = 12 * R.F + 2 * (width + 3) * R.F * x.double().square().sum(1) * want
+    assert bool((c.row_loss >= 0).all())
+    R.assert_within(c.row_loss, want, bound, "row_loss")
+    along = (c.dweight[t.long()].double() * x.double()).sum(1) / x.double().square().sum(1)              # the coefficients
+    once = torch.bincount(t.long(), minlength=vocab)[t.long()] == 1
+    R.assert_within(along[once], torch.expm1(-want)[once], bound[once] + 2.0 ** -8 * want[once], "coefficients")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("scale", [1.0, 0.7])
 @pytest.mark.parametrize("n,vocab,width", SIZES + [(1024, 9216, 128)])
 def test_losses_of_equal_exact_logits(n, vocab, width, scale, dtype):
