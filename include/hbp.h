@@ -486,7 +486,8 @@ hbp_status hbp_embedding_backward(const hbp_embedding_desc* desc, const hbp_embe
  * Other rows (padding) have row_loss 0 and a dx of zeros, and nothing in their x reaches any result; where no row counts
  * the loss is 0 and dweight zeros, whatever weight holds.  The vocabulary is taken in pieces and the logits are not kept.
  * A logit of minus infinity (a weight that masks an entry) has a probability and a dweight of zero; in dx, zero times an infinite weight is NaN.
- * bf16 storage: dS is rounded to bf16 before it meets weight and x; logits, their sums and all products' sums are fp32. */
+ * bf16 storage: dS is rounded to bf16 before it meets weight and x (of up to 128 rows it keeps twice the bits, as few roundings do not average
+ * out); logits, their sums and all products' sums are fp32. */
 typedef struct {
   uint32_t struct_size;      /* = sizeof(hbp_cross_entropy_desc) */
   int32_t dtype;             /* hbp_dtype of x, weight, dx */

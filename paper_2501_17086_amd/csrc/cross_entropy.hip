@@ -13,9 +13,9 @@
 // Logits lie [vocabulary][rows]: the vocabulary may have any size (it is the product's rows), the number of rows is filled up
 // with zeros to a multiple of 8 or 256, and both gradients' products find their contraction where the kernels want it.
 // Rows whose target is no token take no part: they are zeros in the copy of x that the products read, so that not even
-// an infinity or a NaN in them reaches the others.  Logits, sums, dx and dweight are held in fp32; dS is rounded to the storage type once, as the
-// matrix instructions want it, with a power of two as its factor (the rest of the factor comes after the products), and dx gets back what
-// that leaves out of the target's coefficient, the one that a confident row is made of.
+// an infinity or a NaN in them reaches the others.  Logits, sums, dx and dweight are held in fp32; dS is rounded to the storage type once (twice the bits
+// for few rows, TWO_TERMS), as the matrix instructions want it, with a power of two as its factor (the rest of the factor comes after the
+// products), and dx gets back what that leaves out of the target's coefficient, the one that a confident row is made of.
 #include "hbp_common.h"
 
 namespace hbp {
@@ -28,7 +28,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int BLOCK_V = 64;                                // rows of the vocabulary whose sum is one number per row of x
 
 struct Parts {
-  void* x;                // [np, wp], storage type: x, zeros where a row does not count and behind its channels
+  void* x;                // [gp, wp], storage type: x, zeros where a row does not count and behind its channels; once for each term of dS
   void* weight;           // [vocab, wp]: the weights with zeros behind their channels, where wp is not the width; else NULL
   float* target_logit;    // [np]
   float* lse;             // [np], base 2; infinity where a row does not count: its probabilities are zeros
@@ -38,10 +38,10 @@ struct Parts {
   float* scalars;         // [2]: the factor on dS, and what dx and dweight are multiplied by afterwards
   float2* sums;           // [blocks][np]: a block's largest logit, and its sum of exponentials relative to that
   float* logits;          // [piece][np]
-  void* grad;             // [piece][np], storage type (fp32: the logits' place)
-  float* dx;              // [shares][np, wp]
+  void* grad;             // [piece][gp], storage type (fp32: the logits' place); of two terms the second behind the first
+  float* dx;              // [shares][gp, wp]
   float* dweight;         // [shares of the contraction][rows at hand, width], where there are several
-  long np, piece;
+  long np, gp, piece;     // gp: np once for each term of dS
   int wp;                 // channels with those that fill up
   long fused;             // rows of the vocabulary whose logits meet no memory
   int blocks, pieces, shares;   // shares: products whose results lie side by side until they are added up
@@ -63,10 +63,12 @@ struct CeArgs {
 template <typename T>
 __device__ __forceinline__ void copy_row(const CeArgs& a, long n, int lane, bool counts) {
   T* copy = reinterpret_cast<T*>(a.p.x) + n * a.p.wp;
+  const bool twice = a.p.gp > a.p.np;
   for (int c = 8 * lane; c < a.p.wp; c += 512) {
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (counts && c < a.c.width) load8(reinterpret_cast<const T*>(a.c.x.p) + n * a.c.x.row + c, v);
     store8(copy + c, v);
+    if (twice) store8(copy + a.p.np * a.p.wp + c, v);
   }
 }
 __device__ __forceinline__ int target_of(const CeArgs& a, long n) {
@@ -367,6 +369,7 @@ __global__ __launch_bounds__(1024) void few_loss_kernel(CeArgs a) {
   whole_loss(a, sum, cnt);
 }
 
+__device__ __forceinline__ float bf16_of(float v) { return __uint_as_float(pack_bf16x2(0.f, v) & 0xFFFF0000u); }
 // dS of a piece: 8 rows of x and GRAD_V rows of the vocabulary a thread, whose logits go out together.  (Four: 1000 rows against 32000 x 256 fp32, all
 // in all, 664 us, one 703; a small problem, which needs the threads, 35.1 and 33.2.)
 template <typename T, int GRAD_V>
@@ -406,7 +409,14 @@ __global__ __launch_bounds__(NTHR) void grad_kernel(CeArgs a, Divisor by_row) {
       for (int j = 0; j < 8; ++j)
         if (target[j] == a.v0 + v + i) s[j] = a.p.at_target[n + j] * g;
     }
-    store8(reinterpret_cast<T*>(a.p.grad) + (a.grad0 + v + i) * a.p.np + n, s);
+    T* to = reinterpret_cast<T*>(a.p.grad) + (a.grad0 + v + i) * a.p.gp + n;
+    store8(to, s);
+    if constexpr (sizeof(T) == 2)
+      if (a.p.gp > a.p.np) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] -= bf16_of(s[j]);
+        store8(to + a.p.np, s);
+      }
   }
 }
 
@@ -436,16 +446,17 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
   const long c = 8l * (r - q * per);
   float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (a.p.target[n] >= 0) {
+    const bool twice = a.p.gp > a.p.np;
 #pragma unroll 4
-    for (int k = 0; k < shares; ++k) {
+    for (int k = 0; k < (twice ? 2 * shares : shares); ++k) {          // (two terms: 2 np rows a share, row n of either)
       float v[8];
       load8(a.p.dx + ((long)k * a.p.np + n) * a.p.wp + c, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += v[j];
     }
     if constexpr (sizeof(T) == 2) {      // a confident row's dx is next to its target's coefficient times a row of the weights: what
-      const float g = a.p.at_target[n] * a.p.scalars[0], rest = g - __uint_as_float(pack_bf16x2(0.f, g) & 0xFFFF0000u);   // its rounding
-      float w[8];                                                                                                // left out
+      const float g = a.p.at_target[n] * a.p.scalars[0], rest = twice ? 0.f : g - bf16_of(g);   // its rounding left out
+      float w[8];
       load8(reinterpret_cast<const T*>(a.c.weight.p) + (long)a.p.target[n] * a.c.weight.row + c, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = fmaf(rest, w[j], s[j]);
@@ -500,6 +511,12 @@ bool small_problem(const Parts& p, long vocab, int width) {
 constexpr size_t PIECE_BYTES = 1ul << 30;
 constexpr long PIECE_ROWS = 1l << 20;
 constexpr int MAX_SPLIT = 16;
+// bf16 of up to so many rows, their logits in memory: dS keeps two terms, what its rounding leaves out rounded in turn, side by side in one product
+// each.  A row of dweight is the sum of few coefficients then, down to one, and would take over their roundings whole.  Relative L2 of dweight in bf16, of
+// which 0.0017 is the result's own rounding, with two terms / one: 1 row against 50 x 64 0.0018 / 0.0034, 5 against 70 x 2048 0.0017 / 0.0028, 100 against
+// 30000 x 264 0.0017 / 0.0020; beyond, 130 against 700 x 1024 - / 0.0021, 4000 against 256 x 1024 - / 0.0019.  Time, us: 64 against 5000 x 256 31.3 / 28.5, 32
+// against 131072 x 2048 383 / 367, 100 against 131072 x 1024 346 / 329.
+constexpr long TWO_TERMS = 128;
 
 // Channels are filled up with zeros to a multiple of 32, and to one of 256 where that is an eighth more at most, for the sake of the
 // 256 x 256 kernel; the weights are copied for it, which takes as long as one of the four products with 500 rows of x.
@@ -604,7 +621,8 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.pieces = (int)((vocab + p.piece - 1) / p.piece);
   if (p.piece > vocab) p.piece = vocab;
   p.blocks = p.fused ? (int)(p.fused / 128 + (vocab - p.fused + BLOCK_V - 1) / BLOCK_V) : (int)((vocab + BLOCK_V - 1) / BLOCK_V);
-  p.x = take(p.np * p.wp * es);
+  p.gp = gradients && dtype == 1 && !p.fused && p.np <= TWO_TERMS ? 2 * p.np : p.np;
+  p.x = take(p.gp * p.wp * es);
   if (p.wp != width) p.weight = take((size_t)vocab * p.wp * es);
   p.target_logit = reinterpret_cast<float*>(take(4 * p.np));
   p.lse = reinterpret_cast<float*>(take(4 * p.np));
@@ -616,15 +634,15 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.logits = reinterpret_cast<float*>(take((size_t)(p.fused ? vocab - p.fused : p.piece) * p.np * 4));
   p.grad = p.logits;
   if (gradients) {
-    if (dtype == 1) p.grad = take((size_t)p.piece * p.np * 2);
+    if (dtype == 1) p.grad = take((size_t)p.piece * p.gp * 2);
     // as many as there are, and of many pieces the largest product's, what was added up before it, and a rest, four at least
     const long last_piece = vocab - (p.pieces - 1) * p.piece;
-    const DxParts each = dx_parts(dtype, p.np ? p.np : 8, p.wp, p.piece), end = dx_parts(dtype, p.np ? p.np : 8, p.wp, last_piece);
+    const DxParts each = dx_parts(dtype, p.gp ? p.gp : 8, p.wp, p.piece), end = dx_parts(dtype, p.gp ? p.gp : 8, p.wp, last_piece);
     const long all = (p.pieces - 1l) * (each.split + each.rest) + end.split + end.rest, split = each.split > end.split ? each.split : end.split;
     const long room = split + 2 < 4 ? 4 : split + 2;
     p.shares = (int)(all < room ? all : room);
-    p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.np * p.wp * 4));
-    const size_t most = dweight_room(dtype, p.np, width, p.piece), last = dweight_room(dtype, p.np, width, last_piece);
+    p.dx = reinterpret_cast<float*>(take((size_t)p.shares * p.gp * p.wp * 4));
+    const size_t most = dweight_room(dtype, p.gp, width, p.piece), last = dweight_room(dtype, p.gp, width, last_piece);
     p.dweight_bytes = most > last ? most : last;
     p.dweight = reinterpret_cast<float*>(take(p.dweight_bytes));
   }
@@ -638,10 +656,10 @@ bool fits(const Parts& p, int dtype, long vocab, int width) {
   for (int i = 0; i < p.pieces; ++i) {
     const long v0 = i * p.piece, nv = vocab - v0 < p.piece ? vocab - v0 : p.piece;
     for (long r = 0, n; r < nv; r += n) {
-      n = dweight_rows_of(dtype, p.np, width, nv - r);
-      if (dweight_part(dtype, p.np, width, n) > p.dweight_bytes) return false;
+      n = dweight_rows_of(dtype, p.gp, width, nv - r);
+      if (dweight_part(dtype, p.gp, width, n) > p.dweight_bytes) return false;
     }
-    const DxParts d = dx_parts(dtype, p.np, p.wp, nv);
+    const DxParts d = dx_parts(dtype, p.gp, p.wp, nv);
     for (const int k : {d.split, d.rest}) {
       if (shares + k > p.shares) shares = 1;               // (Run::fold)
       if (shares + k > p.shares) return false;
@@ -734,7 +752,7 @@ struct Run {
     return hipGetLastError();
   }
   hipError_t fold() {
-    const long n8 = p.np * p.wp / 8;
+    const long n8 = p.gp * p.wp / 8;
     fold_kernel<<<(unsigned)((n8 + NTHR - 1) / NTHR), NTHR, 0, s>>>(p.dx, n8, shares);
     shares = 1;
     return hipGetLastError();
@@ -779,11 +797,11 @@ struct Run {
     return softmax_grad();
   }
   hipError_t dweight_rows(long v0, long r0, long nr) {
-    const int n = dweight_split(DTYPE, p.np, c.width, nr);
+    const int n = dweight_split(DTYPE, p.gp, c.width, nr);
     GemmArgs g = plain();
-    g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = p.np; g.a_sk = 1;
+    g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.gp; g.a_sm = p.gp; g.a_sk = 1;
     g.B = p.x; g.b_sk = p.wp; g.b_sn = 1;
-    g.M = nr; g.N = c.width; g.K = p.np;
+    g.M = nr; g.N = c.width; g.K = p.gp;
     const long o = (v0 + r0) * c.dweight.row;
     float* f = reinterpret_cast<float*>(c.dweight.p) + o;
     bf16_t* b = reinterpret_cast<bf16_t*>(c.dweight.p) + o;
@@ -792,10 +810,10 @@ struct Run {
       if (g.c_is_f32) g.C = f; else g.C = b;
       g.ldc = c.dweight.row;
       g.scale = DTYPE == 1 ? p.scalars + 1 : nullptr;
-      return by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr));
+      return by_columns(g, dweight_wide(DTYPE, p.gp, c.width, nr));
     }
     g.c_is_f32 = 1; g.C = p.dweight; g.ldc = c.width; g.c_sb = nr * c.width; g.split_k = n;
-    CE_TRY(by_columns(g, dweight_wide(DTYPE, p.np, c.width, nr)));
+    CE_TRY(by_columns(g, dweight_wide(DTYPE, p.gp, c.width, nr)));
     const long n8 = nr * c.width / 8;
     const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR);
     const Divisor per((unsigned)(c.width / 8));
@@ -805,25 +823,25 @@ struct Run {
   }
   hipError_t dweight(long v0, long nv) {
     for (long r = 0, n; r < nv; r += n) {
-      n = dweight_rows_of(DTYPE, p.np, c.width, nv - r);
+      n = dweight_rows_of(DTYPE, p.gp, c.width, nv - r);
       CE_TRY(dweight_rows(v0, r, n));
     }
     return hipSuccess;
   }
   hipError_t dx_rows(long v0, long r0, long nr, int split) {
     GemmArgs g = plain();
-    g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.np; g.a_sm = 1; g.a_sk = p.np;
+    g.A = reinterpret_cast<const T*>(p.grad) + r0 * p.gp; g.a_sm = 1; g.a_sk = p.gp;
     g.B = weight_at(v0 + r0); g.b_sk = weight_row(); g.b_sn = 1;
     if (shares + split > p.shares) CE_TRY(fold());
-    g.C = p.dx + (long)shares * p.np * p.wp; g.ldc = p.wp; g.c_is_f32 = 1;
-    g.c_sb = p.np * p.wp;
+    g.C = p.dx + (long)shares * p.gp * p.wp; g.ldc = p.wp; g.c_is_f32 = 1;
+    g.c_sb = p.gp * p.wp;
     g.split_k = split;
     shares += split;
-    g.M = p.np; g.N = p.wp; g.K = nr;
-    return by_columns(g, dx_wide(DTYPE, p.np, p.wp, nr));
+    g.M = p.gp; g.N = p.wp; g.K = nr;
+    return by_columns(g, dx_wide(DTYPE, p.gp, p.wp, nr));
   }
   hipError_t dx(long v0, long nv) {
-    const DxParts d = dx_parts(DTYPE, p.np, p.wp, nv);
+    const DxParts d = dx_parts(DTYPE, p.gp, p.wp, nv);
     CE_TRY(dx_rows(v0, 0, d.whole, d.split));
     return d.rest ? dx_rows(v0, d.whole, nv - d.whole, d.rest) : hipSuccess;
   }

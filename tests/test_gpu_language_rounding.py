@@ -63,3 +63,19 @@ def test_gradients_of_plain_rows(n, vocab, width, grad):
     assert off(c.dweight, want["dweight"][0]) < ONE * (math.sqrt(2) if grad == torch.bfloat16 else 1)
     assert off(c.dx, want["dx"][0]) < ONE * math.sqrt(2)
     assert off(c.loss, want["loss"][0]) < 16 * R.F and off(c.row_loss, want["row_loss"][0]) < 16 * R.F
+
+
+@pytest.mark.parametrize("n,vocab,width", [(1, 50, 64), (1, 131072, 1024), (2, 300, 128), (5, 70, 2048), (8, 16384, 256), (64, 5000, 256), (128, 700, 1032),
+                                           (120, 30000, 264), (3, (1 << 20) + 300, 8)])
+def test_gradients_of_few_rows(n, vocab, width):
+    """A row of dweight is a sum of few coefficients, whose roundings do not average out: dS keeps two terms here, each rounding half a step, 2^-8 of what
+    the one before left out, 2^-16 together.  Beside it the logits' own errors in a coefficient, (width + 3) f of their size at most and a fraction
+    of it on the average: as much again."""
+    x, w = normal((n, width), torch.bfloat16, 1), normal((vocab, width), torch.bfloat16, 2, 1.0 / math.sqrt(width))
+    t = torch.randint(0, vocab, (n,), generator=torch.Generator().manual_seed(3)).int().cuda()
+    want = R.cross_entropy(x, w, t)
+    for grad in (torch.float32, torch.bfloat16):
+        c = B.make_cross_entropy(x, w, t, dweight=torch.empty((vocab, width), dtype=grad, device="cuda"))
+        B.hbp_loss_cross_entropy(c)
+        assert off(c.dweight, want["dweight"][0]) < (2.0 ** -15 if grad == torch.float32 else 1.1 * ONE)
+        assert off(c.dx, want["dx"][0]) < 1.1 * ONE
