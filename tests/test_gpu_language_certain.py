@@ -34,7 +34,7 @@ def test_certain_rows_have_no_negative_loss(n, vocab, width, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,vocab,width", SIZES + [(100, 1 << 20, 64), (600, 20001, 1000)])
+@pytest.mark.parametrize("n,vocab,width", SIZES + [(100, 1 << 20, 64), (600, 20001, 1000), (1000, 9300, 160)])
 def test_certain_rows_have_no_loss(n, vocab, width, dtype):
     """The same rows: a target's logit of 4 width cancels against the largest, bit by bit itself, and what is left is the logarithm of a sum of one
     term: three exponentials of a step each, two products and the logarithm, 12 f.  (A logit's own rounding is 2 width f and more.)  At 64 channels
