@@ -494,7 +494,8 @@ typedef struct {
   int32_t grad_dtype;        /* hbp_dtype of dweight: HBP_F32, or dtype */
   int32_t mean;              /* 0 or 1 */
   float scale;               /* > 0, at most 2^127; usually 1 */
-  float factor;              /* finite; usually 1 (a loss scale, or one over the number of batches whose gradients are added) */
+  float factor;              /* finite; usually 1 (a loss scale, or one over the number of batches whose gradients the caller adds up: dx and
+                              * dweight are written, not added to) */
   int64_t rows;              /* 0 .. 2^20 */
   int64_t vocab;             /* 1 .. 2^24 */
   int64_t width;

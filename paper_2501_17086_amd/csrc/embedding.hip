@@ -1,8 +1,9 @@
 // The embedding of a language model's tokens, its gradient, and dropout.
 //
 // All of it is bound by memory: a unit of 8 channels is read once and written once, one product an element, and with dropout ten
-// rounds of two wide integer products a unit.  Dropout of 16384 x 2048 bf16 onto a residual 37 us (5.4 TB/s; a copy: 5.1); the embedding
-// of 32768 tokens in 256 channels with dropout 8.0 us; calls of a few rows 6.7, which is the host's share of a launch.
+// rounds of two wide integer products a unit.  Calls, one after the other: dropout of 16384 x 2048 bf16 onto a residual 36.7 us with rows from memory
+// (5.5 TB/s; a copy: 5.1), 28.3 with the same rows again and again, which the memory side's cache holds; the embedding of 32768 tokens in 256 channels
+// with dropout 8.0 us; calls of a few rows 6.7, which is the host's share of a launch.
 //
 // The gradient adds up rows of the same token, in 32 bits and in an order that does not change from run to run, so without atomics on
 // its sums.  Tokens are sorted (least significant digit first, up to 9 bits a pass, stable, so that a token's rows stay in order);
@@ -10,8 +11,8 @@
 // Text repeats few tokens very often: 16 sorted places that begin at a multiple of 16 and hold one token are added up beforehand by a
 // workgroup of their own, and the table's row adds that sum.  A table's row is written once, rows without tokens as zeros: that is most
 // of the bytes.
-// Measured: 16384 tokens, a tenth of them none, into 131072 x 2048 250 us, 215 of them the table's write (5 TB/s); 32768 into 16384 x 256 with
-// dropout 45: sorting 24, chunks 7, the table 16.
+// Measured: 16384 tokens, a tenth of them none, into 131072 x 2048 a call of 251 us, its kernels 24 for the sort, 13 chunks, 213 the table (1.07 GB
+// written, 5 TB/s); 32768 into 16384 x 256 with dropout a call of 44, its kernels (traced) 26, 7 and 16.
 #include "philox.h"
 
 namespace hbp {
@@ -38,7 +39,8 @@ __device__ __forceinline__ void keep8(unsigned mask, float factor, float (&v)[8]
   for (int j = 0; j < 8; ++j) v[j] = (mask >> j) & 1u ? v[j] * factor : 0.f;
 }
 
-// (One unit a thread: 16384 x 2048 bf16 onto a residual 30.1 us, two 30.4, four 32.0; 65536 x 2048 without 90, 100, 100.)
+// (Kernel times, the same rows again and again: one unit a thread 16384 x 2048 bf16 onto a residual 30.1 us, two 30.4, four 32.0; 65536 x 2048 without 90,
+// 100, 100.)
 template <typename T, bool RES>
 __global__ __launch_bounds__(NTHR) void dropout_kernel(DropoutArgs a, DropoutKey key, Units u) {
   const long base = (long)blockIdx.x * NTHR;

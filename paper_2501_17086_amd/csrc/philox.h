@@ -6,8 +6,8 @@
 namespace hbp {
 
 // Eight consecutive elements of a row are one call, 16 bits each: an element is left out where its bits are below the threshold, so
-// rates are multiples of 2^-16.  (32 bits each would be two calls of 20 wide products: 16384 x 2048 in bf16 onto a residual 32.2 -> 37.0 us,
-// bound by them and not by memory.)
+// rates are multiples of 2^-16.  (32 bits each would be two calls of 20 wide products: 16384 x 2048 in bf16 onto a residual 28.3 -> 29.0 us with the same
+// rows again and again, which the memory side's cache holds.)
 struct DropoutKey {
   unsigned k0, k1;            // seed
   unsigned long offset;
