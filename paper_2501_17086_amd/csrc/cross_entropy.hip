@@ -26,6 +26,7 @@ namespace {
 typedef float float16v __attribute__((ext_vector_type(16)));
 constexpr int NTHR = 256;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int AFTER = 4;                                   // (16 bytes on)
 constexpr int BLOCK_V = 64;                                // rows of the vocabulary whose sum is one number per row of x
 
 struct Parts {
@@ -36,7 +37,7 @@ struct Parts {
   int* target;            // [np], -1 where a row does not count
   float* rows;            // [np] row losses
   float* at_target;       // [np] the target's softmax less 1
-  float* scalars;         // [2]: the factor on dS, and what dx and dweight are multiplied by afterwards
+  float* scalars;         // [0]: the factor on dS; [AFTER]: what dx and dweight are multiplied by afterwards
   float2* sums;           // [blocks][np]: a block's largest logit, and its sum of exponentials relative to that
   float* logits;          // [piece][np]
   void* grad;             // [piece][gp], storage type (fp32: the logits' place); of two terms the second behind the first
@@ -345,7 +346,7 @@ __device__ __forceinline__ void whole_loss(const CeArgs& a, double (&sum)[1024],
     const double m = frexp(g, &e);
     const bool apart = a.power && g != 0.0 && e > -100 && e < 100;
     a.p.scalars[0] = (float)(apart ? ldexp(1.0, e - 1) : g);
-    a.p.scalars[1] = apart ? (float)(2.0 * m) : 1.f;
+    a.p.scalars[AFTER] = apart ? (float)(2.0 * m) : 1.f;
   }
 }
 template <int TB>
@@ -462,7 +463,7 @@ __global__ __launch_bounds__(NTHR) void dx_kernel(CeArgs a, Divisor by_row, int 
       load8(reinterpret_cast<const T*>(a.c.weight.p) + (long)a.p.target[n] * a.c.weight.row + c, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = fmaf(rest, w[j], s[j]);
-      const float f = a.p.scalars[1];
+      const float f = a.p.scalars[AFTER];
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] *= f;
     }
@@ -631,7 +632,7 @@ Parts carve(char* base, int dtype, long rows, long vocab, int width, bool gradie
   p.target = reinterpret_cast<int*>(take(4 * p.np));
   p.rows = reinterpret_cast<float*>(take(4 * p.np));
   p.at_target = reinterpret_cast<float*>(take(4 * p.np));
-  p.scalars = reinterpret_cast<float*>(take(16));
+  p.scalars = reinterpret_cast<float*>(take(4 * (AFTER + 1)));
   p.sums = reinterpret_cast<float2*>(take((size_t)p.blocks * p.np * 8));
   p.logits = reinterpret_cast<float*>(take((size_t)(p.fused ? vocab - p.fused : p.piece) * p.np * 4));
   p.grad = p.logits;
@@ -675,7 +676,7 @@ hipError_t product(int dtype, const GemmArgs& g, hipStream_t s) {
   if (dtype == 1) {
     hipError_t e;
     if (launch_gemm_mfma(g, s, &e)) return e;
-    if (g.scale) return hipErrorInvalidValue;
+    if (g.mode == EPI_SCALED) return hipErrorInvalidValue;
   } else if (gemm_f32_ok(g)) {
     return launch_gemm_f32(g, s);
   }
@@ -811,7 +812,7 @@ struct Run {
       g.c_is_f32 = c.grad_dtype == 0;
       if (g.c_is_f32) g.C = f; else g.C = b;
       g.ldc = c.dweight.row;
-      g.scale = DTYPE == 1 ? p.scalars + 1 : nullptr;
+      if (DTYPE == 1) { g.mode = EPI_SCALED; g.lambda = p.scalars + AFTER; }
       return by_columns(g, dweight_wide(DTYPE, p.gp, c.width, nr));
     }
     g.c_is_f32 = 1; g.C = p.dweight; g.ldc = c.width; g.c_sb = nr * c.width; g.split_k = n;
@@ -819,8 +820,8 @@ struct Run {
     const long n8 = nr * c.width / 8;
     const unsigned blocks = (unsigned)((n8 + NTHR - 1) / NTHR);
     const Divisor per((unsigned)(c.width / 8));
-    if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per, p.scalars + 1);
-    else dweight_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(p.dweight, b, c.dweight.row, n8, n, per, p.scalars + 1);
+    if (c.grad_dtype == 0) dweight_kernel<float><<<blocks, NTHR, 0, s>>>(p.dweight, f, c.dweight.row, n8, n, per, p.scalars + AFTER);
+    else dweight_kernel<bf16_t><<<blocks, NTHR, 0, s>>>(p.dweight, b, c.dweight.row, n8, n, per, p.scalars + AFTER);
     return hipGetLastError();
   }
   hipError_t dweight(long v0, long nv) {

@@ -195,8 +195,8 @@ enum FastEpi {
   FAST_ACT_GELU = 7,   // C(bf16) = gelu(acc), out2(bf16) = gelu'(acc)   (forward: z and act')
   FAST_VOCAB_SUMS = 8, // sums over 128 rows (EPI_VOCAB_SUMS)
   FAST_VOCAB_GRAD = 9, // C(bf16) = gain (2^(alpha acc - lse[n]) - onehot)
-  FAST_SCALED = 10,    // C(bf16) = *scale acc
-  FAST_SCALED_F32 = 11 // C(fp32) = *scale acc
+  FAST_SCALED = 10,    // C(bf16) = *lambda acc
+  FAST_SCALED_F32 = 11 // C(fp32) = *lambda acc
 };
 
 // What a vocabulary's logits are formed for (cross_entropy.hip); rows are the vocabulary's, columns those of x.  Measured, M x N x K, kernel times on a
@@ -239,7 +239,7 @@ __device__ __forceinline__ void epilogue_f32(const GemmArgs& g, const TileCoord&
                                              int lane) {
   const long cb = g.split_k > 1 ? ((long)tc.split * g.batch + tc.batch) * g.c_sb : tc.batch * g.c_sb;
   float* c = reinterpret_cast<float*>(g.C) + cb + (tc.m0 + wm0 + (lane & 31)) * g.ldc + tc.n0 + wn0 + 4 * (lane >> 5);
-  const float f = SCALED ? *g.scale : 1.f;
+  const float f = SCALED ? *g.lambda : 1.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -323,7 +323,7 @@ __device__ __forceinline__ void epilogue_staged_fn(const GemmArgs& g, const Tile
   float lse[8][4];
   unsigned long on = ~0ul;
   uint4v keep = {~0u, ~0u, ~0u, ~0u};
-  const float scale = FAST == FAST_SCALED ? *g.scale : 1.f;
+  const float scale = FAST == FAST_SCALED ? *g.lambda : 1.f;
   float gain = 0.f, at_target = 0.f;
   int target = 0;
   if (VOCAB) {
@@ -762,6 +762,7 @@ inline bool has_lean(const GemmArgs& g, bool a_kc, bool b_kc) {
   if (!a_kc) return g.mode == EPI_STORE && !g.addf && (g.c_is_f32 || g.split_k > 1);     // parameter gradients
   if (g.addf || (g.split_k > 1 && b_kc)) return false;
   if (g.split_k > 1) return g.mode == EPI_STORE && g.batch == 1;                         // a vocabulary's gradient in shares
+  if (g.mode == EPI_SCALED) return true;
   if (g.c_is_f32) return g.mode == EPI_STORE && (b_kc || g.batch == 1);   // the recurrent kinds' U xin; a vocabulary's gradient
   if (g.mode == EPI_STORE) return true;
   if (!b_kc) return g.mode == EPI_MUL_AUX || g.mode == EPI_MUL_1MZ2 || g.mode == EPI_ADD_AUX;   // block VJPs
@@ -769,7 +770,7 @@ inline bool has_lean(const GemmArgs& g, bool a_kc, bool b_kc) {
   return g.mode == EPI_RESID && g.aux && !g.lambda_mn;
 }
 hipError_t launch_lean_nn(const GemmArgs& g, hipStream_t s) {
-  if (g.scale) {
+  if (g.mode == EPI_SCALED) {
     const bool pair = g.K % (2 * BK) == 0;
     if (g.c_is_f32)
       return pair ? launch_lean_walk<true, false, FAST_SCALED_F32, false, true>(g, s) : launch_lean_walk<true, false, FAST_SCALED_F32, false, false>(g, s);
@@ -813,7 +814,7 @@ GemmArgs part_of(const GemmArgs& g, long m0, long m1, long n0, long n1) {
   if (g.aux) p.aux = reinterpret_cast<const bf16_t*>(g.aux) + o;
   if (g.out2) p.out2 = reinterpret_cast<bf16_t*>(g.out2) + o;
   if (g.addf) p.addf = g.addf + o;
-  if (g.lambda) p.lambda = g.lambda + n0;
+  if (g.lambda && g.mode != EPI_SCALED) p.lambda = g.lambda + n0;
   if (g.lambda_mn) p.lambda_mn = reinterpret_cast<const bf16_t*>(g.lambda_mn) + o;
   return p;
 }
@@ -838,7 +839,7 @@ bool covered(const GemmArgs& g) {
     return false;
   if (lda > (1L << 22) || ldb > (1L << 22)) return false;   // per-lane source offsets are 32-bit
   if (g.split_k > 1 && g.mode != EPI_STORE) return false;
-  if (g.scale && (g.split_k > 1 || g.batch > 1 || g.mode != EPI_STORE || g.addf || !a_kc || b_kc)) return false;
+  if (g.mode == EPI_SCALED && (g.batch > 1 || g.addf || !a_kc || b_kc)) return false;
   if (g.M <= 0 || g.N <= 0 || g.K <= 0 || g.batch <= 0 || g.split_k <= 0) return false;
   const bool act = g.mode == EPI_ACT_GELU || g.mode == EPI_ACT_TANH;
   return (a_kc && (b_kc || (b_rc && !act))) || (a_rc && b_rc && !act);
@@ -848,7 +849,7 @@ enum Lean { LEAN_NOT, LEAN_WHOLE, LEAN_PART };
 Lean lean_share(const GemmArgs& g) {
   const bool a_kc = g.a_sk == 1, b_kc = g.b_sk == 1;
   // (a fused operand is asked for two slices before a tile's end, the first two being waited for otherwise: four at least)
-  if (!has_lean(g, a_kc, b_kc) || g.K % BK != 0 || g.K / BK < g.split_k || (g.mode != EPI_STORE && g.K < 4 * BK)) return LEAN_NOT;
+  if (!has_lean(g, a_kc, b_kc) || g.K % BK != 0 || g.K / BK < g.split_k || (g.mode != EPI_STORE && g.mode != EPI_SCALED && g.K < 4 * BK)) return LEAN_NOT;
   const long hm = g.M / BM * BM, hn = g.N / BN * BN;
   const long tiles = (hm / BM) * (hn / BN) * g.batch * g.split_k;
   if (hm == g.M && hn == g.N) return gemm_fills_chip(tiles) ? LEAN_WHOLE : LEAN_NOT;

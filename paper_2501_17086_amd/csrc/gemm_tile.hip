@@ -70,8 +70,9 @@ __device__ __forceinline__ bool fuses_aux(const GemmArgs& g) {
   return g.split_k == 1 && (g.mode == EPI_MUL_AUX || g.mode == EPI_MUL_1MZ2 || g.mode == EPI_RESID || g.mode == EPI_ADD_AUX);
 }
 // 8 consecutive sums of a row, at element off of C: what the launch fuses, and the store.  ra: the fused operand there; lm: the
-// columns' coefficients (EPI_RESID without coefficients per element).
-template <bool ACT>
+// columns' coefficients (EPI_RESID without coefficients per element).  SCALED: EPI_SCALED is among the modes, which no group has (its
+// test took 3 to 4 % of other layouts' short launches).
+template <bool ACT, bool SCALED>
 __device__ __forceinline__ void finish8(const GemmArgs& g, long batch, int split, long off, bool use_aux, float (&v)[8],
                                         const Raw8<bf16_t>& ra, const float (&lm)[8]) {
   if (g.split_k > 1) {
@@ -112,9 +113,8 @@ __device__ __forceinline__ void finish8(const GemmArgs& g, long batch, int split
 #pragma unroll
       for (int x = 0; x < 8; ++x) v[x] = fmaf(g.lambda_mn ? l8[x] : lm[x], f[x], v[x]);
     }
-  }
-  if (!ACT && g.scale) {
-    const float f = *g.scale;
+  } else if (SCALED && g.mode == EPI_SCALED) {
+    const float f = *g.lambda;
 #pragma unroll
     for (int x = 0; x < 8; ++x) v[x] *= f;
   }
@@ -124,7 +124,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& g, long batch, int split
 
 // T x T output tile per workgroup, a ring of NST stages, WGS workgroups per compute unit.  ACT: the forward's activations (kept
 // out of the other kernels' registers).  t: the tile's number in the product's list.
-template <int T, int BK, int NST, bool A_KC, bool B_KC, bool ACT>
+template <int T, int BK, int NST, bool A_KC, bool B_KC, bool ACT, bool SCALED>
 __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, int tiles_m, int tiles_n, int t) {
   typedef Tile<T, BK, A_KC> TA;
   typedef Tile<T, BK, B_KC> TB;
@@ -262,7 +262,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, int tiles_m, i
       float v[8];
       load8(stg + (lane / LPR + ps * RPP) * LD + 8 * (lane % LPR), v);
       if (row >= g.M || col >= g.N) continue;
-      finish8<ACT>(g, batch, split, row * g.ldc + col, use_aux, v, ra[ps], lm);
+      finish8<ACT, SCALED>(g, batch, split, row * g.ldc + col, use_aux, v, ra[ps], lm);
     }
     __builtin_amdgcn_wave_barrier();                       // the next rows' writes stay behind these reads
   }
@@ -273,7 +273,7 @@ __device__ __forceinline__ int tile_of_id(int per_xcd) { return (int)(blockIdx.x
 template <int T, int BK, int NST, int WGS, bool A_KC, bool B_KC, bool ACT>
 __global__ __launch_bounds__(NTHR, WGS) void gemm_tile_kernel(GemmArgs g, int tiles_m, int tiles_n, int total, int per_xcd) {
   const int t = tile_of_id(per_xcd);
-  if (t < total) gemm_tile_body<T, BK, NST, A_KC, B_KC, ACT>(g, tiles_m, tiles_n, t);
+  if (t < total) gemm_tile_body<T, BK, NST, A_KC, B_KC, ACT, !ACT && A_KC && !B_KC>(g, tiles_m, tiles_n, t);
 }
 // several products' tiles in one list
 template <int T, int BK, int NST, int WGS, bool A_KC, bool B_KC>
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(NTHR, WGS) void gemm_tile_group_kernel(GemmGroup q)
   const int t = tile_of_id(q.per_xcd);
   if (t >= q.total) return;
   const int i = q.of(t);
-  gemm_tile_body<T, BK, NST, A_KC, B_KC, false>(q.g[i], q.tiles_m[i], q.tiles_n[i], t - q.start[i]);
+  gemm_tile_body<T, BK, NST, A_KC, B_KC, false, false>(q.g[i], q.tiles_m[i], q.tiles_n[i], t - q.start[i]);
 }
 
 // Launches of few tiles: a workgroup of four wavefronts owns TM x 32 of C and the wavefronts share the contraction out, each
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(NTHR, WGS) void gemm_tile_group_kernel(GemmGroup q)
 // What bounds such a launch is the time a compute unit takes to stream its tile's operands, about 64 KB of requests in flight over
 // their latency.  Here 96 KB are asked for ahead (the 64 x 64 kernel: 48), over more compute units: 1200 x 256 x 1024 8.3 -> 6.2
 // us, 54 GB/s per compute unit.  The fused operand is asked for before the first slice.
-template <int TM, int STG, bool A_KC, bool B_KC, bool ACT>
+template <int TM, int STG, bool A_KC, bool B_KC, bool ACT, bool SCALED>
 __device__ __forceinline__ void gemm_small_body(const GemmArgs& g, int tiles_m, int tiles_n, int t) {
   constexpr int TN = 32, BK = 64, NB = TM / 32;
   typedef Tile<TM, BK, A_KC, 1> TA;
@@ -418,20 +418,20 @@ __device__ __forceinline__ void gemm_small_body(const GemmArgs& g, int tiles_m, 
 #pragma unroll
     for (int x = 0; x < 8; ++x) v[x] += f[x];
   }
-  finish8<ACT>(g, batch, split, off, use_aux, v, ra, lm);
+  finish8<ACT, SCALED>(g, batch, split, off, use_aux, v, ra, lm);
 }
 
 template <int TM, int STG, bool A_KC, bool B_KC, bool ACT>
 __global__ __launch_bounds__(NTHR, 1) void gemm_small_kernel(GemmArgs g, int tiles_m, int tiles_n, int total, int per_xcd) {
   const int t = tile_of_id(per_xcd);
-  if (t < total) gemm_small_body<TM, STG, A_KC, B_KC, ACT>(g, tiles_m, tiles_n, t);
+  if (t < total) gemm_small_body<TM, STG, A_KC, B_KC, ACT, !ACT && A_KC && !B_KC>(g, tiles_m, tiles_n, t);
 }
 template <int TM, int STG, bool A_KC, bool B_KC>
 __global__ __launch_bounds__(NTHR, 1) void gemm_small_group_kernel(GemmGroup q) {
   const int t = tile_of_id(q.per_xcd);
   if (t >= q.total) return;
   const int i = q.of(t);
-  gemm_small_body<TM, STG, A_KC, B_KC, false>(q.g[i], q.tiles_m[i], q.tiles_n[i], t - q.start[i]);
+  gemm_small_body<TM, STG, A_KC, B_KC, false, false>(q.g[i], q.tiles_m[i], q.tiles_n[i], t - q.start[i]);
 }
 
 template <int T, int BK, int NST, int WGS, bool A_KC, bool B_KC, bool ACT>

@@ -130,7 +130,8 @@ enum EpiMode {
   EPI_ADD_AUX = 6,     // C = acc + aux[m,n]
   // products of a vocabulary's weights (rows m) with rows n (launch_gemm_vocab only; cross_entropy.hip)
   EPI_VOCAB_SUMS = 7,  // C(2 x fp32)[m / 128][n] = the largest acc of those 128 m, the sum of 2^(alpha (acc - it))
-  EPI_VOCAB_GRAD = 8   // C(bf16) = gain (2^(alpha acc - lse[n]) - [row0 + m = target[n]])
+  EPI_VOCAB_GRAD = 8,  // C(bf16) = gain (2^(alpha acc - lse[n]) - [row0 + m = target[n]])
+  EPI_SCALED = 9       // C = *lambda acc, one number (bf16 kernels, one share, A K-contiguous and B not)
 };
 struct VocabEpilogue {
   float alpha;
@@ -151,14 +152,18 @@ struct GemmArgs {
   long a_sb, b_sb, c_sb;  // batch strides (elements)
   int split_k;          // >1: C is fp32 partials [split][batch][M,N] (EPI_STORE only)
   int mode;
-  const void* aux; long aux_sb;       // storage type
-  void* out2; long out2_sb;           // storage type
-  const float* addf; long addf_sb;    // fp32 [M,N], added to acc before the epilogue
-  const float* lambda; long lambda_sb;  // fp32 [N]
+  // (what a product is launched with counts in the smallest: 56 bytes more took 0.8 % of a pass over a small transformer, four products a launch)
+  union {
+    struct {
+      const void* aux; long aux_sb;       // storage type
+      void* out2; long out2_sb;           // storage type
+      const float* addf; long addf_sb;    // fp32 [M,N], added to acc before the epilogue
+      const float* lambda; long lambda_sb;  // fp32 [N]; EPI_SCALED: one number
+    };
+    VocabEpilogue vocab;                  // EPI_VOCAB_...
+  };
   const void* lambda_mn;              // storage type [M,N] (row stride ldc, batch stride aux_sb): EPI_RESID per element
   int c_is_f32;         // C stored as fp32 regardless of the storage type
-  VocabEpilogue vocab;  // EPI_VOCAB_...
-  const float* scale;   // bf16 kernels, EPI_STORE in one share, A K-contiguous and B not: C = *scale acc; or NULL
 };
 
 // storage type: 0 = fp32, 1 = bf16
