@@ -220,12 +220,22 @@ __device__ __forceinline__ void epilogue_sums(const GemmArgs& g, const TileCoord
       for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
     top = fmaxf(top, __shfl_xor(top, 32));
     const float shift = top == -INFINITY ? 0.f : top * alpha;      // (alpha > 0)
-    const float left_out = top == -INFINITY ? 0.f : fmaf(top, alpha, -shift);
+    // (where the product's rounding is no longer small, as of rows masked by the lowest value, or the product passes the largest number)
+    const bool far = !(fabsf(shift) < 0x1p24f);
+    const float left_out = top == -INFINITY || far ? 0.f : fmaf(top, alpha, -shift);
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (__any(far)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum[i] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], alpha, -shift));
+        for (int r = 0; r < 16; ++r)
+          sum[i] += __builtin_amdgcn_exp2f(far ? (acc[i][j][r] - top) * alpha : fmaf(acc[i][j][r], alpha, -shift));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[i] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], alpha, -shift));
+    }
     float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     l += __shfl_xor(l, 32);
     l *= __builtin_amdgcn_exp2f(-left_out);

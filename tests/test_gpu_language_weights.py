@@ -54,3 +54,28 @@ def test_entries_masked_by_a_weight(n, vocab, width, dtype, padding):
     assert bool((c.dx[~on] == 0).all())
     R.assert_within(c.dweight[left], *want["dweight"], "dweight")
     assert bool((c.dweight[masked] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,width", SIZES)
+@pytest.mark.parametrize("padding", [0.0, 0.3])
+def test_entries_masked_by_the_lowest_value(n, vocab, width, dtype, padding):
+    """The same with the type's lowest value, whole blocks of 128 entries among the masked: logits from -1.7e38 to -infinity, finite ones beyond the largest
+    number once they are taken to base 2.  Zero times such a weight is zero: dx too is as without the entries."""
+    x, w = normal((n, width), TYPES[dtype], 1), normal((vocab, width), TYPES[dtype], 2, 2.0 / math.sqrt(width))
+    x[:, 3] = x[:, 3].abs() + 0.5
+    masked = torch.zeros(vocab, dtype=torch.bool, device="cuda")
+    masked[120:520] = True
+    masked[vocab - 3:] = True
+    w[masked, 3] = torch.finfo(TYPES[dtype]).min
+    left = (~masked).nonzero()[:, 0]
+    t = some_tokens(n, left.numel(), 3, padding=padding)
+    on = (t >= 0) & (t < left.numel())
+    targets = torch.where(on, left[t.long().clamp(0, left.numel() - 1)], torch.full_like(left[:1], -1)).int()
+    c = B.make_cross_entropy(x, w, targets)
+    B.hbp_loss_cross_entropy(c)
+    want = R.cross_entropy(x, w[left].contiguous(), t)
+    for name in ("loss", "row_loss", "dx"):
+        R.assert_within(getattr(c, name), *want[name], name)
+    R.assert_within(c.dweight[left], *want["dweight"], "dweight")
+    assert bool((c.dweight[masked] == 0).all())
