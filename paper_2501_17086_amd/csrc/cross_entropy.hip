@@ -4,10 +4,10 @@
 // rows x vocabulary is kept.  Three forms, by sizes alone:
 //   many tiles  (bf16) the logits meet no memory: the 256 x 256 kernel's epilogues take sums of 128 rows of the vocabulary from its
 //               accumulators, and once more, when a row's sum is known, dS.  Four products of 2 rows x vocabulary x width where keeping the
-//               logits would leave three; what bounds it are the matrix cores, busy for 70 to 82 % of the four products' cycles: 16384 rows against
-//               131072 x 2048, kernel times on a card where a large product of the library reaches 1351 TFLOP/s, 6.84 ms for the sums, 7.41 dS, 6.34 dW,
-//               6.94 dx, 27.8 in all, 1280 TFLOP/s over the four (cards differ by some 6 %).  With 256 channels a tile's exponentials and stores take
-//               as long as its products: 32768 rows against 16384 x 256 274, 354, 243, 232 us, matrix cores busy for 50, 36, 54 and 57 %.
+//               logits would leave three; what bounds it are the matrix cores, busy for 70 to 80 % of the four products' cycles: 16384 rows against
+//               131072 x 2048, kernel times on a card where a large product of the library reaches 1373 TFLOP/s, 6.79 ms for the sums, 7.14 dS, 6.40 dW,
+//               6.65 dx, 27.2 in all, 1300 TFLOP/s over the four (cards differ by some 6 %).  With 256 channels a tile's exponentials and stores take
+//               as long as its products: 32768 rows against 16384 x 256 275, 347, 243, 235 us, matrix cores busy for 50, 37, 54 and 52 %.
 //   pieces      logits in memory in fp32, at most 1 GB at a time; with one piece they are formed once.  fp32, and few rows.
 //   small       the same with logits and sums in one launch (small_logits_kernel): launches bound it, 2 to 10 us each.
 //
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(NTHR) void small_logits_kernel(CeArgs a, int keep) 
 // keeps the diagonal.  Same instruction, same order along the channels: bit by bit the logits that the 256 x 256 kernel's epilogues see, so that where a
 // target holds next to all of a row's mass its logit cancels against the sum's.  (A sum in another order, as a plain dot product is, leaves a
 // rounding of the logit's size in the loss and in the target's coefficient, however small these are: fp32 dx, where the same was so, of 30000 rows against
-// 1000 x 1000 3.7e-6 instead of 9.3e-7 off in relative L2.)  What bounds it is the wait for each row's channels in turn: 16384 rows of 2048 48 us, 32768 of 256 8.
+// 1000 x 1000 3.7e-6 instead of 9.3e-7 off in relative L2.)  What bounds it is the wait for each row's channels in turn: 16384 rows of 2048 39 us, 32768 of 256 8.
 __global__ __launch_bounds__(NTHR) void target_kernel(CeArgs a) {
   constexpr int STEP = Frag<bf16_t>::STEP, U = 4;
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;

@@ -200,8 +200,8 @@ enum FastEpi {
 };
 
 // What a vocabulary's logits are formed for (cross_entropy.hip); rows are the vocabulary's, columns those of x.  Measured, M x N x K, kernel times on a
-// card where a large product of the library reaches 1351 TFLOP/s: sums 131072 x 16384 x 2048 6.84 ms (1290 TFLOP/s), 49920 x 8192 x 1024 0.70 (1190),
-// 16384 x 32768 x 256 0.274 (1000); their gradient 7.41, 0.75, 0.354.  At 256 channels the epilogue's 128 exponentials a lane take as long as the
+// card where a large product of the library reaches 1373 TFLOP/s: sums 131072 x 16384 x 2048 6.79 ms (1295 TFLOP/s), 49920 x 8192 x 1024 0.69 (1210),
+// 16384 x 32768 x 256 0.275 (1000); their gradient 7.14, 0.73, 0.347.  At 256 channels the epilogue's 128 exponentials a lane take as long as the
 // products; with plain stores in place of non-temporal ones the gradient's 1 GB costs a tenth more.
 //
 // The largest of a wavefront's 128 rows and the sum of 2^(alpha (acc - it)), for each of its 64 columns.  The products of this form are issued with
